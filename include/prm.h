@@ -445,6 +445,81 @@ PRM_API int prm_partition_matrices(const int64_t* shapes, int n_mats, int world,
  */
 PRM_API double prm_shape_scale(int mode, int64_t rows, int64_t cols);
 
+/*
+ * 8-bit operators around a linear layer whose weight the optimizer owns.  (The paper has no
+ * counterpart: they are offered to users who train or serve the layers in 8 bits.)
+ *
+ * A quantised matrix is a row-major matrix of 8-bit codes plus one fp32 scale per row or per
+ * column; it stands for code * scale.  Formats: PRM_Q8_INT8 (codes -127..127) and PRM_Q8_E4M3
+ * (8-bit floats, +-448).  The largest magnitude T that shares a scale maps to the limit (127 or
+ * 448): code = round-to-nearest-even(value * (limit * (1 / T))), scale = T / limit, each step in
+ * fp32.  T below 2^-100 counts as zero (codes and scale 0); a row (column) that holds an infinity or
+ * a NaN gets the scale NaN and zero codes, and no other row is touched by it.
+ *
+ * Weights are stored in x out (rows x cols as everywhere in this library: y = x W).  A training
+ * step of a layer is then, with x8/sx from prm_rmsnorm_q8 and w8/sw by columns from
+ * prm_quantize_q8,
+ *     y      = prm_matmul_q8(x8, sx, w8, sw)
+ *     g_r, g_c = prm_quantize_q8(grad_y; by rows with fold_cols = sw, by columns with fold_rows = sx)
+ *     grad_x = prm_matmul_q8(g_r, its scale, w8 transposed, none)
+ *     grad_W = prm_matmul_q8(x8 transposed, none, g_c, its scale)
+ * The folds carry the scales that run along the sums: a product can take factors out of its sums
+ * per row of the left and per column of the right operand only.  grad_W is what prm_step reads.
+ *
+ * Conventions: ld_* are row strides in elements; strides of inputs may be any number >= 0 (0
+ * repeats one row), those of outputs at least cols.  io_fp32, weight_fp32, out_fp32: 0 = bf16,
+ * 1 = fp32.  Pointers need the alignment of their element; 16-byte aligned pointers, row strides
+ * and column counts that are multiples of 8 elements take the vectorised kernels (prm_matmul_q8
+ * needs more, below).  Sums, statistics and scales are fp32 (int8 sums: exact integers).  The calls
+ * only enqueue work on cuda_stream, allocate nothing, and can be captured into a graph; sizes of
+ * zero are allowed where stated.  Outputs must not overlap inputs.
+ *
+ * prm_rmsnorm_q8   per row: h = x + residual, rounded to the stream's type and stored (residual
+ *   NULL: h = x, nothing stored, h_out ignored); t = h * weight; codes of t by row;
+ *   scale = T / limit / sqrt(mean(h^2) + eps).  q_out * scale_out is the norm's output.  rows may
+ *   be 0.
+ * prm_rmsnorm_q8_backward   the norm's gradient, the rounding to 8 bits taken as the identity.
+ *   With s = 1 / sqrt(mean(h^2) + eps) and g = grad_y * weight:
+ *     grad_x = s g - h s^3 mean(g h) + grad_h   (the gradient of x and of residual alike;
+ *                                                grad_h, what reaches h from elsewhere, may be NULL)
+ *     grad_weight[j] = sum over rows of grad_y h s   (in the weight's type, added in a fixed order)
+ *   scratch: device, 16-byte aligned, prm_rmsnorm_q8_scratch_bytes(rows, cols) bytes.  With rows = 0
+ *   grad_weight is set to zero.
+ * prm_quantize_q8   codes of a matrix by rows (of x * fold_cols, scale_rows[rows]), by columns (of
+ *   x * fold_rows, scale_cols[cols]), or both from one call; q_rows or q_cols may be NULL, the folds
+ *   (fp32) too.  scratch (by columns only): device, 16-byte aligned,
+ *   prm_quantize_q8_scratch_bytes(rows, cols) bytes.  With rows = 0 scale_cols is set to zero.
+ * prm_matmul_q8   out[i,j] = scale_a[i] * scale_b[j] * sum_l a[i,l] b[l,j], i < m, l < k, j < n,
+ *   on tensor cores; int8 sums exactly in integers, e4m3 in fp32; one rounding at the store.
+ *   a_transposed = 0: a is stored m x k; 1: k x m.  b_transposed = 0: b is stored k x n; 1: n x k.
+ *   Either scale may be NULL (1).  a and b 16-byte aligned with row strides that are multiples of 16
+ *   (else PRM_ERR_ALIGN); m, k, n are free; m or n = 0 does nothing, k = 0 writes zeros.  int8: k at
+ *   most 1047552 (PRM_ERR_SHAPE).
+ * prm_q8_status    as prm_status, for the waits inside prm_matmul_q8 on the current device
+ *   (synchronises it): PRM_OK, or PRM_ERR_DEVICE_TIMEOUT once after a wait that ran out.
+ */
+#define PRM_Q8_INT8  0
+#define PRM_Q8_E4M3  1
+PRM_API int prm_rmsnorm_q8(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual,
+                           const void* weight, int64_t rows, int64_t cols, int io_fp32, int weight_fp32,
+                           float eps, int format, void* h_out, int64_t ld_h, void* q_out, int64_t ld_q,
+                           float* scale_out, void* cuda_stream);
+PRM_API size_t prm_rmsnorm_q8_scratch_bytes(int64_t rows, int64_t cols);
+PRM_API int prm_rmsnorm_q8_backward(const void* grad_y, int64_t ld_grad_y, const void* h, int64_t ld_h,
+                                    const void* weight, const void* grad_h, int64_t ld_grad_h, int64_t rows,
+                                    int64_t cols, int io_fp32, int weight_fp32, float eps, void* grad_x,
+                                    int64_t ld_grad_x, void* grad_weight, void* scratch, size_t scratch_bytes,
+                                    void* cuda_stream);
+PRM_API size_t prm_quantize_q8_scratch_bytes(int64_t rows, int64_t cols);
+PRM_API int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_t cols, int io_fp32, int format,
+                            const float* fold_rows, const float* fold_cols, void* q_rows, int64_t ld_q_rows,
+                            float* scale_rows, void* q_cols, int64_t ld_q_cols, float* scale_cols, void* scratch,
+                            size_t scratch_bytes, void* cuda_stream);
+PRM_API int prm_matmul_q8(const void* a, int64_t ld_a, int a_transposed, const float* scale_a, const void* b,
+                          int64_t ld_b, int b_transposed, const float* scale_b, int64_t m, int64_t k, int64_t n,
+                          int format, void* out, int64_t ld_out, int out_fp32, void* cuda_stream);
+PRM_API int prm_q8_status(void);
+
 /* Frees host resources.  Device memory belongs to the caller. */
 PRM_API int prm_destroy(prm_ctx* ctx);
 

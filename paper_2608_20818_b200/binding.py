@@ -8,6 +8,7 @@ there is no fallback path.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int64, c_size_t, c_void_p
@@ -42,6 +43,9 @@ PRM_OPT_TALL_KERNEL = 13
 PRM_OPT_NS_SPLIT_INPUT = 14
 PRM_OPT_WIDE_KERNEL = 15
 
+PRM_Q8_INT8 = 0
+PRM_Q8_E4M3 = 1
+
 EXPORTS = (
     "prm_create", "prm_set_option", "prm_workspace_bytes", "prm_set_workspace", "prm_step",
     "prm_step_h2d", "prm_plan", "prm_status", "prm_last_error", "prm_launch_count", "prm_destroy",
@@ -49,6 +53,8 @@ EXPORTS = (
     "prm_tall_shard_scratch_bytes", "prm_tall_shard_stats", "prm_tall_shard_apply", "prm_group_info",
     "prm_shard_rows", "prm_bucket_plan", "prm_shard_momentum_pack", "prm_refresh_gathered", "prm_refresh_segments", "prm_pipeline_model",
     "prm_partition_matrices", "prm_shape_scale",
+    "prm_rmsnorm_q8", "prm_rmsnorm_q8_scratch_bytes", "prm_rmsnorm_q8_backward",
+    "prm_quantize_q8", "prm_quantize_q8_scratch_bytes", "prm_matmul_q8", "prm_q8_status",
 )
 PRM_PROF_ROW_WIDE, PRM_PROF_ROW_TALL, PRM_PROF_PREPASS, PRM_PROF_GRAM = 0, 1, 2, 3
 PRM_PROF_POLY, PRM_PROF_UPDATE, PRM_PROF_UPDATE_FINAL, PRM_PROF_GRAMSPACE, PRM_PROF_COUNT = 4, 5, 6, 7, 8
@@ -141,6 +147,25 @@ def lib():
     L.prm_partition_matrices.restype = c_int
     L.prm_shape_scale.argtypes = [c_int, c_int64, c_int64]
     L.prm_shape_scale.restype = c_double
+    L.prm_rmsnorm_q8.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int, c_int,
+                                 c_float, c_int, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]
+    L.prm_rmsnorm_q8.restype = c_int
+    L.prm_rmsnorm_q8_scratch_bytes.argtypes = [c_int64, c_int64]
+    L.prm_rmsnorm_q8_scratch_bytes.restype = c_size_t
+    L.prm_rmsnorm_q8_backward.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_int64,
+                                          c_int64, c_int, c_int, c_float, c_void_p, c_int64, c_void_p, c_void_p,
+                                          c_size_t, c_void_p]
+    L.prm_rmsnorm_q8_backward.restype = c_int
+    L.prm_quantize_q8_scratch_bytes.argtypes = [c_int64, c_int64]
+    L.prm_quantize_q8_scratch_bytes.restype = c_size_t
+    L.prm_quantize_q8.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int, c_int, c_void_p, c_void_p, c_void_p,
+                                  c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.prm_quantize_q8.restype = c_int
+    L.prm_matmul_q8.argtypes = [c_void_p, c_int64, c_int, c_void_p, c_void_p, c_int64, c_int, c_void_p, c_int64,
+                                c_int64, c_int64, c_int, c_void_p, c_int64, c_int, c_void_p]
+    L.prm_matmul_q8.restype = c_int
+    L.prm_q8_status.argtypes = []
+    L.prm_q8_status.restype = c_int
     _lib_handle = L
     return L
 
@@ -376,6 +401,246 @@ def prm_shape_scale(mode, rows, cols):
     if v == 0.0:
         raise PrmError(PRM_ERR_ARG, "prm_shape_scale: bad argument")
     return v
+
+
+_Q8_DTYPE = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+_Q8_FORMAT = {"int8": PRM_Q8_INT8, "e4m3": PRM_Q8_E4M3}
+_Q8_CODE = {torch.int8: PRM_Q8_INT8, torch.float8_e4m3fn: PRM_Q8_E4M3}
+_IO_FP32 = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _on_stream(stream, inputs, call):
+    """Runs call() with `stream` current, so that what it allocates belongs to that stream, and
+    keeps the inputs' memory from being handed out again before the stream is done with it."""
+    with torch.cuda.stream(stream):
+        out = call()
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    return out
+
+
+def _raw_stream(device):
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _stream_matrix(t, name, dtype=None, shape=None):
+    """A 2-D bf16 or fp32 CUDA tensor whose rows are contiguous (copied if they are not)."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D matrix")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must sit on a CUDA device")
+    if t.dtype not in _IO_FP32:
+        raise TypeError(f"{name} must be bfloat16 or float32")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} like the matrix it goes with")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}")
+    return t if t.stride(1) == 1 or t.shape[1] == 1 else t.contiguous()
+
+
+def _vector(t, name, n, device, dtypes=(torch.float32,)):
+    """A contiguous vector of n elements on `device` (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {dtypes}")
+    if t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name} must be a vector of {n} elements")
+    if t.device != device:
+        raise ValueError(f"{name} must sit on {device}")
+    return t if n <= 1 or t.stride(0) == 1 else t.contiguous()
+
+
+_NO_GUARD = contextlib.nullcontext()
+
+
+def _device_guard(device):
+    """Makes `device` current for a call, where it is not already."""
+    return _NO_GUARD if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _codes(rows, cols, dtype, device):
+    """An uninitialised matrix of 8-bit codes whose rows start a multiple of 16 bytes apart."""
+    return torch.empty_strided((rows, cols), ((cols + 15) // 16 * 16, 1), dtype=dtype, device=device)
+
+
+def _q8_check(code, what):
+    if code != PRM_OK:
+        raise PrmError(code, f"{what} failed (see include/prm.h for its limits)")
+
+
+def prm_rmsnorm_q8(x, weight, eps, residual=None, format="int8", stream=None):
+    """Root-mean-square norm of x (+ residual) in 8 bits: (codes, scale per row, h).
+
+    x, residual: rows x cols, bf16 or fp32; weight: cols, bf16 or fp32; format "int8" or "e4m3".
+    h = x + residual in x's type is what the norm is taken of and what the stream carries on; it is
+    None without a residual (h = x).  codes * scale[:, None] is the norm's output."""
+    if stream is not None:
+        return _on_stream(stream, (x, weight, residual),
+                          lambda: prm_rmsnorm_q8(x, weight, eps, residual, format))
+    fmt = _Q8_FORMAT.get(format)
+    if fmt is None:
+        raise ValueError('format must be "int8" or "e4m3"')
+    x = _stream_matrix(x, "x")
+    rows, cols = x.shape
+    device = x.device
+    weight = _vector(weight, "weight", cols, device, (torch.bfloat16, torch.float32))
+    h, ld_r, ld_h = None, 0, 0
+    if residual is not None:
+        residual = _stream_matrix(residual, "residual", x.dtype, x.shape)
+        if residual.device != device:
+            raise ValueError(f"residual must sit on {device}")
+        h = torch.empty((rows, cols), dtype=x.dtype, device=device)
+        ld_r, ld_h = residual.stride(0), cols
+    q = _codes(rows, cols, _Q8_DTYPE[format], device)
+    scale = torch.empty(rows, dtype=torch.float32, device=device)
+    with _device_guard(device):
+        code = lib().prm_rmsnorm_q8(x.data_ptr(), x.stride(0), _ptr(residual), ld_r, weight.data_ptr(), rows, cols,
+                                    _IO_FP32[x.dtype], _IO_FP32[weight.dtype], eps, fmt, _ptr(h), ld_h, q.data_ptr(),
+                                    q.stride(0), scale.data_ptr(), _raw_stream(device))
+    _q8_check(code, "prm_rmsnorm_q8")
+    return q, scale, h
+
+
+def prm_rmsnorm_q8_backward(grad_y, h, weight, eps, grad_h=None, stream=None):
+    """Gradient of the norm at h (the sum that prm_rmsnorm_q8 returned, or its x without a residual):
+    (grad_x, grad_weight).  grad_x is the gradient of x and of the residual alike; grad_h, if given,
+    is what reaches h along the residual stream and is added to it."""
+    if stream is not None:
+        return _on_stream(stream, (grad_y, h, weight, grad_h),
+                          lambda: prm_rmsnorm_q8_backward(grad_y, h, weight, eps, grad_h))
+    h = _stream_matrix(h, "h")
+    grad_y = _stream_matrix(grad_y, "grad_y", h.dtype, h.shape)
+    rows, cols = h.shape
+    device = h.device
+    weight = _vector(weight, "weight", cols, device, (torch.bfloat16, torch.float32))
+    ld_gh = 0
+    if grad_h is not None:
+        grad_h = _stream_matrix(grad_h, "grad_h", h.dtype, h.shape)
+        ld_gh = grad_h.stride(0)
+    if grad_y.device != device or (grad_h is not None and grad_h.device != device):
+        raise ValueError(f"the gradients must sit on {device}")
+    L = lib()
+    nbytes = L.prm_rmsnorm_q8_scratch_bytes(rows, cols)
+    grad_x = torch.empty((rows, cols), dtype=h.dtype, device=device)
+    grad_w = torch.empty(cols, dtype=weight.dtype, device=device)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with _device_guard(device):
+        code = L.prm_rmsnorm_q8_backward(grad_y.data_ptr(), grad_y.stride(0), h.data_ptr(), h.stride(0),
+                                         weight.data_ptr(), _ptr(grad_h), ld_gh, rows, cols, _IO_FP32[h.dtype],
+                                         _IO_FP32[weight.dtype], eps, grad_x.data_ptr(), cols, grad_w.data_ptr(),
+                                         scratch.data_ptr(), nbytes, _raw_stream(device))
+    _q8_check(code, "prm_rmsnorm_q8_backward")
+    return grad_x, grad_w
+
+
+def prm_quantize_q8(x, *, by_rows=True, by_cols=False, fold_rows=None, fold_cols=None, format="int8", stream=None):
+    """8-bit codes of a bf16 or fp32 matrix: (codes by row, scale per row, codes by column, scale per
+    column), None for what was not asked for.  By row it quantises x * fold_cols, by column
+    x * fold_rows[:, None] (fp32 vectors, optional)."""
+    if stream is not None:
+        return _on_stream(stream, (x, fold_rows, fold_cols),
+                          lambda: prm_quantize_q8(x, by_rows=by_rows, by_cols=by_cols, fold_rows=fold_rows,
+                                                  fold_cols=fold_cols, format=format))
+    fmt = _Q8_FORMAT.get(format)
+    if fmt is None:
+        raise ValueError('format must be "int8" or "e4m3"')
+    if not by_rows and not by_cols:
+        raise ValueError("ask for codes by rows, by columns, or both")
+    x = _stream_matrix(x, "x")
+    rows, cols = x.shape
+    device = x.device
+    fold_rows = _vector(fold_rows, "fold_rows", rows, device)
+    fold_cols = _vector(fold_cols, "fold_cols", cols, device)
+    L = lib()
+    qr = sr = qc = sc = scratch = None
+    ld_r = ld_c = nbytes = 0
+    if by_rows:
+        qr = _codes(rows, cols, _Q8_DTYPE[format], device)
+        sr = torch.empty(rows, dtype=torch.float32, device=device)
+        ld_r = qr.stride(0)
+    if by_cols:
+        qc = _codes(rows, cols, _Q8_DTYPE[format], device)
+        sc = torch.empty(cols, dtype=torch.float32, device=device)
+        ld_c = qc.stride(0)
+        nbytes = L.prm_quantize_q8_scratch_bytes(rows, cols)
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if rows == 0:                       # nothing to point at: columns without an element have the scale 0
+        return qr, sr, qc, None if sc is None else sc.zero_()
+    with _device_guard(device):
+        code = L.prm_quantize_q8(x.data_ptr(), x.stride(0), rows, cols, _IO_FP32[x.dtype], fmt, _ptr(fold_rows),
+                                 _ptr(fold_cols), _ptr(qr), ld_r, _ptr(sr), _ptr(qc), ld_c, _ptr(sc), _ptr(scratch),
+                                 nbytes, _raw_stream(device))
+    _q8_check(code, "prm_quantize_q8")
+    return qr, sr, qc, sc
+
+
+def _q8_operand(t):
+    """(matrix, its row stride, 1 if it is stored the other way round) as prm_matmul_q8 reads it;
+    a matrix that lies in neither way, or unaligned, is copied."""
+    r, c = t.shape
+    s0, s1 = t.stride()
+    if t.data_ptr() % 16 == 0:
+        if s1 == 1 or c == 1:
+            ld = s0 if r > 1 else (c + 15) // 16 * 16
+            if ld % 16 == 0 and ld >= c:
+                return t, ld, 0
+        if s0 == 1 or r == 1:
+            ld = s1 if c > 1 else (r + 15) // 16 * 16
+            if ld % 16 == 0 and ld >= r:
+                return t, ld, 1
+    laid = _codes(r, c, t.dtype, t.device)
+    laid.copy_(t)
+    return laid, (c + 15) // 16 * 16, 0
+
+
+def prm_matmul_q8(a, scale_a, b, scale_b, out_dtype=torch.bfloat16, out=None, stream=None):
+    """(a @ b) * scale_a[:, None] * scale_b for 8-bit codes a (m x k) and b (k x n), both int8 or both
+    float8_e4m3fn; a scale may be None.  Either operand may be a transposed view (`w.t()`).  Returns
+    out: m x n, bf16 or fp32, a new matrix unless one with contiguous rows is given."""
+    if stream is not None:
+        return _on_stream(stream, (a, scale_a, b, scale_b, out),
+                          lambda: prm_matmul_q8(a, scale_a, b, scale_b, out_dtype, out))
+    if a.dim() != 2 or b.dim() != 2 or a.shape[1] != b.shape[0]:
+        raise ValueError("a must be m x k and b k x n")
+    fmt = _Q8_CODE.get(a.dtype)
+    if fmt is None or b.dtype != a.dtype:
+        raise TypeError("a and b must both be int8 or both float8_e4m3fn")
+    device = a.device
+    if not a.is_cuda or b.device != device:
+        raise ValueError("a and b must sit on the same CUDA device")
+    m, k = a.shape
+    n = b.shape[1]
+    scale_a = _vector(scale_a, "scale_a", m, device)
+    scale_b = _vector(scale_b, "scale_b", n, device)
+    if out is None:
+        if out_dtype not in _IO_FP32:
+            raise TypeError("out_dtype must be bfloat16 or float32")
+        out = torch.empty((m, n), dtype=out_dtype, device=device)
+    else:
+        if out.dtype not in _IO_FP32:
+            raise TypeError("out must be bfloat16 or float32")
+        if out.shape != (m, n) or out.device != device:
+            raise ValueError(f"out must be a {m} x {n} matrix on {device}")
+        if n > 1 and out.stride(1) != 1 or m > 1 and out.stride(0) < n:
+            raise ValueError("the rows of out must be contiguous and must not overlap")
+    a, ld_a, a_t = _q8_operand(a)
+    b, ld_b, b_t = _q8_operand(b)
+    with _device_guard(device):
+        code = lib().prm_matmul_q8(a.data_ptr(), ld_a, a_t, _ptr(scale_a), b.data_ptr(), ld_b, b_t, _ptr(scale_b),
+                                   m, k, n, fmt, out.data_ptr(), out.stride(0) if m > 1 else n, _IO_FP32[out.dtype],
+                                   _raw_stream(device))
+    _q8_check(code, "prm_matmul_q8")
+    return out
+
+
+def prm_q8_status():
+    return int(lib().prm_q8_status())
 
 
 def prm_destroy(h):

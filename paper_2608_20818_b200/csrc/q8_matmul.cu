@@ -1,0 +1,363 @@
+// Product of 8-bit matrices with a scale per row of the left and per column of the right operand:
+//
+//   out[m, n] = scale_a[m] * scale_b[n] * sum_k a[m, k] * b[k, n]
+//
+// int8 codes are summed exactly in 32-bit integers, e4m3 codes in fp32.  Either operand may be
+// stored either way round: a as rows of k or rows of m, b as rows of n or rows of k.  A layer's
+// three products are then y = x8 W8, grad_x = g8 W8^T and grad_W = x8^T g8 on matrices as they lie.
+//
+// One CTA computes a tile of 128 columns n (the matrix instruction's M, so that a tensor-memory
+// lane is an output column and a warp stores 32 neighbouring columns) by up to 256 rows m (its N):
+// one token costs the instruction no more columns than it has to.  The k loop of a tile may be
+// split over the CTAs of a cluster, which then add their parts through distributed shared memory:
+// with few tiles this is what puts every SM on the weight's bytes.
+//
+//   warp 0      TMA producer: boxes of 128 bytes x 128 rows, 128-byte swizzle, no multicast
+//   warp 1      tcgen05.mma issuer, owner of the tensor memory
+//   warps 2..5  epilogue
+//
+// Every barrier wait is bounded; one that runs out sets the status word that prm_q8_status reads,
+// the CTA drains its copies and leaves.
+#include <string.h>
+
+#include "q8.cuh"
+#include "tcgen05.cuh"
+
+namespace prm {
+namespace {
+
+__device__ int g_q8_status;
+
+constexpr int kTileN = 128;            // output columns per CTA (lanes of the accumulator)
+constexpr int kBlockK = 128;           // k per stage: one 128-byte swizzled row
+constexpr int kMaxStages = 10;
+constexpr int kThreads = 192;
+constexpr uint32_t kBytesP = kTileN * kBlockK;
+constexpr int kMaxSplit = 8;           // portable cluster size
+// 32-bit sums of products of int8 hold for this many k-blocks (2^14 * 128 * 1023 < 2^31); longer
+// sums are split over the cluster, whose parts are added in 64 bits.
+constexpr int kMaxBlocksInt8 = 1023;
+
+struct MatmulArgs {
+  const float* scale_a;   // [m] or null
+  const float* scale_b;   // [n] or null
+  void* out;
+  int64_t ld_out;
+  int m, n;
+  int kblocks;            // ceil(k / 128)
+  int tile_m;             // rows m per tile: 16, 32, 64, 128 or 256
+  int n_tiles;
+  int split;              // CTAs per tile (cluster size)
+  int stages;
+  uint32_t stage_bytes;
+  int out_fp32;
+};
+
+// Dynamic shared memory: stages (P tile, Q tile), reused for the split's partial sums.
+template <bool INT8, bool P_MN, bool Q_MN>
+__global__ void __launch_bounds__(kThreads, 1)
+matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
+                 const MatmulArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], done;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  volatile int* abort_flag = &abort_word;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = a.split > 1 ? (int)cluster_ctarank() : 0;
+  const int tile = blockIdx.x / a.split;
+  const int n0 = (tile % a.n_tiles) * kTileN, m0 = (tile / a.n_tiles) * a.tile_m;
+  const int kb0 = (int)((int64_t)a.kblocks * rank / a.split), kb1 = (int)((int64_t)a.kblocks * (rank + 1) / a.split);
+  const uint32_t tmem_cols = a.tile_m < 32 ? 32u : (uint32_t)a.tile_m;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < a.stages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    mbar_init(&done, 1);
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)),
+                 "r"(tmem_cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tcgen05_before_sync();
+  __syncthreads();
+  tcgen05_after_sync();
+  const uint32_t tmem = tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int it = 0;
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        const int s = it % a.stages;
+        if (!mbar_wait(&empty[s], ((it / a.stages) & 1) ^ 1, abort_flag, &g_q8_status)) break;
+        uint8_t* sp = smem + (size_t)s * a.stage_bytes;
+        uint8_t* sq = sp + kBytesP;
+        mbar_expect_tx(&full[s], a.stage_bytes);
+        const int k0 = kb * kBlockK;
+        if (P_MN) tma_load_2d(sp, &map_p, &full[s], n0, k0);
+        else tma_load_2d(sp, &map_p, &full[s], k0, n0);
+        if (Q_MN) {
+          tma_load_2d(sq, &map_q, &full[s], m0, k0);
+          if (a.tile_m > 128) tma_load_2d(sq + 128 * kBlockK, &map_q, &full[s], m0 + 128, k0);
+        } else {
+          tma_load_2d(sq, &map_q, &full[s], k0, m0);
+        }
+      }
+      if (*abort_flag) {                 // copies in flight must land before the CTA leaves
+        for (int j = it > a.stages ? it - a.stages : 0; j < it; ++j) {
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(&full[j % a.stages], (j / a.stages) & 1) && global_ns() - t0 < 1000000ull) {
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = idesc_8bit(INT8, kTileN, a.tile_m, P_MN, Q_MN);
+      constexpr uint32_t kStepP = P_MN ? 256 : 2, kStepQ = Q_MN ? 256 : 2;    // 32 k, in units of 16 bytes
+      bool ok = true;
+      int it = 0;
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        const int s = it % a.stages;
+        if (!mbar_wait(&full[s], (it / a.stages) & 1, abort_flag, &g_q8_status)) { ok = false; break; }
+        tcgen05_after_sync();
+        const uint32_t sp = smem_u32(smem + (size_t)s * a.stage_bytes), sq = sp + kBytesP;
+        const uint64_t dp = P_MN ? desc_mn_major(sp, 128 * kBlockK) : desc_k_major(sp);
+        const uint64_t dq = Q_MN ? desc_mn_major(sq, 128 * kBlockK) : desc_k_major(sq);
+#pragma unroll
+        for (int j = 0; j < kBlockK / 32; ++j)
+          umma_8bit_1cta<INT8>(tmem, dp + kStepP * j, dq + kStepQ * j, idesc, (it | j) != 0);
+        umma_commit_1cta(&empty[s]);
+      }
+      if (ok) umma_commit_1cta(&done);
+    }
+  }
+  bool ok = true;
+  if (warp >= 2) {
+    ok = mbar_wait(&done, 0, abort_flag, &g_q8_status);
+    ok = __all_sync(0xffffffffu, ok);
+    tcgen05_after_sync();
+  }
+  const int quad = warp & 3;
+  const int col = quad * 32 + lane;            // this thread's output column in the tile
+  const int n = n0 + col;
+  const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+  const int m_here = min(a.tile_m, a.m - m0);
+  const float sb = warp >= 2 && a.scale_b && n < a.n ? __ldg(a.scale_b + n) : 1.f;
+  auto put = [&](int t, float v) {
+    const int m = m0 + t;
+    if (a.scale_a) v *= __ldg(a.scale_a + m);
+    v *= sb;
+    const int64_t at = (int64_t)m * a.ld_out + n;
+    if (a.out_fp32) reinterpret_cast<float*>(a.out)[at] = v;
+    else reinterpret_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+  };
+  if (a.split == 1) {
+    if (warp >= 2 && ok) {
+      for (int t0 = 0; t0 < m_here; t0 += 16) {
+        uint32_t r[16];
+        tmem_ld16(trow + t0, r);
+        tmem_wait_ld();
+        if (n < a.n) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (t0 + j < m_here) put(t0 + j, INT8 ? (float)(int)r[j] : __uint_as_float(r[j]));
+        }
+      }
+    }
+  } else {
+    uint32_t* part = reinterpret_cast<uint32_t*>(smem);       // [tile_m][128], all copies have been consumed
+    if (warp >= 2 && ok) {
+      for (int t0 = 0; t0 < m_here; t0 += 16) {
+        uint32_t r[16];
+        tmem_ld16(trow + t0, r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) part[(t0 + j) * kTileN + col] = r[j];
+      }
+    }
+    __syncwarp();
+    cluster_barrier();
+    if (warp >= 2 && ok && n < a.n) {
+      const uint32_t base = smem_u32(part) + (uint32_t)col * 4;
+      for (int t = rank; t < m_here; t += a.split) {
+        if (INT8) {
+          long long sum = 0;
+          for (int q = 0; q < a.split; ++q) sum += (int)ld_cluster_u32(cluster_map(base + t * kTileN * 4, q));
+          put(t, (float)sum);
+        } else {
+          float sum = 0.f;
+          for (int q = 0; q < a.split; ++q)
+            sum += __uint_as_float(ld_cluster_u32(cluster_map(base + t * kTileN * 4, q)));
+          put(t, sum);
+        }
+      }
+    }
+    __syncwarp();
+    cluster_barrier();                   // nobody leaves while its part is being read
+  }
+  tcgen05_before_sync();
+  __syncwarp();
+  __syncthreads();
+  if (warp == 1) {
+    tcgen05_after_sync();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols) : "memory");
+  }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = []() -> EncodeTiledFn {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult res;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &res) != cudaSuccess ||
+        res != cudaDriverEntryPointSuccess)
+      return nullptr;
+    return (EncodeTiledFn)p;
+  }();
+  return fn;
+}
+
+// Map over rows x cols bytes (row-major, ld bytes apart), boxes of box_rows x 128 bytes; what lies
+// outside reads as zero.
+bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+  EncodeTiledFn encode = encode_fn();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  const cuuint32_t step[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr size_t kSmemBudget = 200 * 1024;
+
+template <bool INT8, bool P_MN, bool Q_MN>
+int launch_matmul(const CUtensorMap& mp, const CUtensorMap& mq, const MatmulArgs& a, int ctas, size_t smem,
+                  cudaStream_t stream) {
+  static PerDeviceOnce once;
+  int dev;
+  if (once.need(&dev)) {
+    if (cudaFuncSetAttribute(matmul_q8_kernel<INT8, P_MN, Q_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)(kSmemBudget + 1024)) != cudaSuccess)
+      return PRM_ERR_CUDA;
+    once.mark(dev);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)a.split;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, matmul_q8_kernel<INT8, P_MN, Q_MN>, mp, mq, a) == cudaSuccess ? PRM_OK
+                                                                                              : PRM_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace prm
+
+using namespace prm;
+
+extern "C" int prm_matmul_q8(const void* a, int64_t ld_a, int a_transposed, const float* scale_a, const void* b,
+                             int64_t ld_b, int b_transposed, const float* scale_b, int64_t m, int64_t k, int64_t n,
+                             int format, void* out, int64_t ld_out, int out_fp32, void* cuda_stream) {
+  if (!q8_format_ok(format)) return PRM_ERR_ARG;
+  const int64_t most = 0x7fffffffLL - 1024;
+  if (m < 0 || n < 0 || k < 0 || m > most || n > most || k > most) return PRM_ERR_SHAPE;
+  if (m == 0 || n == 0) return PRM_OK;
+  if (!out) return PRM_ERR_ARG;
+  const int es = out_fp32 ? 4 : 2;
+  if (ld_out < n || ld_out > ((int64_t)1 << 40)) return PRM_ERR_SHAPE;
+  if ((uintptr_t)out % es != 0 || ((uintptr_t)scale_a | (uintptr_t)scale_b) % 4 != 0) return PRM_ERR_ALIGN;
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  if (k == 0)                             // an empty sum
+    return cudaMemset2DAsync(out, (size_t)ld_out * es, 0, (size_t)n * es, (size_t)m, stream) == cudaSuccess
+               ? PRM_OK
+               : PRM_ERR_CUDA;
+  if (!a || !b) return PRM_ERR_ARG;
+  const int64_t a_rows = a_transposed ? k : m, a_cols = a_transposed ? m : k;
+  const int64_t b_rows = b_transposed ? n : k, b_cols = b_transposed ? k : n;
+  if (ld_a < a_cols || ld_b < b_cols || ld_a >= ((int64_t)1 << 39) || ld_b >= ((int64_t)1 << 39)) return PRM_ERR_SHAPE;
+  if (!aligned16(a) || !aligned16(b) || ld_a % 16 != 0 || ld_b % 16 != 0) return PRM_ERR_ALIGN;
+
+  const bool int8 = format == PRM_Q8_INT8;
+  const bool p_mn = !b_transposed, q_mn = a_transposed != 0;
+  MatmulArgs g = {};
+  g.scale_a = scale_a;
+  g.scale_b = scale_b;
+  g.out = out;
+  g.ld_out = ld_out;
+  g.m = (int)m;
+  g.n = (int)n;
+  g.out_fp32 = out_fp32;
+  g.kblocks = (int)((k + kBlockK - 1) / kBlockK);
+  g.tile_m = 16;
+  while (g.tile_m < 256 && g.tile_m < m) g.tile_m *= 2;
+  g.n_tiles = (int)((n + kTileN - 1) / kTileN);
+  const int64_t tiles = (int64_t)g.n_tiles * ((m + g.tile_m - 1) / g.tile_m);
+  // Split k while every SM would otherwise not get a tile, but leave each CTA four k-blocks.
+  int split = 1;
+  while (split < kMaxSplit && tiles * (split + 1) <= 148 && g.kblocks >= 4 * (split + 1)) ++split;
+  if (int8) {
+    const int need = (g.kblocks + kMaxBlocksInt8 - 1) / kMaxBlocksInt8;
+    if (need > kMaxSplit) return PRM_ERR_SHAPE;
+    split = std::max(split, need);
+  }
+  g.split = split;
+  if (tiles * split > 0x7fffffffLL) return PRM_ERR_SHAPE;
+  const uint32_t q_bytes = (q_mn ? (uint32_t)std::max(g.tile_m, 128) : (uint32_t)g.tile_m) * kBlockK;
+  g.stage_bytes = kBytesP + q_bytes;
+  const int blocks_each = (g.kblocks + split - 1) / split;
+  g.stages = std::max(1, std::min<int>({kMaxStages, blocks_each, (int)(kSmemBudget / g.stage_bytes)}));
+  size_t smem = (size_t)g.stages * g.stage_bytes;
+  if (split > 1) smem = std::max(smem, (size_t)g.tile_m * kTileN * 4);
+  smem += 1024;
+
+  CUtensorMap mp, mq;
+  if (!make_map(&mp, b, b_rows, b_cols, ld_b, 128) ||
+      !make_map(&mq, a, a_rows, a_cols, ld_a, q_mn ? 128 : g.tile_m))
+    return PRM_ERR_CUDA;
+  const int ctas = (int)(tiles * split);
+#define PRM_Q8_LAUNCH(I8, PM, QM) \
+  if (int8 == I8 && p_mn == PM && q_mn == QM) return launch_matmul<I8, PM, QM>(mp, mq, g, ctas, smem, stream)
+  PRM_Q8_LAUNCH(true, true, false);
+  PRM_Q8_LAUNCH(true, false, false);
+  PRM_Q8_LAUNCH(true, true, true);
+  PRM_Q8_LAUNCH(true, false, true);
+  PRM_Q8_LAUNCH(false, true, false);
+  PRM_Q8_LAUNCH(false, false, false);
+  PRM_Q8_LAUNCH(false, true, true);
+  PRM_Q8_LAUNCH(false, false, true);
+#undef PRM_Q8_LAUNCH
+  return PRM_ERR_ARG;
+}
+
+extern "C" int prm_q8_status(void) {
+  int v = 0;
+  const int zero = 0;
+  if (cudaDeviceSynchronize() != cudaSuccess) return PRM_ERR_CUDA;
+  if (cudaMemcpyFromSymbol(&v, g_q8_status, sizeof(int)) != cudaSuccess) return PRM_ERR_CUDA;
+  if (v == 0) return PRM_OK;
+  if (cudaMemcpyToSymbol(g_q8_status, &zero, sizeof(int)) != cudaSuccess) return PRM_ERR_CUDA;
+  return PRM_ERR_DEVICE_TIMEOUT;
+}
