@@ -18,46 +18,46 @@
 //
 // Every barrier wait is bounded; one that runs out sets the status word that prm_q8_status reads,
 // the CTA drains its copies and leaves.
-#include <string.h>
-
-#include "q8.cuh"
-#include "tcgen05.cuh"
+#include "q8_matmul.cuh"
 
 namespace prm {
 namespace {
 
 __device__ int g_q8_status;
 
+// The status word's address on the current device.
+int* status_word() {
+  static int* at[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+  if (!at[dev]) {
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, g_q8_status) != cudaSuccess) return nullptr;
+    at[dev] = (int*)p;
+  }
+  return at[dev];
+}
+
 constexpr int kTileN = 128;            // output columns per CTA (lanes of the accumulator)
-constexpr int kBlockK = 128;           // k per stage: one 128-byte swizzled row
 constexpr int kMaxStages = 10;
 constexpr int kThreads = 192;
 constexpr uint32_t kBytesP = kTileN * kBlockK;
 constexpr int kMaxSplit = 8;           // portable cluster size
-// 32-bit sums of products of int8 hold for this many k-blocks (2^14 * 128 * 1023 < 2^31); longer
-// sums are split over the cluster, whose parts are added in 64 bits.
-constexpr int kMaxBlocksInt8 = 1023;
 
-struct MatmulArgs {
-  const float* scale_a;   // [m] or null
-  const float* scale_b;   // [n] or null
-  void* out;
-  int64_t ld_out;
-  int m, n;
-  int kblocks;            // ceil(k / 128)
+struct SplitArgs {
+  MatmulArgs c;
   int tile_m;             // rows m per tile: 16, 32, 64, 128 or 256
   int n_tiles;
   int split;              // CTAs per tile (cluster size)
   int stages;
   uint32_t stage_bytes;
-  int out_fp32;
 };
 
 // Dynamic shared memory: stages (P tile, Q tile), reused for the split's partial sums.
 template <bool INT8, bool P_MN, bool Q_MN>
 __global__ void __launch_bounds__(kThreads, 1)
 matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
-                 const MatmulArgs a) {
+                 const SplitArgs a) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], done;
   __shared__ uint32_t tmem_slot;
@@ -69,7 +69,7 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
   const int rank = a.split > 1 ? (int)cluster_ctarank() : 0;
   const int tile = blockIdx.x / a.split;
   const int n0 = (tile % a.n_tiles) * kTileN, m0 = (tile / a.n_tiles) * a.tile_m;
-  const int kb0 = (int)((int64_t)a.kblocks * rank / a.split), kb1 = (int)((int64_t)a.kblocks * (rank + 1) / a.split);
+  const int kb0 = (int)((int64_t)a.c.kblocks * rank / a.split), kb1 = (int)((int64_t)a.c.kblocks * (rank + 1) / a.split);
   const uint32_t tmem_cols = a.tile_m < 32 ? 32u : (uint32_t)a.tile_m;
 
   if (threadIdx.x == 0) {
@@ -98,7 +98,7 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
       int it = 0;
       for (int kb = kb0; kb < kb1; ++kb, ++it) {
         const int s = it % a.stages;
-        if (!mbar_wait(&empty[s], ((it / a.stages) & 1) ^ 1, abort_flag, &g_q8_status)) break;
+        if (!mbar_wait(&empty[s], ((it / a.stages) & 1) ^ 1, abort_flag, a.c.status)) break;
         uint8_t* sp = smem + (size_t)s * a.stage_bytes;
         uint8_t* sq = sp + kBytesP;
         mbar_expect_tx(&full[s], a.stage_bytes);
@@ -128,7 +128,7 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
       int it = 0;
       for (int kb = kb0; kb < kb1; ++kb, ++it) {
         const int s = it % a.stages;
-        if (!mbar_wait(&full[s], (it / a.stages) & 1, abort_flag, &g_q8_status)) { ok = false; break; }
+        if (!mbar_wait(&full[s], (it / a.stages) & 1, abort_flag, a.c.status)) { ok = false; break; }
         tcgen05_after_sync();
         const uint32_t sp = smem_u32(smem + (size_t)s * a.stage_bytes), sq = sp + kBytesP;
         const uint64_t dp = P_MN ? desc_mn_major(sp, 128 * kBlockK) : desc_k_major(sp);
@@ -143,7 +143,7 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
   }
   bool ok = true;
   if (warp >= 2) {
-    ok = mbar_wait(&done, 0, abort_flag, &g_q8_status);
+    ok = mbar_wait(&done, 0, abort_flag, a.c.status);
     ok = __all_sync(0xffffffffu, ok);
     tcgen05_after_sync();
   }
@@ -151,15 +151,15 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
   const int col = quad * 32 + lane;            // this thread's output column in the tile
   const int n = n0 + col;
   const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
-  const int m_here = min(a.tile_m, a.m - m0);
-  const float sb = warp >= 2 && a.scale_b && n < a.n ? __ldg(a.scale_b + n) : 1.f;
+  const int m_here = min(a.tile_m, a.c.m - m0);
+  const float sb = warp >= 2 && a.c.scale_b && n < a.c.n ? __ldg(a.c.scale_b + n) : 1.f;
   auto put = [&](int t, float v) {
     const int m = m0 + t;
-    if (a.scale_a) v *= __ldg(a.scale_a + m);
+    if (a.c.scale_a) v *= __ldg(a.c.scale_a + m);
     v *= sb;
-    const int64_t at = (int64_t)m * a.ld_out + n;
-    if (a.out_fp32) reinterpret_cast<float*>(a.out)[at] = v;
-    else reinterpret_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+    const int64_t at = (int64_t)m * a.c.ld_out + n;
+    if (a.c.out_fp32) reinterpret_cast<float*>(a.c.out)[at] = v;
+    else reinterpret_cast<__nv_bfloat16*>(a.c.out)[at] = __float2bfloat16_rn(v);
   };
   if (a.split == 1) {
     if (warp >= 2 && ok) {
@@ -167,7 +167,7 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
         uint32_t r[16];
         tmem_ld16(trow + t0, r);
         tmem_wait_ld();
-        if (n < a.n) {
+        if (n < a.c.n) {
 #pragma unroll
           for (int j = 0; j < 16; ++j)
             if (t0 + j < m_here) put(t0 + j, INT8 ? (float)(int)r[j] : __uint_as_float(r[j]));
@@ -187,7 +187,7 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
     }
     __syncwarp();
     cluster_barrier();
-    if (warp >= 2 && ok && n < a.n) {
+    if (warp >= 2 && ok && n < a.c.n) {
       const uint32_t base = smem_u32(part) + (uint32_t)col * 4;
       for (int t = rank; t < m_here; t += a.split) {
         if (INT8) {
@@ -214,40 +214,10 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
   }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = []() -> EncodeTiledFn {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult res;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &res) != cudaSuccess ||
-        res != cudaDriverEntryPointSuccess)
-      return nullptr;
-    return (EncodeTiledFn)p;
-  }();
-  return fn;
-}
-
-// Map over rows x cols bytes (row-major, ld bytes apart), boxes of box_rows x 128 bytes; what lies
-// outside reads as zero.
-bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
-  EncodeTiledFn encode = encode_fn();
-  if (!encode) return false;
-  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)ld};
-  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
-  const cuuint32_t step[2] = {1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, step,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 constexpr size_t kSmemBudget = 200 * 1024;
 
 template <bool INT8, bool P_MN, bool Q_MN>
-int launch_matmul(const CUtensorMap& mp, const CUtensorMap& mq, const MatmulArgs& a, int ctas, size_t smem,
+int launch_matmul(const CUtensorMap& mp, const CUtensorMap& mq, const SplitArgs& a, int ctas, size_t smem,
                   cudaStream_t stream) {
   static PerDeviceOnce once;
   int dev;
@@ -271,6 +241,50 @@ int launch_matmul(const CUtensorMap& mp, const CUtensorMap& mq, const MatmulArgs
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, matmul_q8_kernel<INT8, P_MN, Q_MN>, mp, mq, a) == cudaSuccess ? PRM_OK
                                                                                               : PRM_ERR_CUDA;
+}
+
+int matmul_split(const MatmulProblem& p) {
+  const int64_t m = p.c.m, n = p.c.n;
+  SplitArgs g = {};
+  g.c = p.c;
+  g.tile_m = 16;
+  while (g.tile_m < 256 && g.tile_m < m) g.tile_m *= 2;
+  g.n_tiles = (int)((n + kTileN - 1) / kTileN);
+  const int64_t tiles = (int64_t)g.n_tiles * ((m + g.tile_m - 1) / g.tile_m);
+  // Split k while every SM would otherwise not get a tile, but leave each CTA four k-blocks.
+  int split = 1;
+  while (split < kMaxSplit && tiles * (split + 1) <= 148 && g.c.kblocks >= 4 * (split + 1)) ++split;
+  if (p.int8) {
+    const int need = (g.c.kblocks + kMaxBlocksInt8 - 1) / kMaxBlocksInt8;
+    if (need > kMaxSplit) return PRM_ERR_SHAPE;
+    split = std::max(split, need);
+  }
+  g.split = split;
+  if (tiles * split > 0x7fffffffLL) return PRM_ERR_SHAPE;
+  const uint32_t q_bytes = (p.a_t ? (uint32_t)std::max(g.tile_m, 128) : (uint32_t)g.tile_m) * kBlockK;
+  g.stage_bytes = kBytesP + q_bytes;
+  const int blocks_each = (g.c.kblocks + split - 1) / split;
+  g.stages = std::max(1, std::min<int>({kMaxStages, blocks_each, (int)(kSmemBudget / g.stage_bytes)}));
+  size_t smem = (size_t)g.stages * g.stage_bytes;
+  if (split > 1) smem = std::max(smem, (size_t)g.tile_m * kTileN * 4);
+  smem += 1024;
+  CUtensorMap mp, mq;
+  if (!q8_make_map(&mp, p.b, p.b_rows, p.b_cols, p.ld_b, 128) ||
+      !q8_make_map(&mq, p.a, p.a_rows, p.a_cols, p.ld_a, p.a_t ? 128 : g.tile_m))
+    return PRM_ERR_CUDA;
+  const int ctas = (int)(tiles * split);
+#define PRM_Q8_LAUNCH(I8, PM, QM) \
+  if (p.int8 == I8 && !p.b_t == PM && p.a_t == QM) return launch_matmul<I8, PM, QM>(mp, mq, g, ctas, smem, p.stream)
+  PRM_Q8_LAUNCH(true, true, false);
+  PRM_Q8_LAUNCH(true, false, false);
+  PRM_Q8_LAUNCH(true, true, true);
+  PRM_Q8_LAUNCH(true, false, true);
+  PRM_Q8_LAUNCH(false, true, false);
+  PRM_Q8_LAUNCH(false, false, false);
+  PRM_Q8_LAUNCH(false, true, true);
+  PRM_Q8_LAUNCH(false, false, true);
+#undef PRM_Q8_LAUNCH
+  return PRM_ERR_ARG;
 }
 
 }  // namespace
@@ -300,56 +314,24 @@ extern "C" int prm_matmul_q8(const void* a, int64_t ld_a, int a_transposed, cons
   if (ld_a < a_cols || ld_b < b_cols || ld_a >= ((int64_t)1 << 39) || ld_b >= ((int64_t)1 << 39)) return PRM_ERR_SHAPE;
   if (!aligned16(a) || !aligned16(b) || ld_a % 16 != 0 || ld_b % 16 != 0) return PRM_ERR_ALIGN;
 
-  const bool int8 = format == PRM_Q8_INT8;
   const bool p_mn = !b_transposed, q_mn = a_transposed != 0;
-  MatmulArgs g = {};
-  g.scale_a = scale_a;
-  g.scale_b = scale_b;
-  g.out = out;
-  g.ld_out = ld_out;
-  g.m = (int)m;
-  g.n = (int)n;
-  g.out_fp32 = out_fp32;
-  g.kblocks = (int)((k + kBlockK - 1) / kBlockK);
-  g.tile_m = 16;
-  while (g.tile_m < 256 && g.tile_m < m) g.tile_m *= 2;
-  g.n_tiles = (int)((n + kTileN - 1) / kTileN);
-  const int64_t tiles = (int64_t)g.n_tiles * ((m + g.tile_m - 1) / g.tile_m);
-  // Split k while every SM would otherwise not get a tile, but leave each CTA four k-blocks.
-  int split = 1;
-  while (split < kMaxSplit && tiles * (split + 1) <= 148 && g.kblocks >= 4 * (split + 1)) ++split;
-  if (int8) {
-    const int need = (g.kblocks + kMaxBlocksInt8 - 1) / kMaxBlocksInt8;
-    if (need > kMaxSplit) return PRM_ERR_SHAPE;
-    split = std::max(split, need);
-  }
-  g.split = split;
-  if (tiles * split > 0x7fffffffLL) return PRM_ERR_SHAPE;
-  const uint32_t q_bytes = (q_mn ? (uint32_t)std::max(g.tile_m, 128) : (uint32_t)g.tile_m) * kBlockK;
-  g.stage_bytes = kBytesP + q_bytes;
-  const int blocks_each = (g.kblocks + split - 1) / split;
-  g.stages = std::max(1, std::min<int>({kMaxStages, blocks_each, (int)(kSmemBudget / g.stage_bytes)}));
-  size_t smem = (size_t)g.stages * g.stage_bytes;
-  if (split > 1) smem = std::max(smem, (size_t)g.tile_m * kTileN * 4);
-  smem += 1024;
-
-  CUtensorMap mp, mq;
-  if (!make_map(&mp, b, b_rows, b_cols, ld_b, 128) ||
-      !make_map(&mq, a, a_rows, a_cols, ld_a, q_mn ? 128 : g.tile_m))
-    return PRM_ERR_CUDA;
-  const int ctas = (int)(tiles * split);
-#define PRM_Q8_LAUNCH(I8, PM, QM) \
-  if (int8 == I8 && p_mn == PM && q_mn == QM) return launch_matmul<I8, PM, QM>(mp, mq, g, ctas, smem, stream)
-  PRM_Q8_LAUNCH(true, true, false);
-  PRM_Q8_LAUNCH(true, false, false);
-  PRM_Q8_LAUNCH(true, true, true);
-  PRM_Q8_LAUNCH(true, false, true);
-  PRM_Q8_LAUNCH(false, true, false);
-  PRM_Q8_LAUNCH(false, false, false);
-  PRM_Q8_LAUNCH(false, true, true);
-  PRM_Q8_LAUNCH(false, false, true);
-#undef PRM_Q8_LAUNCH
-  return PRM_ERR_ARG;
+  MatmulProblem p = {};
+  p.c = {scale_a, scale_b, out, status_word(), ld_out, (int)m, (int)n, (int)((k + kBlockK - 1) / kBlockK), out_fp32};
+  p.a = a;
+  p.b = b;
+  p.ld_a = ld_a;
+  p.ld_b = ld_b;
+  p.a_rows = a_rows;
+  p.a_cols = a_cols;
+  p.b_rows = b_rows;
+  p.b_cols = b_cols;
+  p.a_t = q_mn;
+  p.b_t = !p_mn;
+  p.int8 = format == PRM_Q8_INT8;
+  p.stream = stream;
+  if (!p.c.status) return PRM_ERR_CUDA;
+  if (matmul_q8_wants_pairs(p)) return matmul_q8_pairs(p);
+  return matmul_split(p);
 }
 
 extern "C" int prm_q8_status(void) {

@@ -1,0 +1,69 @@
+// What the two kernels of the 8-bit product share: the problem, its tensor maps, the choice.
+#pragma once
+
+#include "q8.cuh"
+#include "tcgen05.cuh"
+
+namespace prm {
+
+constexpr int kBlockK = 128;           // one 128-byte swizzled row of k
+// 32-bit sums of products of int8 hold for this many k-blocks (2^14 * 128 * 1023 < 2^31); longer
+// sums are split over a cluster, whose parts are added in 64 bits.
+constexpr int kMaxBlocksInt8 = 1023;
+
+// What both kernels read besides their tensor maps.
+struct MatmulArgs {
+  const float* scale_a;   // [m] or null
+  const float* scale_b;   // [n] or null
+  void* out;
+  int* status;
+  int64_t ld_out;
+  int m, n;
+  int kblocks;            // ceil(k / 128)
+  int out_fp32;
+};
+
+struct MatmulProblem {
+  MatmulArgs c;
+  const void *a, *b;
+  int64_t ld_a, ld_b, a_rows, a_cols, b_rows, b_cols;   // as stored
+  bool a_t, b_t;          // stored k x m, n x k
+  bool int8;
+  cudaStream_t stream;
+};
+
+// Pairs of CTAs on 256 x 256 tiles, for products that fill the GPU with them.
+bool matmul_q8_wants_pairs(const MatmulProblem& p);
+int matmul_q8_pairs(const MatmulProblem& p);
+
+typedef CUresult (*Q8EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline Q8EncodeFn q8_encode_fn() {
+  static Q8EncodeFn fn = []() -> Q8EncodeFn {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult res;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &res) != cudaSuccess ||
+        res != cudaDriverEntryPointSuccess)
+      return nullptr;
+    return (Q8EncodeFn)p;
+  }();
+  return fn;
+}
+
+// Map over rows x cols bytes (row-major, ld bytes apart), boxes of box_rows x 128 bytes; what lies
+// outside reads as zero.
+inline bool q8_make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+  Q8EncodeFn encode = q8_encode_fn();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  const cuuint32_t step[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace prm

@@ -1,0 +1,306 @@
+// The 8-bit product for shapes that fill the GPU with 256 x 256 tiles: persistent CTA pairs on
+// tcgen05.mma.cta_group::2.
+//
+// A pair computes out[m0 .. m0+255, n0 .. n0+255].  The matrix instruction's M is the output's n
+// (CTA r of the pair holds columns n0 + 128 r .. + 127 of b, and those lanes of the accumulator),
+// its N is the output's m (each CTA holds 128 of the 256 rows of a): a tensor-memory lane is then an
+// output column, so a warp stores 32 neighbouring columns of a row straight from registers,
+// whatever the alignment of the output.
+//
+//   warp 0      TMA producer: per stage 256 k of both operands (64 KB), 128-byte swizzle, no multicast;
+//               the copies of both CTAs count on the leader's barrier.  Three stages
+//   warp 1      tcgen05.mma issuer (one lane of the leader); owns its CTA's tensor memory
+//   warps 2..9  epilogue: two warps per lane quadrant, half of the 256 rows m each
+// Two accumulators of 256 columns let the epilogue of a tile run under the next tile's main loop.
+// Every barrier wait is bounded; one that runs out sets the status word, the pair drains and leaves.
+#include "q8_matmul.cuh"
+
+namespace prm {
+namespace {
+
+constexpr int kTile = 256;                       // tile edge, both ways
+constexpr int kSub = 2;                          // k-blocks per stage
+constexpr int kStages = 3;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 32 * (2 + kEpiWarps);
+constexpr uint32_t kBoxBytes = 128 * kBlockK;    // 128 rows of one k-block
+constexpr uint32_t kStageBytes = 2 * kSub * kBoxBytes;
+constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes;
+
+// Load whose completion is counted on the pair leader's barrier (a shared::cluster address).
+__device__ __forceinline__ void tma_load_pair(void* dst, const CUtensorMap* map, uint32_t bar_cluster, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(smem_u32(dst)), "l"((uint64_t)map), "r"(bar_cluster), "r"(x), "r"(y)
+      : "memory");
+}
+template <bool INT8>
+__device__ __forceinline__ void umma_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                          uint32_t accumulate) {
+  if constexpr (INT8) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+  }
+}
+// Arrives, once all matrix instructions issued so far are done, on the barrier at this
+// shared-memory offset in both CTAs of the pair (a barrier arrival, not a load).
+__device__ __forceinline__ void umma_commit_both(uint32_t bar) {
+  const uint16_t mask = 3;
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(bar), "h"(mask)
+               : "memory");
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar_cluster) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+
+struct PairArgs {
+  MatmulArgs c;
+  int m_tiles, tiles;
+};
+
+template <bool INT8, bool P_MN, bool Q_MN>
+__global__ void __launch_bounds__(kThreads, 1)
+matmul_q8_pair_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
+                      const PairArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kStages], empty[kStages], tfull[2], tempty[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  volatile int* abort_flag = &abort_word;
+  int* status = a.c.status;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int stages_k = (a.c.kblocks + kSub - 1) / kSub;          // stages per tile
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&tfull[i], 1);
+      mbar_init(&tempty[i], 2 * kEpiWarps);
+    }
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)),
+                 "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tcgen05_before_sync();
+  __syncthreads();
+  cluster_barrier();                             // the peer's barriers are initialised too
+  tcgen05_after_sync();
+  const uint32_t tmem = tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      const uint32_t lead_full = cluster_map(smem_u32(&full[0]), 0);
+      for (int t = pair; t < a.tiles && ok; t += pairs) {
+        const int n0 = (t / a.m_tiles) * kTile + (int)rank * 128, m0 = (t % a.m_tiles) * kTile + (int)rank * 128;
+        for (int kt = 0; kt < stages_k; ++kt, ++it) {
+          const int s = it % kStages;
+          if (!mbar_wait(&empty[s], ((it / kStages) & 1) ^ 1, abort_flag, status)) { ok = false; break; }
+          uint8_t* sp = smem + (size_t)s * kStageBytes;
+          uint8_t* sq = sp + kSub * kBoxBytes;
+          const int subs = min(kSub, a.c.kblocks - kt * kSub);
+          if (rank == 0) mbar_expect_tx(&full[s], (uint32_t)subs * 4 * kBoxBytes);   // both CTAs' bytes
+          const uint32_t bar = lead_full + 8u * s;
+#pragma unroll
+          for (int j = 0; j < kSub; ++j) {
+            if (j < subs) {
+              const int k0 = (kt * kSub + j) * kBlockK;
+              tma_load_pair(sp + j * kBoxBytes, &map_p, bar, P_MN ? n0 : k0, P_MN ? k0 : n0);
+              tma_load_pair(sq + j * kBoxBytes, &map_q, bar, Q_MN ? m0 : k0, Q_MN ? k0 : m0);
+            }
+          }
+        }
+      }
+      // Copies in flight must land before shared memory is released; the leader sees both CTAs'.
+      if (rank == 0) {
+        for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j) {
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(&full[j % kStages], (j / kStages) & 1) && global_ns() - t0 < 1000000ull) {
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = idesc_8bit(INT8, kTile, kTile, P_MN, Q_MN);
+      constexpr uint32_t kStepP = P_MN ? 256 : 2, kStepQ = Q_MN ? 256 : 2;    // 32 k, in units of 16 bytes
+      uint32_t it = 0, acc = 0;
+      bool ok = true;
+      const uint32_t smem0 = smem_u32(smem);
+      for (int t = pair; t < a.tiles && ok; t += pairs, ++acc) {
+        const uint32_t ab = acc & 1;
+        if (!mbar_wait(&tempty[ab], ((acc >> 1) & 1) ^ 1, abort_flag, status)) break;
+        tcgen05_after_sync();
+        const uint32_t d = tmem + ab * kTile;
+        for (int kt = 0; kt < stages_k; ++kt, ++it) {
+          const int s = it % kStages;
+          if (!mbar_wait(&full[s], (it / kStages) & 1, abort_flag, status)) { ok = false; break; }
+          tcgen05_after_sync();
+          const uint32_t sp = smem0 + (uint32_t)s * kStageBytes, sq = sp + kSub * kBoxBytes;
+          const int subs = min(kSub, a.c.kblocks - kt * kSub);
+#pragma unroll
+          for (int j = 0; j < kSub; ++j) {
+            if (j < subs) {
+              const uint64_t dp = P_MN ? desc_mn_major(sp + j * kBoxBytes, kBoxBytes) : desc_k_major(sp + j * kBoxBytes);
+              const uint64_t dq = Q_MN ? desc_mn_major(sq + j * kBoxBytes, kBoxBytes) : desc_k_major(sq + j * kBoxBytes);
+#pragma unroll
+              for (int i = 0; i < kBlockK / 32; ++i)
+                umma_pair<INT8>(d, dp + kStepP * i, dq + kStepQ * i, idesc, (kt | j | i) != 0);
+            }
+          }
+          umma_commit_both(smem_u32(&empty[s]));
+        }
+        if (ok) umma_commit_both(smem_u32(&tfull[ab]));
+      }
+    }
+  } else {
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const int col = quad * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    const uint32_t lead_tempty = cluster_map(smem_u32(&tempty[0]), 0);
+    uint32_t acc = 0;
+    for (int t = pair; t < a.tiles; t += pairs, ++acc) {
+      const uint32_t ab = acc & 1;
+      const bool got = mbar_wait(&tfull[ab], (acc >> 1) & 1, abort_flag, status);
+      if (!__all_sync(0xffffffffu, got)) break;
+      tcgen05_after_sync();
+      const int n = (t / a.m_tiles) * kTile + (int)rank * 128 + col;
+      const int m0 = (t % a.m_tiles) * kTile + half * 128;
+      const float sb = a.c.scale_b && n < a.c.n ? __ldg(a.c.scale_b + n) : 1.f;
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        uint32_t r[32];
+        tmem_ld32(trow + ab * kTile + half * 128 + c * 32, r);
+        tmem_wait_ld();
+        const int m1 = m0 + c * 32;
+        if (n < a.c.n) {
+          const int64_t at = (int64_t)m1 * a.c.ld_out + n;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            if (m1 + j < a.c.m) {
+              float v = INT8 ? (float)(int)r[j] : __uint_as_float(r[j]);
+              if (a.c.scale_a) v *= __ldg(a.c.scale_a + m1 + j);
+              v *= sb;
+              const int64_t o = at + j * a.c.ld_out;
+              if (a.c.out_fp32) reinterpret_cast<float*>(a.c.out)[o] = v;
+              else reinterpret_cast<__nv_bfloat16*>(a.c.out)[o] = __float2bfloat16_rn(v);
+            }
+          }
+        }
+      }
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) arrive_cluster(lead_tempty + 8u * ab);
+    }
+  }
+  // Neither CTA leaves while its partner can still touch its shared or tensor memory.
+  tcgen05_before_sync();
+  __syncwarp();
+  __syncthreads();
+  cluster_barrier();
+  if (warp == 1) {
+    tcgen05_after_sync();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+template <bool INT8, bool P_MN, bool Q_MN>
+int launch_pairs(const CUtensorMap& mp, const CUtensorMap& mq, const PairArgs& a, cudaStream_t stream) {
+  static PerDeviceOnce once;
+  static int resident[64];
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int dev;
+  if (once.need(&dev)) {
+    int n = 0, sms = 0;
+    if (dev < 0 || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaFuncSetAttribute(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)kSmemBytes) != cudaSuccess)
+      return PRM_ERR_CUDA;
+    cfg.gridDim = dim3((unsigned)(sms & ~1), 1, 1);
+    if (cudaOccupancyMaxActiveClusters(&n, matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, &cfg) != cudaSuccess || n < 1)
+      return PRM_ERR_CUDA;
+    resident[dev] = n;
+    once.mark(dev);
+  }
+  cfg.gridDim = dim3(2u * (unsigned)std::min(a.tiles, resident[dev]), 1, 1);
+  return cudaLaunchKernelEx(&cfg, matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, mp, mq, a) == cudaSuccess ? PRM_OK
+                                                                                                   : PRM_ERR_CUDA;
+}
+
+}  // namespace
+
+bool matmul_q8_wants_pairs(const MatmulProblem& p) {
+  const int64_t tiles = (int64_t)((p.c.m + kTile - 1) / kTile) * ((p.c.n + kTile - 1) / kTile);
+  return tiles >= 56 && tiles < (1 << 30) && (!p.int8 || p.c.kblocks <= kMaxBlocksInt8);
+}
+
+int matmul_q8_pairs(const MatmulProblem& p) {
+  PairArgs g = {};
+  g.c = p.c;
+  g.m_tiles = (p.c.m + kTile - 1) / kTile;
+  g.tiles = g.m_tiles * ((p.c.n + kTile - 1) / kTile);
+  CUtensorMap mp, mq;
+  if (!q8_make_map(&mp, p.b, p.b_rows, p.b_cols, p.ld_b, 128) ||
+      !q8_make_map(&mq, p.a, p.a_rows, p.a_cols, p.ld_a, 128))
+    return PRM_ERR_CUDA;
+#define PRM_Q8_LAUNCH(I8, PM, QM) \
+  if (p.int8 == I8 && !p.b_t == PM && p.a_t == QM) return launch_pairs<I8, PM, QM>(mp, mq, g, p.stream)
+  PRM_Q8_LAUNCH(true, true, false);
+  PRM_Q8_LAUNCH(true, false, false);
+  PRM_Q8_LAUNCH(true, true, true);
+  PRM_Q8_LAUNCH(true, false, true);
+  PRM_Q8_LAUNCH(false, true, false);
+  PRM_Q8_LAUNCH(false, false, false);
+  PRM_Q8_LAUNCH(false, true, true);
+  PRM_Q8_LAUNCH(false, false, true);
+#undef PRM_Q8_LAUNCH
+  return PRM_ERR_ARG;
+}
+
+}  // namespace prm
