@@ -153,25 +153,30 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
   const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
   const int m_here = min(a.tile_m, a.c.m - m0);
   const float sb = warp >= 2 && a.c.scale_b && n < a.c.n ? __ldg(a.c.scale_b + n) : 1.f;
-  auto put = [&](int t, float v) {
-    const int m = m0 + t;
-    if (a.c.scale_a) v *= __ldg(a.c.scale_a + m);
-    v *= sb;
-    const int64_t at = (int64_t)m * a.c.ld_out + n;
+  auto put = [&](int t, float v, float sa) {   // row t of this tile
+    const int64_t at = (int64_t)(m0 + t) * a.c.ld_out + n;
+    v = v * sa * sb;
     if (a.c.out_fp32) reinterpret_cast<float*>(a.c.out)[at] = v;
     else reinterpret_cast<__nv_bfloat16*>(a.c.out)[at] = __float2bfloat16_rn(v);
+  };
+  // The scale of row t, one per lane and handed round by shuffles: a load per row would serialise
+  // on its latency.
+  auto row_scale = [&](int t) {
+    return a.c.scale_a && t < m_here ? __ldg(a.c.scale_a + m0 + t) : 1.f;
   };
   if (a.split == 1) {
     if (warp >= 2 && ok) {
       for (int t0 = 0; t0 < m_here; t0 += 16) {
         uint32_t r[16];
         tmem_ld16(trow + t0, r);
+        const float sa = row_scale(t0 + (lane & 15));
         tmem_wait_ld();
-        if (n < a.c.n) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (t0 + j < m_here) put(t0 + j, INT8 ? (float)(int)r[j] : __uint_as_float(r[j]));
-        }
+        const int64_t at = (int64_t)(m0 + t0) * a.c.ld_out + n;
+        if (a.c.out_fp32)
+          store_column<INT8, 16>(reinterpret_cast<float*>(a.c.out) + at, a.c.ld_out, r, sa, sb, m_here - t0, n < a.c.n);
+        else
+          store_column<INT8, 16>(reinterpret_cast<__nv_bfloat16*>(a.c.out) + at, a.c.ld_out, r, sa, sb, m_here - t0,
+                                 n < a.c.n);
       }
     }
   } else {
@@ -187,18 +192,32 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
     }
     __syncwarp();
     cluster_barrier();
-    if (warp >= 2 && ok && n < a.c.n) {
+    if (warp >= 2 && ok) {
+      // Rows t = rank, rank + split, ...: four at a time, so that their parts are fetched together.
       const uint32_t base = smem_u32(part) + (uint32_t)col * 4;
-      for (int t = rank; t < m_here; t += a.split) {
-        if (INT8) {
-          long long sum = 0;
-          for (int q = 0; q < a.split; ++q) sum += (int)ld_cluster_u32(cluster_map(base + t * kTileN * 4, q));
-          put(t, (float)sum);
-        } else {
-          float sum = 0.f;
-          for (int q = 0; q < a.split; ++q)
-            sum += __uint_as_float(ld_cluster_u32(cluster_map(base + t * kTileN * 4, q)));
-          put(t, sum);
+      for (int t0 = rank; t0 < m_here; t0 += 4 * a.split) {
+        const float sa = row_scale(t0 + (lane & 3) * a.split);
+        long long isum[4] = {0, 0, 0, 0};
+        float fsum[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int q = 0; q < a.split; ++q) {
+          const uint32_t at = cluster_map(base, q);
+          uint32_t v[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int t = t0 + j * a.split;
+            v[j] = t < m_here ? ld_cluster_u32(at + (uint32_t)t * kTileN * 4) : 0u;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (INT8) isum[j] += (int)v[j];
+            else fsum[j] += __uint_as_float(v[j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float s = __shfl_sync(0xffffffffu, sa, j);
+          const int t = t0 + j * a.split;
+          if (n < a.c.n && t < m_here) put(t, INT8 ? (float)isum[j] : fsum[j], s);
         }
       }
     }

@@ -207,21 +207,16 @@ matmul_q8_pair_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_co
       for (int c = 0; c < 4; ++c) {
         uint32_t r[32];
         tmem_ld32(trow + ab * kTile + half * 128 + c * 32, r);
-        tmem_wait_ld();
         const int m1 = m0 + c * 32;
-        if (n < a.c.n) {
-          const int64_t at = (int64_t)m1 * a.c.ld_out + n;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            if (m1 + j < a.c.m) {
-              float v = INT8 ? (float)(int)r[j] : __uint_as_float(r[j]);
-              if (a.c.scale_a) v *= __ldg(a.c.scale_a + m1 + j);
-              v *= sb;
-              const int64_t o = at + j * a.c.ld_out;
-              if (a.c.out_fp32) reinterpret_cast<float*>(a.c.out)[o] = v;
-              else reinterpret_cast<__nv_bfloat16*>(a.c.out)[o] = __float2bfloat16_rn(v);
-            }
-          }
+        // one row scale per lane, handed round by shuffles: a load per row would serialise on its latency
+        const float sa = a.c.scale_a && m1 + lane < a.c.m ? __ldg(a.c.scale_a + m1 + lane) : 1.f;
+        tmem_wait_ld();
+        const int rows = min(32, a.c.m - m1);
+        const int64_t at = (int64_t)m1 * a.c.ld_out + n;
+        if (a.c.out_fp32) {
+          store_column<INT8, 32>(reinterpret_cast<float*>(a.c.out) + at, a.c.ld_out, r, sa, sb, rows, n < a.c.n);
+        } else {
+          store_column<INT8, 32>(reinterpret_cast<__nv_bfloat16*>(a.c.out) + at, a.c.ld_out, r, sa, sb, rows, n < a.c.n);
         }
       }
       tcgen05_before_sync();
