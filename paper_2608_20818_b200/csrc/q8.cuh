@@ -25,76 +25,151 @@ __host__ __device__ inline float q8_limit(int format) { return format == PRM_Q8_
 // What a set of values with the largest magnitude `top` is multiplied by, and the scale that undoes
 // it.  The factor is limit * (1 / top), each step rounded, which is how array libraries evaluate a
 // number over an array: codes then agree bit for bit with `(t * (limit / top)).round()` written
-// there.  `top_bits` is the maximum of the magnitudes' bit patterns as unsigned integers, which orders
-// NaN above infinity above every number: a set that holds either gets the scale NaN and zero codes,
-// so it marks its own row (column) of whatever is computed from it and no other.
+// there.  A set that holds an infinity or a NaN (which maxima here keep) gets the scale NaN and zero
+// codes, so it marks its own row (column) of whatever is computed from it and no other.
 struct Q8Scale {
   float mul, scale;
   bool finite;
 };
-__device__ __forceinline__ Q8Scale q8_scale(uint32_t top_bits, float limit) {
+__device__ __forceinline__ Q8Scale q8_scale(float top, float limit) {
   Q8Scale s;
-  const float top = __uint_as_float(top_bits);
-  s.finite = top_bits < 0x7f800000u;
+  s.finite = top < __uint_as_float(0x7f800000u);
   const bool live = s.finite && top >= kQ8Tiny;
   s.mul = live ? __fmul_rn(limit, __frcp_rn(top)) : 0.f;
   s.scale = live ? __fdiv_rn(top, limit) : (s.finite ? 0.f : __uint_as_float(0x7fc00000u));
   return s;
 }
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// ------------------------------------------------------------- eight elements at a time
+// The row operators read 2 to 6 bytes per element, so what bounds them next to memory is the number
+// of instructions per element: everything below works on pairs (fp32x2 products, sums and fused
+// products round like their scalar forms; bf16x2 conversions; a three-way maximum).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return d;
+}
+// Largest of m and the two magnitudes; a NaN among them stays.
+__device__ __forceinline__ float max_abs(float m, float2 v) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(m), "f"(fabsf(v.x)), "f"(fabsf(v.y)));
+  return d;
+}
+__device__ __forceinline__ float2 pair_of(uint32_t bf16x2) {
+  return make_float2(__uint_as_float(bf16x2 << 16), __uint_as_float(bf16x2 & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t pair_to_bf16(float2 v) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+  return reinterpret_cast<const uint32_t&>(h);
+}
+
+// Eight elements as stored (16-byte aligned), converted on use, so that a kernel that takes several
+// has all its loads under way before it waits for the first.
+template <typename T> struct Oct;
+template <> struct Oct<__nv_bfloat16> {
+  uint4 r;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { r = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void load_stream(const __nv_bfloat16* p) { r = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = r; }
+  __device__ __forceinline__ void get(float2 (&v)[4]) const {
+    v[0] = pair_of(r.x);
+    v[1] = pair_of(r.y);
+    v[2] = pair_of(r.z);
+    v[3] = pair_of(r.w);
+  }
+  __device__ __forceinline__ void set(const float2 (&v)[4]) {
+    r = make_uint4(pair_to_bf16(v[0]), pair_to_bf16(v[1]), pair_to_bf16(v[2]), pair_to_bf16(v[3]));
+  }
+  __device__ __forceinline__ void zero() { r = make_uint4(0, 0, 0, 0); }
+};
+template <> struct Oct<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const float4*>(p);
+    b = *reinterpret_cast<const float4*>(p + 4);
+  }
+  __device__ __forceinline__ void load_stream(const float* p) {
+    a = __ldcs(reinterpret_cast<const float4*>(p));
+    b = __ldcs(reinterpret_cast<const float4*>(p + 4));
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    *reinterpret_cast<float4*>(p) = a;
+    *reinterpret_cast<float4*>(p + 4) = b;
+  }
+  __device__ __forceinline__ void get(float2 (&v)[4]) const {
+    v[0] = make_float2(a.x, a.y);
+    v[1] = make_float2(a.z, a.w);
+    v[2] = make_float2(b.x, b.y);
+    v[3] = make_float2(b.z, b.w);
+  }
+  __device__ __forceinline__ void set(const float2 (&v)[4]) {
+    a = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+    b = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+  }
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+};
 
 // Four values, already multiplied, to four codes (first value in the lowest byte).
-__device__ __forceinline__ uint32_t q8_pack4(float a, float b, float c, float d, int format) {
-  if (format == PRM_Q8_INT8) {
+template <int FORMAT>
+__device__ __forceinline__ uint32_t codes4(float2 a, float2 b) {
+  if constexpr (FORMAT == PRM_Q8_INT8) {
     // |v| <= 127: adding 1.5 * 2^23 leaves the value rounded to nearest-even in the low bits.
-    const float m = 12582912.f;
-    const uint32_t x = __float_as_uint(__fadd_rn(a, m)), y = __float_as_uint(__fadd_rn(b, m));
-    const uint32_t z = __float_as_uint(__fadd_rn(c, m)), w = __float_as_uint(__fadd_rn(d, m));
-    return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
+    const float2 m = make_float2(12582912.f, 12582912.f);
+    a = add2(a, m);
+    b = add2(b, m);
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
+                       __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+  } else {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(a, __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(b, __NV_SATFINITE, __NV_E4M3);
+    return lo | (hi << 16);
   }
-  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
-  return lo | (hi << 16);
 }
-__device__ __forceinline__ uint8_t q8_pack1(float a, int format) {
-  return (uint8_t)(q8_pack4(a, 0.f, 0.f, 0.f, format) & 0xffu);
+// Eight codes of t * mul.
+template <int FORMAT>
+__device__ __forceinline__ uint2 codes8(const float2 (&t)[4], float2 mul) {
+  return make_uint2(codes4<FORMAT>(mul2(t[0], mul), mul2(t[1], mul)), codes4<FORMAT>(mul2(t[2], mul), mul2(t[3], mul)));
+}
+__device__ __forceinline__ uint8_t code1(float v, int format) {
+  const float2 p = make_float2(v, 0.f), z = make_float2(0.f, 0.f);
+  return (uint8_t)((format == PRM_Q8_INT8 ? codes4<PRM_Q8_INT8>(p, z) : codes4<PRM_Q8_E4M3>(p, z)) & 0xffu);
+}
+// The codes of NV octs of a thread, `stride` elements apart, below `cols`; zeros where the row has no
+// number for a scale.
+template <int NV>
+__device__ __forceinline__ void store_octs(uint8_t* q, const float2 (&t)[NV][4], int c0, int stride, int cols,
+                                           const Q8Scale& s, int format) {
+  const float2 mul = make_float2(s.mul, s.mul);
+  auto each = [&](auto code) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = c0 + v * stride;
+      if (c < cols) *reinterpret_cast<uint2*>(q + c) = code(t[v]);
+    }
+  };
+  if (!s.finite) each([](const float2 (&)[4]) { return make_uint2(0u, 0u); });
+  else if (format == PRM_Q8_INT8) each([&](const float2 (&x)[4]) { return codes8<PRM_Q8_INT8>(x, mul); });
+  else each([&](const float2 (&x)[4]) { return codes8<PRM_Q8_E4M3>(x, mul); });
 }
 
-// VEC consecutive elements as fp32 (VEC = 8: 16-byte aligned; VEC = 1: anywhere).
-template <int VEC, typename T>
-__device__ __forceinline__ void load_vec(const T* p, float (&out)[VEC]) {
-  if constexpr (VEC == 8) {
-    load8(p, out);
-  } else {
-    out[0] = to_f32(*p);
-  }
-}
-template <int VEC, typename T>
-__device__ __forceinline__ void store_vec(T* p, const float (&in)[VEC]) {
-  if constexpr (VEC == 8) {
-    store8(p, in);
-  } else {
-    from_f32(p, in[0]);
-  }
-}
-template <int VEC>
-__device__ __forceinline__ void load_weight(const void* w, int fp32, int64_t i, float (&out)[VEC]) {
-  if (fp32) {
-    load_vec<VEC>(reinterpret_cast<const float*>(w) + i, out);
-  } else {
-    load_vec<VEC>(reinterpret_cast<const __nv_bfloat16*>(w) + i, out);
-  }
-}
-template <int VEC>
-__device__ __forceinline__ void store_codes(uint8_t* p, const float (&v)[VEC], int format) {
-  if constexpr (VEC == 8) {
-    uint2 c;
-    c.x = q8_pack4(v[0], v[1], v[2], v[3], format);
-    c.y = q8_pack4(v[4], v[5], v[6], v[7], format);
-    *reinterpret_cast<uint2*>(p) = c;
-  } else {
-    *p = q8_pack1(v[0], format);
-  }
+__device__ __forceinline__ float load1(const void* p, int fp32, int64_t i) {
+  return fp32 ? reinterpret_cast<const float*>(p)[i] : to_f32(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
 }
 // The value as it is kept in the stream's type.
 __device__ __forceinline__ float as_stored(float v, const float*) { return v; }
@@ -102,25 +177,48 @@ __device__ __forceinline__ float as_stored(float v, const __nv_bfloat16*) {
   return __bfloat162float(__float2bfloat16_rn(v));
 }
 
-// Sum and (unsigned) maximum over the first `THREADS` threads of a block of exactly that size;
-// every thread gets both.  `red` holds 2 * 32 words and may be used again after the next call's
-// first barrier (calls alternate between two arrays).
+// Largest value over a warp; a NaN in any lane stays (`top` is no negative number).
+__device__ __forceinline__ float warp_top(float top) {
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+}
+// Sum and largest magnitude over a block of THREADS threads (32: each warp by itself); every thread
+// gets both.  `red`: 64 words, used once between two barriers.
 template <int THREADS>
-__device__ __forceinline__ void block_sum_max(float& sum, uint32_t& top, uint32_t* red) {
+__device__ __forceinline__ void block_sum_top(float& sum, float& top, float* red) {
   sum = warp_sum(sum);
-  top = __reduce_max_sync(0xffffffffu, top);
+  top = warp_top(top);
   if constexpr (THREADS > 32) {
     constexpr int kWarps = THREADS / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (lane == 0) {
-      red[warp] = __float_as_uint(sum);
+      red[warp] = sum;
       red[32 + warp] = top;
     }
     __syncthreads();
-    sum = lane < kWarps ? __uint_as_float(red[lane]) : 0.f;
-    top = lane < kWarps ? red[32 + lane] : 0u;
+    sum = lane < kWarps ? red[lane] : 0.f;
+    top = lane < kWarps ? red[32 + lane] : 0.f;
     sum = warp_sum(sum);
-    top = __reduce_max_sync(0xffffffffu, top);
+    top = warp_top(top);
+  }
+}
+
+// Sums of two numbers over a block of THREADS threads.  `red`: 64 words; calls in turn use two sets.
+template <int THREADS>
+__device__ __forceinline__ void block_sum2(float& p, float& q, float* red) {
+  p = warp_sum(p);
+  q = warp_sum(q);
+  if constexpr (THREADS > 32) {
+    constexpr int kWarps = THREADS / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) {
+      red[warp] = p;
+      red[32 + warp] = q;
+    }
+    __syncthreads();
+    p = lane < kWarps ? red[lane] : 0.f;
+    q = lane < kWarps ? red[32 + lane] : 0.f;
+    p = warp_sum(p);
+    q = warp_sum(q);
   }
 }
 

@@ -25,19 +25,6 @@ namespace {
 
 __device__ int g_q8_status;
 
-// The status word's address on the current device.
-int* status_word() {
-  static int* at[64] = {};
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-  if (!at[dev]) {
-    void* p = nullptr;
-    if (cudaGetSymbolAddress(&p, g_q8_status) != cudaSuccess) return nullptr;
-    at[dev] = (int*)p;
-  }
-  return at[dev];
-}
-
 constexpr int kTileN = 128;            // output columns per CTA (lanes of the accumulator)
 constexpr int kMaxStages = 10;
 constexpr int kThreads = 192;
@@ -307,6 +294,20 @@ int matmul_split(const MatmulProblem& p) {
 }
 
 }  // namespace
+
+// The status word's address on the current device.
+int* q8_status_word() {
+  static int* at[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+  if (!at[dev]) {
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, g_q8_status) != cudaSuccess) return nullptr;
+    at[dev] = (int*)p;
+  }
+  return at[dev];
+}
+
 }  // namespace prm
 
 using namespace prm;
@@ -335,7 +336,7 @@ extern "C" int prm_matmul_q8(const void* a, int64_t ld_a, int a_transposed, cons
 
   const bool p_mn = !b_transposed, q_mn = a_transposed != 0;
   MatmulProblem p = {};
-  p.c = {scale_a, scale_b, out, status_word(), ld_out, (int)m, (int)n, (int)((k + kBlockK - 1) / kBlockK), out_fp32};
+  p.c = {scale_a, scale_b, out, q8_status_word(), ld_out, (int)m, (int)n, (int)((k + kBlockK - 1) / kBlockK), out_fp32};
   p.a = a;
   p.b = b;
   p.ld_a = ld_a;

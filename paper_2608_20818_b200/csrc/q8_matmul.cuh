@@ -45,6 +45,9 @@ __device__ __forceinline__ void store_column(OUT* out, int64_t ld, const uint32_
   }
 }
 
+// The status word that prm_q8_status reads, on the current device (null if it has none).
+int* q8_status_word();
+
 struct MatmulProblem {
   MatmulArgs c;
   const void *a, *b;

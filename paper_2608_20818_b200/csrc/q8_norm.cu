@@ -8,7 +8,12 @@
 //
 // Gradient, the rounding taken as the identity, with g = grad_y * w:
 //   grad_x = s g - h s^3 mean(g h) + grad_h,    grad_w = sum over rows of grad_y h s
-#include "q8.cuh"
+//
+// Both are bound by HBM (7 and 8 bytes per element of a bf16 stream with its residual).  Three
+// forms each: rows of octs (8 elements) held in registers, one row per block; for large matrices the
+// same arithmetic on rows streamed through shared memory; and single elements in two passes for rows
+// that are not aligned or longer than the registers of a block.
+#include "row_ring.cuh"
 
 namespace prm {
 namespace {
@@ -25,135 +30,197 @@ struct NormArgs {
   float eps;
 };
 
-// One row per group of TPR threads (a warp: eight rows per block; else a block), kept in registers
-// between the reduction and the rounding: VEC * NV elements per thread.
-template <typename IO, int VEC, int NV, int TPR>
+__device__ __forceinline__ float inv_rms(float sum, int cols, float eps) { return 1.f / sqrtf(sum / (float)cols + eps); }
+
+// h (= x, plus r if RES, rounded to the stream's type and stored), t = h * w, sum of squares and top.
+template <typename IO, bool RES>
+__device__ __forceinline__ void norm_oct(Oct<IO> x, Oct<IO> r, const float2 (&w)[4], IO* h_out, float2 (&t)[4],
+                                         float2& sum, float& top) {
+  if constexpr (RES) {
+    float2 b[4];
+    x.get(t);
+    r.get(b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = add2(t[e], b[e]);
+    x.set(t);
+    x.store(h_out);
+  }
+  x.get(t);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    sum = fma2(t[e], t[e], sum);
+    t[e] = mul2(t[e], w[e]);
+    top = max_abs(top, t[e]);
+  }
+}
+
+// One row per group of TPR threads (a warp: eight rows per block; else a block), 8 * NV elements per
+// thread.
+template <typename IO, typename WT, int NV, int TPR, bool RES>
 __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const NormArgs a) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
-  __shared__ uint32_t red[64];
-  const int lane = threadIdx.x % TPR;
+  __shared__ float red[64];
+  const int c0 = (threadIdx.x % TPR) * 8;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   if (row >= a.rows) return;              // whole warps (kRows > 1) or no thread
   const IO* x = reinterpret_cast<const IO*>(a.x) + row * a.ld_x;
-  const IO* r = a.residual ? reinterpret_cast<const IO*>(a.residual) + row * a.ld_r : nullptr;
-  float t[NV][VEC];
-  float sum = 0.f;
-  uint32_t top = 0;
+  const IO* r = RES ? reinterpret_cast<const IO*>(a.residual) + row * a.ld_r : nullptr;
+  IO* h = RES ? reinterpret_cast<IO*>(a.h) + row * a.ld_h : nullptr;
+  Oct<IO> xv[NV], rv[NV];
+  Oct<WT> wv[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = (v * TPR + lane) * VEC;
+    const int c = c0 + v * TPR * 8;
     if (c < a.cols) {
-      load_vec<VEC>(x + c, t[v]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) t[v][e] = 0.f;
+      xv[v].load_stream(x + c);
+      if constexpr (RES) rv[v].load_stream(r + c);
+      wv[v].load(reinterpret_cast<const WT*>(a.weight) + c);
     }
   }
-  if (r) {
-    IO* h = reinterpret_cast<IO*>(a.h) + row * a.ld_h;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = (v * TPR + lane) * VEC;
-      if (c < a.cols) {
-        float b[VEC];
-        load_vec<VEC>(r + c, b);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) t[v][e] = as_stored(t[v][e] + b[e], (const IO*)nullptr);
-        store_vec<VEC>(h + c, t[v]);
-      }
-    }
-  }
+  float2 t[NV][4], sum2 = make_float2(0.f, 0.f);
+  float top = 0.f;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = (v * TPR + lane) * VEC;
+    const int c = c0 + v * TPR * 8;
     if (c < a.cols) {
-      float w[VEC];
-      load_weight<VEC>(a.weight, a.weight_fp32, c, w);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        sum += t[v][e] * t[v][e];
-        t[v][e] = __fmul_rn(t[v][e], w[e]);
-        top = max(top, abs_bits(t[v][e]));
-      }
+      float2 w[4];
+      wv[v].get(w);
+      norm_oct<IO, RES>(xv[v], rv[v], w, h + c, t[v], sum2, top);
     }
   }
-  block_sum_max<TPR>(sum, top, red);
+  float sum = sum2.x + sum2.y;
+  block_sum_top<TPR>(sum, top, red);
   const Q8Scale s = q8_scale(top, q8_limit(a.format));
-  uint8_t* q = a.q + row * a.ld_q;
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c = (v * TPR + lane) * VEC;
-    if (c < a.cols) {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) t[v][e] = s.finite ? __fmul_rn(t[v][e], s.mul) : 0.f;
-      store_codes<VEC>(q + c, t[v], a.format);
-    }
-  }
-  if (lane == 0) a.scale[row] = s.scale * (1.f / sqrtf(sum / (float)a.cols + a.eps));
+  store_octs<NV>(a.q + row * a.ld_q, t, c0, TPR * 8, a.cols, s, a.format);
+  if (c0 == 0) a.scale[row] = s.scale * inv_rms(sum, a.cols, a.eps);
 }
 
-// Rows too long for the registers of a block: the same in two passes over the row, the second of
-// which finds it in L2.
-template <typename IO>
-__global__ void __launch_bounds__(1024) rmsnorm_q8_long_kernel(const NormArgs a) {
-  __shared__ uint32_t red[64];
+// Large matrices: rows streamed through a ring, a group of W warps each.
+template <typename IO, typename WT, int W, bool RES>
+__global__ void __launch_bounds__(kRingWarps<IO> * 32, 1)
+rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
+  constexpr int kArr = RES ? 2 : 1, kNV = 4, kStep = W * 32 * 8;
+  RingBlock<IO, W, kArr>& b = ring_block<IO, W, kArr>();
+  const int c0 = (threadIdx.x % (W * 32)) * 8;
+  const void* const src[2] = {a.x, a.residual};
+  const int64_t ld[2] = {a.ld_x, a.ld_r};
+  RowRing<IO, W, kArr> ring(b, src, ld, a.rows, a.cols, stages, status);
+  Oct<WT> wv[kNV];
+#pragma unroll
+  for (int v = 0; v < kNV; ++v)
+    if (c0 + v * kStep < a.cols) wv[v].load(reinterpret_cast<const WT*>(a.weight) + c0 + v * kStep);
+  ring.start();
+  for (int64_t i = 0; i < ring.n; ++i) {
+    const int64_t row = ring.row(i);
+    float2 t[kNV][4], sum2 = make_float2(0.f, 0.f);
+    float top = 0.f;
+    if (ring.wait()) {
+      IO* h = RES ? reinterpret_cast<IO*>(a.h) + row * a.ld_h : nullptr;
+      Oct<IO> xv[kNV], rv[kNV];
+#pragma unroll
+      for (int v = 0; v < kNV; ++v) {
+        const int c = c0 + v * kStep;
+        if (c < a.cols) {
+          xv[v].load(ring.at(0) + c);
+          if constexpr (RES) rv[v].load(ring.at(1) + c);
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < kNV; ++v) {
+        const int c = c0 + v * kStep;
+        if (c < a.cols) {
+          float2 w[4];
+          wv[v].get(w);
+          norm_oct<IO, RES>(xv[v], rv[v], w, h + c, t[v], sum2, top);
+        }
+      }
+    }
+    float sum = sum2.x + sum2.y;
+    ring.sum_top(i, sum, top);
+    ring.next(i);
+    if (ring.ok) {
+      const Q8Scale s = q8_scale(top, q8_limit(a.format));
+      store_octs<kNV>(a.q + row * a.ld_q, t, c0, kStep, a.cols, s, a.format);
+      if (c0 == 0) a.scale[row] = s.scale * inv_rms(sum, a.cols, a.eps);
+    }
+  }
+  ring.finish();
+}
+
+// Any alignment, any length: two passes over the row, the second of which finds it in cache.
+template <typename IO, int THREADS>
+__global__ void __launch_bounds__(THREADS) rmsnorm_q8_single_kernel(const NormArgs a) {
+  __shared__ float red[64];
   const int64_t row = blockIdx.x;
   const IO* x = reinterpret_cast<const IO*>(a.x) + row * a.ld_x;
   const IO* r = a.residual ? reinterpret_cast<const IO*>(a.residual) + row * a.ld_r : nullptr;
   IO* h = r ? reinterpret_cast<IO*>(a.h) + row * a.ld_h : nullptr;
-  float sum = 0.f;
-  uint32_t top = 0;
-  for (int c = threadIdx.x; c < a.cols; c += 1024) {
+  float sum = 0.f, top = 0.f;
+#pragma unroll 4
+  for (int c = threadIdx.x; c < a.cols; c += THREADS) {
     float v = to_f32(x[c]);
     if (r) {
       v = as_stored(v + to_f32(r[c]), (const IO*)nullptr);
       from_f32(h + c, v);
     }
-    float w[1];
-    load_weight<1>(a.weight, a.weight_fp32, c, w);
     sum += v * v;
-    top = max(top, abs_bits(__fmul_rn(v, w[0])));
+    top = max_abs(top, make_float2(__fmul_rn(v, load1(a.weight, a.weight_fp32, c)), 0.f));
   }
-  block_sum_max<1024>(sum, top, red);
+  block_sum_top<THREADS>(sum, top, red);
   const Q8Scale s = q8_scale(top, q8_limit(a.format));
   const IO* src = r ? h : x;
   uint8_t* q = a.q + row * a.ld_q;
-  for (int c = threadIdx.x; c < a.cols; c += 1024) {      // each thread reads what it wrote itself
-    float w[1];
-    load_weight<1>(a.weight, a.weight_fp32, c, w);
-    const float t = __fmul_rn(to_f32(src[c]), w[0]);
-    q[c] = q8_pack1(s.finite ? __fmul_rn(t, s.mul) : 0.f, a.format);
+#pragma unroll 4
+  for (int c = threadIdx.x; c < a.cols; c += THREADS) {      // each thread reads what it wrote itself
+    const float t = __fmul_rn(to_f32(src[c]), load1(a.weight, a.weight_fp32, c));
+    q[c] = code1(s.finite ? __fmul_rn(t, s.mul) : 0.f, a.format);
   }
-  if (threadIdx.x == 0) a.scale[row] = s.scale * (1.f / sqrtf(sum / (float)a.cols + a.eps));
+  if (threadIdx.x == 0) a.scale[row] = s.scale * inv_rms(sum, a.cols, a.eps);
 }
 
-template <typename IO, int VEC, int NV, int TPR>
-void launch_norm(const NormArgs& a, cudaStream_t stream) {
+template <typename IO, typename WT, int NV, int TPR>
+int launch_norm(const NormArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
-  rmsnorm_q8_kernel<IO, VEC, NV, TPR>
-      <<<(unsigned)((a.rows + kRows - 1) / kRows), TPR == 32 ? 256 : TPR, 0, stream>>>(a);
+  const unsigned blocks = (unsigned)((a.rows + kRows - 1) / kRows);
+  if (a.residual) rmsnorm_q8_kernel<IO, WT, NV, TPR, true><<<blocks, TPR == 32 ? 256 : TPR, 0, stream>>>(a);
+  else rmsnorm_q8_kernel<IO, WT, NV, TPR, false><<<blocks, TPR == 32 ? 256 : TPR, 0, stream>>>(a);
+  return PRM_OK;
+}
+
+template <typename IO, typename WT, int W>
+int launch_norm_stream(const NormArgs& a, cudaStream_t stream) {
+  auto go = [&](auto kernel, int arrays, PerDeviceOnce& once) {
+    return launch_ring<IO, W>(kernel, arrays, once, a.rows, a.cols, 0, stream, a);
+  };
+  static PerDeviceOnce with, without;
+  return a.residual ? go(rmsnorm_q8_stream_kernel<IO, WT, W, true>, 2, with)
+                    : go(rmsnorm_q8_stream_kernel<IO, WT, W, false>, 1, without);
+}
+
+template <typename IO, typename WT>
+int run_norm(const NormArgs& a, cudaStream_t stream) {
+  const int c = a.cols;
+  if (ring_worth(a.rows, c)) {
+    if (c <= 1024) return launch_norm_stream<IO, WT, 1>(a, stream);
+    if (c <= 2048) return launch_norm_stream<IO, WT, 2>(a, stream);
+    if (c <= 4096) return launch_norm_stream<IO, WT, 4>(a, stream);
+    return launch_norm_stream<IO, WT, 8>(a, stream);
+  }
+  if (c <= 256) return launch_norm<IO, WT, 1, 32>(a, stream);
+  if (c <= 512) return launch_norm<IO, WT, 2, 32>(a, stream);
+  if (c <= 1024) return launch_norm<IO, WT, 1, 128>(a, stream);
+  if (c <= 2048) return launch_norm<IO, WT, 2, 128>(a, stream);
+  if (c <= 4096) return launch_norm<IO, WT, 2, 256>(a, stream);
+  if (c <= 8192) return launch_norm<IO, WT, 2, 512>(a, stream);
+  return launch_norm<IO, WT, 2, 1024>(a, stream);
 }
 
 template <typename IO>
-void run_norm(const NormArgs& a, bool vec, cudaStream_t stream) {
-  const int c = a.cols;
-  if (vec) {
-    if (c <= 256) launch_norm<IO, 8, 1, 32>(a, stream);
-    else if (c <= 512) launch_norm<IO, 8, 2, 32>(a, stream);
-    else if (c <= 1024) launch_norm<IO, 8, 1, 128>(a, stream);
-    else if (c <= 2048) launch_norm<IO, 8, 2, 128>(a, stream);
-    else if (c <= 4096) launch_norm<IO, 8, 2, 256>(a, stream);
-    else if (c <= 8192) launch_norm<IO, 8, 2, 512>(a, stream);
-    else if (c <= 16384) launch_norm<IO, 8, 2, 1024>(a, stream);
-    else if (c <= 32768) launch_norm<IO, 8, 4, 1024>(a, stream);
-    else rmsnorm_q8_long_kernel<IO><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
-  } else {
-    if (c <= 256) launch_norm<IO, 1, 8, 32>(a, stream);
-    else if (c <= 2048) launch_norm<IO, 1, 8, 256>(a, stream);
-    else if (c <= 8192) launch_norm<IO, 1, 16, 512>(a, stream);
-    else if (c <= 16384) launch_norm<IO, 1, 16, 1024>(a, stream);
-    else rmsnorm_q8_long_kernel<IO><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
-  }
+int run_norm_single(const NormArgs& a, cudaStream_t stream) {
+  if (a.cols <= 1024) rmsnorm_q8_single_kernel<IO, 128><<<(unsigned)a.rows, 128, 0, stream>>>(a);
+  else if (a.cols <= 8192) rmsnorm_q8_single_kernel<IO, 256><<<(unsigned)a.rows, 256, 0, stream>>>(a);
+  else rmsnorm_q8_single_kernel<IO, 1024><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
+  return PRM_OK;
 }
 
 // ------------------------------------------------------------------ gradient
@@ -164,105 +231,199 @@ struct NormGradArgs {
   const void* weight;
   const void* gh;         // may be null
   void* gx;
-  float* part;            // [parts][cols] partial sums of grad_w
+  float* part;            // [blocks][cols] partial sums of grad_w
   int64_t rows, ld_gy, ld_h, ld_gh, ld_gx;
   int cols, weight_fp32;
   float eps;
 };
 
-// Sums of two numbers over a block.
-template <int THREADS>
-__device__ __forceinline__ void block_sum2(float& p, float& q, float* red) {
-  p = warp_sum(p);
-  q = warp_sum(q);
-  if constexpr (THREADS > 32) {
-    constexpr int kWarps = THREADS / 32;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0) {
-      red[warp] = p;
-      red[32 + warp] = q;
-    }
-    __syncthreads();
-    p = lane < kWarps ? red[lane] : 0.f;
-    q = lane < kWarps ? red[32 + lane] : 0.f;
-    p = warp_sum(p);
-    q = warp_sum(q);
+// The two sums of a row over one oct.
+__device__ __forceinline__ void grad_sums(const float2 (&gy)[4], const float2 (&h)[4], const float2 (&w)[4],
+                                          float2& ss, float2& gh) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    ss = fma2(h[e], h[e], ss);
+    gh = fma2(mul2(gy[e], w[e]), h[e], gh);
   }
+}
+// One oct of grad_x, and of grad_w added to gw.
+template <typename IO>
+__device__ __forceinline__ void grad_oct(const float2 (&gy)[4], const float2 (&h)[4], const float2 (&w)[4],
+                                         const Oct<IO>* add, float s, float k, IO* out, float2 (&gw)[4]) {
+  const float2 s2 = make_float2(s, s), nk = make_float2(-k, -k);
+  float2 o[4];
+  if (add) {
+    add->get(o);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fma2(h[e], nk, o[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = mul2(h[e], nk);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 gs = mul2(gy[e], s2);
+    gw[e] = fma2(gs, h[e], gw[e]);
+    o[e] = fma2(gs, w[e], o[e]);
+  }
+  Oct<IO> r;
+  r.set(o);
+  r.store(out);
 }
 
 // A block walks over rows; a thread keeps the same columns in all of them, so its share of grad_w
 // stays in registers until the block's last row.
-template <typename IO, int VEC, int NV, int TPR>
+template <typename IO, typename WT, int NV, int TPR>
 __global__ void __launch_bounds__(TPR) rmsnorm_q8_grad_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
-  const int lane = threadIdx.x;
-  float gw[NV][VEC];
+  const int c0 = threadIdx.x * 8;
+  float2 gw[NV][4];
+  Oct<WT> wv[NV];
 #pragma unroll
-  for (int v = 0; v < NV; ++v)
+  for (int v = 0; v < NV; ++v) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) gw[v][e] = 0.f;
+    for (int e = 0; e < 4; ++e) gw[v][e] = make_float2(0.f, 0.f);
+    if (c0 + v * TPR * 8 < a.cols) wv[v].load(reinterpret_cast<const WT*>(a.weight) + c0 + v * TPR * 8);
+  }
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
     const IO* gyp = reinterpret_cast<const IO*>(a.gy) + row * a.ld_gy;
     const IO* hp = reinterpret_cast<const IO*>(a.h) + row * a.ld_h;
-    float gy[NV][VEC], h[NV][VEC];
-    float ss = 0.f, gh = 0.f;
+    const IO* ghp = a.gh ? reinterpret_cast<const IO*>(a.gh) + row * a.ld_gh : nullptr;
+    Oct<IO> gyv[NV], hv[NV], ghv[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * TPR + lane) * VEC;
+      const int c = c0 + v * TPR * 8;
       if (c < a.cols) {
-        float w[VEC];
-        load_vec<VEC>(gyp + c, gy[v]);
-        load_vec<VEC>(hp + c, h[v]);
-        load_weight<VEC>(a.weight, a.weight_fp32, c, w);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          ss += h[v][e] * h[v][e];
-          gh += gy[v][e] * w[e] * h[v][e];
-        }
+        gyv[v].load_stream(gyp + c);
+        hv[v].load_stream(hp + c);
+        if (ghp) ghv[v].load_stream(ghp + c);
       }
     }
+    float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (c0 + v * TPR * 8 < a.cols) {
+        float2 gy[4], h[4], w[4];
+        gyv[v].get(gy);
+        hv[v].get(h);
+        wv[v].get(w);
+        grad_sums(gy, h, w, ss2, gh2);
+      }
+    }
+    float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
     block_sum2<TPR>(ss, gh, red[turn]);
-    const float s = 1.f / sqrtf(ss / (float)a.cols + a.eps);
-    const float k = s * s * s * (gh / (float)a.cols);
-    const IO* ghp = a.gh ? reinterpret_cast<const IO*>(a.gh) + row * a.ld_gh : nullptr;
+    const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
     IO* gxp = reinterpret_cast<IO*>(a.gx) + row * a.ld_gx;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * TPR + lane) * VEC;
+      const int c = c0 + v * TPR * 8;
       if (c < a.cols) {
-        float w[VEC], out[VEC];
-        load_weight<VEC>(a.weight, a.weight_fp32, c, w);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          gw[v][e] += gy[v][e] * h[v][e] * s;
-          out[e] = s * (gy[v][e] * w[e]) - h[v][e] * k;
-        }
-        if (ghp) {
-          float d[VEC];
-          load_vec<VEC>(ghp + c, d);
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) out[e] += d[e];
-        }
-        store_vec<VEC>(gxp + c, out);
+        float2 gy[4], h[4], w[4];
+        gyv[v].get(gy);
+        hv[v].get(h);
+        wv[v].get(w);
+        grad_oct<IO>(gy, h, w, ghp ? &ghv[v] : nullptr, s, k, gxp + c, gw[v]);
       }
     }
   }
   float* part = a.part + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = (v * TPR + lane) * VEC;
+    const int c = c0 + v * TPR * 8;
     if (c < a.cols) {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) part[c + e] = gw[v][e];
+      Oct<float> o;
+      o.set(gw[v]);
+      o.store(part + c);
     }
   }
 }
 
-// Rows too long for registers: two passes over the row, and the block's share of grad_w collected
-// in its line of the scratch (each thread its own columns).
-template <typename IO>
-__global__ void __launch_bounds__(1024) rmsnorm_q8_grad_long_kernel(const NormGradArgs a) {
+// Large matrices: rows streamed through a ring.  The groups' shares of grad_w meet in the ring's
+// memory at the end, so that a block leaves one line of partial sums.
+template <typename IO, typename WT, int W, bool GH>
+__global__ void __launch_bounds__(kRingWarps<IO> * 32, 1)
+rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
+  constexpr int kArr = GH ? 3 : 2, kNV = 4, kStep = W * 32 * 8, kGroups = kRingWarps<IO> / W;
+  RingBlock<IO, W, kArr>& b = ring_block<IO, W, kArr>();
+  const int c0 = (threadIdx.x % (W * 32)) * 8;
+  const void* const src[3] = {a.gy, a.h, a.gh};
+  const int64_t ld[3] = {a.ld_gy, a.ld_h, a.ld_gh};
+  RowRing<IO, W, kArr> ring(b, src, ld, a.rows, a.cols, stages, status);
+  float2 gw[kNV][4];
+#pragma unroll
+  for (int v = 0; v < kNV; ++v)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) gw[v][e] = make_float2(0.f, 0.f);
+  ring.start();
+  for (int64_t i = 0; i < ring.n; ++i) {
+    const int64_t row = ring.row(i);
+    Oct<IO> gyv[kNV], hv[kNV], ghv[kNV];
+    float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
+    if (ring.wait()) {
+#pragma unroll
+      for (int v = 0; v < kNV; ++v) {
+        const int c = c0 + v * kStep;
+        if (c < a.cols) {
+          float2 gy[4], h[4], w[4];
+          Oct<WT> wv;
+          wv.load(reinterpret_cast<const WT*>(a.weight) + c);
+          gyv[v].load(ring.at(0) + c);
+          hv[v].load(ring.at(1) + c);
+          if constexpr (GH) ghv[v].load(ring.at(2) + c);
+          gyv[v].get(gy);
+          hv[v].get(h);
+          wv.get(w);
+          grad_sums(gy, h, w, ss2, gh2);
+        }
+      }
+    }
+    float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
+    ring.sum2(i, ss, gh);
+    ring.next(i);
+    if (ring.ok) {
+      const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
+      IO* gxp = reinterpret_cast<IO*>(a.gx) + row * a.ld_gx;
+#pragma unroll
+      for (int v = 0; v < kNV; ++v) {
+        const int c = c0 + v * kStep;
+        if (c < a.cols) {
+          float2 gy[4], h[4], w[4];
+          Oct<WT> wv;
+          wv.load(reinterpret_cast<const WT*>(a.weight) + c);
+          gyv[v].get(gy);
+          hv[v].get(h);
+          wv.get(w);
+          grad_oct<IO>(gy, h, w, GH ? &ghv[v] : nullptr, s, k, gxp + c, gw[v]);
+        }
+      }
+    }
+  }
+  ring.finish();
+  __syncthreads();                        // every group's copies have been consumed
+  float* sums = reinterpret_cast<float*>(ring_memory());
+#pragma unroll
+  for (int v = 0; v < kNV; ++v) {
+    const int c = c0 + v * kStep;
+    if (c < a.cols) {
+      Oct<float> o;
+      o.set(gw[v]);
+      o.store(sums + (size_t)ring.group * a.cols + c);
+    }
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.cols; c += kRingWarps<IO> * 32) {
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) sum += sums[(size_t)g * a.cols + c];
+    a.part[(int64_t)blockIdx.x * a.cols + c] = sum;
+  }
+}
+
+// Any alignment, any length: two passes over the row, and the block's share of grad_w collected in
+// its line of the scratch (each thread its own columns).
+template <typename IO, int THREADS>
+__global__ void __launch_bounds__(THREADS) rmsnorm_q8_grad_single_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
   float* part = a.part + (int64_t)blockIdx.x * a.cols;
   int turn = 0;
@@ -272,21 +433,18 @@ __global__ void __launch_bounds__(1024) rmsnorm_q8_grad_long_kernel(const NormGr
     const IO* ghp = a.gh ? reinterpret_cast<const IO*>(a.gh) + row * a.ld_gh : nullptr;
     IO* gxp = reinterpret_cast<IO*>(a.gx) + row * a.ld_gx;
     float ss = 0.f, gh = 0.f;
-    for (int c = threadIdx.x; c < a.cols; c += 1024) {
-      float w[1];
-      load_weight<1>(a.weight, a.weight_fp32, c, w);
+#pragma unroll 4
+    for (int c = threadIdx.x; c < a.cols; c += THREADS) {
       const float h = to_f32(hp[c]);
       ss += h * h;
-      gh += to_f32(gyp[c]) * w[0] * h;
+      gh += to_f32(gyp[c]) * load1(a.weight, a.weight_fp32, c) * h;
     }
-    block_sum2<1024>(ss, gh, red[turn]);
-    const float s = 1.f / sqrtf(ss / (float)a.cols + a.eps);
-    const float k = s * s * s * (gh / (float)a.cols);
-    for (int c = threadIdx.x; c < a.cols; c += 1024) {
-      float w[1];
-      load_weight<1>(a.weight, a.weight_fp32, c, w);
+    block_sum2<THREADS>(ss, gh, red[turn]);
+    const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
+#pragma unroll 4
+    for (int c = threadIdx.x; c < a.cols; c += THREADS) {
       const float h = to_f32(hp[c]), gy = to_f32(gyp[c]);
-      float out = s * (gy * w[0]) - h * k;
+      float out = s * (gy * load1(a.weight, a.weight_fp32, c)) - h * k;
       if (ghp) out += to_f32(ghp[c]);
       from_f32(gxp + c, out);
       const float add = gy * h * s;
@@ -295,22 +453,24 @@ __global__ void __launch_bounds__(1024) rmsnorm_q8_grad_long_kernel(const NormGr
   }
 }
 
-// grad_w: the parts added in a fixed order, 32 columns per block, eight parts at a time.
-__global__ void __launch_bounds__(256)
+// grad_w: the parts added in a fixed order, 32 columns per block, a 32nd of the parts per warp.
+__global__ void __launch_bounds__(1024)
 rmsnorm_q8_grad_weight_kernel(const float* part, int parts, int cols, void* gw, int fp32) {
-  __shared__ float s[8][33];
+  __shared__ float s[32][33];
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
   float sum = 0.f;
-  if (c < cols)
-    for (int p = k; p < parts; p += 8) sum += part[(int64_t)p * cols + c];
+  if (c < cols) {
+#pragma unroll 4
+    for (int p = k; p < parts; p += 32) sum += part[(int64_t)p * cols + c];
+  }
   s[k][threadIdx.x & 31] = sum;
   __syncthreads();
-  if (k == 0 && c < cols) {
-    sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum += s[j][threadIdx.x];
-    if (fp32) reinterpret_cast<float*>(gw)[c] = sum;
-    else reinterpret_cast<__nv_bfloat16*>(gw)[c] = __float2bfloat16_rn(sum);
+  // column k of the block now lies in s[0..31][k]
+  sum = warp_sum(s[threadIdx.x & 31][k]);
+  const int out = blockIdx.x * 32 + k;
+  if ((threadIdx.x & 31) == 0 && out < cols) {
+    if (fp32) reinterpret_cast<float*>(gw)[out] = sum;
+    else reinterpret_cast<__nv_bfloat16*>(gw)[out] = __float2bfloat16_rn(sum);
   }
 }
 
@@ -318,27 +478,39 @@ constexpr int kGradParts = 296;    // two blocks per SM
 
 int grad_parts(int64_t rows) { return (int)std::min<int64_t>(rows, kGradParts); }
 
-template <typename IO, int VEC, int NV, int TPR>
-void launch_grad(const NormGradArgs& a, int parts, cudaStream_t stream) {
-  rmsnorm_q8_grad_kernel<IO, VEC, NV, TPR><<<parts, TPR, 0, stream>>>(a);
+template <typename IO, typename WT, int W>
+int launch_grad_stream(const NormGradArgs& a, int* parts, cudaStream_t stream) {
+  constexpr int kGroups = kRingWarps<IO> / W;
+  *parts = ring_blocks(a.rows, kGroups);
+  static PerDeviceOnce with, without;
+  const size_t sums = (size_t)kGroups * a.cols * 4;
+  return a.gh ? launch_ring<IO, W>(rmsnorm_q8_grad_stream_kernel<IO, WT, W, true>, 3, with, a.rows, a.cols, sums, stream, a)
+              : launch_ring<IO, W>(rmsnorm_q8_grad_stream_kernel<IO, WT, W, false>, 2, without, a.rows, a.cols, sums,
+                                   stream, a);
+}
+
+template <typename IO, typename WT>
+int run_grad(const NormGradArgs& a, int* parts, cudaStream_t stream) {
+  const int c = a.cols;
+  if (ring_worth(a.rows, c)) {
+    if (c <= 1024) return launch_grad_stream<IO, WT, 1>(a, parts, stream);
+    if (c <= 2048) return launch_grad_stream<IO, WT, 2>(a, parts, stream);
+    if (c <= 4096) return launch_grad_stream<IO, WT, 4>(a, parts, stream);
+    return launch_grad_stream<IO, WT, 8>(a, parts, stream);
+  }
+  if (c <= 256) rmsnorm_q8_grad_kernel<IO, WT, 1, 32><<<*parts, 32, 0, stream>>>(a);
+  else if (c <= 1024) rmsnorm_q8_grad_kernel<IO, WT, 1, 128><<<*parts, 128, 0, stream>>>(a);
+  else if (c <= 4096) rmsnorm_q8_grad_kernel<IO, WT, 1, 512><<<*parts, 512, 0, stream>>>(a);
+  else rmsnorm_q8_grad_kernel<IO, WT, 2, 512><<<*parts, 512, 0, stream>>>(a);
+  return PRM_OK;
 }
 
 template <typename IO>
-void run_grad(const NormGradArgs& a, bool vec, int parts, cudaStream_t stream) {
-  const int c = a.cols;
-  if (vec) {
-    if (c <= 256) launch_grad<IO, 8, 1, 32>(a, parts, stream);
-    else if (c <= 1024) launch_grad<IO, 8, 1, 128>(a, parts, stream);
-    else if (c <= 2048) launch_grad<IO, 8, 1, 256>(a, parts, stream);
-    else if (c <= 4096) launch_grad<IO, 8, 1, 512>(a, parts, stream);
-    else if (c <= 8192) launch_grad<IO, 8, 1, 1024>(a, parts, stream);
-    else rmsnorm_q8_grad_long_kernel<IO><<<parts, 1024, 0, stream>>>(a);
-  } else {
-    if (c <= 256) launch_grad<IO, 1, 8, 32>(a, parts, stream);
-    else if (c <= 2048) launch_grad<IO, 1, 8, 256>(a, parts, stream);
-    else if (c <= 8192) launch_grad<IO, 1, 8, 1024>(a, parts, stream);
-    else rmsnorm_q8_grad_long_kernel<IO><<<parts, 1024, 0, stream>>>(a);
-  }
+int run_grad_single(const NormGradArgs& a, int parts, cudaStream_t stream) {
+  if (a.cols <= 1024) rmsnorm_q8_grad_single_kernel<IO, 128><<<parts, 128, 0, stream>>>(a);
+  else if (a.cols <= 8192) rmsnorm_q8_grad_single_kernel<IO, 512><<<parts, 512, 0, stream>>>(a);
+  else rmsnorm_q8_grad_single_kernel<IO, 1024><<<parts, 1024, 0, stream>>>(a);
+  return PRM_OK;
 }
 
 bool ld_ok(int64_t ld) { return ld >= 0 && ld <= ((int64_t)1 << 40); }
@@ -362,15 +534,19 @@ extern "C" int prm_rmsnorm_q8(const void* x, int64_t ld_x, const void* residual,
   if (((uintptr_t)x | (uintptr_t)residual | (uintptr_t)(residual ? h_out : nullptr)) % es != 0 ||
       (uintptr_t)weight % (weight_fp32 ? 4 : 2) != 0 || (uintptr_t)scale_out % 4 != 0)
     return PRM_ERR_ALIGN;
-  NormArgs a = {x, residual, weight, h_out, (uint8_t*)q_out, scale_out, rows, ld_x, ld_residual, ld_h, ld_q,
-                (int)cols, weight_fp32, format, eps};
-  const bool vec = cols % 8 == 0 && ld_x % 8 == 0 && ld_q % 8 == 0 && aligned16(x) && aligned16(weight) &&
-                   ((uintptr_t)q_out & 7) == 0 &&
-                   (!residual || (ld_residual % 8 == 0 && ld_h % 8 == 0 && aligned16(residual) && aligned16(h_out)));
+  const NormArgs a = {x,    residual,    weight, h_out, (uint8_t*)q_out, scale_out, rows,
+                      ld_x, ld_residual, ld_h,   ld_q,  (int)cols,       weight_fp32, format, eps};
+  const bool octs = cols % 8 == 0 && cols <= 16384 && ld_x % 8 == 0 && ld_q % 8 == 0 && aligned16(x) &&
+                    aligned16(weight) && ((uintptr_t)q_out & 7) == 0 &&
+                    (!residual || (ld_residual % 8 == 0 && ld_h % 8 == 0 && aligned16(residual) && aligned16(h_out)));
   cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if (io_fp32) run_norm<float>(a, vec, stream);
-  else run_norm<__nv_bfloat16>(a, vec, stream);
-  return cudaGetLastError() == cudaSuccess ? PRM_OK : PRM_ERR_CUDA;
+  int code;
+  if (!octs) code = io_fp32 ? run_norm_single<float>(a, stream) : run_norm_single<__nv_bfloat16>(a, stream);
+  else if (io_fp32)
+    code = weight_fp32 ? run_norm<float, float>(a, stream) : run_norm<float, __nv_bfloat16>(a, stream);
+  else
+    code = weight_fp32 ? run_norm<__nv_bfloat16, float>(a, stream) : run_norm<__nv_bfloat16, __nv_bfloat16>(a, stream);
+  return code != PRM_OK ? code : (cudaGetLastError() == cudaSuccess ? PRM_OK : PRM_ERR_CUDA);
 }
 
 extern "C" size_t prm_rmsnorm_q8_scratch_bytes(int64_t rows, int64_t cols) {
@@ -399,15 +575,20 @@ extern "C" int prm_rmsnorm_q8_backward(const void* grad_y, int64_t ld_grad_y, co
   if (((uintptr_t)grad_y | (uintptr_t)h | (uintptr_t)grad_h | (uintptr_t)grad_x) % es != 0 ||
       (uintptr_t)weight % (weight_fp32 ? 4 : 2) != 0 || ((uintptr_t)scratch & 15) != 0)
     return PRM_ERR_ALIGN;
-  NormGradArgs a = {grad_y, h, weight, grad_h, grad_x, (float*)scratch, rows, ld_grad_y, ld_h, ld_grad_h, ld_grad_x,
-                    (int)cols, weight_fp32, eps};
-  const bool vec = cols % 8 == 0 && ld_grad_y % 8 == 0 && ld_h % 8 == 0 && ld_grad_x % 8 == 0 && aligned16(grad_y) &&
-                   aligned16(h) && aligned16(grad_x) && aligned16(weight) &&
-                   (!grad_h || (ld_grad_h % 8 == 0 && aligned16(grad_h)));
-  const int parts = grad_parts(rows);
-  if (io_fp32) run_grad<float>(a, vec, parts, stream);
-  else run_grad<__nv_bfloat16>(a, vec, parts, stream);
-  rmsnorm_q8_grad_weight_kernel<<<(unsigned)((cols + 31) / 32), 256, 0, stream>>>(a.part, parts, (int)cols,
-                                                                                grad_weight, weight_fp32);
+  const NormGradArgs a = {grad_y, h,    weight,    grad_h,    grad_x,    (float*)scratch, rows,
+                          ld_grad_y, ld_h, ld_grad_h, ld_grad_x, (int)cols, weight_fp32,     eps};
+  const bool octs = cols % 8 == 0 && cols <= 8192 && ld_grad_y % 8 == 0 && ld_h % 8 == 0 && ld_grad_x % 8 == 0 &&
+                    aligned16(grad_y) && aligned16(h) && aligned16(grad_x) && aligned16(weight) &&
+                    (!grad_h || (ld_grad_h % 8 == 0 && aligned16(grad_h)));
+  int parts = grad_parts(rows), code;
+  if (!octs) code = io_fp32 ? run_grad_single<float>(a, parts, stream) : run_grad_single<__nv_bfloat16>(a, parts, stream);
+  else if (io_fp32)
+    code = weight_fp32 ? run_grad<float, float>(a, &parts, stream) : run_grad<float, __nv_bfloat16>(a, &parts, stream);
+  else
+    code = weight_fp32 ? run_grad<__nv_bfloat16, float>(a, &parts, stream)
+                       : run_grad<__nv_bfloat16, __nv_bfloat16>(a, &parts, stream);
+  if (code != PRM_OK) return code;
+  rmsnorm_q8_grad_weight_kernel<<<(unsigned)((cols + 31) / 32), 1024, 0, stream>>>(a.part, parts, (int)cols,
+                                                                                 grad_weight, weight_fp32);
   return cudaGetLastError() == cudaSuccess ? PRM_OK : PRM_ERR_CUDA;
 }

@@ -24,95 +24,98 @@ struct QuantArgs {
   int cols, format;
 };
 
-template <int VEC>
-__device__ __forceinline__ void fold_by_col(const float* f, int c, float (&t)[VEC]) {
+// x * f for one oct (f: eight factors from c on, or null).
+__device__ __forceinline__ void fold_oct(const float* f, int c, float2 (&t)[4]) {
   if (f) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) t[e] = __fmul_rn(t[e], __ldg(f + c + e));
+    for (int e = 0; e < 4; ++e) t[e] = mul2(t[e], make_float2(__ldg(f + c + 2 * e), __ldg(f + c + 2 * e + 1)));
   }
 }
 
 // One row per group of TPR threads, in registers between the maximum and the rounding.
-template <typename IO, int VEC, int NV, int TPR>
+template <typename IO, int NV, int TPR>
 __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_kernel(const QuantArgs a) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
-  __shared__ uint32_t red[64];
-  const int lane = threadIdx.x % TPR;
+  __shared__ float red[64];
+  const int c0 = (threadIdx.x % TPR) * 8;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   if (row >= a.rows) return;
   const IO* x = reinterpret_cast<const IO*>(a.x) + row * a.ld_x;
-  float t[NV][VEC];
-  float none = 0.f;
-  uint32_t top = 0;
+  Oct<IO> xv[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+    if (c0 + v * TPR * 8 < a.cols) xv[v].load_stream(x + c0 + v * TPR * 8);
+  float2 t[NV][4];
+  float none = 0.f, top = 0.f;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = (v * TPR + lane) * VEC;
+    const int c = c0 + v * TPR * 8;
     if (c < a.cols) {
-      load_vec<VEC>(x + c, t[v]);
-      fold_by_col<VEC>(a.fold_cols, c, t[v]);
+      xv[v].get(t[v]);
+      fold_oct(a.fold_cols, c, t[v]);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) top = max(top, abs_bits(t[v][e]));
+      for (int e = 0; e < 4; ++e) top = max_abs(top, t[v][e]);
     }
   }
-  block_sum_max<TPR>(none, top, red);
+  block_sum_top<TPR>(none, top, red);
   const Q8Scale s = q8_scale(top, q8_limit(a.format));
-  uint8_t* q = a.q_rows + row * a.ld_qr;
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c = (v * TPR + lane) * VEC;
-    if (c < a.cols) {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) t[v][e] = s.finite ? __fmul_rn(t[v][e], s.mul) : 0.f;
-      store_codes<VEC>(q + c, t[v], a.format);
-    }
-  }
-  if (lane == 0) a.scale_rows[row] = s.scale;
+  store_octs<NV>(a.q_rows + row * a.ld_qr, t, c0, TPR * 8, a.cols, s, a.format);
+  if (c0 == 0) a.scale_rows[row] = s.scale;
 }
 
-template <typename IO>
-__global__ void __launch_bounds__(1024) quantize_rows_long_kernel(const QuantArgs a) {
-  __shared__ uint32_t red[64];
+// Any alignment, any length: two passes over the row.
+template <typename IO, int THREADS>
+__global__ void __launch_bounds__(THREADS) quantize_rows_single_kernel(const QuantArgs a) {
+  __shared__ float red[64];
   const int64_t row = blockIdx.x;
   const IO* x = reinterpret_cast<const IO*>(a.x) + row * a.ld_x;
-  float none = 0.f;
-  uint32_t top = 0;
-  for (int c = threadIdx.x; c < a.cols; c += 1024) {
-    float t[1] = {to_f32(x[c])};
-    fold_by_col<1>(a.fold_cols, c, t);
-    top = max(top, abs_bits(t[0]));
-  }
-  block_sum_max<1024>(none, top, red);
+  auto value = [&](int c) {
+    const float v = to_f32(x[c]);
+    return a.fold_cols ? __fmul_rn(v, __ldg(a.fold_cols + c)) : v;
+  };
+  float none = 0.f, top = 0.f;
+#pragma unroll 4
+  for (int c = threadIdx.x; c < a.cols; c += THREADS) top = max_abs(top, make_float2(value(c), 0.f));
+  block_sum_top<THREADS>(none, top, red);
   const Q8Scale s = q8_scale(top, q8_limit(a.format));
-  for (int c = threadIdx.x; c < a.cols; c += 1024) {
-    float t[1] = {to_f32(x[c])};
-    fold_by_col<1>(a.fold_cols, c, t);
-    a.q_rows[row * a.ld_qr + c] = q8_pack1(s.finite ? __fmul_rn(t[0], s.mul) : 0.f, a.format);
-  }
+#pragma unroll 4
+  for (int c = threadIdx.x; c < a.cols; c += THREADS)
+    a.q_rows[row * a.ld_qr + c] = code1(s.finite ? __fmul_rn(value(c), s.mul) : 0.f, a.format);
   if (threadIdx.x == 0) a.scale_rows[row] = s.scale;
 }
 
-// Largest magnitude of every column: a block takes 256 * VEC columns of a slab of rows; the integer
-// maximum joins the slabs in any order with the same result.
+// Largest magnitude of every column: a block takes 256 * VEC columns of a slab of rows; the maximum of
+// the bit patterns (NaN above infinity above numbers) joins the slabs in any order alike.
 constexpr int kColThreads = 256;
 template <typename IO, int VEC>
 __global__ void __launch_bounds__(kColThreads) column_top_kernel(const QuantArgs a, int slab) {
   const int c = (blockIdx.x * kColThreads + threadIdx.x) * VEC;
   if (c >= a.cols) return;
   const int64_t r0 = (int64_t)blockIdx.y * slab, r1 = min(a.rows, r0 + slab);
-  uint32_t top[VEC];
+  float top[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) top[e] = 0;
+  for (int e = 0; e < VEC; ++e) top[e] = 0.f;
   const IO* x = reinterpret_cast<const IO*>(a.x) + r0 * a.ld_x + c;
 #pragma unroll 4
   for (int64_t r = r0; r < r1; ++r, x += a.ld_x) {
-    float t[VEC];
-    load_vec<VEC>(x, t);
     const float f = a.fold_rows ? __ldg(a.fold_rows + r) : 1.f;
+    if constexpr (VEC == 8) {
+      Oct<IO> o;
+      float2 t[4];
+      o.load(x);
+      o.get(t);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) top[e] = max(top[e], abs_bits(__fmul_rn(t[e], f)));
+      for (int e = 0; e < 4; ++e) {
+        t[e] = mul2(t[e], make_float2(f, f));
+        top[2 * e] = max_abs(top[2 * e], make_float2(t[e].x, 0.f));
+        top[2 * e + 1] = max_abs(top[2 * e + 1], make_float2(t[e].y, 0.f));
+      }
+    } else {
+      top[0] = max_abs(top[0], make_float2(__fmul_rn(to_f32(*x), f), 0.f));
+    }
   }
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) atomicMax(a.top + c + e, top[e]);
+  for (int e = 0; e < VEC; ++e) atomicMax(a.top + c + e, __float_as_uint(top[e]));
 }
 
 template <typename IO, int VEC>
@@ -120,52 +123,73 @@ __global__ void __launch_bounds__(kColThreads) quantize_cols_kernel(const QuantA
   const int c = (blockIdx.x * kColThreads + threadIdx.x) * VEC;
   if (c >= a.cols) return;
   const int64_t r0 = (int64_t)blockIdx.y * slab, r1 = min(a.rows, r0 + slab);
-  Q8Scale s[VEC];
+  float mul[VEC];
+  bool finite = true;
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) s[e] = q8_scale(a.top[c + e], q8_limit(a.format));
-  if (blockIdx.y == 0) {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) a.scale_cols[c + e] = s[e].scale;
+  for (int e = 0; e < VEC; ++e) {
+    const Q8Scale s = q8_scale(__uint_as_float(a.top[c + e]), q8_limit(a.format));
+    if (blockIdx.y == 0) a.scale_cols[c + e] = s.scale;
+    mul[e] = s.mul;
+    finite = finite && s.finite;
   }
   const IO* x = reinterpret_cast<const IO*>(a.x) + r0 * a.ld_x + c;
   uint8_t* q = a.q_cols + r0 * a.ld_qc + c;
 #pragma unroll 4
   for (int64_t r = r0; r < r1; ++r, x += a.ld_x, q += a.ld_qc) {
-    float t[VEC];
-    load_vec<VEC>(x, t);
     const float f = a.fold_rows ? __ldg(a.fold_rows + r) : 1.f;
+    float v[VEC];
+    if constexpr (VEC == 8) {
+      Oct<IO> o;
+      float2 t[4];
+      o.load(x);
+      o.get(t);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) t[e] = s[e].finite ? __fmul_rn(__fmul_rn(t[e], f), s[e].mul) : 0.f;
-    store_codes<VEC>(q, t, a.format);
+      for (int e = 0; e < 4; ++e) {
+        t[e] = mul2(mul2(t[e], make_float2(f, f)), make_float2(mul[2 * e], mul[2 * e + 1]));
+        v[2 * e] = t[e].x;
+        v[2 * e + 1] = t[e].y;
+      }
+    } else {
+      v[0] = __fmul_rn(__fmul_rn(to_f32(*x), f), mul[0]);
+    }
+    if (!finite) {                        // a column without a scale: its codes are zero
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] = a.top[c + e] < 0x7f800000u ? v[e] : 0.f;
+    }
+    if constexpr (VEC == 8) {
+      const float2 p0 = make_float2(v[0], v[1]), p1 = make_float2(v[2], v[3]), p2 = make_float2(v[4], v[5]),
+                   p3 = make_float2(v[6], v[7]);
+      *reinterpret_cast<uint2*>(q) =
+          a.format == PRM_Q8_INT8 ? make_uint2(codes4<PRM_Q8_INT8>(p0, p1), codes4<PRM_Q8_INT8>(p2, p3))
+                                  : make_uint2(codes4<PRM_Q8_E4M3>(p0, p1), codes4<PRM_Q8_E4M3>(p2, p3));
+    } else {
+      *q = code1(v[0], a.format);
+    }
   }
 }
 
-template <typename IO, int VEC, int NV, int TPR>
+template <typename IO, int NV, int TPR>
 void launch_rows(const QuantArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
-  quantize_rows_kernel<IO, VEC, NV, TPR>
+  quantize_rows_kernel<IO, NV, TPR>
       <<<(unsigned)((a.rows + kRows - 1) / kRows), TPR == 32 ? 256 : TPR, 0, stream>>>(a);
 }
 
 template <typename IO>
-void run_rows(const QuantArgs& a, bool vec, cudaStream_t stream) {
+void run_rows(const QuantArgs& a, bool octs, cudaStream_t stream) {
   const int c = a.cols;
-  if (vec) {
-    if (c <= 256) launch_rows<IO, 8, 1, 32>(a, stream);
-    else if (c <= 512) launch_rows<IO, 8, 2, 32>(a, stream);
-    else if (c <= 1024) launch_rows<IO, 8, 1, 128>(a, stream);
-    else if (c <= 2048) launch_rows<IO, 8, 2, 128>(a, stream);
-    else if (c <= 4096) launch_rows<IO, 8, 2, 256>(a, stream);
-    else if (c <= 8192) launch_rows<IO, 8, 2, 512>(a, stream);
-    else if (c <= 16384) launch_rows<IO, 8, 2, 1024>(a, stream);
-    else if (c <= 32768) launch_rows<IO, 8, 4, 1024>(a, stream);
-    else quantize_rows_long_kernel<IO><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
+  if (octs && c <= 16384) {
+    if (c <= 256) launch_rows<IO, 1, 32>(a, stream);
+    else if (c <= 512) launch_rows<IO, 2, 32>(a, stream);
+    else if (c <= 1024) launch_rows<IO, 1, 128>(a, stream);
+    else if (c <= 2048) launch_rows<IO, 2, 128>(a, stream);
+    else if (c <= 4096) launch_rows<IO, 2, 256>(a, stream);
+    else if (c <= 8192) launch_rows<IO, 2, 512>(a, stream);
+    else launch_rows<IO, 2, 1024>(a, stream);
   } else {
-    if (c <= 256) launch_rows<IO, 1, 8, 32>(a, stream);
-    else if (c <= 2048) launch_rows<IO, 1, 8, 256>(a, stream);
-    else if (c <= 8192) launch_rows<IO, 1, 16, 512>(a, stream);
-    else if (c <= 16384) launch_rows<IO, 1, 16, 1024>(a, stream);
-    else quantize_rows_long_kernel<IO><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
+    if (c <= 1024) quantize_rows_single_kernel<IO, 128><<<(unsigned)a.rows, 128, 0, stream>>>(a);
+    else if (c <= 8192) quantize_rows_single_kernel<IO, 256><<<(unsigned)a.rows, 256, 0, stream>>>(a);
+    else quantize_rows_single_kernel<IO, 1024><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
   }
 }
 

@@ -1,0 +1,202 @@
+// Rows streamed through shared memory by bulk asynchronous copies, for the row operators on large
+// matrices: one persistent CTA per SM, whose warps form groups of W that walk over rows of their
+// own.  A group's ring holds up to kRingStages rows of each of its input matrices; a row is moved to
+// registers, the group's reduction says that every thread has done so, and the group's first
+// thread sends for the row that will take its place.  Bytes in flight are then set by the ring
+// (up to 200 KB per SM), not by how many loads threads hold in registers between barriers.
+//
+// Waits are bounded.  A thread whose wait ran out sets the status word and touches no data any
+// more, but keeps arriving at its group's barriers, so that nobody waits for it.
+#pragma once
+
+#include "async_copy.cuh"
+#include "q8.cuh"
+
+namespace prm {
+
+constexpr int kRingStages = 6;
+constexpr size_t kRingBytes = 200 * 1024;
+
+// Warps of a persistent CTA: a thread holds up to 32 elements of a row of each matrix.
+template <typename IO>
+constexpr int kRingWarps = sizeof(IO) == 2 ? 16 : 8;
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+      ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ uint8_t* ring_memory() {
+  extern __shared__ __align__(128) uint8_t ring_mem[];
+  return ring_mem;
+}
+
+// The static shared memory of a CTA's rings.
+template <typename IO, int W, int ARR>
+struct RingBlock {
+  static constexpr int kGroups = kRingWarps<IO> / W;
+  uint64_t full[kGroups][kRingStages];
+  float red[kGroups][2][32];
+  int abort_word;
+};
+template <typename IO, int W, int ARR>
+__device__ __forceinline__ RingBlock<IO, W, ARR>& ring_block() {
+  __shared__ RingBlock<IO, W, ARR> b;
+  return b;
+}
+
+// One group's ring over ARR matrices of the same number of rows.  The group's row number i (0, 1,
+// ..., n - 1) is row first + i * step.
+template <typename IO, int W, int ARR>
+struct RowRing {
+  RingBlock<IO, W, ARR>& b;
+  const IO* src[ARR];
+  int64_t ld[ARR];
+  int64_t first, step, n;
+  uint8_t* base;          // [stages][ARR][row_bytes]
+  uint32_t row_bytes;
+  int stages, group, stage;
+  uint32_t phase;
+  bool lead, ok;
+  int* status;
+
+  __device__ __forceinline__ RowRing(RingBlock<IO, W, ARR>& block, const void* const* srcs, const int64_t* lds,
+                                     int64_t rows, int cols, int n_stages, int* status_word)
+      : b(block), stages(n_stages), stage(0), phase(0), ok(true), status(status_word) {
+    constexpr int kGroups = kRingWarps<IO> / W;
+    group = threadIdx.x / (W * 32);
+    lead = threadIdx.x % (W * 32) == 0;
+#pragma unroll
+    for (int k = 0; k < ARR; ++k) {
+      src[k] = reinterpret_cast<const IO*>(srcs[k]);
+      ld[k] = lds[k];
+    }
+    row_bytes = (uint32_t)cols * sizeof(IO);
+    base = ring_memory() + (size_t)group * stages * ARR * row_bytes;
+    first = (int64_t)blockIdx.x * kGroups + group;
+    step = (int64_t)gridDim.x * kGroups;
+    n = first < rows ? (rows - first + step - 1) / step : 0;
+  }
+  __device__ __forceinline__ int64_t row(int64_t i) const { return first + i * step; }
+  __device__ __forceinline__ const IO* at(int k) const {
+    return reinterpret_cast<const IO*>(base + ((size_t)stage * ARR + k) * row_bytes);
+  }
+  __device__ __forceinline__ void fetch(int64_t i, int s) const {
+    const int64_t r = row(i);
+    mbar_expect_tx(&b.full[group][s], ARR * row_bytes);
+#pragma unroll
+    for (int k = 0; k < ARR; ++k)
+      bulk_load(base + ((size_t)s * ARR + k) * row_bytes, src[k] + r * ld[k], row_bytes, &b.full[group][s]);
+  }
+  // All threads of the block, once.
+  __device__ __forceinline__ void start() {
+    if (threadIdx.x < (kRingWarps<IO> / W) * kRingStages) mbar_init(&b.full[0][0] + threadIdx.x, 1);
+    if (threadIdx.x == 0) b.abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    if (lead)
+      for (int64_t i = 0; i < n && i < stages; ++i) fetch(i, (int)i);
+  }
+  // The current row has landed.
+  __device__ __forceinline__ bool wait() {
+    ok = ok && mbar_wait(&b.full[group][stage], phase, &b.abort_word, status);
+    return ok;
+  }
+  // Barrier of the group (named barriers 1 .. 8; a group of one warp needs none).
+  __device__ __forceinline__ void sync() const {
+    if constexpr (W == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(W * 32) : "memory");
+  }
+  // After the reduction of row i, which tells that the whole group holds the row in registers: send
+  // for the row that takes its stage, go on to the next stage.
+  __device__ __forceinline__ void next(int64_t i) {
+    if (lead && ok && i + stages < n) fetch(i + stages, stage);
+    if (++stage == stages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  }
+  // Reductions over the group; the words of row i and row i + 1 lie apart.
+  __device__ __forceinline__ void sum2(int64_t i, float& p, float& q) const {
+    p = warp_sum(p);
+    q = warp_sum(q);
+    if constexpr (W > 1) {
+      float* red = b.red[group][i & 1];
+      const int warp = (threadIdx.x >> 5) % W;
+      if ((threadIdx.x & 31) == 0) {
+        red[warp] = p;
+        red[16 + warp] = q;
+      }
+      sync();
+      p = red[0];
+      q = red[16];
+#pragma unroll
+      for (int k = 1; k < W; ++k) {
+        p += red[k];
+        q += red[16 + k];
+      }
+    }
+  }
+  __device__ __forceinline__ void sum_top(int64_t i, float& p, float& top) const {
+    p = warp_sum(p);
+    top = warp_top(top);
+    if constexpr (W > 1) {
+      float* red = b.red[group][i & 1];
+      const int warp = (threadIdx.x >> 5) % W;
+      if ((threadIdx.x & 31) == 0) {
+        red[warp] = p;
+        red[16 + warp] = top;
+      }
+      sync();
+      p = red[0];
+      top = red[16];
+#pragma unroll
+      for (int k = 1; k < W; ++k) {
+        p += red[k];
+        top = max_abs(top, make_float2(red[16 + k], 0.f));
+      }
+    }
+  }
+  // Copies in flight land before the CTA's memory goes (only after a wait that ran out are there any).
+  __device__ __forceinline__ void finish() const {
+    if (!ok && lead) {
+      const uint64_t t0 = global_ns();
+      while (global_ns() - t0 < 1000000ull) {
+      }
+    }
+  }
+};
+
+// ------------------------------------------------------------------ host side
+
+// The status word that prm_q8_status reads, on the current device (null if it has none).
+int* q8_status_word();
+
+// From here on streaming is faster than one row per block.
+constexpr int64_t kRingElements = 1 << 22;
+inline bool ring_worth(int64_t rows, int cols) { return cols >= 512 && cols <= 8192 && rows * cols >= kRingElements; }
+inline int ring_blocks(int64_t rows, int groups) { return (int)std::min<int64_t>(148, (rows + groups - 1) / groups); }
+
+// One CTA per SM; `extra` bytes are what the kernel wants of the ring's memory after the last row.
+template <typename IO, int W, typename K, typename A>
+int launch_ring(K kernel, int arrays, PerDeviceOnce& once, int64_t rows, int cols, size_t extra, cudaStream_t stream,
+                const A& a) {
+  constexpr int kGroups = kRingWarps<IO> / W;
+  int dev;
+  if (once.need(&dev)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes) != cudaSuccess)
+      return PRM_ERR_CUDA;
+    once.mark(dev);
+  }
+  int* status = q8_status_word();
+  const size_t row = (size_t)cols * sizeof(IO) * arrays * kGroups;
+  const int stages = (int)std::min<size_t>(kRingStages, kRingBytes / row);
+  if (!status || stages < 1 || extra > kRingBytes) return PRM_ERR_CUDA;
+  kernel<<<(unsigned)ring_blocks(rows, kGroups), kRingWarps<IO> * 32, std::max(extra, row * stages), stream>>>(a, stages,
+                                                                                                            status);
+  return PRM_OK;
+}
+
+}  // namespace prm

@@ -11,7 +11,9 @@ EPS = 1e-6
 # one row, one column, less than a vector, odd, a warp's, a block's, past each limit of the row kernels
 SHAPES = [(1, 1), (1, 8), (3, 5), (2, 256), (9, 257), (7, 512), (5, 1000), (3, 1024), (4, 1111), (1, 2048),
           (130, 2056), (3, 4096), (2, 4104), (2, 8192), (2, 8193), (1, 16384), (1, 16400), (1, 16401), (1, 32768),
-          (2, 32776), (1, 40001), (1000, 64), (4099, 24), (0, 16)]
+          (2, 32776), (1, 40001), (1000, 64), (4099, 24), (0, 16),
+          # large enough to be streamed: each group width, full and partly filled, rows that do not divide
+          (8201, 512), (4700, 1000), (4099, 1024), (2050, 2056), (2100, 2048), (1030, 4096), (700, 6000), (519, 8192)]
 
 
 def gen(seed):
