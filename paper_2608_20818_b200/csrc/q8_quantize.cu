@@ -6,7 +6,15 @@
 // The folds carry the scales that run along the sum of the product that will read the codes: a
 // product can take out one factor per row of its left operand and per column of its right one, and
 // nothing that varies inside its sums.
-#include "q8.cuh"
+//
+// Three numbers per element (read, two writes at most) make this HBM's work, but a column's scale
+// waits for the whole column.  The streaming kernel reads the matrix once, writes the codes by row on
+// the way and keeps the largest magnitude of every column; after a grid-wide reduction of these it
+// goes over the rows again in the opposite order, the last ones still in shared memory, those before
+// them in L2.
+#include <cooperative_groups.h>
+
+#include "row_ring.cuh"
 
 namespace prm {
 namespace {
@@ -20,8 +28,10 @@ struct QuantArgs {
   float* scale_rows;
   float* scale_cols;
   uint32_t* top;            // [cols] largest magnitude of a column, as bits
+  float* part;              // [blocks][panel] the same of a block's rows
   int64_t rows, ld_x, ld_qr, ld_qc;
   int cols, format;
+  int panel, panels;        // columns that a block of the streaming kernel works on; cols / panel
 };
 
 // x * f for one oct (f: eight factors from c on, or null).
@@ -168,6 +178,202 @@ __global__ void __launch_bounds__(kColThreads) quantize_cols_kernel(const QuantA
   }
 }
 
+// The streaming kernel.  Blocks with the same blockIdx % panels work on the same panel of columns;
+// with codes by row there is one panel, the whole width.  Phase 1: groups of W warps walk over rows.
+// Then the blocks' column maxima are joined (shared memory, scratch, a slice of the columns per block)
+// between two grid-wide barriers of the cooperative launch.  Phase 2 walks back.
+template <typename IO, int W, bool ROWS>
+__global__ void __launch_bounds__(kRingWarps<IO> * 32, 1)
+quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
+  constexpr int kNV = 4, kStep = W * 32 * 8, kThreads = kRingWarps<IO> * 32;
+  RingBlock<IO, W, 1>& b = ring_block<IO, W, 1>();
+  const int pan = blockIdx.x % a.panels, line = blockIdx.x / a.panels;
+  const int lines = ((int)gridDim.x - pan + a.panels - 1) / a.panels;   // blocks of this panel
+  const int cbase = pan * a.panel, cols = min(a.panel, a.cols - cbase);
+  const int c0 = (threadIdx.x % (W * 32)) * 8;
+  const void* const src[1] = {reinterpret_cast<const IO*>(a.x) + cbase};
+  const int64_t ld[1] = {a.ld_x};
+  RowRing<IO, W, 1> ring(b, src, ld, a.rows, cols, stages, status);
+  ring.place(line, lines, a.rows);
+  uint32_t* tops = reinterpret_cast<uint32_t*>(ring_memory() + (size_t)(kRingWarps<IO> / W) * stages * ring.row_bytes);
+  for (int c = threadIdx.x; c < cols; c += kThreads) tops[c] = 0;
+  ring.start();
+  float ct[kNV][8];
+#pragma unroll
+  for (int v = 0; v < kNV; ++v)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ct[v][e] = 0.f;
+  for (int64_t i = 0; i < ring.n; ++i) {
+    const int64_t row = ring.row(i);
+    const float fr = a.fold_rows ? __ldg(a.fold_rows + row) : 1.f;
+    float2 t[kNV][4];
+    float none = 0.f, top = 0.f;
+    if (ring.wait()) {
+#pragma unroll
+      for (int v = 0; v < kNV; ++v) {
+        const int c = c0 + v * kStep;
+        if (c < cols) {
+          Oct<IO> x;
+          x.load(ring.at(0) + c);
+          x.get(t[v]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = mul2(t[v][e], make_float2(fr, fr));
+            ct[v][2 * e] = max_abs(ct[v][2 * e], make_float2(f.x, 0.f));
+            ct[v][2 * e + 1] = max_abs(ct[v][2 * e + 1], make_float2(f.y, 0.f));
+          }
+          if constexpr (ROWS) {
+            fold_oct(a.fold_cols, c, t[v]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max_abs(top, t[v][e]);
+          }
+        }
+      }
+    }
+    if constexpr (ROWS) ring.sum_top(i, none, top);
+    else ring.sync();
+    ring.next(i);
+    if constexpr (ROWS) {
+      if (ring.ok) {
+        const Q8Scale s = q8_scale(top, q8_limit(a.format));
+        store_octs<kNV>(a.q_rows + row * a.ld_qr, t, c0, kStep, cols, s, a.format);
+        if (c0 == 0) a.scale_rows[row] = s.scale;
+      }
+    }
+  }
+  cooperative_groups::grid_group grid = cooperative_groups::this_grid();
+#pragma unroll
+  for (int v = 0; v < kNV; ++v) {
+    const int c = c0 + v * kStep;
+    if (c < cols) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) atomicMax(tops + c + e, __float_as_uint(ct[v][e]));
+    }
+  }
+  __syncthreads();
+  uint32_t* part = reinterpret_cast<uint32_t*>(a.part);
+  for (int c = threadIdx.x; c < cols; c += kThreads) part[(int64_t)blockIdx.x * a.panel + c] = tops[c];
+  grid.sync();
+  // this block's slice of the panel's columns: 32 at a time, the lines dealt out to the warps
+  const int per = ((cols + lines - 1) / lines + 31) / 32 * 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int s0 = line * per; s0 < min(cols, (line + 1) * per); s0 += 32) {
+    const int c = s0 + lane;
+    __syncthreads();
+    if (threadIdx.x < 32) tops[threadIdx.x] = 0;
+    __syncthreads();
+    uint32_t m = 0;
+    if (c < cols) {
+#pragma unroll 4
+      for (int l = warp; l < lines; l += kThreads / 32)
+        m = max(m, __ldcg(part + (int64_t)(l * a.panels + pan) * a.panel + c));
+      atomicMax(tops + lane, m);
+    }
+    __syncthreads();
+    if (threadIdx.x < 32 && c < cols) {
+      a.top[cbase + c] = tops[lane];
+      a.scale_cols[cbase + c] = q8_scale(__uint_as_float(tops[lane]), q8_limit(a.format)).scale;
+    }
+  }
+  grid.sync();
+  float2 mul[kNV][4];
+  uint32_t odd = 0;                     // octs that hold a column without a number for a scale
+#pragma unroll
+  for (int v = 0; v < kNV; ++v) {
+    const int c = c0 + v * kStep;
+    if (c < cols) {
+      float m[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const Q8Scale s = q8_scale(__uint_as_float(__ldcg(a.top + cbase + c + e)), q8_limit(a.format));
+        m[e] = s.mul;
+        if (!s.finite) odd |= 1u << v;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mul[v][e] = make_float2(m[2 * e], m[2 * e + 1]);
+    }
+  }
+  ring.turn_back();
+  for (int64_t i = ring.n - 1; i >= 0; --i) {
+    const int64_t row = ring.row(i);
+    const float fr = a.fold_rows ? __ldg(a.fold_rows + row) : 1.f;
+    Oct<IO> x[kNV];
+    if (ring.wait_back(i)) {
+#pragma unroll
+      for (int v = 0; v < kNV; ++v)
+        if (c0 + v * kStep < cols) x[v].load(ring.at(0) + c0 + v * kStep);
+    }
+    ring.sync();
+    ring.next_back(i);
+    if (!ring.ok) continue;
+    uint8_t* q = a.q_cols + row * a.ld_qc + cbase;
+#pragma unroll
+    for (int v = 0; v < kNV; ++v) {
+      const int c = c0 + v * kStep;
+      if (c < cols) {
+        float2 t[4];
+        x[v].get(t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = mul2(mul2(t[e], make_float2(fr, fr)), mul[v][e]);
+        if (odd & (1u << v)) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (__ldcg(a.top + cbase + c + 2 * e) >= 0x7f800000u) t[e].x = 0.f;
+            if (__ldcg(a.top + cbase + c + 2 * e + 1) >= 0x7f800000u) t[e].y = 0.f;
+          }
+        }
+        *reinterpret_cast<uint2*>(q + c) =
+            a.format == PRM_Q8_INT8
+                ? make_uint2(codes4<PRM_Q8_INT8>(t[0], t[1]), codes4<PRM_Q8_INT8>(t[2], t[3]))
+                : make_uint2(codes4<PRM_Q8_E4M3>(t[0], t[1]), codes4<PRM_Q8_E4M3>(t[2], t[3]));
+      }
+    }
+  }
+  ring.finish();
+}
+
+template <typename IO, int W, bool ROWS>
+int launch_stream(const QuantArgs& a, cudaStream_t stream) {
+  constexpr int kGroups = kRingWarps<IO> / W;
+  static PerDeviceOnce once;
+  int dev;
+  if (once.need(&dev)) {
+    if (cudaFuncSetAttribute(quantize_stream_kernel<IO, W, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)kRingBytes) != cudaSuccess)
+      return PRM_ERR_CUDA;
+    once.mark(dev);
+  }
+  int* status = q8_status_word();
+  const size_t row = (size_t)a.panel * sizeof(IO) * kGroups, tops = (size_t)a.panel * 4;
+  int stages = (int)std::min<size_t>(kRingStages, (kRingBytes - tops) / row);
+  if (!status || stages < 1) return PRM_ERR_CUDA;
+  // as many blocks as there are groups' worth of rows, a whole number of them for each panel
+  const int per_panel = std::min<int64_t>(kRingBlocks / a.panels, (a.rows + kGroups - 1) / kGroups);
+  QuantArgs arg = a;
+  void* args[3] = {&arg, &stages, &status};
+  return cudaLaunchCooperativeKernel(quantize_stream_kernel<IO, W, ROWS>, dim3((unsigned)(per_panel * a.panels)),
+                                     dim3(kRingWarps<IO> * 32), args, row * stages + tops, stream) == cudaSuccess
+             ? PRM_OK
+             : PRM_ERR_CUDA;
+}
+
+// Widest row that one group holds with codes by row.
+template <typename IO>
+constexpr int kWidest = kRingWarps<IO> * 32 * 32;
+
+template <typename IO, bool ROWS>
+int run_stream(QuantArgs a, cudaStream_t stream) {
+  a.panels = ROWS ? 1 : (a.cols + 8191) / 8192;
+  a.panel = (a.cols + 8 * a.panels - 1) / (8 * a.panels) * 8;
+  if (a.panel <= 1024) return launch_stream<IO, 1, ROWS>(a, stream);
+  if (a.panel <= 2048) return launch_stream<IO, 2, ROWS>(a, stream);
+  if (a.panel <= 4096) return launch_stream<IO, 4, ROWS>(a, stream);
+  if constexpr (sizeof(IO) == 2) {
+    if (a.panel > 8192) return launch_stream<IO, 16, ROWS>(a, stream);
+  }
+  return launch_stream<IO, 8, ROWS>(a, stream);
+}
+
 template <typename IO, int NV, int TPR>
 void launch_rows(const QuantArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
@@ -212,7 +418,8 @@ using namespace prm;
 
 extern "C" size_t prm_quantize_q8_scratch_bytes(int64_t rows, int64_t cols) {
   if (rows < 1 || cols < 1) return 0;
-  return (size_t)cols * 4;
+  // the columns' maxima, and those of every block's rows
+  return ((size_t)std::min<int64_t>(rows, kRingBlocks) + 1) * ((size_t)cols + 256) * 4;
 }
 
 extern "C" int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_t cols, int io_fp32, int format,
@@ -238,21 +445,32 @@ extern "C" int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_
   if ((uintptr_t)x % (io_fp32 ? 4 : 2) != 0) return PRM_ERR_ALIGN;
   if (q_cols && (!scratch || scratch_bytes < prm_quantize_q8_scratch_bytes(rows, cols))) return PRM_ERR_WORKSPACE;
   QuantArgs a = {x, fold_rows, fold_cols, (uint8_t*)q_rows, (uint8_t*)q_cols, scale_rows, scale_cols,
-                 (uint32_t*)scratch, rows, ld_x, ld_q_rows, ld_q_cols, (int)cols, format};
-  const bool vec_x = cols % 8 == 0 && ld_x % 8 == 0 && aligned16(x);
+                 (uint32_t*)scratch, (float*)scratch + (cols + 7) / 8 * 8, rows, ld_x, ld_q_rows, ld_q_cols, (int)cols, format};
+  const bool octs_x = cols % 8 == 0 && ld_x % 8 == 0 && aligned16(x);
+  const bool octs_r = octs_x && ld_q_rows % 8 == 0 && ((uintptr_t)q_rows & 7) == 0;
+  const bool octs_c = octs_x && ld_q_cols % 8 == 0 && ((uintptr_t)q_cols & 7) == 0;
+  // Codes by column of an aligned matrix: one launch, with the codes by row in the same pass where a
+  // row fits a group's registers.
+  if (q_cols && octs_c && cols >= 256 && cols <= 32 * 8192) {
+    const bool joint = q_rows && octs_r && cols <= (io_fp32 ? kWidest<float> : kWidest<__nv_bfloat16>);
+    int code;
+    if (joint) code = io_fp32 ? run_stream<float, true>(a, stream) : run_stream<__nv_bfloat16, true>(a, stream);
+    else code = io_fp32 ? run_stream<float, false>(a, stream) : run_stream<__nv_bfloat16, false>(a, stream);
+    if (code != PRM_OK) return code;
+    if (joint) q_rows = nullptr;
+    q_cols = nullptr;
+  }
   if (q_rows) {
-    const bool vec = vec_x && ld_q_rows % 8 == 0 && ((uintptr_t)q_rows & 7) == 0;
-    if (io_fp32) run_rows<float>(a, vec, stream);
-    else run_rows<__nv_bfloat16>(a, vec, stream);
+    if (io_fp32) run_rows<float>(a, octs_r, stream);
+    else run_rows<__nv_bfloat16>(a, octs_r, stream);
   }
   if (q_cols) {
-    const bool vec = vec_x && ld_q_cols % 8 == 0 && ((uintptr_t)q_cols & 7) == 0;
     if (cudaMemsetAsync(scratch, 0, (size_t)cols * 4, stream) != cudaSuccess) return PRM_ERR_CUDA;
     if (io_fp32) {
-      if (vec) run_cols<float, 8>(a, stream);
+      if (octs_c) run_cols<float, 8>(a, stream);
       else run_cols<float, 1>(a, stream);
     } else {
-      if (vec) run_cols<__nv_bfloat16, 8>(a, stream);
+      if (octs_c) run_cols<__nv_bfloat16, 8>(a, stream);
       else run_cols<__nv_bfloat16, 1>(a, stream);
     }
   }

@@ -78,6 +78,13 @@ struct RowRing {
     step = (int64_t)gridDim.x * kGroups;
     n = first < rows ? (rows - first + step - 1) / step : 0;
   }
+  // The rows of a block that is number `line` of `lines`, where that is not blockIdx.x of gridDim.x.
+  __device__ __forceinline__ void place(int line, int lines, int64_t rows) {
+    constexpr int kGroups = kRingWarps<IO> / W;
+    first = (int64_t)line * kGroups + group;
+    step = (int64_t)lines * kGroups;
+    n = first < rows ? (rows - first + step - 1) / step : 0;
+  }
   __device__ __forceinline__ int64_t row(int64_t i) const { return first + i * step; }
   __device__ __forceinline__ const IO* at(int k) const {
     return reinterpret_cast<const IO*>(base + ((size_t)stage * ARR + k) * row_bytes);
@@ -117,6 +124,22 @@ struct RowRing {
       stage = 0;
       phase ^= 1;
     }
+  }
+  // A second walk over the same rows, last row first.  The last `stages` rows are still in the ring;
+  // the others are sent for again as their stages fall free.  wait_back(i) / next_back(i) go with
+  // i = n - 1, ..., 0.
+  __device__ __forceinline__ void turn_back() { stage = n > 0 ? (int)((n - 1) % stages) : 0; }
+  __device__ __forceinline__ bool wait_back(int64_t i) {
+    if (i < n - stages) {
+      // copies into this stage on the way out, and those since
+      const int64_t copies = (n - 1 - stage) / stages + 1 + (n - 1 - i) / stages;
+      ok = ok && mbar_wait(&b.full[group][stage], (uint32_t)(copies - 1) & 1u, &b.abort_word, status);
+    }
+    return ok;
+  }
+  __device__ __forceinline__ void next_back(int64_t i) {
+    if (lead && ok && i >= stages) fetch(i - stages, stage);
+    stage = stage == 0 ? stages - 1 : stage - 1;
   }
   // Reductions over the group; the words of row i and row i + 1 lie apart.
   __device__ __forceinline__ void sum2(int64_t i, float& p, float& q) const {
@@ -174,10 +197,12 @@ struct RowRing {
 // The status word that prm_q8_status reads, on the current device (null if it has none).
 int* q8_status_word();
 
+constexpr int kRingBlocks = 148;     // one CTA per SM
+
 // From here on streaming is faster than one row per block.
 constexpr int64_t kRingElements = 1 << 22;
 inline bool ring_worth(int64_t rows, int cols) { return cols >= 512 && cols <= 8192 && rows * cols >= kRingElements; }
-inline int ring_blocks(int64_t rows, int groups) { return (int)std::min<int64_t>(148, (rows + groups - 1) / groups); }
+inline int ring_blocks(int64_t rows, int groups) { return (int)std::min<int64_t>(kRingBlocks, (rows + groups - 1) / groups); }
 
 // One CTA per SM; `extra` bytes are what the kernel wants of the ring's memory after the last row.
 template <typename IO, int W, typename K, typename A>

@@ -89,7 +89,7 @@ def test_norm_gradient_formula_against_differences():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows,cols", [s for s in SHAPES if s[0]])
+@pytest.mark.parametrize("rows,cols", [s for s in SHAPES if s[0]] + [(300, 16384), (5, 24584), (2, 24584), (700, 40968)])
 @pytest.mark.parametrize("io", ["bf16", "fp32"])
 def test_quantize(rows, cols, io):
     g = gen(rows * 7 + cols)
