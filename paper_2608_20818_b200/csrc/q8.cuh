@@ -22,22 +22,17 @@ constexpr float kQ8Tiny = 0x1p-100f;
 __host__ __device__ inline bool q8_format_ok(int format) { return format == PRM_Q8_INT8 || format == PRM_Q8_E4M3; }
 __host__ __device__ inline float q8_limit(int format) { return format == PRM_Q8_INT8 ? kLimitInt8 : kLimitE4m3; }
 
-// What a set of values with the largest magnitude `top` is multiplied by, and the scale that undoes
-// it.  The factor is limit * (1 / top), each step rounded, which is how array libraries evaluate a
-// number over an array: codes then agree bit for bit with `(t * (limit / top)).round()` written
-// there.  A set that holds an infinity or a NaN (which maxima here keep) gets the scale NaN and zero
-// codes, so it marks its own row (column) of whatever is computed from it and no other.
-struct Q8Scale {
-  float mul, scale;
-  bool finite;
-};
-__device__ __forceinline__ Q8Scale q8_scale(float top, float limit) {
-  Q8Scale s;
-  s.finite = top < __uint_as_float(0x7f800000u);
-  const bool live = s.finite && top >= kQ8Tiny;
-  s.mul = live ? __fmul_rn(limit, __frcp_rn(top)) : 0.f;
-  s.scale = live ? __fdiv_rn(top, limit) : (s.finite ? 0.f : __uint_as_float(0x7fc00000u));
-  return s;
+// A set of values with the largest magnitude `top` is multiplied by q8_mul and marked with q8_scale,
+// which undoes it.  The factor is limit * (1 / top), each step rounded, which is how array libraries
+// evaluate a number over an array, so that codes agree with `round(t * (limit / top))` written there.
+// A set that holds an infinity or a NaN (which maxima here keep) gets the scale NaN and zero codes: it
+// marks its own row (column) of whatever is computed from it and no other.
+__device__ __forceinline__ bool q8_finite(float top) { return top < __uint_as_float(0x7f800000u); }
+__device__ __forceinline__ float q8_mul(float top, float limit) {
+  return top >= kQ8Tiny && q8_finite(top) ? __fmul_rn(limit, __frcp_rn(top)) : 0.f;
+}
+__device__ __forceinline__ float q8_scale(float top, float limit) {
+  return !q8_finite(top) ? __uint_as_float(0x7fc00000u) : top >= kQ8Tiny ? __fdiv_rn(top, limit) : 0.f;
 }
 
 // ------------------------------------------------------------- eight elements at a time
@@ -125,47 +120,54 @@ template <> struct Oct<float> {
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
 };
 
-// Four values, already multiplied, to four codes (first value in the lowest byte).
+// Four codes of t * mul (first value in the lowest byte).
 template <int FORMAT>
-__device__ __forceinline__ uint32_t codes4(float2 a, float2 b) {
+__device__ __forceinline__ uint32_t codes4(float2 a, float2 b, float2 mul) {
   if constexpr (FORMAT == PRM_Q8_INT8) {
-    // |v| <= 127: adding 1.5 * 2^23 leaves the value rounded to nearest-even in the low bits.
+    // |t * mul| <= 127: adding 1.5 * 2^23 leaves it rounded to nearest-even in the low bits, and as one
+    // fused product it is rounded once.
     const float2 m = make_float2(12582912.f, 12582912.f);
-    a = add2(a, m);
-    b = add2(b, m);
+    a = fma2(a, mul, m);
+    b = fma2(b, mul, m);
     return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
                        __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
   } else {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(a, __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(b, __NV_SATFINITE, __NV_E4M3);
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(mul2(a, mul), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(mul2(b, mul), __NV_SATFINITE, __NV_E4M3);
     return lo | (hi << 16);
   }
 }
-// Eight codes of t * mul.
-template <int FORMAT>
-__device__ __forceinline__ uint2 codes8(const float2 (&t)[4], float2 mul) {
-  return make_uint2(codes4<FORMAT>(mul2(t[0], mul), mul2(t[1], mul)), codes4<FORMAT>(mul2(t[2], mul), mul2(t[3], mul)));
-}
-__device__ __forceinline__ uint8_t code1(float v, int format) {
-  const float2 p = make_float2(v, 0.f), z = make_float2(0.f, 0.f);
-  return (uint8_t)((format == PRM_Q8_INT8 ? codes4<PRM_Q8_INT8>(p, z) : codes4<PRM_Q8_E4M3>(p, z)) & 0xffu);
+__device__ __forceinline__ uint8_t code1(float v, float mul, int format) {
+  const float2 p = make_float2(v, 0.f), f = make_float2(mul, mul);
+  return (uint8_t)((format == PRM_Q8_INT8 ? codes4<PRM_Q8_INT8>(p, p, f) : codes4<PRM_Q8_E4M3>(p, p, f)) & 0xffu);
 }
 // The codes of NV octs of a thread, `stride` elements apart, below `cols`; zeros where the row has no
 // number for a scale.
+template <int NV, int FORMAT>
+__device__ __forceinline__ void store_octs_as(uint8_t* q, const float2 (&t)[NV][4], int c0, int stride, int cols,
+                                              float top) {
+  const float f = q8_mul(top, q8_limit(FORMAT));
+  const float2 mul = make_float2(f, f);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = c0 + v * stride;
+    if (c < cols)
+      *reinterpret_cast<uint2*>(q + c) =
+          make_uint2(codes4<FORMAT>(t[v][0], t[v][1], mul), codes4<FORMAT>(t[v][2], t[v][3], mul));
+  }
+}
 template <int NV>
 __device__ __forceinline__ void store_octs(uint8_t* q, const float2 (&t)[NV][4], int c0, int stride, int cols,
-                                           const Q8Scale& s, int format) {
-  const float2 mul = make_float2(s.mul, s.mul);
-  auto each = [&](auto code) {
+                                           float top, int format) {
+  if (!q8_finite(top)) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = c0 + v * stride;
-      if (c < cols) *reinterpret_cast<uint2*>(q + c) = code(t[v]);
-    }
-  };
-  if (!s.finite) each([](const float2 (&)[4]) { return make_uint2(0u, 0u); });
-  else if (format == PRM_Q8_INT8) each([&](const float2 (&x)[4]) { return codes8<PRM_Q8_INT8>(x, mul); });
-  else each([&](const float2 (&x)[4]) { return codes8<PRM_Q8_E4M3>(x, mul); });
+    for (int v = 0; v < NV; ++v)
+      if (c0 + v * stride < cols) *reinterpret_cast<uint2*>(q + c0 + v * stride) = make_uint2(0u, 0u);
+  } else if (format == PRM_Q8_INT8) {
+    store_octs_as<NV, PRM_Q8_INT8>(q, t, c0, stride, cols, top);
+  } else {
+    store_octs_as<NV, PRM_Q8_E4M3>(q, t, c0, stride, cols, top);
+  }
 }
 
 __device__ __forceinline__ float load1(const void* p, int fp32, int64_t i) {

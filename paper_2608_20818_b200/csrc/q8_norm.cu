@@ -90,9 +90,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const
   }
   float sum = sum2.x + sum2.y;
   block_sum_top<TPR>(sum, top, red);
-  const Q8Scale s = q8_scale(top, q8_limit(a.format));
-  store_octs<NV>(a.q + row * a.ld_q, t, c0, TPR * 8, a.cols, s, a.format);
-  if (c0 == 0) a.scale[row] = s.scale * inv_rms(sum, a.cols, a.eps);
+  store_octs<NV>(a.q + row * a.ld_q, t, c0, TPR * 8, a.cols, top, a.format);
+  if (c0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
 }
 
 // Large matrices: rows streamed through a ring, a group of W warps each.
@@ -139,9 +138,8 @@ rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
     ring.sum_top(i, sum, top);
     ring.next(i);
     if (ring.ok) {
-      const Q8Scale s = q8_scale(top, q8_limit(a.format));
-      store_octs<kNV>(a.q + row * a.ld_q, t, c0, kStep, a.cols, s, a.format);
-      if (c0 == 0) a.scale[row] = s.scale * inv_rms(sum, a.cols, a.eps);
+      store_octs<kNV>(a.q + row * a.ld_q, t, c0, kStep, a.cols, top, a.format);
+      if (c0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
     }
   }
   ring.finish();
@@ -167,15 +165,16 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_q8_single_kernel(const NormAr
     top = max_abs(top, make_float2(__fmul_rn(v, load1(a.weight, a.weight_fp32, c)), 0.f));
   }
   block_sum_top<THREADS>(sum, top, red);
-  const Q8Scale s = q8_scale(top, q8_limit(a.format));
+  const bool finite = q8_finite(top);
+  const float mul = q8_mul(top, q8_limit(a.format));
   const IO* src = r ? h : x;
   uint8_t* q = a.q + row * a.ld_q;
 #pragma unroll 4
   for (int c = threadIdx.x; c < a.cols; c += THREADS) {      // each thread reads what it wrote itself
     const float t = __fmul_rn(to_f32(src[c]), load1(a.weight, a.weight_fp32, c));
-    q[c] = code1(s.finite ? __fmul_rn(t, s.mul) : 0.f, a.format);
+    q[c] = finite ? code1(t, mul, a.format) : 0;
   }
-  if (threadIdx.x == 0) a.scale[row] = s.scale * inv_rms(sum, a.cols, a.eps);
+  if (threadIdx.x == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
 }
 
 template <typename IO, typename WT, int NV, int TPR>

@@ -68,9 +68,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_kernel(co
     }
   }
   block_sum_top<TPR>(none, top, red);
-  const Q8Scale s = q8_scale(top, q8_limit(a.format));
-  store_octs<NV>(a.q_rows + row * a.ld_qr, t, c0, TPR * 8, a.cols, s, a.format);
-  if (c0 == 0) a.scale_rows[row] = s.scale;
+  store_octs<NV>(a.q_rows + row * a.ld_qr, t, c0, TPR * 8, a.cols, top, a.format);
+  if (c0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
 }
 
 // Any alignment, any length: two passes over the row.
@@ -87,11 +86,12 @@ __global__ void __launch_bounds__(THREADS) quantize_rows_single_kernel(const Qua
 #pragma unroll 4
   for (int c = threadIdx.x; c < a.cols; c += THREADS) top = max_abs(top, make_float2(value(c), 0.f));
   block_sum_top<THREADS>(none, top, red);
-  const Q8Scale s = q8_scale(top, q8_limit(a.format));
+  const bool finite = q8_finite(top);
+  const float mul = q8_mul(top, q8_limit(a.format));
 #pragma unroll 4
   for (int c = threadIdx.x; c < a.cols; c += THREADS)
-    a.q_rows[row * a.ld_qr + c] = code1(s.finite ? __fmul_rn(value(c), s.mul) : 0.f, a.format);
-  if (threadIdx.x == 0) a.scale_rows[row] = s.scale;
+    a.q_rows[row * a.ld_qr + c] = finite ? code1(value(c), mul, a.format) : 0;
+  if (threadIdx.x == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
 }
 
 // Largest magnitude of every column: a block takes 256 * VEC columns of a slab of rows; the maximum of
@@ -128,6 +128,27 @@ __global__ void __launch_bounds__(kColThreads) column_top_kernel(const QuantArgs
   for (int e = 0; e < VEC; ++e) atomicMax(a.top + c + e, __float_as_uint(top[e]));
 }
 
+// Eight codes, a factor for each.
+template <int FORMAT>
+__device__ __forceinline__ uint2 column_codes(const float2 (&t)[4], const float2 (&mul)[4]) {
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float2 a = t[2 * k], b = t[2 * k + 1], f = mul[2 * k], g = mul[2 * k + 1];
+    if constexpr (FORMAT == PRM_Q8_INT8) {
+      const float2 m = make_float2(12582912.f, 12582912.f);
+      const float2 x = fma2(a, f, m), y = fma2(b, g, m);
+      w[k] = __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040),
+                         __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
+    } else {
+      const uint32_t lo = __nv_cvt_float2_to_fp8x2(mul2(a, f), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t hi = __nv_cvt_float2_to_fp8x2(mul2(b, g), __NV_SATFINITE, __NV_E4M3);
+      w[k] = lo | (hi << 16);
+    }
+  }
+  return make_uint2(w[0], w[1]);
+}
+
 template <typename IO, int VEC>
 __global__ void __launch_bounds__(kColThreads) quantize_cols_kernel(const QuantArgs a, int slab) {
   const int c = (blockIdx.x * kColThreads + threadIdx.x) * VEC;
@@ -137,43 +158,62 @@ __global__ void __launch_bounds__(kColThreads) quantize_cols_kernel(const QuantA
   bool finite = true;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    const Q8Scale s = q8_scale(__uint_as_float(a.top[c + e]), q8_limit(a.format));
-    if (blockIdx.y == 0) a.scale_cols[c + e] = s.scale;
-    mul[e] = s.mul;
-    finite = finite && s.finite;
+    const float top = __uint_as_float(a.top[c + e]);
+    if (blockIdx.y == 0) a.scale_cols[c + e] = q8_scale(top, q8_limit(a.format));
+    mul[e] = q8_mul(top, q8_limit(a.format));
+    finite = finite && q8_finite(top);
   }
   const IO* x = reinterpret_cast<const IO*>(a.x) + r0 * a.ld_x + c;
   uint8_t* q = a.q_cols + r0 * a.ld_qc + c;
 #pragma unroll 4
   for (int64_t r = r0; r < r1; ++r, x += a.ld_x, q += a.ld_qc) {
     const float f = a.fold_rows ? __ldg(a.fold_rows + r) : 1.f;
-    float v[VEC];
     if constexpr (VEC == 8) {
       Oct<IO> o;
-      float2 t[4];
+      float2 t[4], m[4];
       o.load(x);
       o.get(t);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        t[e] = mul2(mul2(t[e], make_float2(f, f)), make_float2(mul[2 * e], mul[2 * e + 1]));
-        v[2 * e] = t[e].x;
-        v[2 * e + 1] = t[e].y;
+        t[e] = mul2(t[e], make_float2(f, f));
+        m[e] = make_float2(mul[2 * e], mul[2 * e + 1]);
+        if (!finite) {
+          if (!q8_finite(__uint_as_float(a.top[c + 2 * e]))) t[e].x = 0.f;
+          if (!q8_finite(__uint_as_float(a.top[c + 2 * e + 1]))) t[e].y = 0.f;
+        }
       }
+      *reinterpret_cast<uint2*>(q) = a.format == PRM_Q8_INT8 ? column_codes<PRM_Q8_INT8>(t, m)
+                                                             : column_codes<PRM_Q8_E4M3>(t, m);
     } else {
-      v[0] = __fmul_rn(__fmul_rn(to_f32(*x), f), mul[0]);
+      *q = finite ? code1(__fmul_rn(to_f32(*x), f), mul[0], a.format) : 0;
     }
-    if (!finite) {                        // a column without a scale: its codes are zero
+  }
+}
+
+// A thread's share of one row of codes by column.
+template <typename IO, int NV, int FORMAT>
+__device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], const float2 (&mul)[NV][4], float fr,
+                                         uint32_t odd, int c0, int step, int cols) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) v[e] = a.top[c + e] < 0x7f800000u ? v[e] : 0.f;
-    }
-    if constexpr (VEC == 8) {
-      const float2 p0 = make_float2(v[0], v[1]), p1 = make_float2(v[2], v[3]), p2 = make_float2(v[4], v[5]),
-                   p3 = make_float2(v[6], v[7]);
-      *reinterpret_cast<uint2*>(q) =
-          a.format == PRM_Q8_INT8 ? make_uint2(codes4<PRM_Q8_INT8>(p0, p1), codes4<PRM_Q8_INT8>(p2, p3))
-                                  : make_uint2(codes4<PRM_Q8_E4M3>(p0, p1), codes4<PRM_Q8_E4M3>(p2, p3));
-    } else {
-      *q = code1(v[0], a.format);
+  for (int v = 0; v < NV; ++v) {
+    const int c = c0 + v * step;
+    if (c < cols) {
+      float2 t[4];
+      x[v].get(t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = mul2(t[e], make_float2(fr, fr));
+      if (odd == 0) {
+        *reinterpret_cast<uint2*>(q + c) = column_codes<FORMAT>(t, mul[v]);
+      } else {
+        float2 m[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          m[e] = mul[v][e];
+          if (isnan(m[e].x)) t[e].x = m[e].x = 0.f;
+          if (isnan(m[e].y)) t[e].y = m[e].y = 0.f;
+        }
+        *reinterpret_cast<uint2*>(q + c) = column_codes<FORMAT>(t, m);
+      }
     }
   }
 }
@@ -195,8 +235,8 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
   const int64_t ld[1] = {a.ld_x};
   RowRing<IO, W, 1> ring(b, src, ld, a.rows, cols, stages, status);
   ring.place(line, lines, a.rows);
-  uint32_t* tops = reinterpret_cast<uint32_t*>(ring_memory() + (size_t)(kRingWarps<IO> / W) * stages * ring.row_bytes);
-  for (int c = threadIdx.x; c < cols; c += kThreads) tops[c] = 0;
+  __shared__ float slice[kThreads / 32][32];
+  float* tops = reinterpret_cast<float*>(ring_memory() + (size_t)(kRingWarps<IO> / W) * stages * ring.row_bytes);
   ring.start();
   float ct[kNV][8];
 #pragma unroll
@@ -235,64 +275,85 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
     ring.next(i);
     if constexpr (ROWS) {
       if (ring.ok) {
-        const Q8Scale s = q8_scale(top, q8_limit(a.format));
-        store_octs<kNV>(a.q_rows + row * a.ld_qr, t, c0, kStep, cols, s, a.format);
-        if (c0 == 0) a.scale_rows[row] = s.scale;
+        store_octs<kNV>(a.q_rows + row * a.ld_qr, t, c0, kStep, cols, top, a.format);
+        if (c0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
       }
     }
   }
   cooperative_groups::grid_group grid = cooperative_groups::this_grid();
+  for (int g = 0; g < kRingWarps<IO> / W; ++g) {      // the groups take turns
+    if (ring.group == g) {
 #pragma unroll
-  for (int v = 0; v < kNV; ++v) {
-    const int c = c0 + v * kStep;
-    if (c < cols) {
+      for (int v = 0; v < kNV; ++v) {
+        const int c = c0 + v * kStep;
+        if (c < cols) {
+          Oct<float> o;
+          if (g > 0) {
+            float2 m[4];
+            o.load(tops + c);
+            o.get(m);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) atomicMax(tops + c + e, __float_as_uint(ct[v][e]));
+            for (int e = 0; e < 4; ++e) {
+              ct[v][2 * e] = max_abs(ct[v][2 * e], make_float2(m[e].x, 0.f));
+              ct[v][2 * e + 1] = max_abs(ct[v][2 * e + 1], make_float2(m[e].y, 0.f));
+            }
+          }
+          o.a = make_float4(ct[v][0], ct[v][1], ct[v][2], ct[v][3]);
+          o.b = make_float4(ct[v][4], ct[v][5], ct[v][6], ct[v][7]);
+          o.store(tops + c);
+        }
+      }
     }
+    __syncthreads();
   }
-  __syncthreads();
-  uint32_t* part = reinterpret_cast<uint32_t*>(a.part);
-  for (int c = threadIdx.x; c < cols; c += kThreads) part[(int64_t)blockIdx.x * a.panel + c] = tops[c];
+  for (int c = threadIdx.x; c < cols; c += kThreads) a.part[(int64_t)blockIdx.x * a.panel + c] = tops[c];
   grid.sync();
   // this block's slice of the panel's columns: 32 at a time, the lines dealt out to the warps
   const int per = ((cols + lines - 1) / lines + 31) / 32 * 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int s0 = line * per; s0 < min(cols, (line + 1) * per); s0 += 32) {
     const int c = s0 + lane;
-    __syncthreads();
-    if (threadIdx.x < 32) tops[threadIdx.x] = 0;
-    __syncthreads();
-    uint32_t m = 0;
+    float m = 0.f;
     if (c < cols) {
 #pragma unroll 4
       for (int l = warp; l < lines; l += kThreads / 32)
-        m = max(m, __ldcg(part + (int64_t)(l * a.panels + pan) * a.panel + c));
-      atomicMax(tops + lane, m);
+        m = max_abs(m, make_float2(__ldcg(a.part + (int64_t)(l * a.panels + pan) * a.panel + c), 0.f));
+    }
+    slice[warp][lane] = m;
+    __syncthreads();
+    if (warp == 0 && c < cols) {
+#pragma unroll
+      for (int k = 1; k < kThreads / 32; ++k) m = max_abs(m, make_float2(slice[k][lane], 0.f));
+      // a column without a number for a scale passes on a NaN, and gets zero codes
+      reinterpret_cast<float*>(a.top)[cbase + c] = q8_finite(m) ? q8_mul(m, q8_limit(a.format)) : m - m;
+      a.scale_cols[cbase + c] = q8_scale(m, q8_limit(a.format));
     }
     __syncthreads();
-    if (threadIdx.x < 32 && c < cols) {
-      a.top[cbase + c] = tops[lane];
-      a.scale_cols[cbase + c] = q8_scale(__uint_as_float(tops[lane]), q8_limit(a.format)).scale;
-    }
   }
   grid.sync();
+  // All factors of this thread's columns are fetched before the first is used, in 16-byte pieces: one
+  // load after the other from lines that every SM wants at once took 15 us.
   float2 mul[kNV][4];
-  uint32_t odd = 0;                     // octs that hold a column without a number for a scale
 #pragma unroll
   for (int v = 0; v < kNV; ++v) {
     const int c = c0 + v * kStep;
     if (c < cols) {
-      float m[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const Q8Scale s = q8_scale(__uint_as_float(__ldcg(a.top + cbase + c + e)), q8_limit(a.format));
-        m[e] = s.mul;
-        if (!s.finite) odd |= 1u << v;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) mul[v][e] = make_float2(m[2 * e], m[2 * e + 1]);
+      const float4 p = __ldcg(reinterpret_cast<const float4*>(a.top + cbase + c));
+      const float4 q = __ldcg(reinterpret_cast<const float4*>(a.top + cbase + c + 4));
+      mul[v][0] = make_float2(p.x, p.y);
+      mul[v][1] = make_float2(p.z, p.w);
+      mul[v][2] = make_float2(q.x, q.y);
+      mul[v][3] = make_float2(q.z, q.w);
     }
   }
+  uint32_t odd = 0;                       // octs that hold a column without a number for a scale
+#pragma unroll
+  for (int v = 0; v < kNV; ++v)
+    if (c0 + v * kStep < cols) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (isnan(mul[v][e].x) || isnan(mul[v][e].y)) odd |= 1u << v;
+    }
   ring.turn_back();
   for (int64_t i = ring.n - 1; i >= 0; --i) {
     const int64_t row = ring.row(i);
@@ -307,27 +368,8 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
     ring.next_back(i);
     if (!ring.ok) continue;
     uint8_t* q = a.q_cols + row * a.ld_qc + cbase;
-#pragma unroll
-    for (int v = 0; v < kNV; ++v) {
-      const int c = c0 + v * kStep;
-      if (c < cols) {
-        float2 t[4];
-        x[v].get(t);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = mul2(mul2(t[e], make_float2(fr, fr)), mul[v][e]);
-        if (odd & (1u << v)) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (__ldcg(a.top + cbase + c + 2 * e) >= 0x7f800000u) t[e].x = 0.f;
-            if (__ldcg(a.top + cbase + c + 2 * e + 1) >= 0x7f800000u) t[e].y = 0.f;
-          }
-        }
-        *reinterpret_cast<uint2*>(q + c) =
-            a.format == PRM_Q8_INT8
-                ? make_uint2(codes4<PRM_Q8_INT8>(t[0], t[1]), codes4<PRM_Q8_INT8>(t[2], t[3]))
-                : make_uint2(codes4<PRM_Q8_E4M3>(t[0], t[1]), codes4<PRM_Q8_E4M3>(t[2], t[3]));
-      }
-    }
+    if (a.format == PRM_Q8_INT8) back_row<IO, kNV, PRM_Q8_INT8>(q, x, mul, fr, odd, c0, kStep, cols);
+    else back_row<IO, kNV, PRM_Q8_E4M3>(q, x, mul, fr, odd, c0, kStep, cols);
   }
   ring.finish();
 }

@@ -37,7 +37,7 @@ template <typename IO, int W, int ARR>
 struct RingBlock {
   static constexpr int kGroups = kRingWarps<IO> / W;
   uint64_t full[kGroups][kRingStages];
-  float red[kGroups][2][32];
+  alignas(16) float red[kGroups][2][32];
   int abort_word;
 };
 template <typename IO, int W, int ARR>
@@ -141,7 +141,23 @@ struct RowRing {
     if (lead && ok && i >= stages) fetch(i - stages, stage);
     stage = stage == 0 ? stages - 1 : stage - 1;
   }
-  // Reductions over the group; the words of row i and row i + 1 lie apart.
+  // Reductions over the group; the words of row i and row i + 1 lie apart and are read in pieces.
+  static constexpr int kPiece = W >= 4 ? 4 : 2;
+  struct Words {
+    float v[kPiece];
+    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+  };
+  static __device__ __forceinline__ Words words(const float* p) {
+    Words w;
+    if constexpr (kPiece == 4) {
+      const float4 f = *reinterpret_cast<const float4*>(p);
+      w.v[0] = f.x; w.v[1] = f.y; w.v[2] = f.z; w.v[3] = f.w;
+    } else {
+      const float2 f = *reinterpret_cast<const float2*>(p);
+      w.v[0] = f.x; w.v[1] = f.y;
+    }
+    return w;
+  }
   __device__ __forceinline__ void sum2(int64_t i, float& p, float& q) const {
     p = warp_sum(p);
     q = warp_sum(q);
@@ -153,12 +169,15 @@ struct RowRing {
         red[16 + warp] = q;
       }
       sync();
-      p = red[0];
-      q = red[16];
+      p = q = 0.f;
 #pragma unroll
-      for (int k = 1; k < W; ++k) {
-        p += red[k];
-        q += red[16 + k];
+      for (int k = 0; k < W; k += kPiece) {
+        const auto u = words(red + k), v = words(red + 16 + k);
+#pragma unroll
+        for (int e = 0; e < kPiece; ++e) {
+          p += u[e];
+          q += v[e];
+        }
       }
     }
   }
@@ -173,12 +192,15 @@ struct RowRing {
         red[16 + warp] = top;
       }
       sync();
-      p = red[0];
-      top = red[16];
+      p = top = 0.f;
 #pragma unroll
-      for (int k = 1; k < W; ++k) {
-        p += red[k];
-        top = max_abs(top, make_float2(red[16 + k], 0.f));
+      for (int k = 0; k < W; k += kPiece) {
+        const auto u = words(red + k), v = words(red + 16 + k);
+#pragma unroll
+        for (int e = 0; e < kPiece; e += 2) {
+          p += u[e] + u[e + 1];
+          top = max_abs(top, make_float2(v[e], v[e + 1]));
+        }
       }
     }
   }
