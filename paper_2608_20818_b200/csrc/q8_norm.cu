@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const
 
 // Large matrices: rows streamed through a ring, a group of W warps each.
 template <typename IO, typename WT, int W, bool RES>
-__global__ void __launch_bounds__(kRingWarps<IO> * 32, 1)
+__global__ void __launch_bounds__(kRingThreads<IO>, 1)
 rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
   constexpr int kArr = RES ? 2 : 1, kNV = 4, kStep = W * 32 * 8;
   RingBlock<IO, W, kArr>& b = ring_block<IO, W, kArr>();
@@ -109,40 +109,39 @@ rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
   for (int v = 0; v < kNV; ++v)
     if (c0 + v * kStep < a.cols) wv[v].load(reinterpret_cast<const WT*>(a.weight) + c0 + v * kStep);
   ring.start();
+  if (ring.producer) {
+    ring.serve();
+    ring.finish();
+    return;
+  }
   for (int64_t i = 0; i < ring.n; ++i) {
     const int64_t row = ring.row(i);
     float2 t[kNV][4], sum2 = make_float2(0.f, 0.f);
     float top = 0.f;
     if (ring.wait()) {
       IO* h = RES ? reinterpret_cast<IO*>(a.h) + row * a.ld_h : nullptr;
-      Oct<IO> xv[kNV], rv[kNV];
 #pragma unroll
       for (int v = 0; v < kNV; ++v) {
         const int c = c0 + v * kStep;
         if (c < a.cols) {
-          xv[v].load(ring.at(0) + c);
-          if constexpr (RES) rv[v].load(ring.at(1) + c);
-        }
-      }
-#pragma unroll
-      for (int v = 0; v < kNV; ++v) {
-        const int c = c0 + v * kStep;
-        if (c < a.cols) {
+          Oct<IO> x, r;
           float2 w[4];
+          x.load(ring.at(0) + c);
+          if constexpr (RES) r.load(ring.at(1) + c);
           wv[v].get(w);
-          norm_oct<IO, RES>(xv[v], rv[v], w, h + c, t[v], sum2, top);
+          norm_oct<IO, RES>(x, r, w, h + c, t[v], sum2, top);
         }
       }
     }
+    ring.release();
+    ring.advance();
     float sum = sum2.x + sum2.y;
     ring.sum_top(i, sum, top);
-    ring.next(i);
     if (ring.ok) {
       store_octs<kNV>(a.q + row * a.ld_q, t, c0, kStep, a.cols, top, a.format);
       if (c0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
     }
   }
-  ring.finish();
 }
 
 // Any alignment, any length: two passes over the row, the second of which finds it in cache.
@@ -236,6 +235,12 @@ struct NormGradArgs {
   float eps;
 };
 
+template <typename T>
+__device__ __forceinline__ void load_oct(const T* p, float2 (&v)[4]) {
+  Oct<T> o;
+  o.load(p);
+  o.get(v);
+}
 // The two sums of a row over one oct.
 __device__ __forceinline__ void grad_sums(const float2 (&gy)[4], const float2 (&h)[4], const float2 (&w)[4],
                                           float2& ss, float2& gh) {
@@ -338,10 +343,11 @@ __global__ void __launch_bounds__(TPR) rmsnorm_q8_grad_kernel(const NormGradArgs
   }
 }
 
-// Large matrices: rows streamed through a ring.  The groups' shares of grad_w meet in the ring's
+// Large matrices: rows streamed through a ring and read from it twice (held in registers between the
+// sums and the outputs they would spill).  The groups' shares of grad_w meet in the ring's
 // memory at the end, so that a block leaves one line of partial sums.
 template <typename IO, typename WT, int W, bool GH>
-__global__ void __launch_bounds__(kRingWarps<IO> * 32, 1)
+__global__ void __launch_bounds__(kRingThreads<IO>, 1)
 rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
   constexpr int kArr = GH ? 3 : 2, kNV = 4, kStep = W * 32 * 8, kGroups = kRingWarps<IO> / W;
   RingBlock<IO, W, kArr>& b = ring_block<IO, W, kArr>();
@@ -355,9 +361,10 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) gw[v][e] = make_float2(0.f, 0.f);
   ring.start();
-  for (int64_t i = 0; i < ring.n; ++i) {
+  if (ring.producer) ring.serve();
+  const int64_t n = ring.producer ? 0 : ring.n;
+  for (int64_t i = 0; i < n; ++i) {
     const int64_t row = ring.row(i);
-    Oct<IO> gyv[kNV], hv[kNV], ghv[kNV];
     float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
     if (ring.wait()) {
 #pragma unroll
@@ -365,21 +372,15 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
         const int c = c0 + v * kStep;
         if (c < a.cols) {
           float2 gy[4], h[4], w[4];
-          Oct<WT> wv;
-          wv.load(reinterpret_cast<const WT*>(a.weight) + c);
-          gyv[v].load(ring.at(0) + c);
-          hv[v].load(ring.at(1) + c);
-          if constexpr (GH) ghv[v].load(ring.at(2) + c);
-          gyv[v].get(gy);
-          hv[v].get(h);
-          wv.get(w);
+          load_oct(reinterpret_cast<const WT*>(a.weight) + c, w);
+          load_oct(ring.at(0) + c, gy);
+          load_oct(ring.at(1) + c, h);
           grad_sums(gy, h, w, ss2, gh2);
         }
       }
     }
     float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
     ring.sum2(i, ss, gh);
-    ring.next(i);
     if (ring.ok) {
       const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
       IO* gxp = reinterpret_cast<IO*>(a.gx) + row * a.ld_gx;
@@ -388,15 +389,17 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
         const int c = c0 + v * kStep;
         if (c < a.cols) {
           float2 gy[4], h[4], w[4];
-          Oct<WT> wv;
-          wv.load(reinterpret_cast<const WT*>(a.weight) + c);
-          gyv[v].get(gy);
-          hv[v].get(h);
-          wv.get(w);
-          grad_oct<IO>(gy, h, w, GH ? &ghv[v] : nullptr, s, k, gxp + c, gw[v]);
+          Oct<IO> add;
+          load_oct(reinterpret_cast<const WT*>(a.weight) + c, w);
+          load_oct(ring.at(0) + c, gy);
+          load_oct(ring.at(1) + c, h);
+          if constexpr (GH) add.load(ring.at(2) + c);
+          grad_oct<IO>(gy, h, w, GH ? &add : nullptr, s, k, gxp + c, gw[v]);
         }
       }
     }
+    ring.release();
+    ring.advance();
   }
   ring.finish();
   __syncthreads();                        // every group's copies have been consumed
@@ -404,14 +407,14 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
 #pragma unroll
   for (int v = 0; v < kNV; ++v) {
     const int c = c0 + v * kStep;
-    if (c < a.cols) {
+    if (!ring.producer && c < a.cols) {
       Oct<float> o;
       o.set(gw[v]);
       o.store(sums + (size_t)ring.group * a.cols + c);
     }
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < a.cols; c += kRingWarps<IO> * 32) {
+  for (int c = threadIdx.x; c < a.cols; c += kRingThreads<IO>) {
     float sum = 0.f;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) sum += sums[(size_t)g * a.cols + c];

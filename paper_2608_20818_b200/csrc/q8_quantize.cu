@@ -223,9 +223,9 @@ __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], con
 // Then the blocks' column maxima are joined (shared memory, scratch, a slice of the columns per block)
 // between two grid-wide barriers of the cooperative launch.  Phase 2 walks back.
 template <typename IO, int W, bool ROWS>
-__global__ void __launch_bounds__(kRingWarps<IO> * 32, 1)
+__global__ void __launch_bounds__(kRingThreads<IO>, 1)
 quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
-  constexpr int kNV = 4, kStep = W * 32 * 8, kThreads = kRingWarps<IO> * 32;
+  constexpr int kNV = 4, kStep = W * 32 * 8, kThreads = kRingThreads<IO>;
   RingBlock<IO, W, 1>& b = ring_block<IO, W, 1>();
   const int pan = blockIdx.x % a.panels, line = blockIdx.x / a.panels;
   const int lines = ((int)gridDim.x - pan + a.panels - 1) / a.panels;   // blocks of this panel
@@ -243,7 +243,9 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
   for (int v = 0; v < kNV; ++v)
 #pragma unroll
     for (int e = 0; e < 8; ++e) ct[v][e] = 0.f;
-  for (int64_t i = 0; i < ring.n; ++i) {
+  const int64_t n = ring.producer ? 0 : ring.n;
+  if (ring.producer) ring.serve();
+  for (int64_t i = 0; i < n; ++i) {
     const int64_t row = ring.row(i);
     const float fr = a.fold_rows ? __ldg(a.fold_rows + row) : 1.f;
     float2 t[kNV][4];
@@ -270,10 +272,10 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
         }
       }
     }
-    if constexpr (ROWS) ring.sum_top(i, none, top);
-    else ring.sync();
-    ring.next(i);
+    ring.release();
+    ring.advance();
     if constexpr (ROWS) {
+      ring.sum_top(i, none, top);
       if (ring.ok) {
         store_octs<kNV>(a.q_rows + row * a.ld_qr, t, c0, kStep, cols, top, a.format);
         if (c0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
@@ -282,7 +284,7 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
   }
   cooperative_groups::grid_group grid = cooperative_groups::this_grid();
   for (int g = 0; g < kRingWarps<IO> / W; ++g) {      // the groups take turns
-    if (ring.group == g) {
+    if (!ring.producer && ring.group == g) {
 #pragma unroll
       for (int v = 0; v < kNV; ++v) {
         const int c = c0 + v * kStep;
@@ -355,7 +357,8 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
         if (isnan(mul[v][e].x) || isnan(mul[v][e].y)) odd |= 1u << v;
     }
   ring.turn_back();
-  for (int64_t i = ring.n - 1; i >= 0; --i) {
+  if (ring.producer) ring.serve_back();
+  for (int64_t i = n - 1; i >= 0; --i) {
     const int64_t row = ring.row(i);
     const float fr = a.fold_rows ? __ldg(a.fold_rows + row) : 1.f;
     Oct<IO> x[kNV];
@@ -364,8 +367,8 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
       for (int v = 0; v < kNV; ++v)
         if (c0 + v * kStep < cols) x[v].load(ring.at(0) + c0 + v * kStep);
     }
-    ring.sync();
-    ring.next_back(i);
+    ring.release();
+    ring.retreat();
     if (!ring.ok) continue;
     uint8_t* q = a.q_cols + row * a.ld_qc + cbase;
     if (a.format == PRM_Q8_INT8) back_row<IO, kNV, PRM_Q8_INT8>(q, x, mul, fr, odd, c0, kStep, cols);
@@ -394,7 +397,7 @@ int launch_stream(const QuantArgs& a, cudaStream_t stream) {
   QuantArgs arg = a;
   void* args[3] = {&arg, &stages, &status};
   return cudaLaunchCooperativeKernel(quantize_stream_kernel<IO, W, ROWS>, dim3((unsigned)(per_panel * a.panels)),
-                                     dim3(kRingWarps<IO> * 32), args, row * stages + tops, stream) == cudaSuccess
+                                     dim3(kRingThreads<IO>), args, row * stages + tops, stream) == cudaSuccess
              ? PRM_OK
              : PRM_ERR_CUDA;
 }

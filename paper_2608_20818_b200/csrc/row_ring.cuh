@@ -1,9 +1,10 @@
 // Rows streamed through shared memory by bulk asynchronous copies, for the row operators on large
 // matrices: one persistent CTA per SM, whose warps form groups of W that walk over rows of their
-// own.  A group's ring holds up to kRingStages rows of each of its input matrices; a row is moved to
-// registers, the group's reduction says that every thread has done so, and the group's first
-// thread sends for the row that will take its place.  Bytes in flight are then set by the ring
-// (up to 200 KB per SM), not by how many loads threads hold in registers between barriers.
+// own.  A group's ring holds up to kRingStages rows of each of its input matrices.  A warp that
+// is done with its part of a row says so on the stage's barrier; one more warp, a lane per group,
+// sends for the row that takes the stage when all warps of the group have.  Bytes in flight are then
+// set by the ring (up to 200 KB per SM), not by how many loads threads hold in registers between
+// barriers.  (With a thread of the group sending, each row cost its group about 500 cycles more.)
 //
 // Waits are bounded.  A thread whose wait ran out sets the status word and touches no data any
 // more, but keeps arriving at its group's barriers, so that nobody waits for it.
@@ -17,9 +18,11 @@ namespace prm {
 constexpr int kRingStages = 6;
 constexpr size_t kRingBytes = 200 * 1024;
 
-// Warps of a persistent CTA: a thread holds up to 32 elements of a row of each matrix.
+// Warps of a persistent CTA that work on rows: a thread holds up to 32 elements of a row of each matrix.
 template <typename IO>
 constexpr int kRingWarps = sizeof(IO) == 2 ? 16 : 8;
+template <typename IO>
+constexpr int kRingThreads = kRingWarps<IO> * 32 + 32;
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile(
@@ -36,7 +39,8 @@ __device__ __forceinline__ uint8_t* ring_memory() {
 template <typename IO, int W, int ARR>
 struct RingBlock {
   static constexpr int kGroups = kRingWarps<IO> / W;
-  uint64_t full[kGroups][kRingStages];
+  uint64_t full[kGroups][kRingStages];    // the copies of a row have landed
+  uint64_t empty[kGroups][kRingStages];   // W warps are done with the row
   alignas(16) float red[kGroups][2][32];
   int abort_word;
 };
@@ -58,15 +62,15 @@ struct RowRing {
   uint32_t row_bytes;
   int stages, group, stage;
   uint32_t phase;
-  bool lead, ok;
+  bool producer, ok;
   int* status;
 
   __device__ __forceinline__ RowRing(RingBlock<IO, W, ARR>& block, const void* const* srcs, const int64_t* lds,
                                      int64_t rows, int cols, int n_stages, int* status_word)
       : b(block), stages(n_stages), stage(0), phase(0), ok(true), status(status_word) {
     constexpr int kGroups = kRingWarps<IO> / W;
-    group = threadIdx.x / (W * 32);
-    lead = threadIdx.x % (W * 32) == 0;
+    producer = threadIdx.x >= kRingWarps<IO> * 32;
+    group = producer ? threadIdx.x - kRingWarps<IO> * 32 : threadIdx.x / (W * 32);   // a lane per group
 #pragma unroll
     for (int k = 0; k < ARR; ++k) {
       src[k] = reinterpret_cast<const IO*>(srcs[k]);
@@ -74,16 +78,14 @@ struct RowRing {
     }
     row_bytes = (uint32_t)cols * sizeof(IO);
     base = ring_memory() + (size_t)group * stages * ARR * row_bytes;
-    first = (int64_t)blockIdx.x * kGroups + group;
-    step = (int64_t)gridDim.x * kGroups;
-    n = first < rows ? (rows - first + step - 1) / step : 0;
+    place(blockIdx.x, gridDim.x, rows);
   }
-  // The rows of a block that is number `line` of `lines`, where that is not blockIdx.x of gridDim.x.
+  // The rows of a block that is number `line` of `lines`.
   __device__ __forceinline__ void place(int line, int lines, int64_t rows) {
     constexpr int kGroups = kRingWarps<IO> / W;
     first = (int64_t)line * kGroups + group;
     step = (int64_t)lines * kGroups;
-    n = first < rows ? (rows - first + step - 1) / step : 0;
+    n = group < kGroups && first < rows ? (rows - first + step - 1) / step : 0;
   }
   __device__ __forceinline__ int64_t row(int64_t i) const { return first + i * step; }
   __device__ __forceinline__ const IO* at(int k) const {
@@ -98,48 +100,93 @@ struct RowRing {
   }
   // All threads of the block, once.
   __device__ __forceinline__ void start() {
-    if (threadIdx.x < (kRingWarps<IO> / W) * kRingStages) mbar_init(&b.full[0][0] + threadIdx.x, 1);
+    constexpr int kBars = (kRingWarps<IO> / W) * kRingStages;
+    if (threadIdx.x < kBars) {
+      mbar_init(&b.full[0][0] + threadIdx.x, 1);
+      mbar_init(&b.empty[0][0] + threadIdx.x, W);
+    }
     if (threadIdx.x == 0) b.abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
-    if (lead)
-      for (int64_t i = 0; i < n && i < stages; ++i) fetch(i, (int)i);
+  }
+  // The producer's lanes, each for its group: rows 0 .. n - 1.  No lane waits for another's row.
+  __device__ __forceinline__ void serve() {
+    int64_t i = 0;
+    uint64_t t0 = global_ns();
+    while (__any_sync(0xffffffffu, ok && i < n)) {
+      if (ok && i < n) {
+        const bool room = i < stages || mbar_try_wait(&b.empty[group][stage], phase ^ 1);
+        if (room) {
+          fetch(i, stage);
+          ++i;
+          advance();
+          t0 = global_ns();
+        } else {
+          gave_up(t0);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void advance() {
+    if (++stage == stages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  }
+  __device__ __forceinline__ void gave_up(uint64_t t0) {
+    if (*(volatile int*)&b.abort_word) ok = false;
+    if (global_ns() - t0 > kWaitLimitNs) {
+      ok = false;
+      *(volatile int*)&b.abort_word = 1;
+      atomicOr(status, kStatusTimeout);
+    }
   }
   // The current row has landed.
   __device__ __forceinline__ bool wait() {
     ok = ok && mbar_wait(&b.full[group][stage], phase, &b.abort_word, status);
     return ok;
   }
+  // This warp is done with the current row.
+  __device__ __forceinline__ void release() const {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0 && ok) mbar_arrive(&b.empty[group][stage]);
+  }
   // Barrier of the group (named barriers 1 .. 8; a group of one warp needs none).
   __device__ __forceinline__ void sync() const {
     if constexpr (W == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(W * 32) : "memory");
   }
-  // After the reduction of row i, which tells that the whole group holds the row in registers: send
-  // for the row that takes its stage, go on to the next stage.
-  __device__ __forceinline__ void next(int64_t i) {
-    if (lead && ok && i + stages < n) fetch(i + stages, stage);
-    if (++stage == stages) {
-      stage = 0;
-      phase ^= 1;
-    }
-  }
   // A second walk over the same rows, last row first.  The last `stages` rows are still in the ring;
-  // the others are sent for again as their stages fall free.  wait_back(i) / next_back(i) go with
-  // i = n - 1, ..., 0.
+  // the others are sent for again as their stages fall free.  Between the two walks lies a barrier of
+  // the block.  wait_back(i) / release() / retreat() go with i = n - 1, ..., 0.
   __device__ __forceinline__ void turn_back() { stage = n > 0 ? (int)((n - 1) % stages) : 0; }
+  // Copies into (and releases of) the current stage on the way out.
+  __device__ __forceinline__ int64_t outward() const { return (n - 1 - stage) / stages + 1; }
   __device__ __forceinline__ bool wait_back(int64_t i) {
     if (i < n - stages) {
-      // copies into this stage on the way out, and those since
-      const int64_t copies = (n - 1 - stage) / stages + 1 + (n - 1 - i) / stages;
+      const int64_t copies = outward() + (n - 1 - i) / stages;
       ok = ok && mbar_wait(&b.full[group][stage], (uint32_t)(copies - 1) & 1u, &b.abort_word, status);
     }
     return ok;
   }
-  __device__ __forceinline__ void next_back(int64_t i) {
-    if (lead && ok && i >= stages) fetch(i - stages, stage);
-    stage = stage == 0 ? stages - 1 : stage - 1;
+  __device__ __forceinline__ void retreat() { stage = stage == 0 ? stages - 1 : stage - 1; }
+  __device__ __forceinline__ void serve_back() {
+    int64_t i = n - 1 - stages;             // row i takes the stage of row i + stages
+    uint64_t t0 = global_ns();
+    while (__any_sync(0xffffffffu, ok && i >= 0)) {
+      if (ok && i >= 0) {
+        const int64_t releases = outward() + (n - 1 - i) / stages;
+        if (mbar_try_wait(&b.empty[group][stage], (uint32_t)(releases - 1) & 1u)) {
+          fetch(i, stage);
+          --i;
+          retreat();
+          t0 = global_ns();
+        } else {
+          gave_up(t0);
+        }
+      }
+    }
   }
   // Reductions over the group; the words of row i and row i + 1 lie apart and are read in pieces.
   static constexpr int kPiece = W >= 4 ? 4 : 2;
@@ -206,7 +253,7 @@ struct RowRing {
   }
   // Copies in flight land before the CTA's memory goes (only after a wait that ran out are there any).
   __device__ __forceinline__ void finish() const {
-    if (!ok && lead) {
+    if (*(volatile int*)&b.abort_word && producer) {
       const uint64_t t0 = global_ns();
       while (global_ns() - t0 < 1000000ull) {
       }
@@ -241,7 +288,7 @@ int launch_ring(K kernel, int arrays, PerDeviceOnce& once, int64_t rows, int col
   const size_t row = (size_t)cols * sizeof(IO) * arrays * kGroups;
   const int stages = (int)std::min<size_t>(kRingStages, kRingBytes / row);
   if (!status || stages < 1 || extra > kRingBytes) return PRM_ERR_CUDA;
-  kernel<<<(unsigned)ring_blocks(rows, kGroups), kRingWarps<IO> * 32, std::max(extra, row * stages), stream>>>(a, stages,
+  kernel<<<(unsigned)ring_blocks(rows, kGroups), kRingThreads<IO>, std::max(extra, row * stages), stream>>>(a, stages,
                                                                                                             status);
   return PRM_OK;
 }
