@@ -14,10 +14,12 @@
 //
 //   warp 0      TMA producer: boxes of 128 bytes x 128 rows, 128-byte swizzle, no multicast
 //   warp 1      tcgen05.mma issuer, owner of the tensor memory
-//   warps 2..5  epilogue
+//   warps 2..9  epilogue: two warps per lane quadrant, every other set of 16 rows m each
 //
 // Every barrier wait is bounded; one that runs out sets the status word that prm_q8_status reads,
 // the CTA drains its copies and leaves.
+#include <type_traits>
+
 #include "q8_matmul.cuh"
 
 namespace prm {
@@ -27,7 +29,7 @@ __device__ int g_q8_status;
 
 constexpr int kTileN = 128;            // output columns per CTA (lanes of the accumulator)
 constexpr int kMaxStages = 10;
-constexpr int kThreads = 192;
+constexpr int kThreads = 320;
 constexpr uint32_t kBytesP = kTileN * kBlockK;
 constexpr int kMaxSplit = 8;           // portable cluster size
 
@@ -59,6 +61,20 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
   const int kb0 = (int)((int64_t)a.c.kblocks * rank / a.split), kb1 = (int)((int64_t)a.c.kblocks * (rank + 1) / a.split);
   const uint32_t tmem_cols = a.tile_m < 32 ? 32u : (uint32_t)a.tile_m;
 
+  auto load = [&](int kb, int s) {               // k-block kb into stage s
+    uint8_t* sp = smem + (size_t)s * a.stage_bytes;
+    uint8_t* sq = sp + kBytesP;
+    mbar_expect_tx(&full[s], a.stage_bytes);
+    const int k0 = kb * kBlockK;
+    if (P_MN) tma_load_2d(sp, &map_p, &full[s], n0, k0);
+    else tma_load_2d(sp, &map_p, &full[s], k0, n0);
+    if (Q_MN) {
+      tma_load_2d(sq, &map_q, &full[s], m0, k0);
+      if (a.tile_m > 128) tma_load_2d(sq + 128 * kBlockK, &map_q, &full[s], m0 + 128, k0);
+    } else {
+      tma_load_2d(sq, &map_q, &full[s], k0, m0);
+    }
+  };
   if (threadIdx.x == 0) {
     for (int s = 0; s < a.stages; ++s) {
       mbar_init(&full[s], 1);
@@ -68,6 +84,9 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    grid_wait();
+    // the first copies need nobody else
+    for (int it = 0; it < a.stages && kb0 + it < kb1; ++it) load(kb0 + it, it);
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)),
@@ -76,28 +95,20 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tcgen05_before_sync();
+  __syncwarp();
   __syncthreads();
   tcgen05_after_sync();
   const uint32_t tmem = tmem_slot;
+  grid_wait();
+  grid_trigger();                              // not before the tensor memory is this kernel's
 
   if (warp == 0) {
     if (lane == 0) {
-      int it = 0;
-      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+      int it = min(a.stages, kb1 - kb0);
+      for (; kb0 + it < kb1; ++it) {
         const int s = it % a.stages;
         if (!mbar_wait(&empty[s], ((it / a.stages) & 1) ^ 1, abort_flag, a.c.status)) break;
-        uint8_t* sp = smem + (size_t)s * a.stage_bytes;
-        uint8_t* sq = sp + kBytesP;
-        mbar_expect_tx(&full[s], a.stage_bytes);
-        const int k0 = kb * kBlockK;
-        if (P_MN) tma_load_2d(sp, &map_p, &full[s], n0, k0);
-        else tma_load_2d(sp, &map_p, &full[s], k0, n0);
-        if (Q_MN) {
-          tma_load_2d(sq, &map_q, &full[s], m0, k0);
-          if (a.tile_m > 128) tma_load_2d(sq + 128 * kBlockK, &map_q, &full[s], m0 + 128, k0);
-        } else {
-          tma_load_2d(sq, &map_q, &full[s], k0, m0);
-        }
+        load(kb0 + it, s);
       }
       if (*abort_flag) {                 // copies in flight must land before the CTA leaves
         for (int j = it > a.stages ? it - a.stages : 0; j < it; ++j) {
@@ -134,82 +145,98 @@ matmul_q8_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constan
     ok = __all_sync(0xffffffffu, ok);
     tcgen05_after_sync();
   }
-  const int quad = warp & 3;
+  const int quad = warp & 3, half = (warp - 2) >> 2;
   const int col = quad * 32 + lane;            // this thread's output column in the tile
   const int n = n0 + col;
   const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
   const int m_here = min(a.tile_m, a.c.m - m0);
   const float sb = warp >= 2 && a.c.scale_b && n < a.c.n ? __ldg(a.c.scale_b + n) : 1.f;
-  auto put = [&](int t, float v, float sa) {   // row t of this tile
-    const int64_t at = (int64_t)(m0 + t) * a.c.ld_out + n;
-    v = v * sa * sb;
-    if (a.c.out_fp32) reinterpret_cast<float*>(a.c.out)[at] = v;
-    else reinterpret_cast<__nv_bfloat16*>(a.c.out)[at] = __float2bfloat16_rn(v);
-  };
-  // The scale of row t, one per lane and handed round by shuffles: a load per row would serialise
-  // on its latency.
-  auto row_scale = [&](int t) {
+  // The scales of 16 rows from t on, one per lane and handed round by shuffles: a load per row would
+  // serialise on its latency.
+  auto row_scales = [&](int t) {
+    t += lane & 15;
     return a.c.scale_a && t < m_here ? __ldg(a.c.scale_a + m0 + t) : 1.f;
   };
+  // Rows t .. t + rows - 1 of the tile; `ints`: integer sums.
+  auto store = [&](auto ints, int t, const uint32_t (&r)[16], float sa, int rows) {
+    const int64_t at = (int64_t)(m0 + t) * a.c.ld_out + n;
+    float* out_f = reinterpret_cast<float*>(a.c.out) + at;
+    __nv_bfloat16* out_h = reinterpret_cast<__nv_bfloat16*>(a.c.out) + at;
+    if (a.c.out_fp32) store_column<decltype(ints)::value, 16>(out_f, a.c.ld_out, r, sa, sb, rows, n < a.c.n);
+    else store_column<decltype(ints)::value, 16>(out_h, a.c.ld_out, r, sa, sb, rows, n < a.c.n);
+  };
+  using Sums = std::integral_constant<bool, INT8>;
   if (a.split == 1) {
     if (warp >= 2 && ok) {
-      for (int t0 = 0; t0 < m_here; t0 += 16) {
+      for (int t = half * 16; t < m_here; t += 32) {
         uint32_t r[16];
-        tmem_ld16(trow + t0, r);
-        const float sa = row_scale(t0 + (lane & 15));
+        tmem_ld16(trow + t, r);
+        const float sa = row_scales(t);
         tmem_wait_ld();
-        const int64_t at = (int64_t)(m0 + t0) * a.c.ld_out + n;
-        if (a.c.out_fp32)
-          store_column<INT8, 16>(reinterpret_cast<float*>(a.c.out) + at, a.c.ld_out, r, sa, sb, m_here - t0, n < a.c.n);
-        else
-          store_column<INT8, 16>(reinterpret_cast<__nv_bfloat16*>(a.c.out) + at, a.c.ld_out, r, sa, sb, m_here - t0,
-                                 n < a.c.n);
+        store(Sums(), t, r, sa, m_here - t);
       }
     }
   } else {
-    uint32_t* part = reinterpret_cast<uint32_t*>(smem);       // [tile_m][128], all copies have been consumed
+    // CTA q of the cluster finishes rows q * own .. of the tile: every CTA writes its part of them into
+    // q's shared memory (stores, so that nobody waits for a far load), then q adds what lies at home.
+    // The stages may be overwritten once all CTAs' matrix instructions are done.
+    const int own = ((m_here + a.split - 1) / a.split + 15) / 16 * 16;
+    const uint32_t part = smem_u32(smem);        // [split][own][128]
+    __syncwarp();
+    cluster_barrier();
     if (warp >= 2 && ok) {
-      for (int t0 = 0; t0 < m_here; t0 += 16) {
+      for (int t = half * 16; t < m_here; t += 32) {
         uint32_t r[16];
-        tmem_ld16(trow + t0, r);
+        tmem_ld16(trow + t, r);
+        const int q = t / own;                   // 16 rows have one owner
+        const uint32_t at = cluster_map(part + (uint32_t)((rank * own + t - q * own) * kTileN + col) * 4, q);
         tmem_wait_ld();
+        if (m_here - t >= 16) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) part[(t0 + j) * kTileN + col] = r[j];
+          for (int j = 0; j < 16; ++j) st_cluster_u32(at + j * kTileN * 4, r[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (t + j < m_here) st_cluster_u32(at + j * kTileN * 4, r[j]);
+        }
       }
     }
     __syncwarp();
     cluster_barrier();
     if (warp >= 2 && ok) {
-      // Rows t = rank, rank + split, ...: four at a time, so that their parts are fetched together.
-      const uint32_t base = smem_u32(part) + (uint32_t)col * 4;
-      for (int t0 = rank; t0 < m_here; t0 += 4 * a.split) {
-        const float sa = row_scale(t0 + (lane & 3) * a.split);
-        long long isum[4] = {0, 0, 0, 0};
-        float fsum[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int q = 0; q < a.split; ++q) {
-          const uint32_t at = cluster_map(base, q);
-          uint32_t v[4];
+      const uint32_t* home = reinterpret_cast<const uint32_t*>(smem) + col;
+      const int mine = min(own, m_here - rank * own);
+      for (int t = half * 16; t < mine; t += 32) {
+        const float sa = row_scales(rank * own + t);
+        uint32_t sum[16];
+        if (INT8) {
+          // the parts' sum may leave 32 bits only where k is too long for one of them
+          if (a.c.kblocks <= kMaxBlocksInt8) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int t = t0 + j * a.split;
-            v[j] = t < m_here ? ld_cluster_u32(at + (uint32_t)t * kTileN * 4) : 0u;
+            for (int j = 0; j < 16; ++j) sum[j] = 0;
+            for (int q = 0; q < a.split; ++q)
+#pragma unroll
+              for (int j = 0; j < 16; ++j) sum[j] += home[(q * own + t + j) * kTileN];
+            store(Sums(), rank * own + t, sum, sa, mine - t);
+            continue;
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (INT8) isum[j] += (int)v[j];
-            else fsum[j] += __uint_as_float(v[j]);
+          for (int j = 0; j < 16; ++j) {
+            long long v = 0;
+            for (int q = 0; q < a.split; ++q) v += (int)home[(q * own + t + j) * kTileN];
+            sum[j] = __float_as_uint((float)v);
           }
-        }
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float s = __shfl_sync(0xffffffffu, sa, j);
-          const int t = t0 + j * a.split;
-          if (n < a.c.n && t < m_here) put(t, INT8 ? (float)isum[j] : fsum[j], s);
+          for (int j = 0; j < 16; ++j) sum[j] = 0;
+          for (int q = 0; q < a.split; ++q)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              sum[j] = __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(home[(q * own + t + j) * kTileN]));
         }
+        store(std::false_type(), rank * own + t, sum, sa, mine - t);
       }
     }
-    __syncwarp();
-    cluster_barrier();                   // nobody leaves while its part is being read
   }
   tcgen05_before_sync();
   __syncwarp();
@@ -233,46 +260,75 @@ int launch_matmul(const CUtensorMap& mp, const CUtensorMap& mq, const SplitArgs&
       return PRM_ERR_CUDA;
     once.mark(dev);
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas, 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)a.split;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, matmul_q8_kernel<INT8, P_MN, Q_MN>, mp, mq, a) == cudaSuccess ? PRM_OK
-                                                                                              : PRM_ERR_CUDA;
+  return launch_after(matmul_q8_kernel<INT8, P_MN, Q_MN>, (unsigned)ctas, kThreads, smem, stream, (unsigned)a.split, mp,
+                      mq, a) == cudaSuccess
+             ? PRM_OK
+             : PRM_ERR_CUDA;
 }
 
-int matmul_split(const MatmulProblem& p) {
+// CTAs in clusters of `split` that are resident at once (1 per SM; how many clusters fit depends on how
+// many SMs the GPCs have).
+int resident_ctas(int split) {
+  static int at[64][kMaxSplit + 1];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  if (at[dev][split] == 0) {
+    if (cudaFuncSetAttribute(matmul_q8_kernel<true, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)(kSmemBudget + 1024)) != cudaSuccess)
+      return 0;
+    at[dev][split] =
+        split * q8_resident_clusters(matmul_q8_kernel<true, true, false>, kThreads, kSmemBudget + 1024, (unsigned)split);
+  }
+  return at[dev][split];
+}
+
+struct Plan {
+  int tile_m = 0, split = 0;
+  double cycles = 1e30;
+};
+
+// Which tile height and how many CTAs to a tile: the cheapest of all by an estimate of SM cycles, with
+// the rates measured on a B200: 2 tile_m cycles of matrix instructions per k-block, 60 bytes per cycle
+// and SM from L2, 24 cycles per row of the epilogue.
+Plan plan_split(const MatmulProblem& p) {
+  Plan best;
+  const int need = p.int8 ? (p.c.kblocks + kMaxBlocksInt8 - 1) / kMaxBlocksInt8 : 1;
+  const double memory = matmul_q8_memory_cycles(p);
+  const int64_t n_tiles = (p.c.n + kTileN - 1) / kTileN;
+  for (int tile_m = 16; tile_m <= 256; tile_m *= 2) {
+    const int64_t tiles = n_tiles * ((p.c.m + tile_m - 1) / tile_m);
+    for (int split = need; split <= kMaxSplit && (split == need || split * 2 <= p.c.kblocks); ++split) {
+      const int slots = resident_ctas(split);
+      if (slots < 1) continue;
+      const double waves = std::ceil((double)tiles * split / slots);
+      if (waves > 1 && split > need) break;
+      const int blocks = (p.c.kblocks + split - 1) / split;
+      const double block = std::max(2.0 * tile_m, (128.0 + tile_m) * kBlockK / 60);
+      const double tail = split > 1 ? 1200 + 12.0 * tile_m + 24.0 * tile_m / split : 24.0 * tile_m;
+      const double cycles = std::max(waves * blocks * block, memory) + waves * tail + (waves - 1) * 4000;
+      if (cycles < best.cycles) best = {tile_m, split, cycles};
+    }
+    if (tile_m >= p.c.m) break;
+  }
+  return best;
+}
+
+int matmul_split(const MatmulProblem& p, const Plan& plan) {
   const int64_t m = p.c.m, n = p.c.n;
   SplitArgs g = {};
   g.c = p.c;
-  g.tile_m = 16;
-  while (g.tile_m < 256 && g.tile_m < m) g.tile_m *= 2;
+  g.tile_m = plan.tile_m;
+  g.split = plan.split;
   g.n_tiles = (int)((n + kTileN - 1) / kTileN);
   const int64_t tiles = (int64_t)g.n_tiles * ((m + g.tile_m - 1) / g.tile_m);
-  // Split k while every SM would otherwise not get a tile, but leave each CTA four k-blocks.
-  int split = 1;
-  while (split < kMaxSplit && tiles * (split + 1) <= 148 && g.c.kblocks >= 4 * (split + 1)) ++split;
-  if (p.int8) {
-    const int need = (g.c.kblocks + kMaxBlocksInt8 - 1) / kMaxBlocksInt8;
-    if (need > kMaxSplit) return PRM_ERR_SHAPE;
-    split = std::max(split, need);
-  }
-  g.split = split;
+  const int split = g.split;
   if (tiles * split > 0x7fffffffLL) return PRM_ERR_SHAPE;
   const uint32_t q_bytes = (p.a_t ? (uint32_t)std::max(g.tile_m, 128) : (uint32_t)g.tile_m) * kBlockK;
   g.stage_bytes = kBytesP + q_bytes;
   const int blocks_each = (g.c.kblocks + split - 1) / split;
   g.stages = std::max(1, std::min<int>({kMaxStages, blocks_each, (int)(kSmemBudget / g.stage_bytes)}));
   size_t smem = (size_t)g.stages * g.stage_bytes;
-  if (split > 1) smem = std::max(smem, (size_t)g.tile_m * kTileN * 4);
+  if (split > 1) smem = std::max(smem, (size_t)(g.tile_m + 16 * split) * kTileN * 4);
   smem += 1024;
   CUtensorMap mp, mq;
   if (!q8_make_map(&mp, p.b, p.b_rows, p.b_cols, p.ld_b, 128) ||
@@ -349,9 +405,11 @@ extern "C" int prm_matmul_q8(const void* a, int64_t ld_a, int a_transposed, cons
   p.b_t = !p_mn;
   p.int8 = format == PRM_Q8_INT8;
   p.stream = stream;
+  if (p.int8 && p.c.kblocks > kMaxSplit * kMaxBlocksInt8) return PRM_ERR_SHAPE;
   if (!p.c.status) return PRM_ERR_CUDA;
-  if (matmul_q8_wants_pairs(p)) return matmul_q8_pairs(p);
-  return matmul_split(p);
+  const Plan plan = plan_split(p);
+  if (matmul_q8_pairs_cycles(p) < plan.cycles) return matmul_q8_pairs(p);
+  return plan.tile_m > 0 ? matmul_split(p, plan) : PRM_ERR_CUDA;
 }
 
 extern "C" int prm_q8_status(void) {

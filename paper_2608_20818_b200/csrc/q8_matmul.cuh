@@ -1,6 +1,8 @@
 // What the two kernels of the 8-bit product share: the problem, its tensor maps, the choice.
 #pragma once
 
+#include <cmath>
+
 #include "q8.cuh"
 #include "tcgen05.cuh"
 
@@ -58,7 +60,8 @@ struct MatmulProblem {
 };
 
 // Pairs of CTAs on 256 x 256 tiles, for products that fill the GPU with them.
-bool matmul_q8_wants_pairs(const MatmulProblem& p);
+// Estimated SM cycles, without what every launch costs.
+double matmul_q8_pairs_cycles(const MatmulProblem& p);
 int matmul_q8_pairs(const MatmulProblem& p);
 
 typedef CUresult (*Q8EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -89,6 +92,32 @@ inline bool q8_make_map(CUtensorMap* map, const void* base, int64_t rows, int64_
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, step,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Cycles that HBM needs for the operands at 6.4 TB/s and 1.9 GHz.
+inline double matmul_q8_memory_cycles(const MatmulProblem& p) {
+  return ((double)p.a_rows * p.a_cols + (double)p.b_rows * p.b_cols) / 3400.0;
+}
+
+// Clusters of `size` CTAs that can be resident at once (0: an error).
+template <typename K>
+inline int q8_resident_clusters(K kernel, unsigned threads, size_t smem, unsigned size) {
+  int dev = 0, sms = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 0;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)sms / size * size, 1, 1);
+  cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = size;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess ? n : 0;
 }
 
 }  // namespace prm

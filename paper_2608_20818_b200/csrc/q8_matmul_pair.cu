@@ -121,6 +121,8 @@ matmul_q8_pair_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_co
   cluster_barrier();                             // the peer's barriers are initialised too
   tcgen05_after_sync();
   const uint32_t tmem = tmem_slot;
+  grid_wait();
+  grid_trigger();                                // not before the tensor memory is this kernel's
 
   if (warp == 0) {
     if (lane == 0) {
@@ -239,40 +241,30 @@ template <bool INT8, bool P_MN, bool Q_MN>
 int launch_pairs(const CUtensorMap& mp, const CUtensorMap& mq, const PairArgs& a, cudaStream_t stream) {
   static PerDeviceOnce once;
   static int resident[64];
-  cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = kSmemBytes;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
   int dev;
   if (once.need(&dev)) {
-    int n = 0, sms = 0;
-    if (dev < 0 || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-        cudaFuncSetAttribute(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    if (dev < 0 || cudaFuncSetAttribute(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              (int)kSmemBytes) != cudaSuccess)
       return PRM_ERR_CUDA;
-    cfg.gridDim = dim3((unsigned)(sms & ~1), 1, 1);
-    if (cudaOccupancyMaxActiveClusters(&n, matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, &cfg) != cudaSuccess || n < 1)
-      return PRM_ERR_CUDA;
+    const int n = q8_resident_clusters(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, kThreads, kSmemBytes, 2);
+    if (n < 1) return PRM_ERR_CUDA;
     resident[dev] = n;
     once.mark(dev);
   }
-  cfg.gridDim = dim3(2u * (unsigned)std::min(a.tiles, resident[dev]), 1, 1);
-  return cudaLaunchKernelEx(&cfg, matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, mp, mq, a) == cudaSuccess ? PRM_OK
-                                                                                                   : PRM_ERR_CUDA;
+  return launch_after(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, 2u * (unsigned)std::min(a.tiles, resident[dev]), kThreads,
+                      kSmemBytes, stream, 2, mp, mq, a) == cudaSuccess
+             ? PRM_OK
+             : PRM_ERR_CUDA;
 }
 
 }  // namespace
 
-bool matmul_q8_wants_pairs(const MatmulProblem& p) {
-  const int64_t tiles = (int64_t)((p.c.m + kTile - 1) / kTile) * ((p.c.n + kTile - 1) / kTile);
-  return tiles >= 56 && tiles < (1 << 30) && (!p.int8 || p.c.kblocks <= kMaxBlocksInt8);
+double matmul_q8_pairs_cycles(const MatmulProblem& p) {
+  const double tiles = (double)((p.c.m + kTile - 1) / kTile) * ((p.c.n + kTile - 1) / kTile);
+  if (tiles >= (1 << 30) || (p.int8 && p.c.kblocks > kMaxBlocksInt8)) return 1e30;
+  // 512 cycles of matrix instructions per k-block of a tile; the epilogue of the last tile alone
+  const double waves = std::ceil(tiles / 74);
+  return std::max(waves * (p.c.kblocks * 520.0 + 1600), matmul_q8_memory_cycles(p)) + 4500;
 }
 
 int matmul_q8_pairs(const MatmulProblem& p) {

@@ -60,6 +60,8 @@ template <typename IO, typename WT, int NV, int TPR, bool RES>
 __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const NormArgs a) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
   __shared__ float red[64];
+  grid_wait();
+  grid_trigger();
   const int c0 = (threadIdx.x % TPR) * 8;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   if (row >= a.rows) return;              // whole warps (kRows > 1) or no thread
@@ -104,11 +106,13 @@ rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
   const void* const src[2] = {a.x, a.residual};
   const int64_t ld[2] = {a.ld_x, a.ld_r};
   RowRing<IO, W, kArr> ring(b, src, ld, a.rows, a.cols, stages, status);
+  ring.start();
+  grid_wait();
+  grid_trigger();
   Oct<WT> wv[kNV];
 #pragma unroll
   for (int v = 0; v < kNV; ++v)
     if (c0 + v * kStep < a.cols) wv[v].load(reinterpret_cast<const WT*>(a.weight) + c0 + v * kStep);
-  ring.start();
   if (ring.producer) {
     ring.serve();
     ring.finish();
@@ -148,6 +152,8 @@ rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
 template <typename IO, int THREADS>
 __global__ void __launch_bounds__(THREADS) rmsnorm_q8_single_kernel(const NormArgs a) {
   __shared__ float red[64];
+  grid_wait();
+  grid_trigger();
   const int64_t row = blockIdx.x;
   const IO* x = reinterpret_cast<const IO*>(a.x) + row * a.ld_x;
   const IO* r = a.residual ? reinterpret_cast<const IO*>(a.residual) + row * a.ld_r : nullptr;
@@ -180,8 +186,8 @@ template <typename IO, typename WT, int NV, int TPR>
 int launch_norm(const NormArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
   const unsigned blocks = (unsigned)((a.rows + kRows - 1) / kRows);
-  if (a.residual) rmsnorm_q8_kernel<IO, WT, NV, TPR, true><<<blocks, TPR == 32 ? 256 : TPR, 0, stream>>>(a);
-  else rmsnorm_q8_kernel<IO, WT, NV, TPR, false><<<blocks, TPR == 32 ? 256 : TPR, 0, stream>>>(a);
+  if (a.residual) launch_after(rmsnorm_q8_kernel<IO, WT, NV, TPR, true>, blocks, TPR == 32 ? 256 : TPR, 0, stream, 0, a);
+  else launch_after(rmsnorm_q8_kernel<IO, WT, NV, TPR, false>, blocks, TPR == 32 ? 256 : TPR, 0, stream, 0, a);
   return PRM_OK;
 }
 
@@ -215,9 +221,9 @@ int run_norm(const NormArgs& a, cudaStream_t stream) {
 
 template <typename IO>
 int run_norm_single(const NormArgs& a, cudaStream_t stream) {
-  if (a.cols <= 1024) rmsnorm_q8_single_kernel<IO, 128><<<(unsigned)a.rows, 128, 0, stream>>>(a);
-  else if (a.cols <= 8192) rmsnorm_q8_single_kernel<IO, 256><<<(unsigned)a.rows, 256, 0, stream>>>(a);
-  else rmsnorm_q8_single_kernel<IO, 1024><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
+  if (a.cols <= 1024) launch_after(rmsnorm_q8_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a);
+  else if (a.cols <= 8192) launch_after(rmsnorm_q8_single_kernel<IO, 256>, (unsigned)a.rows, 256, 0, stream, 0, a);
+  else launch_after(rmsnorm_q8_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a);
   return PRM_OK;
 }
 
@@ -280,6 +286,8 @@ __device__ __forceinline__ void grad_oct(const float2 (&gy)[4], const float2 (&h
 template <typename IO, typename WT, int NV, int TPR>
 __global__ void __launch_bounds__(TPR) rmsnorm_q8_grad_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
+  grid_wait();
+  grid_trigger();
   const int c0 = threadIdx.x * 8;
   float2 gw[NV][4];
   Oct<WT> wv[NV];
@@ -361,6 +369,8 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) gw[v][e] = make_float2(0.f, 0.f);
   ring.start();
+  grid_wait();
+  grid_trigger();
   if (ring.producer) ring.serve();
   const int64_t n = ring.producer ? 0 : ring.n;
   for (int64_t i = 0; i < n; ++i) {
@@ -427,6 +437,8 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
 template <typename IO, int THREADS>
 __global__ void __launch_bounds__(THREADS) rmsnorm_q8_grad_single_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
+  grid_wait();
+  grid_trigger();
   float* part = a.part + (int64_t)blockIdx.x * a.cols;
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
@@ -459,6 +471,8 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_q8_grad_single_kernel(const N
 __global__ void __launch_bounds__(1024)
 rmsnorm_q8_grad_weight_kernel(const float* part, int parts, int cols, void* gw, int fp32) {
   __shared__ float s[32][33];
+  grid_wait();
+  grid_trigger();
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
   float sum = 0.f;
   if (c < cols) {
@@ -500,18 +514,18 @@ int run_grad(const NormGradArgs& a, int* parts, cudaStream_t stream) {
     if (c <= 4096) return launch_grad_stream<IO, WT, 4>(a, parts, stream);
     return launch_grad_stream<IO, WT, 8>(a, parts, stream);
   }
-  if (c <= 256) rmsnorm_q8_grad_kernel<IO, WT, 1, 32><<<*parts, 32, 0, stream>>>(a);
-  else if (c <= 1024) rmsnorm_q8_grad_kernel<IO, WT, 1, 128><<<*parts, 128, 0, stream>>>(a);
-  else if (c <= 4096) rmsnorm_q8_grad_kernel<IO, WT, 1, 512><<<*parts, 512, 0, stream>>>(a);
-  else rmsnorm_q8_grad_kernel<IO, WT, 2, 512><<<*parts, 512, 0, stream>>>(a);
+  if (c <= 256) launch_after(rmsnorm_q8_grad_kernel<IO, WT, 1, 32>, *parts, 32, 0, stream, 0, a);
+  else if (c <= 1024) launch_after(rmsnorm_q8_grad_kernel<IO, WT, 1, 128>, *parts, 128, 0, stream, 0, a);
+  else if (c <= 4096) launch_after(rmsnorm_q8_grad_kernel<IO, WT, 1, 512>, *parts, 512, 0, stream, 0, a);
+  else launch_after(rmsnorm_q8_grad_kernel<IO, WT, 2, 512>, *parts, 512, 0, stream, 0, a);
   return PRM_OK;
 }
 
 template <typename IO>
 int run_grad_single(const NormGradArgs& a, int parts, cudaStream_t stream) {
-  if (a.cols <= 1024) rmsnorm_q8_grad_single_kernel<IO, 128><<<parts, 128, 0, stream>>>(a);
-  else if (a.cols <= 8192) rmsnorm_q8_grad_single_kernel<IO, 512><<<parts, 512, 0, stream>>>(a);
-  else rmsnorm_q8_grad_single_kernel<IO, 1024><<<parts, 1024, 0, stream>>>(a);
+  if (a.cols <= 1024) launch_after(rmsnorm_q8_grad_single_kernel<IO, 128>, parts, 128, 0, stream, 0, a);
+  else if (a.cols <= 8192) launch_after(rmsnorm_q8_grad_single_kernel<IO, 512>, parts, 512, 0, stream, 0, a);
+  else launch_after(rmsnorm_q8_grad_single_kernel<IO, 1024>, parts, 1024, 0, stream, 0, a);
   return PRM_OK;
 }
 
@@ -590,7 +604,6 @@ extern "C" int prm_rmsnorm_q8_backward(const void* grad_y, int64_t ld_grad_y, co
     code = weight_fp32 ? run_grad<__nv_bfloat16, float>(a, &parts, stream)
                        : run_grad<__nv_bfloat16, __nv_bfloat16>(a, &parts, stream);
   if (code != PRM_OK) return code;
-  rmsnorm_q8_grad_weight_kernel<<<(unsigned)((cols + 31) / 32), 1024, 0, stream>>>(a.part, parts, (int)cols,
-                                                                                 grad_weight, weight_fp32);
+  launch_after(rmsnorm_q8_grad_weight_kernel, (unsigned)((cols + 31) / 32), 1024, 0, stream, 0, a.part, parts, (int)cols, grad_weight, weight_fp32);
   return cudaGetLastError() == cudaSuccess ? PRM_OK : PRM_ERR_CUDA;
 }

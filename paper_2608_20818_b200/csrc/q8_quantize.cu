@@ -47,6 +47,8 @@ template <typename IO, int NV, int TPR>
 __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_kernel(const QuantArgs a) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
   __shared__ float red[64];
+  grid_wait();
+  grid_trigger();
   const int c0 = (threadIdx.x % TPR) * 8;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   if (row >= a.rows) return;
@@ -76,6 +78,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_kernel(co
 template <typename IO, int THREADS>
 __global__ void __launch_bounds__(THREADS) quantize_rows_single_kernel(const QuantArgs a) {
   __shared__ float red[64];
+  grid_wait();
+  grid_trigger();
   const int64_t row = blockIdx.x;
   const IO* x = reinterpret_cast<const IO*>(a.x) + row * a.ld_x;
   auto value = [&](int c) {
@@ -283,6 +287,7 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
     }
   }
   cooperative_groups::grid_group grid = cooperative_groups::this_grid();
+  grid_trigger();
   for (int g = 0; g < kRingWarps<IO> / W; ++g) {      // the groups take turns
     if (!ring.producer && ring.group == g) {
 #pragma unroll
@@ -422,8 +427,7 @@ int run_stream(QuantArgs a, cudaStream_t stream) {
 template <typename IO, int NV, int TPR>
 void launch_rows(const QuantArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
-  quantize_rows_kernel<IO, NV, TPR>
-      <<<(unsigned)((a.rows + kRows - 1) / kRows), TPR == 32 ? 256 : TPR, 0, stream>>>(a);
+  launch_after(quantize_rows_kernel<IO, NV, TPR>, (unsigned)((a.rows + kRows - 1) / kRows), TPR == 32 ? 256 : TPR, 0, stream, 0, a);
 }
 
 template <typename IO>
@@ -438,9 +442,9 @@ void run_rows(const QuantArgs& a, bool octs, cudaStream_t stream) {
     else if (c <= 8192) launch_rows<IO, 2, 512>(a, stream);
     else launch_rows<IO, 2, 1024>(a, stream);
   } else {
-    if (c <= 1024) quantize_rows_single_kernel<IO, 128><<<(unsigned)a.rows, 128, 0, stream>>>(a);
-    else if (c <= 8192) quantize_rows_single_kernel<IO, 256><<<(unsigned)a.rows, 256, 0, stream>>>(a);
-    else quantize_rows_single_kernel<IO, 1024><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
+    if (c <= 1024) launch_after(quantize_rows_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a);
+    else if (c <= 8192) launch_after(quantize_rows_single_kernel<IO, 256>, (unsigned)a.rows, 256, 0, stream, 0, a);
+    else launch_after(quantize_rows_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a);
   }
 }
 

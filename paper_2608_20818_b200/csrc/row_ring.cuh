@@ -288,9 +288,10 @@ int launch_ring(K kernel, int arrays, PerDeviceOnce& once, int64_t rows, int col
   const size_t row = (size_t)cols * sizeof(IO) * arrays * kGroups;
   const int stages = (int)std::min<size_t>(kRingStages, kRingBytes / row);
   if (!status || stages < 1 || extra > kRingBytes) return PRM_ERR_CUDA;
-  kernel<<<(unsigned)ring_blocks(rows, kGroups), kRingThreads<IO>, std::max(extra, row * stages), stream>>>(a, stages,
-                                                                                                            status);
-  return PRM_OK;
+  return launch_after(kernel, (unsigned)ring_blocks(rows, kGroups), kRingThreads<IO>, std::max(extra, row * stages),
+                      stream, 0, a, stages, status) == cudaSuccess
+             ? PRM_OK
+             : PRM_ERR_CUDA;
 }
 
 }  // namespace prm
