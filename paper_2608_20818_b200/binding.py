@@ -8,7 +8,6 @@ there is no fallback path.
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int64, c_size_t, c_void_p
@@ -403,11 +402,14 @@ def prm_shape_scale(mode, rows, cols):
     return v
 
 
-_Q8_DTYPE = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
-_Q8_FORMAT = {"int8": PRM_Q8_INT8, "e4m3": PRM_Q8_E4M3}
+_Q8_FORMAT = {"int8": (PRM_Q8_INT8, torch.int8), "e4m3": (PRM_Q8_E4M3, torch.float8_e4m3fn)}
 _Q8_CODE = {torch.int8: PRM_Q8_INT8, torch.float8_e4m3fn: PRM_Q8_E4M3}
 _IO_FP32 = {torch.bfloat16: 0, torch.float32: 1}
 
+
+# The 8-bit operators below are called many times per training step, on small matrices too, where the
+# time on the host is what a call costs: their checks are written out on attributes that are cheap to
+# read, and the reasons for a refusal are worked out by helpers that a good call does not reach.
 
 def _on_stream(stream, inputs, call):
     """Runs call() with `stream` current, so that what it allocates belongs to that stream, and
@@ -420,48 +422,58 @@ def _on_stream(stream, inputs, call):
     return out
 
 
-def _raw_stream(device):
-    return torch._C._cuda_getCurrentRawStream(device.index)
+def _raw_stream(index):
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _stream_matrix(t, name, dtype=None, shape=None):
-    """A 2-D bf16 or fp32 CUDA tensor whose rows are contiguous (copied if they are not)."""
+def _on_device(index, fn, *args):
+    """fn(*args) with device `index` current (callers test whether it is already)."""
+    with torch.cuda.device(index):
+        return fn(*args)
+
+
+def _refuse_matrix(t, name, like):
     if t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D matrix")
     if not t.is_cuda:
         raise ValueError(f"{name} must sit on a CUDA device")
     if t.dtype not in _IO_FP32:
         raise TypeError(f"{name} must be bfloat16 or float32")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype} like the matrix it goes with")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have the shape {tuple(shape)}")
+    if like is not None:
+        if t.dtype != like.dtype:
+            raise TypeError(f"{name} must be {like.dtype} like the matrix it goes with")
+        if t.shape != like.shape:
+            raise ValueError(f"{name} must have the shape {tuple(like.shape)}")
+        raise ValueError(f"{name} must sit on {like.device}")
+
+
+def _matrix(t, name, like=None):
+    """t, a 2-D bf16 or fp32 CUDA tensor (of the type, shape and device of `like`) whose rows are
+    contiguous; copied if they are not."""
+    if like is None:
+        if not t.is_cuda or t.dtype not in _IO_FP32 or t.dim() != 2:
+            _refuse_matrix(t, name, like)
+    elif t.dtype is not like.dtype or t.shape != like.shape or t.get_device() != like.get_device():
+        _refuse_matrix(t, name, like)
     return t if t.stride(1) == 1 or t.shape[1] == 1 else t.contiguous()
 
 
-def _vector(t, name, n, device, dtypes=(torch.float32,)):
-    """A contiguous vector of n elements on `device` (None stays None)."""
-    if t is None:
-        return None
+def _refuse_vector(t, name, n, index, dtypes):
     if t.dtype not in dtypes:
-        raise TypeError(f"{name} must be one of {dtypes}")
+        raise TypeError(f"{name} must be one of {tuple(dtypes)}")
     if t.dim() != 1 or t.shape[0] != n:
         raise ValueError(f"{name} must be a vector of {n} elements")
-    if t.device != device:
-        raise ValueError(f"{name} must sit on {device}")
+    raise ValueError(f"{name} must sit on cuda:{index}")
+
+
+_FP32_ONLY = {torch.float32: 1}
+
+
+def _vector(t, name, n, index, dtypes=_FP32_ONLY):
+    """t, a contiguous vector of n elements on device `index` (copied if it is strided)."""
+    if t.dtype not in dtypes or t.shape != (n,) or t.get_device() != index:
+        _refuse_vector(t, name, n, index, dtypes)
     return t if n <= 1 or t.stride(0) == 1 else t.contiguous()
-
-
-_NO_GUARD = contextlib.nullcontext()
-
-
-def _device_guard(device):
-    """Makes `device` current for a call, where it is not already."""
-    return _NO_GUARD if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
 
 
 def _codes(rows, cols, dtype, device):
@@ -469,9 +481,15 @@ def _codes(rows, cols, dtype, device):
     return torch.empty_strided((rows, cols), ((cols + 15) // 16 * 16, 1), dtype=dtype, device=device)
 
 
+def _format(format):
+    try:
+        return _Q8_FORMAT[format]
+    except KeyError:
+        raise ValueError('format must be "int8" or "e4m3"') from None
+
+
 def _q8_check(code, what):
-    if code != PRM_OK:
-        raise PrmError(code, f"{what} failed (see include/prm.h for its limits)")
+    raise PrmError(code, f"{what} failed (see include/prm.h for its limits)")
 
 
 def prm_rmsnorm_q8(x, weight, eps, residual=None, format="int8", stream=None):
@@ -483,27 +501,28 @@ def prm_rmsnorm_q8(x, weight, eps, residual=None, format="int8", stream=None):
     if stream is not None:
         return _on_stream(stream, (x, weight, residual),
                           lambda: prm_rmsnorm_q8(x, weight, eps, residual, format))
-    fmt = _Q8_FORMAT.get(format)
-    if fmt is None:
-        raise ValueError('format must be "int8" or "e4m3"')
-    x = _stream_matrix(x, "x")
+    fmt, dtype = _format(format)
+    x = _matrix(x, "x")
     rows, cols = x.shape
+    index = x.get_device()
     device = x.device
-    weight = _vector(weight, "weight", cols, device, (torch.bfloat16, torch.float32))
-    h, ld_r, ld_h = None, 0, 0
+    weight = _vector(weight, "weight", cols, index, _IO_FP32)
     if residual is not None:
-        residual = _stream_matrix(residual, "residual", x.dtype, x.shape)
-        if residual.device != device:
-            raise ValueError(f"residual must sit on {device}")
-        h = torch.empty((rows, cols), dtype=x.dtype, device=device)
-        ld_r, ld_h = residual.stride(0), cols
-    q = _codes(rows, cols, _Q8_DTYPE[format], device)
-    scale = torch.empty(rows, dtype=torch.float32, device=device)
-    with _device_guard(device):
-        code = lib().prm_rmsnorm_q8(x.data_ptr(), x.stride(0), _ptr(residual), ld_r, weight.data_ptr(), rows, cols,
-                                    _IO_FP32[x.dtype], _IO_FP32[weight.dtype], eps, fmt, _ptr(h), ld_h, q.data_ptr(),
-                                    q.stride(0), scale.data_ptr(), _raw_stream(device))
-    _q8_check(code, "prm_rmsnorm_q8")
+        residual = _matrix(residual, "residual", x)
+        h = torch.empty_strided((rows, cols), (cols, 1), dtype=x.dtype, device=device)
+        r_ptr, ld_r, h_ptr = residual.data_ptr(), residual.stride(0), h.data_ptr()
+    else:
+        h = r_ptr = h_ptr = None
+        ld_r = 0
+    q = _codes(rows, cols, dtype, device)
+    scale = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device)
+    args = (x.data_ptr(), x.stride(0), r_ptr, ld_r, weight.data_ptr(), rows, cols, _IO_FP32[x.dtype],
+            _IO_FP32[weight.dtype], eps, fmt, h_ptr, cols, q.data_ptr(), q.stride(0), scale.data_ptr(),
+            _raw_stream(index))
+    fn = (_lib_handle or lib()).prm_rmsnorm_q8
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_rmsnorm_q8")
     return q, scale, h
 
 
@@ -514,28 +533,29 @@ def prm_rmsnorm_q8_backward(grad_y, h, weight, eps, grad_h=None, stream=None):
     if stream is not None:
         return _on_stream(stream, (grad_y, h, weight, grad_h),
                           lambda: prm_rmsnorm_q8_backward(grad_y, h, weight, eps, grad_h))
-    h = _stream_matrix(h, "h")
-    grad_y = _stream_matrix(grad_y, "grad_y", h.dtype, h.shape)
+    h = _matrix(h, "h")
+    grad_y = _matrix(grad_y, "grad_y", h)
     rows, cols = h.shape
+    index = h.get_device()
     device = h.device
-    weight = _vector(weight, "weight", cols, device, (torch.bfloat16, torch.float32))
-    ld_gh = 0
+    weight = _vector(weight, "weight", cols, index, _IO_FP32)
     if grad_h is not None:
-        grad_h = _stream_matrix(grad_h, "grad_h", h.dtype, h.shape)
-        ld_gh = grad_h.stride(0)
-    if grad_y.device != device or (grad_h is not None and grad_h.device != device):
-        raise ValueError(f"the gradients must sit on {device}")
-    L = lib()
+        grad_h = _matrix(grad_h, "grad_h", h)
+        gh_ptr, ld_gh = grad_h.data_ptr(), grad_h.stride(0)
+    else:
+        gh_ptr, ld_gh = None, 0
+    L = _lib_handle or lib()
     nbytes = L.prm_rmsnorm_q8_scratch_bytes(rows, cols)
-    grad_x = torch.empty((rows, cols), dtype=h.dtype, device=device)
-    grad_w = torch.empty(cols, dtype=weight.dtype, device=device)
-    scratch = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    with _device_guard(device):
-        code = L.prm_rmsnorm_q8_backward(grad_y.data_ptr(), grad_y.stride(0), h.data_ptr(), h.stride(0),
-                                         weight.data_ptr(), _ptr(grad_h), ld_gh, rows, cols, _IO_FP32[h.dtype],
-                                         _IO_FP32[weight.dtype], eps, grad_x.data_ptr(), cols, grad_w.data_ptr(),
-                                         scratch.data_ptr(), nbytes, _raw_stream(device))
-    _q8_check(code, "prm_rmsnorm_q8_backward")
+    grad_x = torch.empty_strided((rows, cols), (cols, 1), dtype=h.dtype, device=device)
+    grad_w = torch.empty_strided((cols,), (1,), dtype=weight.dtype, device=device)
+    scratch = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)
+    args = (grad_y.data_ptr(), grad_y.stride(0), h.data_ptr(), h.stride(0), weight.data_ptr(), gh_ptr, ld_gh, rows, cols,
+            _IO_FP32[h.dtype], _IO_FP32[weight.dtype], eps, grad_x.data_ptr(), cols, grad_w.data_ptr(),
+            scratch.data_ptr(), nbytes, _raw_stream(index))
+    fn = L.prm_rmsnorm_q8_backward
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_rmsnorm_q8_backward")
     return grad_x, grad_w
 
 
@@ -547,56 +567,69 @@ def prm_quantize_q8(x, *, by_rows=True, by_cols=False, fold_rows=None, fold_cols
         return _on_stream(stream, (x, fold_rows, fold_cols),
                           lambda: prm_quantize_q8(x, by_rows=by_rows, by_cols=by_cols, fold_rows=fold_rows,
                                                   fold_cols=fold_cols, format=format))
-    fmt = _Q8_FORMAT.get(format)
-    if fmt is None:
-        raise ValueError('format must be "int8" or "e4m3"')
+    fmt, dtype = _format(format)
     if not by_rows and not by_cols:
         raise ValueError("ask for codes by rows, by columns, or both")
-    x = _stream_matrix(x, "x")
+    x = _matrix(x, "x")
     rows, cols = x.shape
+    index = x.get_device()
     device = x.device
-    fold_rows = _vector(fold_rows, "fold_rows", rows, device)
-    fold_cols = _vector(fold_cols, "fold_cols", cols, device)
-    L = lib()
-    qr = sr = qc = sc = scratch = None
-    ld_r = ld_c = nbytes = 0
+    fr_ptr = fc_ptr = None
+    if fold_rows is not None:
+        fold_rows = _vector(fold_rows, "fold_rows", rows, index)
+        fr_ptr = fold_rows.data_ptr()
+    if fold_cols is not None:
+        fold_cols = _vector(fold_cols, "fold_cols", cols, index)
+        fc_ptr = fold_cols.data_ptr()
+    L = _lib_handle or lib()
+    qr = sr = qc = sc = qr_ptr = sr_ptr = qc_ptr = sc_ptr = scratch_ptr = None
+    ld = (cols + 15) // 16 * 16
+    nbytes = 0
     if by_rows:
-        qr = _codes(rows, cols, _Q8_DTYPE[format], device)
-        sr = torch.empty(rows, dtype=torch.float32, device=device)
-        ld_r = qr.stride(0)
+        qr = _codes(rows, cols, dtype, device)
+        sr = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device)
+        qr_ptr, sr_ptr = qr.data_ptr(), sr.data_ptr()
     if by_cols:
-        qc = _codes(rows, cols, _Q8_DTYPE[format], device)
-        sc = torch.empty(cols, dtype=torch.float32, device=device)
-        ld_c = qc.stride(0)
+        qc = _codes(rows, cols, dtype, device)
+        sc = torch.empty_strided((cols,), (1,), dtype=torch.float32, device=device)
         nbytes = L.prm_quantize_q8_scratch_bytes(rows, cols)
-        scratch = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        scratch = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)
+        qc_ptr, sc_ptr, scratch_ptr = qc.data_ptr(), sc.data_ptr(), scratch.data_ptr()
     if rows == 0:                       # nothing to point at: columns without an element have the scale 0
         return qr, sr, qc, None if sc is None else sc.zero_()
-    with _device_guard(device):
-        code = L.prm_quantize_q8(x.data_ptr(), x.stride(0), rows, cols, _IO_FP32[x.dtype], fmt, _ptr(fold_rows),
-                                 _ptr(fold_cols), _ptr(qr), ld_r, _ptr(sr), _ptr(qc), ld_c, _ptr(sc), _ptr(scratch),
-                                 nbytes, _raw_stream(device))
-    _q8_check(code, "prm_quantize_q8")
+    args = (x.data_ptr(), x.stride(0), rows, cols, _IO_FP32[x.dtype], fmt, fr_ptr, fc_ptr, qr_ptr, ld, sr_ptr, qc_ptr, ld,
+            sc_ptr, scratch_ptr, nbytes, _raw_stream(index))
+    fn = L.prm_quantize_q8
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_quantize_q8")
     return qr, sr, qc, sc
 
 
-def _q8_operand(t):
+def _q8_operand(t, r, c):
     """(matrix, its row stride, 1 if it is stored the other way round) as prm_matmul_q8 reads it;
     a matrix that lies in neither way, or unaligned, is copied."""
-    r, c = t.shape
     s0, s1 = t.stride()
-    if t.data_ptr() % 16 == 0:
+    if t.data_ptr() & 15 == 0:
         if s1 == 1 or c == 1:
             ld = s0 if r > 1 else (c + 15) // 16 * 16
-            if ld % 16 == 0 and ld >= c:
+            if ld & 15 == 0 and ld >= c:
                 return t, ld, 0
         if s0 == 1 or r == 1:
             ld = s1 if c > 1 else (r + 15) // 16 * 16
-            if ld % 16 == 0 and ld >= r:
+            if ld & 15 == 0 and ld >= r:
                 return t, ld, 1
     laid = _codes(r, c, t.dtype, t.device)
     laid.copy_(t)
     return laid, (c + 15) // 16 * 16, 0
+
+
+def _refuse_product(a, b):
+    if a.dim() != 2 or b.dim() != 2 or a.shape[1] != b.shape[0]:
+        raise ValueError("a must be m x k and b k x n")
+    if a.dtype not in _Q8_CODE or b.dtype != a.dtype:
+        raise TypeError("a and b must both be int8 or both float8_e4m3fn")
+    raise ValueError("a and b must sit on the same CUDA device")
 
 
 def prm_matmul_q8(a, scale_a, b, scale_b, out_dtype=torch.bfloat16, out=None, stream=None):
@@ -606,36 +639,42 @@ def prm_matmul_q8(a, scale_a, b, scale_b, out_dtype=torch.bfloat16, out=None, st
     if stream is not None:
         return _on_stream(stream, (a, scale_a, b, scale_b, out),
                           lambda: prm_matmul_q8(a, scale_a, b, scale_b, out_dtype, out))
-    if a.dim() != 2 or b.dim() != 2 or a.shape[1] != b.shape[0]:
-        raise ValueError("a must be m x k and b k x n")
+    index = a.get_device()
     fmt = _Q8_CODE.get(a.dtype)
-    if fmt is None or b.dtype != a.dtype:
-        raise TypeError("a and b must both be int8 or both float8_e4m3fn")
-    device = a.device
-    if not a.is_cuda or b.device != device:
-        raise ValueError("a and b must sit on the same CUDA device")
+    if (fmt is None or b.dtype is not a.dtype or index < 0 or b.get_device() != index or a.dim() != 2 or b.dim() != 2
+            or a.shape[1] != b.shape[0]):
+        _refuse_product(a, b)
     m, k = a.shape
     n = b.shape[1]
-    scale_a = _vector(scale_a, "scale_a", m, device)
-    scale_b = _vector(scale_b, "scale_b", n, device)
+    sa_ptr = sb_ptr = None
+    if scale_a is not None:
+        scale_a = _vector(scale_a, "scale_a", m, index)
+        sa_ptr = scale_a.data_ptr()
+    if scale_b is not None:
+        scale_b = _vector(scale_b, "scale_b", n, index)
+        sb_ptr = scale_b.data_ptr()
     if out is None:
         if out_dtype not in _IO_FP32:
             raise TypeError("out_dtype must be bfloat16 or float32")
-        out = torch.empty((m, n), dtype=out_dtype, device=device)
+        out = torch.empty_strided((m, n), (n, 1), dtype=out_dtype, device=a.device)
+        ld_out = n
     else:
-        if out.dtype not in _IO_FP32:
+        out_dtype = out.dtype
+        if out_dtype not in _IO_FP32:
             raise TypeError("out must be bfloat16 or float32")
-        if out.shape != (m, n) or out.device != device:
-            raise ValueError(f"out must be a {m} x {n} matrix on {device}")
+        if out.shape != (m, n) or out.get_device() != index:
+            raise ValueError(f"out must be a {m} x {n} matrix on cuda:{index}")
         if n > 1 and out.stride(1) != 1 or m > 1 and out.stride(0) < n:
             raise ValueError("the rows of out must be contiguous and must not overlap")
-    a, ld_a, a_t = _q8_operand(a)
-    b, ld_b, b_t = _q8_operand(b)
-    with _device_guard(device):
-        code = lib().prm_matmul_q8(a.data_ptr(), ld_a, a_t, _ptr(scale_a), b.data_ptr(), ld_b, b_t, _ptr(scale_b),
-                                   m, k, n, fmt, out.data_ptr(), out.stride(0) if m > 1 else n, _IO_FP32[out.dtype],
-                                   _raw_stream(device))
-    _q8_check(code, "prm_matmul_q8")
+        ld_out = out.stride(0) if m > 1 else n
+    a, ld_a, a_t = _q8_operand(a, m, k)
+    b, ld_b, b_t = _q8_operand(b, k, n)
+    args = (a.data_ptr(), ld_a, a_t, sa_ptr, b.data_ptr(), ld_b, b_t, sb_ptr, m, k, n, fmt, out.data_ptr(), ld_out,
+            _IO_FP32[out_dtype], _raw_stream(index))
+    fn = (_lib_handle or lib()).prm_matmul_q8
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_matmul_q8")
     return out
 
 

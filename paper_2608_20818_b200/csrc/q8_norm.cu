@@ -13,6 +13,8 @@
 // forms each: rows of octs (8 elements) held in registers, one row per block; for large matrices the
 // same arithmetic on rows streamed through shared memory; and single elements in two passes for rows
 // that are not aligned or longer than the registers of a block.
+#include <cooperative_groups.h>
+
 #include "row_ring.cuh"
 
 namespace prm {
@@ -235,6 +237,7 @@ struct NormGradArgs {
   const void* weight;
   const void* gh;         // may be null
   void* gx;
+  void* gw;
   float* part;            // [blocks][cols] partial sums of grad_w
   int64_t rows, ld_gy, ld_h, ld_gh, ld_gx;
   int cols, weight_fp32;
@@ -247,6 +250,33 @@ __device__ __forceinline__ void load_oct(const T* p, float2 (&v)[4]) {
   o.load(p);
   o.get(v);
 }
+// grad_w from the blocks' lines of partial sums, after a barrier of the whole (cooperative) grid: 32
+// columns per block and turn, each warp adds its share of the lines, all in a fixed order.
+template <int THREADS>
+__device__ __forceinline__ void grad_weight(const NormGradArgs& a) {
+  constexpr int kWarps = THREADS / 32;
+  __shared__ float s[kWarps][32];
+  cooperative_groups::this_grid().sync();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lines = gridDim.x;
+  for (int c0 = blockIdx.x * 32; c0 < a.cols; c0 += gridDim.x * 32) {
+    const int c = c0 + lane;
+    float sum = 0.f;
+    if (c < a.cols) {
+#pragma unroll 8
+      for (int l = warp; l < lines; l += kWarps) sum += __ldcg(a.part + (int64_t)l * a.cols + c);
+    }
+    s[warp][lane] = sum;
+    __syncthreads();
+    if (warp == 0 && c < a.cols) {
+#pragma unroll
+      for (int k = 1; k < kWarps; ++k) sum += s[k][lane];
+      if (a.weight_fp32) reinterpret_cast<float*>(a.gw)[c] = sum;
+      else reinterpret_cast<__nv_bfloat16*>(a.gw)[c] = __float2bfloat16_rn(sum);
+    }
+    __syncthreads();
+  }
+}
+
 // The two sums of a row over one oct.
 __device__ __forceinline__ void grad_sums(const float2 (&gy)[4], const float2 (&h)[4], const float2 (&w)[4],
                                           float2& ss, float2& gh) {
@@ -282,7 +312,8 @@ __device__ __forceinline__ void grad_oct(const float2 (&gy)[4], const float2 (&h
 }
 
 // A block walks over rows; a thread keeps the same columns in all of them, so its share of grad_w
-// stays in registers until the block's last row.
+// stays in registers until the block's last row.  One cooperative launch: the blocks' shares are added
+// behind a grid-wide barrier, which costs less than a second launch.
 template <typename IO, typename WT, int NV, int TPR>
 __global__ void __launch_bounds__(TPR) rmsnorm_q8_grad_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
@@ -349,6 +380,7 @@ __global__ void __launch_bounds__(TPR) rmsnorm_q8_grad_kernel(const NormGradArgs
       o.store(part + c);
     }
   }
+  grad_weight<TPR>(a);
 }
 
 // Large matrices: rows streamed through a ring and read from it twice (held in registers between the
@@ -430,6 +462,7 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
     for (int g = 0; g < kGroups; ++g) sum += sums[(size_t)g * a.cols + c];
     a.part[(int64_t)blockIdx.x * a.cols + c] = sum;
   }
+  grad_weight<kRingThreads<IO>>(a);
 }
 
 // Any alignment, any length: two passes over the row, and the block's share of grad_w collected in
@@ -465,68 +498,50 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_q8_grad_single_kernel(const N
       part[c] = row == (int64_t)blockIdx.x ? add : part[c] + add;
     }
   }
-}
-
-// grad_w: the parts added in a fixed order, 32 columns per block, a 32nd of the parts per warp.
-__global__ void __launch_bounds__(1024)
-rmsnorm_q8_grad_weight_kernel(const float* part, int parts, int cols, void* gw, int fp32) {
-  __shared__ float s[32][33];
-  grid_wait();
-  grid_trigger();
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
-  float sum = 0.f;
-  if (c < cols) {
-#pragma unroll 4
-    for (int p = k; p < parts; p += 32) sum += part[(int64_t)p * cols + c];
-  }
-  s[k][threadIdx.x & 31] = sum;
-  __syncthreads();
-  // column k of the block now lies in s[0..31][k]
-  sum = warp_sum(s[threadIdx.x & 31][k]);
-  const int out = blockIdx.x * 32 + k;
-  if ((threadIdx.x & 31) == 0 && out < cols) {
-    if (fp32) reinterpret_cast<float*>(gw)[out] = sum;
-    else reinterpret_cast<__nv_bfloat16*>(gw)[out] = __float2bfloat16_rn(sum);
-  }
+  grad_weight<THREADS>(a);
 }
 
 constexpr int kGradParts = 296;    // two blocks per SM
 
-int grad_parts(int64_t rows) { return (int)std::min<int64_t>(rows, kGradParts); }
-
 template <typename IO, typename WT, int W>
-int launch_grad_stream(const NormGradArgs& a, int* parts, cudaStream_t stream) {
-  constexpr int kGroups = kRingWarps<IO> / W;
-  *parts = ring_blocks(a.rows, kGroups);
+int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
   static PerDeviceOnce with, without;
-  const size_t sums = (size_t)kGroups * a.cols * 4;
-  return a.gh ? launch_ring<IO, W>(rmsnorm_q8_grad_stream_kernel<IO, WT, W, true>, 3, with, a.rows, a.cols, sums, stream, a)
-              : launch_ring<IO, W>(rmsnorm_q8_grad_stream_kernel<IO, WT, W, false>, 2, without, a.rows, a.cols, sums,
-                                   stream, a);
+  const size_t sums = (size_t)(kRingWarps<IO> / W) * a.cols * 4;
+  return a.gh ? launch_ring<IO, W, true>(rmsnorm_q8_grad_stream_kernel<IO, WT, W, true>, 3, with, a.rows, a.cols, sums,
+                                         stream, a)
+              : launch_ring<IO, W, true>(rmsnorm_q8_grad_stream_kernel<IO, WT, W, false>, 2, without, a.rows, a.cols,
+                                         sums, stream, a);
+}
+// `blocks`: how many of them an SM is sure to hold at once.
+int launch_grad(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int blocks, cudaStream_t stream) {
+  void* args[1] = {&a};
+  const unsigned grid = (unsigned)std::min<int64_t>(a.rows, blocks * kRingBlocks);
+  return cudaLaunchCooperativeKernel((const void*)kernel, dim3(grid), dim3((unsigned)threads), args, 0, stream) ==
+                 cudaSuccess
+             ? PRM_OK
+             : PRM_ERR_CUDA;
 }
 
 template <typename IO, typename WT>
-int run_grad(const NormGradArgs& a, int* parts, cudaStream_t stream) {
+int run_grad(const NormGradArgs& a, cudaStream_t stream) {
   const int c = a.cols;
   if (ring_worth(a.rows, c)) {
-    if (c <= 1024) return launch_grad_stream<IO, WT, 1>(a, parts, stream);
-    if (c <= 2048) return launch_grad_stream<IO, WT, 2>(a, parts, stream);
-    if (c <= 4096) return launch_grad_stream<IO, WT, 4>(a, parts, stream);
-    return launch_grad_stream<IO, WT, 8>(a, parts, stream);
+    if (c <= 1024) return launch_grad_stream<IO, WT, 1>(a, stream);
+    if (c <= 2048) return launch_grad_stream<IO, WT, 2>(a, stream);
+    if (c <= 4096) return launch_grad_stream<IO, WT, 4>(a, stream);
+    return launch_grad_stream<IO, WT, 8>(a, stream);
   }
-  if (c <= 256) launch_after(rmsnorm_q8_grad_kernel<IO, WT, 1, 32>, *parts, 32, 0, stream, 0, a);
-  else if (c <= 1024) launch_after(rmsnorm_q8_grad_kernel<IO, WT, 1, 128>, *parts, 128, 0, stream, 0, a);
-  else if (c <= 4096) launch_after(rmsnorm_q8_grad_kernel<IO, WT, 1, 512>, *parts, 512, 0, stream, 0, a);
-  else launch_after(rmsnorm_q8_grad_kernel<IO, WT, 2, 512>, *parts, 512, 0, stream, 0, a);
-  return PRM_OK;
+  if (c <= 256) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 32>, a, 32, 2, stream);
+  if (c <= 1024) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 128>, a, 128, 2, stream);
+  if (c <= 4096) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 512>, a, 512, 1, stream);
+  return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 2, 512>, a, 512, 1, stream);
 }
 
 template <typename IO>
-int run_grad_single(const NormGradArgs& a, int parts, cudaStream_t stream) {
-  if (a.cols <= 1024) launch_after(rmsnorm_q8_grad_single_kernel<IO, 128>, parts, 128, 0, stream, 0, a);
-  else if (a.cols <= 8192) launch_after(rmsnorm_q8_grad_single_kernel<IO, 512>, parts, 512, 0, stream, 0, a);
-  else launch_after(rmsnorm_q8_grad_single_kernel<IO, 1024>, parts, 1024, 0, stream, 0, a);
-  return PRM_OK;
+int run_grad_single(const NormGradArgs& a, cudaStream_t stream) {
+  if (a.cols <= 1024) return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 128>, a, 128, 2, stream);
+  if (a.cols <= 8192) return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 512>, a, 512, 2, stream);
+  return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 1024>, a, 1024, 1, stream);
 }
 
 bool ld_ok(int64_t ld) { return ld >= 0 && ld <= ((int64_t)1 << 40); }
@@ -567,7 +582,7 @@ extern "C" int prm_rmsnorm_q8(const void* x, int64_t ld_x, const void* residual,
 
 extern "C" size_t prm_rmsnorm_q8_scratch_bytes(int64_t rows, int64_t cols) {
   if (rows < 1 || cols < 1) return 0;
-  return (size_t)grad_parts(rows) * (size_t)cols * 4;
+  return (size_t)std::min<int64_t>(rows, kGradParts) * (size_t)cols * 4;
 }
 
 extern "C" int prm_rmsnorm_q8_backward(const void* grad_y, int64_t ld_grad_y, const void* h, int64_t ld_h,
@@ -591,19 +606,12 @@ extern "C" int prm_rmsnorm_q8_backward(const void* grad_y, int64_t ld_grad_y, co
   if (((uintptr_t)grad_y | (uintptr_t)h | (uintptr_t)grad_h | (uintptr_t)grad_x) % es != 0 ||
       (uintptr_t)weight % (weight_fp32 ? 4 : 2) != 0 || ((uintptr_t)scratch & 15) != 0)
     return PRM_ERR_ALIGN;
-  const NormGradArgs a = {grad_y, h,    weight,    grad_h,    grad_x,    (float*)scratch, rows,
-                          ld_grad_y, ld_h, ld_grad_h, ld_grad_x, (int)cols, weight_fp32,     eps};
+  const NormGradArgs a = {grad_y, h,         weight, grad_h,    grad_x,    grad_weight, (float*)scratch, rows,
+                          ld_grad_y, ld_h,   ld_grad_h, ld_grad_x, (int)cols, weight_fp32, eps};
   const bool octs = cols % 8 == 0 && cols <= 8192 && ld_grad_y % 8 == 0 && ld_h % 8 == 0 && ld_grad_x % 8 == 0 &&
                     aligned16(grad_y) && aligned16(h) && aligned16(grad_x) && aligned16(weight) &&
                     (!grad_h || (ld_grad_h % 8 == 0 && aligned16(grad_h)));
-  int parts = grad_parts(rows), code;
-  if (!octs) code = io_fp32 ? run_grad_single<float>(a, parts, stream) : run_grad_single<__nv_bfloat16>(a, parts, stream);
-  else if (io_fp32)
-    code = weight_fp32 ? run_grad<float, float>(a, &parts, stream) : run_grad<float, __nv_bfloat16>(a, &parts, stream);
-  else
-    code = weight_fp32 ? run_grad<__nv_bfloat16, float>(a, &parts, stream)
-                       : run_grad<__nv_bfloat16, __nv_bfloat16>(a, &parts, stream);
-  if (code != PRM_OK) return code;
-  launch_after(rmsnorm_q8_grad_weight_kernel, (unsigned)((cols + 31) / 32), 1024, 0, stream, 0, a.part, parts, (int)cols, grad_weight, weight_fp32);
-  return cudaGetLastError() == cudaSuccess ? PRM_OK : PRM_ERR_CUDA;
+  if (!octs) return io_fp32 ? run_grad_single<float>(a, stream) : run_grad_single<__nv_bfloat16>(a, stream);
+  if (io_fp32) return weight_fp32 ? run_grad<float, float>(a, stream) : run_grad<float, __nv_bfloat16>(a, stream);
+  return weight_fp32 ? run_grad<__nv_bfloat16, float>(a, stream) : run_grad<__nv_bfloat16, __nv_bfloat16>(a, stream);
 }

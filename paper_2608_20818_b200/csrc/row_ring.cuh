@@ -274,9 +274,9 @@ inline bool ring_worth(int64_t rows, int cols) { return cols >= 512 && cols <= 8
 inline int ring_blocks(int64_t rows, int groups) { return (int)std::min<int64_t>(kRingBlocks, (rows + groups - 1) / groups); }
 
 // One CTA per SM; `extra` bytes are what the kernel wants of the ring's memory after the last row.
-template <typename IO, int W, typename K, typename A>
-int launch_ring(K kernel, int arrays, PerDeviceOnce& once, int64_t rows, int cols, size_t extra, cudaStream_t stream,
-                const A& a) {
+template <typename IO, int W, bool COOPERATIVE = false, typename A>
+int launch_ring(void (*kernel)(A, int, int*), int arrays, PerDeviceOnce& once, int64_t rows, int cols, size_t extra, cudaStream_t stream,
+                A a) {
   constexpr int kGroups = kRingWarps<IO> / W;
   int dev;
   if (once.need(&dev)) {
@@ -288,10 +288,17 @@ int launch_ring(K kernel, int arrays, PerDeviceOnce& once, int64_t rows, int col
   const size_t row = (size_t)cols * sizeof(IO) * arrays * kGroups;
   const int stages = (int)std::min<size_t>(kRingStages, kRingBytes / row);
   if (!status || stages < 1 || extra > kRingBytes) return PRM_ERR_CUDA;
-  return launch_after(kernel, (unsigned)ring_blocks(rows, kGroups), kRingThreads<IO>, std::max(extra, row * stages),
-                      stream, 0, a, stages, status) == cudaSuccess
-             ? PRM_OK
-             : PRM_ERR_CUDA;
+  const unsigned blocks = (unsigned)ring_blocks(rows, kGroups);
+  const size_t smem = std::max(extra, row * stages);
+  cudaError_t e;
+  if constexpr (COOPERATIVE) {
+    int n = stages;
+    void* args[3] = {&a, &n, &status};
+    e = cudaLaunchCooperativeKernel((const void*)kernel, dim3(blocks), dim3(kRingThreads<IO>), args, smem, stream);
+  } else {
+    e = launch_after(kernel, blocks, kRingThreads<IO>, smem, stream, 0, a, stages, status);
+  }
+  return e == cudaSuccess ? PRM_OK : PRM_ERR_CUDA;
 }
 
 }  // namespace prm
