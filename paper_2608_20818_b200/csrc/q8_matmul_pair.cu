@@ -78,8 +78,18 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
 
 struct PairArgs {
   MatmulArgs c;
-  int m_tiles, tiles;
+  int m_tiles, n_tiles, tiles;
+  int band;               // m-tiles that are walked through together
 };
+
+// Order of the tiles: bands of `band` m-tiles, in a band n by n, m-tiles fastest.  Pairs that run at the
+// same time then share the band's rows of a and a few columns' worth of b.
+__device__ __forceinline__ void tile_origin(const PairArgs& a, int t, int& m0, int& n0) {
+  const int per = a.band * a.n_tiles, first = t / per * a.band, rest = t % per;
+  const int height = min(a.band, a.m_tiles - first);
+  m0 = (first + rest % height) * kTile;
+  n0 = rest / height * kTile;
+}
 
 template <bool INT8, bool P_MN, bool Q_MN>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -130,7 +140,10 @@ matmul_q8_pair_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_co
       bool ok = true;
       const uint32_t lead_full = cluster_map(smem_u32(&full[0]), 0);
       for (int t = pair; t < a.tiles && ok; t += pairs) {
-        const int n0 = (t / a.m_tiles) * kTile + (int)rank * 128, m0 = (t % a.m_tiles) * kTile + (int)rank * 128;
+        int m0, n0;
+        tile_origin(a, t, m0, n0);
+        m0 += (int)rank * 128;
+        n0 += (int)rank * 128;
         for (int kt = 0; kt < stages_k; ++kt, ++it) {
           const int s = it % kStages;
           if (!mbar_wait(&empty[s], ((it / kStages) & 1) ^ 1, abort_flag, status)) { ok = false; break; }
@@ -202,8 +215,10 @@ matmul_q8_pair_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_co
       const bool got = mbar_wait(&tfull[ab], (acc >> 1) & 1, abort_flag, status);
       if (!__all_sync(0xffffffffu, got)) break;
       tcgen05_after_sync();
-      const int n = (t / a.m_tiles) * kTile + (int)rank * 128 + col;
-      const int m0 = (t % a.m_tiles) * kTile + half * 128;
+      int m0, n0;
+      tile_origin(a, t, m0, n0);
+      const int n = n0 + (int)rank * 128 + col;
+      m0 += half * 128;
       const float sb = a.c.scale_b && n < a.c.n ? __ldg(a.c.scale_b + n) : 1.f;
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
@@ -271,7 +286,13 @@ int matmul_q8_pairs(const MatmulProblem& p) {
   PairArgs g = {};
   g.c = p.c;
   g.m_tiles = (p.c.m + kTile - 1) / kTile;
-  g.tiles = g.m_tiles * ((p.c.n + kTile - 1) / kTile);
+  g.n_tiles = (p.c.n + kTile - 1) / kTile;
+  g.tiles = g.m_tiles * g.n_tiles;
+  // As many m-tiles as keep their rows of a within 32 MB of the L2, at least 8 (a quarter of a wave).
+  // With all m-tiles in one band 8192 x 16384 x 4096, whose a alone is larger than the L2, reads a
+  // again for every wave.
+  const int64_t fit = ((int64_t)32 << 20) / ((int64_t)kTile * p.c.kblocks * kBlockK);
+  g.band = (int)std::min<int64_t>(g.m_tiles, std::max<int64_t>(8, fit));
   CUtensorMap mp, mq;
   if (!q8_make_map(&mp, p.b, p.b_rows, p.b_cols, p.ld_b, 128) ||
       !q8_make_map(&mq, p.a, p.a_rows, p.a_cols, p.ld_a, 128))
