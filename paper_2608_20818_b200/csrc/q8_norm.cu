@@ -107,7 +107,7 @@ rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
   const int c0 = (threadIdx.x % (W * 32)) * 8;
   const void* const src[2] = {a.x, a.residual};
   const int64_t ld[2] = {a.ld_x, a.ld_r};
-  RowRing<IO, W, kArr> ring(b, src, ld, a.rows, a.cols, stages, status);
+  RowRing<IO, W, kArr> ring(b, src, ld, (int)a.rows, a.cols, stages, status);
   ring.start();
   grid_wait();
   grid_trigger();
@@ -120,7 +120,7 @@ rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
     ring.finish();
     return;
   }
-  for (int64_t i = 0; i < ring.n; ++i) {
+  for (int i = 0; i < ring.n; ++i) {
     const int64_t row = ring.row(i);
     float2 t[kNV][4], sum2 = make_float2(0.f, 0.f);
     float top = 0.f;
@@ -394,7 +394,7 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
   const int c0 = (threadIdx.x % (W * 32)) * 8;
   const void* const src[3] = {a.gy, a.h, a.gh};
   const int64_t ld[3] = {a.ld_gy, a.ld_h, a.ld_gh};
-  RowRing<IO, W, kArr> ring(b, src, ld, a.rows, a.cols, stages, status);
+  RowRing<IO, W, kArr> ring(b, src, ld, (int)a.rows, a.cols, stages, status);
   float2 gw[kNV][4];
 #pragma unroll
   for (int v = 0; v < kNV; ++v)
@@ -404,8 +404,8 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
   grid_wait();
   grid_trigger();
   if (ring.producer) ring.serve();
-  const int64_t n = ring.producer ? 0 : ring.n;
-  for (int64_t i = 0; i < n; ++i) {
+  const int n = ring.producer ? 0 : ring.n;
+  for (int i = 0; i < n; ++i) {
     const int64_t row = ring.row(i);
     float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
     if (ring.wait()) {

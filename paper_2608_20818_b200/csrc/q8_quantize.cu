@@ -237,9 +237,9 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
   const int c0 = (threadIdx.x % (W * 32)) * 8;
   const void* const src[1] = {reinterpret_cast<const IO*>(a.x) + cbase};
   const int64_t ld[1] = {a.ld_x};
-  RowRing<IO, W, 1> ring(b, src, ld, a.rows, cols, stages, status);
-  ring.place(line, lines, a.rows);
-  __shared__ float slice[kThreads / 32][32];
+  RowRing<IO, W, 1> ring(b, src, ld, (int)a.rows, cols, stages, status);
+  ring.place(line, lines, (int)a.rows);
+  __shared__ float slice[kThreads / 32][128];
   float* tops = reinterpret_cast<float*>(ring_memory() + (size_t)(kRingWarps<IO> / W) * stages * ring.row_bytes);
   ring.start();
   float ct[kNV][8];
@@ -247,13 +247,13 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
   for (int v = 0; v < kNV; ++v)
 #pragma unroll
     for (int e = 0; e < 8; ++e) ct[v][e] = 0.f;
-  const int64_t n = ring.producer ? 0 : ring.n;
+  const int n = ring.producer ? 0 : ring.n;
   if (ring.producer) ring.serve();
-  for (int64_t i = 0; i < n; ++i) {
+  for (int i = 0; i < n; ++i) {
     const int64_t row = ring.row(i);
     const float fr = a.fold_rows ? __ldg(a.fold_rows + row) : 1.f;
     float2 t[kNV][4];
-    float none = 0.f, top = 0.f;
+    float top = 0.f;
     if (ring.wait()) {
 #pragma unroll
       for (int v = 0; v < kNV; ++v) {
@@ -279,7 +279,7 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
     ring.release();
     ring.advance();
     if constexpr (ROWS) {
-      ring.sum_top(i, none, top);
+      ring.max_top(i, top);
       if (ring.ok) {
         store_octs<kNV>(a.q_rows + row * a.ld_qr, t, c0, kStep, cols, top, a.format);
         if (c0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
@@ -315,25 +315,30 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
   }
   for (int c = threadIdx.x; c < cols; c += kThreads) a.part[(int64_t)blockIdx.x * a.panel + c] = tops[c];
   grid.sync();
-  // this block's slice of the panel's columns: 32 at a time, the lines dealt out to the warps
-  const int per = ((cols + lines - 1) / lines + 31) / 32 * 32;
+  // this block's slice of the panel's columns: 128 at a time, four per lane, the lines dealt out to
+  // the warps
+  const int per = ((cols + lines - 1) / lines + 31) / 32 * 32, end = min(cols, (line + 1) * per);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int s0 = line * per; s0 < min(cols, (line + 1) * per); s0 += 32) {
-    const int c = s0 + lane;
-    float m = 0.f;
-    if (c < cols) {
+  for (int s0 = line * per; s0 < end; s0 += 128) {
+    float m[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-      for (int l = warp; l < lines; l += kThreads / 32)
-        m = max_abs(m, make_float2(__ldcg(a.part + (int64_t)(l * a.panels + pan) * a.panel + c), 0.f));
-    }
-    slice[warp][lane] = m;
-    __syncthreads();
-    if (warp == 0 && c < cols) {
+    for (int l = warp; l < lines; l += kThreads / 32) {
+      const float* p = a.part + (int64_t)(l * a.panels + pan) * a.panel + s0 + lane;
 #pragma unroll
-      for (int k = 1; k < kThreads / 32; ++k) m = max_abs(m, make_float2(slice[k][lane], 0.f));
+      for (int k = 0; k < 4; ++k)
+        if (s0 + k * 32 + lane < end) m[k] = max_abs(m[k], make_float2(__ldcg(p + k * 32), 0.f));
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) slice[warp][k * 32 + lane] = m[k];
+    __syncthreads();
+    const int c = s0 + threadIdx.x;
+    if (threadIdx.x < 128 && c < end) {
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < kThreads / 32; ++k) top = max_abs(top, make_float2(slice[k][threadIdx.x], 0.f));
       // a column without a number for a scale passes on a NaN, and gets zero codes
-      reinterpret_cast<float*>(a.top)[cbase + c] = q8_finite(m) ? q8_mul(m, q8_limit(a.format)) : m - m;
-      a.scale_cols[cbase + c] = q8_scale(m, q8_limit(a.format));
+      reinterpret_cast<float*>(a.top)[cbase + c] = q8_finite(top) ? q8_mul(top, q8_limit(a.format)) : top - top;
+      a.scale_cols[cbase + c] = q8_scale(top, q8_limit(a.format));
     }
     __syncthreads();
   }
@@ -363,7 +368,7 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
     }
   ring.turn_back();
   if (ring.producer) ring.serve_back();
-  for (int64_t i = n - 1; i >= 0; --i) {
+  for (int i = n - 1; i >= 0; --i) {
     const int64_t row = ring.row(i);
     const float fr = a.fold_rows ? __ldg(a.fold_rows + row) : 1.f;
     Oct<IO> x[kNV];

@@ -30,6 +30,19 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
       : "memory");
 }
+// Whether a phase is complete, without the suspension that mbarrier.try_wait may put in: the producer's
+// lanes wait for barriers of their own and none may hold up the others.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ uint8_t* ring_memory() {
   extern __shared__ __align__(128) uint8_t ring_mem[];
   return ring_mem;
@@ -57,16 +70,17 @@ struct RowRing {
   RingBlock<IO, W, ARR>& b;
   const IO* src[ARR];
   int64_t ld[ARR];
-  int64_t first, step, n;
+  int first, step, n;     // rows (below 2^31)
   uint8_t* base;          // [stages][ARR][row_bytes]
   uint32_t row_bytes;
   int stages, group, stage;
   uint32_t phase;
+  int laps, last;         // of the walk back: (n - 1) / stages and its remainder
   bool producer, ok;
   int* status;
 
   __device__ __forceinline__ RowRing(RingBlock<IO, W, ARR>& block, const void* const* srcs, const int64_t* lds,
-                                     int64_t rows, int cols, int n_stages, int* status_word)
+                                     int rows, int cols, int n_stages, int* status_word)
       : b(block), stages(n_stages), stage(0), phase(0), ok(true), status(status_word) {
     constexpr int kGroups = kRingWarps<IO> / W;
     producer = threadIdx.x >= kRingWarps<IO> * 32;
@@ -81,17 +95,17 @@ struct RowRing {
     place(blockIdx.x, gridDim.x, rows);
   }
   // The rows of a block that is number `line` of `lines`.
-  __device__ __forceinline__ void place(int line, int lines, int64_t rows) {
+  __device__ __forceinline__ void place(int line, int lines, int rows) {
     constexpr int kGroups = kRingWarps<IO> / W;
-    first = (int64_t)line * kGroups + group;
-    step = (int64_t)lines * kGroups;
-    n = group < kGroups && first < rows ? (rows - first + step - 1) / step : 0;
+    first = line * kGroups + group;
+    step = lines * kGroups;
+    n = group < kGroups && first < rows ? (rows - first - 1) / step + 1 : 0;
   }
-  __device__ __forceinline__ int64_t row(int64_t i) const { return first + i * step; }
+  __device__ __forceinline__ int64_t row(int i) const { return first + (int64_t)i * step; }
   __device__ __forceinline__ const IO* at(int k) const {
     return reinterpret_cast<const IO*>(base + ((size_t)stage * ARR + k) * row_bytes);
   }
-  __device__ __forceinline__ void fetch(int64_t i, int s) const {
+  __device__ __forceinline__ void fetch(int i, int s) const {
     const int64_t r = row(i);
     mbar_expect_tx(&b.full[group][s], ARR * row_bytes);
 #pragma unroll
@@ -112,18 +126,17 @@ struct RowRing {
   }
   // The producer's lanes, each for its group: rows 0 .. n - 1.  No lane waits for another's row.
   __device__ __forceinline__ void serve() {
-    int64_t i = 0;
-    uint64_t t0 = global_ns();
+    int i = 0;
+    Patience p;
     while (__any_sync(0xffffffffu, ok && i < n)) {
       if (ok && i < n) {
-        const bool room = i < stages || mbar_try_wait(&b.empty[group][stage], phase ^ 1);
-        if (room) {
+        if (i < stages || mbar_test(&b.empty[group][stage], phase ^ 1)) {
           fetch(i, stage);
           ++i;
           advance();
-          t0 = global_ns();
+          p = Patience();
         } else {
-          gave_up(t0);
+          lose(p);
         }
       }
     }
@@ -134,9 +147,17 @@ struct RowRing {
       phase ^= 1;
     }
   }
-  __device__ __forceinline__ void gave_up(uint64_t t0) {
+  // One more poll without success: every 256th looks at the clock and at the others.
+  struct Patience {
+    uint32_t polls = 0;
+    uint64_t t0 = 0;
+  };
+  __device__ __forceinline__ void lose(Patience& p) {
+    if ((++p.polls & 255u) != 0) return;
+    const uint64_t now = global_ns();
+    if (p.t0 == 0) p.t0 = now;
     if (*(volatile int*)&b.abort_word) ok = false;
-    if (global_ns() - t0 > kWaitLimitNs) {
+    if (now - p.t0 > kWaitLimitNs) {
       ok = false;
       *(volatile int*)&b.abort_word = 1;
       atomicOr(status, kStatusTimeout);
@@ -160,30 +181,36 @@ struct RowRing {
   // A second walk over the same rows, last row first.  The last `stages` rows are still in the ring;
   // the others are sent for again as their stages fall free.  Between the two walks lies a barrier of
   // the block.  wait_back(i) / release() / retreat() go with i = n - 1, ..., 0.
-  __device__ __forceinline__ void turn_back() { stage = n > 0 ? (int)((n - 1) % stages) : 0; }
-  // Copies into (and releases of) the current stage on the way out.
-  __device__ __forceinline__ int64_t outward() const { return (n - 1 - stage) / stages + 1; }
-  __device__ __forceinline__ bool wait_back(int64_t i) {
-    if (i < n - stages) {
-      const int64_t copies = outward() + (n - 1 - i) / stages;
-      ok = ok && mbar_wait(&b.full[group][stage], (uint32_t)(copies - 1) & 1u, &b.abort_word, status);
-    }
+  __device__ __forceinline__ void turn_back() {
+    laps = n > 0 ? (n - 1) / stages : 0;
+    last = stage = n > 0 ? (n - 1) % stages : 0;
+    phase = 0;
+  }
+  // Copies into (and releases of) the current stage on the way out, plus the laps since.
+  __device__ __forceinline__ uint32_t fills() const { return (uint32_t)laps + (stage <= last ? 1u : 0u) + phase; }
+  __device__ __forceinline__ bool wait_back(int i) {
+    if (i < n - stages)
+      ok = ok && mbar_wait(&b.full[group][stage], (fills() - 1) & 1u, &b.abort_word, status);
     return ok;
   }
-  __device__ __forceinline__ void retreat() { stage = stage == 0 ? stages - 1 : stage - 1; }
+  __device__ __forceinline__ void retreat() {
+    if (stage == 0) stage = stages;
+    --stage;
+    if (stage == last) ++phase;             // laps of the walk back
+  }
   __device__ __forceinline__ void serve_back() {
-    int64_t i = n - 1 - stages;             // row i takes the stage of row i + stages
-    uint64_t t0 = global_ns();
+    int i = n - 1 - stages;                 // row i takes the stage of row i + stages
+    phase = 1;
+    Patience p;
     while (__any_sync(0xffffffffu, ok && i >= 0)) {
       if (ok && i >= 0) {
-        const int64_t releases = outward() + (n - 1 - i) / stages;
-        if (mbar_try_wait(&b.empty[group][stage], (uint32_t)(releases - 1) & 1u)) {
+        if (mbar_test(&b.empty[group][stage], (fills() - 1) & 1u)) {
           fetch(i, stage);
           --i;
           retreat();
-          t0 = global_ns();
+          p = Patience();
         } else {
-          gave_up(t0);
+          lose(p);
         }
       }
     }
@@ -205,7 +232,7 @@ struct RowRing {
     }
     return w;
   }
-  __device__ __forceinline__ void sum2(int64_t i, float& p, float& q) const {
+  __device__ __forceinline__ void sum2(int i, float& p, float& q) const {
     p = warp_sum(p);
     q = warp_sum(q);
     if constexpr (W > 1) {
@@ -228,7 +255,22 @@ struct RowRing {
       }
     }
   }
-  __device__ __forceinline__ void sum_top(int64_t i, float& p, float& top) const {
+  __device__ __forceinline__ void max_top(int i, float& top) const {
+    top = warp_top(top);
+    if constexpr (W > 1) {
+      float* red = b.red[group][i & 1];
+      if ((threadIdx.x & 31) == 0) red[(threadIdx.x >> 5) % W] = top;
+      sync();
+      top = 0.f;
+#pragma unroll
+      for (int k = 0; k < W; k += kPiece) {
+        const auto v = words(red + k);
+#pragma unroll
+        for (int e = 0; e < kPiece; e += 2) top = max_abs(top, make_float2(v[e], v[e + 1]));
+      }
+    }
+  }
+  __device__ __forceinline__ void sum_top(int i, float& p, float& top) const {
     p = warp_sum(p);
     top = warp_top(top);
     if constexpr (W > 1) {
