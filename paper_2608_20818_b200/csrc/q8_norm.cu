@@ -34,6 +34,12 @@ struct NormArgs {
 
 __device__ __forceinline__ float inv_rms(float sum, int cols, float eps) { return 1.f / sqrtf(sum / (float)cols + eps); }
 
+template <typename T>
+__device__ __forceinline__ void load_oct(const T* p, float2 (&v)[4]) {
+  Oct<T> o;
+  o.load(p);
+  o.get(v);
+}
 // h (= x, plus r if RES, rounded to the stream's type and stored), t = h * w, sum of squares and top.
 template <typename IO, bool RES>
 __device__ __forceinline__ void norm_oct(Oct<IO> x, Oct<IO> r, const float2 (&w)[4], IO* h_out, float2 (&t)[4],
@@ -78,6 +84,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const
     if (c < a.cols) {
       xv[v].load_stream(x + c);
       if constexpr (RES) rv[v].load_stream(r + c);
+      else rv[v].zero();
       wv[v].load(reinterpret_cast<const WT*>(a.weight) + c);
     }
   }
@@ -98,32 +105,32 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const
   if (c0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
 }
 
-// Large matrices: rows streamed through a ring, a group of W warps each.
+constexpr int kNormOcts = 4;              // per thread and row in the streaming kernel
+
+// Large matrices: rows streamed through a ring, a group of W warps to a row.
 template <typename IO, typename WT, int W, bool RES>
-__global__ void __launch_bounds__(kRingThreads<IO>, 1)
-rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
-  constexpr int kArr = RES ? 2 : 1, kNV = 4, kStep = W * 32 * 8;
-  RingBlock<IO, W, kArr>& b = ring_block<IO, W, kArr>();
+__global__ void __launch_bounds__(kRingThreads, 1) rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
+  constexpr int kArr = RES ? 2 : 1, kNV = kNormOcts, kStep = W * 32 * 8;
   const int c0 = (threadIdx.x % (W * 32)) * 8;
   const void* const src[2] = {a.x, a.residual};
   const int64_t ld[2] = {a.ld_x, a.ld_r};
-  RowRing<IO, W, kArr> ring(b, src, ld, (int)a.rows, a.cols, stages, status);
+  RowRing<IO, W, 1, kArr> ring(ring_block<W, 1>(), src, ld, a.rows, a.cols, stages, status);
   ring.start();
   grid_wait();
   grid_trigger();
-  Oct<WT> wv[kNV];
-#pragma unroll
-  for (int v = 0; v < kNV; ++v)
-    if (c0 + v * kStep < a.cols) wv[v].load(reinterpret_cast<const WT*>(a.weight) + c0 + v * kStep);
   if (ring.producer) {
     ring.serve();
     ring.finish();
     return;
   }
+  Oct<WT> wv[kNV];
+#pragma unroll
+  for (int v = 0; v < kNV; ++v)
+    if (c0 + v * kStep < a.cols) wv[v].load(reinterpret_cast<const WT*>(a.weight) + c0 + v * kStep);
   for (int i = 0; i < ring.n; ++i) {
     const int64_t row = ring.row(i);
     float2 t[kNV][4], sum2 = make_float2(0.f, 0.f);
-    float top = 0.f;
+    float sum[1], top[1] = {0.f};
     if (ring.wait()) {
       IO* h = RES ? reinterpret_cast<IO*>(a.h) + row * a.ld_h : nullptr;
 #pragma unroll
@@ -132,20 +139,21 @@ rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
         if (c < a.cols) {
           Oct<IO> x, r;
           float2 w[4];
-          x.load(ring.at(0) + c);
-          if constexpr (RES) r.load(ring.at(1) + c);
+          x.load(ring.at(0, 0) + c);
+          if constexpr (RES) r.load(ring.at(0, 1) + c);
+          else r.zero();
           wv[v].get(w);
-          norm_oct<IO, RES>(x, r, w, h + c, t[v], sum2, top);
+          norm_oct<IO, RES>(x, r, w, h + c, t[v], sum2, top[0]);
         }
       }
     }
     ring.release();
     ring.advance();
-    float sum = sum2.x + sum2.y;
-    ring.sum_top(i, sum, top);
+    sum[0] = sum2.x + sum2.y;
+    ring.template reduce<true, false>(i, sum, top);
     if (ring.ok) {
-      store_octs<kNV>(a.q + row * a.ld_q, t, c0, kStep, a.cols, top, a.format);
-      if (c0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
+      store_octs<kNV>(a.q + row * a.ld_q, t, c0, kStep, a.cols, top[0], a.format);
+      if (c0 == 0) a.scale[row] = q8_scale(top[0], q8_limit(a.format)) * inv_rms(sum[0], a.cols, a.eps);
     }
   }
 }
@@ -193,25 +201,22 @@ int launch_norm(const NormArgs& a, cudaStream_t stream) {
   return PRM_OK;
 }
 
-template <typename IO, typename WT, int W>
+template <typename IO, typename WT, int W, bool RES>
 int launch_norm_stream(const NormArgs& a, cudaStream_t stream) {
-  auto go = [&](auto kernel, int arrays, PerDeviceOnce& once) {
-    return launch_ring<IO, W>(kernel, arrays, once, a.rows, a.cols, 0, stream, a);
-  };
-  static PerDeviceOnce with, without;
-  return a.residual ? go(rmsnorm_q8_stream_kernel<IO, WT, W, true>, 2, with)
-                    : go(rmsnorm_q8_stream_kernel<IO, WT, W, false>, 1, without);
+  constexpr int kGroups = kRingWarps / W;
+  static PerDeviceOnce once;
+  return launch_ring(rmsnorm_q8_stream_kernel<IO, WT, W, RES>, once, ring_blocks(a.rows, 1, kGroups),
+                     (size_t)a.cols * sizeof(IO) * (RES ? 2 : 1) * kGroups, 0, 0, false, stream, a);
 }
 
 template <typename IO, typename WT>
 int run_norm(const NormArgs& a, cudaStream_t stream) {
   const int c = a.cols;
-  if (ring_worth(a.rows, c)) {
-    if (c <= 1024) return launch_norm_stream<IO, WT, 1>(a, stream);
-    if (c <= 2048) return launch_norm_stream<IO, WT, 2>(a, stream);
-    if (c <= 4096) return launch_norm_stream<IO, WT, 4>(a, stream);
-    return launch_norm_stream<IO, WT, 8>(a, stream);
-  }
+  if (ring_worth(a.rows, c))
+    return with_ring_warps<kNormOcts>(c, [&](auto w) {
+      return a.residual ? launch_norm_stream<IO, WT, decltype(w)::value, true>(a, stream)
+                        : launch_norm_stream<IO, WT, decltype(w)::value, false>(a, stream);
+    });
   if (c <= 256) return launch_norm<IO, WT, 1, 32>(a, stream);
   if (c <= 512) return launch_norm<IO, WT, 2, 32>(a, stream);
   if (c <= 1024) return launch_norm<IO, WT, 1, 128>(a, stream);
@@ -244,12 +249,6 @@ struct NormGradArgs {
   float eps;
 };
 
-template <typename T>
-__device__ __forceinline__ void load_oct(const T* p, float2 (&v)[4]) {
-  Oct<T> o;
-  o.load(p);
-  o.get(v);
-}
 // grad_w from the blocks' lines of partial sums, after a barrier of the whole (cooperative) grid: 32
 // columns per block and turn, each warp adds its share of the lines, all in a fixed order.
 template <int THREADS>
@@ -383,60 +382,71 @@ __global__ void __launch_bounds__(TPR) rmsnorm_q8_grad_kernel(const NormGradArgs
   grad_weight<TPR>(a);
 }
 
-// Large matrices: rows streamed through a ring and read from it twice (held in registers between the
-// sums and the outputs they would spill).  The groups' shares of grad_w meet in the ring's
+// Large matrices: rows streamed through a ring.  The groups' shares of grad_w meet in the ring's
 // memory at the end, so that a block leaves one line of partial sums.
 template <typename IO, typename WT, int W, bool GH>
-__global__ void __launch_bounds__(kRingThreads<IO>, 1)
+__global__ void __launch_bounds__(kRingThreads, 1)
 rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
-  constexpr int kArr = GH ? 3 : 2, kNV = 4, kStep = W * 32 * 8, kGroups = kRingWarps<IO> / W;
-  RingBlock<IO, W, kArr>& b = ring_block<IO, W, kArr>();
+  constexpr int kArr = GH ? 3 : 2, kNV = 2, kR = kRingRows<IO>, kStep = W * 32 * 8, kGroups = kRingWarps / W;
   const int c0 = (threadIdx.x % (W * 32)) * 8;
   const void* const src[3] = {a.gy, a.h, a.gh};
   const int64_t ld[3] = {a.ld_gy, a.ld_h, a.ld_gh};
-  RowRing<IO, W, kArr> ring(b, src, ld, (int)a.rows, a.cols, stages, status);
-  float2 gw[kNV][4];
+  RowRing<IO, W, kR, kArr> ring(ring_block<W, kR>(), src, ld, a.rows, a.cols, stages, status);
+  float2 gw[kNV][4], w[kNV][4];
 #pragma unroll
-  for (int v = 0; v < kNV; ++v)
+  for (int v = 0; v < kNV; ++v) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) gw[v][e] = make_float2(0.f, 0.f);
+    if (c0 + v * kStep < a.cols) load_oct(reinterpret_cast<const WT*>(a.weight) + c0 + v * kStep, w[v]);
+  }
   ring.start();
-  grid_wait();
-  grid_trigger();
   if (ring.producer) ring.serve();
   const int n = ring.producer ? 0 : ring.n;
   for (int i = 0; i < n; ++i) {
     const int64_t row = ring.row(i);
-    float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
+    const int high = ring.height(i);
+    float2 gy[kR][kNV][4];                // h is read again: both would spill
+    float ss[kR], gh[kR];
+#pragma unroll
+    for (int r = 0; r < kR; ++r) ss[r] = gh[r] = 0.f;
     if (ring.wait()) {
 #pragma unroll
-      for (int v = 0; v < kNV; ++v) {
-        const int c = c0 + v * kStep;
-        if (c < a.cols) {
-          float2 gy[4], h[4], w[4];
-          load_oct(reinterpret_cast<const WT*>(a.weight) + c, w);
-          load_oct(ring.at(0) + c, gy);
-          load_oct(ring.at(1) + c, h);
-          grad_sums(gy, h, w, ss2, gh2);
+      for (int r = 0; r < kR; ++r) {
+        if (r < high) {
+          float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
+#pragma unroll
+          for (int v = 0; v < kNV; ++v) {
+            const int c = c0 + v * kStep;
+            if (c < a.cols) {
+              float2 h[4];
+              load_oct(ring.at(r, 0) + c, gy[r][v]);
+              load_oct(ring.at(r, 1) + c, h);
+              grad_sums(gy[r][v], h, w[v], ss2, gh2);
+            }
+          }
+          ss[r] = ss2.x + ss2.y;
+          gh[r] = gh2.x + gh2.y;
         }
       }
     }
-    float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
-    ring.sum2(i, ss, gh);
+    ring.template reduce<true, true>(i, ss, gh);
     if (ring.ok) {
-      const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
-      IO* gxp = reinterpret_cast<IO*>(a.gx) + row * a.ld_gx;
 #pragma unroll
-      for (int v = 0; v < kNV; ++v) {
-        const int c = c0 + v * kStep;
-        if (c < a.cols) {
-          float2 gy[4], h[4], w[4];
-          Oct<IO> add;
-          load_oct(reinterpret_cast<const WT*>(a.weight) + c, w);
-          load_oct(ring.at(0) + c, gy);
-          load_oct(ring.at(1) + c, h);
-          if constexpr (GH) add.load(ring.at(2) + c);
-          grad_oct<IO>(gy, h, w, GH ? &add : nullptr, s, k, gxp + c, gw[v]);
+      for (int r = 0; r < kR; ++r) {
+        if (r < high) {
+          const float s = inv_rms(ss[r], a.cols, a.eps), k = s * s * s * (gh[r] / (float)a.cols);
+          IO* gxp = reinterpret_cast<IO*>(a.gx) + (row + r) * a.ld_gx;
+#pragma unroll
+          for (int v = 0; v < kNV; ++v) {
+            const int c = c0 + v * kStep;
+            if (c < a.cols) {
+              Oct<IO> add;
+              float2 h[4];
+              load_oct(ring.at(r, 1) + c, h);
+              if constexpr (GH) add.load(ring.at(r, 2) + c);
+              grad_oct<IO>(gy[r][v], h, w[v], GH ? &add : nullptr, s, k, gxp + c, gw[v]);
+            }
+          }
         }
       }
     }
@@ -456,13 +466,13 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
     }
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < a.cols; c += kRingThreads<IO>) {
+  for (int c = threadIdx.x; c < a.cols; c += kRingThreads) {
     float sum = 0.f;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) sum += sums[(size_t)g * a.cols + c];
     a.part[(int64_t)blockIdx.x * a.cols + c] = sum;
   }
-  grad_weight<kRingThreads<IO>>(a);
+  grad_weight<kRingThreads>(a);
 }
 
 // Any alignment, any length: two passes over the row, and the block's share of grad_w collected in
@@ -503,14 +513,13 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_q8_grad_single_kernel(const N
 
 constexpr int kGradParts = 296;    // two blocks per SM
 
-template <typename IO, typename WT, int W>
+template <typename IO, typename WT, int W, bool GH>
 int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
-  static PerDeviceOnce with, without;
-  const size_t sums = (size_t)(kRingWarps<IO> / W) * a.cols * 4;
-  return a.gh ? launch_ring<IO, W, true>(rmsnorm_q8_grad_stream_kernel<IO, WT, W, true>, 3, with, a.rows, a.cols, sums,
-                                         stream, a)
-              : launch_ring<IO, W, true>(rmsnorm_q8_grad_stream_kernel<IO, WT, W, false>, 2, without, a.rows, a.cols,
-                                         sums, stream, a);
+  constexpr int kGroups = kRingWarps / W, kR = kRingRows<IO>;
+  static PerDeviceOnce once;
+  return launch_ring(rmsnorm_q8_grad_stream_kernel<IO, WT, W, GH>, once, ring_blocks(a.rows, kR, kGroups),
+                     (size_t)a.cols * sizeof(IO) * (GH ? 3 : 2) * kR * kGroups, 0, (size_t)kGroups * a.cols * 4, true,
+                     stream, a);
 }
 // `blocks`: how many of them an SM is sure to hold at once.
 int launch_grad(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int blocks, cudaStream_t stream) {
@@ -525,12 +534,11 @@ int launch_grad(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int b
 template <typename IO, typename WT>
 int run_grad(const NormGradArgs& a, cudaStream_t stream) {
   const int c = a.cols;
-  if (ring_worth(a.rows, c)) {
-    if (c <= 1024) return launch_grad_stream<IO, WT, 1>(a, stream);
-    if (c <= 2048) return launch_grad_stream<IO, WT, 2>(a, stream);
-    if (c <= 4096) return launch_grad_stream<IO, WT, 4>(a, stream);
-    return launch_grad_stream<IO, WT, 8>(a, stream);
-  }
+  if (ring_worth(a.rows, c))
+    return with_ring_warps<2>(c, [&](auto w) {
+      return a.gh ? launch_grad_stream<IO, WT, decltype(w)::value, true>(a, stream)
+                  : launch_grad_stream<IO, WT, decltype(w)::value, false>(a, stream);
+    });
   if (c <= 256) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 32>, a, 32, 2, stream);
   if (c <= 1024) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 128>, a, 128, 2, stream);
   if (c <= 4096) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 512>, a, 512, 1, stream);

@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kColThreads) quantize_cols_kernel(const QuantA
 // A thread's share of one row of codes by column.
 template <typename IO, int NV, int FORMAT>
 __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], const float2 (&mul)[NV][4], float fr,
-                                         uint32_t odd, int c0, int step, int cols) {
+                                         bool odd, int c0, int step, int cols) {
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = c0 + v * step;
@@ -206,7 +206,7 @@ __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], con
       x[v].get(t);
 #pragma unroll
       for (int e = 0; e < 4; ++e) t[e] = mul2(t[e], make_float2(fr, fr));
-      if (odd == 0) {
+      if (!odd) {
         *reinterpret_cast<uint2*>(q + c) = column_codes<FORMAT>(t, mul[v]);
       } else {
         float2 m[4];
@@ -223,55 +223,76 @@ __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], con
 }
 
 // The streaming kernel.  Blocks with the same blockIdx % panels work on the same panel of columns;
-// with codes by row there is one panel, the whole width.  Phase 1: groups of W warps walk over rows.
-// Then the blocks' column maxima are joined (shared memory, scratch, a slice of the columns per block)
-// between two grid-wide barriers of the cooperative launch.  Phase 2 walks back.
-template <typename IO, int W, bool ROWS>
-__global__ void __launch_bounds__(kRingThreads<IO>, 1)
-quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
-  constexpr int kNV = 4, kStep = W * 32 * 8, kThreads = kRingThreads<IO>;
-  RingBlock<IO, W, 1>& b = ring_block<IO, W, 1>();
+// with codes by row there is one panel, the whole width.  Phase 1: groups of W warps walk over sets of
+// R rows, NV octs per thread and row.  Then the blocks' column maxima are joined (shared memory, scratch,
+// a slice of the columns per block) between two grid-wide barriers of the cooperative launch.  Phase 2
+// walks back.
+template <typename IO, int W, int NV, int R, bool ROWS>
+__global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
+  constexpr int kStep = W * 32 * 8;
+  __shared__ float slice[kRingThreads / 32][128];
   const int pan = blockIdx.x % a.panels, line = blockIdx.x / a.panels;
   const int lines = ((int)gridDim.x - pan + a.panels - 1) / a.panels;   // blocks of this panel
   const int cbase = pan * a.panel, cols = min(a.panel, a.cols - cbase);
   const int c0 = (threadIdx.x % (W * 32)) * 8;
   const void* const src[1] = {reinterpret_cast<const IO*>(a.x) + cbase};
   const int64_t ld[1] = {a.ld_x};
-  RowRing<IO, W, 1> ring(b, src, ld, (int)a.rows, cols, stages, status);
-  ring.place(line, lines, (int)a.rows);
-  __shared__ float slice[kThreads / 32][128];
-  float* tops = reinterpret_cast<float*>(ring_memory() + (size_t)(kRingWarps<IO> / W) * stages * ring.row_bytes);
+  RowRing<IO, W, R, 1> ring(ring_block<W, R>(), src, ld, a.rows, cols, stages, status);
+  ring.place(line, lines);
+  float* tops = reinterpret_cast<float*>(ring_memory() + (size_t)(kRingWarps / W) * stages * R * ring.row_bytes);
   ring.start();
-  float ct[kNV][8];
+  float ct[NV][8];
 #pragma unroll
-  for (int v = 0; v < kNV; ++v)
+  for (int v = 0; v < NV; ++v)
 #pragma unroll
     for (int e = 0; e < 8; ++e) ct[v][e] = 0.f;
   const int n = ring.producer ? 0 : ring.n;
   if (ring.producer) ring.serve();
   for (int i = 0; i < n; ++i) {
     const int64_t row = ring.row(i);
-    const float fr = a.fold_rows ? __ldg(a.fold_rows + row) : 1.f;
-    float2 t[kNV][4];
-    float top = 0.f;
+    const int h = ring.height(i);
+    float fr[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) fr[r] = a.fold_rows && r < h ? __ldg(a.fold_rows + row + r) : 1.f;
+    float2 t[R][NV][4];
+    float none[R], top[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) none[r] = top[r] = 0.f;
     if (ring.wait()) {
 #pragma unroll
-      for (int v = 0; v < kNV; ++v) {
+      for (int v = 0; v < NV; ++v) {
         const int c = c0 + v * kStep;
         if (c < cols) {
-          Oct<IO> x;
-          x.load(ring.at(0) + c);
-          x.get(t[v]);
+          float2 f[R][4];
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            Oct<IO> x;
+            if (r < h) x.load(ring.at(r, 0) + c);
+            else x.zero();
+            x.get(t[r][v]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[r][e] = mul2(t[r][v][e], make_float2(fr[r], fr[r]));
+          }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float2 f = mul2(t[v][e], make_float2(fr, fr));
-            ct[v][2 * e] = max_abs(ct[v][2 * e], make_float2(f.x, 0.f));
-            ct[v][2 * e + 1] = max_abs(ct[v][2 * e + 1], make_float2(f.y, 0.f));
+            ct[v][2 * e] = max_abs(ct[v][2 * e], make_float2(f[0][e].x, f[R - 1][e].x));
+            ct[v][2 * e + 1] = max_abs(ct[v][2 * e + 1], make_float2(f[0][e].y, f[R - 1][e].y));
           }
           if constexpr (ROWS) {
-            fold_oct(a.fold_cols, c, t[v]);
+            if (a.fold_cols) {
+              float2 fc[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) top = max_abs(top, t[v][e]);
+              for (int e = 0; e < 4; ++e)
+                fc[e] = make_float2(__ldg(a.fold_cols + c + 2 * e), __ldg(a.fold_cols + c + 2 * e + 1));
+#pragma unroll
+              for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[r][v][e] = mul2(t[r][v][e], fc[e]);
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) top[r] = max_abs(top[r], t[r][v][e]);
           }
         }
       }
@@ -279,19 +300,24 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
     ring.release();
     ring.advance();
     if constexpr (ROWS) {
-      ring.max_top(i, top);
+      ring.template reduce<false, false>(i, none, top);
       if (ring.ok) {
-        store_octs<kNV>(a.q_rows + row * a.ld_qr, t, c0, kStep, cols, top, a.format);
-        if (c0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (r < h) {
+            store_octs<NV>(a.q_rows + (row + r) * a.ld_qr, t[r], c0, kStep, cols, top[r], a.format);
+            if (c0 == 0) a.scale_rows[row + r] = q8_scale(top[r], q8_limit(a.format));
+          }
+        }
       }
     }
   }
   cooperative_groups::grid_group grid = cooperative_groups::this_grid();
   grid_trigger();
-  for (int g = 0; g < kRingWarps<IO> / W; ++g) {      // the groups take turns
+  for (int g = 0; g < kRingWarps / W; ++g) {          // the groups take turns
     if (!ring.producer && ring.group == g) {
 #pragma unroll
-      for (int v = 0; v < kNV; ++v) {
+      for (int v = 0; v < NV; ++v) {
         const int c = c0 + v * kStep;
         if (c < cols) {
           Oct<float> o;
@@ -313,7 +339,7 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
     }
     __syncthreads();
   }
-  for (int c = threadIdx.x; c < cols; c += kThreads) a.part[(int64_t)blockIdx.x * a.panel + c] = tops[c];
+  for (int c = threadIdx.x; c < cols; c += kRingThreads) a.part[(int64_t)blockIdx.x * a.panel + c] = tops[c];
   grid.sync();
   // this block's slice of the panel's columns: 128 at a time, four per lane, the lines dealt out to
   // the warps
@@ -322,7 +348,7 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
   for (int s0 = line * per; s0 < end; s0 += 128) {
     float m[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int l = warp; l < lines; l += kThreads / 32) {
+    for (int l = warp; l < lines; l += kRingThreads / 32) {
       const float* p = a.part + (int64_t)(l * a.panels + pan) * a.panel + s0 + lane;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -335,7 +361,7 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
     if (threadIdx.x < 128 && c < end) {
       float top = 0.f;
 #pragma unroll
-      for (int k = 0; k < kThreads / 32; ++k) top = max_abs(top, make_float2(slice[k][threadIdx.x], 0.f));
+      for (int k = 0; k < kRingThreads / 32; ++k) top = max_abs(top, make_float2(slice[k][threadIdx.x], 0.f));
       // a column without a number for a scale passes on a NaN, and gets zero codes
       reinterpret_cast<float*>(a.top)[cbase + c] = q8_finite(top) ? q8_mul(top, q8_limit(a.format)) : top - top;
       a.scale_cols[cbase + c] = q8_scale(top, q8_limit(a.format));
@@ -345,9 +371,9 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
   grid.sync();
   // All factors of this thread's columns are fetched before the first is used, in 16-byte pieces: one
   // load after the other from lines that every SM wants at once took 15 us.
-  float2 mul[kNV][4];
+  float2 mul[NV][4];
 #pragma unroll
-  for (int v = 0; v < kNV; ++v) {
+  for (int v = 0; v < NV; ++v) {
     const int c = c0 + v * kStep;
     if (c < cols) {
       const float4 p = __ldcg(reinterpret_cast<const float4*>(a.top + cbase + c));
@@ -358,75 +384,68 @@ quantize_stream_kernel(const QuantArgs a, int stages, int* status) {
       mul[v][3] = make_float2(q.z, q.w);
     }
   }
-  uint32_t odd = 0;                       // octs that hold a column without a number for a scale
+  bool odd = false;                       // a column without a number for a scale among them
 #pragma unroll
-  for (int v = 0; v < kNV; ++v)
+  for (int v = 0; v < NV; ++v)
     if (c0 + v * kStep < cols) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (isnan(mul[v][e].x) || isnan(mul[v][e].y)) odd |= 1u << v;
+      for (int e = 0; e < 4; ++e) odd = odd || isnan(mul[v][e].x) || isnan(mul[v][e].y);
     }
   ring.turn_back();
   if (ring.producer) ring.serve_back();
   for (int i = n - 1; i >= 0; --i) {
     const int64_t row = ring.row(i);
-    const float fr = a.fold_rows ? __ldg(a.fold_rows + row) : 1.f;
-    Oct<IO> x[kNV];
+    const int h = ring.height(i);
+    Oct<IO> x[R][NV];
     if (ring.wait_back(i)) {
 #pragma unroll
-      for (int v = 0; v < kNV; ++v)
-        if (c0 + v * kStep < cols) x[v].load(ring.at(0) + c0 + v * kStep);
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+          if (r < h && c0 + v * kStep < cols) x[r][v].load(ring.at(r, 0) + c0 + v * kStep);
     }
     ring.release();
     ring.retreat();
     if (!ring.ok) continue;
-    uint8_t* q = a.q_cols + row * a.ld_qc + cbase;
-    if (a.format == PRM_Q8_INT8) back_row<IO, kNV, PRM_Q8_INT8>(q, x, mul, fr, odd, c0, kStep, cols);
-    else back_row<IO, kNV, PRM_Q8_E4M3>(q, x, mul, fr, odd, c0, kStep, cols);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r < h) {
+        const float f = a.fold_rows ? __ldg(a.fold_rows + row + r) : 1.f;
+        uint8_t* q = a.q_cols + (row + r) * a.ld_qc + cbase;
+        if (a.format == PRM_Q8_INT8) back_row<IO, NV, PRM_Q8_INT8>(q, x[r], mul, f, odd, c0, kStep, cols);
+        else back_row<IO, NV, PRM_Q8_E4M3>(q, x[r], mul, f, odd, c0, kStep, cols);
+      }
+    }
   }
   ring.finish();
 }
 
-template <typename IO, int W, bool ROWS>
+template <typename IO, int W, int NV, int R, bool ROWS>
 int launch_stream(const QuantArgs& a, cudaStream_t stream) {
-  constexpr int kGroups = kRingWarps<IO> / W;
+  constexpr int kGroups = kRingWarps / W;
   static PerDeviceOnce once;
-  int dev;
-  if (once.need(&dev)) {
-    if (cudaFuncSetAttribute(quantize_stream_kernel<IO, W, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)kRingBytes) != cudaSuccess)
-      return PRM_ERR_CUDA;
-    once.mark(dev);
-  }
-  int* status = q8_status_word();
-  const size_t row = (size_t)a.panel * sizeof(IO) * kGroups, tops = (size_t)a.panel * 4;
-  int stages = (int)std::min<size_t>(kRingStages, (kRingBytes - tops) / row);
-  if (!status || stages < 1) return PRM_ERR_CUDA;
   // as many blocks as there are groups' worth of rows, a whole number of them for each panel
-  const int per_panel = std::min<int64_t>(kRingBlocks / a.panels, (a.rows + kGroups - 1) / kGroups);
-  QuantArgs arg = a;
-  void* args[3] = {&arg, &stages, &status};
-  return cudaLaunchCooperativeKernel(quantize_stream_kernel<IO, W, ROWS>, dim3((unsigned)(per_panel * a.panels)),
-                                     dim3(kRingThreads<IO>), args, row * stages + tops, stream) == cudaSuccess
-             ? PRM_OK
-             : PRM_ERR_CUDA;
+  const unsigned per_panel = std::min<unsigned>(kRingBlocks / a.panels, ring_blocks(a.rows, R, kGroups));
+  return launch_ring(quantize_stream_kernel<IO, W, NV, R, ROWS>, once, per_panel * (unsigned)a.panels,
+                     (size_t)a.panel * sizeof(IO) * R * kGroups, (size_t)a.panel * 4, 0, true, stream, a);
 }
 
-// Widest row that one group holds with codes by row.
+// Widest row that one group holds with codes by row: 16 warps, 32 elements (bf16) or 16 per thread.
 template <typename IO>
-constexpr int kWidest = kRingWarps<IO> * 32 * 32;
+constexpr int kWidest = sizeof(IO) == 2 ? 16384 : 8192;
 
 template <typename IO, bool ROWS>
 int run_stream(QuantArgs a, cudaStream_t stream) {
   a.panels = ROWS ? 1 : (a.cols + 8191) / 8192;
   a.panel = (a.cols + 8 * a.panels - 1) / (8 * a.panels) * 8;
-  if (a.panel <= 1024) return launch_stream<IO, 1, ROWS>(a, stream);
-  if (a.panel <= 2048) return launch_stream<IO, 2, ROWS>(a, stream);
-  if (a.panel <= 4096) return launch_stream<IO, 4, ROWS>(a, stream);
   if constexpr (sizeof(IO) == 2) {
-    if (a.panel > 8192) return launch_stream<IO, 16, ROWS>(a, stream);
+    // two rows of two octs up to 4096 columns (8192 x 2048: 20.7 us against 24.6 with one row of four),
+    // one row of four beyond (4096 x 5120 both ways: 36.9 us against 40.9)
+    if (ROWS && a.panel > 8192) return launch_stream<IO, 16, 4, 1, ROWS>(a, stream);
+    if (a.panel > 4096) return launch_stream<IO, 8, 4, 1, ROWS>(a, stream);
   }
-  return launch_stream<IO, 8, ROWS>(a, stream);
+  return with_ring_warps<2>(
+      a.panel, [&](auto w) { return launch_stream<IO, decltype(w)::value, 2, kRingRows<IO>, ROWS>(a, stream); });
 }
 
 template <typename IO, int NV, int TPR>

@@ -1,14 +1,22 @@
 // Rows streamed through shared memory by bulk asynchronous copies, for the row operators on large
-// matrices: one persistent CTA per SM, whose warps form groups of W that walk over rows of their
-// own.  A group's ring holds up to kRingStages rows of each of its input matrices.  A warp that
-// is done with its part of a row says so on the stage's barrier; one more warp, a lane per group,
-// sends for the row that takes the stage when all warps of the group have.  Bytes in flight are then
-// set by the ring (up to 200 KB per SM), not by how many loads threads hold in registers between
-// barriers.  (With a thread of the group sending, each row cost its group about 500 cycles more.)
+// matrices: one persistent CTA per SM, whose 16 warps form groups of W that walk over sets of R
+// neighbouring rows of their own.  A group's ring holds up to kRingStages sets of each of its input
+// matrices.  A warp that is done with its part of a set says so on the stage's barrier; one more warp,
+// a lane per group, sends for the set that takes the stage when all warps of the group have.  Bytes in
+// flight are then set by the ring (up to 200 KB per SM), not by how many loads threads hold in
+// registers between barriers.
+//
+// What bounds such a kernel next to HBM is instructions per element: the barrier, the addressing and
+// (with R = 2) the weights or factors that a thread holds for its columns are shared by the 32 elements
+// that it has of a set, as one row of four octs or as two rows of two.  Which of the two is faster was
+// measured for each kernel: narrow rows and sums over rows gain by two rows, wide rows lose by a
+// group that is the whole CTA.
 //
 // Waits are bounded.  A thread whose wait ran out sets the status word and touches no data any
 // more, but keeps arriving at its group's barriers, so that nobody waits for it.
 #pragma once
+
+#include <type_traits>
 
 #include "async_copy.cuh"
 #include "q8.cuh"
@@ -17,12 +25,13 @@ namespace prm {
 
 constexpr int kRingStages = 6;
 constexpr size_t kRingBytes = 200 * 1024;
+constexpr int kRingWarps = 16;                        // that work on rows
+constexpr int kRingThreads = kRingWarps * 32 + 32;    // and the producer
+constexpr int kRingBlocks = 148;                      // one CTA per SM
 
-// Warps of a persistent CTA that work on rows: a thread holds up to 32 elements of a row of each matrix.
+// Rows per set of the kernels that take two: one where the elements are 32 bits wide, for the registers.
 template <typename IO>
-constexpr int kRingWarps = sizeof(IO) == 2 ? 16 : 8;
-template <typename IO>
-constexpr int kRingThreads = kRingWarps<IO> * 32 + 32;
+constexpr int kRingRows = sizeof(IO) == 2 ? 2 : 1;
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile(
@@ -49,29 +58,30 @@ __device__ __forceinline__ uint8_t* ring_memory() {
 }
 
 // The static shared memory of a CTA's rings.
-template <typename IO, int W, int ARR>
+template <int W, int R>
 struct RingBlock {
-  static constexpr int kGroups = kRingWarps<IO> / W;
-  uint64_t full[kGroups][kRingStages];    // the copies of a row have landed
-  uint64_t empty[kGroups][kRingStages];   // W warps are done with the row
-  alignas(16) float red[kGroups][2][32];
+  static constexpr int kGroups = kRingWarps / W;
+  uint64_t full[kGroups][kRingStages];    // the copies of a set have landed
+  uint64_t empty[kGroups][kRingStages];   // W warps are done with the set
+  alignas(16) float red[kGroups][2][R][2][16];
   int abort_word;
 };
-template <typename IO, int W, int ARR>
-__device__ __forceinline__ RingBlock<IO, W, ARR>& ring_block() {
-  __shared__ RingBlock<IO, W, ARR> b;
+template <int W, int R>
+__device__ __forceinline__ RingBlock<W, R>& ring_block() {
+  __shared__ RingBlock<W, R> b;
   return b;
 }
 
-// One group's ring over ARR matrices of the same number of rows.  The group's row number i (0, 1,
-// ..., n - 1) is row first + i * step.
-template <typename IO, int W, int ARR>
+// One group's ring over ARR matrices of the same number of rows.  The group's set number i (0, 1,
+// ..., n - 1) are the rows (first + i * step) * R and up to R - 1 after it.
+template <typename IO, int W, int R, int ARR>
 struct RowRing {
-  RingBlock<IO, W, ARR>& b;
+  static constexpr int kGroups = kRingWarps / W;
+  RingBlock<W, R>& b;
   const IO* src[ARR];
   int64_t ld[ARR];
-  int first, step, n;     // rows (below 2^31)
-  uint8_t* base;          // [stages][ARR][row_bytes]
+  int rows, first, step, n;
+  uint8_t* base;          // [stages][R][ARR][row_bytes]
   uint32_t row_bytes;
   int stages, group, stage;
   uint32_t phase;
@@ -79,42 +89,50 @@ struct RowRing {
   bool producer, ok;
   int* status;
 
-  __device__ __forceinline__ RowRing(RingBlock<IO, W, ARR>& block, const void* const* srcs, const int64_t* lds,
-                                     int rows, int cols, int n_stages, int* status_word)
-      : b(block), stages(n_stages), stage(0), phase(0), ok(true), status(status_word) {
-    constexpr int kGroups = kRingWarps<IO> / W;
-    producer = threadIdx.x >= kRingWarps<IO> * 32;
-    group = producer ? threadIdx.x - kRingWarps<IO> * 32 : threadIdx.x / (W * 32);   // a lane per group
+  __device__ __forceinline__ RowRing(RingBlock<W, R>& block, const void* const* srcs, const int64_t* lds, int64_t n_rows,
+                                     int cols, int n_stages, int* status_word)
+      : b(block), rows((int)n_rows), stages(n_stages), stage(0), phase(0), ok(true), status(status_word) {
+    producer = threadIdx.x >= kRingWarps * 32;
+    group = producer ? threadIdx.x - kRingWarps * 32 : threadIdx.x / (W * 32);   // a lane per group
 #pragma unroll
     for (int k = 0; k < ARR; ++k) {
       src[k] = reinterpret_cast<const IO*>(srcs[k]);
       ld[k] = lds[k];
     }
     row_bytes = (uint32_t)cols * sizeof(IO);
-    base = ring_memory() + (size_t)group * stages * ARR * row_bytes;
-    place(blockIdx.x, gridDim.x, rows);
+    base = ring_memory() + (size_t)group * stages * R * ARR * row_bytes;
+    place(blockIdx.x, gridDim.x);
   }
-  // The rows of a block that is number `line` of `lines`.
-  __device__ __forceinline__ void place(int line, int lines, int rows) {
-    constexpr int kGroups = kRingWarps<IO> / W;
+  // The sets of a block that is number `line` of `lines`.
+  __device__ __forceinline__ void place(int line, int lines) {
+    const int sets = (rows - 1) / R + 1;
     first = line * kGroups + group;
     step = lines * kGroups;
-    n = group < kGroups && first < rows ? (rows - first - 1) / step + 1 : 0;
+    n = group < kGroups && first < sets ? (sets - first - 1) / step + 1 : 0;
   }
-  __device__ __forceinline__ int64_t row(int i) const { return first + (int64_t)i * step; }
-  __device__ __forceinline__ const IO* at(int k) const {
-    return reinterpret_cast<const IO*>(base + ((size_t)stage * ARR + k) * row_bytes);
+  __device__ __forceinline__ int64_t row(int i) const { return ((int64_t)i * step + first) * R; }
+  // Rows of set i: R, but for the last one.
+  __device__ __forceinline__ int height(int i) const { return R == 1 ? 1 : (int)min((int64_t)R, rows - row(i)); }
+  // Row r of matrix k of the current set.
+  __device__ __forceinline__ const IO* at(int r, int k) const {
+    return reinterpret_cast<const IO*>(base + (uint32_t)((stage * R + r) * ARR + k) * row_bytes);
   }
   __device__ __forceinline__ void fetch(int i, int s) const {
-    const int64_t r = row(i);
-    mbar_expect_tx(&b.full[group][s], ARR * row_bytes);
+    const int h = height(i);
+    mbar_expect_tx(&b.full[group][s], (uint32_t)(h * ARR) * row_bytes);
 #pragma unroll
-    for (int k = 0; k < ARR; ++k)
-      bulk_load(base + ((size_t)s * ARR + k) * row_bytes, src[k] + r * ld[k], row_bytes, &b.full[group][s]);
+    for (int r = 0; r < R; ++r) {
+      if (r < h) {
+#pragma unroll
+        for (int k = 0; k < ARR; ++k)
+          bulk_load(base + (uint32_t)((s * R + r) * ARR + k) * row_bytes, src[k] + (row(i) + r) * ld[k], row_bytes,
+                    &b.full[group][s]);
+      }
+    }
   }
   // All threads of the block, once.
   __device__ __forceinline__ void start() {
-    constexpr int kBars = (kRingWarps<IO> / W) * kRingStages;
+    constexpr int kBars = kGroups * kRingStages;
     if (threadIdx.x < kBars) {
       mbar_init(&b.full[0][0] + threadIdx.x, 1);
       mbar_init(&b.empty[0][0] + threadIdx.x, W);
@@ -124,7 +142,7 @@ struct RowRing {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
   }
-  // The producer's lanes, each for its group: rows 0 .. n - 1.  No lane waits for another's row.
+  // The producer's lanes, each for its group: sets 0 .. n - 1.  No lane waits for another's set.
   __device__ __forceinline__ void serve() {
     int i = 0;
     Patience p;
@@ -163,12 +181,12 @@ struct RowRing {
       atomicOr(status, kStatusTimeout);
     }
   }
-  // The current row has landed.
+  // The current set has landed.
   __device__ __forceinline__ bool wait() {
     ok = ok && mbar_wait(&b.full[group][stage], phase, &b.abort_word, status);
     return ok;
   }
-  // This warp is done with the current row.
+  // This warp is done with the current set.
   __device__ __forceinline__ void release() const {
     __syncwarp();
     if ((threadIdx.x & 31) == 0 && ok) mbar_arrive(&b.empty[group][stage]);
@@ -178,13 +196,13 @@ struct RowRing {
     if constexpr (W == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(W * 32) : "memory");
   }
-  // A second walk over the same rows, last row first.  The last `stages` rows are still in the ring;
+  // A second walk over the same sets, last one first.  The last `stages` sets are still in the ring;
   // the others are sent for again as their stages fall free.  Between the two walks lies a barrier of
   // the block.  wait_back(i) / release() / retreat() go with i = n - 1, ..., 0.
   __device__ __forceinline__ void turn_back() {
     laps = n > 0 ? (n - 1) / stages : 0;
     last = stage = n > 0 ? (n - 1) % stages : 0;
-    phase = 0;
+    phase = 0;                              // laps of the walk back
   }
   // Copies into (and releases of) the current stage on the way out, plus the laps since.
   __device__ __forceinline__ uint32_t fills() const { return (uint32_t)laps + (stage <= last ? 1u : 0u) + phase; }
@@ -196,10 +214,10 @@ struct RowRing {
   __device__ __forceinline__ void retreat() {
     if (stage == 0) stage = stages;
     --stage;
-    if (stage == last) ++phase;             // laps of the walk back
+    if (stage == last) ++phase;
   }
   __device__ __forceinline__ void serve_back() {
-    int i = n - 1 - stages;                 // row i takes the stage of row i + stages
+    int i = n - 1 - stages;                 // set i takes the stage of set i + stages
     phase = 1;
     Patience p;
     while (__any_sync(0xffffffffu, ok && i >= 0)) {
@@ -215,82 +233,53 @@ struct RowRing {
       }
     }
   }
-  // Reductions over the group; the words of row i and row i + 1 lie apart and are read in pieces.
+  // Reductions over the group, R rows with one barrier.  The words of set i and set i + 1 lie apart.
+  // SUMS: how many of p and q are sums (p first), the rest are largest magnitudes.
   static constexpr int kPiece = W >= 4 ? 4 : 2;
-  struct Words {
-    float v[kPiece];
-    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
-  };
-  static __device__ __forceinline__ Words words(const float* p) {
-    Words w;
+  template <bool P, bool Q_SUM>
+  __device__ __forceinline__ void reduce(int i, float (&p)[R], float (&q)[R]) const {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if constexpr (P) p[r] = warp_sum(p[r]);
+      q[r] = Q_SUM ? warp_sum(q[r]) : warp_top(q[r]);
+    }
+    if constexpr (W > 1) {
+      float(*red)[2][16] = b.red[group][i & 1];
+      const int warp = (threadIdx.x >> 5) % W;
+      if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if constexpr (P) red[r][0][warp] = p[r];
+          red[r][1][warp] = q[r];
+        }
+      }
+      sync();
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if constexpr (P) p[r] = 0.f;
+        q[r] = 0.f;
+#pragma unroll
+        for (int k = 0; k < W; k += kPiece) {
+          float u[kPiece], v[kPiece];
+          if constexpr (P) words(red[r][0] + k, u);
+          words(red[r][1] + k, v);
+#pragma unroll
+          for (int e = 0; e < kPiece; e += 2) {
+            if constexpr (P) p[r] += u[e] + u[e + 1];
+            if constexpr (Q_SUM) q[r] += v[e] + v[e + 1];
+            else q[r] = max_abs(q[r], make_float2(v[e], v[e + 1]));
+          }
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ void words(const float* p, float (&w)[kPiece]) {
     if constexpr (kPiece == 4) {
       const float4 f = *reinterpret_cast<const float4*>(p);
-      w.v[0] = f.x; w.v[1] = f.y; w.v[2] = f.z; w.v[3] = f.w;
+      w[0] = f.x; w[1] = f.y; w[2] = f.z; w[3] = f.w;
     } else {
       const float2 f = *reinterpret_cast<const float2*>(p);
-      w.v[0] = f.x; w.v[1] = f.y;
-    }
-    return w;
-  }
-  __device__ __forceinline__ void sum2(int i, float& p, float& q) const {
-    p = warp_sum(p);
-    q = warp_sum(q);
-    if constexpr (W > 1) {
-      float* red = b.red[group][i & 1];
-      const int warp = (threadIdx.x >> 5) % W;
-      if ((threadIdx.x & 31) == 0) {
-        red[warp] = p;
-        red[16 + warp] = q;
-      }
-      sync();
-      p = q = 0.f;
-#pragma unroll
-      for (int k = 0; k < W; k += kPiece) {
-        const auto u = words(red + k), v = words(red + 16 + k);
-#pragma unroll
-        for (int e = 0; e < kPiece; ++e) {
-          p += u[e];
-          q += v[e];
-        }
-      }
-    }
-  }
-  __device__ __forceinline__ void max_top(int i, float& top) const {
-    top = warp_top(top);
-    if constexpr (W > 1) {
-      float* red = b.red[group][i & 1];
-      if ((threadIdx.x & 31) == 0) red[(threadIdx.x >> 5) % W] = top;
-      sync();
-      top = 0.f;
-#pragma unroll
-      for (int k = 0; k < W; k += kPiece) {
-        const auto v = words(red + k);
-#pragma unroll
-        for (int e = 0; e < kPiece; e += 2) top = max_abs(top, make_float2(v[e], v[e + 1]));
-      }
-    }
-  }
-  __device__ __forceinline__ void sum_top(int i, float& p, float& top) const {
-    p = warp_sum(p);
-    top = warp_top(top);
-    if constexpr (W > 1) {
-      float* red = b.red[group][i & 1];
-      const int warp = (threadIdx.x >> 5) % W;
-      if ((threadIdx.x & 31) == 0) {
-        red[warp] = p;
-        red[16 + warp] = top;
-      }
-      sync();
-      p = top = 0.f;
-#pragma unroll
-      for (int k = 0; k < W; k += kPiece) {
-        const auto u = words(red + k), v = words(red + 16 + k);
-#pragma unroll
-        for (int e = 0; e < kPiece; e += 2) {
-          p += u[e] + u[e + 1];
-          top = max_abs(top, make_float2(v[e], v[e + 1]));
-        }
-      }
+      w[0] = f.x; w[1] = f.y;
     }
   }
   // Copies in flight land before the CTA's memory goes (only after a wait that ran out are there any).
@@ -308,18 +297,26 @@ struct RowRing {
 // The status word that prm_q8_status reads, on the current device (null if it has none).
 int* q8_status_word();
 
-constexpr int kRingBlocks = 148;     // one CTA per SM
-
 // From here on streaming is faster than one row per block.
 constexpr int64_t kRingElements = 1 << 22;
-inline bool ring_worth(int64_t rows, int cols) { return cols >= 512 && cols <= 8192 && rows * cols >= kRingElements; }
-inline int ring_blocks(int64_t rows, int groups) { return (int)std::min<int64_t>(kRingBlocks, (rows + groups - 1) / groups); }
+inline bool ring_worth(int64_t rows, int cols) { return cols >= 256 && cols <= 8192 && rows * cols >= kRingElements; }
 
-// One CTA per SM; `extra` bytes are what the kernel wants of the ring's memory after the last row.
-template <typename IO, int W, bool COOPERATIVE = false, typename A>
-int launch_ring(void (*kernel)(A, int, int*), int arrays, PerDeviceOnce& once, int64_t rows, int cols, size_t extra, cudaStream_t stream,
-                A a) {
-  constexpr int kGroups = kRingWarps<IO> / W;
+// Calls f with the number of warps to a row of `cols` elements, NV octs per thread.
+template <int NV, typename F>
+int with_ring_warps(int cols, F f) {
+  if (cols <= 256 * NV) return f(std::integral_constant<int, 1>());
+  if (cols <= 512 * NV) return f(std::integral_constant<int, 2>());
+  if (cols <= 1024 * NV) return f(std::integral_constant<int, 4>());
+  if (cols <= 2048 * NV) return f(std::integral_constant<int, 8>());
+  if constexpr (NV <= 2) return f(std::integral_constant<int, 16>());
+  return PRM_ERR_SHAPE;
+}
+
+// Launches kernel(a, stages, status): `set_bytes` of ring per stage and CTA, then `tail` bytes that the
+// kernel uses beside the ring and `after` bytes that it wants of all of it after the last set.
+template <typename A>
+int launch_ring(void (*kernel)(A, int, int*), PerDeviceOnce& once, unsigned blocks, size_t set_bytes, size_t tail,
+                size_t after, bool cooperative, cudaStream_t stream, A a) {
   int dev;
   if (once.need(&dev)) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes) != cudaSuccess)
@@ -327,20 +324,22 @@ int launch_ring(void (*kernel)(A, int, int*), int arrays, PerDeviceOnce& once, i
     once.mark(dev);
   }
   int* status = q8_status_word();
-  const size_t row = (size_t)cols * sizeof(IO) * arrays * kGroups;
-  const int stages = (int)std::min<size_t>(kRingStages, kRingBytes / row);
-  if (!status || stages < 1 || extra > kRingBytes) return PRM_ERR_CUDA;
-  const unsigned blocks = (unsigned)ring_blocks(rows, kGroups);
-  const size_t smem = std::max(extra, row * stages);
+  if (tail > kRingBytes || after > kRingBytes) return PRM_ERR_CUDA;
+  int stages = (int)std::min<size_t>(kRingStages, (kRingBytes - tail) / set_bytes);
+  if (!status || stages < 1) return PRM_ERR_CUDA;
+  const size_t smem = std::max(after, set_bytes * stages + tail);
   cudaError_t e;
-  if constexpr (COOPERATIVE) {
-    int n = stages;
-    void* args[3] = {&a, &n, &status};
-    e = cudaLaunchCooperativeKernel((const void*)kernel, dim3(blocks), dim3(kRingThreads<IO>), args, smem, stream);
+  if (cooperative) {
+    void* args[3] = {&a, &stages, &status};
+    e = cudaLaunchCooperativeKernel((const void*)kernel, dim3(blocks), dim3(kRingThreads), args, smem, stream);
   } else {
-    e = launch_after(kernel, blocks, kRingThreads<IO>, smem, stream, 0, a, stages, status);
+    e = launch_after(kernel, blocks, kRingThreads, smem, stream, 0, a, stages, status);
   }
   return e == cudaSuccess ? PRM_OK : PRM_ERR_CUDA;
+}
+inline unsigned ring_blocks(int64_t rows, int rows_per_set, int groups) {
+  const int64_t sets = (rows + rows_per_set - 1) / rows_per_set;
+  return (unsigned)std::min<int64_t>(kRingBlocks, (sets + groups - 1) / groups);
 }
 
 }  // namespace prm
