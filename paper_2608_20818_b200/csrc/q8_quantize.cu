@@ -34,12 +34,20 @@ struct QuantArgs {
   int panel, panels;        // columns that a block of the streaming kernel works on; cols / panel
 };
 
-// x * f for one oct (f: eight factors from c on, or null).
+// x * f for one oct (f: eight factors from c on, or null; 16-byte loads where they are aligned).
 __device__ __forceinline__ void fold_oct(const float* f, int c, float2 (&t)[4]) {
-  if (f) {
+  if (!f) return;
+  float2 m[4];
+  if (((uintptr_t)f & 15) == 0) {
+    Oct<float> o;
+    o.load(f + c);
+    o.get(m);
+  } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = mul2(t[e], make_float2(__ldg(f + c + 2 * e), __ldg(f + c + 2 * e + 1)));
+    for (int e = 0; e < 4; ++e) m[e] = make_float2(__ldg(f + c + 2 * e), __ldg(f + c + 2 * e + 1));
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) t[e] = mul2(t[e], m[e]);
 }
 
 // One row per group of TPR threads, in registers between the maximum and the rounding.
@@ -240,6 +248,13 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
   RowRing<IO, W, R, 1> ring(ring_block<W, R>(), src, ld, a.rows, cols, stages, status);
   ring.place(line, lines);
   float* tops = reinterpret_cast<float*>(ring_memory() + (size_t)(kRingWarps / W) * stages * R * ring.row_bytes);
+  // The column factors come from shared memory: eight neighbouring fp32 per thread and row are loads
+  // of 32 sectors each (4096 x 8192 both ways with folds: 76 us).
+  float* fold = tops + a.panel;
+  if constexpr (ROWS) {
+    if (a.fold_cols)
+      for (int c = threadIdx.x; c < cols; c += kRingThreads) fold[c] = __ldg(a.fold_cols + c);
+  }
   ring.start();
   float ct[NV][8];
 #pragma unroll
@@ -248,12 +263,21 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
     for (int e = 0; e < 8; ++e) ct[v][e] = 0.f;
   const int n = ring.producer ? 0 : ring.n;
   if (ring.producer) ring.serve();
+  // The row factors are fetched a set ahead.
+  auto row_factors = [&](int i, float (&f)[R]) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      f[r] = a.fold_rows && i >= 0 && i < n && r < ring.height(i) ? __ldg(a.fold_rows + ring.row(i) + r) : 1.f;
+  };
+  float next[R];
+  row_factors(0, next);
   for (int i = 0; i < n; ++i) {
     const int64_t row = ring.row(i);
     const int h = ring.height(i);
     float fr[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) fr[r] = a.fold_rows && r < h ? __ldg(a.fold_rows + row + r) : 1.f;
+    for (int r = 0; r < R; ++r) fr[r] = next[r];
+    row_factors(i + 1, next);
     float2 t[R][NV][4];
     float none[R], top[R];
 #pragma unroll
@@ -281,9 +305,9 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
           if constexpr (ROWS) {
             if (a.fold_cols) {
               float2 fc[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                fc[e] = make_float2(__ldg(a.fold_cols + c + 2 * e), __ldg(a.fold_cols + c + 2 * e + 1));
+              Oct<float> o;
+              o.load(fold + c);
+              o.get(fc);
 #pragma unroll
               for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -393,9 +417,14 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
     }
   ring.turn_back();
   if (ring.producer) ring.serve_back();
+  row_factors(n - 1, next);
   for (int i = n - 1; i >= 0; --i) {
     const int64_t row = ring.row(i);
     const int h = ring.height(i);
+    float fr[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) fr[r] = next[r];
+    row_factors(i - 1, next);
     Oct<IO> x[R][NV];
     if (ring.wait_back(i)) {
 #pragma unroll
@@ -410,10 +439,9 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (r < h) {
-        const float f = a.fold_rows ? __ldg(a.fold_rows + row + r) : 1.f;
         uint8_t* q = a.q_cols + (row + r) * a.ld_qc + cbase;
-        if (a.format == PRM_Q8_INT8) back_row<IO, NV, PRM_Q8_INT8>(q, x[r], mul, f, odd, c0, kStep, cols);
-        else back_row<IO, NV, PRM_Q8_E4M3>(q, x[r], mul, f, odd, c0, kStep, cols);
+        if (a.format == PRM_Q8_INT8) back_row<IO, NV, PRM_Q8_INT8>(q, x[r], mul, fr[r], odd, c0, kStep, cols);
+        else back_row<IO, NV, PRM_Q8_E4M3>(q, x[r], mul, fr[r], odd, c0, kStep, cols);
       }
     }
   }
@@ -427,7 +455,7 @@ int launch_stream(const QuantArgs& a, cudaStream_t stream) {
   // as many blocks as there are groups' worth of rows, a whole number of them for each panel
   const unsigned per_panel = std::min<unsigned>(kRingBlocks / a.panels, ring_blocks(a.rows, R, kGroups));
   return launch_ring(quantize_stream_kernel<IO, W, NV, R, ROWS>, once, per_panel * (unsigned)a.panels,
-                     (size_t)a.panel * sizeof(IO) * R * kGroups, (size_t)a.panel * 4, 0, true, stream, a);
+                     (size_t)a.panel * sizeof(IO) * R * kGroups, (size_t)a.panel * (ROWS && a.fold_cols ? 8 : 4), 0, true, stream, a);
 }
 
 // Widest row that one group holds with codes by row: 16 warps, 32 elements (bf16) or 16 per thread.
