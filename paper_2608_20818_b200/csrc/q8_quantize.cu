@@ -230,6 +230,9 @@ __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], con
   }
 }
 
+// Bytes of the matrix that the first walk leaves in the L2 for the second.
+constexpr int64_t kKeep = (int64_t)64 << 20;
+
 // The streaming kernel.  Blocks with the same blockIdx % panels work on the same panel of columns;
 // with codes by row there is one panel, the whole width.  Phase 1: groups of W warps walk over sets of
 // R rows, NV octs per thread and row.  Then the blocks' column maxima are joined (shared memory, scratch,
@@ -262,7 +265,12 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
 #pragma unroll
     for (int e = 0; e < 8; ++e) ct[v][e] = 0.f;
   const int n = ring.producer ? 0 : ring.n;
-  if (ring.producer) ring.serve();
+  // What the second walk reads first stays in the L2: the rows that are read last, up to kKeep bytes in
+  // all CTAs' rings together.
+  if (ring.producer) {
+    const int64_t set = (int64_t)R * (kRingWarps / W) * gridDim.x * ring.row_bytes;
+    ring.serve(ring.n - stages - (int)(kKeep / set));
+  }
   // The row factors are fetched a set ahead.
   auto row_factors = [&](int i, float (&f)[R]) {
 #pragma unroll

@@ -33,11 +33,22 @@ constexpr int kRingBlocks = 148;                      // one CTA per SM
 template <typename IO>
 constexpr int kRingRows = sizeof(IO) == 2 ? 2 : 1;
 
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+// `policy`: how long the L2 should hold the lines (evict_first / evict_last below).
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-      ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+      ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
       : "memory");
+}
+__device__ __forceinline__ uint64_t evict_first() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint64_t evict_last() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  return p;
 }
 // Whether a phase is complete, without the suspension that mbarrier.try_wait may put in: the producer's
 // lanes wait for barriers of their own and none may hold up the others.
@@ -117,7 +128,7 @@ struct RowRing {
   __device__ __forceinline__ const IO* at(int r, int k) const {
     return reinterpret_cast<const IO*>(base + (uint32_t)((stage * R + r) * ARR + k) * row_bytes);
   }
-  __device__ __forceinline__ void fetch(int i, int s) const {
+  __device__ __forceinline__ void fetch(int i, int s, uint64_t policy) const {
     const int h = height(i);
     mbar_expect_tx(&b.full[group][s], (uint32_t)(h * ARR) * row_bytes);
 #pragma unroll
@@ -126,7 +137,7 @@ struct RowRing {
 #pragma unroll
         for (int k = 0; k < ARR; ++k)
           bulk_load(base + (uint32_t)((s * R + r) * ARR + k) * row_bytes, src[k] + (row(i) + r) * ld[k], row_bytes,
-                    &b.full[group][s]);
+                    &b.full[group][s], policy);
       }
     }
   }
@@ -142,14 +153,16 @@ struct RowRing {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
   }
-  // The producer's lanes, each for its group: sets 0 .. n - 1.  No lane waits for another's set.
-  __device__ __forceinline__ void serve() {
+  // The producer's lanes, each for its group: sets 0 .. n - 1.  No lane waits for another's set.  Sets
+  // from `keep` on will be read again and stay in the L2; those before them make room.
+  __device__ __forceinline__ void serve(int keep = 0x7fffffff) {
+    const uint64_t once = evict_first(), again = evict_last();
     int i = 0;
     Patience p;
     while (__any_sync(0xffffffffu, ok && i < n)) {
       if (ok && i < n) {
         if (i < stages || mbar_test(&b.empty[group][stage], phase ^ 1)) {
-          fetch(i, stage);
+          fetch(i, stage, i < keep ? once : again);
           ++i;
           advance();
           p = Patience();
@@ -217,13 +230,14 @@ struct RowRing {
     if (stage == last) ++phase;
   }
   __device__ __forceinline__ void serve_back() {
+    const uint64_t once = evict_first();
     int i = n - 1 - stages;                 // set i takes the stage of set i + stages
     phase = 1;
     Patience p;
     while (__any_sync(0xffffffffu, ok && i >= 0)) {
       if (ok && i >= 0) {
         if (mbar_test(&b.empty[group][stage], (fills() - 1) & 1u)) {
-          fetch(i, stage);
+          fetch(i, stage, once);
           --i;
           retreat();
           p = Patience();
