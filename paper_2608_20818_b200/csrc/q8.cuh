@@ -170,6 +170,137 @@ __device__ __forceinline__ void store_octs(uint8_t* q, const float2 (&t)[NV][4],
   }
 }
 
+// ---------------------------------------------- rows that do not start on an oct's boundary
+// A row is walked through in octs that are aligned in memory: oct o holds elements 8 o - shift .. 8 o -
+// shift + 7, `shift` = what the row's start lies behind a boundary, alike for all matrices that are
+// walked together.  Octs that reach over either end of the row go element by element.
+template <typename T>
+__host__ __device__ __forceinline__ int oct_shift(const T* row) {
+  return (int)(((uintptr_t)row / sizeof(T)) & 7);
+}
+// One row of a matrix as the octs see it: the elements before and behind it that belong to the same
+// matrix may be fetched along (an oct at the end of a row is one load like all others, and nothing
+// waits for it before the other loads are under way), nothing beyond the matrix is.
+template <typename T>
+struct OctRow {
+  const T* p;
+  int before, after;                       // elements of the matrix before the row's start (8 are enough), and from it on
+  __device__ __forceinline__ OctRow(const void* base, int64_t row, int64_t rows, int64_t ld, int cols)
+      : p(reinterpret_cast<const T*>(base) + row * ld),
+        before((int)min((int64_t)8, row * ld)),
+        after((int)min((int64_t)cols + 8, (rows - 1 - row) * ld + cols)) {}
+  __device__ __forceinline__ void load(int first, int cols, Oct<T>& o) const {
+    if (first >= cols) {
+      o.zero();
+    } else if (first + before >= 0 && first + 8 <= after) {
+      o.load_stream(p + first);
+    } else {
+      float2 v[4];
+      float e[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) e[k] = first + k >= 0 && first + k < cols ? to_f32(p[first + k]) : 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = make_float2(e[2 * k], e[2 * k + 1]);
+      o.set(v);
+    }
+  }
+};
+// The oct's elements that lie in the row, zeros for the others.
+template <typename T>
+__device__ __forceinline__ void get_part(const Oct<T>& o, int first, int cols, float2 (&v)[4]) {
+  o.get(v);
+  if (first < 0 || first + 8 > cols) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (first + 2 * k < 0 || first + 2 * k >= cols) v[k].x = 0.f;
+      if (first + 2 * k + 1 < 0 || first + 2 * k + 1 >= cols) v[k].y = 0.f;
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T* row, int first, int cols, const float2 (&v)[4]) {
+  if (first >= 0 && first + 8 <= cols) {
+    Oct<T> o;
+    o.set(v);
+    o.store(row + first);
+  } else if (first < cols) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (first + k >= 0 && first + k < cols) from_f32(row + first + k, k & 1 ? v[k / 2].y : v[k / 2].x);
+  }
+}
+// Eight factors from `first` on of a vector of any alignment (0 outside it).  Inside it the loads have no
+// conditions, so that they are under way together.
+template <typename T>
+__device__ __forceinline__ void load_factors(const T* f, int first, int cols, float2 (&v)[4]) {
+  if (first >= 0 && first + 8 <= cols) {
+    const T* p = f + first;
+    if (((uintptr_t)p & 15) == 0) {
+      Oct<T> o;
+      o.load(p);
+      o.get(v);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = make_float2(to_f32(p[2 * k]), to_f32(p[2 * k + 1]));
+    }
+  } else if (first >= cols) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = make_float2(0.f, 0.f);
+  } else {
+    float e[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e[k] = first + k >= 0 && first + k < cols ? to_f32(f[first + k]) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = make_float2(e[2 * k], e[2 * k + 1]);
+  }
+}
+__device__ __forceinline__ void load_factors(const void* f, int fp32, int first, int cols, float2 (&v)[4]) {
+  if (fp32) load_factors(reinterpret_cast<const float*>(f), first, cols, v);
+  else load_factors(reinterpret_cast<const __nv_bfloat16*>(f), first, cols, v);
+}
+// The codes of a row's octs (NV per thread of TPR) to a row of codes whose start is 8-byte aligned.  Word
+// k of it is made of the end of oct k and the beginning of oct k + 1, which another thread holds: the
+// octs meet in `stage`, NV * TPR + 1 words of shared memory.
+template <int NV, int TPR>
+__device__ __forceinline__ void store_octs_shifted(uint64_t* stage, uint8_t* q, const float2 (&t)[NV][4], int o0,
+                                                   int shift, int cols, float top, int format) {
+  const bool finite = q8_finite(top);
+  const float f = q8_mul(top, q8_limit(format));
+  const float2 mul = make_float2(f, f);
+  uint64_t c[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    uint2 w = make_uint2(0u, 0u);
+    if (finite)
+      w = format == PRM_Q8_INT8 ? make_uint2(codes4<PRM_Q8_INT8>(t[v][0], t[v][1], mul), codes4<PRM_Q8_INT8>(t[v][2], t[v][3], mul))
+                                : make_uint2(codes4<PRM_Q8_E4M3>(t[v][0], t[v][1], mul), codes4<PRM_Q8_E4M3>(t[v][2], t[v][3], mul));
+    c[v] = (uint64_t)w.x | ((uint64_t)w.y << 32);
+  }
+  if (shift) {                             // alike for all threads of the row
+#pragma unroll
+    for (int v = 0; v < NV; ++v) stage[o0 + v * TPR] = c[v];
+    if constexpr (TPR == 32) __syncwarp();
+    else __syncthreads();
+#pragma unroll
+    for (int v = 0; v < NV; ++v) c[v] = (c[v] >> (8 * shift)) | (stage[o0 + v * TPR + 1] << (64 - 8 * shift));
+  }
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int word = (o0 + v * TPR) * 8;
+    if (word + 8 <= cols) {
+      *reinterpret_cast<uint64_t*>(q + word) = c[v];
+    } else {
+      for (int k = 0; word + k < cols; ++k) q[word + k] = (uint8_t)(c[v] >> (8 * k));
+    }
+  }
+}
+// Whether rows of the two matrices start alike: then their octs are aligned together.
+template <typename T>
+inline bool octs_alike(const void* p, int64_t ld_p, const void* q, int64_t ld_q) {
+  return oct_shift((const T*)p) == oct_shift((const T*)q) && ((ld_p - ld_q) & 7) == 0 &&
+         ((uintptr_t)p % sizeof(T)) == 0 && ((uintptr_t)q % sizeof(T)) == 0;
+}
+
 __device__ __forceinline__ float load1(const void* p, int fp32, int64_t i) {
   return fp32 ? reinterpret_cast<const float*>(p)[i] : to_f32(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
 }

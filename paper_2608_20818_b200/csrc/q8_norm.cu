@@ -158,6 +158,58 @@ __global__ void __launch_bounds__(kRingThreads, 1) rmsnorm_q8_stream_kernel(cons
   }
 }
 
+// Rows that start anywhere (odd widths), or too wide for the kernels above: as rmsnorm_q8_kernel, on
+// octs aligned in memory.
+template <typename IO, int NV, int TPR>
+__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_shifted_kernel(const NormArgs a) {
+  constexpr int kRows = TPR == 32 ? 8 : 1;
+  __shared__ float red[64];
+  __shared__ uint64_t stage[kRows][NV * TPR + 1];
+  grid_wait();
+  grid_trigger();
+  const int o0 = threadIdx.x % TPR;
+  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+  if (row >= a.rows) return;
+  const OctRow<IO> x(a.x, row, a.rows, a.ld_x, a.cols);
+  const OctRow<IO> r(a.residual ? a.residual : a.x, row, a.rows, a.residual ? a.ld_r : a.ld_x, a.cols);
+  const int shift = oct_shift(x.p);
+  Oct<IO> xv[NV], rv[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (o0 + v * TPR) * 8 - shift;
+    x.load(c, a.cols, xv[v]);
+    if (a.residual) r.load(c, a.cols, rv[v]);
+  }
+  float2 t[NV][4], sum2 = make_float2(0.f, 0.f);
+  float top = 0.f;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (o0 + v * TPR) * 8 - shift;
+    float2 w[4];
+    load_factors(a.weight, a.weight_fp32, c, a.cols, w);
+    get_part(xv[v], c, a.cols, t[v]);
+    if (a.residual) {
+      float2 b[4];
+      get_part(rv[v], c, a.cols, b);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[v][e] = add2(t[v][e], b[e]);
+      xv[v].set(t[v]);
+      xv[v].get(t[v]);
+      store_part(reinterpret_cast<IO*>(a.h) + row * a.ld_h, c, a.cols, t[v]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sum2 = fma2(t[v][e], t[v][e], sum2);
+      t[v][e] = mul2(t[v][e], w[e]);
+      top = max_abs(top, t[v][e]);
+    }
+  }
+  float sum = sum2.x + sum2.y;
+  block_sum_top<TPR>(sum, top, red);
+  store_octs_shifted<NV, TPR>(stage[threadIdx.x / TPR], a.q + row * a.ld_q, t, o0, shift, a.cols, top, a.format);
+  if (o0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
+}
+
 // Any alignment, any length: two passes over the row, the second of which finds it in cache.
 template <typename IO, int THREADS>
 __global__ void __launch_bounds__(THREADS) rmsnorm_q8_single_kernel(const NormArgs a) {
@@ -226,11 +278,35 @@ int run_norm(const NormArgs& a, cudaStream_t stream) {
   return launch_norm<IO, WT, 2, 1024>(a, stream);
 }
 
+template <typename IO, int NV, int TPR>
+void launch_norm_shifted(const NormArgs& a, cudaStream_t stream) {
+  constexpr int kRows = TPR == 32 ? 8 : 1;
+  launch_after(rmsnorm_q8_shifted_kernel<IO, NV, TPR>, (unsigned)((a.rows + kRows - 1) / kRows), TPR == 32 ? 256 : TPR, 0,
+               stream, 0, a);
+}
+
+// `alike`: the matrices' rows start alike and the codes' rows on 8 bytes.
 template <typename IO>
-int run_norm_single(const NormArgs& a, cudaStream_t stream) {
-  if (a.cols <= 1024) launch_after(rmsnorm_q8_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a);
-  else if (a.cols <= 8192) launch_after(rmsnorm_q8_single_kernel<IO, 256>, (unsigned)a.rows, 256, 0, stream, 0, a);
-  else launch_after(rmsnorm_q8_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a);
+int run_norm_single(const NormArgs& a, bool alike, cudaStream_t stream) {
+  const int c = a.cols + 7;               // a row may need one more oct
+  if (alike && c <= 32768) {
+    if (c <= 256) launch_norm_shifted<IO, 1, 32>(a, stream);
+    else if (c <= 512) launch_norm_shifted<IO, 2, 32>(a, stream);
+    else if (c <= 1024) launch_norm_shifted<IO, 1, 128>(a, stream);
+    else if (c <= 2048) launch_norm_shifted<IO, 2, 128>(a, stream);
+    else if (c <= 3072) launch_norm_shifted<IO, 3, 128>(a, stream);
+    else if (c <= 4096) launch_norm_shifted<IO, 2, 256>(a, stream);
+    else if (c <= 6144) launch_norm_shifted<IO, 3, 256>(a, stream);
+    else if (c <= 8192) launch_norm_shifted<IO, 2, 512>(a, stream);
+    else if (c <= 12288) launch_norm_shifted<IO, 3, 512>(a, stream);
+    else if (c <= 16384) launch_norm_shifted<IO, 2, 1024>(a, stream);
+    else if (c <= 24576) launch_norm_shifted<IO, 3, 1024>(a, stream);
+    else launch_norm_shifted<IO, 4, 1024>(a, stream);
+  } else if (c <= 1024) {
+    launch_after(rmsnorm_q8_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a);
+  } else {
+    launch_after(rmsnorm_q8_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a);
+  }
   return PRM_OK;
 }
 
@@ -248,6 +324,16 @@ struct NormGradArgs {
   int cols, weight_fp32;
   float eps;
 };
+
+// Blocks of `threads` threads that an SM holds in the gradient's kernels without a ring: 768 threads at 80
+// registers with one oct per thread, 512 at 128 with more.
+__host__ __device__ constexpr int grad_blocks(int threads, int nv = 1) {
+  return threads <= 32 ? 8 : threads <= 128 ? 6 : threads <= 256 ? (nv == 1 ? 3 : 2) : 1;
+}
+// Asks the L2 for the line of p (one lane in eight: 128 bytes of 16-byte pieces).
+__device__ __forceinline__ void prefetch_line(const void* p) {
+  if ((threadIdx.x & 7) == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
 
 // grad_w from the blocks' lines of partial sums, after a barrier of the whole (cooperative) grid: 32
 // columns per block and turn, each warp adds its share of the lines, all in a fixed order.
@@ -314,7 +400,7 @@ __device__ __forceinline__ void grad_oct(const float2 (&gy)[4], const float2 (&h
 // stays in registers until the block's last row.  One cooperative launch: the blocks' shares are added
 // behind a grid-wide barrier, which costs less than a second launch.
 template <typename IO, typename WT, int NV, int TPR>
-__global__ void __launch_bounds__(TPR) rmsnorm_q8_grad_kernel(const NormGradArgs a) {
+__global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
   grid_wait();
   grid_trigger();
@@ -340,6 +426,11 @@ __global__ void __launch_bounds__(TPR) rmsnorm_q8_grad_kernel(const NormGradArgs
         gyv[v].load_stream(gyp + c);
         hv[v].load_stream(hp + c);
         if (ghp) ghv[v].load_stream(ghp + c);
+        if (row + gridDim.x < a.rows) {                          // the row after this one
+          prefetch_line(gyp + (int64_t)gridDim.x * a.ld_gy + c);
+          prefetch_line(hp + (int64_t)gridDim.x * a.ld_h + c);
+          if (ghp) prefetch_line(ghp + (int64_t)gridDim.x * a.ld_gh + c);
+        }
       }
     }
     float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
@@ -475,10 +566,85 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
   grad_weight<kRingThreads>(a);
 }
 
+// Rows that start anywhere, or too wide for the kernels above.  The grid is a multiple of eight blocks
+// (or has one row per block), so that all rows of a block start alike and a thread keeps its columns.
+template <typename IO, int NV, int TPR>
+__global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_shifted_kernel(const NormGradArgs a) {
+  __shared__ float red[2][64];
+  const int shift = oct_shift(reinterpret_cast<const IO*>(a.h) + (int64_t)blockIdx.x * a.ld_h);
+  float2 gw[NV][4], w[NV][4];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    load_factors(a.weight, a.weight_fp32, ((int)threadIdx.x + v * TPR) * 8 - shift, a.cols, w[v]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) gw[v][e] = make_float2(0.f, 0.f);
+  }
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    const OctRow<IO> gyr(a.gy, row, a.rows, a.ld_gy, a.cols), hr(a.h, row, a.rows, a.ld_h, a.cols),
+        ghr(a.gh ? a.gh : a.h, row, a.rows, a.gh ? a.ld_gh : a.ld_h, a.cols);
+    Oct<IO> gyv[NV], hv[NV], ghv[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = ((int)threadIdx.x + v * TPR) * 8 - shift;
+      gyr.load(c, a.cols, gyv[v]);
+      hr.load(c, a.cols, hv[v]);
+      if (a.gh) ghr.load(c, a.cols, ghv[v]);
+      if (row + gridDim.x < a.rows && c >= 0 && c < a.cols) {     // the row after this one
+        prefetch_line(gyr.p + (int64_t)gridDim.x * a.ld_gy + c);
+        prefetch_line(hr.p + (int64_t)gridDim.x * a.ld_h + c);
+        if (a.gh) prefetch_line(ghr.p + (int64_t)gridDim.x * a.ld_gh + c);
+      }
+    }
+    float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = ((int)threadIdx.x + v * TPR) * 8 - shift;
+      float2 gy[4], h[4];
+      get_part(gyv[v], c, a.cols, gy);
+      get_part(hv[v], c, a.cols, h);
+      grad_sums(gy, h, w[v], ss2, gh2);
+    }
+    float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
+    block_sum2<TPR>(ss, gh, red[turn]);
+    const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
+    const float2 s2 = make_float2(s, s), nk = make_float2(-k, -k);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = ((int)threadIdx.x + v * TPR) * 8 - shift;
+      float2 gy[4], h[4], o[4];
+      get_part(gyv[v], c, a.cols, gy);
+      get_part(hv[v], c, a.cols, h);
+      if (a.gh) {
+        ghv[v].get(o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = make_float2(0.f, 0.f);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 gs = mul2(gy[e], s2);
+        gw[v][e] = fma2(gs, h[e], gw[v][e]);
+        o[e] = fma2(gs, w[v][e], fma2(h[e], nk, o[e]));
+      }
+      store_part(reinterpret_cast<IO*>(a.gx) + row * a.ld_gx, c, a.cols, o);
+    }
+  }
+  float* part = a.part + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = ((int)threadIdx.x + v * TPR) * 8 - shift;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c + k >= 0 && c + k < a.cols) part[c + k] = k & 1 ? gw[v][k / 2].y : gw[v][k / 2].x;
+  }
+  grad_weight<TPR>(a);
+}
+
 // Any alignment, any length: two passes over the row, and the block's share of grad_w collected in
 // its line of the scratch (each thread its own columns).
 template <typename IO, int THREADS>
-__global__ void __launch_bounds__(THREADS) rmsnorm_q8_grad_single_kernel(const NormGradArgs a) {
+__global__ void __launch_bounds__(THREADS, grad_blocks(THREADS)) rmsnorm_q8_grad_single_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
   grid_wait();
   grid_trigger();
@@ -511,7 +677,10 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_q8_grad_single_kernel(const N
   grad_weight<THREADS>(a);
 }
 
-constexpr int kGradParts = 296;    // two blocks per SM
+// Lines of partial sums: what the launches below come to at most.
+int grad_parts(int64_t rows, int64_t cols) {
+  return (int)std::min<int64_t>(rows, kRingBlocks * (cols <= 256 ? 8 : cols <= 1024 ? 6 : cols <= 6144 ? 3 : 1));
+}
 
 template <typename IO, typename WT, int W, bool GH>
 int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
@@ -521,10 +690,9 @@ int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
                      (size_t)a.cols * sizeof(IO) * (GH ? 3 : 2) * kR * kGroups, 0, (size_t)kGroups * a.cols * 4, true,
                      stream, a);
 }
-// `blocks`: how many of them an SM is sure to hold at once.
-int launch_grad(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int blocks, cudaStream_t stream) {
+int launch_grad(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int nv, cudaStream_t stream) {
   void* args[1] = {&a};
-  const unsigned grid = (unsigned)std::min<int64_t>(a.rows, blocks * kRingBlocks);
+  const unsigned grid = (unsigned)std::min<int64_t>(a.rows, grad_blocks(threads, nv) * kRingBlocks / 8 * 8);
   return cudaLaunchCooperativeKernel((const void*)kernel, dim3(grid), dim3((unsigned)threads), args, 0, stream) ==
                  cudaSuccess
              ? PRM_OK
@@ -539,16 +707,27 @@ int run_grad(const NormGradArgs& a, cudaStream_t stream) {
       return a.gh ? launch_grad_stream<IO, WT, decltype(w)::value, true>(a, stream)
                   : launch_grad_stream<IO, WT, decltype(w)::value, false>(a, stream);
     });
-  if (c <= 256) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 32>, a, 32, 2, stream);
-  if (c <= 1024) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 128>, a, 128, 2, stream);
+  if (c <= 256) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 32>, a, 32, 1, stream);
+  if (c <= 1024) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 128>, a, 128, 1, stream);
+  if (c <= 2048) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 256>, a, 256, 1, stream);
   if (c <= 4096) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 512>, a, 512, 1, stream);
-  return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 2, 512>, a, 512, 1, stream);
+  return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 2, 512>, a, 512, 2, stream);
 }
 
+// `alike`: the matrices' rows start alike.
 template <typename IO>
-int run_grad_single(const NormGradArgs& a, cudaStream_t stream) {
-  if (a.cols <= 1024) return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 128>, a, 128, 2, stream);
-  if (a.cols <= 8192) return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 512>, a, 512, 2, stream);
+int run_grad_single(const NormGradArgs& a, bool alike, cudaStream_t stream) {
+  const int c = a.cols + 7;
+  if (alike && c <= 16384) {
+    if (c <= 256) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 1, 32>, a, 32, 1, stream);
+    if (c <= 1024) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 1, 128>, a, 128, 1, stream);
+    if (c <= 2048) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 1, 256>, a, 256, 1, stream);
+    if (c <= 4096) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 2, 256>, a, 256, 2, stream);
+    if (c <= 6144) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 3, 256>, a, 256, 3, stream);
+    if (c <= 8192) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 2, 512>, a, 512, 2, stream);
+    return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 2, 1024>, a, 1024, 2, stream);
+  }
+  if (a.cols <= 1024) return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 128>, a, 128, 1, stream);
   return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 1024>, a, 1024, 1, stream);
 }
 
@@ -580,7 +759,15 @@ extern "C" int prm_rmsnorm_q8(const void* x, int64_t ld_x, const void* residual,
                     (!residual || (ld_residual % 8 == 0 && ld_h % 8 == 0 && aligned16(residual) && aligned16(h_out)));
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   int code;
-  if (!octs) code = io_fp32 ? run_norm_single<float>(a, stream) : run_norm_single<__nv_bfloat16>(a, stream);
+  if (!octs) {
+    auto alike = [&](auto type) {
+      using T = decltype(type);
+      return ((uintptr_t)q_out & 7) == 0 && ld_q % 8 == 0 &&
+             (!residual || (octs_alike<T>(x, ld_x, residual, ld_residual) && octs_alike<T>(x, ld_x, h_out, ld_h)));
+    };
+    code = io_fp32 ? run_norm_single<float>(a, alike(float()), stream)
+                   : run_norm_single<__nv_bfloat16>(a, alike(__nv_bfloat16()), stream);
+  }
   else if (io_fp32)
     code = weight_fp32 ? run_norm<float, float>(a, stream) : run_norm<float, __nv_bfloat16>(a, stream);
   else
@@ -590,7 +777,7 @@ extern "C" int prm_rmsnorm_q8(const void* x, int64_t ld_x, const void* residual,
 
 extern "C" size_t prm_rmsnorm_q8_scratch_bytes(int64_t rows, int64_t cols) {
   if (rows < 1 || cols < 1) return 0;
-  return (size_t)std::min<int64_t>(rows, kGradParts) * (size_t)cols * 4;
+  return (size_t)grad_parts(rows, cols) * (size_t)cols * 4;
 }
 
 extern "C" int prm_rmsnorm_q8_backward(const void* grad_y, int64_t ld_grad_y, const void* h, int64_t ld_h,
@@ -619,7 +806,15 @@ extern "C" int prm_rmsnorm_q8_backward(const void* grad_y, int64_t ld_grad_y, co
   const bool octs = cols % 8 == 0 && cols <= 8192 && ld_grad_y % 8 == 0 && ld_h % 8 == 0 && ld_grad_x % 8 == 0 &&
                     aligned16(grad_y) && aligned16(h) && aligned16(grad_x) && aligned16(weight) &&
                     (!grad_h || (ld_grad_h % 8 == 0 && aligned16(grad_h)));
-  if (!octs) return io_fp32 ? run_grad_single<float>(a, stream) : run_grad_single<__nv_bfloat16>(a, stream);
+  if (!octs) {
+    auto alike = [&](auto type) {
+      using T = decltype(type);
+      return octs_alike<T>(h, ld_h, grad_y, ld_grad_y) && octs_alike<T>(h, ld_h, grad_x, ld_grad_x) &&
+             (!grad_h || octs_alike<T>(h, ld_h, grad_h, ld_grad_h));
+    };
+    return io_fp32 ? run_grad_single<float>(a, alike(float()), stream)
+                   : run_grad_single<__nv_bfloat16>(a, alike(__nv_bfloat16()), stream);
+  }
   if (io_fp32) return weight_fp32 ? run_grad<float, float>(a, stream) : run_grad<float, __nv_bfloat16>(a, stream);
   return weight_fp32 ? run_grad<__nv_bfloat16, float>(a, stream) : run_grad<__nv_bfloat16, __nv_bfloat16>(a, stream);
 }

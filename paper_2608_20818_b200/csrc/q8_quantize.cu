@@ -82,6 +82,43 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_kernel(co
   if (c0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
 }
 
+// Rows that start anywhere (odd widths), or too wide for the kernel above: the same on octs aligned in
+// memory.
+template <typename IO, int NV, int TPR>
+__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_shifted_kernel(const QuantArgs a) {
+  constexpr int kRows = TPR == 32 ? 8 : 1;
+  __shared__ float red[64];
+  __shared__ uint64_t stage[kRows][NV * TPR + 1];
+  grid_wait();
+  grid_trigger();
+  const int o0 = threadIdx.x % TPR;
+  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+  if (row >= a.rows) return;
+  const OctRow<IO> x(a.x, row, a.rows, a.ld_x, a.cols);
+  const int shift = oct_shift(x.p);
+  Oct<IO> xv[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) x.load((o0 + v * TPR) * 8 - shift, a.cols, xv[v]);
+  float2 t[NV][4];
+  float none = 0.f, top = 0.f;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (o0 + v * TPR) * 8 - shift;
+    get_part(xv[v], c, a.cols, t[v]);
+    if (a.fold_cols) {
+      float2 f[4];
+      load_factors(a.fold_cols, 1, c, a.cols, f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[v][e] = mul2(t[v][e], f[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max_abs(top, t[v][e]);
+  }
+  block_sum_top<TPR>(none, top, red);
+  store_octs_shifted<NV, TPR>(stage[threadIdx.x / TPR], a.q_rows + row * a.ld_qr, t, o0, shift, a.cols, top, a.format);
+  if (o0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
+}
+
 // Any alignment, any length: two passes over the row.
 template <typename IO, int THREADS>
 __global__ void __launch_bounds__(THREADS) quantize_rows_single_kernel(const QuantArgs a) {
@@ -501,10 +538,27 @@ void run_rows(const QuantArgs& a, bool octs, cudaStream_t stream) {
     else if (c <= 4096) launch_rows<IO, 2, 256>(a, stream);
     else if (c <= 8192) launch_rows<IO, 2, 512>(a, stream);
     else launch_rows<IO, 2, 1024>(a, stream);
+  } else if (c + 7 <= 32768 && a.ld_qr % 8 == 0 && ((uintptr_t)a.q_rows & 7) == 0) {
+    auto go = [&](auto kernel, int per_block, int threads) {
+      launch_after(kernel, (unsigned)((a.rows + per_block - 1) / per_block), (unsigned)threads, 0, stream, 0, a);
+    };
+    const int w = c + 7;                  // a row may need one more oct
+    if (w <= 256) go(quantize_rows_shifted_kernel<IO, 1, 32>, 8, 256);
+    else if (w <= 512) go(quantize_rows_shifted_kernel<IO, 2, 32>, 8, 256);
+    else if (w <= 1024) go(quantize_rows_shifted_kernel<IO, 1, 128>, 1, 128);
+    else if (w <= 2048) go(quantize_rows_shifted_kernel<IO, 2, 128>, 1, 128);
+    else if (w <= 3072) go(quantize_rows_shifted_kernel<IO, 3, 128>, 1, 128);
+    else if (w <= 4096) go(quantize_rows_shifted_kernel<IO, 2, 256>, 1, 256);
+    else if (w <= 6144) go(quantize_rows_shifted_kernel<IO, 3, 256>, 1, 256);
+    else if (w <= 8192) go(quantize_rows_shifted_kernel<IO, 2, 512>, 1, 512);
+    else if (w <= 12288) go(quantize_rows_shifted_kernel<IO, 3, 512>, 1, 512);
+    else if (w <= 16384) go(quantize_rows_shifted_kernel<IO, 2, 1024>, 1, 1024);
+    else if (w <= 24576) go(quantize_rows_shifted_kernel<IO, 3, 1024>, 1, 1024);
+    else go(quantize_rows_shifted_kernel<IO, 4, 1024>, 1, 1024);
+  } else if (c <= 1024) {
+    launch_after(quantize_rows_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a);
   } else {
-    if (c <= 1024) launch_after(quantize_rows_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a);
-    else if (c <= 8192) launch_after(quantize_rows_single_kernel<IO, 256>, (unsigned)a.rows, 256, 0, stream, 0, a);
-    else launch_after(quantize_rows_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a);
+    launch_after(quantize_rows_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a);
   }
 }
 

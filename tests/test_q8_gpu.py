@@ -12,6 +12,9 @@ EPS = 1e-6
 SHAPES = [(1, 1), (1, 8), (3, 5), (2, 256), (9, 257), (7, 512), (5, 1000), (3, 1024), (4, 1111), (1, 2048),
           (130, 2056), (3, 4096), (2, 4104), (2, 8192), (2, 8193), (1, 16384), (1, 16400), (1, 16401), (1, 32768),
           (2, 32776), (1, 40001), (1000, 64), (4099, 24), (0, 16),
+          # rows that start on every offset from a vector, for each width of the kernels that walk them
+          (17, 3), (40, 249), (33, 505), (310, 1001), (19, 2041), (310, 4089), (11, 8185), (9, 16377), (9, 20001),
+          (9, 16378), (300, 4100), (12, 12), (3, 24576), (2, 32768),
           # large enough to be streamed: each group width, full and partly filled, rows that do not divide
           (8201, 512), (4700, 1000), (4099, 1024), (2050, 2056), (2100, 2048), (1030, 4096), (700, 6000), (519, 8192)]
 
