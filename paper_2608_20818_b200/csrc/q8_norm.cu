@@ -105,59 +105,6 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const
   if (c0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
 }
 
-constexpr int kNormOcts = 4;              // per thread and row in the streaming kernel
-
-// Large matrices: rows streamed through a ring, a group of W warps to a row.
-template <typename IO, typename WT, int W, bool RES>
-__global__ void __launch_bounds__(kRingThreads, 1) rmsnorm_q8_stream_kernel(const NormArgs a, int stages, int* status) {
-  constexpr int kArr = RES ? 2 : 1, kNV = kNormOcts, kStep = W * 32 * 8;
-  const int c0 = (threadIdx.x % (W * 32)) * 8;
-  const void* const src[2] = {a.x, a.residual};
-  const int64_t ld[2] = {a.ld_x, a.ld_r};
-  RowRing<IO, W, 1, kArr> ring(ring_block<W, 1>(), src, ld, a.rows, a.cols, stages, status);
-  ring.start();
-  grid_wait();
-  grid_trigger();
-  if (ring.producer) {
-    ring.serve();
-    ring.finish();
-    return;
-  }
-  Oct<WT> wv[kNV];
-#pragma unroll
-  for (int v = 0; v < kNV; ++v)
-    if (c0 + v * kStep < a.cols) wv[v].load(reinterpret_cast<const WT*>(a.weight) + c0 + v * kStep);
-  for (int i = 0; i < ring.n; ++i) {
-    const int64_t row = ring.row(i);
-    float2 t[kNV][4], sum2 = make_float2(0.f, 0.f);
-    float sum[1], top[1] = {0.f};
-    if (ring.wait()) {
-      IO* h = RES ? reinterpret_cast<IO*>(a.h) + row * a.ld_h : nullptr;
-#pragma unroll
-      for (int v = 0; v < kNV; ++v) {
-        const int c = c0 + v * kStep;
-        if (c < a.cols) {
-          Oct<IO> x, r;
-          float2 w[4];
-          x.load(ring.at(0, 0) + c);
-          if constexpr (RES) r.load(ring.at(0, 1) + c);
-          else r.zero();
-          wv[v].get(w);
-          norm_oct<IO, RES>(x, r, w, h + c, t[v], sum2, top[0]);
-        }
-      }
-    }
-    ring.release();
-    ring.advance();
-    sum[0] = sum2.x + sum2.y;
-    ring.template reduce<true, false>(i, sum, top);
-    if (ring.ok) {
-      store_octs<kNV>(a.q + row * a.ld_q, t, c0, kStep, a.cols, top[0], a.format);
-      if (c0 == 0) a.scale[row] = q8_scale(top[0], q8_limit(a.format)) * inv_rms(sum[0], a.cols, a.eps);
-    }
-  }
-}
-
 // Rows that start anywhere (odd widths), or too wide for the kernels above: as rmsnorm_q8_kernel, on
 // octs aligned in memory.
 template <typename IO, int NV, int TPR>
@@ -253,24 +200,14 @@ int launch_norm(const NormArgs& a, cudaStream_t stream) {
   return PRM_OK;
 }
 
-template <typename IO, typename WT, int W, bool RES>
-int launch_norm_stream(const NormArgs& a, cudaStream_t stream) {
-  constexpr int kGroups = kRingWarps / W;
-  static PerDeviceOnce once;
-  return launch_ring(rmsnorm_q8_stream_kernel<IO, WT, W, RES>, once, ring_blocks(a.rows, 1, kGroups),
-                     (size_t)a.cols * sizeof(IO) * (RES ? 2 : 1) * kGroups, 0, 0, false, stream, a);
-}
-
 template <typename IO, typename WT>
 int run_norm(const NormArgs& a, cudaStream_t stream) {
   const int c = a.cols;
-  if (ring_worth(a.rows, c))
-    return with_ring_warps<kNormOcts>(c, [&](auto w) {
-      return a.residual ? launch_norm_stream<IO, WT, decltype(w)::value, true>(a, stream)
-                        : launch_norm_stream<IO, WT, decltype(w)::value, false>(a, stream);
-    });
   if (c <= 256) return launch_norm<IO, WT, 1, 32>(a, stream);
   if (c <= 512) return launch_norm<IO, WT, 2, 32>(a, stream);
+  // One block per row costs 1 ns each, more than a short row's bytes (16384 x 1024: 18.8 us, eight rows per
+  // block 15.4); few rows end sooner with more threads (256 x 1024: 2.1 us, a warp 2.5).
+  if (c <= 1024 && a.rows >= 2048) return launch_norm<IO, WT, 4, 32>(a, stream);
   if (c <= 1024) return launch_norm<IO, WT, 1, 128>(a, stream);
   if (c <= 2048) return launch_norm<IO, WT, 2, 128>(a, stream);
   if (c <= 4096) return launch_norm<IO, WT, 2, 256>(a, stream);
@@ -335,24 +272,27 @@ __device__ __forceinline__ void prefetch_line(const void* p) {
   if ((threadIdx.x & 7) == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
 }
 
-// grad_w from the blocks' lines of partial sums, after a barrier of the whole (cooperative) grid: 32
-// columns per block and turn, each warp adds its share of the lines, all in a fixed order.
-template <int THREADS>
-__device__ __forceinline__ void grad_weight(const NormGradArgs& a) {
-  constexpr int kWarps = THREADS / 32;
-  __shared__ float s[kWarps][32];
-  cooperative_groups::this_grid().sync();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lines = gridDim.x;
-  for (int c0 = blockIdx.x * 32; c0 < a.cols; c0 += gridDim.x * 32) {
-    const int c = c0 + lane;
+// grad_w from the blocks' lines of partial sums: WIDTH columns per block and turn, 32 / WIDTH lines per
+// warp at a time, all in a fixed order.
+template <int THREADS, int WIDTH>
+__device__ __forceinline__ void grad_weight_columns(const NormGradArgs& a) {
+  constexpr int kWarps = THREADS / 32, kLines = 32 / WIDTH;
+  __shared__ float s[kWarps][WIDTH];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int lines = (int)min((int64_t)gridDim.x, a.rows);        // blocks that had a row
+  for (int c0 = blockIdx.x * WIDTH; c0 < a.cols; c0 += gridDim.x * WIDTH) {
+    const int c = c0 + lane % WIDTH;
     float sum = 0.f;
     if (c < a.cols) {
 #pragma unroll 8
-      for (int l = warp; l < lines; l += kWarps) sum += __ldcg(a.part + (int64_t)l * a.cols + c);
+      for (int l = warp * kLines + lane / WIDTH; l < lines; l += kWarps * kLines)
+        sum += __ldcg(a.part + (int64_t)l * a.cols + c);
     }
-    s[warp][lane] = sum;
+#pragma unroll
+    for (int k = WIDTH; k < 32; k *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+    if (lane < WIDTH) s[warp][lane] = sum;
     __syncthreads();
-    if (warp == 0 && c < a.cols) {
+    if (threadIdx.x < WIDTH && c < a.cols) {
 #pragma unroll
       for (int k = 1; k < kWarps; ++k) sum += s[k][lane];
       if (a.weight_fp32) reinterpret_cast<float*>(a.gw)[c] = sum;
@@ -360,6 +300,17 @@ __device__ __forceinline__ void grad_weight(const NormGradArgs& a) {
     }
     __syncthreads();
   }
+}
+
+// After a barrier of the whole (cooperative) grid: the fewest columns per turn (a sector at least) that
+// leave each block one turn, for a block that goes through many lines alone is slow (1000 x 1000, 444
+// lines: 32 columns 19 us, 8 columns 12), and so are several turns (8192 x 4096: 48.8 us, with 8 54.2).
+template <int THREADS>
+__device__ __forceinline__ void grad_weight(const NormGradArgs& a) {
+  cooperative_groups::this_grid().sync();
+  if (a.cols <= (int)gridDim.x * 8) grad_weight_columns<THREADS, 8>(a);
+  else if (a.cols <= (int)gridDim.x * 16) grad_weight_columns<THREADS, 16>(a);
+  else grad_weight_columns<THREADS, 32>(a);
 }
 
 // The two sums of a row over one oct.
@@ -462,7 +413,7 @@ __global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_ker
   }
   float* part = a.part + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
+  for (int v = 0; v < NV && blockIdx.x < a.rows; ++v) {
     const int c = c0 + v * TPR * 8;
     if (c < a.cols) {
       Oct<float> o;
@@ -632,7 +583,7 @@ __global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_shi
   }
   float* part = a.part + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
+  for (int v = 0; v < NV && blockIdx.x < a.rows; ++v) {
     const int c = ((int)threadIdx.x + v * TPR) * 8 - shift;
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -692,7 +643,10 @@ int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
 }
 int launch_grad(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int nv, cudaStream_t stream) {
   void* args[1] = {&a};
-  const unsigned grid = (unsigned)std::min<int64_t>(a.rows, grad_blocks(threads, nv) * kRingBlocks / 8 * 8);
+  // A block per row, and for few rows as many more as share the columns of grad_w at the end (1 x 4096, one
+  // block: 56 us).
+  const int64_t want = std::max<int64_t>(a.rows, (a.cols + 31) / 32);
+  const unsigned grid = (unsigned)std::min<int64_t>(want, grad_blocks(threads, nv) * kRingBlocks / 8 * 8);
   return cudaLaunchCooperativeKernel((const void*)kernel, dim3(grid), dim3((unsigned)threads), args, 0, stream) ==
                  cudaSuccess
              ? PRM_OK
@@ -702,7 +656,9 @@ int launch_grad(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int n
 template <typename IO, typename WT>
 int run_grad(const NormGradArgs& a, cudaStream_t stream) {
   const int c = a.cols;
-  if (ring_worth(a.rows, c))
+  // Streamed from these sizes on (512 x 4096: 11.6 us against 12.5), one row per block below them (256 x
+  // 4096: 10.0 us against 12.0).
+  if (c >= 256 && c <= 8192 && a.rows * c >= (int64_t)3 << 19)
     return with_ring_warps<2>(c, [&](auto w) {
       return a.gh ? launch_grad_stream<IO, WT, decltype(w)::value, true>(a, stream)
                   : launch_grad_stream<IO, WT, decltype(w)::value, false>(a, stream);

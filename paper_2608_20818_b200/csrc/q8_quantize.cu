@@ -489,7 +489,7 @@ void run_rows(const QuantArgs& a, bool octs, cudaStream_t stream) {
   if (octs && c <= 16384) {
     if (c <= 256) launch_rows<IO, 1, 32>(a, stream);
     else if (c <= 512) launch_rows<IO, 2, 32>(a, stream);
-    else if (c <= 1024) launch_rows<IO, 1, 128>(a, stream);
+    else if (c <= 1024) launch_rows<IO, 4, 32>(a, stream);   // 16384 x 1024: 8.3 us, a block per row 17.5
     else if (c <= 2048) launch_rows<IO, 2, 128>(a, stream);
     else if (c <= 4096) launch_rows<IO, 2, 256>(a, stream);
     else if (c <= 8192) launch_rows<IO, 2, 512>(a, stream);

@@ -311,10 +311,6 @@ struct RowRing {
 // The status word that prm_q8_status reads, on the current device (null if it has none).
 int* q8_status_word();
 
-// From here on streaming is faster than one row per block.
-constexpr int64_t kRingElements = 1 << 22;
-inline bool ring_worth(int64_t rows, int cols) { return cols >= 256 && cols <= 8192 && rows * cols >= kRingElements; }
-
 // Calls f with the number of warps to a row of `cols` elements, NV octs per thread.
 template <int NV, typename F>
 int with_ring_warps(int cols, F f) {
