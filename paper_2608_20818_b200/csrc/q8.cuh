@@ -310,16 +310,28 @@ __device__ __forceinline__ float as_stored(float v, const __nv_bfloat16*) {
   return __bfloat162float(__float2bfloat16_rn(v));
 }
 
-// Largest value over a warp; a NaN in any lane stays (`top` is no negative number).
-__device__ __forceinline__ float warp_top(float top) {
-  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+// Sum over groups of N neighbouring lanes of a warp, for each of them.
+template <int N>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
 }
-// Sum and largest magnitude over a block of THREADS threads (32: each warp by itself); every thread
+// Largest value over the same; a NaN in any lane stays (`top` is no negative number).
+template <int N = 32>
+__device__ __forceinline__ float group_top(float top) {
+  uint32_t v = __float_as_uint(top);
+  if constexpr (N == 32) return __uint_as_float(__reduce_max_sync(0xffffffffu, v));
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return __uint_as_float(v);
+}
+// Sum and largest magnitude over a block of THREADS threads (up to 32: groups of lanes); every thread
 // gets both.  `red`: 64 words, used once between two barriers.
 template <int THREADS>
 __device__ __forceinline__ void block_sum_top(float& sum, float& top, float* red) {
-  sum = warp_sum(sum);
-  top = warp_top(top);
+  sum = group_sum<(THREADS < 32 ? THREADS : 32)>(sum);
+  top = group_top<(THREADS < 32 ? THREADS : 32)>(top);
   if constexpr (THREADS > 32) {
     constexpr int kWarps = THREADS / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -331,7 +343,7 @@ __device__ __forceinline__ void block_sum_top(float& sum, float& top, float* red
     sum = lane < kWarps ? red[lane] : 0.f;
     top = lane < kWarps ? red[32 + lane] : 0.f;
     sum = warp_sum(sum);
-    top = warp_top(top);
+    top = group_top(top);
   }
 }
 

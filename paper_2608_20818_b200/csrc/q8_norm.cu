@@ -62,17 +62,17 @@ __device__ __forceinline__ void norm_oct(Oct<IO> x, Oct<IO> r, const float2 (&w)
   }
 }
 
-// One row per group of TPR threads (a warp: eight rows per block; else a block), 8 * NV elements per
-// thread.
+// One row per group of TPR threads (up to a warp: 256 / TPR rows per block; else a block), 8 * NV elements
+// per thread.
 template <typename IO, typename WT, int NV, int TPR, bool RES>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const NormArgs a) {
-  constexpr int kRows = TPR == 32 ? 8 : 1;
+__global__ void __launch_bounds__(TPR <= 32 ? 256 : TPR) rmsnorm_q8_kernel(const NormArgs a) {
+  constexpr int kRows = TPR <= 32 ? 256 / TPR : 1;
   __shared__ float red[64];
   grid_wait();
   grid_trigger();
   const int c0 = (threadIdx.x % TPR) * 8;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-  if (row >= a.rows) return;              // whole warps (kRows > 1) or no thread
+  const int cols = row < a.rows ? a.cols : 0;                   // what this thread has of the row's columns
   const IO* x = reinterpret_cast<const IO*>(a.x) + row * a.ld_x;
   const IO* r = RES ? reinterpret_cast<const IO*>(a.residual) + row * a.ld_r : nullptr;
   IO* h = RES ? reinterpret_cast<IO*>(a.h) + row * a.ld_h : nullptr;
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = c0 + v * TPR * 8;
-    if (c < a.cols) {
+    if (c < cols) {
       xv[v].load_stream(x + c);
       if constexpr (RES) rv[v].load_stream(r + c);
       else rv[v].zero();
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = c0 + v * TPR * 8;
-    if (c < a.cols) {
+    if (c < cols) {
       float2 w[4];
       wv[v].get(w);
       norm_oct<IO, RES>(xv[v], rv[v], w, h + c, t[v], sum2, top);
@@ -101,8 +101,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_kernel(const
   }
   float sum = sum2.x + sum2.y;
   block_sum_top<TPR>(sum, top, red);
-  store_octs<NV>(a.q + row * a.ld_q, t, c0, TPR * 8, a.cols, top, a.format);
-  if (c0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
+  store_octs<NV>(a.q + row * a.ld_q, t, c0, TPR * 8, cols, top, a.format);
+  if (c0 == 0 && cols) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
 }
 
 // Rows that start anywhere (odd widths), or too wide for the kernels above: as rmsnorm_q8_kernel, on
@@ -193,16 +193,18 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_q8_single_kernel(const NormAr
 
 template <typename IO, typename WT, int NV, int TPR>
 int launch_norm(const NormArgs& a, cudaStream_t stream) {
-  constexpr int kRows = TPR == 32 ? 8 : 1;
+  constexpr int kRows = TPR <= 32 ? 256 / TPR : 1, kThreads = TPR <= 32 ? 256 : TPR;
   const unsigned blocks = (unsigned)((a.rows + kRows - 1) / kRows);
-  if (a.residual) launch_after(rmsnorm_q8_kernel<IO, WT, NV, TPR, true>, blocks, TPR == 32 ? 256 : TPR, 0, stream, 0, a);
-  else launch_after(rmsnorm_q8_kernel<IO, WT, NV, TPR, false>, blocks, TPR == 32 ? 256 : TPR, 0, stream, 0, a);
+  if (a.residual) launch_after(rmsnorm_q8_kernel<IO, WT, NV, TPR, true>, blocks, kThreads, 0, stream, 0, a);
+  else launch_after(rmsnorm_q8_kernel<IO, WT, NV, TPR, false>, blocks, kThreads, 0, stream, 0, a);
   return PRM_OK;
 }
 
 template <typename IO, typename WT>
 int run_norm(const NormArgs& a, cudaStream_t stream) {
   const int c = a.cols;
+  if (c <= 64) return launch_norm<IO, WT, 1, 8>(a, stream);
+  if (c <= 128) return launch_norm<IO, WT, 1, 16>(a, stream);
   if (c <= 256) return launch_norm<IO, WT, 1, 32>(a, stream);
   if (c <= 512) return launch_norm<IO, WT, 2, 32>(a, stream);
   // One block per row costs 1 ns each, more than a short row's bytes (16384 x 1024: 18.8 us, eight rows per
@@ -267,6 +269,8 @@ struct NormGradArgs {
 __host__ __device__ constexpr int grad_blocks(int threads, int nv = 1) {
   return threads <= 32 ? 8 : threads <= 128 ? 6 : threads <= 256 ? (nv == 1 ? 3 : 2) : 1;
 }
+constexpr int kNarrowBlocks = 4;          // per SM, of 256 threads
+
 // Asks the L2 for the line of p (one lane in eight: 128 bytes of 16-byte pieces).
 __device__ __forceinline__ void prefetch_line(const void* p) {
   if ((threadIdx.x & 7) == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
@@ -275,11 +279,10 @@ __device__ __forceinline__ void prefetch_line(const void* p) {
 // grad_w from the blocks' lines of partial sums: WIDTH columns per block and turn, 32 / WIDTH lines per
 // warp at a time, all in a fixed order.
 template <int THREADS, int WIDTH>
-__device__ __forceinline__ void grad_weight_columns(const NormGradArgs& a) {
+__device__ __forceinline__ void grad_weight_columns(const NormGradArgs& a, int lines) {
   constexpr int kWarps = THREADS / 32, kLines = 32 / WIDTH;
   __shared__ float s[kWarps][WIDTH];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int lines = (int)min((int64_t)gridDim.x, a.rows);        // blocks that had a row
   for (int c0 = blockIdx.x * WIDTH; c0 < a.cols; c0 += gridDim.x * WIDTH) {
     const int c = c0 + lane % WIDTH;
     float sum = 0.f;
@@ -306,11 +309,12 @@ __device__ __forceinline__ void grad_weight_columns(const NormGradArgs& a) {
 // leave each block one turn, for a block that goes through many lines alone is slow (1000 x 1000, 444
 // lines: 32 columns 19 us, 8 columns 12), and so are several turns (8192 x 4096: 48.8 us, with 8 54.2).
 template <int THREADS>
-__device__ __forceinline__ void grad_weight(const NormGradArgs& a) {
+__device__ __forceinline__ void grad_weight(const NormGradArgs& a, int rows_per_block = 1) {
   cooperative_groups::this_grid().sync();
-  if (a.cols <= (int)gridDim.x * 8) grad_weight_columns<THREADS, 8>(a);
-  else if (a.cols <= (int)gridDim.x * 16) grad_weight_columns<THREADS, 16>(a);
-  else grad_weight_columns<THREADS, 32>(a);
+  const int lines = (int)min((int64_t)gridDim.x, (a.rows + rows_per_block - 1) / rows_per_block);   // blocks with rows
+  if (a.cols <= (int)gridDim.x * 8) grad_weight_columns<THREADS, 8>(a, lines);
+  else if (a.cols <= (int)gridDim.x * 16) grad_weight_columns<THREADS, 16>(a, lines);
+  else grad_weight_columns<THREADS, 32>(a, lines);
 }
 
 // The two sums of a row over one oct.
@@ -345,6 +349,58 @@ __device__ __forceinline__ void grad_oct(const float2 (&gy)[4], const float2 (&h
   Oct<IO> r;
   r.set(o);
   r.store(out);
+}
+
+// Narrow rows (the heads of a query-key norm): a group of TPR lanes to a row, 256 / TPR rows per block and
+// turn, the next turn's loads in flight; a block's groups add their shares of grad_w in shared memory.
+template <typename IO, typename WT, int TPR>
+__global__ void __launch_bounds__(256, kNarrowBlocks) rmsnorm_q8_grad_narrow_kernel(const NormGradArgs a) {
+  constexpr int kRows = 256 / TPR;
+  __shared__ __align__(16) float sums[kRows][TPR * 8];
+  grid_wait();
+  grid_trigger();
+  const int c0 = (threadIdx.x % TPR) * 8, group = threadIdx.x / TPR;
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  float2 gw[4], w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) gw[e] = w[e] = make_float2(0.f, 0.f);
+  if (c0 < a.cols) load_oct(reinterpret_cast<const WT*>(a.weight) + c0, w);
+  Oct<IO> next[3];
+  auto fetch = [&](int64_t row) {
+    if (row < a.rows && c0 < a.cols) {
+      next[0].load_stream(reinterpret_cast<const IO*>(a.gy) + row * a.ld_gy + c0);
+      next[1].load_stream(reinterpret_cast<const IO*>(a.h) + row * a.ld_h + c0);
+      if (a.gh) next[2].load_stream(reinterpret_cast<const IO*>(a.gh) + row * a.ld_gh + c0);
+    } else {
+      next[0].zero();
+      next[1].zero();
+    }
+  };
+  fetch((int64_t)blockIdx.x * kRows + group);
+  for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += step) {
+    const int64_t row = base + group;
+    Oct<IO> add = next[2];
+    float2 gy[4], h[4], ss2 = make_float2(0.f, 0.f), gh2 = ss2;
+    next[0].get(gy);
+    next[1].get(h);
+    fetch(row + step);
+    grad_sums(gy, h, w, ss2, gh2);
+    const float ss = group_sum<TPR>(ss2.x + ss2.y), gh = group_sum<TPR>(gh2.x + gh2.y);
+    const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
+    if (row < a.rows && c0 < a.cols)
+      grad_oct<IO>(gy, h, w, a.gh ? &add : nullptr, s, k, reinterpret_cast<IO*>(a.gx) + row * a.ld_gx + c0, gw);
+  }
+  Oct<float> o;
+  o.set(gw);
+  o.store(&sums[group][c0]);
+  __syncthreads();
+  if ((int)threadIdx.x < a.cols && (int64_t)blockIdx.x * kRows < a.rows) {
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < kRows; ++g) sum += sums[g][threadIdx.x];
+    a.part[(int64_t)blockIdx.x * a.cols + threadIdx.x] = sum;
+  }
+  grad_weight<256>(a, kRows);
 }
 
 // A block walks over rows; a thread keeps the same columns in all of them, so its share of grad_w
@@ -471,7 +527,7 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
         }
       }
     }
-    ring.template reduce<true, true>(i, ss, gh);
+    ring.template reduce<true>(i, ss, gh);
     if (ring.ok) {
 #pragma unroll
       for (int r = 0; r < kR; ++r) {
@@ -641,29 +697,43 @@ int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
                      (size_t)a.cols * sizeof(IO) * (GH ? 3 : 2) * kR * kGroups, 0, (size_t)kGroups * a.cols * 4, true,
                      stream, a);
 }
-int launch_grad(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int nv, cudaStream_t stream) {
+// At least as many blocks as share the columns of grad_w at the end (1 x 4096, one block: 56 us).
+int launch_grad_blocks(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int64_t blocks, cudaStream_t stream) {
   void* args[1] = {&a};
-  // A block per row, and for few rows as many more as share the columns of grad_w at the end (1 x 4096, one
-  // block: 56 us).
-  const int64_t want = std::max<int64_t>(a.rows, (a.cols + 31) / 32);
-  const unsigned grid = (unsigned)std::min<int64_t>(want, grad_blocks(threads, nv) * kRingBlocks / 8 * 8);
+  const unsigned grid = (unsigned)std::max<int64_t>(blocks, std::min(kRingBlocks, (a.cols + 31) / 32));
   return cudaLaunchCooperativeKernel((const void*)kernel, dim3(grid), dim3((unsigned)threads), args, 0, stream) ==
                  cudaSuccess
              ? PRM_OK
              : PRM_ERR_CUDA;
 }
+// Two blocks per SM until they have six rows each: a block more is a line more of partial sums (512 x
+// 2048: 7.5 us, three per SM 9.4; 5000 x 1001: 23 us, two per SM 31).
+int launch_grad(void (*kernel)(NormGradArgs), const NormGradArgs& a, int threads, int nv, cudaStream_t stream) {
+  const int64_t want = std::min<int64_t>(a.rows, std::max<int64_t>(2 * kRingBlocks, (a.rows + 47) / 48 * 8));
+  return launch_grad_blocks(kernel, a, threads, std::min<int64_t>(want, grad_blocks(threads, nv) * kRingBlocks / 8 * 8),
+                            stream);
+}
+template <typename IO, typename WT, int TPR>
+int launch_grad_narrow(const NormGradArgs& a, cudaStream_t stream) {
+  constexpr int kRows = 256 / TPR;
+  return launch_grad_blocks(rmsnorm_q8_grad_narrow_kernel<IO, WT, TPR>, a, 256,
+                            std::min<int64_t>((a.rows + kRows - 1) / kRows, kNarrowBlocks * kRingBlocks), stream);
+}
 
 template <typename IO, typename WT>
 int run_grad(const NormGradArgs& a, cudaStream_t stream) {
   const int c = a.cols;
-  // Streamed from these sizes on (512 x 4096: 11.6 us against 12.5), one row per block below them (256 x
-  // 4096: 10.0 us against 12.0).
-  if (c >= 256 && c <= 8192 && a.rows * c >= (int64_t)3 << 19)
+  if (c <= 64) return launch_grad_narrow<IO, WT, 8>(a, stream);
+  if (c <= 128) return launch_grad_narrow<IO, WT, 16>(a, stream);
+  if (c <= 256) return launch_grad_narrow<IO, WT, 32>(a, stream);
+  // Streamed from these sizes on, in fewer blocks that last longer (1024 x 1024: 8.6 us against 12.3; 1024 x
+  // 4096: 11.9 against 15.0), else a row or two per block (256 x 4096: 7.1 us against 10.1; 512 x 512: 6.3
+  // against 9.0).
+  if (c <= 8192 && (a.rows >= 768 || a.rows * c >= (int64_t)1 << 21))
     return with_ring_warps<2>(c, [&](auto w) {
       return a.gh ? launch_grad_stream<IO, WT, decltype(w)::value, true>(a, stream)
                   : launch_grad_stream<IO, WT, decltype(w)::value, false>(a, stream);
     });
-  if (c <= 256) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 32>, a, 32, 1, stream);
   if (c <= 1024) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 128>, a, 128, 1, stream);
   if (c <= 2048) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 256>, a, 256, 1, stream);
   if (c <= 4096) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 512>, a, 512, 1, stream);

@@ -52,25 +52,25 @@ __device__ __forceinline__ void fold_oct(const float* f, int c, float2 (&t)[4]) 
 
 // One row per group of TPR threads, in registers between the maximum and the rounding.
 template <typename IO, int NV, int TPR>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_kernel(const QuantArgs a) {
-  constexpr int kRows = TPR == 32 ? 8 : 1;
+__global__ void __launch_bounds__(TPR <= 32 ? 256 : TPR) quantize_rows_kernel(const QuantArgs a) {
+  constexpr int kRows = TPR <= 32 ? 256 / TPR : 1;
   __shared__ float red[64];
   grid_wait();
   grid_trigger();
   const int c0 = (threadIdx.x % TPR) * 8;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-  if (row >= a.rows) return;
+  const int cols = row < a.rows ? a.cols : 0;                   // what this thread has of the row's columns
   const IO* x = reinterpret_cast<const IO*>(a.x) + row * a.ld_x;
   Oct<IO> xv[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v)
-    if (c0 + v * TPR * 8 < a.cols) xv[v].load_stream(x + c0 + v * TPR * 8);
+    if (c0 + v * TPR * 8 < cols) xv[v].load_stream(x + c0 + v * TPR * 8);
   float2 t[NV][4];
   float none = 0.f, top = 0.f;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = c0 + v * TPR * 8;
-    if (c < a.cols) {
+    if (c < cols) {
       xv[v].get(t[v]);
       fold_oct(a.fold_cols, c, t[v]);
 #pragma unroll
@@ -78,8 +78,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_kernel(co
     }
   }
   block_sum_top<TPR>(none, top, red);
-  store_octs<NV>(a.q_rows + row * a.ld_qr, t, c0, TPR * 8, a.cols, top, a.format);
-  if (c0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
+  store_octs<NV>(a.q_rows + row * a.ld_qr, t, c0, TPR * 8, cols, top, a.format);
+  if (c0 == 0 && cols) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
 }
 
 // Rows that start anywhere (odd widths), or too wide for the kernel above: the same on octs aligned in
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
     ring.release();
     ring.advance();
     if constexpr (ROWS) {
-      ring.template reduce<false, false>(i, none, top);
+      ring.template reduce<false>(i, none, top);
       if (ring.ok) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -479,15 +479,18 @@ int run_stream(QuantArgs a, cudaStream_t stream) {
 
 template <typename IO, int NV, int TPR>
 void launch_rows(const QuantArgs& a, cudaStream_t stream) {
-  constexpr int kRows = TPR == 32 ? 8 : 1;
-  launch_after(quantize_rows_kernel<IO, NV, TPR>, (unsigned)((a.rows + kRows - 1) / kRows), TPR == 32 ? 256 : TPR, 0, stream, 0, a);
+  constexpr int kRows = TPR <= 32 ? 256 / TPR : 1;
+  launch_after(quantize_rows_kernel<IO, NV, TPR>, (unsigned)((a.rows + kRows - 1) / kRows), TPR <= 32 ? 256 : TPR, 0,
+               stream, 0, a);
 }
 
 template <typename IO>
 void run_rows(const QuantArgs& a, bool octs, cudaStream_t stream) {
   const int c = a.cols;
   if (octs && c <= 16384) {
-    if (c <= 256) launch_rows<IO, 1, 32>(a, stream);
+    if (c <= 64) launch_rows<IO, 1, 8>(a, stream);
+    else if (c <= 128) launch_rows<IO, 1, 16>(a, stream);
+    else if (c <= 256) launch_rows<IO, 1, 32>(a, stream);
     else if (c <= 512) launch_rows<IO, 2, 32>(a, stream);
     else if (c <= 1024) launch_rows<IO, 4, 32>(a, stream);   // 16384 x 1024: 8.3 us, a block per row 17.5
     else if (c <= 2048) launch_rows<IO, 2, 128>(a, stream);

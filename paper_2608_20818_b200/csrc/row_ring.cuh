@@ -248,14 +248,14 @@ struct RowRing {
     }
   }
   // Reductions over the group, R rows with one barrier.  The words of set i and set i + 1 lie apart.
-  // SUMS: how many of p and q are sums (p first), the rest are largest magnitudes.
+  // SUMS: two sums, else one largest magnitude (q).
   static constexpr int kPiece = W >= 4 ? 4 : 2;
-  template <bool P, bool Q_SUM>
+  template <bool SUMS>
   __device__ __forceinline__ void reduce(int i, float (&p)[R], float (&q)[R]) const {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if constexpr (P) p[r] = warp_sum(p[r]);
-      q[r] = Q_SUM ? warp_sum(q[r]) : warp_top(q[r]);
+      if constexpr (SUMS) p[r] = warp_sum(p[r]);
+      q[r] = SUMS ? warp_sum(q[r]) : group_top(q[r]);
     }
     if constexpr (W > 1) {
       float(*red)[2][16] = b.red[group][i & 1];
@@ -263,24 +263,24 @@ struct RowRing {
       if ((threadIdx.x & 31) == 0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          if constexpr (P) red[r][0][warp] = p[r];
+          if constexpr (SUMS) red[r][0][warp] = p[r];
           red[r][1][warp] = q[r];
         }
       }
       sync();
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        if constexpr (P) p[r] = 0.f;
+        if constexpr (SUMS) p[r] = 0.f;
         q[r] = 0.f;
 #pragma unroll
         for (int k = 0; k < W; k += kPiece) {
           float u[kPiece], v[kPiece];
-          if constexpr (P) words(red[r][0] + k, u);
+          if constexpr (SUMS) words(red[r][0] + k, u);
           words(red[r][1] + k, v);
 #pragma unroll
           for (int e = 0; e < kPiece; e += 2) {
-            if constexpr (P) p[r] += u[e] + u[e + 1];
-            if constexpr (Q_SUM) q[r] += v[e] + v[e + 1];
+            if constexpr (SUMS) p[r] += u[e] + u[e + 1];
+            if constexpr (SUMS) q[r] += v[e] + v[e + 1];
             else q[r] = max_abs(q[r], make_float2(v[e], v[e + 1]));
           }
         }

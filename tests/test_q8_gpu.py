@@ -16,7 +16,9 @@ SHAPES = [(1, 1), (1, 8), (3, 5), (2, 256), (9, 257), (7, 512), (5, 1000), (3, 1
           (17, 3), (40, 249), (33, 505), (310, 1001), (19, 2041), (310, 4089), (11, 8185), (9, 16377), (9, 20001),
           (9, 16378), (300, 4100), (12, 12), (3, 24576), (2, 32768),
           # large enough to be streamed: each group width, full and partly filled, rows that do not divide
-          (8201, 512), (4700, 1000), (4099, 1024), (2050, 2056), (2100, 2048), (1030, 4096), (700, 6000), (519, 8192)]
+          (8201, 512), (4700, 1000), (4099, 1024), (2050, 2056), (2100, 2048), (1030, 4096), (700, 6000), (519, 8192),
+          # narrow rows, several to a warp: more than the grid takes in one turn; short rows by the block
+          (40003, 64), (20011, 128), (10001, 256), (37, 120), (2051, 1000)]
 
 
 def gen(seed):
