@@ -321,9 +321,12 @@ __device__ __forceinline__ float group_sum(float v) {
 template <int N = 32>
 __device__ __forceinline__ float group_top(float top) {
   uint32_t v = __float_as_uint(top);
-  if constexpr (N == 32) return __uint_as_float(__reduce_max_sync(0xffffffffu, v));
+  if constexpr (N == 32) {
+    v = __reduce_max_sync(0xffffffffu, v);
+  } else {
 #pragma unroll
-  for (int o = N / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int o = N / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  }
   return __uint_as_float(v);
 }
 // Sum and largest magnitude over a block of THREADS threads (up to 32: groups of lanes); every thread

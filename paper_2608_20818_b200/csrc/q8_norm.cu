@@ -9,10 +9,12 @@
 // Gradient, the rounding taken as the identity, with g = grad_y * w:
 //   grad_x = s g - h s^3 mean(g h) + grad_h,    grad_w = sum over rows of grad_y h s
 //
-// Both are bound by HBM (7 and 8 bytes per element of a bf16 stream with its residual).  Three
-// forms each: rows of octs (8 elements) held in registers, one row per block; for large matrices the
-// same arithmetic on rows streamed through shared memory; and single elements in two passes for rows
-// that are not aligned or longer than the registers of a block.
+// Both are bound by HBM (7 and 8 bytes per element of a bf16 stream with its residual), so a row is read
+// once and stays in registers, in octs (8 elements), between its sums and its output.  Measured on 8192
+// x 4096 in bf16 with residual: norm 38.2 us, 6.1 TB/s; gradient 52.7 us, 5.1 TB/s (it also waits for
+// the whole grid to add grad_w).  For one token each takes 2 to 5 us, the launch and one trip to memory.
+// Forms: rows of aligned octs; octs aligned in memory for rows that start anywhere; the gradient of rows
+// of 4097 to 8192 streamed through shared memory; and single elements in two passes for what is left.
 #include <cooperative_groups.h>
 
 #include "row_ring.cuh"
@@ -269,7 +271,12 @@ struct NormGradArgs {
 __host__ __device__ constexpr int grad_blocks(int threads, int nv = 1) {
   return threads <= 32 ? 8 : threads <= 128 ? 6 : threads <= 256 ? (nv == 1 ? 3 : 2) : 1;
 }
-constexpr int kNarrowBlocks = 4;          // per SM, of 256 threads
+// The same for the kernel below, of 256 threads: 64 registers per thread with one oct, 128 with two; twice that
+// where the elements are 32 bits wide.
+template <typename IO>
+__host__ __device__ constexpr int group_blocks(int nv) {
+  return (nv == 1 ? 4 : 2) * 2 / (int)sizeof(IO);
+}
 
 // Asks the L2 for the line of p (one lane in eight: 128 bytes of 16-byte pieces).
 __device__ __forceinline__ void prefetch_line(const void* p) {
@@ -351,63 +358,114 @@ __device__ __forceinline__ void grad_oct(const float2 (&gy)[4], const float2 (&h
   r.store(out);
 }
 
-// Narrow rows (the heads of a query-key norm): a group of TPR lanes to a row, 256 / TPR rows per block and
-// turn, the next turn's loads in flight; a block's groups add their shares of grad_w in shared memory.
-template <typename IO, typename WT, int TPR>
-__global__ void __launch_bounds__(256, kNarrowBlocks) rmsnorm_q8_grad_narrow_kernel(const NormGradArgs a) {
+// Two sums over a group of TPR threads; `red`: a word pair per warp, two sets in turn.
+template <int TPR>
+__device__ __forceinline__ void group_sum2(float& p, float& q, float2* red, int group) {
+  p = group_sum<(TPR < 32 ? TPR : 32)>(p);
+  q = group_sum<(TPR < 32 ? TPR : 32)>(q);
+  if constexpr (TPR > 32) {
+    if (threadIdx.x % 32 == 0) red[threadIdx.x % TPR / 32] = make_float2(p, q);
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
+    p = q = 0.f;
+#pragma unroll
+    for (int k = 0; k < TPR / 32; ++k) {
+      p += red[k].x;
+      q += red[k].y;
+    }
+  }
+}
+
+// Rows up to 4096: a group of TPR threads to a row, 256 / TPR rows per block and turn, the next turn's
+// loads in flight while this one is summed; a thread keeps the same columns in all its rows, so its share
+// of grad_w stays in registers, and a block's groups add theirs in shared memory.  One cooperative launch:
+// the blocks' shares are added behind a grid-wide barrier, which costs less than a second launch.  Heads
+// of a query-key norm, 262144 x 128: 47 us, 5.7 TB/s (a warp per row and block of 32: 191).
+template <typename IO, typename WT, int NV, int TPR>
+__global__ void __launch_bounds__(256, group_blocks<IO>(NV)) rmsnorm_q8_grad_kernel(const NormGradArgs a) {
   constexpr int kRows = 256 / TPR;
-  __shared__ __align__(16) float sums[kRows][TPR * 8];
+  __shared__ __align__(16) float sums[kRows][NV * TPR * 8];
+  __shared__ float2 red[2][TPR > 32 ? kRows : 1][TPR > 32 ? TPR / 32 : 1];
+  int turn = 0;
   grid_wait();
   grid_trigger();
   const int c0 = (threadIdx.x % TPR) * 8, group = threadIdx.x / TPR;
   const int64_t step = (int64_t)gridDim.x * kRows;
-  float2 gw[4], w[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) gw[e] = w[e] = make_float2(0.f, 0.f);
-  if (c0 < a.cols) load_oct(reinterpret_cast<const WT*>(a.weight) + c0, w);
-  Oct<IO> next[3];
+  float2 gw[NV][4];
+  Oct<WT> wv[NV];
+  Oct<IO> next[NV][3];
   auto fetch = [&](int64_t row) {
-    if (row < a.rows && c0 < a.cols) {
-      next[0].load_stream(reinterpret_cast<const IO*>(a.gy) + row * a.ld_gy + c0);
-      next[1].load_stream(reinterpret_cast<const IO*>(a.h) + row * a.ld_h + c0);
-      if (a.gh) next[2].load_stream(reinterpret_cast<const IO*>(a.gh) + row * a.ld_gh + c0);
-    } else {
-      next[0].zero();
-      next[1].zero();
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = c0 + v * TPR * 8;
+      next[v][0].zero();
+      next[v][1].zero();
+      if (row < a.rows && c < a.cols) {
+        next[v][0].load_stream(reinterpret_cast<const IO*>(a.gy) + row * a.ld_gy + c);
+        next[v][1].load_stream(reinterpret_cast<const IO*>(a.h) + row * a.ld_h + c);
+        if (a.gh) next[v][2].load_stream(reinterpret_cast<const IO*>(a.gh) + row * a.ld_gh + c);
+      }
     }
   };
   fetch((int64_t)blockIdx.x * kRows + group);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) gw[v][e] = make_float2(0.f, 0.f);
+    wv[v].zero();
+    if (c0 + v * TPR * 8 < a.cols) wv[v].load(reinterpret_cast<const WT*>(a.weight) + c0 + v * TPR * 8);
+  }
   for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += step) {
     const int64_t row = base + group;
-    Oct<IO> add = next[2];
-    float2 gy[4], h[4], ss2 = make_float2(0.f, 0.f), gh2 = ss2;
-    next[0].get(gy);
-    next[1].get(h);
+    Oct<IO> now[NV][3];
+    float2 ss2 = make_float2(0.f, 0.f), gh2 = ss2;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) now[v][k] = next[v][k];
     fetch(row + step);
-    grad_sums(gy, h, w, ss2, gh2);
-    const float ss = group_sum<TPR>(ss2.x + ss2.y), gh = group_sum<TPR>(gh2.x + gh2.y);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float2 gy[4], h[4], w[4];
+      now[v][0].get(gy);
+      now[v][1].get(h);
+      wv[v].get(w);
+      grad_sums(gy, h, w, ss2, gh2);
+    }
+    float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
+    group_sum2<TPR>(ss, gh, red[turn][TPR > 32 ? group : 0], group);
+    turn ^= 1;
     const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
-    if (row < a.rows && c0 < a.cols)
-      grad_oct<IO>(gy, h, w, a.gh ? &add : nullptr, s, k, reinterpret_cast<IO*>(a.gx) + row * a.ld_gx + c0, gw);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = c0 + v * TPR * 8;
+      if (row < a.rows && c < a.cols) {
+        float2 gy[4], h[4], w[4];
+        now[v][0].get(gy);
+        now[v][1].get(h);
+        wv[v].get(w);
+        grad_oct<IO>(gy, h, w, a.gh ? &now[v][2] : nullptr, s, k, reinterpret_cast<IO*>(a.gx) + row * a.ld_gx + c, gw[v]);
+      }
+    }
   }
-  Oct<float> o;
-  o.set(gw);
-  o.store(&sums[group][c0]);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    Oct<float> o;
+    o.set(gw[v]);
+    o.store(&sums[group][c0 + v * TPR * 8]);
+  }
   __syncthreads();
-  if ((int)threadIdx.x < a.cols && (int64_t)blockIdx.x * kRows < a.rows) {
+  for (int c = threadIdx.x; c < a.cols && (int64_t)blockIdx.x * kRows < a.rows; c += 256) {
     float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < kRows; ++g) sum += sums[g][threadIdx.x];
-    a.part[(int64_t)blockIdx.x * a.cols + threadIdx.x] = sum;
+    for (int g = 0; g < kRows; ++g) sum += sums[g][c];
+    a.part[(int64_t)blockIdx.x * a.cols + c] = sum;
   }
   grad_weight<256>(a, kRows);
 }
 
-// A block walks over rows; a thread keeps the same columns in all of them, so its share of grad_w
-// stays in registers until the block's last row.  One cooperative launch: the blocks' shares are added
-// behind a grid-wide barrier, which costs less than a second launch.
+// Few rows of 4097 to 8192: as above with a block per row, the next row asked into the L2.
 template <typename IO, typename WT, int NV, int TPR>
-__global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_kernel(const NormGradArgs a) {
+__global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_wide_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
   grid_wait();
   grid_trigger();
@@ -713,31 +771,29 @@ int launch_grad(void (*kernel)(NormGradArgs), const NormGradArgs& a, int threads
   return launch_grad_blocks(kernel, a, threads, std::min<int64_t>(want, grad_blocks(threads, nv) * kRingBlocks / 8 * 8),
                             stream);
 }
-template <typename IO, typename WT, int TPR>
-int launch_grad_narrow(const NormGradArgs& a, cudaStream_t stream) {
+template <typename IO, typename WT, int NV, int TPR>
+int launch_grad_groups(const NormGradArgs& a, cudaStream_t stream) {
   constexpr int kRows = 256 / TPR;
-  return launch_grad_blocks(rmsnorm_q8_grad_narrow_kernel<IO, WT, TPR>, a, 256,
-                            std::min<int64_t>((a.rows + kRows - 1) / kRows, kNarrowBlocks * kRingBlocks), stream);
+  return launch_grad_blocks(rmsnorm_q8_grad_kernel<IO, WT, NV, TPR>, a, 256,
+                            std::min<int64_t>((a.rows + kRows - 1) / kRows, group_blocks<IO>(NV) * kRingBlocks), stream);
 }
 
 template <typename IO, typename WT>
 int run_grad(const NormGradArgs& a, cudaStream_t stream) {
   const int c = a.cols;
-  if (c <= 64) return launch_grad_narrow<IO, WT, 8>(a, stream);
-  if (c <= 128) return launch_grad_narrow<IO, WT, 16>(a, stream);
-  if (c <= 256) return launch_grad_narrow<IO, WT, 32>(a, stream);
-  // Streamed from these sizes on, in fewer blocks that last longer (1024 x 1024: 8.6 us against 12.3; 1024 x
-  // 4096: 11.9 against 15.0), else a row or two per block (256 x 4096: 7.1 us against 10.1; 512 x 512: 6.3
-  // against 9.0).
-  if (c <= 8192 && (a.rows >= 768 || a.rows * c >= (int64_t)1 << 21))
-    return with_ring_warps<2>(c, [&](auto w) {
-      return a.gh ? launch_grad_stream<IO, WT, decltype(w)::value, true>(a, stream)
-                  : launch_grad_stream<IO, WT, decltype(w)::value, false>(a, stream);
-    });
-  if (c <= 1024) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 128>, a, 128, 1, stream);
-  if (c <= 2048) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 256>, a, 256, 1, stream);
-  if (c <= 4096) return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 1, 512>, a, 512, 1, stream);
-  return launch_grad(rmsnorm_q8_grad_kernel<IO, WT, 2, 512>, a, 512, 2, stream);
+  if (c <= 64) return launch_grad_groups<IO, WT, 1, 8>(a, stream);
+  if (c <= 128) return launch_grad_groups<IO, WT, 1, 16>(a, stream);
+  if (c <= 256) return launch_grad_groups<IO, WT, 1, 32>(a, stream);
+  if (c <= 512) return launch_grad_groups<IO, WT, 2, 32>(a, stream);
+  if (c <= 1024) return launch_grad_groups<IO, WT, 2, 64>(a, stream);
+  if (c <= 2048) return launch_grad_groups<IO, WT, 2, 128>(a, stream);
+  if (c <= 4096) return launch_grad_groups<IO, WT, 2, 256>(a, stream);
+  // Streamed from these sizes on (8192 x 5120: 70 us, by groups of 512 threads 75, in fp32 111 and 238), else
+  // a row or two per block (100 x 8192: 10.3 us).  Up to 4096 columns the ring is no faster than groups
+  // (8192 x 4096: 49.0 us against 49.6) or slower (2048 x 2048: 13.3 against 10.4).
+  if (a.rows * c < (int64_t)1 << 21) return launch_grad(rmsnorm_q8_grad_wide_kernel<IO, WT, 2, 512>, a, 512, 2, stream);
+  return a.gh ? launch_grad_stream<IO, WT, kRingWarps, true>(a, stream)
+              : launch_grad_stream<IO, WT, kRingWarps, false>(a, stream);
 }
 
 // `alike`: the matrices' rows start alike.
