@@ -15,6 +15,7 @@
 #include <cooperative_groups.h>
 
 #include "row_ring.cuh"
+#include "tcgen05.cuh"
 
 namespace prm {
 namespace {
@@ -220,6 +221,118 @@ __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], con
         *reinterpret_cast<uint2*>(q + c) = column_codes<FORMAT>(t, m);
       }
     }
+  }
+}
+
+// Codes by column: a cluster of up to eight blocks to a panel of LANES octs of columns, so that a column's
+// scale waits for these and not for the grid.  A thread has one oct of one row in (blocks * kRowLanes); the
+// rows of its last turn stay in its registers, those before them it finds in the L2.
+constexpr int kPanelThreads = 256, kPanelCluster = 8, kPanelRows = 8;
+template <typename IO, int LANES>
+__global__ void __launch_bounds__(kPanelThreads) quantize_panel_kernel(const QuantArgs a) {
+  constexpr int kRowLanes = kPanelThreads / LANES, kWidth = LANES * 8, kWarps = kPanelThreads / 32;
+  static_assert(LANES <= 32 && kWidth <= kPanelThreads, "a warp holds whole rows of the panel, a thread has one column");
+  __shared__ __align__(16) uint32_t own[kWarps][kWidth], all[kPanelCluster][kWidth];
+  __shared__ __align__(16) float factor[kWidth];
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  grid_wait();
+  grid_trigger();
+  const uint32_t rank = cluster_ctarank(), blocks = cluster_nctarank();
+  const int cbase = (int)(blockIdx.x / blocks) * kWidth, lane = threadIdx.x % LANES;
+  const int cols = a.cols - cbase < lane * 8 ? 0 : a.cols - cbase - lane * 8;   // from this thread's oct on
+  const int64_t first = (int64_t)rank * kRowLanes + threadIdx.x / LANES, step = blocks * kRowLanes;
+  const IO* x = reinterpret_cast<const IO*>(a.x) + cbase + lane * 8;
+  uint8_t* q = a.q_cols + cbase + lane * 8;
+  const int64_t turns = (a.rows + step * kPanelRows - 1) / (step * kPanelRows);
+  Oct<IO> v[kPanelRows];
+  float f[kPanelRows];
+  auto fetch = [&](int64_t turn) {
+#pragma unroll
+    for (int k = 0; k < kPanelRows; ++k) {
+      const int64_t r = first + (turn * kPanelRows + k) * step;
+      v[k].zero();
+      f[k] = 1.f;
+      if (r < a.rows && cols > 0) {
+        v[k].load(x + r * a.ld_x);
+        if (a.fold_rows) f[k] = __ldg(a.fold_rows + r);
+      }
+    }
+  };
+  float top[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top[e] = 0.f;
+  for (int64_t turn = 0; turn < turns; ++turn) {
+    fetch(turn);
+#pragma unroll
+    for (int k = 0; k < kPanelRows; k += 2) {
+      float2 t[4], u[4];
+      v[k].get(t);
+      v[k + 1].get(u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        t[e] = mul2(t[e], make_float2(f[k], f[k]));
+        u[e] = mul2(u[e], make_float2(f[k + 1], f[k + 1]));
+        top[2 * e] = max_abs(top[2 * e], make_float2(t[e].x, u[e].x));
+        top[2 * e + 1] = max_abs(top[2 * e + 1], make_float2(t[e].y, u[e].y));
+      }
+    }
+  }
+  // Joined as bit patterns (NaN above infinity above numbers): over the warp's rows, the block's warps, the
+  // cluster's blocks.
+  uint32_t bits[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    bits[e] = __float_as_uint(top[e]);
+#pragma unroll
+    for (int o = LANES; o < 32; o *= 2) bits[e] = max(bits[e], __shfl_xor_sync(0xffffffffu, bits[e], o));
+  }
+  if (threadIdx.x % 32 < LANES) {
+    uint4* to = reinterpret_cast<uint4*>(&own[threadIdx.x / 32][lane * 8]);
+    to[0] = make_uint4(bits[0], bits[1], bits[2], bits[3]);
+    to[1] = make_uint4(bits[4], bits[5], bits[6], bits[7]);
+  }
+  __syncthreads();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // all blocks of the cluster are there
+  if (threadIdx.x < kWidth) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) most = max(most, own[w][threadIdx.x]);
+    const uint32_t mine = smem_u32(&all[rank][threadIdx.x]);
+#pragma unroll
+    for (uint32_t r = 0; r < kPanelCluster; ++r)
+      if (r < blocks) st_cluster_u32(cluster_map(mine, r), most);
+  }
+  cluster_barrier();
+  bool odd = false;
+  if (threadIdx.x < kWidth) {
+    uint32_t most = 0;
+#pragma unroll
+    for (uint32_t r = 0; r < kPanelCluster; ++r)
+      if (r < blocks) most = max(most, all[r][threadIdx.x]);
+    const float t = __uint_as_float(most), limit = q8_limit(a.format);
+    odd = !q8_finite(t);
+    factor[threadIdx.x] = odd ? __uint_as_float(0x7fffffffu) : q8_mul(t, limit);
+    if (rank == 0 && cbase + (int)threadIdx.x < a.cols) a.scale_cols[cbase + threadIdx.x] = q8_scale(t, limit);
+  }
+  odd = __syncthreads_or(odd);
+  float2 mul[1][4];
+  {
+    Oct<float> o;
+    o.load(factor + lane * 8);
+    o.get(mul[0]);
+  }
+  for (int64_t turn = turns - 1;; --turn) {
+#pragma unroll
+    for (int k = 0; k < kPanelRows; ++k) {
+      const int64_t r = first + (turn * kPanelRows + k) * step;
+      if (r < a.rows) {
+        const Oct<IO> one[1] = {v[k]};
+        if (a.format == PRM_Q8_INT8) back_row<IO, 1, PRM_Q8_INT8>(q + r * a.ld_qc, one, mul, f[k], odd, 0, 0, cols);
+        else back_row<IO, 1, PRM_Q8_E4M3>(q + r * a.ld_qc, one, mul, f[k], odd, 0, 0, cols);
+      }
+    }
+    if (turn == 0) break;
+    fetch(turn - 1);
   }
 }
 
@@ -477,6 +590,20 @@ int run_stream(QuantArgs a, cudaStream_t stream) {
       a.panel, [&](auto w) { return launch_stream<IO, decltype(w)::value, 2, kRingRows<IO>, ROWS>(a, stream); });
 }
 
+template <typename IO, int LANES>
+void launch_panels(const QuantArgs& a, cudaStream_t stream) {
+  // as many blocks as there are turns' worth of rows
+  unsigned blocks = 1;
+  while (blocks < kPanelCluster && a.rows > (int64_t)blocks * kPanelRows * (kPanelThreads / LANES)) blocks *= 2;
+  launch_after(quantize_panel_kernel<IO, LANES>, (unsigned)((a.cols + LANES * 8 - 1) / (LANES * 8)) * blocks,
+               kPanelThreads, 0, stream, blocks, a);
+}
+template <typename IO>
+void run_panels(const QuantArgs& a, cudaStream_t stream) {
+  if (a.cols <= 2048 && a.rows >= 1024) launch_panels<IO, 8>(a, stream);
+  else launch_panels<IO, 16>(a, stream);
+}
+
 template <typename IO, int NV, int TPR>
 void launch_rows(const QuantArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR <= 32 ? 256 / TPR : 1;
@@ -575,13 +702,21 @@ extern "C" int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_
   const bool octs_c = octs_x && ld_q_cols % 8 == 0 && ((uintptr_t)q_cols & 7) == 0;
   // Codes by column of an aligned matrix: one launch, with the codes by row in the same pass where a
   // row fits a group's registers.
-  if (q_cols && octs_c && cols >= 256 && cols <= 32 * 8192) {
+  // Up to these sizes by panels (1500 x 2048 both ways with folds: 10.0 us, streamed 14.4; 4096 x 4096 columns:
+  // 16.3 against 19.8), beyond them streamed (8192 x 8192: 57.4 against 64.5; 32768 x 512: 27.5 against 42.5).
+  const bool panels = q_cols && octs_c && rows <= (cols < 256 ? 2048 : 8192) && rows * cols <= (int64_t)1 << 24;
+  if (!panels && q_cols && octs_c && cols >= 256 && cols <= 32 * 8192) {
     const bool joint = q_rows && octs_r && cols <= (io_fp32 ? kWidest<float> : kWidest<__nv_bfloat16>);
     int code;
     if (joint) code = io_fp32 ? run_stream<float, true>(a, stream) : run_stream<__nv_bfloat16, true>(a, stream);
     else code = io_fp32 ? run_stream<float, false>(a, stream) : run_stream<__nv_bfloat16, false>(a, stream);
     if (code != PRM_OK) return code;
     if (joint) q_rows = nullptr;
+    q_cols = nullptr;
+  }
+  if (panels) {
+    if (io_fp32) run_panels<float>(a, stream);
+    else run_panels<__nv_bfloat16>(a, stream);
     q_cols = nullptr;
   }
   if (q_rows) {
