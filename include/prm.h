@@ -452,8 +452,8 @@ PRM_API double prm_shape_scale(int mode, int64_t rows, int64_t cols);
  * A quantised matrix is a row-major matrix of 8-bit codes plus one fp32 scale per row or per
  * column; it stands for code * scale.  Formats: PRM_Q8_INT8 (codes -127..127) and PRM_Q8_E4M3
  * (8-bit floats, +-448).  The largest magnitude T that shares a scale maps to the limit (127 or
- * 448): code = round-to-nearest-even(value * (limit * (1 / T))), scale = T / limit, each step in
- * fp32.  T below 2^-100 counts as zero (codes and scale 0); a row (column) that holds an infinity or
+ * 448): code = round-to-nearest-even(value * (limit * (1 / T))), scale = T / limit, each step
+ * rounded to fp32.  T below 2^-100 counts as zero (codes and scale 0); a row (column) that holds an infinity or
  * a NaN gets the scale NaN and zero codes, and no other row is touched by it.
  *
  * Weights are stored in x out (rows x cols as everywhere in this library: y = x W).  A training

@@ -23,8 +23,8 @@ __host__ __device__ inline bool q8_format_ok(int format) { return format == PRM_
 __host__ __device__ inline float q8_limit(int format) { return format == PRM_Q8_INT8 ? kLimitInt8 : kLimitE4m3; }
 
 // A set of values with the largest magnitude `top` is multiplied by q8_mul and marked with q8_scale,
-// which undoes it.  The factor is limit * (1 / top), each step rounded, which is how array libraries
-// evaluate a number over an array, so that codes agree with `round(t * (limit / top))` written there.
+// which undoes it.  The factor is limit * (1 / top) and a code the rounded product, each step rounded to
+// fp32, which is how array libraries evaluate `round(t * (limit / top))` with a number over an array.
 // A set that holds an infinity or a NaN (which maxima here keep) gets the scale NaN and zero codes: it
 // marks its own row (column) of whatever is computed from it and no other.
 __device__ __forceinline__ bool q8_finite(float top) { return top < __uint_as_float(0x7f800000u); }
@@ -120,15 +120,21 @@ template <> struct Oct<float> {
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
 };
 
+// The int8 codes of t * mul in the low bytes: |t * mul| <= 127, and adding 1.5 * 2^23 leaves it rounded to
+// nearest-even there.  The product has to be rounded before: in one fused step 1 in 2,700 bf16 values, next
+// to a tie, gets another code than by the rule above.  A product and a sum of pairs come out of the
+// assembler as one fused step, explicit rounding or not, so the product is itself a fused step, with a -0
+// from constant memory, which the assembler does not take for a known number.
+static __constant__ float2 kMinusZero = {-0.f, -0.f};
+__device__ __forceinline__ float2 int8_bits(float2 t, float2 mul) {
+  return add2(fma2(t, mul, kMinusZero), make_float2(12582912.f, 12582912.f));
+}
 // Four codes of t * mul (first value in the lowest byte).
 template <int FORMAT>
 __device__ __forceinline__ uint32_t codes4(float2 a, float2 b, float2 mul) {
   if constexpr (FORMAT == PRM_Q8_INT8) {
-    // |t * mul| <= 127: adding 1.5 * 2^23 leaves it rounded to nearest-even in the low bits, and as one
-    // fused product it is rounded once.
-    const float2 m = make_float2(12582912.f, 12582912.f);
-    a = fma2(a, mul, m);
-    b = fma2(b, mul, m);
+    a = int8_bits(a, mul);
+    b = int8_bits(b, mul);
     return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
                        __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
   } else {

@@ -168,8 +168,7 @@ __device__ __forceinline__ uint2 column_codes(const float2 (&t)[4], const float2
   for (int k = 0; k < 2; ++k) {
     const float2 a = t[2 * k], b = t[2 * k + 1], f = mul[2 * k], g = mul[2 * k + 1];
     if constexpr (FORMAT == PRM_Q8_INT8) {
-      const float2 m = make_float2(12582912.f, 12582912.f);
-      const float2 x = fma2(a, f, m), y = fma2(b, g, m);
+      const float2 x = int8_bits(a, f), y = int8_bits(b, g);
       w[k] = __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040),
                          __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
     } else {

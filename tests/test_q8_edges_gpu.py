@@ -1,0 +1,38 @@
+"""Edges of the 8-bit operators: the documented rounding bit by bit, sizes and values at the ends of their ranges."""
+
+import pytest
+import torch
+
+import q8_reference as R
+from paper_2608_20818_b200 import binding as B
+
+EPS = 1e-6
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+def codes_by_the_rule(t, dim, fmt):
+    """round(t * (limit * (1 / T))) with each step rounded to fp32, on the host."""
+    t = t.cpu()
+    v = t * (R.LIMIT[fmt] * (1.0 / t.abs().amax(dim, keepdim=True)))
+    return (v.round() if fmt == "int8" else v).to(R.EIGHT[fmt]).float()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("io", [torch.bfloat16, torch.float32])
+# rows in registers, rows that start anywhere, single elements; columns by panels, streamed (one and two rows
+# per set), and single elements
+@pytest.mark.parametrize("rows,cols", [(700, 256), (90, 2048), (160, 1111), (5, 40001), (900, 515), (4200, 4096),
+                                       (8300, 512), (2100, 9000)])
+def test_codes_follow_the_rule_bit_by_bit(rows, cols, io, fmt):
+    x = randn(rows + cols, rows, cols).to(io)
+    w = (1 + 0.2 * randn(cols, cols)).to(io)
+    fr, fc = torch.exp(randn(rows, rows)), torch.exp(randn(cols + 1, cols))
+    q, _, _ = B.prm_rmsnorm_q8(x, w, EPS, format=fmt)
+    assert torch.equal(q.float().cpu(), codes_by_the_rule(x.float() * w.float(), 1, fmt))
+    qr, _, qc, _ = B.prm_quantize_q8(x, by_cols=True, fold_rows=fr, fold_cols=fc, format=fmt)
+    assert torch.equal(qr.float().cpu(), codes_by_the_rule(x.float() * fc, 1, fmt))
+    assert torch.equal(qc.float().cpu(), codes_by_the_rule(x.float() * fr[:, None], 0, fmt))
