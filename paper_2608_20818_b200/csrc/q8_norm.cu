@@ -266,13 +266,8 @@ struct NormGradArgs {
   float eps;
 };
 
-// Blocks of `threads` threads that an SM holds in the gradient's kernels without a ring: 768 threads at 80
-// registers with one oct per thread, 512 at 128 with more.
-__host__ __device__ constexpr int grad_blocks(int threads, int nv = 1) {
-  return threads <= 32 ? 8 : threads <= 128 ? 6 : threads <= 256 ? (nv == 1 ? 3 : 2) : 1;
-}
-// The same for the kernel below, of 256 threads: 64 registers per thread with one oct, 128 with two; twice that
-// where the elements are 32 bits wide.
+// Blocks per SM of the kernel below, of 256 threads: 64 registers per thread with one oct, 128 with two; twice
+// that where the elements are 32 bits wide.
 template <typename IO>
 __host__ __device__ constexpr int group_blocks(int nv) {
   return (nv == 1 ? 4 : 2) * 2 / (int)sizeof(IO);
@@ -632,7 +627,8 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
 }
 
 // Rows that start anywhere, or too wide for the kernels above.  The grid is a multiple of eight blocks
-// (or has one row per block), so that all rows of a block start alike and a thread keeps its columns.
+// (or has one row per block: grad_shifted_grid), so that all rows of a block start alike and a thread keeps
+// its columns.
 template <typename IO, int NV, int TPR>
 __global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_shifted_kernel(const NormGradArgs a) {
   __shared__ float red[2][64];
@@ -742,11 +738,6 @@ __global__ void __launch_bounds__(THREADS, grad_blocks(THREADS)) rmsnorm_q8_grad
   grad_weight<THREADS>(a);
 }
 
-// Lines of partial sums: what the launches below come to at most.
-int grad_parts(int64_t rows, int64_t cols) {
-  return (int)std::min<int64_t>(rows, kRingBlocks * (cols <= 256 ? 8 : cols <= 1024 ? 6 : cols <= 6144 ? 3 : 1));
-}
-
 template <typename IO, typename WT, int W, bool GH>
 int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
   constexpr int kGroups = kRingWarps / W, kR = kRingRows<IO>;
@@ -755,27 +746,21 @@ int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
                      (size_t)a.cols * sizeof(IO) * (GH ? 3 : 2) * kR * kGroups, 0, (size_t)kGroups * a.cols * 4, true,
                      stream, a);
 }
-// At least as many blocks as share the columns of grad_w at the end (1 x 4096, one block: 56 us).
-int launch_grad_blocks(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int64_t blocks, cudaStream_t stream) {
+int launch_grad_grid(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int64_t grid, cudaStream_t stream) {
   void* args[1] = {&a};
-  const unsigned grid = (unsigned)std::max<int64_t>(blocks, std::min(kRingBlocks, (a.cols + 31) / 32));
-  return cudaLaunchCooperativeKernel((const void*)kernel, dim3(grid), dim3((unsigned)threads), args, 0, stream) ==
-                 cudaSuccess
+  return cudaLaunchCooperativeKernel((const void*)kernel, dim3((unsigned)grid), dim3((unsigned)threads), args, 0,
+                                     stream) == cudaSuccess
              ? PRM_OK
              : PRM_ERR_CUDA;
 }
-// Two blocks per SM until they have six rows each: a block more is a line more of partial sums (512 x
-// 2048: 7.5 us, three per SM 9.4; 5000 x 1001: 23 us, two per SM 31).
 int launch_grad(void (*kernel)(NormGradArgs), const NormGradArgs& a, int threads, int nv, cudaStream_t stream) {
-  const int64_t want = std::min<int64_t>(a.rows, std::max<int64_t>(2 * kRingBlocks, (a.rows + 47) / 48 * 8));
-  return launch_grad_blocks(kernel, a, threads, std::min<int64_t>(want, grad_blocks(threads, nv) * kRingBlocks / 8 * 8),
-                            stream);
+  return launch_grad_grid(kernel, a, threads, grad_grid(a.rows, a.cols, grad_blocks(threads, nv)), stream);
 }
 template <typename IO, typename WT, int NV, int TPR>
 int launch_grad_groups(const NormGradArgs& a, cudaStream_t stream) {
   constexpr int kRows = 256 / TPR;
-  return launch_grad_blocks(rmsnorm_q8_grad_kernel<IO, WT, NV, TPR>, a, 256,
-                            std::min<int64_t>((a.rows + kRows - 1) / kRows, group_blocks<IO>(NV) * kRingBlocks), stream);
+  const int64_t blocks = std::min<int64_t>((a.rows + kRows - 1) / kRows, group_blocks<IO>(NV) * kRingBlocks);
+  return launch_grad_grid(rmsnorm_q8_grad_kernel<IO, WT, NV, TPR>, a, 256, grad_grid_for_columns(blocks, a.cols), stream);
 }
 
 template <typename IO, typename WT>
@@ -799,15 +784,19 @@ int run_grad(const NormGradArgs& a, cudaStream_t stream) {
 // `alike`: the matrices' rows start alike.
 template <typename IO>
 int run_grad_single(const NormGradArgs& a, bool alike, cudaStream_t stream) {
-  const int c = a.cols + 7;
-  if (alike && c <= 16384) {
-    if (c <= 256) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 1, 32>, a, 32, 1, stream);
-    if (c <= 1024) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 1, 128>, a, 128, 1, stream);
-    if (c <= 2048) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 1, 256>, a, 256, 1, stream);
-    if (c <= 4096) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 2, 256>, a, 256, 2, stream);
-    if (c <= 6144) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 3, 256>, a, 256, 3, stream);
-    if (c <= 8192) return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 2, 512>, a, 512, 2, stream);
-    return launch_grad(rmsnorm_q8_grad_shifted_kernel<IO, 2, 1024>, a, 1024, 2, stream);
+  const GradForm form = alike ? grad_shifted_form(a.cols) : GradForm{0, 0};
+  auto go = [&](auto kernel) {
+    return launch_grad_grid(kernel, a, form.threads, grad_shifted_grid(a.rows, a.cols, form), stream);
+  };
+  switch (form.threads) {
+    case 32: return go(rmsnorm_q8_grad_shifted_kernel<IO, 1, 32>);
+    case 128: return go(rmsnorm_q8_grad_shifted_kernel<IO, 1, 128>);
+    case 256:
+      return form.nv == 1   ? go(rmsnorm_q8_grad_shifted_kernel<IO, 1, 256>)
+             : form.nv == 2 ? go(rmsnorm_q8_grad_shifted_kernel<IO, 2, 256>)
+                            : go(rmsnorm_q8_grad_shifted_kernel<IO, 3, 256>);
+    case 512: return go(rmsnorm_q8_grad_shifted_kernel<IO, 2, 512>);
+    case 1024: return go(rmsnorm_q8_grad_shifted_kernel<IO, 2, 1024>);
   }
   if (a.cols <= 1024) return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 128>, a, 128, 1, stream);
   return launch_grad(rmsnorm_q8_grad_single_kernel<IO, 1024>, a, 1024, 1, stream);

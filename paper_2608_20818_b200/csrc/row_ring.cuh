@@ -20,6 +20,7 @@
 
 #include "async_copy.cuh"
 #include "q8.cuh"
+#include "q8_plan.h"
 
 namespace prm {
 
@@ -27,7 +28,6 @@ constexpr int kRingStages = 6;
 constexpr size_t kRingBytes = 200 * 1024;
 constexpr int kRingWarps = 16;                        // that work on rows
 constexpr int kRingThreads = kRingWarps * 32 + 32;    // and the producer
-constexpr int kRingBlocks = 148;                      // one CTA per SM
 
 // Rows per set of the kernels that take two: one where the elements are 32 bits wide, for the registers.
 template <typename IO>

@@ -36,3 +36,24 @@ def test_codes_follow_the_rule_bit_by_bit(rows, cols, io, fmt):
     qr, _, qc, _ = B.prm_quantize_q8(x, by_cols=True, fold_rows=fr, fold_cols=fc, format=fmt)
     assert torch.equal(qr.float().cpu(), codes_by_the_rule(x.float() * fc, 1, fmt))
     assert torch.equal(qc.float().cpu(), codes_by_the_rule(x.float() * fr[:, None], 0, fmt))
+
+
+def check_norm_backward(gy, h, w, eps, gh):
+    gx, gw = B.prm_rmsnorm_q8_backward(gy, h, w, eps, grad_h=gh)
+    rx, rw, sx, sw = R.norm_backward(gy, h, w, eps, gh)
+    # every term goes through the two row sums and a handful of products, 100 roundings at most; grad_w is added
+    # over the rows in turn at worst
+    for got, ref, size, rounds in ((gx, rx, sx, 100), (gw, rw, sw, 100 + len(h))):
+        store = R.BF16 if got.dtype == torch.bfloat16 else R.F32
+        assert torch.all((got.double() - ref).abs() <= rounds * R.F32 * size + 1.01 * store * ref.abs())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [torch.bfloat16, torch.float32])
+# wide rows of odd widths, more of them than blocks
+@pytest.mark.parametrize("rows,cols", [(149, 6139), (310, 8185), (160, 8187), (300, 9001), (160, 16377), (1500, 6141)])
+def test_norm_backward_of_many_wide_odd_rows(rows, cols, io):
+    h, gy, gh = (randn(rows + cols + k, rows, cols).to(io) for k in range(3))
+    w = (1 + 0.2 * randn(cols, cols)).to(io)
+    check_norm_backward(gy, h, w, EPS, gh)
+    check_norm_backward(gy, h, w, EPS, None)
