@@ -684,8 +684,8 @@ extern "C" int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_
     return PRM_ERR_SHAPE;
   if ((q_rows && !scale_rows) || (q_cols && !scale_cols)) return PRM_ERR_ARG;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if (((uintptr_t)scale_rows | (uintptr_t)scale_cols | (uintptr_t)fold_rows | (uintptr_t)fold_cols |
-       (uintptr_t)scratch) % 4 != 0)
+  if (((uintptr_t)scale_rows | (uintptr_t)scale_cols | (uintptr_t)fold_rows | (uintptr_t)fold_cols) % 4 != 0 ||
+      (q_cols && !aligned16(scratch)))
     return PRM_ERR_ALIGN;
   if (rows == 0) {                        // columns without an element: scale 0
     if (q_cols && cudaMemsetAsync(scale_cols, 0, (size_t)cols * 4, stream) != cudaSuccess) return PRM_ERR_CUDA;
