@@ -14,7 +14,8 @@ A step of training is
 What a layer keeps for its backward pass is one byte per element of its input.  Both products of the
 backward pass run on 8-bit operands: the scales that run along a product's sum are folded into the
 gradient before it is quantised, by row for dx = g W^T and by column for dW = x^T g.  The rounding to
-8 bits is taken as the identity by the gradients (straight-through).
+8 bits is taken as the identity by the gradients (straight-through).  The gradients have no derivatives of
+their own: a backward pass with create_graph=True is refused.
 """
 
 from __future__ import annotations
@@ -38,6 +39,13 @@ class Weight8:
                                                        format=self.format)
 
 
+def _refuse_second_derivative():
+    # Gradient mode is on in a backward pass whose own graph is wanted.  A node that raises only when it is
+    # differentiated would be passed by: the gradient's dependence on x and W runs through codes, not the graph.
+    if torch.is_grad_enabled():
+        raise RuntimeError("the 8-bit layers have no second derivatives: run backward without create_graph")
+
+
 def _backward_products(grad_out, x8, sx, codes, scale, format, x_dtype, w_dtype, need_x, need_w):
     """(dx, dW) of y = (x8 * sx) @ (codes * scale), None for what is not needed."""
     gr, sr, gc, sc = prm_quantize_q8(grad_out, by_rows=need_x, by_cols=need_w, fold_rows=sx if need_w else None,
@@ -57,6 +65,7 @@ class _Linear(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_out):
+        _refuse_second_derivative()
         x8, sx, codes, scale = ctx.saved_tensors
         need = ctx.needs_input_grad
         if not (need[0] or need[1]):
@@ -77,6 +86,7 @@ class _NormLinear(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_out, grad_h=None):
+        _refuse_second_derivative()
         x8, sx, codes, scale, h, norm_weight = ctx.saved_tensors
         need = ctx.needs_input_grad
         if grad_out is None:                # only the stream goes on

@@ -5,6 +5,7 @@ import torch
 
 import q8_reference as R
 from paper_2608_20818_b200 import binding as B
+from paper_2608_20818_b200 import q8 as Q
 
 EPS = 1e-6
 
@@ -57,3 +58,22 @@ def test_norm_backward_of_many_wide_odd_rows(rows, cols, io):
     w = (1 + 0.2 * randn(cols, cols)).to(io)
     check_norm_backward(gy, h, w, EPS, gh)
     check_norm_backward(gy, h, w, EPS, None)
+
+
+@pytest.mark.gpu
+def test_second_derivatives_are_refused():
+    """Other paths (the residual stream, a term of the weight) keep the graph of a second derivative alive beside
+    the layers: their terms must not drop out of it silently."""
+    x, r = (randn(k, 6, 64).requires_grad_() for k in (1, 2))
+    n = torch.ones(64, device="cuda", requires_grad=True)
+    W = randn(3, 64, 32).requires_grad_()
+    w8 = Q.Weight8(W)
+    for f in (lambda: Q.norm_linear(x, r, n, w8)[0].square().sum() + x.pow(3).sum(),
+              lambda: Q.norm_linear(x, None, n, w8)[0].sum() + x.pow(3).sum(),
+              lambda: Q.linear(x, w8).square().sum() + x.pow(3).sum(),
+              lambda: Q.linear(x, w8).sum() + W.pow(3).sum() + x.pow(3).sum()):
+        first = torch.autograd.grad(f(), [x, W], allow_unused=True)
+        assert all(g is not None for g in first)
+        with pytest.raises(RuntimeError):
+            gx, gw = torch.autograd.grad(f(), [x, W], create_graph=True)
+            torch.autograd.grad(gx.square().sum() + gw.square().sum(), x)
