@@ -101,10 +101,14 @@ class _NormLinear(torch.autograd.Function):
         return (dx if need[0] else None, dx if need[1] else None, dn if need[2] else None, dw, None, None)
 
 
+def _as_given(y, x):
+    return y.reshape(*x.shape[:-1], y.shape[-1])
+
+
 def linear(x, w8):
-    """x @ W in 8 bits: x (..., in) bf16 or fp32, quantised by row; w8 a Weight8.  Returns (..., out) in
+    """x @ W in 8 bits: x (..., in), one vector too, bf16 or fp32, quantised by row; w8 a Weight8.  Returns (..., out) in
     x's type."""
-    return _Linear.apply(x.reshape(-1, x.shape[-1]), w8.weight, w8).unflatten(0, x.shape[:-1])
+    return _as_given(_Linear.apply(x.reshape(-1, x.shape[-1]), w8.weight, w8), x)
 
 
 def norm_linear(x, residual, norm_weight, w8, eps=1e-6):
@@ -113,8 +117,8 @@ def norm_linear(x, residual, norm_weight, w8, eps=1e-6):
     flat = x.reshape(-1, x.shape[-1])
     if residual is None:
         y = _NormLinear.apply(flat, None, norm_weight, w8.weight, w8, eps)
-        return y.unflatten(0, x.shape[:-1]), x
+        return _as_given(y, x), x
     if residual.shape != x.shape:
         raise ValueError("x and residual must have the same shape")
     y, h = _NormLinear.apply(flat, residual.reshape(flat.shape), norm_weight, w8.weight, w8, eps)
-    return y.unflatten(0, x.shape[:-1]), h.unflatten(0, x.shape[:-1])
+    return _as_given(y, x), _as_given(h, x)

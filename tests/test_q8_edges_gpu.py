@@ -77,3 +77,28 @@ def test_second_derivatives_are_refused():
         with pytest.raises(RuntimeError):
             gx, gw = torch.autograd.grad(f(), [x, W], create_graph=True)
             torch.autograd.grad(gx.square().sum() + gw.square().sum(), x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lead", [(), (1,), (2, 3), (2, 0), (0,)])
+def test_layers_take_any_leading_dimensions(lead):
+    """One vector, no tokens at all: as the rows of a matrix, gradients too."""
+    W, n = randn(3, 64, 32).requires_grad_(), torch.ones(64, device="cuda", requires_grad=True)
+    w8 = Q.Weight8(W)
+    x, r = (randn(k, *lead, 64).requires_grad_() for k in (1, 2))
+    gy, gh = randn(4, *lead, 32), randn(5, *lead, 64)
+
+    def run(f, x, r, gy, gh):
+        y, h = f(x, r)
+        return y, h, torch.autograd.grad([y, h], [x, r, n, W], [gy, gh])
+
+    flat = lambda t: t.detach().reshape(-1, t.shape[-1])  # noqa: E731
+    for f in (lambda x, r: Q.norm_linear(x, r, n, w8),
+              lambda x, r: (Q.norm_linear(x, None, n, w8)[0], x + r),
+              lambda x, r: (Q.linear(x, w8) + n.sum(), x + r)):
+        y, h, got = run(f, x, r, gy, gh)
+        assert y.shape == (*lead, 32) and h.shape == (*lead, 64)
+        y2, h2, want = run(f, flat(x).requires_grad_(), flat(r).requires_grad_(), flat(gy), flat(gh))
+        assert torch.equal(flat(y), y2) and torch.equal(flat(h), h2)
+        assert all(torch.equal(a.reshape(b.shape), b) for a, b in zip(got, want))
+        assert [g.shape for g in got] == [t.shape for t in (x, r, n, W)]
