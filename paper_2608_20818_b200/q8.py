@@ -75,9 +75,15 @@ class _Linear(torch.autograd.Function):
 
 
 class _NormLinear(torch.autograd.Function):
+    # x and residual come in the shape they were given: both get the same gradient, which autograd keeps apart
+    # only where both get the same tensor, not two views of one.
     @staticmethod
     def forward(ctx, x, residual, norm_weight, weight, w8, eps):
         ctx.set_materialize_grads(False)
+        ctx.shape = x.shape
+        x = x.reshape(-1, x.shape[-1])
+        if residual is not None:
+            residual = residual.reshape(x.shape)
         x8, sx, h = prm_rmsnorm_q8(x, norm_weight, eps, residual=residual, format=w8.format)
         ctx.save_for_backward(x8, sx, w8.codes, w8.scale, x if h is None else h, norm_weight)
         ctx.format, ctx.eps, ctx.types = w8.format, eps, (x.dtype, weight.dtype)
@@ -89,7 +95,8 @@ class _NormLinear(torch.autograd.Function):
         _refuse_second_derivative()
         x8, sx, codes, scale, h, norm_weight = ctx.saved_tensors
         need = ctx.needs_input_grad
-        if grad_out is None:                # only the stream goes on
+        if grad_out is None:                # only the stream goes on; the caller may hold grad_h
+            grad_h = grad_h.clone().reshape(ctx.shape)
             return (grad_h if need[0] else None, grad_h if need[1] else None, None, None, None, None)
         need_stream = need[0] or need[1] or need[2]
         if not (need_stream or need[3]):
@@ -98,6 +105,7 @@ class _NormLinear(torch.autograd.Function):
         dx = dn = None
         if need_stream:
             dx, dn = prm_rmsnorm_q8_backward(dy, h, norm_weight, ctx.eps, grad_h=grad_h)
+            dx = dx.reshape(ctx.shape)
         return (dx if need[0] else None, dx if need[1] else None, dn if need[2] else None, dw, None, None)
 
 
@@ -114,11 +122,9 @@ def linear(x, w8):
 def norm_linear(x, residual, norm_weight, w8, eps=1e-6):
     """Root-mean-square norm of h = x + residual, then @ W, both in 8 bits: (y, h).  residual may be None
     (h = x); h carries the residual stream on."""
-    flat = x.reshape(-1, x.shape[-1])
     if residual is None:
-        y = _NormLinear.apply(flat, None, norm_weight, w8.weight, w8, eps)
-        return _as_given(y, x), x
+        return _as_given(_NormLinear.apply(x, None, norm_weight, w8.weight, w8, eps), x), x
     if residual.shape != x.shape:
         raise ValueError("x and residual must have the same shape")
-    y, h = _NormLinear.apply(flat, residual.reshape(flat.shape), norm_weight, w8.weight, w8, eps)
+    y, h = _NormLinear.apply(x, residual, norm_weight, w8.weight, w8, eps)
     return _as_given(y, x), _as_given(h, x)

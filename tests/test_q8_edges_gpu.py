@@ -102,3 +102,24 @@ def test_layers_take_any_leading_dimensions(lead):
         assert torch.equal(flat(y), y2) and torch.equal(flat(h), h2)
         assert all(torch.equal(a.reshape(b.shape), b) for a, b in zip(got, want))
         assert [g.shape for g in got] == [t.shape for t in (x, r, n, W)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(6, 64), (2, 3, 64)])
+def test_gradients_of_x_and_residual_accumulate_apart(shape):
+    """Both get the same gradient; what is added to one in a later backward pass must not reach the other."""
+    n = torch.ones(64, device="cuda", requires_grad=True)
+    w8 = Q.Weight8(randn(3, 64, 32).requires_grad_())
+    gy, gh = randn(4, *shape[:-1], 32), randn(5, *shape)
+    for used in ((0, 1), (0,), (1,)):
+        x, r = (randn(k, *shape).requires_grad_() for k in (1, 2))
+
+        def out():
+            both = Q.norm_linear(x, r, n, w8)
+            return [both[i] for i in used], [(gy, gh)[i] for i in used]
+
+        one, = torch.autograd.grad(out()[0], x, out()[1])
+        for _ in range(3):
+            torch.autograd.backward(*out())
+        assert torch.equal(x.grad, one + one + one) and torch.equal(r.grad, x.grad)
+        assert x.grad.data_ptr() != r.grad.data_ptr()
