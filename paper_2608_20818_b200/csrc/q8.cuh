@@ -377,7 +377,7 @@ __device__ __forceinline__ void block_sum2(float& p, float& q, float* red) {
 }
 
 // Launches that overlap the end of the kernel before them (programmatic dependent launch): every
-// kernel here calls grid_wait() before it touches global memory, which holds it until all kernels
+// kernel that is launched so calls grid_wait() before it touches global memory, which holds it until all kernels
 // before it in the stream have finished and their writes are visible, and grid_trigger() once it
 // holds all resources that it will ever ask for, which lets the next kernel start setting up.
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -401,6 +401,24 @@ inline cudaError_t launch_after(void (*kernel)(P...), unsigned grid, unsigned bl
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 0 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
+// The same without the overlap and without clusters.
+template <typename... P, typename... A>
+inline cudaError_t launch_in_turn(void (*kernel)(P...), dim3 grid, unsigned block, cudaStream_t stream, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block, 1, 1);
+  cfg.stream = stream;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
+// What a call returns for its own CUDA calls: not what an earlier one has left as the thread's last error,
+// and leaving none behind for those who ask for it.
+inline int q8_code(cudaError_t e) {
+  if (e == cudaSuccess) return PRM_OK;
+  cudaGetLastError();
+  return PRM_ERR_CUDA;
 }
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }

@@ -255,15 +255,13 @@ int launch_matmul(const CUtensorMap& mp, const CUtensorMap& mq, const SplitArgs&
   static PerDeviceOnce once;
   int dev;
   if (once.need(&dev)) {
-    if (cudaFuncSetAttribute(matmul_q8_kernel<INT8, P_MN, Q_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)(kSmemBudget + 1024)) != cudaSuccess)
-      return PRM_ERR_CUDA;
+    const cudaError_t e = cudaFuncSetAttribute(matmul_q8_kernel<INT8, P_MN, Q_MN>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmemBudget + 1024));
+    if (e != cudaSuccess) return q8_code(e);
     once.mark(dev);
   }
-  return launch_after(matmul_q8_kernel<INT8, P_MN, Q_MN>, (unsigned)ctas, kThreads, smem, stream, (unsigned)a.split, mp,
-                      mq, a) == cudaSuccess
-             ? PRM_OK
-             : PRM_ERR_CUDA;
+  return q8_code(launch_after(matmul_q8_kernel<INT8, P_MN, Q_MN>, (unsigned)ctas, kThreads, smem, stream,
+                              (unsigned)a.split, mp, mq, a));
 }
 
 // CTAs in clusters of `split` that are resident at once (1 per SM; how many clusters fit depends on how
@@ -381,9 +379,7 @@ extern "C" int prm_matmul_q8(const void* a, int64_t ld_a, int a_transposed, cons
   if ((uintptr_t)out % es != 0 || ((uintptr_t)scale_a | (uintptr_t)scale_b) % 4 != 0) return PRM_ERR_ALIGN;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (k == 0)                             // an empty sum
-    return cudaMemset2DAsync(out, (size_t)ld_out * es, 0, (size_t)n * es, (size_t)m, stream) == cudaSuccess
-               ? PRM_OK
-               : PRM_ERR_CUDA;
+    return q8_code(cudaMemset2DAsync(out, (size_t)ld_out * es, 0, (size_t)n * es, (size_t)m, stream));
   if (!a || !b) return PRM_ERR_ARG;
   const int64_t a_rows = a_transposed ? k : m, a_cols = a_transposed ? m : k;
   const int64_t b_rows = b_transposed ? n : k, b_cols = b_transposed ? k : n;
@@ -415,9 +411,8 @@ extern "C" int prm_matmul_q8(const void* a, int64_t ld_a, int a_transposed, cons
 extern "C" int prm_q8_status(void) {
   int v = 0;
   const int zero = 0;
-  if (cudaDeviceSynchronize() != cudaSuccess) return PRM_ERR_CUDA;
-  if (cudaMemcpyFromSymbol(&v, g_q8_status, sizeof(int)) != cudaSuccess) return PRM_ERR_CUDA;
-  if (v == 0) return PRM_OK;
-  if (cudaMemcpyToSymbol(g_q8_status, &zero, sizeof(int)) != cudaSuccess) return PRM_ERR_CUDA;
-  return PRM_ERR_DEVICE_TIMEOUT;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&v, g_q8_status, sizeof(int));
+  if (e == cudaSuccess && v != 0) e = cudaMemcpyToSymbol(g_q8_status, &zero, sizeof(int));
+  return e != cudaSuccess ? q8_code(e) : v != 0 ? PRM_ERR_DEVICE_TIMEOUT : PRM_OK;
 }

@@ -320,18 +320,17 @@ int launch_pairs(const CUtensorMap& mp, const CUtensorMap& mq, const PairArgs& a
   static int resident[64];
   int dev;
   if (once.need(&dev)) {
-    if (dev < 0 || cudaFuncSetAttribute(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)kSmemBytes) != cudaSuccess)
-      return PRM_ERR_CUDA;
+    if (dev < 0) return PRM_ERR_CUDA;
+    const cudaError_t e = cudaFuncSetAttribute(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+    if (e != cudaSuccess) return q8_code(e);
     const int n = q8_resident_clusters(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, kThreads, kSmemBytes, 2);
     if (n < 1) return PRM_ERR_CUDA;
     resident[dev] = n;
     once.mark(dev);
   }
-  return launch_after(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, 2u * (unsigned)std::min(a.tiles, resident[dev]), kThreads,
-                      kSmemBytes, stream, 2, mp, mq, a) == cudaSuccess
-             ? PRM_OK
-             : PRM_ERR_CUDA;
+  return q8_code(launch_after(matmul_q8_pair_kernel<INT8, P_MN, Q_MN>, 2u * (unsigned)std::min(a.tiles, resident[dev]),
+                              kThreads, kSmemBytes, stream, 2, mp, mq, a));
 }
 
 }  // namespace

@@ -197,9 +197,8 @@ template <typename IO, typename WT, int NV, int TPR>
 int launch_norm(const NormArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR <= 32 ? 256 / TPR : 1, kThreads = TPR <= 32 ? 256 : TPR;
   const unsigned blocks = (unsigned)((a.rows + kRows - 1) / kRows);
-  if (a.residual) launch_after(rmsnorm_q8_kernel<IO, WT, NV, TPR, true>, blocks, kThreads, 0, stream, 0, a);
-  else launch_after(rmsnorm_q8_kernel<IO, WT, NV, TPR, false>, blocks, kThreads, 0, stream, 0, a);
-  return PRM_OK;
+  return q8_code(launch_after(a.residual ? rmsnorm_q8_kernel<IO, WT, NV, TPR, true> : rmsnorm_q8_kernel<IO, WT, NV, TPR, false>,
+                              blocks, kThreads, 0, stream, 0, a));
 }
 
 template <typename IO, typename WT>
@@ -220,10 +219,10 @@ int run_norm(const NormArgs& a, cudaStream_t stream) {
 }
 
 template <typename IO, int NV, int TPR>
-void launch_norm_shifted(const NormArgs& a, cudaStream_t stream) {
+int launch_norm_shifted(const NormArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR == 32 ? 8 : 1;
-  launch_after(rmsnorm_q8_shifted_kernel<IO, NV, TPR>, (unsigned)((a.rows + kRows - 1) / kRows), TPR == 32 ? 256 : TPR, 0,
-               stream, 0, a);
+  return q8_code(launch_after(rmsnorm_q8_shifted_kernel<IO, NV, TPR>, (unsigned)((a.rows + kRows - 1) / kRows),
+                              TPR == 32 ? 256 : TPR, 0, stream, 0, a));
 }
 
 // `alike`: the matrices' rows start alike and the codes' rows on 8 bytes.
@@ -231,24 +230,21 @@ template <typename IO>
 int run_norm_single(const NormArgs& a, bool alike, cudaStream_t stream) {
   const int c = a.cols + 7;               // a row may need one more oct
   if (alike && c <= 32768) {
-    if (c <= 256) launch_norm_shifted<IO, 1, 32>(a, stream);
-    else if (c <= 512) launch_norm_shifted<IO, 2, 32>(a, stream);
-    else if (c <= 1024) launch_norm_shifted<IO, 1, 128>(a, stream);
-    else if (c <= 2048) launch_norm_shifted<IO, 2, 128>(a, stream);
-    else if (c <= 3072) launch_norm_shifted<IO, 3, 128>(a, stream);
-    else if (c <= 4096) launch_norm_shifted<IO, 2, 256>(a, stream);
-    else if (c <= 6144) launch_norm_shifted<IO, 3, 256>(a, stream);
-    else if (c <= 8192) launch_norm_shifted<IO, 2, 512>(a, stream);
-    else if (c <= 12288) launch_norm_shifted<IO, 3, 512>(a, stream);
-    else if (c <= 16384) launch_norm_shifted<IO, 2, 1024>(a, stream);
-    else if (c <= 24576) launch_norm_shifted<IO, 3, 1024>(a, stream);
-    else launch_norm_shifted<IO, 4, 1024>(a, stream);
-  } else if (c <= 1024) {
-    launch_after(rmsnorm_q8_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a);
-  } else {
-    launch_after(rmsnorm_q8_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a);
+    if (c <= 256) return launch_norm_shifted<IO, 1, 32>(a, stream);
+    if (c <= 512) return launch_norm_shifted<IO, 2, 32>(a, stream);
+    if (c <= 1024) return launch_norm_shifted<IO, 1, 128>(a, stream);
+    if (c <= 2048) return launch_norm_shifted<IO, 2, 128>(a, stream);
+    if (c <= 3072) return launch_norm_shifted<IO, 3, 128>(a, stream);
+    if (c <= 4096) return launch_norm_shifted<IO, 2, 256>(a, stream);
+    if (c <= 6144) return launch_norm_shifted<IO, 3, 256>(a, stream);
+    if (c <= 8192) return launch_norm_shifted<IO, 2, 512>(a, stream);
+    if (c <= 12288) return launch_norm_shifted<IO, 3, 512>(a, stream);
+    if (c <= 16384) return launch_norm_shifted<IO, 2, 1024>(a, stream);
+    if (c <= 24576) return launch_norm_shifted<IO, 3, 1024>(a, stream);
+    return launch_norm_shifted<IO, 4, 1024>(a, stream);
   }
-  return PRM_OK;
+  if (c <= 1024) return q8_code(launch_after(rmsnorm_q8_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a));
+  return q8_code(launch_after(rmsnorm_q8_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a));
 }
 
 // ------------------------------------------------------------------ gradient
@@ -748,10 +744,8 @@ int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
 }
 int launch_grad_grid(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int64_t grid, cudaStream_t stream) {
   void* args[1] = {&a};
-  return cudaLaunchCooperativeKernel((const void*)kernel, dim3((unsigned)grid), dim3((unsigned)threads), args, 0,
-                                     stream) == cudaSuccess
-             ? PRM_OK
-             : PRM_ERR_CUDA;
+  return q8_code(cudaLaunchCooperativeKernel((const void*)kernel, dim3((unsigned)grid), dim3((unsigned)threads), args, 0,
+                                             stream));
 }
 int launch_grad(void (*kernel)(NormGradArgs), const NormGradArgs& a, int threads, int nv, cudaStream_t stream) {
   return launch_grad_grid(kernel, a, threads, grad_grid(a.rows, a.cols, grad_blocks(threads, nv)), stream);
@@ -829,21 +823,17 @@ extern "C" int prm_rmsnorm_q8(const void* x, int64_t ld_x, const void* residual,
                     aligned16(weight) && ((uintptr_t)q_out & 7) == 0 &&
                     (!residual || (ld_residual % 8 == 0 && ld_h % 8 == 0 && aligned16(residual) && aligned16(h_out)));
   cudaStream_t stream = (cudaStream_t)cuda_stream;
-  int code;
   if (!octs) {
     auto alike = [&](auto type) {
       using T = decltype(type);
       return ((uintptr_t)q_out & 7) == 0 && ld_q % 8 == 0 &&
              (!residual || (octs_alike<T>(x, ld_x, residual, ld_residual) && octs_alike<T>(x, ld_x, h_out, ld_h)));
     };
-    code = io_fp32 ? run_norm_single<float>(a, alike(float()), stream)
+    return io_fp32 ? run_norm_single<float>(a, alike(float()), stream)
                    : run_norm_single<__nv_bfloat16>(a, alike(__nv_bfloat16()), stream);
   }
-  else if (io_fp32)
-    code = weight_fp32 ? run_norm<float, float>(a, stream) : run_norm<float, __nv_bfloat16>(a, stream);
-  else
-    code = weight_fp32 ? run_norm<__nv_bfloat16, float>(a, stream) : run_norm<__nv_bfloat16, __nv_bfloat16>(a, stream);
-  return code != PRM_OK ? code : (cudaGetLastError() == cudaSuccess ? PRM_OK : PRM_ERR_CUDA);
+  if (io_fp32) return weight_fp32 ? run_norm<float, float>(a, stream) : run_norm<float, __nv_bfloat16>(a, stream);
+  return weight_fp32 ? run_norm<__nv_bfloat16, float>(a, stream) : run_norm<__nv_bfloat16, __nv_bfloat16>(a, stream);
 }
 
 extern "C" size_t prm_rmsnorm_q8_scratch_bytes(int64_t rows, int64_t cols) {
@@ -864,8 +854,7 @@ extern "C" int prm_rmsnorm_q8_backward(const void* grad_y, int64_t ld_grad_y, co
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if ((uintptr_t)grad_weight % (weight_fp32 ? 4 : 2) != 0) return PRM_ERR_ALIGN;
   if (rows == 0)                          // an empty sum
-    return cudaMemsetAsync(grad_weight, 0, (size_t)cols * (weight_fp32 ? 4 : 2), stream) == cudaSuccess ? PRM_OK
-                                                                                                     : PRM_ERR_CUDA;
+    return q8_code(cudaMemsetAsync(grad_weight, 0, (size_t)cols * (weight_fp32 ? 4 : 2), stream));
   if (!grad_y || !h || !weight || !grad_x || !scratch) return PRM_ERR_ARG;
   if (scratch_bytes < prm_rmsnorm_q8_scratch_bytes(rows, cols)) return PRM_ERR_WORKSPACE;
   const int es = io_fp32 ? 4 : 2;

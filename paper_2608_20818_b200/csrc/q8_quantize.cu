@@ -590,75 +590,75 @@ int run_stream(QuantArgs a, cudaStream_t stream) {
 }
 
 template <typename IO, int LANES>
-void launch_panels(const QuantArgs& a, cudaStream_t stream) {
+int launch_panels(const QuantArgs& a, cudaStream_t stream) {
   // as many blocks as there are turns' worth of rows
   unsigned blocks = 1;
   while (blocks < kPanelCluster && a.rows > (int64_t)blocks * kPanelRows * (kPanelThreads / LANES)) blocks *= 2;
-  launch_after(quantize_panel_kernel<IO, LANES>, (unsigned)((a.cols + LANES * 8 - 1) / (LANES * 8)) * blocks,
-               kPanelThreads, 0, stream, blocks, a);
+  return q8_code(launch_after(quantize_panel_kernel<IO, LANES>,
+                              (unsigned)((a.cols + LANES * 8 - 1) / (LANES * 8)) * blocks, kPanelThreads, 0, stream, blocks,
+                              a));
 }
 template <typename IO>
-void run_panels(const QuantArgs& a, cudaStream_t stream) {
-  if (a.cols <= 2048 && a.rows >= 1024) launch_panels<IO, 8>(a, stream);
-  else launch_panels<IO, 16>(a, stream);
+int run_panels(const QuantArgs& a, cudaStream_t stream) {
+  return a.cols <= 2048 && a.rows >= 1024 ? launch_panels<IO, 8>(a, stream) : launch_panels<IO, 16>(a, stream);
 }
 
 template <typename IO, int NV, int TPR>
-void launch_rows(const QuantArgs& a, cudaStream_t stream) {
+int launch_rows(const QuantArgs& a, cudaStream_t stream) {
   constexpr int kRows = TPR <= 32 ? 256 / TPR : 1;
-  launch_after(quantize_rows_kernel<IO, NV, TPR>, (unsigned)((a.rows + kRows - 1) / kRows), TPR <= 32 ? 256 : TPR, 0,
-               stream, 0, a);
+  return q8_code(launch_after(quantize_rows_kernel<IO, NV, TPR>, (unsigned)((a.rows + kRows - 1) / kRows),
+                              TPR <= 32 ? 256 : TPR, 0, stream, 0, a));
 }
 
 template <typename IO>
-void run_rows(const QuantArgs& a, bool octs, cudaStream_t stream) {
+int run_rows(const QuantArgs& a, bool octs, cudaStream_t stream) {
   const int c = a.cols;
   if (octs && c <= 16384) {
-    if (c <= 64) launch_rows<IO, 1, 8>(a, stream);
-    else if (c <= 128) launch_rows<IO, 1, 16>(a, stream);
-    else if (c <= 256) launch_rows<IO, 1, 32>(a, stream);
-    else if (c <= 512) launch_rows<IO, 2, 32>(a, stream);
-    else if (c <= 1024) launch_rows<IO, 4, 32>(a, stream);   // 16384 x 1024: 8.3 us, a block per row 17.5
-    else if (c <= 2048) launch_rows<IO, 2, 128>(a, stream);
-    else if (c <= 4096) launch_rows<IO, 2, 256>(a, stream);
-    else if (c <= 8192) launch_rows<IO, 2, 512>(a, stream);
-    else launch_rows<IO, 2, 1024>(a, stream);
-  } else if (c + 7 <= 32768 && a.ld_qr % 8 == 0 && ((uintptr_t)a.q_rows & 7) == 0) {
-    auto go = [&](auto kernel, int per_block, int threads) {
-      launch_after(kernel, (unsigned)((a.rows + per_block - 1) / per_block), (unsigned)threads, 0, stream, 0, a);
-    };
-    const int w = c + 7;                  // a row may need one more oct
-    if (w <= 256) go(quantize_rows_shifted_kernel<IO, 1, 32>, 8, 256);
-    else if (w <= 512) go(quantize_rows_shifted_kernel<IO, 2, 32>, 8, 256);
-    else if (w <= 1024) go(quantize_rows_shifted_kernel<IO, 1, 128>, 1, 128);
-    else if (w <= 2048) go(quantize_rows_shifted_kernel<IO, 2, 128>, 1, 128);
-    else if (w <= 3072) go(quantize_rows_shifted_kernel<IO, 3, 128>, 1, 128);
-    else if (w <= 4096) go(quantize_rows_shifted_kernel<IO, 2, 256>, 1, 256);
-    else if (w <= 6144) go(quantize_rows_shifted_kernel<IO, 3, 256>, 1, 256);
-    else if (w <= 8192) go(quantize_rows_shifted_kernel<IO, 2, 512>, 1, 512);
-    else if (w <= 12288) go(quantize_rows_shifted_kernel<IO, 3, 512>, 1, 512);
-    else if (w <= 16384) go(quantize_rows_shifted_kernel<IO, 2, 1024>, 1, 1024);
-    else if (w <= 24576) go(quantize_rows_shifted_kernel<IO, 3, 1024>, 1, 1024);
-    else go(quantize_rows_shifted_kernel<IO, 4, 1024>, 1, 1024);
-  } else if (c <= 1024) {
-    launch_after(quantize_rows_single_kernel<IO, 128>, (unsigned)a.rows, 128, 0, stream, 0, a);
-  } else {
-    launch_after(quantize_rows_single_kernel<IO, 1024>, (unsigned)a.rows, 1024, 0, stream, 0, a);
+    if (c <= 64) return launch_rows<IO, 1, 8>(a, stream);
+    if (c <= 128) return launch_rows<IO, 1, 16>(a, stream);
+    if (c <= 256) return launch_rows<IO, 1, 32>(a, stream);
+    if (c <= 512) return launch_rows<IO, 2, 32>(a, stream);
+    if (c <= 1024) return launch_rows<IO, 4, 32>(a, stream);   // 16384 x 1024: 8.3 us, a block per row 17.5
+    if (c <= 2048) return launch_rows<IO, 2, 128>(a, stream);
+    if (c <= 4096) return launch_rows<IO, 2, 256>(a, stream);
+    if (c <= 8192) return launch_rows<IO, 2, 512>(a, stream);
+    return launch_rows<IO, 2, 1024>(a, stream);
   }
+  auto go = [&](auto kernel, int per_block, int threads) {
+    return q8_code(launch_after(kernel, (unsigned)((a.rows + per_block - 1) / per_block), (unsigned)threads, 0, stream, 0, a));
+  };
+  if (c + 7 <= 32768 && a.ld_qr % 8 == 0 && ((uintptr_t)a.q_rows & 7) == 0) {
+    const int w = c + 7;                  // a row may need one more oct
+    if (w <= 256) return go(quantize_rows_shifted_kernel<IO, 1, 32>, 8, 256);
+    if (w <= 512) return go(quantize_rows_shifted_kernel<IO, 2, 32>, 8, 256);
+    if (w <= 1024) return go(quantize_rows_shifted_kernel<IO, 1, 128>, 1, 128);
+    if (w <= 2048) return go(quantize_rows_shifted_kernel<IO, 2, 128>, 1, 128);
+    if (w <= 3072) return go(quantize_rows_shifted_kernel<IO, 3, 128>, 1, 128);
+    if (w <= 4096) return go(quantize_rows_shifted_kernel<IO, 2, 256>, 1, 256);
+    if (w <= 6144) return go(quantize_rows_shifted_kernel<IO, 3, 256>, 1, 256);
+    if (w <= 8192) return go(quantize_rows_shifted_kernel<IO, 2, 512>, 1, 512);
+    if (w <= 12288) return go(quantize_rows_shifted_kernel<IO, 3, 512>, 1, 512);
+    if (w <= 16384) return go(quantize_rows_shifted_kernel<IO, 2, 1024>, 1, 1024);
+    if (w <= 24576) return go(quantize_rows_shifted_kernel<IO, 3, 1024>, 1, 1024);
+    return go(quantize_rows_shifted_kernel<IO, 4, 1024>, 1, 1024);
+  }
+  return c <= 1024 ? go(quantize_rows_single_kernel<IO, 128>, 1, 128) : go(quantize_rows_single_kernel<IO, 1024>, 1, 1024);
 }
 
 // Columns of any alignment.  (Octs aligned in memory, as the row kernels walk them, were slower here: the
 // rows that start alike lie eight rows apart, 8192 x 4097 102 us against 77.)
 template <typename IO>
-void run_cols(const QuantArgs& a, cudaStream_t stream) {
+int run_cols(const QuantArgs& a, cudaStream_t stream) {
   const int bx = (a.cols + kColThreads - 1) / kColThreads;
   // enough slabs for about eight blocks per SM, none shorter than 16 rows
   int64_t slabs = std::max<int64_t>(1, std::min<int64_t>((a.rows + 15) / 16, (8 * kRingBlocks + bx - 1) / bx));
   slabs = std::min<int64_t>(slabs, 65535);
   const int slab = (int)((a.rows + slabs - 1) / slabs);
   const dim3 grid((unsigned)bx, (unsigned)((a.rows + slab - 1) / slab));
-  column_top_kernel<IO><<<grid, kColThreads, 0, stream>>>(a, slab);
-  quantize_cols_kernel<IO><<<grid, kColThreads, 0, stream>>>(a, slab);
+  cudaError_t e = cudaMemsetAsync(a.top, 0, (size_t)a.cols * 4, stream);
+  if (e == cudaSuccess) e = launch_in_turn(column_top_kernel<IO>, grid, kColThreads, stream, a, slab);
+  if (e == cudaSuccess) e = launch_in_turn(quantize_cols_kernel<IO>, grid, kColThreads, stream, a, slab);
+  return q8_code(e);
 }
 
 }  // namespace
@@ -688,8 +688,7 @@ extern "C" int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_
       (q_cols && !aligned16(scratch)))
     return PRM_ERR_ALIGN;
   if (rows == 0) {                        // columns without an element: scale 0
-    if (q_cols && cudaMemsetAsync(scale_cols, 0, (size_t)cols * 4, stream) != cudaSuccess) return PRM_ERR_CUDA;
-    return PRM_OK;
+    return q_cols ? q8_code(cudaMemsetAsync(scale_cols, 0, (size_t)cols * 4, stream)) : PRM_OK;
   }
   if (!x) return PRM_ERR_ARG;
   if ((uintptr_t)x % (io_fp32 ? 4 : 2) != 0) return PRM_ERR_ALIGN;
@@ -704,28 +703,19 @@ extern "C" int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_
   // Up to these sizes by panels (1500 x 2048 both ways with folds: 10.0 us, streamed 14.4; 4096 x 4096 columns:
   // 16.3 against 19.8), beyond them streamed (8192 x 8192: 57.4 against 64.5; 32768 x 512: 27.5 against 42.5).
   const bool panels = q_cols && octs_c && rows <= (cols < 256 ? 2048 : 8192) && rows * cols <= (int64_t)1 << 24;
-  if (!panels && q_cols && octs_c && cols >= 256 && cols <= 32 * 8192) {
+  int code = PRM_OK;
+  if (panels) {
+    code = io_fp32 ? run_panels<float>(a, stream) : run_panels<__nv_bfloat16>(a, stream);
+    q_cols = nullptr;
+  } else if (q_cols && octs_c && cols >= 256 && cols <= 32 * 8192) {
     const bool joint = q_rows && octs_r && cols <= (io_fp32 ? kWidest<float> : kWidest<__nv_bfloat16>);
-    int code;
     if (joint) code = io_fp32 ? run_stream<float, true>(a, stream) : run_stream<__nv_bfloat16, true>(a, stream);
     else code = io_fp32 ? run_stream<float, false>(a, stream) : run_stream<__nv_bfloat16, false>(a, stream);
-    if (code != PRM_OK) return code;
     if (joint) q_rows = nullptr;
     q_cols = nullptr;
   }
-  if (panels) {
-    if (io_fp32) run_panels<float>(a, stream);
-    else run_panels<__nv_bfloat16>(a, stream);
-    q_cols = nullptr;
-  }
-  if (q_rows) {
-    if (io_fp32) run_rows<float>(a, octs_r, stream);
-    else run_rows<__nv_bfloat16>(a, octs_r, stream);
-  }
-  if (q_cols) {
-    if (cudaMemsetAsync(scratch, 0, (size_t)cols * 4, stream) != cudaSuccess) return PRM_ERR_CUDA;
-    if (io_fp32) run_cols<float>(a, stream);
-    else run_cols<__nv_bfloat16>(a, stream);
-  }
-  return cudaGetLastError() == cudaSuccess ? PRM_OK : PRM_ERR_CUDA;
+  if (code == PRM_OK && q_rows)
+    code = io_fp32 ? run_rows<float>(a, octs_r, stream) : run_rows<__nv_bfloat16>(a, octs_r, stream);
+  if (code == PRM_OK && q_cols) code = io_fp32 ? run_cols<float>(a, stream) : run_cols<__nv_bfloat16>(a, stream);
+  return code;
 }

@@ -329,8 +329,8 @@ int launch_ring(void (*kernel)(A, int, int*), PerDeviceOnce& once, unsigned bloc
                 size_t after, bool cooperative, cudaStream_t stream, A a) {
   int dev;
   if (once.need(&dev)) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes) != cudaSuccess)
-      return PRM_ERR_CUDA;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+    if (e != cudaSuccess) return q8_code(e);
     once.mark(dev);
   }
   int* status = q8_status_word();
@@ -345,7 +345,7 @@ int launch_ring(void (*kernel)(A, int, int*), PerDeviceOnce& once, unsigned bloc
   } else {
     e = launch_after(kernel, blocks, kRingThreads, smem, stream, 0, a, stages, status);
   }
-  return e == cudaSuccess ? PRM_OK : PRM_ERR_CUDA;
+  return q8_code(e);
 }
 inline unsigned ring_blocks(int64_t rows, int rows_per_set, int groups) {
   const int64_t sets = (rows + rows_per_set - 1) / rows_per_set;

@@ -1,5 +1,9 @@
 """Edges of the 8-bit operators: the documented rounding bit by bit, sizes and values at the ends of their ranges."""
 
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -123,3 +127,49 @@ def test_gradients_of_x_and_residual_accumulate_apart(shape):
             torch.autograd.backward(*out())
         assert torch.equal(x.grad, one + one + one) and torch.equal(r.grad, x.grad)
         assert x.grad.data_ptr() != r.grad.data_ptr()
+
+
+STALE_ERROR = """
+import torch
+from paper_2608_20818_b200 import binding as B
+
+opt = B.PeriodicRowwiseMuon([(64, 64)], K=5, beta=0.9, nesterov=True, lr=0.1, wd=0.0)
+weight, grad = (torch.ones(64, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+momentum = torch.zeros(64, 64, device="cuda")
+opt.step([weight], [grad], [momentum], 1)
+x = torch.randn(300, 256, device="cuda")
+w = torch.ones(256, device="cuda")
+torch.cuda.synchronize()
+
+
+def during_capture(call):
+    # A stream under capture cannot be waited for: CUDA refuses on the host, and the error stays the thread's last.
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        code = call()
+        try:
+            graph.capture_end()
+        except RuntimeError:
+            pass
+    return code
+
+
+calls = [lambda: B.prm_rmsnorm_q8(x, w, 1e-6), lambda: B.prm_rmsnorm_q8(x[:, :255], w[:255], 1e-6),
+         lambda: B.prm_quantize_q8(x), lambda: B.prm_quantize_q8(x[:, :255]), lambda: B.prm_quantize_q8(x, by_cols=True),
+         lambda: B.prm_quantize_q8(x[:, :255], by_rows=False, by_cols=True), lambda: B.prm_rmsnorm_q8_backward(x, x, w, 1e-6)]
+for call in calls:
+    assert during_capture(lambda: B.prm_status(opt.h)) == B.PRM_ERR_CUDA
+    call()
+assert during_capture(B.prm_q8_status) == B.PRM_ERR_CUDA       # leaves no error for the next to find
+B.prm_adamw_step([w], [torch.ones_like(w)], [torch.zeros_like(w)], [torch.zeros_like(w)], 1, lr=1e-3)
+torch.cuda.synchronize()
+print("done")
+"""
+
+
+@pytest.mark.gpu
+def test_errors_of_other_calls_are_not_theirs():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", STALE_ERROR], cwd=root, capture_output=True, text=True, timeout=300)
+    assert run.stdout.strip() == "done", run.stderr[-2000:]
