@@ -124,17 +124,17 @@ template <> struct Oct<float> {
 // nearest-even there.  The product has to be rounded before: in one fused step 1 in 2,700 bf16 values, next
 // to a tie, gets another code than by the rule above.  A product and a sum of pairs come out of the
 // assembler as one fused step, explicit rounding or not, so the product is itself a fused step, with a -0
-// from constant memory, which the assembler does not take for a known number.
-static __constant__ float2 kMinusZero = {-0.f, -0.f};
-__device__ __forceinline__ float2 int8_bits(float2 t, float2 mul) {
-  return add2(fma2(t, mul, kMinusZero), make_float2(12582912.f, 12582912.f));
+// that the assembler does not take for a known number: `nz` comes with the kernel's arguments (from
+// constant memory one token of the norm takes 1.9 us instead of 1.6).
+__device__ __forceinline__ float2 int8_bits(float2 t, float2 mul, float nz) {
+  return add2(fma2(t, mul, make_float2(nz, nz)), make_float2(12582912.f, 12582912.f));
 }
 // Four codes of t * mul (first value in the lowest byte).
 template <int FORMAT>
-__device__ __forceinline__ uint32_t codes4(float2 a, float2 b, float2 mul) {
+__device__ __forceinline__ uint32_t codes4(float2 a, float2 b, float2 mul, float nz) {
   if constexpr (FORMAT == PRM_Q8_INT8) {
-    a = int8_bits(a, mul);
-    b = int8_bits(b, mul);
+    a = int8_bits(a, mul, nz);
+    b = int8_bits(b, mul, nz);
     return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
                        __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
   } else {
@@ -144,14 +144,14 @@ __device__ __forceinline__ uint32_t codes4(float2 a, float2 b, float2 mul) {
   }
 }
 __device__ __forceinline__ uint8_t code1(float v, float mul, int format) {
-  const float2 p = make_float2(v, 0.f), f = make_float2(mul, mul);
-  return (uint8_t)((format == PRM_Q8_INT8 ? codes4<PRM_Q8_INT8>(p, p, f) : codes4<PRM_Q8_E4M3>(p, p, f)) & 0xffu);
+  if (format == PRM_Q8_INT8) return (uint8_t)__float_as_uint(__fadd_rn(__fmul_rn(v, mul), 12582912.f));
+  return (uint8_t)__nv_cvt_float_to_fp8(__fmul_rn(v, mul), __NV_SATFINITE, __NV_E4M3);
 }
 // The codes of NV octs of a thread, `stride` elements apart, below `cols`; zeros where the row has no
 // number for a scale.
 template <int NV, int FORMAT>
 __device__ __forceinline__ void store_octs_as(uint8_t* q, const float2 (&t)[NV][4], int c0, int stride, int cols,
-                                              float top) {
+                                              float top, float nz) {
   const float f = q8_mul(top, q8_limit(FORMAT));
   const float2 mul = make_float2(f, f);
 #pragma unroll
@@ -159,20 +159,20 @@ __device__ __forceinline__ void store_octs_as(uint8_t* q, const float2 (&t)[NV][
     const int c = c0 + v * stride;
     if (c < cols)
       *reinterpret_cast<uint2*>(q + c) =
-          make_uint2(codes4<FORMAT>(t[v][0], t[v][1], mul), codes4<FORMAT>(t[v][2], t[v][3], mul));
+          make_uint2(codes4<FORMAT>(t[v][0], t[v][1], mul, nz), codes4<FORMAT>(t[v][2], t[v][3], mul, nz));
   }
 }
 template <int NV>
 __device__ __forceinline__ void store_octs(uint8_t* q, const float2 (&t)[NV][4], int c0, int stride, int cols,
-                                           float top, int format) {
+                                           float top, int format, float nz) {
   if (!q8_finite(top)) {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
       if (c0 + v * stride < cols) *reinterpret_cast<uint2*>(q + c0 + v * stride) = make_uint2(0u, 0u);
   } else if (format == PRM_Q8_INT8) {
-    store_octs_as<NV, PRM_Q8_INT8>(q, t, c0, stride, cols, top);
+    store_octs_as<NV, PRM_Q8_INT8>(q, t, c0, stride, cols, top, nz);
   } else {
-    store_octs_as<NV, PRM_Q8_E4M3>(q, t, c0, stride, cols, top);
+    store_octs_as<NV, PRM_Q8_E4M3>(q, t, c0, stride, cols, top, nz);
   }
 }
 
@@ -269,7 +269,7 @@ __device__ __forceinline__ void load_factors(const void* f, int fp32, int first,
 // octs meet in `stage`, NV * TPR + 1 words of shared memory.
 template <int NV, int TPR>
 __device__ __forceinline__ void store_octs_shifted(uint64_t* stage, uint8_t* q, const float2 (&t)[NV][4], int o0,
-                                                   int shift, int cols, float top, int format) {
+                                                   int shift, int cols, float top, int format, float nz) {
   const bool finite = q8_finite(top);
   const float f = q8_mul(top, q8_limit(format));
   const float2 mul = make_float2(f, f);
@@ -278,8 +278,8 @@ __device__ __forceinline__ void store_octs_shifted(uint64_t* stage, uint8_t* q, 
   for (int v = 0; v < NV; ++v) {
     uint2 w = make_uint2(0u, 0u);
     if (finite)
-      w = format == PRM_Q8_INT8 ? make_uint2(codes4<PRM_Q8_INT8>(t[v][0], t[v][1], mul), codes4<PRM_Q8_INT8>(t[v][2], t[v][3], mul))
-                                : make_uint2(codes4<PRM_Q8_E4M3>(t[v][0], t[v][1], mul), codes4<PRM_Q8_E4M3>(t[v][2], t[v][3], mul));
+      w = format == PRM_Q8_INT8 ? make_uint2(codes4<PRM_Q8_INT8>(t[v][0], t[v][1], mul, nz), codes4<PRM_Q8_INT8>(t[v][2], t[v][3], mul, nz))
+                                : make_uint2(codes4<PRM_Q8_E4M3>(t[v][0], t[v][1], mul, nz), codes4<PRM_Q8_E4M3>(t[v][2], t[v][3], mul, nz));
     c[v] = (uint64_t)w.x | ((uint64_t)w.y << 32);
   }
   if (shift) {                             // alike for all threads of the row

@@ -32,6 +32,7 @@ struct NormArgs {
   int64_t rows, ld_x, ld_r, ld_h, ld_q;
   int cols, weight_fp32, format;
   float eps;
+  float minus_zero = -0.f;   // see int8_bits
 };
 
 __device__ __forceinline__ float inv_rms(float sum, int cols, float eps) { return 1.f / sqrtf(sum / (float)cols + eps); }
@@ -103,7 +104,7 @@ __global__ void __launch_bounds__(TPR <= 32 ? 256 : TPR) rmsnorm_q8_kernel(const
   }
   float sum = sum2.x + sum2.y;
   block_sum_top<TPR>(sum, top, red);
-  store_octs<NV>(a.q + row * a.ld_q, t, c0, TPR * 8, cols, top, a.format);
+  store_octs<NV>(a.q + row * a.ld_q, t, c0, TPR * 8, cols, top, a.format, a.minus_zero);
   if (c0 == 0 && cols) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
 }
 
@@ -155,7 +156,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_shifted_kern
   }
   float sum = sum2.x + sum2.y;
   block_sum_top<TPR>(sum, top, red);
-  store_octs_shifted<NV, TPR>(stage[threadIdx.x / TPR], a.q + row * a.ld_q, t, o0, shift, a.cols, top, a.format);
+  store_octs_shifted<NV, TPR>(stage[threadIdx.x / TPR], a.q + row * a.ld_q, t, o0, shift, a.cols, top, a.format, a.minus_zero);
   if (o0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
 }
 

@@ -33,6 +33,7 @@ struct QuantArgs {
   int64_t rows, ld_x, ld_qr, ld_qc;
   int cols, format;
   int panel, panels;        // columns that a block of the streaming kernel works on; cols / panel
+  float minus_zero = -0.f;  // see int8_bits
 };
 
 // x * f for one oct (f: eight factors from c on, or null; 16-byte loads where they are aligned).
@@ -79,7 +80,7 @@ __global__ void __launch_bounds__(TPR <= 32 ? 256 : TPR) quantize_rows_kernel(co
     }
   }
   block_sum_top<TPR>(none, top, red);
-  store_octs<NV>(a.q_rows + row * a.ld_qr, t, c0, TPR * 8, cols, top, a.format);
+  store_octs<NV>(a.q_rows + row * a.ld_qr, t, c0, TPR * 8, cols, top, a.format, a.minus_zero);
   if (c0 == 0 && cols) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
 }
 
@@ -116,7 +117,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) quantize_rows_shifted_k
     for (int e = 0; e < 4; ++e) top = max_abs(top, t[v][e]);
   }
   block_sum_top<TPR>(none, top, red);
-  store_octs_shifted<NV, TPR>(stage[threadIdx.x / TPR], a.q_rows + row * a.ld_qr, t, o0, shift, a.cols, top, a.format);
+  store_octs_shifted<NV, TPR>(stage[threadIdx.x / TPR], a.q_rows + row * a.ld_qr, t, o0, shift, a.cols, top, a.format, a.minus_zero);
   if (o0 == 0) a.scale_rows[row] = q8_scale(top, q8_limit(a.format));
 }
 
@@ -162,13 +163,13 @@ __global__ void __launch_bounds__(kColThreads) column_top_kernel(const QuantArgs
 
 // Eight codes, a factor for each.
 template <int FORMAT>
-__device__ __forceinline__ uint2 column_codes(const float2 (&t)[4], const float2 (&mul)[4]) {
+__device__ __forceinline__ uint2 column_codes(const float2 (&t)[4], const float2 (&mul)[4], float nz) {
   uint32_t w[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const float2 a = t[2 * k], b = t[2 * k + 1], f = mul[2 * k], g = mul[2 * k + 1];
     if constexpr (FORMAT == PRM_Q8_INT8) {
-      const float2 x = int8_bits(a, f), y = int8_bits(b, g);
+      const float2 x = int8_bits(a, f, nz), y = int8_bits(b, g, nz);
       w[k] = __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040),
                          __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
     } else {
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(kColThreads) quantize_cols_kernel(const QuantA
 // A thread's share of one row of codes by column.
 template <typename IO, int NV, int FORMAT>
 __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], const float2 (&mul)[NV][4], float fr,
-                                         bool odd, int c0, int step, int cols) {
+                                         bool odd, int c0, int step, int cols, float nz) {
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = c0 + v * step;
@@ -208,7 +209,7 @@ __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], con
 #pragma unroll
       for (int e = 0; e < 4; ++e) t[e] = mul2(t[e], make_float2(fr, fr));
       if (!odd) {
-        *reinterpret_cast<uint2*>(q + c) = column_codes<FORMAT>(t, mul[v]);
+        *reinterpret_cast<uint2*>(q + c) = column_codes<FORMAT>(t, mul[v], nz);
       } else {
         float2 m[4];
 #pragma unroll
@@ -217,7 +218,7 @@ __device__ __forceinline__ void back_row(uint8_t* q, const Oct<IO> (&x)[NV], con
           if (isnan(m[e].x)) t[e].x = m[e].x = 0.f;
           if (isnan(m[e].y)) t[e].y = m[e].y = 0.f;
         }
-        *reinterpret_cast<uint2*>(q + c) = column_codes<FORMAT>(t, m);
+        *reinterpret_cast<uint2*>(q + c) = column_codes<FORMAT>(t, m, nz);
       }
     }
   }
@@ -326,8 +327,8 @@ __global__ void __launch_bounds__(kPanelThreads) quantize_panel_kernel(const Qua
       const int64_t r = first + (turn * kPanelRows + k) * step;
       if (r < a.rows) {
         const Oct<IO> one[1] = {v[k]};
-        if (a.format == PRM_Q8_INT8) back_row<IO, 1, PRM_Q8_INT8>(q + r * a.ld_qc, one, mul, f[k], odd, 0, 0, cols);
-        else back_row<IO, 1, PRM_Q8_E4M3>(q + r * a.ld_qc, one, mul, f[k], odd, 0, 0, cols);
+        if (a.format == PRM_Q8_INT8) back_row<IO, 1, PRM_Q8_INT8>(q + r * a.ld_qc, one, mul, f[k], odd, 0, 0, cols, a.minus_zero);
+        else back_row<IO, 1, PRM_Q8_E4M3>(q + r * a.ld_qc, one, mul, f[k], odd, 0, 0, cols, a.minus_zero);
       }
     }
     if (turn == 0) break;
@@ -442,7 +443,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           if (r < h) {
-            store_octs<NV>(a.q_rows + (row + r) * a.ld_qr, t[r], c0, kStep, cols, top[r], a.format);
+            store_octs<NV>(a.q_rows + (row + r) * a.ld_qr, t[r], c0, kStep, cols, top[r], a.format, a.minus_zero);
             if (c0 == 0) a.scale_rows[row + r] = q8_scale(top[r], q8_limit(a.format));
           }
         }
@@ -553,8 +554,8 @@ __global__ void __launch_bounds__(kRingThreads, 1) quantize_stream_kernel(const 
     for (int r = 0; r < R; ++r) {
       if (r < h) {
         uint8_t* q = a.q_cols + (row + r) * a.ld_qc + cbase;
-        if (a.format == PRM_Q8_INT8) back_row<IO, NV, PRM_Q8_INT8>(q, x[r], mul, fr[r], odd, c0, kStep, cols);
-        else back_row<IO, NV, PRM_Q8_E4M3>(q, x[r], mul, fr[r], odd, c0, kStep, cols);
+        if (a.format == PRM_Q8_INT8) back_row<IO, NV, PRM_Q8_INT8>(q, x[r], mul, fr[r], odd, c0, kStep, cols, a.minus_zero);
+        else back_row<IO, NV, PRM_Q8_E4M3>(q, x[r], mul, fr[r], odd, c0, kStep, cols, a.minus_zero);
       }
     }
   }
