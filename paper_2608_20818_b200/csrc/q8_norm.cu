@@ -316,6 +316,10 @@ __device__ __forceinline__ void grad_weight(const NormGradArgs& a, int rows_per_
   else grad_weight_columns<THREADS, 32>(a, lines);
 }
 
+// s^3 mean(g h), s last thrice: s^3 alone leaves fp32's range where the row's root mean square is below
+// 1e-13 or above 1e13, mean(g h) s does not.
+__device__ __forceinline__ float grad_pull(float s, float gh, int cols) { return s * (s * (s * (gh / (float)cols))); }
+
 // The two sums of a row over one oct.
 __device__ __forceinline__ void grad_sums(const float2 (&gy)[4], const float2 (&h)[4], const float2 (&w)[4],
                                           float2& ss, float2& gh) {
@@ -426,7 +430,7 @@ __global__ void __launch_bounds__(256, group_blocks<IO>(NV)) rmsnorm_q8_grad_ker
     float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
     group_sum2<TPR>(ss, gh, red[turn][TPR > 32 ? group : 0], group);
     turn ^= 1;
-    const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
+    const float s = inv_rms(ss, a.cols, a.eps), k = grad_pull(s, gh, a.cols);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = c0 + v * TPR * 8;
@@ -503,7 +507,7 @@ __global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_wid
     }
     float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
     block_sum2<TPR>(ss, gh, red[turn]);
-    const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
+    const float s = inv_rms(ss, a.cols, a.eps), k = grad_pull(s, gh, a.cols);
     IO* gxp = reinterpret_cast<IO*>(a.gx) + row * a.ld_gx;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -582,7 +586,7 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
 #pragma unroll
       for (int r = 0; r < kR; ++r) {
         if (r < high) {
-          const float s = inv_rms(ss[r], a.cols, a.eps), k = s * s * s * (gh[r] / (float)a.cols);
+          const float s = inv_rms(ss[r], a.cols, a.eps), k = grad_pull(s, gh[r], a.cols);
           IO* gxp = reinterpret_cast<IO*>(a.gx) + (row + r) * a.ld_gx;
 #pragma unroll
           for (int v = 0; v < kNV; ++v) {
@@ -665,7 +669,7 @@ __global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_shi
     }
     float ss = ss2.x + ss2.y, gh = gh2.x + gh2.y;
     block_sum2<TPR>(ss, gh, red[turn]);
-    const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
+    const float s = inv_rms(ss, a.cols, a.eps), k = grad_pull(s, gh, a.cols);
     const float2 s2 = make_float2(s, s), nk = make_float2(-k, -k);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -721,7 +725,7 @@ __global__ void __launch_bounds__(THREADS, grad_blocks(THREADS)) rmsnorm_q8_grad
       gh += to_f32(gyp[c]) * load1(a.weight, a.weight_fp32, c) * h;
     }
     block_sum2<THREADS>(ss, gh, red[turn]);
-    const float s = inv_rms(ss, a.cols, a.eps), k = s * s * s * (gh / (float)a.cols);
+    const float s = inv_rms(ss, a.cols, a.eps), k = grad_pull(s, gh, a.cols);
 #pragma unroll 4
     for (int c = threadIdx.x; c < a.cols; c += THREADS) {
       const float h = to_f32(hp[c]), gy = to_f32(gyp[c]);

@@ -173,3 +173,15 @@ def test_errors_of_other_calls_are_not_theirs():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     run = subprocess.run([sys.executable, "-c", STALE_ERROR], cwd=root, capture_output=True, text=True, timeout=300)
     assert run.stdout.strip() == "done", run.stderr[-2000:]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [torch.bfloat16, torch.float32])
+# each of the gradient's kernels: groups, wide, streamed, rows that start anywhere, single elements
+@pytest.mark.parametrize("rows,cols", [(6, 64), (5, 2048), (4, 6000), (400, 6000), (7, 515), (3, 16384)])
+def test_norm_backward_of_large_and_small_rows(rows, cols, io):
+    """Rows of root mean squares from 1e-15 to 1e15: the powers of s stay in range where the gradient does."""
+    size = torch.tensor([1e-15, 1e15, 1.0, 1e-13, 1e13], device="cuda")[torch.arange(rows, device="cuda") % 5, None]
+    h, gy, gh = ((randn(rows + cols + k, rows, cols) * s).to(io) for k, s in enumerate((size, 1, 0.01 / size)))
+    check_norm_backward(gy, h, (1 + 0.2 * randn(cols, cols)).to(io), 0.0, gh)
+    check_norm_backward(gy, h, (1 + 0.2 * randn(cols, cols)).to(io), 0.0, None)
