@@ -476,13 +476,16 @@ PRM_API double prm_shape_scale(int mode, int64_t rows, int64_t cols);
  *
  * prm_rmsnorm_q8   per row: h = x + residual, rounded to the stream's type and stored (residual
  *   NULL: h = x, nothing stored, h_out ignored); t = h * weight; codes of t by row;
- *   scale = T / limit / sqrt(mean(h^2) + eps).  q_out * scale_out is the norm's output.  rows may
- *   be 0.
+ *   scale = T / limit / sqrt(mean(h^2) + eps), 0 where T counts as zero.  q_out * scale_out is the
+ *   norm's output.  The squares are added in fp32: a row with magnitudes from about 1e19 on has an
+ *   infinite sum and the scale 0; with eps = 0 one that lies below 2e-23 throughout has the sum 0 and
+ *   an infinite scale.  rows may be 0.
  * prm_rmsnorm_q8_backward   the norm's gradient, the rounding to 8 bits taken as the identity.
  *   With s = 1 / sqrt(mean(h^2) + eps) and g = grad_y * weight:
  *     grad_x = s g - h s^3 mean(g h) + grad_h   (the gradient of x and of residual alike;
  *                                                grad_h, what reaches h from elsewhere, may be NULL)
  *     grad_weight[j] = sum over rows of grad_y h s   (in the weight's type, added in a fixed order)
+ *   A zero row with eps = 0 has no gradient: its grad_x and all of grad_weight are NaN.
  *   scratch: device, 16-byte aligned, prm_rmsnorm_q8_scratch_bytes(rows, cols) bytes.  With rows = 0
  *   grad_weight is set to zero.
  * prm_quantize_q8   codes of a matrix by rows (of x * fold_cols, scale_rows[rows]), by columns (of

@@ -37,6 +37,12 @@ struct NormArgs {
 
 __device__ __forceinline__ float inv_rms(float sum, int cols, float eps) { return 1.f / sqrtf(sum / (float)cols + eps); }
 
+// A row that counts as zero has the scale 0 with eps = 0 too.
+__device__ __forceinline__ float norm_scale(float top, float sum, const NormArgs& a) {
+  const float u = q8_scale(top, q8_limit(a.format));
+  return u == 0.f ? 0.f : u * inv_rms(sum, a.cols, a.eps);
+}
+
 template <typename T>
 __device__ __forceinline__ void load_oct(const T* p, float2 (&v)[4]) {
   Oct<T> o;
@@ -105,7 +111,7 @@ __global__ void __launch_bounds__(TPR <= 32 ? 256 : TPR) rmsnorm_q8_kernel(const
   float sum = sum2.x + sum2.y;
   block_sum_top<TPR>(sum, top, red);
   store_octs<NV>(a.q + row * a.ld_q, t, c0, TPR * 8, cols, top, a.format, a.minus_zero);
-  if (c0 == 0 && cols) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
+  if (c0 == 0 && cols) a.scale[row] = norm_scale(top, sum, a);
 }
 
 // Rows that start anywhere (odd widths), or too wide for the kernels above: as rmsnorm_q8_kernel, on
@@ -157,7 +163,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) rmsnorm_q8_shifted_kern
   float sum = sum2.x + sum2.y;
   block_sum_top<TPR>(sum, top, red);
   store_octs_shifted<NV, TPR>(stage[threadIdx.x / TPR], a.q + row * a.ld_q, t, o0, shift, a.cols, top, a.format, a.minus_zero);
-  if (o0 == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
+  if (o0 == 0) a.scale[row] = norm_scale(top, sum, a);
 }
 
 // Any alignment, any length: two passes over the row, the second of which finds it in cache.
@@ -191,7 +197,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_q8_single_kernel(const NormAr
     const float t = __fmul_rn(to_f32(src[c]), load1(a.weight, a.weight_fp32, c));
     q[c] = finite ? code1(t, mul, a.format) : 0;
   }
-  if (threadIdx.x == 0) a.scale[row] = q8_scale(top, q8_limit(a.format)) * inv_rms(sum, a.cols, a.eps);
+  if (threadIdx.x == 0) a.scale[row] = norm_scale(top, sum, a);
 }
 
 template <typename IO, typename WT, int NV, int TPR>

@@ -185,3 +185,15 @@ def test_norm_backward_of_large_and_small_rows(rows, cols, io):
     h, gy, gh = ((randn(rows + cols + k, rows, cols) * s).to(io) for k, s in enumerate((size, 1, 0.01 / size)))
     check_norm_backward(gy, h, (1 + 0.2 * randn(cols, cols)).to(io), 0.0, gh)
     check_norm_backward(gy, h, (1 + 0.2 * randn(cols, cols)).to(io), 0.0, None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("cols", [64, 515, 2048, 40001])
+def test_zero_rows_without_eps(cols, fmt):
+    x = randn(cols, 4, cols)
+    x[1] = 0
+    x[2] = 2.0 ** -110
+    for r in (None, torch.zeros_like(x)):
+        q, scale, _ = B.prm_rmsnorm_q8(x, torch.ones(cols, device="cuda"), 0.0, residual=r, format=fmt)
+        assert not q[1:3].float().any() and not scale[1:3].any() and torch.all(scale[[0, 3]] > 0)
