@@ -21,6 +21,7 @@
 #include <type_traits>
 
 #include "q8_matmul.cuh"
+#include "q8_plan.h"
 
 namespace prm {
 namespace {
@@ -348,6 +349,16 @@ int matmul_split(const MatmulProblem& p, const Plan& plan) {
 }
 
 }  // namespace
+
+int q8_sms() {
+  static int at[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  int sms = 0;
+  if (!at[dev] && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
+    at[dev] = std::min(sms, kRingBlocks);
+  return at[dev];
+}
 
 // The status word's address on the current device.
 int* q8_status_word() {

@@ -749,7 +749,8 @@ template <typename IO, typename WT, int W, bool GH>
 int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
   constexpr int kGroups = kRingWarps / W, kR = kRingRows<IO>;
   static PerDeviceOnce once;
-  return launch_ring(rmsnorm_q8_grad_stream_kernel<IO, WT, W, GH>, once, ring_blocks(a.rows, kR, kGroups),
+  return launch_ring(rmsnorm_q8_grad_stream_kernel<IO, WT, W, GH>, once,
+                     (unsigned)ring_grid(a.rows, kR, kGroups, 1, q8_sms()),
                      (size_t)a.cols * sizeof(IO) * (GH ? 3 : 2) * kR * kGroups, 0, (size_t)kGroups * a.cols * 4, true,
                      stream, a);
 }
@@ -759,13 +760,15 @@ int launch_grad_grid(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, 
                                              stream));
 }
 int launch_grad(void (*kernel)(NormGradArgs), const NormGradArgs& a, int threads, int nv, cudaStream_t stream) {
-  return launch_grad_grid(kernel, a, threads, grad_grid(a.rows, a.cols, grad_blocks(threads, nv)), stream);
+  return launch_grad_grid(kernel, a, threads, grad_grid(a.rows, a.cols, grad_blocks(threads, nv), q8_sms()), stream);
 }
 template <typename IO, typename WT, int NV, int TPR>
 int launch_grad_groups(const NormGradArgs& a, cudaStream_t stream) {
   constexpr int kRows = 256 / TPR;
-  const int64_t blocks = std::min<int64_t>((a.rows + kRows - 1) / kRows, group_blocks<IO>(NV) * kRingBlocks);
-  return launch_grad_grid(rmsnorm_q8_grad_kernel<IO, WT, NV, TPR>, a, 256, grad_grid_for_columns(blocks, a.cols), stream);
+  const int sms = q8_sms();
+  const int64_t blocks = std::min<int64_t>((a.rows + kRows - 1) / kRows, group_blocks<IO>(NV) * sms);
+  return launch_grad_grid(rmsnorm_q8_grad_kernel<IO, WT, NV, TPR>, a, 256, grad_grid_for_columns(blocks, a.cols, sms),
+                          stream);
 }
 
 template <typename IO, typename WT>
@@ -791,7 +794,7 @@ template <typename IO>
 int run_grad_single(const NormGradArgs& a, bool alike, cudaStream_t stream) {
   const GradForm form = alike ? grad_shifted_form(a.cols) : GradForm{0, 0};
   auto go = [&](auto kernel) {
-    return launch_grad_grid(kernel, a, form.threads, grad_shifted_grid(a.rows, a.cols, form), stream);
+    return launch_grad_grid(kernel, a, form.threads, grad_shifted_grid(a.rows, a.cols, form, q8_sms()), stream);
   };
   switch (form.threads) {
     case 32: return go(rmsnorm_q8_grad_shifted_kernel<IO, 1, 32>);

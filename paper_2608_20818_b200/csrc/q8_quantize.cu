@@ -566,9 +566,8 @@ template <typename IO, int W, int NV, int R, bool ROWS>
 int launch_stream(const QuantArgs& a, cudaStream_t stream) {
   constexpr int kGroups = kRingWarps / W;
   static PerDeviceOnce once;
-  // as many blocks as there are groups' worth of rows, a whole number of them for each panel
-  const unsigned per_panel = std::min<unsigned>(kRingBlocks / a.panels, ring_blocks(a.rows, R, kGroups));
-  return launch_ring(quantize_stream_kernel<IO, W, NV, R, ROWS>, once, per_panel * (unsigned)a.panels,
+  return launch_ring(quantize_stream_kernel<IO, W, NV, R, ROWS>, once,
+                     (unsigned)ring_grid(a.rows, R, kGroups, a.panels, q8_sms()),
                      (size_t)a.panel * sizeof(IO) * R * kGroups, (size_t)a.panel * (ROWS && a.fold_cols ? 8 : 4), 0, true, stream, a);
 }
 
@@ -578,8 +577,8 @@ constexpr int kWidest = sizeof(IO) == 2 ? 16384 : 8192;
 
 template <typename IO, bool ROWS>
 int run_stream(QuantArgs a, cudaStream_t stream) {
-  a.panels = ROWS ? 1 : (a.cols + 8191) / 8192;
-  a.panel = (a.cols + 8 * a.panels - 1) / (8 * a.panels) * 8;
+  a.panels = ROWS ? 1 : stream_panels(a.cols);
+  a.panel = stream_panel(a.cols, a.panels);
   if constexpr (sizeof(IO) == 2) {
     // two rows of two octs up to 4096 columns (8192 x 2048: 20.7 us against 24.6 with one row of four),
     // one row of four beyond (4096 x 5120 both ways: 36.9 us against 40.9)
@@ -708,7 +707,7 @@ extern "C" int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_
   if (panels) {
     code = io_fp32 ? run_panels<float>(a, stream) : run_panels<__nv_bfloat16>(a, stream);
     q_cols = nullptr;
-  } else if (q_cols && octs_c && cols >= 256 && cols <= 32 * 8192) {
+  } else if (q_cols && octs_c && stream_takes(cols, q8_sms())) {
     const bool joint = q_rows && octs_r && cols <= (io_fp32 ? kWidest<float> : kWidest<__nv_bfloat16>);
     if (joint) code = io_fp32 ? run_stream<float, true>(a, stream) : run_stream<__nv_bfloat16, true>(a, stream);
     else code = io_fp32 ? run_stream<float, false>(a, stream) : run_stream<__nv_bfloat16, false>(a, stream);

@@ -310,6 +310,8 @@ struct RowRing {
 
 // The status word that prm_q8_status reads, on the current device (null if it has none).
 int* q8_status_word();
+// SMs of the current device that persistent and cooperative launches use (0: an error).
+int q8_sms();
 
 // Calls f with the number of warps to a row of `cols` elements, NV octs per thread.
 template <int NV, typename F>
@@ -346,10 +348,6 @@ int launch_ring(void (*kernel)(A, int, int*), PerDeviceOnce& once, unsigned bloc
     e = launch_after(kernel, blocks, kRingThreads, smem, stream, 0, a, stages, status);
   }
   return q8_code(e);
-}
-inline unsigned ring_blocks(int64_t rows, int rows_per_set, int groups) {
-  const int64_t sets = (rows + rows_per_set - 1) / rows_per_set;
-  return (unsigned)std::min<int64_t>(kRingBlocks, (sets + groups - 1) / groups);
 }
 
 }  // namespace prm
