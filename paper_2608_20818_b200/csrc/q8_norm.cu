@@ -276,9 +276,10 @@ __host__ __device__ constexpr int group_blocks(int nv) {
   return (nv == 1 ? 4 : 2) * 2 / (int)sizeof(IO);
 }
 
-// Asks the L2 for the line of p (one lane in eight: 128 bytes of 16-byte pieces).
-__device__ __forceinline__ void prefetch_line(const void* p) {
-  if ((threadIdx.x & 7) == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+// Asks the L2 for the line of p, a thread's oct: one lane for 128 bytes.
+template <typename IO>
+__device__ __forceinline__ void prefetch_line(const IO* p) {
+  if (threadIdx.x % (16 / sizeof(IO)) == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
 }
 
 // grad_w from the blocks' lines of partial sums: WIDTH columns per block and turn, 32 / WIDTH lines per
