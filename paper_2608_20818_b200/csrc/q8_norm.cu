@@ -541,12 +541,12 @@ __global__ void __launch_bounds__(TPR, grad_blocks(TPR, NV)) rmsnorm_q8_grad_wid
   grad_weight<TPR>(a);
 }
 
-// Large matrices: rows streamed through a ring.  The groups' shares of grad_w meet in the ring's
-// memory at the end, so that a block leaves one line of partial sums.
-template <typename IO, typename WT, int W, bool GH>
+// Large matrices: rows streamed through a ring, all 16 warps to a row (narrower rows go by groups of
+// threads, run_grad), so that a thread's share of grad_w is the block's.
+template <typename IO, typename WT, bool GH>
 __global__ void __launch_bounds__(kRingThreads, 1)
 rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
-  constexpr int kArr = GH ? 3 : 2, kNV = 2, kR = kRingRows<IO>, kStep = W * 32 * 8, kGroups = kRingWarps / W;
+  constexpr int kArr = GH ? 3 : 2, kNV = 2, kR = kRingRows<IO>, W = kRingWarps, kStep = W * 32 * 8;
   const int c0 = (threadIdx.x % (W * 32)) * 8;
   const void* const src[3] = {a.gy, a.h, a.gh};
   const int64_t ld[3] = {a.ld_gy, a.ld_h, a.ld_gh};
@@ -613,23 +613,14 @@ rmsnorm_q8_grad_stream_kernel(const NormGradArgs a, int stages, int* status) {
     ring.advance();
   }
   ring.finish();
-  __syncthreads();                        // every group's copies have been consumed
-  float* sums = reinterpret_cast<float*>(ring_memory());
 #pragma unroll
   for (int v = 0; v < kNV; ++v) {
     const int c = c0 + v * kStep;
     if (!ring.producer && c < a.cols) {
       Oct<float> o;
       o.set(gw[v]);
-      o.store(sums + (size_t)ring.group * a.cols + c);
+      o.store(a.part + (int64_t)blockIdx.x * a.cols + c);
     }
-  }
-  __syncthreads();
-  for (int c = threadIdx.x; c < a.cols; c += kRingThreads) {
-    float sum = 0.f;
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) sum += sums[(size_t)g * a.cols + c];
-    a.part[(int64_t)blockIdx.x * a.cols + c] = sum;
   }
   grad_weight<kRingThreads>(a);
 }
@@ -746,14 +737,12 @@ __global__ void __launch_bounds__(THREADS, grad_blocks(THREADS)) rmsnorm_q8_grad
   grad_weight<THREADS>(a);
 }
 
-template <typename IO, typename WT, int W, bool GH>
+template <typename IO, typename WT, bool GH>
 int launch_grad_stream(const NormGradArgs& a, cudaStream_t stream) {
-  constexpr int kGroups = kRingWarps / W, kR = kRingRows<IO>;
+  constexpr int kR = kRingRows<IO>;
   static PerDeviceOnce once;
-  return launch_ring(rmsnorm_q8_grad_stream_kernel<IO, WT, W, GH>, once,
-                     (unsigned)ring_grid(a.rows, kR, kGroups, 1, q8_sms()),
-                     (size_t)a.cols * sizeof(IO) * (GH ? 3 : 2) * kR * kGroups, 0, (size_t)kGroups * a.cols * 4, true,
-                     stream, a);
+  return launch_ring(rmsnorm_q8_grad_stream_kernel<IO, WT, GH>, once, (unsigned)ring_grid(a.rows, kR, 1, 1, q8_sms()),
+                     (size_t)a.cols * sizeof(IO) * (GH ? 3 : 2) * kR, 0, stream, a);
 }
 int launch_grad_grid(void (*kernel)(NormGradArgs), NormGradArgs a, int threads, int64_t grid, cudaStream_t stream) {
   void* args[1] = {&a};
@@ -786,8 +775,7 @@ int run_grad(const NormGradArgs& a, cudaStream_t stream) {
   // a row or two per block (100 x 8192: 10.3 us).  Up to 4096 columns the ring is no faster than groups
   // (8192 x 4096: 49.0 us against 49.6) or slower (2048 x 2048: 13.3 against 10.4).
   if (a.rows * c < (int64_t)1 << 21) return launch_grad(rmsnorm_q8_grad_wide_kernel<IO, WT, 2, 512>, a, 512, 2, stream);
-  return a.gh ? launch_grad_stream<IO, WT, kRingWarps, true>(a, stream)
-              : launch_grad_stream<IO, WT, kRingWarps, false>(a, stream);
+  return a.gh ? launch_grad_stream<IO, WT, true>(a, stream) : launch_grad_stream<IO, WT, false>(a, stream);
 }
 
 // `alike`: the matrices' rows start alike.

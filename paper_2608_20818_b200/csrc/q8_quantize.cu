@@ -568,7 +568,7 @@ int launch_stream(const QuantArgs& a, cudaStream_t stream) {
   static PerDeviceOnce once;
   return launch_ring(quantize_stream_kernel<IO, W, NV, R, ROWS>, once,
                      (unsigned)ring_grid(a.rows, R, kGroups, a.panels, q8_sms()),
-                     (size_t)a.panel * sizeof(IO) * R * kGroups, (size_t)a.panel * (ROWS && a.fold_cols ? 8 : 4), 0, true, stream, a);
+                     (size_t)a.panel * sizeof(IO) * R * kGroups, (size_t)a.panel * (ROWS && a.fold_cols ? 8 : 4), stream, a);
 }
 
 // Widest row that one group holds with codes by row: 16 warps, 32 elements (bf16) or 16 per thread.
@@ -585,7 +585,7 @@ int run_stream(QuantArgs a, cudaStream_t stream) {
     if (ROWS && a.panel > 8192) return launch_stream<IO, 16, 4, 1, ROWS>(a, stream);
     if (a.panel > 4096) return launch_stream<IO, 8, 4, 1, ROWS>(a, stream);
   }
-  return with_ring_warps<2>(
+  return with_ring_warps(
       a.panel, [&](auto w) { return launch_stream<IO, decltype(w)::value, 2, kRingRows<IO>, ROWS>(a, stream); });
 }
 

@@ -313,22 +313,21 @@ int* q8_status_word();
 // SMs of the current device that persistent and cooperative launches use (0: an error).
 int q8_sms();
 
-// Calls f with the number of warps to a row of `cols` elements, NV octs per thread.
-template <int NV, typename F>
+// Calls f with the number of warps to a row of up to 8192 elements, two octs per thread.
+template <typename F>
 int with_ring_warps(int cols, F f) {
-  if (cols <= 256 * NV) return f(std::integral_constant<int, 1>());
-  if (cols <= 512 * NV) return f(std::integral_constant<int, 2>());
-  if (cols <= 1024 * NV) return f(std::integral_constant<int, 4>());
-  if (cols <= 2048 * NV) return f(std::integral_constant<int, 8>());
-  if constexpr (NV <= 2) return f(std::integral_constant<int, 16>());
-  return PRM_ERR_SHAPE;
+  if (cols <= 512) return f(std::integral_constant<int, 1>());
+  if (cols <= 1024) return f(std::integral_constant<int, 2>());
+  if (cols <= 2048) return f(std::integral_constant<int, 4>());
+  if (cols <= 4096) return f(std::integral_constant<int, 8>());
+  return f(std::integral_constant<int, 16>());
 }
 
-// Launches kernel(a, stages, status): `set_bytes` of ring per stage and CTA, then `tail` bytes that the
-// kernel uses beside the ring and `after` bytes that it wants of all of it after the last set.
+// Cooperative launch of kernel(a, stages, status): `set_bytes` of ring per stage and CTA, then `tail` bytes
+// that the kernel uses beside the ring.
 template <typename A>
 int launch_ring(void (*kernel)(A, int, int*), PerDeviceOnce& once, unsigned blocks, size_t set_bytes, size_t tail,
-                size_t after, bool cooperative, cudaStream_t stream, A a) {
+                cudaStream_t stream, A a) {
   int dev;
   if (once.need(&dev)) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
@@ -336,18 +335,12 @@ int launch_ring(void (*kernel)(A, int, int*), PerDeviceOnce& once, unsigned bloc
     once.mark(dev);
   }
   int* status = q8_status_word();
-  if (tail > kRingBytes || after > kRingBytes) return PRM_ERR_CUDA;
+  if (tail > kRingBytes) return PRM_ERR_CUDA;
   int stages = (int)std::min<size_t>(kRingStages, (kRingBytes - tail) / set_bytes);
   if (!status || stages < 1) return PRM_ERR_CUDA;
-  const size_t smem = std::max(after, set_bytes * stages + tail);
-  cudaError_t e;
-  if (cooperative) {
-    void* args[3] = {&a, &stages, &status};
-    e = cudaLaunchCooperativeKernel((const void*)kernel, dim3(blocks), dim3(kRingThreads), args, smem, stream);
-  } else {
-    e = launch_after(kernel, blocks, kRingThreads, smem, stream, 0, a, stages, status);
-  }
-  return q8_code(e);
+  void* args[3] = {&a, &stages, &status};
+  return q8_code(cudaLaunchCooperativeKernel((const void*)kernel, dim3(blocks), dim3(kRingThreads), args,
+                                             set_bytes * stages + tail, stream));
 }
 
 }  // namespace prm
