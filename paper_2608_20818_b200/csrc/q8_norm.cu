@@ -11,8 +11,9 @@
 //
 // Both are bound by HBM (7 and 8 bytes per element of a bf16 stream with its residual), so a row is read
 // once and stays in registers, in octs (8 elements), between its sums and its output.  Measured on 8192
-// x 4096 in bf16 with residual: norm 38.2 us, 6.1 TB/s; gradient 52.7 us, 5.1 TB/s (it also waits for
+// x 4096 in bf16 with residual: norm 38.2 us, 6.1 TB/s; gradient 52.3 us, 5.1 TB/s (it also waits for
 // the whole grid to add grad_w).  For one token each takes 2 to 5 us, the launch and one trip to memory.
+// (Times here and below are the device's, of calls that follow one another on inputs beyond the L2.)
 // Forms: rows of aligned octs; octs aligned in memory for rows that start anywhere; the gradient of rows
 // of 4097 to 8192 streamed through shared memory; and single elements in two passes for what is left.
 #include <cooperative_groups.h>
@@ -215,8 +216,8 @@ int run_norm(const NormArgs& a, cudaStream_t stream) {
   if (c <= 128) return launch_norm<IO, WT, 1, 16>(a, stream);
   if (c <= 256) return launch_norm<IO, WT, 1, 32>(a, stream);
   if (c <= 512) return launch_norm<IO, WT, 2, 32>(a, stream);
-  // One block per row costs 1 ns each, more than a short row's bytes (16384 x 1024: 18.8 us, eight rows per
-  // block 15.4); few rows end sooner with more threads (256 x 1024: 2.1 us, a warp 2.5).
+  // One block per row costs 1 ns each, more than a short row's bytes (16384 x 1024 without residual: 18.2 us,
+  // eight rows per block 14.3); few rows end sooner with more threads (256 x 1024: 2.2 us, a warp 2.6).
   if (c <= 1024 && a.rows >= 2048) return launch_norm<IO, WT, 4, 32>(a, stream);
   if (c <= 1024) return launch_norm<IO, WT, 1, 128>(a, stream);
   if (c <= 2048) return launch_norm<IO, WT, 2, 128>(a, stream);
@@ -312,8 +313,8 @@ __device__ __forceinline__ void grad_weight_columns(const NormGradArgs& a, int l
 }
 
 // After a barrier of the whole (cooperative) grid: the fewest columns per turn (a sector at least) that
-// leave each block one turn, for a block that goes through many lines alone is slow (1000 x 1000, 444
-// lines: 32 columns 19 us, 8 columns 12), and so are several turns (8192 x 4096: 48.8 us, with 8 54.2).
+// leave each block one turn, for a block that goes through many lines alone is slow (2048 x 2048: 32
+// columns 13.2 us, 8 columns 11.7), and so are several turns (200 x 8192: 11.6 us, with 8 18.5).
 template <int THREADS>
 __device__ __forceinline__ void grad_weight(const NormGradArgs& a, int rows_per_block = 1) {
   cooperative_groups::this_grid().sync();
@@ -382,7 +383,8 @@ __device__ __forceinline__ void group_sum2(float& p, float& q, float2* red, int 
 // loads in flight while this one is summed; a thread keeps the same columns in all its rows, so its share
 // of grad_w stays in registers, and a block's groups add theirs in shared memory.  One cooperative launch:
 // the blocks' shares are added behind a grid-wide barrier, which costs less than a second launch.  Heads
-// of a query-key norm, 262144 x 128: 47 us, 5.7 TB/s (a warp per row and block of 32: 191).
+// of a query-key norm, 262144 x 128: 52.3 us, 5.1 TB/s, without grad_h 44.1 (a warp per row and block of
+// 32: 191).
 template <typename IO, typename WT, int NV, int TPR>
 __global__ void __launch_bounds__(256, group_blocks<IO>(NV)) rmsnorm_q8_grad_kernel(const NormGradArgs a) {
   constexpr int kRows = 256 / TPR;
@@ -771,9 +773,9 @@ int run_grad(const NormGradArgs& a, cudaStream_t stream) {
   if (c <= 1024) return launch_grad_groups<IO, WT, 2, 64>(a, stream);
   if (c <= 2048) return launch_grad_groups<IO, WT, 2, 128>(a, stream);
   if (c <= 4096) return launch_grad_groups<IO, WT, 2, 256>(a, stream);
-  // Streamed from these sizes on (8192 x 5120: 70 us, by groups of 512 threads 75, in fp32 111 and 238), else
-  // a row or two per block (100 x 8192: 10.3 us).  Up to 4096 columns the ring is no faster than groups
-  // (8192 x 4096: 49.0 us against 49.6) or slower (2048 x 2048: 13.3 against 10.4).
+  // Streamed from these sizes on (8192 x 5120: 72 us, a block per row 106, in fp32 113 and 154), else a row or
+  // two per block (100 x 8192: 10.4 us).  Up to 4096 columns the ring is little faster than groups (8192 x
+  // 4096: 50.9 us against 52.3) or slower (2048 x 2048: 14.8 against 11.4).
   if (a.rows * c < (int64_t)1 << 21) return launch_grad(rmsnorm_q8_grad_wide_kernel<IO, WT, 2, 512>, a, 512, 2, stream);
   return a.gh ? launch_grad_stream<IO, WT, true>(a, stream) : launch_grad_stream<IO, WT, false>(a, stream);
 }

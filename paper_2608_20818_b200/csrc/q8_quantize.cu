@@ -580,8 +580,8 @@ int run_stream(QuantArgs a, cudaStream_t stream) {
   a.panels = ROWS ? 1 : stream_panels(a.cols);
   a.panel = stream_panel(a.cols, a.panels);
   if constexpr (sizeof(IO) == 2) {
-    // two rows of two octs up to 4096 columns (8192 x 2048: 20.7 us against 24.6 with one row of four),
-    // one row of four beyond (4096 x 5120 both ways: 36.9 us against 40.9)
+    // two rows of two octs up to 4096 columns (16384 x 2048: 36.3 us against 38.4 with one row of four),
+    // one row of four beyond (4096 x 5120 both ways: 35.7 us against 41.9)
     if (ROWS && a.panel > 8192) return launch_stream<IO, 16, 4, 1, ROWS>(a, stream);
     if (a.panel > 4096) return launch_stream<IO, 8, 4, 1, ROWS>(a, stream);
   }
@@ -598,6 +598,10 @@ int launch_panels(const QuantArgs& a, cudaStream_t stream) {
                               (unsigned)((a.cols + LANES * 8 - 1) / (LANES * 8)) * blocks, kPanelThreads, 0, stream, blocks,
                               a));
 }
+// 16 octs are 256 bytes of a bf16 row, and 1024 rows in one turn of a cluster of eight blocks; more rows are
+// done sooner by 8 octs, which take twice the rows in a turn and have twice the clusters (1100 x 512: 3.8 us
+// against 5.8, 4096 x 2048: 10.6 against 15.4; 1000 x 512: 4.3 against 4.2).  Beyond 2048 columns 16 octs fill
+// the GPU with fewer, larger pieces (2048 x 4096: 10.1 us against 13.7).
 template <typename IO>
 int run_panels(const QuantArgs& a, cudaStream_t stream) {
   return a.cols <= 2048 && a.rows >= 1024 ? launch_panels<IO, 8>(a, stream) : launch_panels<IO, 16>(a, stream);
@@ -618,7 +622,7 @@ int run_rows(const QuantArgs& a, bool octs, cudaStream_t stream) {
     if (c <= 128) return launch_rows<IO, 1, 16>(a, stream);
     if (c <= 256) return launch_rows<IO, 1, 32>(a, stream);
     if (c <= 512) return launch_rows<IO, 2, 32>(a, stream);
-    if (c <= 1024) return launch_rows<IO, 4, 32>(a, stream);   // 16384 x 1024: 8.3 us, a block per row 17.5
+    if (c <= 1024) return launch_rows<IO, 4, 32>(a, stream);   // 16384 x 1024: 9.8 us, a block per row 17.7
     if (c <= 2048) return launch_rows<IO, 2, 128>(a, stream);
     if (c <= 4096) return launch_rows<IO, 2, 256>(a, stream);
     if (c <= 8192) return launch_rows<IO, 2, 512>(a, stream);
@@ -700,8 +704,8 @@ extern "C" int prm_quantize_q8(const void* x, int64_t ld_x, int64_t rows, int64_
   const bool octs_c = octs_x && ld_q_cols % 8 == 0 && ((uintptr_t)q_cols & 7) == 0;
   // Codes by column of an aligned matrix: one launch, with the codes by row in the same pass where a
   // row fits a group's registers.
-  // Up to these sizes by panels (1500 x 2048 both ways with folds: 10.0 us, streamed 14.4; 4096 x 4096 columns:
-  // 16.3 against 19.8), beyond them streamed (8192 x 8192: 57.4 against 64.5; 32768 x 512: 27.5 against 42.5).
+  // Up to these sizes by panels (1500 x 2048 both ways with folds: 10.5 us, streamed 19.2; 4096 x 4096 columns:
+  // 17.7 against 22.5), beyond them streamed (8192 x 8192: 58.8 against 67.5; 32768 x 512: 28.5 against 45.1).
   const bool panels = q_cols && octs_c && rows <= (cols < 256 ? 2048 : 8192) && rows * cols <= (int64_t)1 << 24;
   int code = PRM_OK;
   if (panels) {
