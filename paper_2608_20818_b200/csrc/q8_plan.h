@@ -43,7 +43,7 @@ inline int64_t grad_grid_for_columns(int64_t blocks, int64_t cols, int sms) {
   return std::max<int64_t>(blocks, std::min<int64_t>(sms, (cols + 31) / 32));
 }
 // A block per row and turn: two blocks per SM until they have six rows each, for a block more is a line more
-// of partial sums (512 x 2048: 7.5 us, three per SM 9.4; 5000 x 1001: 23 us, two per SM 31).
+// of partial sums (512 x 2041: 10.5 us, three per SM 12.9; 5000 x 1001: 24.5 us, two per SM 32).
 inline int64_t grad_grid(int64_t rows, int64_t cols, int per_sm, int sms) {
   const int64_t want = std::min<int64_t>(rows, std::max<int64_t>(2 * sms, (rows + 47) / 48 * 8));
   return grad_grid_for_columns(std::min<int64_t>(want, (int64_t)per_sm * sms), cols, sms);
