@@ -498,7 +498,7 @@ PRM_API double prm_shape_scale(int mode, int64_t rows, int64_t cols);
  *   Either scale may be NULL (1).  a and b 16-byte aligned with row strides that are multiples of 16
  *   (else PRM_ERR_ALIGN); m, k, n are free; m or n = 0 does nothing, k = 0 writes zeros.  int8: k at
  *   most 1047552 (PRM_ERR_SHAPE).
- * prm_q8_status    as prm_status, for the waits inside prm_matmul_q8 on the current device
+ * prm_q8_status    as prm_status, for the waits inside the four operators on the current device
  *   (synchronises it): PRM_OK, or PRM_ERR_DEVICE_TIMEOUT once after a wait that ran out.
  */
 #define PRM_Q8_INT8  0

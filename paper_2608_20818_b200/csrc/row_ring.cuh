@@ -296,9 +296,11 @@ struct RowRing {
       w[0] = f.x; w[1] = f.y;
     }
   }
-  // Copies in flight land before the CTA's memory goes (only after a wait that ran out are there any).
+  // All threads of the block, after the last set.  Copies in flight land before the CTA's memory goes: there
+  // are any only after a wait that ran out, which may be a consumer's after the producer's last copy.
   __device__ __forceinline__ void finish() const {
-    if (*(volatile int*)&b.abort_word && producer) {
+    __syncthreads();
+    if (*(volatile int*)&b.abort_word) {
       const uint64_t t0 = global_ns();
       while (global_ns() - t0 < 1000000ull) {
       }
