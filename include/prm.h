@@ -523,6 +523,79 @@ PRM_API int prm_matmul_q8(const void* a, int64_t ld_a, int a_transposed, const f
                           int format, void* out, int64_t ld_out, int out_fp32, void* cuda_stream);
 PRM_API int prm_q8_status(void);
 
+/*
+ * Operators of a training step around its matrix products: dropout, layer norm, the loss of a linear
+ * head.  (The paper has no counterpart: its matrix branch starts where a backward pass has ended.)
+ *
+ * Conventions are those of the 8-bit operators above: row strides in elements (>= 0 for inputs, at least
+ * the width for outputs), io_fp32 and weight_fp32 0 = bf16 or 1 = fp32, pointers aligned to their element,
+ * 16-byte aligned pointers and row strides and widths that are multiples of 8 fastest; work is enqueued on
+ * cuda_stream on the current device, nothing is allocated, outputs must not overlap inputs, sums and
+ * statistics are fp32 (in a fixed order: the same call gives the same bits).
+ *
+ * Dropout draws from a counter-based generator and stores no mask.  The element in row i and column j is
+ * kept where word j % 4 of Philox4x32-10 (Salmon et al., SC 2011) at the counter (j / 4, i, low and high
+ * half of s) under the key seed (low, high half) is at least p * 2^32 (rounded), s = offset + *counter
+ * (modulo 2^64).  counter is a device word (NULL: 0), read when the kernel runs, so that a captured graph
+ * draws anew at each replay if it advances it.  What is kept is multiplied by 1 / (1 - p) (rounded to
+ * fp32, the product too); what is dropped is 0, an infinity or NaN too.  0 <= p < 1.
+ *
+ * prm_dropout     out = x dropped out (+ residual, NULL: none), one rounding to the type.  With the same
+ *   p, seed and s it is its own gradient: call it on the gradient.  rows and cols may be 0.
+ * prm_layernorm   per row: h = x (dropped out if p > 0) + residual, rounded to the stream's type and stored
+ *   (neither: h = x, nothing stored, h_out ignored); mean = sum h / cols, rstd = 1 / sqrt(sum (h - mean)^2 /
+ *   cols + eps); y = (h - mean) rstd weight + bias.  weight (NULL: 1) and bias (NULL: 0) have one row for
+ *   every rows_per_group rows, ld_weight and ld_bias apart (rows_per_group >= rows: one row of each);
+ *   add_one: the weight is 1 + what is stored (adaLN).  mean_out and rstd_out, fp32 vectors of rows, are what
+ *   the gradient reads.  rows may be 0.
+ * prm_layernorm_backward   with xhat = (h - mean) rstd and g = grad_y weight:
+ *     grad_residual = rstd (g - mean(g) - xhat mean(g xhat)) + grad_h   (grad_h, what reaches h from elsewhere, may
+ *                     be NULL); without dropout it is the gradient of x too and grad_x is ignored
+ *     grad_x        = the same, before its rounding, dropped out like x
+ *     grad_weight, grad_bias [groups][cols], contiguous, in the weight's type, either may be NULL: sums over
+ *                     the group's rows of grad_y xhat and of grad_y
+ *   rows must be a multiple of rows_per_group (or at most that: one group).  scratch: device, 16-byte aligned,
+ *   prm_layernorm_scratch_bytes(rows, cols, rows_per_group) bytes.  With rows = 0 the sums of one group are set to 0.
+ * prm_head_loss   softmax cross entropy of the logits x W (n x d by d x vocab), which are not kept:
+ *     lse = log sum_v exp(logit_v),  loss = lse - logit_label, 0 for a row whose label is not in 0..vocab-1
+ *   x and weight bf16; weight_transposed = 0: stored d x vocab, 1: vocab x d (an embedding).  Both 16-byte
+ *   aligned with row strides that are multiples of 8 (else PRM_ERR_ALIGN).  loss_out, lse_out: fp32 vectors of n.
+ *   A row with a NaN or an infinite logit gets a NaN.  n may be 0.  scratch: device, 16-byte aligned,
+ *   prm_head_loss_scratch_bytes(n, d, vocab) bytes.
+ * prm_head_loss_backward   from grad_loss (fp32, n): with G = grad_loss (softmax - [label]), 0 for rows without a label,
+ *     grad_x = G W^T (bf16, n x d),  grad_weight = x^T G (bf16, stored like weight); either may be NULL
+ *   G is rounded to bf16 (after division by the largest |grad_loss|) for the products, whose sums are fp32.
+ *   scratch: device, 256-byte aligned, prm_head_loss_backward_scratch_bytes(n, d, vocab) bytes: G for a piece of the
+ *   vocabulary, up to 512 MB, and partial sums.  With n = 0 grad_weight is set to zero.
+ * prm_q8_status covers the waits inside the head's products too.
+ */
+PRM_API int prm_dropout(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int64_t rows,
+                        int64_t cols, int io_fp32, double p, uint64_t seed, uint64_t offset, const uint64_t* counter,
+                        void* out, int64_t ld_out, void* cuda_stream);
+PRM_API int prm_layernorm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* weight,
+                          int64_t ld_weight, const void* bias, int64_t ld_bias, int64_t rows, int64_t cols,
+                          int64_t rows_per_group, int io_fp32, int weight_fp32, int add_one, float eps, double p,
+                          uint64_t seed, uint64_t offset, const uint64_t* counter, void* h_out, int64_t ld_h,
+                          void* y_out, int64_t ld_y, float* mean_out, float* rstd_out, void* cuda_stream);
+PRM_API size_t prm_layernorm_scratch_bytes(int64_t rows, int64_t cols, int64_t rows_per_group);
+PRM_API int prm_layernorm_backward(const void* grad_y, int64_t ld_grad_y, const void* h, int64_t ld_h,
+                                   const float* mean, const float* rstd, const void* weight, int64_t ld_weight,
+                                   const void* grad_h, int64_t ld_grad_h, int64_t rows, int64_t cols,
+                                   int64_t rows_per_group, int io_fp32, int weight_fp32, int add_one, double p,
+                                   uint64_t seed, uint64_t offset, const uint64_t* counter, void* grad_residual,
+                                   int64_t ld_grad_residual, void* grad_x, int64_t ld_grad_x, void* grad_weight,
+                                   void* grad_bias, void* scratch, size_t scratch_bytes, void* cuda_stream);
+PRM_API size_t prm_head_loss_scratch_bytes(int64_t n, int64_t d, int64_t vocab);
+PRM_API int prm_head_loss(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int weight_transposed,
+                          const int64_t* labels, int64_t n, int64_t d, int64_t vocab, float* loss_out,
+                          float* lse_out, void* scratch, size_t scratch_bytes, void* cuda_stream);
+PRM_API size_t prm_head_loss_backward_scratch_bytes(int64_t n, int64_t d, int64_t vocab);
+PRM_API int prm_head_loss_backward(const float* grad_loss, const void* x, int64_t ld_x, const void* weight,
+                                   int64_t ld_weight, int weight_transposed, const int64_t* labels, const float* lse,
+                                   int64_t n, int64_t d, int64_t vocab, void* grad_x, int64_t ld_grad_x,
+                                   void* grad_weight, int64_t ld_grad_weight, void* scratch, size_t scratch_bytes,
+                                   void* cuda_stream);
+
 /* Frees host resources.  Device memory belongs to the caller. */
 PRM_API int prm_destroy(prm_ctx* ctx);
 

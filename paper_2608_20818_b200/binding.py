@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
 
@@ -54,6 +54,8 @@ EXPORTS = (
     "prm_partition_matrices", "prm_shape_scale",
     "prm_rmsnorm_q8", "prm_rmsnorm_q8_scratch_bytes", "prm_rmsnorm_q8_backward",
     "prm_quantize_q8", "prm_quantize_q8_scratch_bytes", "prm_matmul_q8", "prm_q8_status",
+    "prm_dropout", "prm_layernorm", "prm_layernorm_scratch_bytes", "prm_layernorm_backward",
+    "prm_head_loss", "prm_head_loss_scratch_bytes", "prm_head_loss_backward", "prm_head_loss_backward_scratch_bytes",
 )
 PRM_PROF_ROW_WIDE, PRM_PROF_ROW_TALL, PRM_PROF_PREPASS, PRM_PROF_GRAM = 0, 1, 2, 3
 PRM_PROF_POLY, PRM_PROF_UPDATE, PRM_PROF_UPDATE_FINAL, PRM_PROF_GRAMSPACE, PRM_PROF_COUNT = 4, 5, 6, 7, 8
@@ -165,6 +167,29 @@ def lib():
     L.prm_matmul_q8.restype = c_int
     L.prm_q8_status.argtypes = []
     L.prm_q8_status.restype = c_int
+    draw = [c_double, c_uint64, c_uint64, c_void_p]          # p, seed, offset, counter
+    L.prm_dropout.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int64, c_int, *draw, c_void_p, c_int64, c_void_p]
+    L.prm_dropout.restype = c_int
+    L.prm_layernorm.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int64,
+                                c_int64, c_int, c_int, c_int, c_float, *draw, c_void_p, c_int64, c_void_p, c_int64,
+                                c_void_p, c_void_p, c_void_p]
+    L.prm_layernorm.restype = c_int
+    L.prm_layernorm_scratch_bytes.argtypes = [c_int64, c_int64, c_int64]
+    L.prm_layernorm_scratch_bytes.restype = c_size_t
+    L.prm_layernorm_backward.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64,
+                                         c_void_p, c_int64, c_int64, c_int64, c_int64, c_int, c_int, c_int, *draw,
+                                         c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_size_t,
+                                         c_void_p]
+    L.prm_layernorm_backward.restype = c_int
+    for name in ("prm_head_loss_scratch_bytes", "prm_head_loss_backward_scratch_bytes"):
+        getattr(L, name).argtypes = [c_int64, c_int64, c_int64]
+        getattr(L, name).restype = c_size_t
+    L.prm_head_loss.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_void_p,
+                                c_void_p, c_void_p, c_size_t, c_void_p]
+    L.prm_head_loss.restype = c_int
+    L.prm_head_loss_backward.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_void_p, c_int64,
+                                         c_int64, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
+    L.prm_head_loss_backward.restype = c_int
     _lib_handle = L
     return L
 
@@ -680,6 +705,265 @@ def prm_matmul_q8(a, scale_a, b, scale_b, out_dtype=torch.bfloat16, out=None, st
 
 def prm_q8_status():
     return int(lib().prm_q8_status())
+
+
+# Operators of a training step around its products: dropout, layer norm, the loss of a linear head.
+
+_INT64_ONLY = {torch.int64: 1}
+_WORD = (1 << 64) - 1
+
+
+def _draw(p, counter, index):
+    """The counter's address; refuses what is no probability, and a counter that the kernel cannot read."""
+    if not 0.0 <= p < 1.0:
+        raise ValueError("p must be at least 0 and below 1")
+    if counter is None:
+        return None
+    if counter.dtype is not torch.int64 or counter.numel() != 1 or counter.get_device() != index:
+        raise ValueError(f"counter must be one int64 on cuda:{index}")
+    return counter.data_ptr()
+
+
+def prm_dropout(x, p, seed, offset=0, counter=None, residual=None, stream=None):
+    """x (rows x cols, bf16 or fp32) with its elements dropped with probability p and the others divided by
+    1 - p, plus residual.  Which ones is decided by seed, row, column and the number offset + counter (one
+    int64 on the device): the same call on a gradient is the gradient."""
+    if stream is not None:
+        return _on_stream(stream, (x, counter, residual), lambda: prm_dropout(x, p, seed, offset, counter, residual))
+    x = _matrix(x, "x")
+    rows, cols = x.shape
+    index = x.get_device()
+    c_ptr = _draw(p, counter, index)
+    r_ptr, ld_r = None, 0
+    if residual is not None:
+        residual = _matrix(residual, "residual", x)
+        r_ptr, ld_r = residual.data_ptr(), residual.stride(0)
+    out = torch.empty_strided((rows, cols), (cols, 1), dtype=x.dtype, device=x.device)
+    args = (x.data_ptr(), x.stride(0), r_ptr, ld_r, rows, cols, _IO_FP32[x.dtype], p, seed & _WORD, offset & _WORD, c_ptr,
+            out.data_ptr(), cols, _raw_stream(index))
+    fn = (_lib_handle or lib()).prm_dropout
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_dropout")
+    return out
+
+
+def _affine(t, name, rows, cols, index, like=None):
+    """(t, row stride, groups) of a scale or shift: a vector of cols, or groups x cols with groups dividing rows."""
+    if t.dtype not in _IO_FP32:
+        raise TypeError(f"{name} must be bfloat16 or float32")
+    if t.dim() not in (1, 2) or t.shape[-1] != cols or t.get_device() != index:
+        raise ValueError(f"{name} must have {cols} columns, in one or two dimensions, on cuda:{index}")
+    if like is not None and (t.dtype is not like.dtype or t.shape != like.shape):
+        raise ValueError(f"{name} must have the weight's type and shape")
+    groups = t.shape[0] if t.dim() == 2 else 1
+    if groups == 0 or rows % groups:
+        raise ValueError(f"{name}'s rows must divide the {rows} rows of the stream")
+    if cols > 1 and t.stride(-1) != 1:
+        t = t.contiguous()
+    return t, t.stride(0) if t.dim() == 2 else cols, groups
+
+
+def prm_layernorm(x, weight=None, bias=None, eps=1e-6, residual=None, add_one=False, p=0.0, seed=0, offset=0, counter=None,
+                  stream=None):
+    """Layer norm of h = x (dropped out with probability p, see prm_dropout) + residual: (y, h, mean, rstd).
+
+    x, residual: rows x cols, bf16 or fp32.  weight, bias: cols, or groups x cols (each row of them for rows /
+    groups neighbouring rows), bf16 or fp32; add_one takes 1 + weight.  h, in x's type, is what the norm is taken of and
+    what the stream carries on; it is None where it is x itself.  mean and rstd (fp32) go to the gradient."""
+    if stream is not None:
+        return _on_stream(stream, (x, weight, bias, residual, counter),
+                          lambda: prm_layernorm(x, weight, bias, eps, residual, add_one, p, seed, offset, counter))
+    x = _matrix(x, "x")
+    rows, cols = x.shape
+    index = x.get_device()
+    device = x.device
+    c_ptr = _draw(p, counter, index)
+    w_ptr = b_ptr = r_ptr = h_ptr = h = None
+    ld_w = ld_b = ld_r = w_fp32 = 0
+    groups = 1
+    if weight is not None:
+        weight, ld_w, groups = _affine(weight, "weight", rows, cols, index)
+        w_ptr, w_fp32 = weight.data_ptr(), _IO_FP32[weight.dtype]
+    if bias is not None:
+        if weight is None and bias.dim() != 1:
+            raise ValueError("a bias without a weight must be a vector")
+        bias, ld_b, groups = _affine(bias, "bias", rows, cols, index, weight)
+        b_ptr, w_fp32 = bias.data_ptr(), _IO_FP32[bias.dtype]
+    if residual is not None:
+        residual = _matrix(residual, "residual", x)
+        r_ptr, ld_r = residual.data_ptr(), residual.stride(0)
+    if residual is not None or p > 0:
+        h = torch.empty_strided((rows, cols), (cols, 1), dtype=x.dtype, device=device)
+        h_ptr = h.data_ptr()
+    y = torch.empty_strided((rows, cols), (cols, 1), dtype=x.dtype, device=device)
+    stats = torch.empty_strided((2, rows), (rows, 1), dtype=torch.float32, device=device)
+    s_ptr = stats.data_ptr()
+    args = (x.data_ptr(), x.stride(0), r_ptr, ld_r, w_ptr, ld_w, b_ptr, ld_b, rows, cols, max(1, rows // groups),
+            _IO_FP32[x.dtype], w_fp32, 1 if add_one else 0, eps, p, seed & _WORD, offset & _WORD, c_ptr, h_ptr, cols,
+            y.data_ptr(), cols, s_ptr, s_ptr + 4 * rows, _raw_stream(index))
+    fn = (_lib_handle or lib()).prm_layernorm
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_layernorm")
+    return y, h, stats[0], stats[1]
+
+
+def prm_layernorm_backward(grad_y, h, mean, rstd, weight=None, grad_h=None, add_one=False, p=0.0, seed=0, offset=0,
+                           counter=None, need_weight=True, need_bias=True, stream=None):
+    """Gradient of the layer norm at h (what prm_layernorm returned, or its x) with the forward call's p, seed,
+    offset and counter: (grad_x, grad_residual, grad_weight, grad_bias).  grad_residual is None without
+    dropout: it is grad_x.  grad_h, if given, is what reaches h along the residual stream.  grad_weight and
+    grad_bias have weight's shape and type (without a weight they are fp32 vectors)."""
+    if stream is not None:
+        return _on_stream(stream, (grad_y, h, mean, rstd, weight, grad_h, counter),
+                          lambda: prm_layernorm_backward(grad_y, h, mean, rstd, weight, grad_h, add_one, p, seed, offset,
+                                                         counter, need_weight, need_bias))
+    h = _matrix(h, "h")
+    grad_y = _matrix(grad_y, "grad_y", h)
+    rows, cols = h.shape
+    index = h.get_device()
+    device = h.device
+    c_ptr = _draw(p, counter, index)
+    mean = _vector(mean, "mean", rows, index)
+    rstd = _vector(rstd, "rstd", rows, index)
+    w_ptr = gh_ptr = gx_ptr = gw_ptr = gb_ptr = grad_x = grad_w = grad_b = None
+    ld_w = ld_gh = 0
+    groups, w_dtype, w_shape = 1, torch.float32, (cols,)
+    if weight is not None:
+        w_shape = weight.shape
+        weight, ld_w, groups = _affine(weight, "weight", rows, cols, index)
+        w_ptr, w_dtype = weight.data_ptr(), weight.dtype
+    if grad_h is not None:
+        grad_h = _matrix(grad_h, "grad_h", h)
+        gh_ptr, ld_gh = grad_h.data_ptr(), grad_h.stride(0)
+    grad_r = torch.empty_strided((rows, cols), (cols, 1), dtype=h.dtype, device=device)
+    if p > 0:
+        grad_x = torch.empty_strided((rows, cols), (cols, 1), dtype=h.dtype, device=device)
+        gx_ptr = grad_x.data_ptr()
+    if need_weight:
+        grad_w = torch.empty(w_shape, dtype=w_dtype, device=device)
+        gw_ptr = grad_w.data_ptr()
+    if need_bias:
+        grad_b = torch.empty(w_shape, dtype=w_dtype, device=device)
+        gb_ptr = grad_b.data_ptr()
+    per = max(1, rows // groups)
+    L = _lib_handle or lib()
+    nbytes = L.prm_layernorm_scratch_bytes(rows, cols, per)
+    scratch = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)
+    args = (grad_y.data_ptr(), grad_y.stride(0), h.data_ptr(), h.stride(0), mean.data_ptr(), rstd.data_ptr(), w_ptr, ld_w,
+            gh_ptr, ld_gh, rows, cols, per, _IO_FP32[h.dtype], _IO_FP32[w_dtype], 1 if add_one else 0, p, seed & _WORD,
+            offset & _WORD, c_ptr, grad_r.data_ptr(), cols, gx_ptr, cols, gw_ptr, gb_ptr, scratch.data_ptr(), nbytes,
+            _raw_stream(index))
+    fn = L.prm_layernorm_backward
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_layernorm_backward")
+    if rows == 0 and groups > 1:
+        for t in (grad_w, grad_b):
+            if t is not None:
+                t.zero_()
+    return (grad_x, grad_r, grad_w, grad_b) if p > 0 else (grad_r, None, grad_w, grad_b)
+
+
+def _head_operand(t):
+    """(matrix, row stride, 1 if it is stored the other way round) of a bf16 matrix as the head's products read
+    it; one that lies in neither way, or unaligned, is copied."""
+    r, c = t.shape
+    s0, s1 = t.stride()
+    if t.data_ptr() & 15 == 0:
+        if s1 == 1 or c == 1:
+            ld = s0 if r > 1 else (c + 7) // 8 * 8
+            if ld & 7 == 0 and ld >= c:
+                return t, ld, 0
+        if s0 == 1 or r == 1:
+            ld = s1 if c > 1 else (r + 7) // 8 * 8
+            if ld & 7 == 0 and ld >= r:
+                return t, ld, 1
+    if s0 == 1 and r > 1:                   # keep the way it is stored
+        laid = torch.empty_strided((r, c), (1, (r + 7) // 8 * 8), dtype=t.dtype, device=t.device)
+        laid.copy_(t)
+        return laid, (r + 7) // 8 * 8, 1
+    laid = torch.empty_strided((r, c), ((c + 7) // 8 * 8, 1), dtype=t.dtype, device=t.device)
+    laid.copy_(t)
+    return laid, (c + 7) // 8 * 8, 0
+
+
+def _head_arguments(x, weight, labels):
+    """x, its row stride, weight, its row stride, whether it is transposed, labels."""
+    if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[0]:
+        raise ValueError("x must be n x d and weight d x vocab")
+    if x.dtype is not torch.bfloat16 or weight.dtype is not torch.bfloat16:
+        raise TypeError("x and weight must be bfloat16")
+    index = x.get_device()
+    if index < 0 or weight.get_device() != index:
+        raise ValueError("x and weight must sit on the same CUDA device")
+    if x.shape[1] == 0 or weight.shape[1] == 0:
+        raise ValueError("d and vocab must be at least 1")
+    labels = _vector(labels, "labels", x.shape[0], index, _INT64_ONLY)
+    laid, ld_x, x_t = _head_operand(x)
+    if x_t:                                 # x is read by rows
+        laid = torch.empty_strided(x.shape, ((x.shape[1] + 7) // 8 * 8, 1), dtype=x.dtype, device=x.device)
+        laid.copy_(x)
+        ld_x = (x.shape[1] + 7) // 8 * 8
+    return (laid, ld_x, *_head_operand(weight), labels)
+
+
+def prm_head_loss(x, weight, labels, stream=None):
+    """Softmax cross entropy of the logits x @ weight, which are not kept: (loss, lse), fp32 vectors of n.
+
+    x: n x d, weight: d x vocab (or the transposed view of an embedding), both bf16; labels: n int64.  A label
+    outside 0..vocab-1 leaves its row out: loss 0.  lse, the logarithm of the row's sum of exponentials, goes to the
+    gradient.  Matrices whose rows do not start on 16 bytes are copied first."""
+    if stream is not None:
+        return _on_stream(stream, (x, weight, labels), lambda: prm_head_loss(x, weight, labels))
+    n, d = x.shape if x.dim() == 2 else (0, 0)
+    x, ld_x, weight, ld_w, w_t, labels = _head_arguments(x, weight, labels)
+    vocab = weight.shape[1]
+    index = x.get_device()
+    out = torch.empty_strided((2, n), (n, 1), dtype=torch.float32, device=x.device)
+    L = _lib_handle or lib()
+    nbytes = L.prm_head_loss_scratch_bytes(n, d, vocab)
+    scratch = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=x.device)
+    o_ptr = out.data_ptr()
+    args = (x.data_ptr(), ld_x, weight.data_ptr(), ld_w, w_t, labels.data_ptr(), n, d, vocab, o_ptr, o_ptr + 4 * n,
+            scratch.data_ptr(), nbytes, _raw_stream(index))
+    fn = L.prm_head_loss
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_head_loss")
+    return out[0], out[1]
+
+
+def prm_head_loss_backward(grad_loss, x, weight, labels, lse, need_x=True, need_weight=True, stream=None):
+    """Gradient of prm_head_loss from that of each row's loss (fp32, n) and its lse: (grad_x, grad_weight), bf16,
+    None for what is not needed; grad_weight is stored the way weight is."""
+    if stream is not None:
+        return _on_stream(stream, (grad_loss, x, weight, labels, lse),
+                          lambda: prm_head_loss_backward(grad_loss, x, weight, labels, lse, need_x, need_weight))
+    n, d = x.shape if x.dim() == 2 else (0, 0)
+    x, ld_x, weight, ld_w, w_t, labels = _head_arguments(x, weight, labels)
+    vocab = weight.shape[1]
+    index = x.get_device()
+    grad_loss = _vector(grad_loss, "grad_loss", n, index)
+    lse = _vector(lse, "lse", n, index)
+    gx = gw = gx_ptr = gw_ptr = None
+    if need_x:
+        gx = torch.empty_strided((n, d), (d, 1), dtype=torch.bfloat16, device=x.device)
+        gx_ptr = gx.data_ptr()
+    if need_weight:
+        gw = torch.empty_strided((d, vocab), (1, d) if w_t else (vocab, 1), dtype=torch.bfloat16, device=x.device)
+        gw_ptr = gw.data_ptr()
+    L = _lib_handle or lib()
+    nbytes = L.prm_head_loss_backward_scratch_bytes(n, d, vocab)
+    scratch = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=x.device)
+    args = (grad_loss.data_ptr(), x.data_ptr(), ld_x, weight.data_ptr(), ld_w, w_t, labels.data_ptr(), lse.data_ptr(), n, d,
+            vocab, gx_ptr, d, gw_ptr, d if w_t else vocab, scratch.data_ptr(), nbytes, _raw_stream(index))
+    fn = L.prm_head_loss_backward
+    code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
+    if code:
+        _q8_check(code, "prm_head_loss_backward")
+    return gx, gw
 
 
 def prm_destroy(h):

@@ -1,0 +1,720 @@
+// Softmax cross entropy of a linear head, without keeping its logits:
+//
+//   l = x W;   lse_i = log sum_v exp l_iv;   loss_i = lse_i - l_i,label
+//   G_iv = gl_i (exp(l_iv - lse_i) - [v = label_i]);   grad_x = G W^T;   grad_W = x^T G
+//
+// Bound by the tensor pipe (2 n d V flop forward, 6 n d V backward, two of them for the logits again), with
+// few rows by W's bytes.  The logits live in tensor memory only.  Forward, the epilogue of a tile leaves two numbers per
+// row and 128 columns, the largest logit and the sum of exponentials relative to it; a second kernel joins them.
+// Backward, G exists for a piece of the vocabulary at a time, as an operand of the two products that follow.
+//
+// G is rounded to bf16, the type of the operands that it is multiplied with (relative 2^-8 at most, of each entry by
+// itself); the factor of the rows' gradients is kept out of it: G is made of gl_i / c with c = max |gl|, which is
+// exactly 1 for a mean or a sum, and the products' fp32 sums are multiplied by c.  All else is fp32, rounded once.
+//
+// All products run in one kernel on pairs of CTAs (tcgen05.mma.cta_group::2), 256 x 256 tiles:
+//   warp 0      TMA producer: per stage 128 k of both operands (64 KB), 128-byte swizzle, no multicast; the
+//               copies of both CTAs count on the leader's barrier.  Three stages
+//   warp 1      tcgen05.mma issuer (one lane of the leader); owns its CTA's tensor memory
+//   warps 2..9  epilogue: two warps per lane quadrant, half of the 256 columns each; a thread has a row
+// Two accumulators of 256 columns let the epilogue of a tile run under the next tile's main loop.
+// Every barrier wait is bounded; one that runs out sets the status word, the pair drains and leaves.
+#include "q8_matmul.cuh"
+
+namespace prm {
+namespace {
+
+constexpr int kTile = 256;                       // tile edge, both ways
+constexpr int kHeadK = 64;                       // one 128-byte swizzled row of k
+constexpr int kSub = 2;                          // k-blocks per stage
+constexpr int kStages = 3;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 32 * (2 + kEpiWarps);
+constexpr uint32_t kBoxBytes = 128 * 128;        // 128 rows of one k-block
+constexpr uint32_t kStageBytes = 2 * kSub * kBoxBytes;
+constexpr uint32_t kPatchBytes = 32 * 64;        // a warp's 32 rows of 64 bytes on their way out
+constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kPatchBytes;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+enum Epi { kStats, kGrad, kStore };
+
+struct HeadArgs {
+  int m, n, kblocks;               // of this product: rows, columns, ceil(k / 64)
+  int q_n0, q_k0;                  // where it starts in Q
+  int m_tiles, n_tiles, tiles;     // tiles: of all splits of k
+  int band;                        // m-tiles that are walked through together
+  int split;                       // parts of k (kStore)
+  int* status;
+  // kStats, kGrad
+  const int64_t* labels;
+  int64_t vocab;
+  float2* part;                    // [2 n_tiles][m]: largest logit * log2 e, sum of 2^(logit log2 e - that)
+  float* at_label;                 // [m]
+  const float* lse;
+  const float* grad_loss;
+  __nv_bfloat16* g;
+  int64_t ld_g;
+  // kGrad, kStore
+  const float* unit;               // c; null: 1
+  void* out;
+  int64_t ld_out, split_stride;
+  int out_fp32, accumulate;        // accumulate: fp32 out += (16-byte aligned)
+};
+
+__device__ __forceinline__ float ex2(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// Order of the tiles: bands of `band` m-tiles, in a band n by n, m-tiles fastest; the splits of k one after
+// the other.  Pairs that run at the same time then share the band's rows of P and a few columns' worth of Q.
+__device__ __forceinline__ void tile_origin(const HeadArgs& a, int t, int& split, int& m0, int& n0) {
+  const int each = a.m_tiles * a.n_tiles;
+  split = t / each;
+  t -= split * each;
+  const int per = a.band * a.n_tiles, first = t / per * a.band, rest = t % per;
+  const int height = min(a.band, a.m_tiles - first);
+  m0 = (first + rest % height) * kTile;
+  n0 = rest / height * kTile;
+}
+__device__ __forceinline__ void split_range(const HeadArgs& a, int split, int& s0, int& s1) {
+  const int stages = (a.kblocks + kSub - 1) / kSub;
+  s0 = (int)((int64_t)stages * split / a.split);
+  s1 = (int)((int64_t)stages * (split + 1) / a.split);
+}
+
+// The label of a row as a column of the 128 from n0 on, -1 if it is none of them.
+__device__ __forceinline__ int label_column(const HeadArgs& a, int64_t label, int n0) {
+  const int64_t c = label - a.q_n0 - n0;
+  return label >= 0 && label < a.vocab && c >= 0 && c < 128 ? (int)c : -1;
+}
+
+// 128 columns of the lane's row: what they add to the softmax, and the label's logit.
+__device__ __forceinline__ void stats_tile(const HeadArgs& a, uint32_t taddr, int row, int n0, int column) {
+  float top = -INFINITY, top2 = 0.f, sum = 0.f;            // top2: in base 2, 0 while all are -infinity
+  const int label = row < a.m ? label_column(a, a.labels[row], n0) : -1;
+#pragma unroll 1
+  for (int k = 0; k < 4; ++k) {
+    const int wide = a.n - (n0 + k * 32);
+    if (wide <= 0) break;
+    uint32_t r[32];
+    tmem_ld32(taddr + k * 32, r);
+    tmem_wait_ld();
+    float v[32], here = top;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      v[j] = j < wide ? __uint_as_float(r[j]) : -INFINITY;
+      here = fmaxf(here, v[j]);
+    }
+    const float here2 = here == -INFINITY ? 0.f : here * kLog2e;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s[j & 3] += ex2(fmaf(v[j], kLog2e, -here2));
+    sum = (top == -INFINITY ? sum : sum * ex2(top2 - here2)) + ((s[0] + s[1]) + (s[2] + s[3]));
+    top = here;
+    top2 = here2;
+    const int at = label - k * 32;
+    if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (at == j) a.at_label[row] = v[j];
+    }
+  }
+  if (row < a.m) a.part[(int64_t)column * a.m + row] = make_float2(top == -INFINITY ? top : top2, sum);
+}
+
+// 16-byte chunk c of row r of a warp's patch, where neither writing rows nor reading them back meets a bank twice.
+__device__ __forceinline__ uint4* patch_at(uint8_t* patch, int r, int c) {
+  return reinterpret_cast<uint4*>(patch + (r >> 1) * 128 + (r & 1) * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+}
+
+// 128 columns of the lane's row of G.
+__device__ __forceinline__ void grad_tile(const HeadArgs& a, uint32_t taddr, uint8_t* patch, int m0, int n0, int rows) {
+  const int lane = threadIdx.x & 31, row = m0 + lane;
+  float factor = 0.f, lse2 = 0.f;
+  int label = -1;
+  if (row < a.m) {
+    const int64_t l = a.labels[row];
+    if (l >= 0 && l < a.vocab) {
+      factor = __fdiv_rn(a.grad_loss[row], *a.unit);
+      lse2 = a.lse[row] * kLog2e;
+      label = label_column(a, l, n0);
+    }
+  }
+  __nv_bfloat16* out = a.g + (int64_t)m0 * a.ld_g + n0;
+#pragma unroll 1
+  for (int k = 0; k < 4; ++k) {
+    if (n0 + k * 32 >= a.n) break;
+    uint32_t r[32];
+    tmem_ld32(taddr + k * 32, r);
+    tmem_wait_ld();
+    float v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float p = ex2(fmaf(__uint_as_float(r[j]), kLog2e, -lse2)) - (label == k * 32 + j ? 1.f : 0.f);
+      v[j] = factor == 0.f ? 0.f : factor * p;             // a row without a label has no part, whatever its logits
+    }
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *patch_at(patch, lane, c) =
+          make_uint4(pair_to_bf16(make_float2(v[c * 8], v[c * 8 + 1])), pair_to_bf16(make_float2(v[c * 8 + 2], v[c * 8 + 3])),
+                     pair_to_bf16(make_float2(v[c * 8 + 4], v[c * 8 + 5])), pair_to_bf16(make_float2(v[c * 8 + 6], v[c * 8 + 7])));
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = i * 8 + (lane >> 2);
+      const uint4 x = *patch_at(patch, at, lane & 3);
+      if (at < rows) *reinterpret_cast<uint4*>(out + at * a.ld_g + k * 32 + (lane & 3) * 8) = x;   // rows are padded to 64
+    }
+  }
+}
+
+// 128 columns of the lane's row of a product.
+template <typename OUT>
+__device__ __forceinline__ void store_tile(const HeadArgs& a, uint32_t taddr, uint8_t* patch, int split, int m0, int n0,
+                                           int rows, float unit) {
+  constexpr int kCols = 64 / sizeof(OUT);                 // per piece
+  const int lane = threadIdx.x & 31;
+  OUT* out = reinterpret_cast<OUT*>(a.out) + split * a.split_stride + (int64_t)m0 * a.ld_out + n0;
+  const bool vec = ((uintptr_t)out & 15) == 0 && (a.ld_out * (int64_t)sizeof(OUT)) % 16 == 0;
+#pragma unroll 1
+  for (int k = 0; k < 4; ++k) {
+    if (n0 + k * 32 >= a.n) break;
+    uint32_t r[32];
+    tmem_ld32(taddr + k * 32, r);
+    tmem_wait_ld();
+#pragma unroll
+    for (int piece = 0; piece < 32 / kCols; ++piece) {
+      const int wide = min(kCols, a.n - (n0 + k * 32 + piece * kCols));
+      if (wide <= 0) break;
+      uint4 w[4];
+      uint32_t* o = reinterpret_cast<uint32_t*>(w);
+#pragma unroll
+      for (int c = 0; c < kCols; c += 2) {
+        const float2 u = mul2(make_float2(__uint_as_float(r[piece * kCols + c]), __uint_as_float(r[piece * kCols + c + 1])),
+                              make_float2(unit, unit));
+        if constexpr (sizeof(OUT) == 2) {
+          o[c / 2] = pair_to_bf16(u);
+        } else {
+          o[c] = __float_as_uint(u.x);
+          o[c + 1] = __float_as_uint(u.y);
+        }
+      }
+      __syncwarp();                                       // the piece before has been read
+#pragma unroll
+      for (int c = 0; c < 4; ++c) *patch_at(patch, lane, c) = w[c];
+      __syncwarp();
+      OUT* to = out + k * 32 + piece * kCols;
+      if (vec && wide == kCols) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = i * 8 + (lane >> 2);
+          uint4 x = *patch_at(patch, row, lane & 3);
+          if (row < rows) {
+            uint4* p = reinterpret_cast<uint4*>(to + row * a.ld_out + (lane & 3) * (16 / sizeof(OUT)));
+            if constexpr (sizeof(OUT) == 4) {
+              if (a.accumulate) {
+                const float4 old = *reinterpret_cast<const float4*>(p);
+                x = make_uint4(__float_as_uint(old.x + __uint_as_float(x.x)), __float_as_uint(old.y + __uint_as_float(x.y)),
+                               __float_as_uint(old.z + __uint_as_float(x.z)), __float_as_uint(old.w + __uint_as_float(x.w)));
+              }
+            }
+            *p = x;
+          }
+        }
+      } else {
+#pragma unroll 4
+        for (int row = 0; row < rows; ++row) {
+          const int c = lane * (int)sizeof(OUT);
+          if (lane < wide) {
+            OUT v = *reinterpret_cast<const OUT*>(reinterpret_cast<const uint8_t*>(patch_at(patch, row, (c >> 4) & 3)) + (c & 15));
+            if constexpr (sizeof(OUT) == 4) {
+              if (a.accumulate) v += to[row * a.ld_out + lane];
+            }
+            to[row * a.ld_out + lane] = v;
+          }
+        }
+      }
+    }
+  }
+}
+
+template <int EPI, bool P_MN, bool Q_MN>
+__global__ void __launch_bounds__(kThreads, 1)
+head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const HeadArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kStages], empty[kStages], tfull[2], tempty[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  volatile int* abort_flag = &abort_word;
+  int* status = a.status;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&tfull[i], 1);
+      mbar_init(&tempty[i], 2 * kEpiWarps);
+    }
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)),
+                 "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tcgen05_before_sync();
+  __syncthreads();
+  cluster_barrier();                             // the peer's barriers are initialised too
+  tcgen05_after_sync();
+  const uint32_t tmem = tmem_slot;
+  grid_wait();
+  grid_trigger();                                // not before the tensor memory is this kernel's
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      const uint32_t lead_full = cluster_map(smem_u32(&full[0]), 0);
+      for (int t = pair; t < a.tiles && ok; t += pairs) {
+        int split, m0, n0, s0, s1;
+        tile_origin(a, t, split, m0, n0);
+        split_range(a, split, s0, s1);
+        m0 += (int)rank * 128;
+        n0 += (int)rank * 128 + a.q_n0;
+        for (int kt = s0; kt < s1; ++kt, ++it) {
+          const int s = it % kStages;
+          if (!mbar_wait(&empty[s], ((it / kStages) & 1) ^ 1, abort_flag, status)) { ok = false; break; }
+          uint8_t* sp = smem + (size_t)s * kStageBytes;
+          uint8_t* sq = sp + kSub * kBoxBytes;
+          const int subs = min(kSub, a.kblocks - kt * kSub);
+          if (rank == 0) mbar_expect_tx(&full[s], (uint32_t)subs * 4 * kBoxBytes);   // both CTAs' bytes
+          const uint32_t bar = lead_full + 8u * s;
+#pragma unroll
+          for (int j = 0; j < kSub; ++j) {
+            if (j < subs) {
+              const int k0 = (kt * kSub + j) * kHeadK;
+              // an operand whose m (or n) is contiguous: boxes of 64 of them by 64 k
+              if (P_MN) {
+                tma_load_pair(sp + j * kBoxBytes, &map_p, bar, m0, k0);
+                tma_load_pair(sp + j * kBoxBytes + kBoxBytes / 2, &map_p, bar, m0 + 64, k0);
+              } else {
+                tma_load_pair(sp + j * kBoxBytes, &map_p, bar, k0, m0);
+              }
+              if (Q_MN) {
+                tma_load_pair(sq + j * kBoxBytes, &map_q, bar, n0, a.q_k0 + k0);
+                tma_load_pair(sq + j * kBoxBytes + kBoxBytes / 2, &map_q, bar, n0 + 64, a.q_k0 + k0);
+              } else {
+                tma_load_pair(sq + j * kBoxBytes, &map_q, bar, a.q_k0 + k0, n0);
+              }
+            }
+          }
+        }
+      }
+      // Copies in flight must land before shared memory is released; the leader sees both CTAs'.
+      if (rank == 0) {
+        for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j) {
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(&full[j % kStages], (j / kStages) & 1) && global_ns() - t0 < 1000000ull) {
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = idesc_bf16(kTile, kTile, P_MN, Q_MN);
+      constexpr uint32_t kStepP = P_MN ? 128 : 2, kStepQ = Q_MN ? 128 : 2;    // 16 k, in units of 16 bytes
+      uint32_t it = 0, acc = 0;
+      bool ok = true;
+      const uint32_t smem0 = smem_u32(smem);
+      for (int t = pair; t < a.tiles && ok; t += pairs, ++acc) {
+        int split, m0, n0, s0, s1;
+        tile_origin(a, t, split, m0, n0);
+        split_range(a, split, s0, s1);
+        const uint32_t ab = acc & 1;
+        if (!mbar_wait(&tempty[ab], ((acc >> 1) & 1) ^ 1, abort_flag, status)) break;
+        tcgen05_after_sync();
+        const uint32_t d = tmem + ab * kTile;
+        for (int kt = s0; kt < s1; ++kt, ++it) {
+          const int s = it % kStages;
+          if (!mbar_wait(&full[s], (it / kStages) & 1, abort_flag, status)) { ok = false; break; }
+          tcgen05_after_sync();
+          const uint32_t sp = smem0 + (uint32_t)s * kStageBytes, sq = sp + kSub * kBoxBytes;
+          const int subs = min(kSub, a.kblocks - kt * kSub);
+#pragma unroll
+          for (int j = 0; j < kSub; ++j) {
+            if (j < subs) {
+              const uint64_t dp = P_MN ? desc_mn_major(sp + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sp + j * kBoxBytes);
+              const uint64_t dq = Q_MN ? desc_mn_major(sq + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sq + j * kBoxBytes);
+#pragma unroll
+              for (int i = 0; i < kHeadK / 16; ++i)
+                umma_bf16_pair(d, dp + kStepP * i, dq + kStepQ * i, idesc, (uint32_t)(kt > s0) | (uint32_t)((j | i) != 0));
+            }
+          }
+          umma_commit_both(smem_u32(&empty[s]));
+        }
+        if (ok) umma_commit_both(smem_u32(&tfull[ab]));
+      }
+    }
+  } else {
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * 128);
+    const uint32_t lead_tempty = cluster_map(smem_u32(&tempty[0]), 0);
+    uint8_t* patch = smem + (size_t)kStages * kStageBytes + (warp - 2) * kPatchBytes;
+    const float unit = EPI == kStore && a.unit ? *a.unit : 1.f;
+    uint32_t acc = 0;
+    for (int t = pair; t < a.tiles; t += pairs, ++acc) {
+      const uint32_t ab = acc & 1;
+      int split, m0, n0;
+      tile_origin(a, t, split, m0, n0);
+      const int column = (n0 / kTile) * 2 + half;
+      m0 += (int)rank * 128 + quad * 32;                  // this warp's rows and columns
+      n0 += half * 128;
+      const bool got = mbar_wait(&tfull[ab], (acc >> 1) & 1, abort_flag, status);
+      if (!__all_sync(0xffffffffu, got)) break;
+      tcgen05_after_sync();
+      const int rows = min(32, a.m - m0);
+      const uint32_t taddr = trow + ab * kTile;
+      if constexpr (EPI == kStats) stats_tile(a, taddr, m0 + lane, n0, column);
+      if constexpr (EPI == kGrad) grad_tile(a, taddr, patch, m0, n0, rows);
+      if constexpr (EPI == kStore) {
+        if (a.out_fp32) store_tile<float>(a, taddr, patch, split, m0, n0, rows, unit);
+        else store_tile<__nv_bfloat16>(a, taddr, patch, split, m0, n0, rows, unit);
+      }
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) arrive_cluster(lead_tempty + 8u * ab);
+    }
+  }
+  // Neither CTA leaves while its partner can still touch its shared or tensor memory.
+  tcgen05_before_sync();
+  __syncwarp();
+  __syncthreads();
+  cluster_barrier();
+  if (warp == 1) {
+    tcgen05_after_sync();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+// The rows' parts joined: 32 rows per block, eight parts at a time.
+__global__ void __launch_bounds__(256) head_join_kernel(const float2* part, int parts, const float* at_label,
+                                                        const int64_t* labels, int64_t vocab, int rows, float* loss, float* lse) {
+  __shared__ float2 s[8][32];
+  grid_wait();
+  grid_trigger();
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int row = (int)blockIdx.x * 32 + lane;
+  float top = -INFINITY, sum = 0.f;
+  auto add = [&](float2 p) {
+    const float here = fmaxf(top, p.x);
+    // a part of -infinities alone has the sum 0 (NaN with a NaN among them)
+    if (top != here && top != -INFINITY) sum *= exp2f(top - here);
+    sum += p.x == here || p.x == -INFINITY ? p.y : p.y * exp2f(p.x - here);
+    top = here;
+  };
+  if (row < rows) {
+#pragma unroll 4
+    for (int k = warp; k < parts; k += 8) add(__ldcg(part + (int64_t)k * rows + row));
+  }
+  s[warp][lane] = make_float2(top, sum);
+  __syncthreads();
+  if (warp == 0 && row < rows) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k)
+      if (k < parts) add(s[k][lane]);
+    const float l = (top + log2f(sum)) * kLn2;
+    const int64_t label = labels[row];
+    lse[row] = l;
+    loss[row] = label >= 0 && label < vocab ? l - at_label[row] : 0.f;
+  }
+}
+
+// c = max |gl| over the rows with a label (1 if that is 0 or no number).
+__global__ void __launch_bounds__(1024) head_unit_kernel(const float* grad_loss, const int64_t* labels, int64_t vocab, int rows,
+                                                         float* unit) {
+  __shared__ float red[32];
+  grid_wait();
+  grid_trigger();
+  float top = 0.f;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < rows; i += 1024) {
+    const int64_t l = labels[i];
+    const float v = grad_loss[i];
+    if (l >= 0 && l < vocab) top = fmaxf(top, fabsf(v));
+  }
+  top = group_top(top);
+  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    top = group_top(red[threadIdx.x]);
+    if (threadIdx.x == 0) *unit = top > 0.f && top < INFINITY ? top : 1.f;
+  }
+}
+
+// grad_x from the parts of its sums.
+__global__ void __launch_bounds__(256) head_sum_kernel(const float* part, int parts, int64_t stride, int rows, int cols,
+                                                       int64_t ld_part, const float* unit, __nv_bfloat16* out, int64_t ld_out) {
+  grid_wait();
+  grid_trigger();
+  const float c = *unit;
+  const int chunks = (cols + 255) / 256;
+  const int64_t row = blockIdx.x / (unsigned)chunks;
+  const int col = (int)(blockIdx.x % (unsigned)chunks) * 256 + threadIdx.x;
+  if (col >= cols) return;
+  float sum = 0.f;
+  for (int k = 0; k < parts; ++k) sum += __ldcg(part + k * stride + row * ld_part + col);
+  out[row * ld_out + col] = __float2bfloat16_rn(sum * c);
+}
+
+// Map over a row-major rows x cols bf16 matrix, boxes of box_rows x 64; what lies outside reads as zero.
+bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+  Q8EncodeFn encode = q8_encode_fn();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t box[2] = {kHeadK, (cuuint32_t)box_rows};
+  const cuuint32_t step[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Operand {
+  const void* p;
+  int64_t rows, cols, ld;          // as stored
+  bool mn;                         // m (n) contiguous
+};
+
+template <int EPI, bool P_MN, bool Q_MN>
+int launch_head(const Operand& p, const Operand& q, HeadArgs a, int64_t k, cudaStream_t stream) {
+  static PerDeviceOnce once;
+  static int resident[64];
+  int dev;
+  if (once.need(&dev)) {
+    if (dev < 0) return PRM_ERR_CUDA;
+    const cudaError_t e = cudaFuncSetAttribute(head_kernel<EPI, P_MN, Q_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)kSmemBytes);
+    if (e != cudaSuccess) return q8_code(e);
+    const int n = q8_resident_clusters(head_kernel<EPI, P_MN, Q_MN>, kThreads, kSmemBytes, 2);
+    if (n < 1) return PRM_ERR_CUDA;
+    resident[dev] = n;
+    once.mark(dev);
+  }
+  a.status = q8_status_word();
+  if (!a.status) return PRM_ERR_CUDA;
+  a.kblocks = (int)((k + kHeadK - 1) / kHeadK);
+  a.m_tiles = (a.m + kTile - 1) / kTile;
+  a.n_tiles = (a.n + kTile - 1) / kTile;
+  if ((int64_t)a.m_tiles * a.n_tiles * a.split > 0x3fffffffLL) return PRM_ERR_SHAPE;
+  a.tiles = a.m_tiles * a.n_tiles * a.split;
+  // As many m-tiles as keep their rows of P within 32 MB of the L2, at least 8 (a ninth of a wave).
+  const int64_t fit = ((int64_t)32 << 20) / ((int64_t)kTile * a.kblocks * 128);
+  a.band = (int)std::min<int64_t>(a.m_tiles, std::max<int64_t>(8, fit));
+  CUtensorMap mp, mq;
+  if (!make_map(&mp, p.p, p.rows, p.cols, p.ld, P_MN ? 64 : 128) || !make_map(&mq, q.p, q.rows, q.cols, q.ld, Q_MN ? 64 : 128))
+    return PRM_ERR_CUDA;
+  return q8_code(launch_after(head_kernel<EPI, P_MN, Q_MN>, 2u * (unsigned)std::min(a.tiles, resident[dev]), kThreads,
+                              kSmemBytes, stream, 2, mp, mq, a));
+}
+template <int EPI>
+int launch_logits(const Operand& x, const Operand& w, const HeadArgs& a, int64_t d, cudaStream_t stream) {
+  return w.mn ? launch_head<EPI, false, true>(x, w, a, d, stream) : launch_head<EPI, false, false>(x, w, a, d, stream);
+}
+
+// ------------------------------------------------------------------ sizes
+
+inline int64_t ceil_to(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
+
+// Forward: rows whose parts fit 128 MB are taken together.
+int64_t stats_rows(int64_t n, int64_t vocab) {
+  const int64_t parts = 2 * ((vocab + kTile - 1) / kTile);
+  return std::min(n, std::max<int64_t>(2048, ((int64_t)128 << 20) / (8 * parts) / kTile * kTile));
+}
+
+// Backward: pieces of the vocabulary whose G fits 512 MB, of alike width, and grad_x's sums: one product's parts of
+// k where there are few tiles, the pieces' running sums where there are several.
+struct BackwardPlan {
+  int64_t piece, ld_g, ld_part;
+  int pieces, split;
+  size_t g_bytes, part_bytes;
+};
+BackwardPlan backward_plan(int64_t n, int64_t d, int64_t vocab) {
+  BackwardPlan p;
+  const int64_t most = std::max<int64_t>(2048, ((int64_t)512 << 20) / (2 * n) / kTile * kTile);
+  p.pieces = (int)((vocab + most - 1) / most);
+  p.piece = ceil_to((vocab + p.pieces - 1) / p.pieces, kTile);
+  p.pieces = (int)((vocab + p.piece - 1) / p.piece);
+  p.ld_g = ceil_to(std::min(p.piece, vocab), 64);
+  const int64_t tiles = ((n + kTile - 1) / kTile) * ((d + kTile - 1) / kTile);
+  const int64_t stages = (std::min(p.piece, vocab) + kSub * kHeadK - 1) / (kSub * kHeadK);
+  p.split = (int)std::max<int64_t>(1, std::min<int64_t>({74 / tiles, stages / 4, 16}));
+  p.ld_part = ceil_to(d, 4);
+  p.g_bytes = (size_t)ceil_to(n * p.ld_g * 2, 256);
+  p.part_bytes = p.pieces > 1 || p.split > 1 ? (size_t)p.split * n * p.ld_part * 4 : 0;
+  return p;
+}
+
+bool sizes_ok(int64_t n, int64_t d, int64_t vocab) {
+  const int64_t most = 0x7fffffffLL - 1024;
+  return n >= 0 && d >= 1 && vocab >= 1 && n <= most && d <= most && vocab <= most;
+}
+// What a matrix of rows x cols elements has to be for the copies: PRM_OK, or why not.
+int operand_code(const void* p, int64_t ld, int64_t cols) {
+  if (!p) return PRM_ERR_ARG;
+  if (ld < cols || ld >= ((int64_t)1 << 38)) return PRM_ERR_SHAPE;
+  return aligned16(p) && ld % 8 == 0 ? PRM_OK : PRM_ERR_ALIGN;
+}
+
+}  // namespace
+}  // namespace prm
+
+using namespace prm;
+
+extern "C" size_t prm_head_loss_scratch_bytes(int64_t n, int64_t d, int64_t vocab) {
+  if (n < 1 || !sizes_ok(n, d, vocab)) return 0;
+  const int64_t parts = 2 * ((vocab + kTile - 1) / kTile);
+  return (size_t)stats_rows(n, vocab) * ((size_t)parts * 8 + 4);
+}
+
+extern "C" int prm_head_loss(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int weight_transposed,
+                             const int64_t* labels, int64_t n, int64_t d, int64_t vocab, float* loss_out, float* lse_out,
+                             void* scratch, size_t scratch_bytes, void* cuda_stream) {
+  if (!sizes_ok(n, d, vocab)) return PRM_ERR_SHAPE;
+  if (n == 0) return PRM_OK;
+  if (!labels || !loss_out || !lse_out || !scratch) return PRM_ERR_ARG;
+  int code = operand_code(x, ld_x, d);
+  if (code == PRM_OK) code = operand_code(weight, ld_weight, weight_transposed ? d : vocab);
+  if (code != PRM_OK) return code;
+  if (((uintptr_t)loss_out | (uintptr_t)lse_out) % 4 != 0 || (uintptr_t)labels % 8 != 0 || !aligned16(scratch))
+    return PRM_ERR_ALIGN;
+  if (scratch_bytes < prm_head_loss_scratch_bytes(n, d, vocab)) return PRM_ERR_WORKSPACE;
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  const Operand w = {weight, weight_transposed ? vocab : d, weight_transposed ? d : vocab, ld_weight, !weight_transposed};
+  const int64_t step = stats_rows(n, vocab);
+  const int parts = (int)(2 * ((vocab + kTile - 1) / kTile));
+  for (int64_t r = 0; r < n; r += step) {
+    const int64_t rows = std::min(step, n - r);
+    HeadArgs a = {};
+    a.m = (int)rows;
+    a.n = (int)vocab;
+    a.split = 1;
+    a.labels = labels + r;
+    a.vocab = vocab;
+    a.part = (float2*)scratch;
+    a.at_label = (float*)(a.part + (size_t)parts * rows);
+    const Operand xr = {(const __nv_bfloat16*)x + r * ld_x, rows, d, ld_x, false};
+    code = launch_logits<kStats>(xr, w, a, d, stream);
+    if (code != PRM_OK) return code;
+    code = q8_code(launch_after(head_join_kernel, (unsigned)((rows + 31) / 32), 256, 0, stream, 0, a.part, parts, a.at_label,
+                                a.labels, vocab, (int)rows, loss_out + r, lse_out + r));
+    if (code != PRM_OK) return code;
+  }
+  return PRM_OK;
+}
+
+extern "C" size_t prm_head_loss_backward_scratch_bytes(int64_t n, int64_t d, int64_t vocab) {
+  if (n < 1 || !sizes_ok(n, d, vocab)) return 0;
+  const BackwardPlan p = backward_plan(n, d, vocab);
+  return 256 + p.g_bytes + p.part_bytes;
+}
+
+extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int64_t ld_x, const void* weight,
+                                      int64_t ld_weight, int weight_transposed, const int64_t* labels, const float* lse,
+                                      int64_t n, int64_t d, int64_t vocab, void* grad_x, int64_t ld_grad_x,
+                                      void* grad_weight, int64_t ld_grad_weight, void* scratch, size_t scratch_bytes,
+                                      void* cuda_stream) {
+  if (!sizes_ok(n, d, vocab)) return PRM_ERR_SHAPE;
+  const int64_t w_rows = weight_transposed ? vocab : d, w_cols = weight_transposed ? d : vocab;
+  if (grad_x && (ld_grad_x < d || ld_grad_x > ((int64_t)1 << 40))) return PRM_ERR_SHAPE;
+  if (grad_weight && (ld_grad_weight < w_cols || ld_grad_weight > ((int64_t)1 << 40))) return PRM_ERR_SHAPE;
+  if (((uintptr_t)grad_x | (uintptr_t)grad_weight) % 2 != 0) return PRM_ERR_ALIGN;
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  if (n == 0)                             // an empty sum
+    return !grad_weight ? PRM_OK : q8_code(cudaMemset2DAsync(grad_weight, (size_t)ld_grad_weight * 2, 0, (size_t)w_cols * 2,
+                                                             (size_t)w_rows, stream));
+  if (!grad_x && !grad_weight) return PRM_OK;
+  if (!grad_loss || !labels || !lse || !scratch) return PRM_ERR_ARG;
+  int code = operand_code(x, ld_x, d);
+  if (code == PRM_OK) code = operand_code(weight, ld_weight, w_cols);
+  if (code != PRM_OK) return code;
+  if (((uintptr_t)grad_loss | (uintptr_t)lse) % 4 != 0 || (uintptr_t)labels % 8 != 0 || ((uintptr_t)scratch & 255) != 0)
+    return PRM_ERR_ALIGN;
+  if (scratch_bytes < prm_head_loss_backward_scratch_bytes(n, d, vocab)) return PRM_ERR_WORKSPACE;
+  const BackwardPlan plan = backward_plan(n, d, vocab);
+  float* unit = (float*)scratch;
+  __nv_bfloat16* g = (__nv_bfloat16*)((char*)scratch + 256);
+  float* part = (float*)((char*)g + plan.g_bytes);
+  const Operand w = {weight, w_rows, w_cols, ld_weight, !weight_transposed};
+  code = q8_code(launch_after(head_unit_kernel, 1u, 1024, 0, stream, 0, grad_loss, labels, vocab, (int)n, unit));
+  const bool parted = plan.part_bytes > 0;
+  for (int64_t v0 = 0; v0 < vocab && code == PRM_OK; v0 += plan.piece) {
+    const int64_t wide = std::min(plan.piece, vocab - v0);
+    HeadArgs a = {};
+    a.m = (int)n;
+    a.n = (int)wide;
+    a.q_n0 = (int)v0;
+    a.split = 1;
+    a.labels = labels;
+    a.vocab = vocab;
+    a.lse = lse;
+    a.grad_loss = grad_loss;
+    a.g = g;
+    a.ld_g = plan.ld_g;
+    a.unit = unit;
+    code = launch_logits<kGrad>({x, n, d, ld_x, false}, w, a, d, stream);
+    if (code == PRM_OK && grad_x) {
+      HeadArgs b = {};
+      b.m = (int)n;
+      b.n = (int)d;
+      b.q_k0 = (int)v0;
+      b.split = plan.split;
+      b.unit = parted ? nullptr : unit;
+      b.out = parted ? (void*)part : grad_x;
+      b.ld_out = parted ? plan.ld_part : ld_grad_x;
+      b.split_stride = n * plan.ld_part;
+      b.out_fp32 = parted;
+      b.accumulate = v0 > 0;
+      const Operand gp = {g, n, wide, plan.ld_g, false}, wq = {weight, w_rows, w_cols, ld_weight, weight_transposed != 0};
+      code = weight_transposed ? launch_head<kStore, false, true>(gp, wq, b, wide, stream)
+                               : launch_head<kStore, false, false>(gp, wq, b, wide, stream);
+    }
+    if (code == PRM_OK && grad_weight) {
+      HeadArgs b = {};
+      b.split = 1;
+      b.unit = unit;
+      b.ld_out = ld_grad_weight;
+      const Operand gt = {g, n, wide, plan.ld_g, true}, xt = {x, n, d, ld_x, true};
+      if (weight_transposed) {
+        b.m = (int)wide;
+        b.n = (int)d;
+        b.out = (__nv_bfloat16*)grad_weight + v0 * ld_grad_weight;
+        code = launch_head<kStore, true, true>(gt, xt, b, n, stream);
+      } else {
+        b.m = (int)d;
+        b.n = (int)wide;
+        b.out = (__nv_bfloat16*)grad_weight + v0;
+        code = launch_head<kStore, true, true>(xt, gt, b, n, stream);
+      }
+    }
+  }
+  if (code == PRM_OK && grad_x && parted) {
+    const int64_t blocks = n * ((d + 255) / 256);
+    if (blocks > 0x7fffffffLL) return PRM_ERR_SHAPE;
+    code = q8_code(launch_after(head_sum_kernel, (unsigned)blocks, 256, 0, stream, 0, (const float*)part, plan.split,
+                                n * plan.ld_part, (int)n, (int)d, plan.ld_part, (const float*)unit, (__nv_bfloat16*)grad_x,
+                                ld_grad_x));
+  }
+  return code;
+}
