@@ -7,7 +7,7 @@
 //
 // Philox4x32-10 is the generator of Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as
 // 1, 2, 3" (SC 2011): ten rounds of two 32 x 32 -> 64 bit products, whose halves change places, under a key
-// that advances by a constant.  Four elements share one evaluation, 20 products: on 8192 x 8192 elements in
+// that advances by a constant (the rounds' keys come with the kernel's arguments).  Four elements share one evaluation, 20 products: on 8192 x 8192 elements in
 // bf16 the kernel of dropout.cu is held by memory, not by them.
 #pragma once
 
@@ -21,7 +21,7 @@ namespace prm {
 struct Drop {
   uint32_t threshold = 0;                  // a word below it drops its element
   float scale = 1.f;
-  uint32_t key0 = 0, key1 = 0;
+  uint2 key[10] = {};                      // of each round
   uint64_t offset = 0;
   const uint64_t* counter = nullptr;
 };
@@ -31,8 +31,8 @@ inline Drop make_drop(double p, uint64_t seed, uint64_t offset, const uint64_t* 
   Drop d;
   d.threshold = (uint32_t)std::min(std::nearbyint(p * 4294967296.0), 4294967295.0);
   d.scale = (float)(1.0 / (1.0 - p));
-  d.key0 = (uint32_t)seed;
-  d.key1 = (uint32_t)(seed >> 32);
+  for (uint32_t r = 0; r < 10; ++r)
+    d.key[r] = make_uint2((uint32_t)seed + r * 0x9E3779B9u, (uint32_t)(seed >> 32) + r * 0xBB67AE85u);
   d.offset = offset;
   d.counter = counter;
   return d;
@@ -40,19 +40,17 @@ inline Drop make_drop(double p, uint64_t seed, uint64_t offset, const uint64_t* 
 
 __device__ __forceinline__ uint64_t drop_number(const Drop& d) { return d.offset + (d.counter ? *d.counter : 0); }
 
-__device__ __forceinline__ uint4 philox(uint4 c, uint32_t k0, uint32_t k1) {
+__device__ __forceinline__ uint4 philox(uint4 c, const uint2 (&key)[10]) {
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t a = (uint64_t)c.x * 0xD2511F53u, b = (uint64_t)c.z * 0xCD9E8D57u;
-    c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ k0, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ k1, (uint32_t)a);
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
+    c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ key[r].x, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ key[r].y, (uint32_t)a);
   }
   return c;
 }
 // The words of the elements 4 quad .. 4 quad + 3 of a row.
 __device__ __forceinline__ uint4 drop_words(const Drop& d, uint64_t number, uint32_t row, uint32_t quad) {
-  return philox(make_uint4(quad, row, (uint32_t)number, (uint32_t)(number >> 32)), d.key0, d.key1);
+  return philox(make_uint4(quad, row, (uint32_t)number, (uint32_t)(number >> 32)), d.key);
 }
 // The product is rounded by itself (nothing is fused through the choice).
 __device__ __forceinline__ float dropped(const Drop& d, uint32_t word, float v) {
@@ -79,7 +77,10 @@ __device__ __forceinline__ void drop_oct(const Drop& d, uint64_t number, uint32_
     }
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = make_float2(dropped(d, w[2 * k], v[k].x), dropped(d, w[2 * k + 1], v[k].y));
+  for (int k = 0; k < 4; ++k) {
+    const float2 scaled = mul2(v[k], make_float2(d.scale, d.scale));
+    v[k] = make_float2(w[2 * k] >= d.threshold ? scaled.x : 0.f, w[2 * k + 1] >= d.threshold ? scaled.y : 0.f);
+  }
 }
 
 }  // namespace prm

@@ -35,27 +35,14 @@ __device__ __forceinline__ void store_weight(void* out, int fp32, int64_t at, fl
   else reinterpret_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(v);
 }
 
-// Two sums over a group of TPR of the block's threads; `red`: a pair of words per warp of the group.
-template <int TPR, int BLOCK>
-__device__ __forceinline__ void row_sum2(float& p, float& q, float2* red) {
-  p = group_sum<(TPR < 32 ? TPR : 32)>(p);
-  q = group_sum<(TPR < 32 ? TPR : 32)>(q);
-  if constexpr (TPR > 32) {
-    const int group = threadIdx.x / TPR, lane = threadIdx.x % 32;
-    if (lane == 0) red[threadIdx.x % TPR / 32] = make_float2(p, q);
-    if constexpr (TPR == BLOCK) __syncthreads();
-    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
-    const float2 s = lane < TPR / 32 ? red[lane] : make_float2(0.f, 0.f);
-    p = warp_sum(s.x);
-    q = warp_sum(s.y);
-  }
-}
+// Blocks per SM of the kernel below: 128 registers per thread with two octs, 85 with one (64 in blocks of 1024).
+constexpr int layernorm_grad_blocks(int nv, int block) { return block == 256 ? (nv == 1 ? 3 : 2) : 1; }
 
 template <typename IO, int NV, int TPR, int BLOCK, bool DROP, bool SHIFT>
-__global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) layernorm_grad_kernel(const LayerNormGradArgs a) {
+__global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks(NV, BLOCK)) layernorm_grad_kernel(const LayerNormGradArgs a) {
   constexpr int kRows = BLOCK / TPR, kWide = NV * TPR * 8;
   __shared__ float sums[kRows > 1 ? kRows : 1][kRows > 1 ? kWide : 1];
-  __shared__ float2 red[2][kRows][TPR > 32 ? TPR / 32 : 1];
+  __shared__ __align__(16) float red[2][kRows][TPR > 32 ? TPR / 32 * 2 : 1];
   grid_wait();
   grid_trigger();
   const int64_t group = blockIdx.x / (unsigned)a.parts, row0 = group * a.rows_per_group;
@@ -66,28 +53,37 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) layernorm_grad_kernel(con
   const int shift = SHIFT ? oct_shift(reinterpret_cast<const IO*>(a.h) + (row0 + first + line) * a.ld_h) : 0;
   const int c0 = (int)(threadIdx.x % TPR) * 8 - shift;
   const uint64_t number = DROP ? drop_number(a.drop) : 0;
+  const float over = 1.f / (float)a.cols;
   float2 w[NV][4], gw[NV][4], gb[NV][4];
   Oct<IO> next[NV][3];
   float next_mean = 0.f, next_rstd = 0.f;
   auto fetch = [&](int64_t local) {
-    if (local >= rows) return;
-    const int64_t row = row0 + local;
-    next_mean = a.mean[row];
-    next_rstd = a.rstd[row];
-    const OctRow<IO> gyr(a.gy, row, a.rows, a.ld_gy, a.cols), hr(a.h, row, a.rows, a.ld_h, a.cols);
-    const OctRow<IO> ghr(a.gh ? a.gh : a.h, row, a.rows, a.gh ? a.ld_gh : a.ld_h, a.cols);
+    if (local < rows) {
+      const int64_t row = row0 + local;
+      next_mean = a.mean[row];
+      next_rstd = a.rstd[row];
+      if constexpr (SHIFT) {
+        const OctRow<IO> gyr(a.gy, row, a.rows, a.ld_gy, a.cols), hr(a.h, row, a.rows, a.ld_h, a.cols);
+        const OctRow<IO> ghr(a.gh ? a.gh : a.h, row, a.rows, a.gh ? a.ld_gh : a.ld_h, a.cols);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = c0 + v * TPR * 8;
-      if (c < a.cols) {
-        if constexpr (SHIFT) {
+        for (int v = 0; v < NV; ++v) {
+          const int c = c0 + v * TPR * 8;
           gyr.load(c, a.cols, next[v][0]);
           hr.load(c, a.cols, next[v][1]);
           if (a.gh) ghr.load(c, a.cols, next[v][2]);
-        } else {
-          next[v][0].load_stream(gyr.p + c);
-          next[v][1].load_stream(hr.p + c);
-          if (a.gh) next[v][2].load_stream(ghr.p + c);
+        }
+      } else {
+        const IO* gy = reinterpret_cast<const IO*>(a.gy) + row * a.ld_gy;
+        const IO* h = reinterpret_cast<const IO*>(a.h) + row * a.ld_h;
+        const IO* gh = reinterpret_cast<const IO*>(a.gh) + row * a.ld_gh;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int c = c0 + v * TPR * 8;
+          if (c < a.cols) {
+            next[v][0].load_stream(gy + c);
+            next[v][1].load_stream(h + c);
+            if (a.gh) next[v][2].load_stream(gh + c);
+          }
         }
       }
     }
@@ -108,41 +104,41 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) layernorm_grad_kernel(con
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int k = 0; k < 3; ++k) now[v][k] = next[v][k];
-    const float mean = next_mean, rstd = next_rstd;
+    const float2 rs2 = make_float2(next_rstd, next_rstd), off2 = make_float2(-next_mean * next_rstd, -next_mean * next_rstd);
     fetch(local + step);
-    const float2 nm2 = make_float2(-mean, -mean), rs2 = make_float2(rstd, rstd);
     float2 sg2 = make_float2(0.f, 0.f), sx2 = sg2;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = c0 + v * TPR * 8;
       if (c < cols) {
-        float2 gy[4], x[4];
-        now[v][0].get(gy);
-        now[v][1].get(x);
+        float2 g[4], xhat[4];
+        now[v][0].get(g);
+        now[v][1].get(xhat);
         if constexpr (SHIFT) {
-          clear_outside(c, cols, gy);
-          clear_outside(c, cols, x);
+          clear_outside(c, cols, g);
+          clear_outside(c, cols, xhat);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float2 xhat = mul2(add2(x[e], nm2), rs2), g = mul2(gy[e], w[v][e]);
-          gw[v][e] = fma2(gy[e], xhat, gw[v][e]);
-          gb[v][e] = add2(gb[v][e], gy[e]);
-          sg2 = add2(sg2, g);
-          sx2 = fma2(g, xhat, sx2);
+          xhat[e] = fma2(xhat[e], rs2, off2);
+          gw[v][e] = fma2(g[e], xhat[e], gw[v][e]);
+          gb[v][e] = add2(gb[v][e], g[e]);
+          g[e] = mul2(g[e], w[v][e]);
+          sg2 = add2(sg2, g[e]);
+          sx2 = fma2(g[e], xhat[e], sx2);
         }
       }
     }
-    float sg = sg2.x + sg2.y, sx = sx2.x + sx2.y;
-    row_sum2<TPR, BLOCK>(sg, sx, red[turn][line]);
-    const float mg = sg / (float)a.cols, mx = sx / (float)a.cols;
+    float total[2] = {sg2.x + sg2.y, sx2.x + sx2.y};
+    row_sums<TPR, BLOCK>(total, red[turn][line]);
+    const float2 mg2 = make_float2(-total[0] * over, -total[0] * over), mx2 = make_float2(-total[1] * over, -total[1] * over);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = c0 + v * TPR * 8;
       if (c < cols) {
-        float2 gy[4], x[4], o[4];
-        now[v][0].get(gy);
-        now[v][1].get(x);
+        float2 g[4], xhat[4], o[4];
+        now[v][0].get(g);
+        now[v][1].get(xhat);
         if (a.gh) {
           now[v][2].get(o);
         } else {
@@ -150,11 +146,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) layernorm_grad_kernel(con
           for (int e = 0; e < 4; ++e) o[e] = make_float2(0.f, 0.f);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 xhat = mul2(add2(x[e], nm2), rs2);
-          const float2 d = fma2(gy[e], w[v][e], fma2(xhat, make_float2(-mx, -mx), make_float2(-mg, -mg)));
-          o[e] = fma2(d, rs2, o[e]);
-        }
+        for (int e = 0; e < 4; ++e) o[e] = fma2(fma2(fma2(xhat[e], rs2, off2), mx2, fma2(g[e], w[v][e], mg2)), rs2, o[e]);
         IO* gr = reinterpret_cast<IO*>(a.gr) + row * a.ld_gr;
         if constexpr (SHIFT) {
           store_part(gr, c, cols, o);
@@ -214,7 +206,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) layernorm_grad_kernel(con
 // the sums is collected in its line of the scratch (each thread its own columns).
 template <typename IO, int THREADS>
 __global__ void __launch_bounds__(THREADS) layernorm_grad_single_kernel(const LayerNormGradArgs a) {
-  __shared__ float2 red[2][THREADS / 32];
+  __shared__ __align__(16) float red[2][THREADS / 32 * 2];
   grid_wait();
   grid_trigger();
   const int64_t group = blockIdx.x / (unsigned)a.parts, row0 = group * a.rows_per_group;
@@ -244,8 +236,9 @@ __global__ void __launch_bounds__(THREADS) layernorm_grad_single_kernel(const La
         }
       }
     }
-    row_sum2<THREADS, THREADS>(sg, sx, red[turn]);
-    const float mg = sg / (float)a.cols, mx = sx / (float)a.cols;
+    float total[2] = {sg, sx};
+    row_sums<THREADS, THREADS>(total, red[turn]);
+    const float mg = total[0] / (float)a.cols, mx = total[1] / (float)a.cols;
     for (int c = threadIdx.x * 4; c < a.cols; c += THREADS * 4) {
       uint4 w = make_uint4(~0u, ~0u, ~0u, ~0u);
       if (gxp) w = drop_words(a.drop, number, (uint32_t)row, (uint32_t)c >> 2);
@@ -264,9 +257,11 @@ __global__ void __launch_bounds__(THREADS) layernorm_grad_single_kernel(const La
   }
 }
 
-// The blocks' lines added: 32 columns of one of the two gradients of a group per block, eight lines at a time.
-__global__ void __launch_bounds__(256) layernorm_grad_sum_kernel(const LayerNormGradArgs a, int chunks) {
-  __shared__ float s[8][32];
+// The blocks' lines added: 32 columns of one of the two gradients of a group per block, a line per warp at a time (32 warps
+// for many lines: each goes through few, so that all are under way together).
+template <int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) layernorm_grad_sum_kernel(const LayerNormGradArgs a, int chunks) {
+  __shared__ float s[WARPS][33];
   grid_wait();
   grid_trigger();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -277,34 +272,39 @@ __global__ void __launch_bounds__(256) layernorm_grad_sum_kernel(const LayerNorm
   if (!out) return;
   float sum = 0.f;
   if (c < a.cols) {
-#pragma unroll 8
-    for (int l = warp; l < a.parts; l += 8) sum += __ldcg(a.part + ((group * a.parts + l) * 2 + which) * a.cols + c);
+    const float* p = a.part + (group * a.parts * 2 + which) * a.cols + c;
+#pragma unroll 10
+    for (int l = warp; l < a.parts; l += WARPS) sum += __ldcg(p + (int64_t)l * 2 * a.cols);
   }
   s[warp][lane] = sum;
   __syncthreads();
-  if (warp == 0 && c < a.cols) {
+  // warp w adds columns w, w + WARPS, ...: a line per lane
 #pragma unroll
-    for (int k = 1; k < 8; ++k) sum += s[k][lane];
-    store_weight(out, a.affine.fp32, group * a.cols + c, sum);
+  for (int k = warp; k < 32; k += WARPS) {
+    const float v = warp_sum(lane < WARPS ? s[lane][k] : 0.f);
+    const int64_t at = c - lane + k;
+    if (lane == 0 && at < a.cols) store_weight(out, a.affine.fp32, group * a.cols + at, v);
   }
 }
 
 int launch_sum(const LayerNormGradArgs& a, int64_t groups, cudaStream_t stream) {
   if (!a.gw && !a.gb) return PRM_OK;
   const int chunks = (a.cols + 31) / 32;
-  return q8_code(launch_after(layernorm_grad_sum_kernel, (unsigned)(groups * chunks * 2), 256, 0, stream, 0, a, chunks));
+  const unsigned blocks = (unsigned)(groups * chunks * 2);
+  return q8_code(a.parts > 32 ? launch_after(layernorm_grad_sum_kernel<32>, blocks, 1024, 0, stream, 0, a, chunks)
+                              : launch_after(layernorm_grad_sum_kernel<8>, blocks, 256, 0, stream, 0, a, chunks));
 }
 
 template <typename IO, bool DROP, bool SHIFT, int NV, int TPR, int BLOCK>
 int launch_layernorm_grad(LayerNormGradArgs a, int64_t groups, cudaStream_t stream) {
-  a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, BLOCK / TPR, SHIFT);
+  a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, BLOCK / TPR, 148 * layernorm_grad_blocks(NV, BLOCK), SHIFT);
   const int code = q8_code(launch_after(layernorm_grad_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT>, (unsigned)(groups * a.parts),
                                         BLOCK, 0, stream, 0, a));
   return code == PRM_OK && a.parts > 1 ? launch_sum(a, groups, stream) : code;
 }
 template <typename IO>
 int launch_layernorm_grad_single(LayerNormGradArgs a, int64_t groups, cudaStream_t stream) {
-  a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, 1, false);
+  a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, 1, 444, false);
   const int code = a.cols <= 1024
                        ? q8_code(launch_after(layernorm_grad_single_kernel<IO, 256>, (unsigned)(groups * a.parts), 256, 0,
                                               stream, 0, a))
@@ -316,13 +316,16 @@ int launch_layernorm_grad_single(LayerNormGradArgs a, int64_t groups, cudaStream
 template <typename IO, bool DROP, bool SHIFT>
 int run_layernorm_grad(const LayerNormGradArgs& a, int64_t groups, cudaStream_t stream) {
   const int64_t c = (int64_t)a.cols + (SHIFT ? 7 : 0);
+  // Two octs per thread halve what a row's reduction costs each; of 32-bit elements they leave the registers.
+  constexpr int NV = sizeof(IO) == 2 ? 2 : 1, T = NV == 2 ? 1 : 2;
   if (c <= 64) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 8, 256>(a, groups, stream);
+  if (c <= 128) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 16, 256>(a, groups, stream);
   if (c <= 256) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 32, 256>(a, groups, stream);
-  if (c <= 512) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 64, 256>(a, groups, stream);
-  if (c <= 1024) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 128, 256>(a, groups, stream);
-  if (c <= 2048) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 256, 256>(a, groups, stream);
-  if (c <= 4096) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 512, 512>(a, groups, stream);
-  if (c <= 8192) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 1024, 1024>(a, groups, stream);
+  if (c <= 512) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 32 * T, 256>(a, groups, stream);
+  if (c <= 1024) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 64 * T, 256>(a, groups, stream);
+  if (c <= 2048) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 128 * T, 256>(a, groups, stream);
+  if (c <= 4096) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 256 * T, 256 * T>(a, groups, stream);
+  if (c <= 8192) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 512 * T, 512 * T>(a, groups, stream);
   return launch_layernorm_grad_single<IO>(a, groups, stream);
 }
 template <typename IO>
