@@ -34,9 +34,17 @@ constexpr uint32_t kBoxBytes = 128 * 128;        // 128 rows of one k-block
 constexpr uint32_t kStageBytes = 2 * kSub * kBoxBytes;
 constexpr uint32_t kPatchBytes = 32 * 64;        // a warp's 32 rows of 64 bytes on their way out
 constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kPatchBytes;
+constexpr int kMaxStages = 6;
+constexpr int kFewRows = 64;                     // rows that kFew takes (100 x 4096 x 32768: 72 us, the other form 68)
+// The logits' sums are taken out of tensor memory every 1024 k and added in registers: the accumulator cuts off what
+// falls below its last bit at each of its steps (16 k), which over 4096 k puts a logit of the size 1 off by 1e-5.
+constexpr int kChunk = 8;                        // stages
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-enum Epi { kStats, kGrad, kStore };
+// kStats: x (rows) times W (columns).  kFew: the same for few rows, the other way round (the rows are the instruction's N, so
+// that it costs them no more than it has to, and W's bytes have most of shared memory).
+enum Epi { kStats, kFew, kGrad, kStore };
+__host__ __device__ constexpr bool chunked(int epi) { return epi == kStats || epi == kFew; }
 
 struct HeadArgs {
   int m, n, kblocks;               // of this product: rows, columns, ceil(k / 64)
@@ -44,6 +52,8 @@ struct HeadArgs {
   int m_tiles, n_tiles, tiles;     // tiles: of all splits of k
   int band;                        // m-tiles that are walked through together
   int split;                       // parts of k (kStore)
+  int q_tile, stages;              // kFew: N of the instruction, stages that fit
+  uint32_t stage_bytes;
   int* status;
   // kStats, kGrad
   const int64_t* labels;
@@ -56,6 +66,7 @@ struct HeadArgs {
   int64_t ld_g;
   // kGrad, kStore
   const float* unit;               // c; null: 1
+  float* unit_out;                 // kGrad: c is computed by every block, and left here (kUnitRows rows at most)
   void* out;
   int64_t ld_out, split_stride;
   int out_fp32, accumulate;        // accumulate: fp32 out += (16-byte aligned)
@@ -91,37 +102,54 @@ __device__ __forceinline__ int label_column(const HeadArgs& a, int64_t label, in
 }
 
 // 128 columns of the lane's row: what they add to the softmax, and the label's logit.
-__device__ __forceinline__ void stats_tile(const HeadArgs& a, uint32_t taddr, int row, int n0, int column) {
-  float top = -INFINITY, top2 = 0.f, sum = 0.f;            // top2: in base 2, 0 while all are -infinity
+__device__ __forceinline__ void stats_tile(const HeadArgs& a, float (&v)[128], int row, int n0, int column) {
   const int label = row < a.m ? label_column(a, a.labels[row], n0) : -1;
-#pragma unroll 1
-  for (int k = 0; k < 4; ++k) {
-    const int wide = a.n - (n0 + k * 32);
-    if (wide <= 0) break;
-    uint32_t r[32];
-    tmem_ld32(taddr + k * 32, r);
-    tmem_wait_ld();
-    float v[32], here = top;
+  const int wide = a.n - n0;
+  if (wide < 128) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      v[j] = j < wide ? __uint_as_float(r[j]) : -INFINITY;
-      here = fmaxf(here, v[j]);
-    }
-    const float here2 = here == -INFINITY ? 0.f : here * kLog2e;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 32; ++j) s[j & 3] += ex2(fmaf(v[j], kLog2e, -here2));
-    sum = (top == -INFINITY ? sum : sum * ex2(top2 - here2)) + ((s[0] + s[1]) + (s[2] + s[3]));
-    top = here;
-    top2 = here2;
-    const int at = label - k * 32;
-    if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (at == j) a.at_label[row] = v[j];
-    }
+    for (int j = 0; j < 128; ++j)
+      if (j >= wide) v[j] = -INFINITY;
   }
-  if (row < a.m) a.part[(int64_t)column * a.m + row] = make_float2(top == -INFINITY ? top : top2, sum);
+  float t[4] = {v[0], v[1], v[2], v[3]}, s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 4; j < 128; ++j) t[j & 3] = fmaxf(t[j & 3], v[j]);
+  const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+  const float top2 = top == -INFINITY ? 0.f : top * kLog2e;         // in base 2
+#pragma unroll
+  for (int j = 0; j < 128; ++j) s[j & 3] += ex2(fmaf(v[j], kLog2e, -top2));
+  if (__any_sync(0xffffffffu, label >= 0)) {
+#pragma unroll
+    for (int j = 0; j < 128; ++j)
+      if (label == j) a.at_label[row] = v[j];
+  }
+  if (row < a.m)
+    a.part[(int64_t)column * a.m + row] = make_float2(top == -INFINITY ? top : top2, (s[0] + s[1]) + (s[2] + s[3]));
+}
+
+// kFew: 32 columns (lanes) of 16 rows from n0 on.  They pass through shared memory, so that a lane gets 16 columns of one row.
+__device__ __forceinline__ void few_tile(const HeadArgs& a, const float* v, float* patch, int m0, int n0) {
+  const int lane = threadIdx.x & 31, r = lane & 15, part = lane >> 4, row = n0 + r;
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < 16; ++k) patch[k * 32 + (lane ^ k)] = m0 + lane < a.m ? v[k] : -INFINITY;
+  __syncwarp();
+  float t[16], top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    t[j] = patch[r * 32 + ((part * 16 + j) ^ r)];
+    top = fmaxf(top, t[j]);
+  }
+  top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+  const float top2 = top == -INFINITY ? 0.f : top * kLog2e;
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) s += ex2(fmaf(t[j], kLog2e, -top2));
+  s += __shfl_xor_sync(0xffffffffu, s, 16);
+  if (row < a.n && part == 0) {
+    a.part[(int64_t)(m0 / 32) * a.n + row] = make_float2(top == -INFINITY ? top : top2, s);
+    const int64_t c = a.labels[row] - m0;
+    if (c >= 0 && c < 32 && c + m0 < a.vocab) a.at_label[row] = patch[r * 32 + ((int)c ^ r)];
+  }
 }
 
 // 16-byte chunk c of row r of a warp's patch, where neither writing rows nor reading them back meets a bank twice.
@@ -129,15 +157,31 @@ __device__ __forceinline__ uint4* patch_at(uint8_t* patch, int r, int c) {
   return reinterpret_cast<uint4*>(patch + (r >> 1) * 128 + (r & 1) * 64 + ((c ^ ((r >> 1) & 3)) << 4));
 }
 
+// c = max |gl| over the rows with a label, 1 if that is 0 or no number: THREADS threads' share.
+template <int THREADS>
+__device__ __forceinline__ float unit_share(const float* grad_loss, const int64_t* labels, int64_t vocab, int rows, int thread) {
+  float top = 0.f;
+#pragma unroll 4
+  for (int i = thread; i < rows; i += THREADS) {
+    const int64_t l = labels[i];
+    const float v = grad_loss[i];
+    if (l >= 0 && l < vocab) top = fmaxf(top, fabsf(v));
+  }
+  return group_top(top);
+}
+__device__ __forceinline__ float unit_of(float top) { return top > 0.f && top < INFINITY ? top : 1.f; }
+constexpr int kUnitRows = 2048;                  // for more it has a launch of its own
+
 // 128 columns of the lane's row of G.
-__device__ __forceinline__ void grad_tile(const HeadArgs& a, uint32_t taddr, uint8_t* patch, int m0, int n0, int rows) {
+__device__ __forceinline__ void grad_tile(const HeadArgs& a, uint32_t taddr, uint8_t* patch, int m0, int n0, int rows,
+                                          float unit) {
   const int lane = threadIdx.x & 31, row = m0 + lane;
   float factor = 0.f, lse2 = 0.f;
   int label = -1;
   if (row < a.m) {
     const int64_t l = a.labels[row];
     if (l >= 0 && l < a.vocab) {
-      factor = __fdiv_rn(a.grad_loss[row], *a.unit);
+      factor = __fdiv_rn(a.grad_loss[row], unit);
       lse2 = a.lse[row] * kLog2e;
       label = label_column(a, l, n0);
     }
@@ -245,7 +289,7 @@ template <int EPI, bool P_MN, bool Q_MN>
 __global__ void __launch_bounds__(kThreads, 1)
 head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const HeadArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kStages], empty[kStages], tfull[2], tempty[2];
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -254,9 +298,12 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int stages = EPI == kFew ? a.stages : kStages;
+  const uint32_t stage_bytes = EPI == kFew ? a.stage_bytes : kStageBytes;
+  const uint32_t q_box = EPI == kFew ? (uint32_t)a.q_tile / 2 * 128 : kBoxBytes;      // bytes of one k-block of Q
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < stages; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
@@ -292,14 +339,14 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
         tile_origin(a, t, split, m0, n0);
         split_range(a, split, s0, s1);
         m0 += (int)rank * 128;
-        n0 += (int)rank * 128 + a.q_n0;
+        n0 += (EPI == kFew ? (int)rank * a.q_tile / 2 : (int)rank * 128) + a.q_n0;
         for (int kt = s0; kt < s1; ++kt, ++it) {
-          const int s = it % kStages;
-          if (!mbar_wait(&empty[s], ((it / kStages) & 1) ^ 1, abort_flag, status)) { ok = false; break; }
-          uint8_t* sp = smem + (size_t)s * kStageBytes;
+          const int s = it % stages;
+          if (!mbar_wait(&empty[s], ((it / stages) & 1) ^ 1, abort_flag, status)) { ok = false; break; }
+          uint8_t* sp = smem + (size_t)s * stage_bytes;
           uint8_t* sq = sp + kSub * kBoxBytes;
           const int subs = min(kSub, a.kblocks - kt * kSub);
-          if (rank == 0) mbar_expect_tx(&full[s], (uint32_t)subs * 4 * kBoxBytes);   // both CTAs' bytes
+          if (rank == 0) mbar_expect_tx(&full[s], (uint32_t)subs * 2 * (kBoxBytes + q_box));   // both CTAs' bytes
           const uint32_t bar = lead_full + 8u * s;
 #pragma unroll
           for (int j = 0; j < kSub; ++j) {
@@ -316,7 +363,7 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
                 tma_load_pair(sq + j * kBoxBytes, &map_q, bar, n0, a.q_k0 + k0);
                 tma_load_pair(sq + j * kBoxBytes + kBoxBytes / 2, &map_q, bar, n0 + 64, a.q_k0 + k0);
               } else {
-                tma_load_pair(sq + j * kBoxBytes, &map_q, bar, a.q_k0 + k0, n0);
+                tma_load_pair(sq + j * q_box, &map_q, bar, a.q_k0 + k0, n0);
               }
             }
           }
@@ -324,77 +371,153 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
       }
       // Copies in flight must land before shared memory is released; the leader sees both CTAs'.
       if (rank == 0) {
-        for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j) {
+        for (uint32_t j = it > stages ? it - stages : 0; j < it; ++j) {
           const uint64_t t0 = global_ns();
-          while (!mbar_try_wait(&full[j % kStages], (j / kStages) & 1) && global_ns() - t0 < 1000000ull) {
+          while (!mbar_try_wait(&full[j % stages], (j / stages) & 1) && global_ns() - t0 < 1000000ull) {
           }
         }
       }
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      constexpr uint32_t idesc = idesc_bf16(kTile, kTile, P_MN, Q_MN);
+      const uint32_t idesc = idesc_bf16(kTile, EPI == kFew ? a.q_tile : kTile, P_MN, Q_MN);
       constexpr uint32_t kStepP = P_MN ? 128 : 2, kStepQ = Q_MN ? 128 : 2;    // 16 k, in units of 16 bytes
       uint32_t it = 0, acc = 0;
       bool ok = true;
       const uint32_t smem0 = smem_u32(smem);
-      for (int t = pair; t < a.tiles && ok; t += pairs, ++acc) {
+      for (int t = pair; t < a.tiles && ok; t += pairs) {
         int split, m0, n0, s0, s1;
         tile_origin(a, t, split, m0, n0);
         split_range(a, split, s0, s1);
-        const uint32_t ab = acc & 1;
-        if (!mbar_wait(&tempty[ab], ((acc >> 1) & 1) ^ 1, abort_flag, status)) break;
-        tcgen05_after_sync();
-        const uint32_t d = tmem + ab * kTile;
-        for (int kt = s0; kt < s1; ++kt, ++it) {
-          const int s = it % kStages;
-          if (!mbar_wait(&full[s], (it / kStages) & 1, abort_flag, status)) { ok = false; break; }
+        for (int c0 = s0; c0 < s1 && ok; c0 += kChunk, ++acc) {
+          const int c1 = chunked(EPI) ? min(c0 + kChunk, s1) : s1;
+          const uint32_t ab = acc & 1;
+          if (!mbar_wait(&tempty[ab], ((acc >> 1) & 1) ^ 1, abort_flag, status)) { ok = false; break; }
           tcgen05_after_sync();
-          const uint32_t sp = smem0 + (uint32_t)s * kStageBytes, sq = sp + kSub * kBoxBytes;
-          const int subs = min(kSub, a.kblocks - kt * kSub);
+          const uint32_t d = tmem + ab * kTile;
+          for (int kt = c0; kt < c1; ++kt, ++it) {
+            const int s = it % stages;
+            if (!mbar_wait(&full[s], (it / stages) & 1, abort_flag, status)) { ok = false; break; }
+            tcgen05_after_sync();
+            const uint32_t sp = smem0 + (uint32_t)s * stage_bytes, sq = sp + kSub * kBoxBytes;
+            const int subs = min(kSub, a.kblocks - kt * kSub);
 #pragma unroll
-          for (int j = 0; j < kSub; ++j) {
-            if (j < subs) {
-              const uint64_t dp = P_MN ? desc_mn_major(sp + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sp + j * kBoxBytes);
-              const uint64_t dq = Q_MN ? desc_mn_major(sq + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sq + j * kBoxBytes);
+            for (int j = 0; j < kSub; ++j) {
+              if (j < subs) {
+                const uint64_t dp = P_MN ? desc_mn_major(sp + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sp + j * kBoxBytes);
+                const uint64_t dq = Q_MN ? desc_mn_major(sq + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sq + j * q_box);
 #pragma unroll
-              for (int i = 0; i < kHeadK / 16; ++i)
-                umma_bf16_pair(d, dp + kStepP * i, dq + kStepQ * i, idesc, (uint32_t)(kt > s0) | (uint32_t)((j | i) != 0));
+                for (int i = 0; i < kHeadK / 16; ++i)
+                  umma_bf16_pair(d, dp + kStepP * i, dq + kStepQ * i, idesc, (uint32_t)(kt > c0) | (uint32_t)((j | i) != 0));
+              }
             }
+            umma_commit_both(smem_u32(&empty[s]));
           }
-          umma_commit_both(smem_u32(&empty[s]));
+          if (ok) umma_commit_both(smem_u32(&tfull[ab]));
+          if (!chunked(EPI)) {
+            ++acc;
+            break;
+          }
         }
-        if (ok) umma_commit_both(smem_u32(&tfull[ab]));
       }
     }
   } else {
     const int quad = warp & 3, half = (warp - 2) >> 2;
-    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * 128);
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
     const uint32_t lead_tempty = cluster_map(smem_u32(&tempty[0]), 0);
-    uint8_t* patch = smem + (size_t)kStages * kStageBytes + (warp - 2) * kPatchBytes;
-    const float unit = EPI == kStore && a.unit ? *a.unit : 1.f;
+    uint8_t* patch = smem + (size_t)stages * stage_bytes + (warp - 2) * kPatchBytes;
+    float unit = (EPI == kStore || EPI == kGrad) && a.unit ? *a.unit : 1.f;
+    if constexpr (EPI == kGrad) {
+      if (a.unit_out) {
+        float* red = reinterpret_cast<float*>(smem + (size_t)stages * stage_bytes);        // the patches
+        const float share = unit_share<kEpiWarps * 32>(a.grad_loss, a.labels, a.vocab, a.m, (int)threadIdx.x - 64);
+        if (lane == 0) red[warp - 2] = share;
+        asm volatile("bar.sync 1, %0;" ::"n"(kEpiWarps * 32) : "memory");
+        unit = 0.f;
+#pragma unroll
+        for (int k = 0; k < kEpiWarps; ++k) unit = fmaxf(unit, red[k]);
+        unit = unit_of(unit);
+        asm volatile("bar.sync 1, %0;" ::"n"(kEpiWarps * 32) : "memory");
+        if (blockIdx.x == 0 && threadIdx.x == 64) *a.unit_out = unit;
+      }
+    }
     uint32_t acc = 0;
-    for (int t = pair; t < a.tiles; t += pairs, ++acc) {
-      const uint32_t ab = acc & 1;
-      int split, m0, n0;
+    bool ok = true;
+    for (int t = pair; t < a.tiles && ok; t += pairs) {
+      int split, m0, n0, s0, s1;
       tile_origin(a, t, split, m0, n0);
       const int column = (n0 / kTile) * 2 + half;
       m0 += (int)rank * 128 + quad * 32;                  // this warp's rows and columns
-      n0 += half * 128;
-      const bool got = mbar_wait(&tfull[ab], (acc >> 1) & 1, abort_flag, status);
-      if (!__all_sync(0xffffffffu, got)) break;
-      tcgen05_after_sync();
-      const int rows = min(32, a.m - m0);
-      const uint32_t taddr = trow + ab * kTile;
-      if constexpr (EPI == kStats) stats_tile(a, taddr, m0 + lane, n0, column);
-      if constexpr (EPI == kGrad) grad_tile(a, taddr, patch, m0, n0, rows);
-      if constexpr (EPI == kStore) {
-        if (a.out_fp32) store_tile<float>(a, taddr, patch, split, m0, n0, rows, unit);
-        else store_tile<__nv_bfloat16>(a, taddr, patch, split, m0, n0, rows, unit);
+      // The accumulator is the next product's as soon as all warps of the pair have read it.
+      auto wait = [&]() {
+        const bool got = mbar_wait(&tfull[acc & 1], (acc >> 1) & 1, abort_flag, status);
+        ok = __all_sync(0xffffffffu, got);
+        tcgen05_after_sync();
+        return ok;
+      };
+      auto release = [&]() {
+        tcgen05_before_sync();
+        __syncwarp();
+        if (lane == 0) arrive_cluster(lead_tempty + 8u * (acc & 1));
+        ++acc;
+      };
+      if constexpr (EPI == kStats) {
+        float v[128];
+#pragma unroll
+        for (int j = 0; j < 128; ++j) v[j] = 0.f;
+        split_range(a, split, s0, s1);
+#pragma unroll 1
+        for (int c = s0; c < s1; c += kChunk) {
+          if (!wait()) break;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            uint32_t r[16];
+            tmem_ld16(trow + (acc & 1) * kTile + half * 128 + k * 16, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[k * 16 + j] += __uint_as_float(r[j]);
+          }
+          release();
+        }
+        if (ok) stats_tile(a, v, m0 + lane, n0 + half * 128, column);
+      } else if constexpr (EPI == kFew) {
+        float v[kFewRows / 2];                            // every other 16 of the rows
+#pragma unroll
+        for (int j = 0; j < kFewRows / 2; ++j) v[j] = 0.f;
+        split_range(a, split, s0, s1);
+#pragma unroll 1
+        for (int c = s0; c < s1; c += kChunk) {
+          if (!wait()) break;
+#pragma unroll
+          for (int g = 0; g < kFewRows / 32; ++g) {
+            if ((g * 2 + half) * 16 < a.q_tile) {
+              uint32_t r[16];
+              tmem_ld16(trow + (acc & 1) * kTile + (g * 2 + half) * 16, r);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) v[g * 16 + j] += __uint_as_float(r[j]);
+            }
+          }
+          release();
+        }
+        if (ok) {
+#pragma unroll
+          for (int g = 0; g < kFewRows / 32; ++g)
+            if ((g * 2 + half) * 16 < a.q_tile)
+              few_tile(a, v + g * 16, reinterpret_cast<float*>(patch), m0, n0 + (g * 2 + half) * 16);
+        }
+      } else {
+        if (!wait()) break;
+        const int rows = min(32, a.m - m0);
+        const uint32_t taddr = trow + (acc & 1) * kTile + half * 128;
+        n0 += half * 128;
+        if constexpr (EPI == kGrad) grad_tile(a, taddr, patch, m0, n0, rows, unit);
+        if constexpr (EPI == kStore) {
+          if (a.out_fp32) store_tile<float>(a, taddr, patch, split, m0, n0, rows, unit);
+          else store_tile<__nv_bfloat16>(a, taddr, patch, split, m0, n0, rows, unit);
+        }
+        release();
       }
-      tcgen05_before_sync();
-      __syncwarp();
-      if (lane == 0) arrive_cluster(lead_tempty + 8u * ab);
     }
   }
   // Neither CTA leaves while its partner can still touch its shared or tensor memory.
@@ -408,58 +531,61 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
   }
 }
 
-// The rows' parts joined: 32 rows per block, eight parts at a time.
-__global__ void __launch_bounds__(256) head_join_kernel(const float2* part, int parts, const float* at_label,
-                                                        const int64_t* labels, int64_t vocab, int rows, float* loss, float* lse) {
+// A row's largest logit (base 2) and sum relative to it.
+struct Softmax {
+  float top = -INFINITY, sum = 0.f;
+  __device__ __forceinline__ void add(float p_top, float p_sum) {
+    const float here = fmaxf(top, p_top);
+    // a part of -infinities alone has the sum 0 (NaN with a NaN among them)
+    if (top != here && top != -INFINITY) sum *= exp2f(top - here);
+    sum += p_top == here || p_top == -INFINITY ? p_sum : p_sum * exp2f(p_top - here);
+    top = here;
+  }
+};
+
+// The rows' parts joined: `each` rows per block (a power of two up to 32), 256 / each threads to a row.
+__global__ void __launch_bounds__(256) head_join_kernel(const float2* part, int parts, const float* at_label, const int64_t* labels,
+                                                        int64_t vocab, int rows, int each, float* loss, float* lse) {
   __shared__ float2 s[8][32];
   grid_wait();
   grid_trigger();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int row = (int)blockIdx.x * 32 + lane;
-  float top = -INFINITY, sum = 0.f;
-  auto add = [&](float2 p) {
-    const float here = fmaxf(top, p.x);
-    // a part of -infinities alone has the sum 0 (NaN with a NaN among them)
-    if (top != here && top != -INFINITY) sum *= exp2f(top - here);
-    sum += p.x == here || p.x == -INFINITY ? p.y : p.y * exp2f(p.x - here);
-    top = here;
-  };
+  const int row = (int)blockIdx.x * each + threadIdx.x % each;
+  Softmax m;
   if (row < rows) {
 #pragma unroll 4
-    for (int k = warp; k < parts; k += 8) add(__ldcg(part + (int64_t)k * rows + row));
+    for (int k = threadIdx.x / each; k < parts; k += 256 / each) {
+      const float2 p = __ldcg(part + (int64_t)k * rows + row);
+      m.add(p.x, p.y);
+    }
   }
-  s[warp][lane] = make_float2(top, sum);
+  for (int o = each; o < 32; o *= 2) {
+    const float top = __shfl_xor_sync(0xffffffffu, m.top, o), sum = __shfl_xor_sync(0xffffffffu, m.sum, o);
+    m.add(top, sum);
+  }
+  s[warp][lane] = make_float2(m.top, m.sum);
   __syncthreads();
-  if (warp == 0 && row < rows) {
+  if (warp == 0 && lane < each && row < rows) {
 #pragma unroll
-    for (int k = 1; k < 8; ++k)
-      if (k < parts) add(s[k][lane]);
-    const float l = (top + log2f(sum)) * kLn2;
+    for (int k = 1; k < 8; ++k) m.add(s[k][lane].x, s[k][lane].y);
+    const float l = (m.top + log2f(m.sum)) * kLn2;
     const int64_t label = labels[row];
     lse[row] = l;
     loss[row] = label >= 0 && label < vocab ? l - at_label[row] : 0.f;
   }
 }
 
-// c = max |gl| over the rows with a label (1 if that is 0 or no number).
 __global__ void __launch_bounds__(1024) head_unit_kernel(const float* grad_loss, const int64_t* labels, int64_t vocab, int rows,
                                                          float* unit) {
   __shared__ float red[32];
   grid_wait();
   grid_trigger();
-  float top = 0.f;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < rows; i += 1024) {
-    const int64_t l = labels[i];
-    const float v = grad_loss[i];
-    if (l >= 0 && l < vocab) top = fmaxf(top, fabsf(v));
-  }
-  top = group_top(top);
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
+  const float share = unit_share<1024>(grad_loss, labels, vocab, rows, threadIdx.x);
+  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = share;
   __syncthreads();
   if (threadIdx.x < 32) {
-    top = group_top(red[threadIdx.x]);
-    if (threadIdx.x == 0) *unit = top > 0.f && top < INFINITY ? top : 1.f;
+    const float top = group_top(red[threadIdx.x]);
+    if (threadIdx.x == 0) *unit = unit_of(top);
   }
 }
 
@@ -491,6 +617,8 @@ bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, in
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+inline int64_t ceil_to(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
+
 struct Operand {
   const void* p;
   int64_t rows, cols, ld;          // as stored
@@ -514,6 +642,11 @@ int launch_head(const Operand& p, const Operand& q, HeadArgs a, int64_t k, cudaS
   }
   a.status = q8_status_word();
   if (!a.status) return PRM_ERR_CUDA;
+  if constexpr (EPI == kFew) {
+    a.q_tile = (int)ceil_to(a.n, 16);
+    a.stage_bytes = kSub * (kBoxBytes + (uint32_t)a.q_tile / 2 * 128);
+    a.stages = std::min<int>(kMaxStages, (int)(kStages * kStageBytes / a.stage_bytes));
+  }
   a.kblocks = (int)((k + kHeadK - 1) / kHeadK);
   a.m_tiles = (a.m + kTile - 1) / kTile;
   a.n_tiles = (a.n + kTile - 1) / kTile;
@@ -523,10 +656,13 @@ int launch_head(const Operand& p, const Operand& q, HeadArgs a, int64_t k, cudaS
   const int64_t fit = ((int64_t)32 << 20) / ((int64_t)kTile * a.kblocks * 128);
   a.band = (int)std::min<int64_t>(a.m_tiles, std::max<int64_t>(8, fit));
   CUtensorMap mp, mq;
-  if (!make_map(&mp, p.p, p.rows, p.cols, p.ld, P_MN ? 64 : 128) || !make_map(&mq, q.p, q.rows, q.cols, q.ld, Q_MN ? 64 : 128))
+  if (!make_map(&mp, p.p, p.rows, p.cols, p.ld, P_MN ? 64 : 128) || !make_map(&mq, q.p, q.rows, q.cols, q.ld, EPI == kFew ? a.q_tile / 2 : Q_MN ? 64 : 128))
     return PRM_ERR_CUDA;
   return q8_code(launch_after(head_kernel<EPI, P_MN, Q_MN>, 2u * (unsigned)std::min(a.tiles, resident[dev]), kThreads,
                               kSmemBytes, stream, 2, mp, mq, a));
+}
+int launch_few(const Operand& x, const Operand& w, const HeadArgs& a, int64_t d, cudaStream_t stream) {
+  return w.mn ? launch_head<kFew, true, false>(w, x, a, d, stream) : launch_head<kFew, false, false>(w, x, a, d, stream);
 }
 template <int EPI>
 int launch_logits(const Operand& x, const Operand& w, const HeadArgs& a, int64_t d, cudaStream_t stream) {
@@ -535,11 +671,10 @@ int launch_logits(const Operand& x, const Operand& w, const HeadArgs& a, int64_t
 
 // ------------------------------------------------------------------ sizes
 
-inline int64_t ceil_to(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
-
-// Forward: rows whose parts fit 128 MB are taken together.
+// Forward: what is left of each row, and rows whose parts fit 128 MB are taken together.
+int64_t stats_parts(int64_t n, int64_t vocab) { return (n <= kFewRows ? 8 : 2) * ((vocab + kTile - 1) / kTile); }
 int64_t stats_rows(int64_t n, int64_t vocab) {
-  const int64_t parts = 2 * ((vocab + kTile - 1) / kTile);
+  const int64_t parts = stats_parts(n, vocab);
   return std::min(n, std::max<int64_t>(2048, ((int64_t)128 << 20) / (8 * parts) / kTile * kTile));
 }
 
@@ -584,8 +719,7 @@ using namespace prm;
 
 extern "C" size_t prm_head_loss_scratch_bytes(int64_t n, int64_t d, int64_t vocab) {
   if (n < 1 || !sizes_ok(n, d, vocab)) return 0;
-  const int64_t parts = 2 * ((vocab + kTile - 1) / kTile);
-  return (size_t)stats_rows(n, vocab) * ((size_t)parts * 8 + 4);
+  return (size_t)stats_rows(n, vocab) * ((size_t)stats_parts(n, vocab) * 8 + 4);
 }
 
 extern "C" int prm_head_loss(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int weight_transposed,
@@ -603,22 +737,27 @@ extern "C" int prm_head_loss(const void* x, int64_t ld_x, const void* weight, in
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   const Operand w = {weight, weight_transposed ? vocab : d, weight_transposed ? d : vocab, ld_weight, !weight_transposed};
   const int64_t step = stats_rows(n, vocab);
-  const int parts = (int)(2 * ((vocab + kTile - 1) / kTile));
+  const int parts = (int)stats_parts(n, vocab);
   for (int64_t r = 0; r < n; r += step) {
     const int64_t rows = std::min(step, n - r);
     HeadArgs a = {};
-    a.m = (int)rows;
-    a.n = (int)vocab;
+    const bool few = n <= kFewRows;
+    a.m = (int)(few ? vocab : rows);
+    a.n = (int)(few ? rows : vocab);
     a.split = 1;
     a.labels = labels + r;
     a.vocab = vocab;
     a.part = (float2*)scratch;
     a.at_label = (float*)(a.part + (size_t)parts * rows);
     const Operand xr = {(const __nv_bfloat16*)x + r * ld_x, rows, d, ld_x, false};
-    code = launch_logits<kStats>(xr, w, a, d, stream);
+    // in the few rows' form W is the left operand, whose m is W's column
+    const Operand wl = {weight, w.rows, w.cols, ld_weight, !weight_transposed};
+    code = few ? launch_few(xr, wl, a, d, stream) : launch_logits<kStats>(xr, w, a, d, stream);
     if (code != PRM_OK) return code;
-    code = q8_code(launch_after(head_join_kernel, (unsigned)((rows + 31) / 32), 256, 0, stream, 0, a.part, parts, a.at_label,
-                                a.labels, vocab, (int)rows, loss_out + r, lse_out + r));
+    int each = 1;                          // few rows: more threads to each, on all SMs
+    while (each < 32 && rows > (int64_t)each * 148) each *= 2;
+    code = q8_code(launch_after(head_join_kernel, (unsigned)((rows + each - 1) / each), 256, 0, stream, 0, a.part, parts,
+                                a.at_label, a.labels, vocab, (int)rows, each, loss_out + r, lse_out + r));
     if (code != PRM_OK) return code;
   }
   return PRM_OK;
@@ -657,7 +796,7 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
   __nv_bfloat16* g = (__nv_bfloat16*)((char*)scratch + 256);
   float* part = (float*)((char*)g + plan.g_bytes);
   const Operand w = {weight, w_rows, w_cols, ld_weight, !weight_transposed};
-  code = q8_code(launch_after(head_unit_kernel, 1u, 1024, 0, stream, 0, grad_loss, labels, vocab, (int)n, unit));
+  if (n > kUnitRows) code = q8_code(launch_after(head_unit_kernel, 1u, 1024, 0, stream, 0, grad_loss, labels, vocab, (int)n, unit));
   const bool parted = plan.part_bytes > 0;
   for (int64_t v0 = 0; v0 < vocab && code == PRM_OK; v0 += plan.piece) {
     const int64_t wide = std::min(plan.piece, vocab - v0);
@@ -672,7 +811,8 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
     a.grad_loss = grad_loss;
     a.g = g;
     a.ld_g = plan.ld_g;
-    a.unit = unit;
+    a.unit = n > kUnitRows || v0 > 0 ? unit : nullptr;
+    a.unit_out = a.unit ? nullptr : unit;
     code = launch_logits<kGrad>({x, n, d, ld_x, false}, w, a, d, stream);
     if (code == PRM_OK && grad_x) {
       HeadArgs b = {};
