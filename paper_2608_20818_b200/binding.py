@@ -750,6 +750,9 @@ def prm_dropout(x, p, seed, offset=0, counter=None, residual=None, stream=None):
 
 def _affine(t, name, rows, cols, index, like=None):
     """(t, row stride, groups) of a scale or shift: a vector of cols, or groups x cols with groups dividing rows."""
+    if t.shape == (cols,) and t.get_device() == index and t.is_contiguous() and (
+            t.dtype in _IO_FP32 if like is None else t.dtype is like.dtype and t.shape == like.shape):
+        return t, cols, 1
     if t.dtype not in _IO_FP32:
         raise TypeError(f"{name} must be bfloat16 or float32")
     if t.dim() not in (1, 2) or t.shape[-1] != cols or t.get_device() != index:
@@ -778,7 +781,7 @@ def prm_layernorm(x, weight=None, bias=None, eps=1e-6, residual=None, add_one=Fa
     rows, cols = x.shape
     index = x.get_device()
     device = x.device
-    c_ptr = _draw(p, counter, index)
+    c_ptr = None if p == 0 else _draw(p, counter, index)
     w_ptr = b_ptr = r_ptr = h_ptr = h = None
     ld_w = ld_b = ld_r = w_fp32 = 0
     groups = 1
@@ -797,16 +800,16 @@ def prm_layernorm(x, weight=None, bias=None, eps=1e-6, residual=None, add_one=Fa
         h = torch.empty_strided((rows, cols), (cols, 1), dtype=x.dtype, device=device)
         h_ptr = h.data_ptr()
     y = torch.empty_strided((rows, cols), (cols, 1), dtype=x.dtype, device=device)
-    stats = torch.empty_strided((2, rows), (rows, 1), dtype=torch.float32, device=device)
-    s_ptr = stats.data_ptr()
+    mean = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device)
+    rstd = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device)
     args = (x.data_ptr(), x.stride(0), r_ptr, ld_r, w_ptr, ld_w, b_ptr, ld_b, rows, cols, max(1, rows // groups),
             _IO_FP32[x.dtype], w_fp32, 1 if add_one else 0, eps, p, seed & _WORD, offset & _WORD, c_ptr, h_ptr, cols,
-            y.data_ptr(), cols, s_ptr, s_ptr + 4 * rows, _raw_stream(index))
+            y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), _raw_stream(index))
     fn = (_lib_handle or lib()).prm_layernorm
     code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
     if code:
         _q8_check(code, "prm_layernorm")
-    return y, h, stats[0], stats[1]
+    return y, h, mean, rstd
 
 
 def prm_layernorm_backward(grad_y, h, mean, rstd, weight=None, grad_h=None, add_one=False, p=0.0, seed=0, offset=0,
@@ -824,7 +827,7 @@ def prm_layernorm_backward(grad_y, h, mean, rstd, weight=None, grad_h=None, add_
     rows, cols = h.shape
     index = h.get_device()
     device = h.device
-    c_ptr = _draw(p, counter, index)
+    c_ptr = None if p == 0 else _draw(p, counter, index)
     mean = _vector(mean, "mean", rows, index)
     rstd = _vector(rstd, "rstd", rows, index)
     w_ptr = gh_ptr = gx_ptr = gw_ptr = gb_ptr = grad_x = grad_w = grad_b = None
@@ -842,10 +845,10 @@ def prm_layernorm_backward(grad_y, h, mean, rstd, weight=None, grad_h=None, add_
         grad_x = torch.empty_strided((rows, cols), (cols, 1), dtype=h.dtype, device=device)
         gx_ptr = grad_x.data_ptr()
     if need_weight:
-        grad_w = torch.empty(w_shape, dtype=w_dtype, device=device)
+        grad_w = torch.empty_strided(w_shape, (1,) if len(w_shape) == 1 else (cols, 1), dtype=w_dtype, device=device)
         gw_ptr = grad_w.data_ptr()
     if need_bias:
-        grad_b = torch.empty(w_shape, dtype=w_dtype, device=device)
+        grad_b = torch.empty_strided(w_shape, (1,) if len(w_shape) == 1 else (cols, 1), dtype=w_dtype, device=device)
         gb_ptr = grad_b.data_ptr()
     per = max(1, rows // groups)
     L = _lib_handle or lib()

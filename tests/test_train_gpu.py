@@ -259,6 +259,21 @@ def test_head_gradient_in_pieces(how):
 
 
 @pytest.mark.gpu
+def test_head_gradient_in_pieces_of_a_wide_vocabulary():
+    """Few enough rows that their common factor is found by the first piece's product; the second reads it."""
+    n, d, vocab = 2000, 40, 140001
+    x, W, labels = head_inputs(n, d, vocab, "out_in", 11)
+    gl = torch.exp(randn(12, n)) / n
+    loss, lse = B.prm_head_loss(x, W, labels)
+    gx, gw = B.prm_head_loss_backward(gl, x, W, labels, lse)
+    rl, rs, off, rx, rw, bx, bw = R.head(x, W, labels, gl, part=500)
+    room = 2 * off + 2.0 ** -20 + 4 * R.F32 * rs.abs()
+    close(loss, rl, 2 * room, "loss")
+    close(gx, rx, 1.02 * bx + 1.01 * R.BF16 * rx.abs() + 1e-30, "grad_x")
+    close(gw, rw, 1.02 * bw + 1.01 * R.BF16 * rw.abs() + 1e-30, "grad_w")
+
+
+@pytest.mark.gpu
 def test_head_loss_in_parts_of_rows():
     """So many columns that the rows' partial sums are joined before all rows have been seen."""
     n, d, vocab = 9001, 16, 262144
