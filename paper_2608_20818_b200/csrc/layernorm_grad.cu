@@ -36,7 +36,7 @@ __device__ __forceinline__ void store_weight(void* out, int fp32, int64_t at, fl
 }
 
 // Blocks per SM of the kernel below: 128 registers per thread with two octs, 85 with one (64 in blocks of 1024).
-constexpr int layernorm_grad_blocks(int nv, int block) { return block == 256 ? (nv == 1 ? 3 : 2) : 1; }
+constexpr int layernorm_grad_blocks(int nv, int block) { return block >= 1024 ? 1 : (nv == 1 ? 768 : 512) / block; }
 
 template <typename IO, int NV, int TPR, int BLOCK, bool DROP, bool SHIFT>
 __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks(NV, BLOCK)) layernorm_grad_kernel(const LayerNormGradArgs a) {
@@ -57,6 +57,24 @@ __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks(NV, BLOCK)) layer
   float2 w[NV][4], gw[NV][4], gb[NV][4];
   Oct<IO> next[NV][3];
   float next_mean = 0.f, next_rstd = 0.f;
+  // Asks the L2 for a row's lines, one lane for 128 bytes.
+  auto ask = [&](int64_t local) {
+    if (local < rows && threadIdx.x % (16 / sizeof(IO)) == 0) {
+      const int64_t row = row0 + local;
+      const IO* gy = reinterpret_cast<const IO*>(a.gy) + row * a.ld_gy;
+      const IO* h = reinterpret_cast<const IO*>(a.h) + row * a.ld_h;
+      const IO* gh = reinterpret_cast<const IO*>(a.gh) + row * a.ld_gh;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int c = c0 + v * TPR * 8;
+        if (c >= 0 && c < a.cols) {
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(gy + c));
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(h + c));
+          if (a.gh) asm volatile("prefetch.global.L2 [%0];" ::"l"(gh + c));
+        }
+      }
+    }
+  };
   auto fetch = [&](int64_t local) {
     if (local < rows) {
       const int64_t row = row0 + local;
@@ -95,7 +113,10 @@ __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks(NV, BLOCK)) layer
     for (int e = 0; e < 4; ++e) gw[v][e] = gb[v][e] = make_float2(0.f, 0.f);
     affine_weight(a.affine, group, c0 + v * TPR * 8, a.cols, w[v]);
   }
+  constexpr bool AHEAD = kRows == 1 && !SHIFT;
+  if constexpr (AHEAD) ask(first + line + step);
   int turn = 0;
+#pragma unroll (AHEAD ? 2 : 1)
   for (int64_t base = first; base < rows; base += step, turn ^= 1) {
     const int64_t local = base + line, row = row0 + local;
     const int cols = local < rows ? a.cols : 0;
@@ -106,6 +127,7 @@ __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks(NV, BLOCK)) layer
       for (int k = 0; k < 3; ++k) now[v][k] = next[v][k];
     const float2 rs2 = make_float2(next_rstd, next_rstd), off2 = make_float2(-next_mean * next_rstd, -next_mean * next_rstd);
     fetch(local + step);
+    if constexpr (AHEAD) ask(local + 2 * step);
     float2 sg2 = make_float2(0.f, 0.f), sx2 = sg2;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -170,6 +192,21 @@ __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks(NV, BLOCK)) layer
     }
   }
   if (!a.gw && !a.gb) return;
+  if (kRows == 1 && !SHIFT && a.parts > 1) {                     // the block's sums to its line of the scratch, as they are
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int c = c0 + v * TPR * 8;
+        if (c < a.cols) {
+          Oct<float> o;
+          o.set(which ? gb[v] : gw[v]);
+          o.store(a.part + ((int64_t)blockIdx.x * 2 + which) * a.cols + c);
+        }
+      }
+    }
+    return;
+  }
   // The block's sums: to its line of the scratch, or, where it has the group to itself, to the gradients.
   auto put = [&](int which, int c, float v) {
     if (a.parts > 1) a.part[((int64_t)blockIdx.x * 2 + which) * a.cols + c] = v;
@@ -257,11 +294,10 @@ __global__ void __launch_bounds__(THREADS) layernorm_grad_single_kernel(const La
   }
 }
 
-// The blocks' lines added: 32 columns of one of the two gradients of a group per block, a line per warp at a time (32 warps
-// for many lines: each goes through few, so that all are under way together).
-template <int WARPS>
-__global__ void __launch_bounds__(WARPS * 32) layernorm_grad_sum_kernel(const LayerNormGradArgs a, int chunks) {
-  __shared__ float s[WARPS][33];
+// The blocks' lines added, all in a fixed order.  Many lines: 32 columns of one of the two gradients of a group per block, a line
+// per warp at a time, so that all are under way together.
+__global__ void __launch_bounds__(1024) layernorm_grad_sum_kernel(const LayerNormGradArgs a, int chunks) {
+  __shared__ float s[32][33];
   grid_wait();
   grid_trigger();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -274,25 +310,38 @@ __global__ void __launch_bounds__(WARPS * 32) layernorm_grad_sum_kernel(const La
   if (c < a.cols) {
     const float* p = a.part + (group * a.parts * 2 + which) * a.cols + c;
 #pragma unroll 10
-    for (int l = warp; l < a.parts; l += WARPS) sum += __ldcg(p + (int64_t)l * 2 * a.cols);
+    for (int l = warp; l < a.parts; l += 32) sum += __ldcg(p + (int64_t)l * 2 * a.cols);
   }
   s[warp][lane] = sum;
   __syncthreads();
-  // warp w adds columns w, w + WARPS, ...: a line per lane
-#pragma unroll
-  for (int k = warp; k < 32; k += WARPS) {
-    const float v = warp_sum(lane < WARPS ? s[lane][k] : 0.f);
-    const int64_t at = c - lane + k;
-    if (lane == 0 && at < a.cols) store_weight(out, a.affine.fp32, group * a.cols + at, v);
-  }
+  const float v = warp_sum(s[lane][warp]);                       // of column `warp`
+  const int64_t at = c - lane + warp;
+  if (lane == 0 && at < a.cols) store_weight(out, a.affine.fp32, group * a.cols + at, v);
+}
+// Few lines (of many groups): a thread per column.
+__global__ void __launch_bounds__(256) layernorm_grad_sum_few_kernel(const LayerNormGradArgs a, int chunks) {
+  grid_wait();
+  grid_trigger();
+  const int which = blockIdx.x & 1;
+  const int64_t group = (blockIdx.x >> 1) / (unsigned)chunks;
+  const int64_t c = (int64_t)((blockIdx.x >> 1) % (unsigned)chunks) * 256 + threadIdx.x;
+  void* out = which ? a.gb : a.gw;
+  if (!out || c >= a.cols) return;
+  const float* p = a.part + (group * a.parts * 2 + which) * a.cols + c;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int l = 0; l < a.parts; ++l) sum += __ldcg(p + (int64_t)l * 2 * a.cols);
+  store_weight(out, a.affine.fp32, group * a.cols + c, sum);
 }
 
 int launch_sum(const LayerNormGradArgs& a, int64_t groups, cudaStream_t stream) {
   if (!a.gw && !a.gb) return PRM_OK;
-  const int chunks = (a.cols + 31) / 32;
-  const unsigned blocks = (unsigned)(groups * chunks * 2);
-  return q8_code(a.parts > 32 ? launch_after(layernorm_grad_sum_kernel<32>, blocks, 1024, 0, stream, 0, a, chunks)
-                              : launch_after(layernorm_grad_sum_kernel<8>, blocks, 256, 0, stream, 0, a, chunks));
+  if (a.parts > 16) {
+    const int chunks = (a.cols + 31) / 32;
+    return q8_code(launch_after(layernorm_grad_sum_kernel, (unsigned)(groups * chunks * 2), 1024, 0, stream, 0, a, chunks));
+  }
+  const int chunks = (a.cols + 255) / 256;
+  return q8_code(launch_after(layernorm_grad_sum_few_kernel, (unsigned)(groups * chunks * 2), 256, 0, stream, 0, a, chunks));
 }
 
 template <typename IO, bool DROP, bool SHIFT, int NV, int TPR, int BLOCK>
@@ -321,9 +370,9 @@ int run_layernorm_grad(const LayerNormGradArgs& a, int64_t groups, cudaStream_t 
   if (c <= 64) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 8, 256>(a, groups, stream);
   if (c <= 128) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 16, 256>(a, groups, stream);
   if (c <= 256) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 32, 256>(a, groups, stream);
-  if (c <= 512) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 32 * T, 256>(a, groups, stream);
-  if (c <= 1024) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 64 * T, 256>(a, groups, stream);
-  if (c <= 2048) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 128 * T, 256>(a, groups, stream);
+  if (c <= 512) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 32 * T, 128>(a, groups, stream);
+  if (c <= 1024) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 64 * T, 64 * T>(a, groups, stream);
+  if (c <= 2048) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 128 * T, 128 * T>(a, groups, stream);
   if (c <= 4096) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 256 * T, 256 * T>(a, groups, stream);
   if (c <= 8192) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 512 * T, 512 * T>(a, groups, stream);
   return launch_layernorm_grad_single<IO>(a, groups, stream);
@@ -378,7 +427,7 @@ extern "C" int prm_layernorm_backward(const void* grad_y, int64_t ld_grad_y, con
   }
   rows_per_group = std::min(rows_per_group, rows);
   const int64_t groups = rows / rows_per_group;
-  if (groups * rows_per_group != rows || groups * ((cols + 31) / 32) > 0x3fffffffLL || groups * 592 > 0x7fffffffLL)
+  if (groups * rows_per_group != rows || groups * ((cols + 31) / 32) > 0x3fffffffLL || groups * 1184 > 0x7fffffffLL)
     return PRM_ERR_SHAPE;
   if (!grad_y || !h || !mean || !rstd || !grad_residual || (drop.threshold && !grad_x) || !scratch) return PRM_ERR_ARG;
   if (scratch_bytes < prm_layernorm_scratch_bytes(rows, cols, rows_per_group)) return PRM_ERR_WORKSPACE;
