@@ -535,7 +535,7 @@ PRM_API int prm_q8_status(void);
  *
  * Dropout draws from a counter-based generator and stores no mask.  The element in row i and column j is
  * kept where word j % 4 of Philox4x32-10 (Salmon et al., SC 2011) at the counter (j / 4, i, low and high
- * half of s) under the key seed (low, high half) is at least p * 2^32 (rounded), s = offset + *counter
+ * half of s) under the key seed (low, high half) is at least p * 2^32 (rounded; at least 1 if p > 0), s = offset + *counter
  * (modulo 2^64).  counter is a device word (NULL: 0), read when the kernel runs, so that a captured graph
  * draws anew at each replay if it advances it.  What is kept is multiplied by 1 / (1 - p) (rounded to
  * fp32, the product too); what is dropped is 0, an infinity or NaN too.  0 <= p < 1.
@@ -547,7 +547,8 @@ PRM_API int prm_q8_status(void);
  *   cols + eps); y = (h - mean) rstd weight + bias.  weight (NULL: 1) and bias (NULL: 0) have one row for
  *   every rows_per_group rows, ld_weight and ld_bias apart (rows_per_group >= rows: one row of each);
  *   add_one: the weight is 1 + what is stored (adaLN).  mean_out and rstd_out, fp32 vectors of rows, are what
- *   the gradient reads.  rows may be 0.
+ *   the gradient reads.  rows may be 0.  A constant row has y = bias; with eps = 0 it is NaN.  Deviations from
+ *   about 1e19 on have infinite squares and rstd 0.
  * prm_layernorm_backward   with xhat = (h - mean) rstd and g = grad_y weight:
  *     grad_residual = rstd (g - mean(g) - xhat mean(g xhat)) + grad_h   (grad_h, what reaches h from elsewhere, may
  *                     be NULL); without dropout it is the gradient of x too and grad_x is ignored
@@ -564,7 +565,8 @@ PRM_API int prm_q8_status(void);
  *   prm_head_loss_scratch_bytes(n, d, vocab) bytes.
  * prm_head_loss_backward   from grad_loss (fp32, n): with G = grad_loss (softmax - [label]), 0 for rows without a label,
  *     grad_x = G W^T (bf16, n x d),  grad_weight = x^T G (bf16, stored like weight); either may be NULL
- *   G is rounded to bf16 (after division by the largest |grad_loss|) for the products, whose sums are fp32.
+ *   G is rounded to bf16 (after division by the largest |grad_loss|) for the products, whose sums are fp32.  Rows of x
+ *   without a label count as 0 times x in grad_weight: they must be finite.
  *   scratch: device, 256-byte aligned, prm_head_loss_backward_scratch_bytes(n, d, vocab) bytes: G for a piece of the
  *   vocabulary, up to 512 MB, and partial sums.  With n = 0 grad_weight is set to zero.
  * prm_q8_status covers the waits inside the head's products too.

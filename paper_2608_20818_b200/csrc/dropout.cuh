@@ -7,8 +7,10 @@
 //
 // Philox4x32-10 is the generator of Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as
 // 1, 2, 3" (SC 2011): ten rounds of two 32 x 32 -> 64 bit products, whose halves change places, under a key
-// that advances by a constant (the rounds' keys come with the kernel's arguments).  Four elements share one evaluation, 20 products: on 8192 x 8192 elements in
-// bf16 the kernel of dropout.cu is held by memory, not by them.
+// that advances by a constant (the rounds' keys come with the kernel's arguments: computed by every thread they
+// take 8192 x 8192 bf16 elements from 65 to 74 us).  Four elements share one evaluation: 18 to 20 products of four
+// cycles of an SM's quarter and 20 exclusive ors of two, alone 0.66 cycles of an SM, 39 us for 8192 x 8192 elements (memory
+// alone: 41 us); a product as one half from double precision and one from 32-bit integers takes 0.9.
 #pragma once
 
 #include <cmath>
@@ -29,7 +31,8 @@ struct Drop {
 inline bool drop_ok(double p) { return p >= 0.0 && p < 1.0; }      // false for a NaN too
 inline Drop make_drop(double p, uint64_t seed, uint64_t offset, const uint64_t* counter) {
   Drop d;
-  d.threshold = (uint32_t)std::min(std::nearbyint(p * 4294967296.0), 4294967295.0);
+  // p > 0 has a threshold: that there is one is what the kernels go by
+  if (p > 0.0) d.threshold = (uint32_t)std::min(std::max(std::nearbyint(p * 4294967296.0), 1.0), 4294967295.0);
   d.scale = (float)(1.0 / (1.0 - p));
   for (uint32_t r = 0; r < 10; ++r)
     d.key[r] = make_uint2((uint32_t)seed + r * 0x9E3779B9u, (uint32_t)(seed >> 32) + r * 0xBB67AE85u);

@@ -211,8 +211,9 @@ __host__ __device__ inline int staged_words(int cols, bool shift) {
 }
 
 // Many rows: a block's rows are a range, BLOCK / TPR of them at a time, the next rows' loads under way while these are summed.
-// The rows of a group share weight and bias from shared memory, as fp32: fetched by each row for itself (16384 x 2048
-// with a weight for each of 64 groups) they cost as many bytes from L2 as the row, and their conversion.
+// The rows of a group share weight and bias from shared memory, as fp32: fetched by each row for itself they cost as many
+// bytes from L2 as the row, and their conversion (16384 x 2048 with a weight for each of 64 groups, no residual: 31.6
+// us, 4.3 TB/s; a row per block 42).  Asking the L2 for the rows after the next gains nothing here.
 template <typename IO, int NV, int TPR, int BLOCK, bool DROP, bool SHIFT>
 __global__ void __launch_bounds__(BLOCK, layernorm_blocks<IO>(BLOCK)) layernorm_many_kernel(const LayerNormArgs a) {
   constexpr int kLines = BLOCK / TPR;
@@ -489,7 +490,7 @@ int run_layernorm(const LayerNormArgs& a, cudaStream_t stream) {
   PRM_TRY(2, 64);
   PRM_TRY(2, 128);
   PRM_TRY(2, 256);
-  // half of the threads idle with the next size (8192 x 4097: @@ us, 110)
+  // half of the threads idle with the next size (8192 x 4097: 91 us instead of 110)
   if (c <= 8 * 3 * 256) return launch_layernorm<IO, DROP, SHIFT, 3, 256>(a, stream);
   PRM_TRY(2, 512);
 #undef PRM_TRY

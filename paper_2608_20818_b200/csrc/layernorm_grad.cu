@@ -7,7 +7,9 @@
 // Bound by HBM (8 bytes per element of a bf16 stream with grad_h, 10 with dropout).  Blocks walk the rows of
 // one group; a thread keeps the same columns in all its rows, so that its share of grad_w and grad_b stays in
 // registers, and the next row's loads are under way while this one is summed.  With several blocks to a group
-// their lines of sums are added by a second launch, in a fixed order.
+// their lines of sums are added by a second launch, in a fixed order.  Measured: 8192 x 4096 in bf16 with grad_h 54 us, 5.0
+// TB/s (fp32 89 us, 6.0), with dropout 83 us; 16384 x 2048 with a weight for each of 64 groups 54 us; 131072 x 128 32 us;
+// 8192 x 4097 106 us.
 #include "layernorm.cuh"
 
 namespace prm {
@@ -35,11 +37,15 @@ __device__ __forceinline__ void store_weight(void* out, int fp32, int64_t at, fl
   else reinterpret_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(v);
 }
 
-// Blocks per SM of the kernel below: 128 registers per thread with two octs, 85 with one (64 in blocks of 1024).
-constexpr int layernorm_grad_blocks(int nv, int block) { return block >= 1024 ? 1 : (nv == 1 ? 768 : 512) / block; }
+// Blocks per SM of the kernel below: 128 registers per thread with two octs or 32-bit elements (16384 x 2048 in fp32: 88 us,
+// with 85 registers 123), else 85.
+template <typename IO>
+constexpr int layernorm_grad_blocks(int nv, int block) {
+  return (nv == 1 && sizeof(IO) == 2 ? 768 : 512) / block;
+}
 
 template <typename IO, int NV, int TPR, int BLOCK, bool DROP, bool SHIFT>
-__global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks(NV, BLOCK)) layernorm_grad_kernel(const LayerNormGradArgs a) {
+__global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks<IO>(NV, BLOCK)) layernorm_grad_kernel(const LayerNormGradArgs a) {
   constexpr int kRows = BLOCK / TPR, kWide = NV * TPR * 8;
   __shared__ float sums[kRows > 1 ? kRows : 1][kRows > 1 ? kWide : 1];
   __shared__ __align__(16) float red[2][kRows][TPR > 32 ? TPR / 32 * 2 : 1];
@@ -57,7 +63,8 @@ __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks(NV, BLOCK)) layer
   float2 w[NV][4], gw[NV][4], gb[NV][4];
   Oct<IO> next[NV][3];
   float next_mean = 0.f, next_rstd = 0.f;
-  // Asks the L2 for a row's lines, one lane for 128 bytes.
+  // Asks the L2 for a row's lines, one lane for 128 bytes.  (8192 x 4096: 54 us with it and the loop unrolled twice, so that no
+  // registers are copied; 62 without.  Rows that start anywhere spill and take 126 us instead of 106.)
   auto ask = [&](int64_t local) {
     if (local < rows && threadIdx.x % (16 / sizeof(IO)) == 0) {
       const int64_t row = row0 + local;
@@ -346,7 +353,7 @@ int launch_sum(const LayerNormGradArgs& a, int64_t groups, cudaStream_t stream) 
 
 template <typename IO, bool DROP, bool SHIFT, int NV, int TPR, int BLOCK>
 int launch_layernorm_grad(LayerNormGradArgs a, int64_t groups, cudaStream_t stream) {
-  a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, BLOCK / TPR, 148 * layernorm_grad_blocks(NV, BLOCK), SHIFT);
+  a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, BLOCK / TPR, 148 * layernorm_grad_blocks<IO>(NV, BLOCK), SHIFT);
   const int code = q8_code(launch_after(layernorm_grad_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT>, (unsigned)(groups * a.parts),
                                         BLOCK, 0, stream, 0, a));
   return code == PRM_OK && a.parts > 1 ? launch_sum(a, groups, stream) : code;
@@ -365,7 +372,8 @@ int launch_layernorm_grad_single(LayerNormGradArgs a, int64_t groups, cudaStream
 template <typename IO, bool DROP, bool SHIFT>
 int run_layernorm_grad(const LayerNormGradArgs& a, int64_t groups, cudaStream_t stream) {
   const int64_t c = (int64_t)a.cols + (SHIFT ? 7 : 0);
-  // Two octs per thread halve what a row's reduction costs each; of 32-bit elements they leave the registers.
+  // Two octs per thread halve what a row's reduction costs each; of 32-bit elements they leave the registers, but a block of
+  // 1024 threads has too few for one (4096 x 8192 in fp32: 164 us, so 223).
   constexpr int NV = sizeof(IO) == 2 ? 2 : 1, T = NV == 2 ? 1 : 2;
   if (c <= 64) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 8, 256>(a, groups, stream);
   if (c <= 128) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 16, 256>(a, groups, stream);
@@ -374,7 +382,7 @@ int run_layernorm_grad(const LayerNormGradArgs& a, int64_t groups, cudaStream_t 
   if (c <= 1024) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 64 * T, 64 * T>(a, groups, stream);
   if (c <= 2048) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 128 * T, 128 * T>(a, groups, stream);
   if (c <= 4096) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 256 * T, 256 * T>(a, groups, stream);
-  if (c <= 8192) return launch_layernorm_grad<IO, DROP, SHIFT, NV, 512 * T, 512 * T>(a, groups, stream);
+  if (c <= 8192) return launch_layernorm_grad<IO, DROP, SHIFT, 2, 512, 512>(a, groups, stream);
   return launch_layernorm_grad_single<IO>(a, groups, stream);
 }
 template <typename IO>

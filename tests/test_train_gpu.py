@@ -58,6 +58,16 @@ def test_dropout_of_what_is_no_number_and_of_nothing():
 
 
 @pytest.mark.gpu
+def test_a_probability_too_small_to_drop_anything():
+    """Below half of 2^-32: what dropout returns is there all the same."""
+    x = randn(1, 30, 200)
+    y, h, _, _ = B.prm_layernorm(x, p=1e-12, seed=3)
+    assert torch.equal(h, x) and torch.equal(y, B.prm_layernorm(x)[0]) and torch.equal(B.prm_dropout(x, 1e-12, 3), x)
+    gx, gr, _, _ = B.prm_layernorm_backward(x, h, *B.prm_layernorm(x)[2:], p=1e-12, seed=3)
+    assert torch.equal(gx, gr)
+
+
+@pytest.mark.gpu
 def test_dropout_beyond_32_bits_of_offsets():
     """The last rows of a matrix of more than 2^32 bytes and 2^31 elements."""
     rows, cols = 70000, 32768
