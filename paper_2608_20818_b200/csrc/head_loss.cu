@@ -50,6 +50,7 @@ __host__ __device__ constexpr bool chunked(int epi) { return epi == kStats || ep
 
 struct HeadArgs {
   int m, n, kblocks;               // of this product: rows, columns, ceil(k / 64)
+  int p_mn, q_mn;                  // kStore: the operand's m (n) is contiguous, not its k
   int q_n0, q_k0;                  // where it starts in Q
   int m_tiles, n_tiles, tiles;     // tiles: of all splits of k
   int band;                        // m-tiles that are walked through together
@@ -73,6 +74,29 @@ struct HeadArgs {
   int64_t ld_out, split_stride;
   int out_fp32, accumulate;        // accumulate: fp32 out += (16-byte aligned)
 };
+
+// A launch: one product, or (kStore) two that do not depend on one another.
+struct HeadLaunch {
+  CUtensorMap p[2], q[2];
+  HeadArgs a[2];
+  int extra;                       // see next_tile
+};
+
+// The i-th tile of a pair.  Two products: the first one's tiles go round the pairs; those that its last round leaves idle
+// take `extra` tiles of the second for it, as many as take as long as one of the first; then the second's rest goes round.
+template <int EPI>
+__device__ __forceinline__ bool next_tile(const HeadLaunch& l, int pair, int pairs, int i, int& which, int& tile) {
+  const int t0 = l.a[0].tiles;
+  which = 0;
+  tile = pair + i * pairs;
+  if constexpr (EPI != kStore) return tile < t0;
+  if (tile < t0) return true;
+  which = 1;
+  const int t1 = l.a[1].tiles, used = t0 % pairs, extra = used > 0 && pair >= used ? l.extra : 0;
+  i -= t0 / pairs + (pair < used);
+  tile = i < extra ? (pair - used) * extra + i : (used > 0 ? (pairs - used) * l.extra : 0) + pair + (i - extra) * pairs;
+  return tile < t1;
+}
 
 __device__ __forceinline__ float ex2(float v) {
   float r;
@@ -287,22 +311,22 @@ __device__ __forceinline__ void store_tile(const HeadArgs& a, uint32_t taddr, ui
   }
 }
 
+// P_MN, Q_MN: as HeadArgs has them (kStore goes by those).
 template <int EPI, bool P_MN, bool Q_MN>
-__global__ void __launch_bounds__(kThreads, 1)
-head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const HeadArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant__ HeadLaunch l) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   volatile int* abort_flag = &abort_word;
-  int* status = a.status;
+  int* status = l.a[0].status;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const int stages = EPI == kFew ? a.stages : kStages;
-  const uint32_t stage_bytes = EPI == kFew ? a.stage_bytes : kStageBytes;
-  const uint32_t q_box = EPI == kFew ? (uint32_t)a.q_tile / 2 * 128 : kBoxBytes;      // bytes of one k-block of Q
+  const int stages = EPI == kFew ? l.a[0].stages : kStages;
+  const uint32_t stage_bytes = EPI == kFew ? l.a[0].stage_bytes : kStageBytes;
+  const uint32_t q_box = EPI == kFew ? (uint32_t)l.a[0].q_tile / 2 * 128 : kBoxBytes;      // bytes of one k-block of Q
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
@@ -336,7 +360,11 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
       uint32_t it = 0;
       bool ok = true;
       const uint32_t lead_full = cluster_map(smem_u32(&full[0]), 0);
-      for (int t = pair; t < a.tiles && ok; t += pairs) {
+      for (int i = 0, which, t; ok && next_tile<EPI>(l, pair, pairs, i, which, t); ++i) {
+        const HeadArgs& a = l.a[EPI == kStore ? which : 0];
+        const CUtensorMap* map_p = &l.p[EPI == kStore ? which : 0];
+        const CUtensorMap* map_q = &l.q[EPI == kStore ? which : 0];
+        const bool p_mn = EPI == kStore ? a.p_mn != 0 : P_MN, q_mn = EPI == kStore ? a.q_mn != 0 : Q_MN;
         int split, m0, n0, s0, s1;
         tile_origin(a, t, split, m0, n0);
         split_range(a, split, s0, s1);
@@ -355,17 +383,17 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
             if (j < subs) {
               const int k0 = (kt * kSub + j) * kHeadK;
               // an operand whose m (or n) is contiguous: boxes of 64 of them by 64 k
-              if (P_MN) {
-                tma_load_pair(sp + j * kBoxBytes, &map_p, bar, m0, k0);
-                tma_load_pair(sp + j * kBoxBytes + kBoxBytes / 2, &map_p, bar, m0 + 64, k0);
+              if (p_mn) {
+                tma_load_pair(sp + j * kBoxBytes, map_p, bar, m0, k0);
+                tma_load_pair(sp + j * kBoxBytes + kBoxBytes / 2, map_p, bar, m0 + 64, k0);
               } else {
-                tma_load_pair(sp + j * kBoxBytes, &map_p, bar, k0, m0);
+                tma_load_pair(sp + j * kBoxBytes, map_p, bar, k0, m0);
               }
-              if (Q_MN) {
-                tma_load_pair(sq + j * kBoxBytes, &map_q, bar, n0, a.q_k0 + k0);
-                tma_load_pair(sq + j * kBoxBytes + kBoxBytes / 2, &map_q, bar, n0 + 64, a.q_k0 + k0);
+              if (q_mn) {
+                tma_load_pair(sq + j * kBoxBytes, map_q, bar, n0, a.q_k0 + k0);
+                tma_load_pair(sq + j * kBoxBytes + kBoxBytes / 2, map_q, bar, n0 + 64, a.q_k0 + k0);
               } else {
-                tma_load_pair(sq + j * q_box, &map_q, bar, a.q_k0 + k0, n0);
+                tma_load_pair(sq + j * q_box, map_q, bar, a.q_k0 + k0, n0);
               }
             }
           }
@@ -382,12 +410,15 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      const uint32_t idesc = idesc_bf16(kTile, EPI == kFew ? a.q_tile : kTile, P_MN, Q_MN);
-      constexpr uint32_t kStepP = P_MN ? 128 : 2, kStepQ = Q_MN ? 128 : 2;    // 16 k, in units of 16 bytes
       uint32_t it = 0, acc = 0;
       bool ok = true;
       const uint32_t smem0 = smem_u32(smem);
-      for (int t = pair; t < a.tiles && ok; t += pairs) {
+      for (int i = 0, which, t; ok && next_tile<EPI>(l, pair, pairs, i, which, t); ++i) {
+        const HeadArgs& a = l.a[EPI == kStore ? which : 0];
+        const bool p_mn = EPI == kStore ? a.p_mn != 0 : P_MN, q_mn = EPI == kStore ? a.q_mn != 0 : Q_MN;
+        const uint32_t idesc = idesc_bf16(kTile, EPI == kFew ? a.q_tile : kTile, p_mn, q_mn);
+        const uint32_t step_p = p_mn ? 128 : 2, step_q = q_mn ? 128 : 2;      // 16 k, in units of 16 bytes
+        const int kblocks = a.kblocks;
         int split, m0, n0, s0, s1;
         tile_origin(a, t, split, m0, n0);
         split_range(a, split, s0, s1);
@@ -402,15 +433,15 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
             if (!mbar_wait(&full[s], (it / stages) & 1, abort_flag, status)) { ok = false; break; }
             tcgen05_after_sync();
             const uint32_t sp = smem0 + (uint32_t)s * stage_bytes, sq = sp + kSub * kBoxBytes;
-            const int subs = min(kSub, a.kblocks - kt * kSub);
+            const int subs = min(kSub, kblocks - kt * kSub);
 #pragma unroll
             for (int j = 0; j < kSub; ++j) {
               if (j < subs) {
-                const uint64_t dp = P_MN ? desc_mn_major(sp + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sp + j * kBoxBytes);
-                const uint64_t dq = Q_MN ? desc_mn_major(sq + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sq + j * q_box);
+                const uint64_t dp = p_mn ? desc_mn_major(sp + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sp + j * kBoxBytes);
+                const uint64_t dq = q_mn ? desc_mn_major(sq + j * kBoxBytes, kBoxBytes / 2) : desc_k_major(sq + j * q_box);
 #pragma unroll
-                for (int i = 0; i < kHeadK / 16; ++i)
-                  umma_bf16_pair(d, dp + kStepP * i, dq + kStepQ * i, idesc, (uint32_t)(kt > c0) | (uint32_t)((j | i) != 0));
+                for (int k = 0; k < kHeadK / 16; ++k)
+                  umma_bf16_pair(d, dp + step_p * k, dq + step_q * k, idesc, (uint32_t)(kt > c0) | (uint32_t)((j | k) != 0));
               }
             }
             umma_commit_both(smem_u32(&empty[s]));
@@ -428,8 +459,10 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
     const uint32_t lead_tempty = cluster_map(smem_u32(&tempty[0]), 0);
     uint8_t* patch = smem + (size_t)stages * stage_bytes + (warp - 2) * kPatchBytes;
-    float unit = (EPI == kStore || EPI == kGrad) && a.unit ? *a.unit : 1.f;
+    float unit = 1.f;
     if constexpr (EPI == kGrad) {
+      const HeadArgs& a = l.a[0];
+      if (a.unit) unit = *a.unit;
       if (a.unit_out) {
         float* red = reinterpret_cast<float*>(smem + (size_t)stages * stage_bytes);        // the patches
         const float share = unit_share<kEpiWarps * 32>(a.grad_loss, a.labels, a.vocab, a.m, (int)threadIdx.x - 64);
@@ -445,7 +478,8 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
     }
     uint32_t acc = 0;
     bool ok = true;
-    for (int t = pair; t < a.tiles && ok; t += pairs) {
+    for (int i = 0, which, t; ok && next_tile<EPI>(l, pair, pairs, i, which, t); ++i) {
+      const HeadArgs& a = l.a[EPI == kStore ? which : 0];
       int split, m0, n0, s0, s1;
       tile_origin(a, t, split, m0, n0);
       const int column = (n0 / kTile) * 2 + half;
@@ -515,6 +549,7 @@ head_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ C
         n0 += half * 128;
         if constexpr (EPI == kGrad) grad_tile(a, taddr, patch, m0, n0, rows, unit);
         if constexpr (EPI == kStore) {
+          unit = a.unit ? *a.unit : 1.f;
           if (a.out_fp32) store_tile<float>(a, taddr, patch, split, m0, n0, rows, unit);
           else store_tile<__nv_bfloat16>(a, taddr, patch, split, m0, n0, rows, unit);
         }
@@ -627,8 +662,34 @@ struct Operand {
   bool mn;                         // m (n) contiguous
 };
 
+// Fills in product i of a launch.
+template <int EPI>
+int set_product(HeadLaunch& l, int i, const Operand& p, const Operand& q, HeadArgs a, int64_t k) {
+  a.status = q8_status_word();
+  if (!a.status) return PRM_ERR_CUDA;
+  if constexpr (EPI == kFew) {
+    a.q_tile = (int)ceil_to(a.n, 16);
+    a.stage_bytes = kSub * (kBoxBytes + (uint32_t)a.q_tile / 2 * 128);
+    a.stages = std::min<int>(kMaxStages, (int)(kStages * kStageBytes / a.stage_bytes));
+  }
+  a.p_mn = p.mn;
+  a.q_mn = q.mn;
+  a.kblocks = (int)((k + kHeadK - 1) / kHeadK);
+  a.m_tiles = (a.m + kTile - 1) / kTile;
+  a.n_tiles = (a.n + kTile - 1) / kTile;
+  if ((int64_t)a.m_tiles * a.n_tiles * a.split > 0x3fffffffLL) return PRM_ERR_SHAPE;
+  a.tiles = a.m_tiles * a.n_tiles * a.split;
+  // As many m-tiles as keep their rows of P within 32 MB of the L2, at least 8 (a ninth of a wave).
+  const int64_t fit = ((int64_t)32 << 20) / ((int64_t)kTile * a.kblocks * 128);
+  a.band = (int)std::min<int64_t>(a.m_tiles, std::max<int64_t>(8, fit));
+  l.a[i] = a;
+  return make_map(&l.p[i], p.p, p.rows, p.cols, p.ld, p.mn ? 64 : 128) &&
+                 make_map(&l.q[i], q.p, q.rows, q.cols, q.ld, EPI == kFew ? a.q_tile / 2 : q.mn ? 64 : 128)
+             ? PRM_OK
+             : PRM_ERR_CUDA;
+}
 template <int EPI, bool P_MN, bool Q_MN>
-int launch_head(const Operand& p, const Operand& q, HeadArgs a, int64_t k, cudaStream_t stream) {
+int launch_products(const HeadLaunch& l, cudaStream_t stream) {
   static PerDeviceOnce once;
   static int resident[64];
   int dev;
@@ -642,27 +703,17 @@ int launch_head(const Operand& p, const Operand& q, HeadArgs a, int64_t k, cudaS
     resident[dev] = n;
     once.mark(dev);
   }
-  a.status = q8_status_word();
-  if (!a.status) return PRM_ERR_CUDA;
-  if constexpr (EPI == kFew) {
-    a.q_tile = (int)ceil_to(a.n, 16);
-    a.stage_bytes = kSub * (kBoxBytes + (uint32_t)a.q_tile / 2 * 128);
-    a.stages = std::min<int>(kMaxStages, (int)(kStages * kStageBytes / a.stage_bytes));
-  }
-  a.kblocks = (int)((k + kHeadK - 1) / kHeadK);
-  a.m_tiles = (a.m + kTile - 1) / kTile;
-  a.n_tiles = (a.n + kTile - 1) / kTile;
-  if ((int64_t)a.m_tiles * a.n_tiles * a.split > 0x3fffffffLL) return PRM_ERR_SHAPE;
-  a.tiles = a.m_tiles * a.n_tiles * a.split;
-  // As many m-tiles as keep their rows of P within 32 MB of the L2, at least 8 (a ninth of a wave).
-  const int64_t fit = ((int64_t)32 << 20) / ((int64_t)kTile * a.kblocks * 128);
-  a.band = (int)std::min<int64_t>(a.m_tiles, std::max<int64_t>(8, fit));
-  CUtensorMap mp, mq;
-  if (!make_map(&mp, p.p, p.rows, p.cols, p.ld, P_MN ? 64 : 128) || !make_map(&mq, q.p, q.rows, q.cols, q.ld, EPI == kFew ? a.q_tile / 2 : Q_MN ? 64 : 128))
-    return PRM_ERR_CUDA;
-  return q8_code(launch_after(head_kernel<EPI, P_MN, Q_MN>, 2u * (unsigned)std::min(a.tiles, resident[dev]), kThreads,
-                              kSmemBytes, stream, 2, mp, mq, a));
+  return q8_code(launch_after(head_kernel<EPI, P_MN, Q_MN>, 2u * (unsigned)std::min(l.a[0].tiles + l.a[1].tiles, resident[dev]),
+                              kThreads, kSmemBytes, stream, 2, l));
 }
+template <int EPI, bool P_MN, bool Q_MN>
+int launch_head(const Operand& p, const Operand& q, const HeadArgs& a, int64_t k, cudaStream_t stream) {
+  HeadLaunch l = {};
+  const int code = set_product<EPI>(l, 0, p, q, a, k);
+  return code == PRM_OK ? launch_products<EPI, P_MN, Q_MN>(l, stream) : code;
+}
+// How long a tile takes, in stages: its main loop, or its epilogue where that is longer (5 stages).
+inline int tile_cost(const HeadArgs& a) { return std::max(5, (a.kblocks + kSub - 1) / kSub / std::max(1, a.split)); }
 int launch_few(const Operand& x, const Operand& w, const HeadArgs& a, int64_t d, cudaStream_t stream) {
   return w.mn ? launch_head<kFew, true, false>(w, x, a, d, stream) : launch_head<kFew, false, false>(w, x, a, d, stream);
 }
@@ -816,6 +867,8 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
     a.unit = n > kUnitRows || v0 > 0 ? unit : nullptr;
     a.unit_out = a.unit ? nullptr : unit;
     code = launch_logits<kGrad>({x, n, d, ld_x, false}, w, a, d, stream);
+    HeadLaunch l = {};                     // the two products that read G: one launch
+    int products = 0;
     if (code == PRM_OK && grad_x) {
       HeadArgs b = {};
       b.m = (int)n;
@@ -829,8 +882,7 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
       b.out_fp32 = parted;
       b.accumulate = v0 > 0;
       const Operand gp = {g, n, wide, plan.ld_g, false}, wq = {weight, w_rows, w_cols, ld_weight, weight_transposed != 0};
-      code = weight_transposed ? launch_head<kStore, false, true>(gp, wq, b, wide, stream)
-                               : launch_head<kStore, false, false>(gp, wq, b, wide, stream);
+      code = set_product<kStore>(l, products++, gp, wq, b, wide);
     }
     if (code == PRM_OK && grad_weight) {
       HeadArgs b = {};
@@ -842,13 +894,17 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
         b.m = (int)wide;
         b.n = (int)d;
         b.out = (__nv_bfloat16*)grad_weight + v0 * ld_grad_weight;
-        code = launch_head<kStore, true, true>(gt, xt, b, n, stream);
+        code = set_product<kStore>(l, products++, gt, xt, b, n);
       } else {
         b.m = (int)d;
         b.n = (int)wide;
         b.out = (__nv_bfloat16*)grad_weight + v0;
-        code = launch_head<kStore, true, true>(xt, gt, b, n, stream);
+        code = set_product<kStore>(l, products++, xt, gt, b, n);
       }
+    }
+    if (code == PRM_OK) {
+      if (products == 2) l.extra = tile_cost(l.a[0]) / tile_cost(l.a[1]);
+      code = launch_products<kStore, false, false>(l, stream);
     }
   }
   if (code == PRM_OK && grad_x && parted) {
