@@ -25,7 +25,8 @@ from .binding import (prm_dropout, prm_head_loss, prm_head_loss_backward, prm_la
 class Draws:
     """Where dropout takes its numbers from: a seed, and a counter on the device.  Every call of a step takes the next
     number; advance() ends the step, after its backward pass (which reads the counter again, and refuses to run if it has been
-    advanced since)."""
+    advanced since).  A forward pass that is run again (a checkpointed one) takes new numbers, so it draws other masks: set `calls`
+    back before it."""
 
     def __init__(self, seed, device="cuda"):
         self.seed = int(seed)

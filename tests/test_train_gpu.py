@@ -190,6 +190,24 @@ def test_layernorm_edges():
 
 
 @pytest.mark.gpu
+def test_layernorm_beyond_32_bits_of_offsets():
+    """The last rows of a stream of more than 2^31 elements, on both sides of the pass."""
+    rows, cols = 140000, 16384
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[-40:] = randn(1, 40, cols).to(torch.bfloat16)
+    x[:-40] = 1
+    w = torch.ones(cols, device="cuda")
+    y, _, mean, rstd = B.prm_layernorm(x, w)
+    ry, rm, rr, size = R.norm(x[-40:], w, None, EPS)
+    close(y[-40:], ry, 200 * R.F32 * size + 1.01 * R.BF16 * ry.abs(), "y")
+    close(mean[-40:], rm, 100 * R.F32 * x[-40:].double().abs().mean(1), "mean")
+    del y
+    gx, _, gw, gb = B.prm_layernorm_backward(x, x, mean, rstd, w)
+    rx, _, _, sx, _, _ = R.norm_backward(x[-40:], x[-40:], mean[-40:], rstd[-40:], w)
+    close(gx[-40:], rx, 100 * R.F32 * sx + 1.01 * R.BF16 * rx.abs(), "grad_x")
+
+
+@pytest.mark.gpu
 def test_layernorm_refusals():
     x = randn(1, 6, 64)
     w = torch.ones(64, device="cuda")
@@ -281,6 +299,37 @@ def test_head_gradient_in_pieces_of_a_wide_vocabulary():
     close(loss, rl, 2 * room, "loss")
     close(gx, rx, 1.02 * bx + 1.01 * R.BF16 * rx.abs() + 1e-30, "grad_x")
     close(gw, rw, 1.02 * bw + 1.01 * R.BF16 * rw.abs() + 1e-30, "grad_w")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("transposed", [False, True])
+def test_head_weight_beyond_32_bits_of_offsets(transposed):
+    """A weight of more than 2^31 elements: the loss, and the last of its gradient."""
+    n, d, vocab = 70, 16400, 131080
+    x = randn(1, n, d).to(torch.bfloat16)
+    shape = (vocab, d) if transposed else (d, vocab)
+    W = torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_(0.0, d ** -0.5, generator=torch.Generator(device="cuda").manual_seed(2))
+    W = W.t() if transposed else W
+    labels = torch.arange(n, device="cuda") * 1000 + vocab - 1000 * n
+    logits = torch.zeros(n, vocab, dtype=torch.float64, device="cuda")
+    size = 0.0
+    for k in range(0, d, 1024):
+        logits += x[:, k:k + 1024].double() @ W[k:k + 1024].double()
+        size += float((x[:, k:k + 1024].double().abs() @ W[k:k + 1024, ::97].double().abs()).amax())
+    lse = torch.logsumexp(logits, 1)
+    off = 1.1 * (d / 16 + 4) * 2.0 ** -23 * size          # every 97th column's largest sum of magnitudes, and a tenth
+    loss, got = B.prm_head_loss(x, W, labels)
+    room = 2 * off + 2.0 ** -20 + 4 * R.F32 * lse.abs()
+    close(got, lse, room, "lse")
+    close(loss, lse - logits.gather(1, labels[:, None])[:, 0], 2 * room, "loss")
+    gl = torch.full((n,), 1 / 64, device="cuda")
+    _, gw = B.prm_head_loss_backward(gl, x, W, labels, got, need_x=False)
+    g = torch.exp(logits - lse[:, None])
+    g[torch.arange(n, device="cuda"), labels] -= 1
+    g /= 64
+    want = x[:, -9:].double().t() @ g
+    dg = R.BF16 * g.abs() + (2 * off + 2.0 ** -19) / 64 * torch.exp(logits - lse[:, None])
+    close(gw[-9:], want, 1.02 * x[:, -9:].double().abs().t() @ dg + 1.01 * R.BF16 * want.abs() + 1e-30, "grad_w")
 
 
 @pytest.mark.gpu
