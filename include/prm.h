@@ -561,7 +561,7 @@ PRM_API int prm_q8_status(void);
  *     lse = log sum_v exp(logit_v),  loss = lse - logit_label, 0 for a row whose label is not in 0..vocab-1
  *   x and weight bf16; weight_transposed = 0: stored d x vocab, 1: vocab x d (an embedding).  Both 16-byte
  *   aligned with row strides that are multiples of 8 (else PRM_ERR_ALIGN).  loss_out, lse_out: fp32 vectors of n.
- *   A row with a NaN or an infinite logit gets a NaN.  n may be 0.  scratch: device, 16-byte aligned,
+ *   A row with a NaN or an infinite logit gets a NaN.  n may be 0; n, d and vocab 2^27 at most.  scratch: device, 16-byte aligned,
  *   prm_head_loss_scratch_bytes(n, d, vocab) bytes.
  * prm_head_loss_backward   from grad_loss (fp32, n): with G = grad_loss (softmax - [label]), 0 for rows without a label,
  *     grad_x = G W^T (bf16, n x d),  grad_weight = x^T G (bf16, stored like weight); either may be NULL

@@ -763,8 +763,9 @@ BackwardPlan backward_plan(int64_t n, int64_t d, int64_t vocab) {
   return p;
 }
 
+// Sums as long as 2^27 leave a tile in its main loop for less than a second, half of what a wait is given.
 bool sizes_ok(int64_t n, int64_t d, int64_t vocab) {
-  const int64_t most = 0x7fffffffLL - 1024;
+  const int64_t most = (int64_t)1 << 27;
   return n >= 0 && d >= 1 && vocab >= 1 && n <= most && d <= most && vocab <= most;
 }
 // What a matrix of rows x cols elements has to be for the copies: PRM_OK, or why not.

@@ -92,7 +92,8 @@ def head_backward(**change):
 
 
 SHARED = [
-    (dict(n=-1), B.PRM_ERR_SHAPE), (dict(d=0), B.PRM_ERR_SHAPE), (dict(vocab=0), B.PRM_ERR_SHAPE), (dict(vocab=2 ** 31), B.PRM_ERR_SHAPE),
+    (dict(n=-1), B.PRM_ERR_SHAPE), (dict(d=0), B.PRM_ERR_SHAPE), (dict(vocab=0), B.PRM_ERR_SHAPE), (dict(vocab=2 ** 27 + 1, ldw=2 ** 28), B.PRM_ERR_SHAPE),
+    (dict(n=2 ** 27 + 1), B.PRM_ERR_SHAPE), (dict(d=2 ** 27 + 1, ldx=2 ** 28), B.PRM_ERR_SHAPE),
     (dict(x=None), B.PRM_ERR_ARG), (dict(w=None), B.PRM_ERR_ARG), (dict(labels=None), B.PRM_ERR_ARG), (dict(lse=None), B.PRM_ERR_ARG),
     (dict(scratch=None), B.PRM_ERR_ARG), (dict(ldx=63), B.PRM_ERR_SHAPE), (dict(ldw=120), B.PRM_ERR_SHAPE), (dict(ldx=65), B.PRM_ERR_ALIGN),
     (dict(x=P + 8), B.PRM_ERR_ALIGN), (dict(w=P + 2), B.PRM_ERR_ALIGN), (dict(ldw=132), B.PRM_ERR_ALIGN), (dict(labels=P + 4), B.PRM_ERR_ALIGN),
