@@ -559,16 +559,17 @@ PRM_API int prm_q8_status(void);
  *   prm_layernorm_scratch_bytes(rows, cols, rows_per_group) bytes.  With rows = 0 the sums of one group are set to 0.
  * prm_head_loss   softmax cross entropy of the logits x W (n x d by d x vocab), which are not kept:
  *     lse = log sum_v exp(logit_v),  loss = lse - logit_label, 0 for a row whose label is not in 0..vocab-1
- *   x and weight bf16; weight_transposed = 0: stored d x vocab, 1: vocab x d (an embedding).  Both 16-byte
- *   aligned with row strides that are multiples of 8 (else PRM_ERR_ALIGN).  loss_out, lse_out: fp32 vectors of n.
+ *   x and weight bf16; weight_transposed = 0: stored d x vocab, 1: vocab x d (an embedding).  One that is not 16-byte
+ *   aligned with a row stride that is a multiple of 8 is copied first.  loss_out, lse_out: fp32 vectors of n.
  *   A row with a NaN or an infinite logit gets a NaN.  n may be 0; n, d and vocab 2^27 at most.  scratch: device, 16-byte aligned,
- *   prm_head_loss_scratch_bytes(n, d, vocab) bytes.
+ *   prm_head_loss_scratch_bytes(n, d, vocab) bytes, and for each operand that is copied
+ *   prm_head_loss_copy_bytes(rows, columns as stored) more.
  * prm_head_loss_backward   from grad_loss (fp32, n): with G = grad_loss (softmax - [label]), 0 for rows without a label,
  *     grad_x = G W^T (bf16, n x d),  grad_weight = x^T G (bf16, stored like weight); either may be NULL
  *   G is rounded to bf16 (after division by the largest |grad_loss|) for the products, whose sums are fp32.  Rows of x
  *   without a label count as 0 times x in grad_weight: they must be finite.
- *   scratch: device, 256-byte aligned, prm_head_loss_backward_scratch_bytes(n, d, vocab) bytes: G for a piece of the
- *   vocabulary, up to 512 MB, and partial sums.  With n = 0 grad_weight is set to zero.
+ *   scratch: device, 256-byte aligned, prm_head_loss_backward_scratch_bytes(n, d, vocab) bytes (G for a piece of the
+ *   vocabulary, up to 512 MB, and partial sums), and more for copies as above.  With n = 0 grad_weight is set to zero.
  * prm_q8_status covers the waits inside the head's products too.
  */
 PRM_API int prm_dropout(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int64_t rows,
@@ -588,6 +589,7 @@ PRM_API int prm_layernorm_backward(const void* grad_y, int64_t ld_grad_y, const 
                                    int64_t ld_grad_residual, void* grad_x, int64_t ld_grad_x, void* grad_weight,
                                    void* grad_bias, void* scratch, size_t scratch_bytes, void* cuda_stream);
 PRM_API size_t prm_head_loss_scratch_bytes(int64_t n, int64_t d, int64_t vocab);
+PRM_API size_t prm_head_loss_copy_bytes(int64_t rows, int64_t cols);
 PRM_API int prm_head_loss(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int weight_transposed,
                           const int64_t* labels, int64_t n, int64_t d, int64_t vocab, float* loss_out,
                           float* lse_out, void* scratch, size_t scratch_bytes, void* cuda_stream);

@@ -55,7 +55,7 @@ EXPORTS = (
     "prm_rmsnorm_q8", "prm_rmsnorm_q8_scratch_bytes", "prm_rmsnorm_q8_backward",
     "prm_quantize_q8", "prm_quantize_q8_scratch_bytes", "prm_matmul_q8", "prm_q8_status",
     "prm_dropout", "prm_layernorm", "prm_layernorm_scratch_bytes", "prm_layernorm_backward",
-    "prm_head_loss", "prm_head_loss_scratch_bytes", "prm_head_loss_backward", "prm_head_loss_backward_scratch_bytes",
+    "prm_head_loss", "prm_head_loss_scratch_bytes", "prm_head_loss_copy_bytes", "prm_head_loss_backward", "prm_head_loss_backward_scratch_bytes",
 )
 PRM_PROF_ROW_WIDE, PRM_PROF_ROW_TALL, PRM_PROF_PREPASS, PRM_PROF_GRAM = 0, 1, 2, 3
 PRM_PROF_POLY, PRM_PROF_UPDATE, PRM_PROF_UPDATE_FINAL, PRM_PROF_GRAMSPACE, PRM_PROF_COUNT = 4, 5, 6, 7, 8
@@ -184,6 +184,8 @@ def lib():
     for name in ("prm_head_loss_scratch_bytes", "prm_head_loss_backward_scratch_bytes"):
         getattr(L, name).argtypes = [c_int64, c_int64, c_int64]
         getattr(L, name).restype = c_size_t
+    L.prm_head_loss_copy_bytes.argtypes = [c_int64, c_int64]
+    L.prm_head_loss_copy_bytes.restype = c_size_t
     L.prm_head_loss.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int64, c_void_p,
                                 c_void_p, c_void_p, c_size_t, c_void_p]
     L.prm_head_loss.restype = c_int
@@ -869,31 +871,25 @@ def prm_layernorm_backward(grad_y, h, mean, rstd, weight=None, grad_h=None, add_
     return (grad_x, grad_r, grad_w, grad_b) if p > 0 else (grad_r, None, grad_w, grad_b)
 
 
-def _head_operand(t):
-    """(matrix, row stride, 1 if it is stored the other way round) of a bf16 matrix as the head's products read
-    it; one that lies in neither way, or unaligned, is copied."""
+def _head_operand(t, either_way):
+    """(matrix, row stride, 1 if it is stored the other way round, bytes of the copy that the call makes of it) of a bf16
+    matrix as the head's products read it; one whose elements lie in neither way is copied here."""
     r, c = t.shape
     s0, s1 = t.stride()
-    if t.data_ptr() & 15 == 0:
-        if s1 == 1 or c == 1:
-            ld = s0 if r > 1 else (c + 7) // 8 * 8
-            if ld & 7 == 0 and ld >= c:
-                return t, ld, 0
-        if s0 == 1 or r == 1:
-            ld = s1 if c > 1 else (r + 7) // 8 * 8
-            if ld & 7 == 0 and ld >= r:
-                return t, ld, 1
-    if s0 == 1 and r > 1:                   # keep the way it is stored
-        laid = torch.empty_strided((r, c), (1, (r + 7) // 8 * 8), dtype=t.dtype, device=t.device)
-        laid.copy_(t)
-        return laid, (r + 7) // 8 * 8, 1
-    laid = torch.empty_strided((r, c), ((c + 7) // 8 * 8, 1), dtype=t.dtype, device=t.device)
-    laid.copy_(t)
-    return laid, (c + 7) // 8 * 8, 0
+    if (s1 == 1 or c == 1) and (s0 >= c or r == 1):
+        ld, transposed, rows, cols = (s0 if r > 1 else (c + 7) // 8 * 8), 0, r, c
+    elif either_way and (s0 == 1 or r == 1) and (s1 >= r or c == 1):
+        ld, transposed, rows, cols = (s1 if c > 1 else (r + 7) // 8 * 8), 1, c, r
+    else:
+        t = t.contiguous()
+        ld, transposed, rows, cols = c, 0, r, c
+    if t.data_ptr() & 15 == 0 and ld & 7 == 0:
+        return t, ld, transposed, 0
+    return t, ld, transposed, (_lib_handle or lib()).prm_head_loss_copy_bytes(rows, cols)
 
 
 def _head_arguments(x, weight, labels):
-    """x, its row stride, weight, its row stride, whether it is transposed, labels."""
+    """x, its row stride, weight, its row stride, whether it is transposed, labels, bytes for copies."""
     if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[0]:
         raise ValueError("x must be n x d and weight d x vocab")
     if x.dtype is not torch.bfloat16 or weight.dtype is not torch.bfloat16:
@@ -904,12 +900,9 @@ def _head_arguments(x, weight, labels):
     if x.shape[1] == 0 or weight.shape[1] == 0:
         raise ValueError("d and vocab must be at least 1")
     labels = _vector(labels, "labels", x.shape[0], index, _INT64_ONLY)
-    laid, ld_x, x_t = _head_operand(x)
-    if x_t:                                 # x is read by rows
-        laid = torch.empty_strided(x.shape, ((x.shape[1] + 7) // 8 * 8, 1), dtype=x.dtype, device=x.device)
-        laid.copy_(x)
-        ld_x = (x.shape[1] + 7) // 8 * 8
-    return (laid, ld_x, *_head_operand(weight), labels)
+    x, ld_x, _, x_copy = _head_operand(x, False)
+    weight, ld_w, w_t, w_copy = _head_operand(weight, True)
+    return x, ld_x, weight, ld_w, w_t, labels, x_copy + w_copy
 
 
 def prm_head_loss(x, weight, labels, stream=None):
@@ -917,25 +910,25 @@ def prm_head_loss(x, weight, labels, stream=None):
 
     x: n x d, weight: d x vocab (or the transposed view of an embedding), both bf16; labels: n int64.  A label
     outside 0..vocab-1 leaves its row out: loss 0.  lse, the logarithm of the row's sum of exponentials, goes to the
-    gradient.  Matrices whose rows do not start on 16 bytes are copied first."""
+    gradient.  Matrices whose rows do not start on 16 bytes are copied first, by each call."""
     if stream is not None:
         return _on_stream(stream, (x, weight, labels), lambda: prm_head_loss(x, weight, labels))
     n, d = x.shape if x.dim() == 2 else (0, 0)
-    x, ld_x, weight, ld_w, w_t, labels = _head_arguments(x, weight, labels)
+    x, ld_x, weight, ld_w, w_t, labels, copies = _head_arguments(x, weight, labels)
     vocab = weight.shape[1]
     index = x.get_device()
-    out = torch.empty_strided((2, n), (n, 1), dtype=torch.float32, device=x.device)
+    loss = torch.empty_strided((n,), (1,), dtype=torch.float32, device=x.device)
+    lse = torch.empty_strided((n,), (1,), dtype=torch.float32, device=x.device)
     L = _lib_handle or lib()
-    nbytes = L.prm_head_loss_scratch_bytes(n, d, vocab)
+    nbytes = L.prm_head_loss_scratch_bytes(n, d, vocab) + copies
     scratch = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=x.device)
-    o_ptr = out.data_ptr()
-    args = (x.data_ptr(), ld_x, weight.data_ptr(), ld_w, w_t, labels.data_ptr(), n, d, vocab, o_ptr, o_ptr + 4 * n,
+    args = (x.data_ptr(), ld_x, weight.data_ptr(), ld_w, w_t, labels.data_ptr(), n, d, vocab, loss.data_ptr(), lse.data_ptr(),
             scratch.data_ptr(), nbytes, _raw_stream(index))
     fn = L.prm_head_loss
     code = fn(*args) if torch._C._cuda_getDevice() == index else _on_device(index, fn, *args)
     if code:
         _q8_check(code, "prm_head_loss")
-    return out[0], out[1]
+    return loss, lse
 
 
 def prm_head_loss_backward(grad_loss, x, weight, labels, lse, need_x=True, need_weight=True, stream=None):
@@ -945,7 +938,7 @@ def prm_head_loss_backward(grad_loss, x, weight, labels, lse, need_x=True, need_
         return _on_stream(stream, (grad_loss, x, weight, labels, lse),
                           lambda: prm_head_loss_backward(grad_loss, x, weight, labels, lse, need_x, need_weight))
     n, d = x.shape if x.dim() == 2 else (0, 0)
-    x, ld_x, weight, ld_w, w_t, labels = _head_arguments(x, weight, labels)
+    x, ld_x, weight, ld_w, w_t, labels, copies = _head_arguments(x, weight, labels)
     vocab = weight.shape[1]
     index = x.get_device()
     grad_loss = _vector(grad_loss, "grad_loss", n, index)
@@ -958,7 +951,7 @@ def prm_head_loss_backward(grad_loss, x, weight, labels, lse, need_x=True, need_
         gw = torch.empty_strided((d, vocab), (1, d) if w_t else (vocab, 1), dtype=torch.bfloat16, device=x.device)
         gw_ptr = gw.data_ptr()
     L = _lib_handle or lib()
-    nbytes = L.prm_head_loss_backward_scratch_bytes(n, d, vocab)
+    nbytes = L.prm_head_loss_backward_scratch_bytes(n, d, vocab) + copies
     scratch = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=x.device)
     args = (grad_loss.data_ptr(), x.data_ptr(), ld_x, weight.data_ptr(), ld_w, w_t, labels.data_ptr(), lse.data_ptr(), n, d,
             vocab, gx_ptr, d, gw_ptr, d if w_t else vocab, scratch.data_ptr(), nbytes, _raw_stream(index))

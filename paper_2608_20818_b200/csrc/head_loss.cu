@@ -634,6 +634,21 @@ __global__ void __launch_bounds__(1024) head_unit_kernel(const float* grad_loss,
   }
 }
 
+// A copy of an operand whose rows do not start on 16 bytes, which the copies into shared memory need: eight elements per thread.
+__global__ void __launch_bounds__(256) head_copy_kernel(const uint16_t* p, int64_t ld, int64_t rows, int cols, uint16_t* out,
+                                                        int64_t ld_out) {
+  grid_wait();
+  grid_trigger();
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, octs = ld_out / 8, row = at / octs;
+  if (row >= rows) return;
+  const int c = (int)(at - row * octs) * 8;
+  uint32_t v[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? p[row * ld + c + k] : 0;
+  *reinterpret_cast<uint4*>(out + row * ld_out + c) =
+      make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
 // grad_x from the parts of its sums.
 __global__ void __launch_bounds__(256) head_sum_kernel(const float* part, int parts, int64_t stride, int rows, int cols,
                                                        int64_t ld_part, const float* unit, __nv_bfloat16* out, int64_t ld_out) {
@@ -768,11 +783,25 @@ bool sizes_ok(int64_t n, int64_t d, int64_t vocab) {
   const int64_t most = (int64_t)1 << 27;
   return n >= 0 && d >= 1 && vocab >= 1 && n <= most && d <= most && vocab <= most;
 }
-// What a matrix of rows x cols elements has to be for the copies: PRM_OK, or why not.
+// Whether a matrix can be read at all: PRM_OK, or why not.
 int operand_code(const void* p, int64_t ld, int64_t cols) {
   if (!p) return PRM_ERR_ARG;
   if (ld < cols || ld >= ((int64_t)1 << 38)) return PRM_ERR_SHAPE;
-  return aligned16(p) && ld % 8 == 0 ? PRM_OK : PRM_ERR_ALIGN;
+  return (uintptr_t)p % 2 == 0 ? PRM_OK : PRM_ERR_ALIGN;
+}
+bool operand_aligned(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
+size_t copy_bytes(int64_t rows, int64_t cols) { return (size_t)ceil_to(rows * ceil_to(cols, 8) * 2, 256); }
+// Puts a copy of an operand that is not aligned at `tail` and moves both on.
+int place(const void*& p, int64_t& ld, int64_t rows, int64_t cols, char*& tail, cudaStream_t stream) {
+  if (operand_aligned(p, ld)) return PRM_OK;
+  const int64_t wide = ceil_to(cols, 8), blocks = (rows * (wide / 8) + 255) / 256;
+  if (blocks > 0x7fffffffLL) return PRM_ERR_SHAPE;
+  const int code = q8_code(launch_after(head_copy_kernel, (unsigned)blocks, 256, 0, stream, 0, (const uint16_t*)p, ld, rows,
+                                        (int)cols, (uint16_t*)tail, wide));
+  p = tail;
+  ld = wide;
+  tail += copy_bytes(rows, cols);
+  return code;
 }
 
 }  // namespace
@@ -780,9 +809,13 @@ int operand_code(const void* p, int64_t ld, int64_t cols) {
 
 using namespace prm;
 
+extern "C" size_t prm_head_loss_copy_bytes(int64_t rows, int64_t cols) {
+  return rows < 1 || cols < 1 ? 0 : copy_bytes(rows, cols);
+}
+
 extern "C" size_t prm_head_loss_scratch_bytes(int64_t n, int64_t d, int64_t vocab) {
   if (n < 1 || !sizes_ok(n, d, vocab)) return 0;
-  return (size_t)stats_rows(n, vocab) * ((size_t)stats_parts(n, vocab) * 8 + 4);
+  return (size_t)ceil_to((int64_t)stats_rows(n, vocab) * (stats_parts(n, vocab) * 8 + 4), 256);
 }
 
 extern "C" int prm_head_loss(const void* x, int64_t ld_x, const void* weight, int64_t ld_weight, int weight_transposed,
@@ -796,9 +829,17 @@ extern "C" int prm_head_loss(const void* x, int64_t ld_x, const void* weight, in
   if (code != PRM_OK) return code;
   if (((uintptr_t)loss_out | (uintptr_t)lse_out) % 4 != 0 || (uintptr_t)labels % 8 != 0 || !aligned16(scratch))
     return PRM_ERR_ALIGN;
-  if (scratch_bytes < prm_head_loss_scratch_bytes(n, d, vocab)) return PRM_ERR_WORKSPACE;
+  const int64_t w_rows = weight_transposed ? vocab : d, w_cols = weight_transposed ? d : vocab;
+  const size_t base = prm_head_loss_scratch_bytes(n, d, vocab);
+  if (scratch_bytes < base + (operand_aligned(x, ld_x) ? 0 : copy_bytes(n, d)) +
+                          (operand_aligned(weight, ld_weight) ? 0 : copy_bytes(w_rows, w_cols)))
+    return PRM_ERR_WORKSPACE;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
-  const Operand w = {weight, weight_transposed ? vocab : d, weight_transposed ? d : vocab, ld_weight, !weight_transposed};
+  char* tail = (char*)scratch + base;
+  code = place(x, ld_x, n, d, tail, stream);
+  if (code == PRM_OK) code = place(weight, ld_weight, w_rows, w_cols, tail, stream);
+  if (code != PRM_OK) return code;
+  const Operand w = {weight, w_rows, w_cols, ld_weight, !weight_transposed};
   const int64_t step = stats_rows(n, vocab);
   const int parts = (int)stats_parts(n, vocab);
   for (int64_t r = 0; r < n; r += step) {
@@ -829,7 +870,7 @@ extern "C" int prm_head_loss(const void* x, int64_t ld_x, const void* weight, in
 extern "C" size_t prm_head_loss_backward_scratch_bytes(int64_t n, int64_t d, int64_t vocab) {
   if (n < 1 || !sizes_ok(n, d, vocab)) return 0;
   const BackwardPlan p = backward_plan(n, d, vocab);
-  return 256 + p.g_bytes + p.part_bytes;
+  return 256 + p.g_bytes + (size_t)ceil_to((int64_t)p.part_bytes, 256);
 }
 
 extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int64_t ld_x, const void* weight,
@@ -853,13 +894,19 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
   if (code != PRM_OK) return code;
   if (((uintptr_t)grad_loss | (uintptr_t)lse) % 4 != 0 || (uintptr_t)labels % 8 != 0 || ((uintptr_t)scratch & 255) != 0)
     return PRM_ERR_ALIGN;
-  if (scratch_bytes < prm_head_loss_backward_scratch_bytes(n, d, vocab)) return PRM_ERR_WORKSPACE;
+  const size_t base = prm_head_loss_backward_scratch_bytes(n, d, vocab);
+  if (scratch_bytes < base + (operand_aligned(x, ld_x) ? 0 : copy_bytes(n, d)) +
+                          (operand_aligned(weight, ld_weight) ? 0 : copy_bytes(w_rows, w_cols)))
+    return PRM_ERR_WORKSPACE;
+  char* tail = (char*)scratch + base;
+  code = place(x, ld_x, n, d, tail, stream);
+  if (code == PRM_OK) code = place(weight, ld_weight, w_rows, w_cols, tail, stream);
   const BackwardPlan plan = backward_plan(n, d, vocab);
   float* unit = (float*)scratch;
   __nv_bfloat16* g = (__nv_bfloat16*)((char*)scratch + 256);
   float* part = (float*)((char*)g + plan.g_bytes);
   const Operand w = {weight, w_rows, w_cols, ld_weight, !weight_transposed};
-  if (n > kUnitRows) code = q8_code(launch_after(head_unit_kernel, 1u, 1024, 0, stream, 0, grad_loss, labels, vocab, (int)n, unit));
+  if (code == PRM_OK && n > kUnitRows) code = q8_code(launch_after(head_unit_kernel, 1u, 1024, 0, stream, 0, grad_loss, labels, vocab, (int)n, unit));
   const bool parted = plan.part_bytes > 0;
   for (int64_t v0 = 0; v0 < vocab && code == PRM_OK; v0 += plan.piece) {
     const int64_t wide = std::min(plan.piece, vocab - v0);

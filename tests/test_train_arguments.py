@@ -95,8 +95,8 @@ SHARED = [
     (dict(n=-1), B.PRM_ERR_SHAPE), (dict(d=0), B.PRM_ERR_SHAPE), (dict(vocab=0), B.PRM_ERR_SHAPE), (dict(vocab=2 ** 27 + 1, ldw=2 ** 28), B.PRM_ERR_SHAPE),
     (dict(n=2 ** 27 + 1), B.PRM_ERR_SHAPE), (dict(d=2 ** 27 + 1, ldx=2 ** 28), B.PRM_ERR_SHAPE),
     (dict(x=None), B.PRM_ERR_ARG), (dict(w=None), B.PRM_ERR_ARG), (dict(labels=None), B.PRM_ERR_ARG), (dict(lse=None), B.PRM_ERR_ARG),
-    (dict(scratch=None), B.PRM_ERR_ARG), (dict(ldx=63), B.PRM_ERR_SHAPE), (dict(ldw=120), B.PRM_ERR_SHAPE), (dict(ldx=65), B.PRM_ERR_ALIGN),
-    (dict(x=P + 8), B.PRM_ERR_ALIGN), (dict(w=P + 2), B.PRM_ERR_ALIGN), (dict(ldw=132), B.PRM_ERR_ALIGN), (dict(labels=P + 4), B.PRM_ERR_ALIGN),
+    (dict(scratch=None), B.PRM_ERR_ARG), (dict(ldx=63), B.PRM_ERR_SHAPE), (dict(ldw=120), B.PRM_ERR_SHAPE), (dict(x=P + 1), B.PRM_ERR_ALIGN),
+    (dict(w=P + 3), B.PRM_ERR_ALIGN), (dict(labels=P + 4), B.PRM_ERR_ALIGN),
     (dict(lse=P + 2), B.PRM_ERR_ALIGN), (dict(scratch=P + 8), B.PRM_ERR_ALIGN), (dict(nbytes=16), B.PRM_ERR_WORKSPACE),
 ]
 
@@ -114,6 +114,17 @@ def test_head_loss_backward_refusals(change, code):
     assert head_backward(**change) == code
 
 
+@pytest.mark.parametrize("change", [dict(ldx=65), dict(x=P + 8), dict(w=P + 2), dict(ldw=132), dict(ldx=66, ldw=130)])
+def test_head_copies_need_their_scratch(change):
+    """An operand off 16 bytes is copied into scratch of its own: one byte less than that is refused."""
+    L = B.lib()
+    more = (L.prm_head_loss_copy_bytes(4, 64) if change.keys() & {"x", "ldx"} else 0) + \
+        (L.prm_head_loss_copy_bytes(64, 128) if change.keys() & {"w", "ldw"} else 0)
+    assert more >= 4 * 64 * 2
+    assert head(nbytes=L.prm_head_loss_scratch_bytes(4, 64, 128) + more - 1, **change) == B.PRM_ERR_WORKSPACE
+    assert head_backward(nbytes=L.prm_head_loss_backward_scratch_bytes(4, 64, 128) + more - 1, **change) == B.PRM_ERR_WORKSPACE
+
+
 def test_head_scratch_is_bounded():
     """Neither direction asks for the logits: 128 MB forward unless 2048 rows need more, and backward G for a piece of 512 MB (or
     2048 columns), grad_x's sums (16 parts at most, with few rows) and some padding."""
@@ -122,7 +133,7 @@ def test_head_scratch_is_bounded():
         for d in (8, 512, 4096):
             for vocab in (1, 1000, 32768, 262144, 1 << 21):
                 parts = 2 * -(-vocab // 256)
-                assert L.prm_head_loss_scratch_bytes(n, d, vocab) <= max(1 << 27, 2048 * parts * 8) + 4 * n
+                assert L.prm_head_loss_scratch_bytes(n, d, vocab) <= 256 + max(1 << 27, 2048 * parts * 8) + 4 * n
                 g = L.prm_head_loss_backward_scratch_bytes(n, d, vocab)
                 assert g <= 1024 + max(1 << 29, 2 * n * 2048) + 128 * n + 4 * n * (d + 3) * (16 if n <= 74 * 256 else 1)
 

@@ -252,7 +252,7 @@ def check_head(x, W, labels, gl):
     close(got_w, gw, 1.02 * bw + 1.01 * R.BF16 * gw.abs() + tiny, "grad_w")
     # each entry of G and each result is rounded by itself, at most 2^-8 / sqrt(3) in the root of the mean square if a
     # value is anywhere in its binade: few rows and columns do not average
-    if n >= 64 and W.shape[1] >= 64:
+    if n >= 64 and x.shape[1] >= 64 and W.shape[1] >= 64:
         for got, ref in ((got_x, gx), (got_w, gw)):
             assert float((got.double() - ref).norm() / ref.norm()) < R.BF16 * (2 / 3) ** 0.5
     assert torch.all(got_x[~live] == 0)
