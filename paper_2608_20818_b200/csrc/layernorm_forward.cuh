@@ -74,9 +74,9 @@ __device__ __forceinline__ RowStats row_stats(float2 (&t)[NV][4], const bool (&i
   return RowStats(sum[0], make_float2(both[0], both[1]), over, eps);
 }
 
-// Blocks per SM of the kernel for many rows: 64 registers per thread, 80 where the elements have 32 bits.
-template <typename IO>
-constexpr int layernorm_blocks(int block) { return (sizeof(IO) == 2 ? 1024 : 768) / block; }
+// Blocks per SM of the kernel for many rows: 64 registers per thread, 80 and more for wide rows (8192 x 4096 with dropout: 64.6 us,
+// with 64 registers 69.9; 131072 x 128 without: 30.8 and 28.4).
+constexpr int layernorm_blocks(int tpr, int block) { return tpr >= 256 ? 768 / block : 1024 / block; }
 
 // Few rows: one for each group of TPR threads, BLOCK / TPR rows per block, 8 * NV elements per thread.  SHIFT: octs
 // aligned in memory, of rows that start anywhere.
@@ -215,7 +215,7 @@ __host__ __device__ inline int staged_words(int cols, bool shift) {
 // bytes from L2 as the row, and their conversion (16384 x 2048 with a weight for each of 64 groups, no residual: 31.6
 // us, 4.3 TB/s; a row per block 42).  Asking the L2 for the rows after the next gains nothing here.
 template <typename IO, int NV, int TPR, int BLOCK, bool DROP, bool SHIFT>
-__global__ void __launch_bounds__(BLOCK, layernorm_blocks<IO>(BLOCK)) layernorm_many_kernel(const LayerNormArgs a) {
+__global__ void __launch_bounds__(BLOCK, layernorm_blocks(TPR, BLOCK)) layernorm_many_kernel(const LayerNormArgs a) {
   constexpr int kLines = BLOCK / TPR;
   extern __shared__ __align__(16) float staged[];
   __shared__ __align__(16) float red[kLines][TPR > 32 ? TPR / 32 : 4];
@@ -455,6 +455,7 @@ int launch_layernorm(LayerNormArgs a, cudaStream_t stream) {
                               dim3((unsigned)((rows + kRows - 1) / kRows), by_group ? (unsigned)(a.rows / rows) : 1u),
                               BLOCK, 0, stream, 0, a));
 }
+// (bf16 only: 32-bit elements leave room for fewer rows under way; 8192 x 4096 with residual 104 us, with a block per row 89.)
 template <typename IO, bool DROP, bool SHIFT, int NV, int TPR>
 int launch_layernorm_many(const LayerNormArgs& a, cudaStream_t stream) {
   constexpr int BLOCK = TPR < 256 ? 256 : TPR;
@@ -472,27 +473,30 @@ int launch_layernorm_many(const LayerNormArgs& a, cudaStream_t stream) {
   const int sms = q8_sms();
   if (sms < 1) return PRM_ERR_CUDA;
   return q8_code(launch_after(layernorm_many_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT>,
-                              (unsigned)(sms * layernorm_blocks<IO>(BLOCK)), BLOCK, smem, stream, 0, a));
+                              (unsigned)(sms * layernorm_blocks(TPR, BLOCK)), BLOCK, smem, stream, 0, a));
 }
 template <typename IO, bool DROP, bool SHIFT>
 int run_layernorm(const LayerNormArgs& a, cudaStream_t stream) {
   const int64_t c = (int64_t)a.cols + (SHIFT ? 7 : 0);         // a row may need one more oct
-  // At least some rows for each line of a block, of groups that are worth their weights' way to shared memory.  32-bit
-  // elements leave room for fewer rows under way (8192 x 4096 with residual: 104 us, with a block per row 89).
-  const bool many = sizeof(IO) == 2 && a.rows * a.cols >= (int64_t)148 * 4 * 4 * 4096 && a.rows_per_group >= 16;
-#define PRM_TRY(NV, TPR)                                                                  \
-  if (c <= 8 * NV * TPR) return many ? launch_layernorm_many<IO, DROP, SHIFT, NV, TPR>(a, stream) \
-                                     : launch_layernorm<IO, DROP, SHIFT, NV, TPR>(a, stream)
-  PRM_TRY(1, 8);
-  PRM_TRY(1, 16);
-  PRM_TRY(1, 32);
-  PRM_TRY(2, 32);
-  PRM_TRY(2, 64);
-  PRM_TRY(2, 128);
-  PRM_TRY(2, 256);
+  // At least some rows for each line of a block, of groups that are worth their weights' way to shared memory.
+  const bool many = a.rows * a.cols >= (int64_t)148 * 4 * 4 * 4096 && a.rows_per_group >= 16;
+#define PRM_TRY(NV, TPR)                                                                              \
+  if (c <= 8 * NV * TPR) {                                                                            \
+    if constexpr (sizeof(IO) == 2) {                                                                  \
+      if (many) return launch_layernorm_many<IO, DROP, SHIFT, NV, TPR>(a, stream);                    \
+    }                                                                                                 \
+    return launch_layernorm<IO, DROP, SHIFT, NV, TPR>(a, stream);                                     \
+  }
+  PRM_TRY(1, 8)
+  PRM_TRY(1, 16)
+  PRM_TRY(1, 32)
+  PRM_TRY(2, 32)
+  PRM_TRY(2, 64)
+  PRM_TRY(2, 128)
+  PRM_TRY(2, 256)
   // half of the threads idle with the next size (8192 x 4097: 91 us instead of 110)
   if (c <= 8 * 3 * 256) return launch_layernorm<IO, DROP, SHIFT, 3, 256>(a, stream);
-  PRM_TRY(2, 512);
+  PRM_TRY(2, 512)
 #undef PRM_TRY
   if (c <= 8 * 2 * 1024) return launch_layernorm<IO, DROP, SHIFT, 2, 1024>(a, stream);
   return run_layernorm_single<IO>(a, stream);
