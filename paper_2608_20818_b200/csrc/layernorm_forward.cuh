@@ -213,8 +213,9 @@ __host__ __device__ inline int staged_words(int cols, bool shift) {
 // Many rows: a block's rows are a range, BLOCK / TPR of them at a time, the next rows' loads under way while these are summed.
 // The rows of a group share weight and bias from shared memory, as fp32: fetched by each row for itself they cost as many
 // bytes from L2 as the row, and their conversion (16384 x 2048 with a weight for each of 64 groups, no residual: 31.6
-// us, 4.3 TB/s; a row per block 42).  Asking the L2 for the rows after the next gains nothing here.
-template <typename IO, int NV, int TPR, int BLOCK, bool DROP, bool SHIFT>
+// us, 4.3 TB/s; a row per block 42).  Asking the L2 for the rows after the next gains nothing here.  ROUND: one group, whose rows go
+// round the blocks, so that rows under way at a time are neighbours (8192 x 4096 with dropout: 60 us, in ranges 64; 8192 x 8192 98, 102).
+template <typename IO, int NV, int TPR, int BLOCK, bool DROP, bool SHIFT, bool ROUND>
 __global__ void __launch_bounds__(BLOCK, layernorm_blocks(TPR, BLOCK)) layernorm_many_kernel(const LayerNormArgs a) {
   constexpr int kLines = BLOCK / TPR;
   extern __shared__ __align__(16) float staged[];
@@ -223,7 +224,8 @@ __global__ void __launch_bounds__(BLOCK, layernorm_blocks(TPR, BLOCK)) layernorm
   grid_wait();
   grid_trigger();
   const int line = threadIdx.x / TPR, octs = (a.cols + 7) / 8, half = staged_words(a.cols, SHIFT) / 2;
-  const int64_t r0 = a.rows * blockIdx.x / gridDim.x, r1 = a.rows * (blockIdx.x + 1) / gridDim.x;
+  const int64_t r0 = ROUND ? (int64_t)blockIdx.x * kLines : a.rows * blockIdx.x / gridDim.x;
+  const int64_t r1 = ROUND ? a.rows : a.rows * (blockIdx.x + 1) / gridDim.x, step = ROUND ? (int64_t)gridDim.x * kLines : kLines;
   const uint64_t number = DROP ? drop_number(a.drop) : 0;
   const float one = a.affine.add_one ? 1.f : 0.f;
   Oct<IO> xv[NV], rv[NV];
@@ -262,10 +264,10 @@ __global__ void __launch_bounds__(BLOCK, layernorm_blocks(TPR, BLOCK)) layernorm
     rv[v].zero();
   }
   for (int64_t begin = r0; begin < r1;) {
-    const uint32_t group = (uint32_t)begin / a.rows_per_group;
-    const int64_t end = min(r1, (int64_t)(group + 1) * a.rows_per_group);
+    const uint32_t group = ROUND ? 0u : (uint32_t)begin / a.rows_per_group;
+    const int64_t end = ROUND ? r1 : min(r1, (int64_t)(group + 1) * a.rows_per_group);
     fetch(begin + line, end);
-    if (begin > r0) __syncthreads();                            // the group before has been read
+    if (!ROUND && begin > r0) __syncthreads();                            // the group before has been read
     // aligned octs: the first halves of all, then the second halves, so that neighbours read neighbouring 16 bytes;
     // else single words, 33 apart for 32 (neighbours read words that are 8 apart)
     for (int o = threadIdx.x; o < octs; o += BLOCK) {
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(BLOCK, layernorm_blocks(TPR, BLOCK)) layernorm
       }
     }
     __syncthreads();
-    for (int64_t base = begin; base < end; base += kLines) {
+    for (int64_t base = begin; base < end; base += step) {
       const int64_t row = base + line;
       const bool live = row < end;
       const int c0 = (int)(threadIdx.x % TPR) * 8 - shift;
@@ -305,7 +307,7 @@ __global__ void __launch_bounds__(BLOCK, layernorm_blocks(TPR, BLOCK)) layernorm
         }
         res[v] = rv[v];
       }
-      fetch(row + kLines, end);
+      fetch(row + step, end);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int c = c0 + v * TPR * 8;
@@ -456,15 +458,15 @@ int launch_layernorm(LayerNormArgs a, cudaStream_t stream) {
                               BLOCK, 0, stream, 0, a));
 }
 // (bf16 only: 32-bit elements leave room for fewer rows under way; 8192 x 4096 with residual 104 us, with a block per row 89.)
-template <typename IO, bool DROP, bool SHIFT, int NV, int TPR>
-int launch_layernorm_many(const LayerNormArgs& a, cudaStream_t stream) {
+template <typename IO, bool DROP, bool SHIFT, int NV, int TPR, bool ROUND>
+int launch_layernorm_many_as(const LayerNormArgs& a, cudaStream_t stream) {
   constexpr int BLOCK = TPR < 256 ? 256 : TPR;
   const size_t smem = (size_t)staged_words(a.cols, SHIFT) * 4;
   if (NV * TPR * 8 > 4096) {
     static PerDeviceOnce once;
     int dev;
     if (once.need(&dev)) {
-      const cudaError_t e = cudaFuncSetAttribute(layernorm_many_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT>,
+      const cudaError_t e = cudaFuncSetAttribute(layernorm_many_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT, ROUND>,
                                                  cudaFuncAttributeMaxDynamicSharedMemorySize, 72 * 1024);
       if (e != cudaSuccess) return q8_code(e);
       once.mark(dev);
@@ -472,8 +474,16 @@ int launch_layernorm_many(const LayerNormArgs& a, cudaStream_t stream) {
   }
   const int sms = q8_sms();
   if (sms < 1) return PRM_ERR_CUDA;
-  return q8_code(launch_after(layernorm_many_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT>,
+  return q8_code(launch_after(layernorm_many_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT, ROUND>,
                               (unsigned)(sms * layernorm_blocks(TPR, BLOCK)), BLOCK, smem, stream, 0, a));
+}
+template <typename IO, bool DROP, bool SHIFT, int NV, int TPR>
+int launch_layernorm_many(const LayerNormArgs& a, cudaStream_t stream) {
+  // 64 registers per thread leave no room for the step beside the generator (16384 x 2048 with dropout: 78 us instead of 65)
+  if constexpr (!DROP || TPR >= 256) {
+    if (a.rows_per_group >= a.rows) return launch_layernorm_many_as<IO, DROP, SHIFT, NV, TPR, true>(a, stream);
+  }
+  return launch_layernorm_many_as<IO, DROP, SHIFT, NV, TPR, false>(a, stream);
 }
 template <typename IO, bool DROP, bool SHIFT>
 int run_layernorm(const LayerNormArgs& a, cudaStream_t stream) {
