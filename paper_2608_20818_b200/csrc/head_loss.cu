@@ -22,6 +22,7 @@
 // 1374 under the same power cap); 2048 x 1024 x 32768 103 us and 322 us; one token 4096 x 32768 57 us, 4.7 TB/s.
 // Every barrier wait is bounded; one that runs out sets the status word, the pair drains and leaves.
 #include "q8_matmul.cuh"
+#include "train_plan.h"
 
 namespace prm {
 namespace {
@@ -79,23 +80,15 @@ struct HeadArgs {
 struct HeadLaunch {
   CUtensorMap p[2], q[2];
   HeadArgs a[2];
-  int extra;                       // see next_tile
+  int extra;                       // see pair_tile
 };
 
-// The i-th tile of a pair.  Two products: the first one's tiles go round the pairs; those that its last round leaves idle
-// take `extra` tiles of the second for it, as many as take as long as one of the first; then the second's rest goes round.
 template <int EPI>
 __device__ __forceinline__ bool next_tile(const HeadLaunch& l, int pair, int pairs, int i, int& which, int& tile) {
-  const int t0 = l.a[0].tiles;
+  if constexpr (EPI == kStore) return pair_tile(l.a[0].tiles, l.a[1].tiles, l.extra, pair, pairs, i, which, tile);
   which = 0;
   tile = pair + i * pairs;
-  if constexpr (EPI != kStore) return tile < t0;
-  if (tile < t0) return true;
-  which = 1;
-  const int t1 = l.a[1].tiles, used = t0 % pairs, extra = used > 0 && pair >= used ? l.extra : 0;
-  i -= t0 / pairs + (pair < used);
-  tile = i < extra ? (pair - used) * extra + i : (used > 0 ? (pairs - used) * l.extra : 0) + pair + (i - extra) * pairs;
-  return tile < t1;
+  return tile < l.a[0].tiles;
 }
 
 __device__ __forceinline__ float ex2(float v) {

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "dropout.cuh"
+#include "train_plan.h"
 
 namespace prm {
 
@@ -150,29 +151,6 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* red) {
       for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, s, k);
     }
   }
-}
-
-// The gradient's blocks: every group of rows has `parts` of them, as many as are resident together.  The sizes
-// do not depend on the device, so that the scratch's do not either.
-inline int64_t layernorm_parts_most(int64_t cols) {
-  return cols <= 256 ? 444 : cols <= 512 ? 592 : cols <= 1024 ? 1184 : cols <= 2048 ? 592 : cols <= 4096 ? 296 : 148;
-}
-// Rows that start anywhere need 8 | parts * (rows per block and turn), or a turn for all rows, so that all
-// rows of a thread start alike: up to 8 parts.
-inline int64_t layernorm_parts_bound(int64_t rows_per_group, int64_t groups, int64_t cols) {
-  return std::min(rows_per_group, std::max<int64_t>(8, layernorm_parts_most(cols) / groups));
-}
-inline int64_t layernorm_parts(int64_t rows_per_group, int64_t groups, int64_t cols, int rows_per_turn, int blocks,
-                               bool shift) {
-  const int64_t turns = (rows_per_group + rows_per_turn - 1) / rows_per_turn;
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>(blocks, layernorm_parts_most(cols)) / groups);
-  // a block has two rows before more than an SM's worth of blocks have one: each leaves a line to add
-  parts = std::min(parts, std::max<int64_t>((148 + groups - 1) / groups, turns / 2));
-  if (shift) {
-    const int64_t unit = rows_per_turn >= 8 ? 1 : 8 / rows_per_turn;
-    parts = std::max(unit, parts / unit * unit);
-  }
-  return std::min(parts, turns);
 }
 
 }  // namespace prm
