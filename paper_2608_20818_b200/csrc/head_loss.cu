@@ -68,6 +68,10 @@ struct HeadArgs {
   const float* grad_loss;
   __nv_bfloat16* g;
   int64_t ld_g;
+  const __nv_bfloat16* x;          // kGrad: where x is to be copied to without the rows that have no part, else null
+  __nv_bfloat16* clean;
+  int64_t ld_x, ld_clean;
+  int d;
   // kGrad, kStore
   const float* unit;               // c; null: 1
   float* unit_out;                 // kGrad: c is computed by every block, and left here (kUnitRows rows at most)
@@ -190,6 +194,32 @@ __device__ __forceinline__ float unit_share(const float* grad_loss, const int64_
 }
 __device__ __forceinline__ float unit_of(float top) { return top > 0.f && top < INFINITY ? top : 1.f; }
 constexpr int kUnitRows = 2048;                  // for more it has a launch of its own
+
+// Rows first, first + rows_apart, ... of x, one by one, to `clean`: zeros for a row without a label or with the gradient 0.  grad_W's sums
+// run over the rows; what such a row of x holds (padding, which may be no number) must not reach them, not even times 0.
+__device__ __forceinline__ void copy_live_rows(const HeadArgs& a, int first, int rows_apart) {
+  const int lane = threadIdx.x & 31, octs = (a.d + 7) / 8;
+  for (int64_t row = first; row < a.m; row += rows_apart) {
+    const int64_t l = a.labels[row];
+    const bool live = l >= 0 && l < a.vocab && a.grad_loss[row] != 0.f;
+    const __nv_bfloat16* x = a.x + row * a.ld_x;
+    uint4* to = reinterpret_cast<uint4*>(a.clean + row * a.ld_clean);
+#pragma unroll 4
+    for (int o = lane; o < octs; o += 32) {
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (live && o * 8 + 8 <= a.d) {
+        v = *reinterpret_cast<const uint4*>(x + o * 8);
+      } else if (live) {                   // what lies behind the row may be no memory of x
+        const uint16_t* e = reinterpret_cast<const uint16_t*>(x + o * 8);
+        uint32_t h[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) h[k] = o * 8 + k < a.d ? e[k] : 0;
+        v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+      }
+      to[o] = v;
+    }
+  }
+}
 
 // 128 columns of the lane's row of G.
 __device__ __forceinline__ void grad_tile(const HeadArgs& a, uint32_t taddr, uint8_t* patch, int m0, int n0, int rows,
@@ -476,6 +506,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         asm volatile("bar.sync 1, %0;" ::"n"(kEpiWarps * 32) : "memory");
         if (blockIdx.x == 0 && threadIdx.x == 64) *a.unit_out = unit;
       }
+      // under the first tile's main loop
+      if (a.clean) copy_live_rows(a, (int)blockIdx.x * kEpiWarps + warp - 2, (int)gridDim.x * kEpiWarps);
     }
     uint32_t acc = 0;
     bool ok = true;
@@ -863,7 +895,7 @@ extern "C" int prm_head_loss(const void* x, int64_t ld_x, const void* weight, in
 extern "C" size_t prm_head_loss_backward_scratch_bytes(int64_t n, int64_t d, int64_t vocab) {
   if (n < 1 || !sizes_ok(n, d, vocab)) return 0;
   const BackwardPlan p = backward_plan(n, d, vocab);
-  return 256 + p.g_bytes + (size_t)ceil_to((int64_t)p.part_bytes, 256);
+  return 256 + p.g_bytes + (size_t)ceil_to((int64_t)p.part_bytes, 256) + copy_bytes(n, d);
 }
 
 extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int64_t ld_x, const void* weight,
@@ -898,6 +930,8 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
   float* unit = (float*)scratch;
   __nv_bfloat16* g = (__nv_bfloat16*)((char*)scratch + 256);
   float* part = (float*)((char*)g + plan.g_bytes);
+  __nv_bfloat16* clean = (__nv_bfloat16*)((char*)scratch + base - copy_bytes(n, d));
+  const int64_t ld_clean = ceil_to(d, 8);
   const Operand w = {weight, w_rows, w_cols, ld_weight, !weight_transposed};
   if (code == PRM_OK && n > kUnitRows) code = q8_code(launch_after(head_unit_kernel, 1u, 1024, 0, stream, 0, grad_loss, labels, vocab, (int)n, unit));
   const bool parted = plan.part_bytes > 0;
@@ -916,6 +950,11 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
     a.ld_g = plan.ld_g;
     a.unit = n > kUnitRows || v0 > 0 ? unit : nullptr;
     a.unit_out = a.unit ? nullptr : unit;
+    a.x = (const __nv_bfloat16*)x;
+    a.ld_x = ld_x;
+    a.clean = grad_weight && v0 == 0 ? clean : nullptr;
+    a.ld_clean = ld_clean;
+    a.d = (int)d;
     code = launch_logits<kGrad>({x, n, d, ld_x, false}, w, a, d, stream);
     HeadLaunch l = {};                     // the two products that read G: one launch
     int products = 0;
@@ -939,7 +978,7 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
       b.split = 1;
       b.unit = unit;
       b.ld_out = ld_grad_weight;
-      const Operand gt = {g, n, wide, plan.ld_g, true}, xt = {x, n, d, ld_x, true};
+      const Operand gt = {g, n, wide, plan.ld_g, true}, xt = {clean, n, d, ld_clean, true};
       if (weight_transposed) {
         b.m = (int)wide;
         b.n = (int)d;

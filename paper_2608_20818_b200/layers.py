@@ -155,7 +155,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, residual=None, p=0.0, draws=
 
 def head_loss(x, weight, labels):
     """Softmax cross entropy of the logits x @ weight for labels (...): fp32 losses of labels' shape, 0 where a label is not in
-    0..vocab-1 (such rows of x must be finite all the same where the weight needs its gradient).  x (..., d), weight d x vocab,
+    0..vocab-1 (such a row has no part in the gradients, whatever it holds).  x (..., d), weight d x vocab,
     or the transposed view of an embedding, both bf16."""
     if labels.shape != x.shape[:-1]:
         raise ValueError("labels must have x's shape without its last dimension")

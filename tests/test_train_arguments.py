@@ -127,7 +127,7 @@ def test_head_copies_need_their_scratch(change):
 
 def test_head_scratch_is_bounded():
     """Neither direction asks for the logits: 128 MB forward unless 2048 rows need more, and backward G for a piece of 512 MB (or
-    2048 columns), grad_x's sums (16 parts at most, with few rows) and some padding."""
+    2048 columns), grad_x's sums (16 parts at most, with few rows), x once more and some padding."""
     L = B.lib()
     for n in (1, 7, 256, 8192, 65536, 1 << 20):
         for d in (8, 512, 4096):
@@ -135,7 +135,7 @@ def test_head_scratch_is_bounded():
                 parts = 2 * -(-vocab // 256)
                 assert L.prm_head_loss_scratch_bytes(n, d, vocab) <= 256 + max(1 << 27, 2048 * parts * 8) + 4 * n
                 g = L.prm_head_loss_backward_scratch_bytes(n, d, vocab)
-                assert g <= 1024 + max(1 << 29, 2 * n * 2048) + 128 * n + 4 * n * (d + 3) * (16 if n <= 74 * 256 else 1)
+                assert g <= 1024 + max(1 << 29, 2 * n * 2048) + 128 * n + 4 * n * (d + 3) * (16 if n <= 74 * 256 else 1) + 2 * n * d
 
 
 def test_binding_refusals_without_a_device():

@@ -379,6 +379,26 @@ def test_head_loss_of_what_is_no_number():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,d,vocab,how", [(5, 64, 300, "in_out"), (300, 100, 700, "out_in"), (2500, 77, 513, "padded"), (131072, 8, 4000, "in_out")])
+def test_head_gradient_ignores_what_rows_without_a_part_hold(n, d, vocab, how):
+    """Padding that is no number: rows without a label, and rows whose loss has the gradient 0."""
+    x, W, labels = head_inputs(n, d, vocab, how, n)
+    gl = torch.exp(randn(n, n))
+    labels[::3] = -100
+    gl[1::7] = 0
+    dead = (labels < 0) | (labels >= vocab) | (gl == 0)
+    x[dead] = 0
+    _, lse = B.prm_head_loss(x, W, labels)
+    want = B.prm_head_loss_backward(gl, x, W, labels, lse)
+    for junk in (float("nan"), float("inf"), -3e38):
+        x[dead] = junk
+        loss, lse = B.prm_head_loss(x, W, labels)
+        assert torch.all(torch.isfinite(loss[~dead])) and torch.all(loss[(labels < 0) | (labels >= vocab)] == 0)
+        got = B.prm_head_loss_backward(gl, x, W, labels, lse)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.all(got[0][dead] == 0)
+
+
+@pytest.mark.gpu
 def test_head_loss_without_rows_or_labels():
     x, W, labels = head_inputs(20, 64, 700, "in_out", 10)
     loss, lse = B.prm_head_loss(x[:0], W, labels[:0])
