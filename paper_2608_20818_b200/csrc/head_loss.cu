@@ -19,7 +19,7 @@
 //   warps 2..9  epilogue: two warps per lane quadrant, half of the 256 columns each; a thread has a row
 // Two accumulators of 256 columns let the epilogue of a tile run under the next tile's main loop.
 // Measured: 8192 x 4096 x 131072 6.3 ms, 1400 TFLOP/s, its gradient with 65536 columns 10.0 ms, 1325 TFLOP/s (cuBLAS sustains
-// 1374 under the same power cap); 2048 x 1024 x 32768 103 us and 322 us; one token 4096 x 32768 57 us, 4.7 TB/s.
+// 1374 under the same power cap); 2048 x 1024 x 32768 101 us and 318 us; one token 4096 x 32768 57 us, 4.7 TB/s.
 // Every barrier wait is bounded; one that runs out sets the status word, the pair drains and leaves.
 #include "q8_matmul.cuh"
 #include "train_plan.h"
@@ -280,6 +280,7 @@ __device__ __forceinline__ void store_tile(const HeadArgs& a, uint32_t taddr, ui
   const int lane = threadIdx.x & 31;
   OUT* out = reinterpret_cast<OUT*>(a.out) + split * a.split_stride + (int64_t)m0 * a.ld_out + n0;
   const bool vec = ((uintptr_t)out & 15) == 0 && (a.ld_out * (int64_t)sizeof(OUT)) % 16 == 0;
+  const bool by4 = ((uintptr_t)out & 3) == 0 && a.ld_out % 2 == 0;
 #pragma unroll 1
   for (int k = 0; k < 4; ++k) {
     if (n0 + k * 32 >= a.n) break;
@@ -324,6 +325,14 @@ __device__ __forceinline__ void store_tile(const HeadArgs& a, uint32_t taddr, ui
             }
             *p = x;
           }
+        }
+      } else if (sizeof(OUT) == 2 && by4 && wide == kCols) {     // rows that start on 4 bytes: two columns per lane
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+          const int row = i * 2 + (lane >> 4), c = (lane & 15) * 4;
+          if (row < rows)
+            *reinterpret_cast<uint32_t*>(to + row * a.ld_out + c / 2) =
+                *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(patch_at(patch, row, c >> 4)) + (c & 15));
         }
       } else {
 #pragma unroll 4
@@ -667,11 +676,22 @@ __global__ void __launch_bounds__(256) head_copy_kernel(const uint16_t* p, int64
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, octs = ld_out / 8, row = at / octs;
   if (row >= rows) return;
   const int c = (int)(at - row * octs) * 8;
-  uint32_t v[8];
+  p += row * ld + c;
+  uint4 v;
+  if (c + 8 <= cols && ((uintptr_t)p & 2) == 0) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  } else if (c + 8 <= cols) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(p + 1);
+    const uint32_t e0 = p[0], w0 = w[0], w1 = w[1], w2 = w[2], e7 = p[7];
+    v = make_uint4(e0 | w0 << 16, w0 >> 16 | w1 << 16, w1 >> 16 | w2 << 16, w2 >> 16 | e7 << 16);
+  } else {
+    uint32_t e[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? p[row * ld + c + k] : 0;
-  *reinterpret_cast<uint4*>(out + row * ld_out + c) =
-      make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    for (int k = 0; k < 8; ++k) e[k] = c + k < cols ? p[k] : 0;
+    v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+  }
+  *reinterpret_cast<uint4*>(out + row * ld_out + c) = v;
 }
 
 // grad_x from the parts of its sums.
