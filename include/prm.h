@@ -561,7 +561,7 @@ PRM_API int prm_q8_status(void);
  *     lse = log sum_v exp(logit_v),  loss = lse - logit_label, 0 for a row whose label is not in 0..vocab-1
  *   x and weight bf16; weight_transposed = 0: stored d x vocab, 1: vocab x d (an embedding).  One that is not 16-byte
  *   aligned with a row stride that is a multiple of 8 is copied first.  loss_out, lse_out: fp32 vectors of n.
- *   A row with a NaN or an infinite logit gets a NaN.  n may be 0; n, d and vocab 2^27 at most.  scratch: device, 16-byte aligned,
+ *   A row with a logit that is NaN or +infinity gets a NaN (-infinity counts as nothing).  n may be 0; n, d and vocab 2^27 at most.  scratch: device, 16-byte aligned,
  *   prm_head_loss_scratch_bytes(n, d, vocab) bytes, and for each operand that is copied
  *   prm_head_loss_copy_bytes(rows, columns as stored) more.
  * prm_head_loss_backward   from grad_loss (fp32, n): with G = grad_loss (softmax - [label]), 0 for rows without a label,

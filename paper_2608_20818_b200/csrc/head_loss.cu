@@ -62,8 +62,9 @@ struct HeadArgs {
   // kStats, kGrad
   const int64_t* labels;
   int64_t vocab;
-  float2* part;                    // [2 n_tiles][m]: largest logit * log2 e, sum of 2^(logit log2 e - that)
-  float* at_label;                 // [m]
+  float2* part;                    // [2 n_tiles][m] (kFew: [ceil(vocab / 256) 8][n]): largest logit * log2 e, sum of
+                                   // 2^(logit log2 e - that)
+  float* at_label;                 // of each row
   const float* lse;
   const float* grad_loss;
   __nv_bfloat16* g;
