@@ -27,10 +27,11 @@
 namespace prm {
 namespace {
 
-constexpr int kTile = 256;                       // tile edge, both ways
+constexpr int kTile = kHeadTile;                 // tile edge, both ways
 constexpr int kHeadK = 64;                       // one 128-byte swizzled row of k
 constexpr int kSub = 2;                          // k-blocks per stage
 constexpr int kStages = 3;
+static_assert(kHeadStage == kSub * kHeadK, "the plan's stage");
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 32 * (2 + kEpiWarps);
 constexpr uint32_t kBoxBytes = 128 * 128;        // 128 rows of one k-block
@@ -114,9 +115,7 @@ __device__ __forceinline__ void tile_origin(const HeadArgs& a, int t, int& split
   n0 = rest / height * kTile;
 }
 __device__ __forceinline__ void split_range(const HeadArgs& a, int split, int& s0, int& s1) {
-  const int stages = (a.kblocks + kSub - 1) / kSub;
-  s0 = (int)((int64_t)stages * split / a.split);
-  s1 = (int)((int64_t)stages * (split + 1) / a.split);
+  head_part((a.kblocks + kSub - 1) / kSub, a.split, split, s0, s1);
 }
 
 // The label of a row as a column of the 128 from n0 on, -1 if it is none of them.
@@ -723,8 +722,6 @@ bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, in
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-inline int64_t ceil_to(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
-
 struct Operand {
   const void* p;
   int64_t rows, cols, ld;          // as stored
@@ -798,30 +795,6 @@ int64_t stats_parts(int64_t n, int64_t vocab) { return (n <= kFewRows ? 8 : 2) *
 int64_t stats_rows(int64_t n, int64_t vocab) {
   const int64_t parts = stats_parts(n, vocab);
   return std::min(n, std::max<int64_t>(2048, ((int64_t)128 << 20) / (8 * parts) / kTile * kTile));
-}
-
-// Backward: pieces of the vocabulary whose G fits 512 MB, of alike width (pieces that stay in the L2, 64 MB, leave each product
-// too few tiles: 8192 x 64 x 32768 takes 729 us with them, 468 with one piece), and grad_x's sums: one product's parts of
-// k where there are few tiles, the pieces' running sums where there are several.
-struct BackwardPlan {
-  int64_t piece, ld_g, ld_part;
-  int pieces, split;
-  size_t g_bytes, part_bytes;
-};
-BackwardPlan backward_plan(int64_t n, int64_t d, int64_t vocab) {
-  BackwardPlan p;
-  const int64_t most = std::max<int64_t>(2048, ((int64_t)512 << 20) / (2 * n) / kTile * kTile);
-  p.pieces = (int)((vocab + most - 1) / most);
-  p.piece = ceil_to((vocab + p.pieces - 1) / p.pieces, kTile);
-  p.pieces = (int)((vocab + p.piece - 1) / p.piece);
-  p.ld_g = ceil_to(std::min(p.piece, vocab), 64);
-  const int64_t tiles = ((n + kTile - 1) / kTile) * ((d + kTile - 1) / kTile);
-  const int64_t stages = (std::min(p.piece, vocab) + kSub * kHeadK - 1) / (kSub * kHeadK);
-  p.split = (int)std::max<int64_t>(1, std::min<int64_t>({74 / tiles, stages / 4, 16}));
-  p.ld_part = ceil_to(d, 4);
-  p.g_bytes = (size_t)ceil_to(n * p.ld_g * 2, 256);
-  p.part_bytes = p.pieces > 1 || p.split > 1 ? (size_t)p.split * n * p.ld_part * 4 : 0;
-  return p;
 }
 
 // Sums as long as 2^27 leave a tile in its main loop for less than a second, half of what a wait is given.
@@ -915,7 +888,7 @@ extern "C" int prm_head_loss(const void* x, int64_t ld_x, const void* weight, in
 
 extern "C" size_t prm_head_loss_backward_scratch_bytes(int64_t n, int64_t d, int64_t vocab) {
   if (n < 1 || !sizes_ok(n, d, vocab)) return 0;
-  const BackwardPlan p = backward_plan(n, d, vocab);
+  const HeadGradPlan p = head_grad_plan(n, d, vocab);
   return 256 + p.g_bytes + (size_t)ceil_to((int64_t)p.part_bytes, 256) + copy_bytes(n, d);
 }
 
@@ -947,7 +920,7 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
   char* tail = (char*)scratch + base;
   code = place(x, ld_x, n, d, tail, stream);
   if (code == PRM_OK) code = place(weight, ld_weight, w_rows, w_cols, tail, stream);
-  const BackwardPlan plan = backward_plan(n, d, vocab);
+  const HeadGradPlan plan = head_grad_plan(n, d, vocab);
   float* unit = (float*)scratch;
   __nv_bfloat16* g = (__nv_bfloat16*)((char*)scratch + 256);
   float* part = (float*)((char*)g + plan.g_bytes);
@@ -984,7 +957,7 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
       b.m = (int)n;
       b.n = (int)d;
       b.q_k0 = (int)v0;
-      b.split = plan.split;
+      b.split = head_grad_split(plan, wide);
       b.unit = parted ? nullptr : unit;
       b.out = parted ? (void*)part : grad_x;
       b.ld_out = parted ? plan.ld_part : ld_grad_x;

@@ -1,8 +1,9 @@
-// Blocks of the layer norm's gradient and the tiles' way round the pairs of the head's products: arithmetic on sizes alone, so
-// that a host without a device can check it.
+// Blocks of the layer norm's gradient, pieces and splits of the head's gradient, and the tiles' way round the pairs of the head's
+// products: arithmetic on sizes alone, so that a host without a device can check it.
 #pragma once
 
 #include <algorithm>
+#include <cstddef>
 #include <cstdint>
 
 #ifdef __CUDACC__
@@ -34,6 +35,46 @@ inline int64_t layernorm_parts(int64_t rows_per_group, int64_t groups, int64_t c
     parts = std::max(unit, parts / unit * unit);
   }
   return std::min(parts, turns);
+}
+
+constexpr int kHeadTile = 256;                   // edge of the head's tiles
+constexpr int kHeadStage = 128;                  // k that a stage of a tile's main loop holds
+
+inline int64_t ceil_to(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
+
+// The head's gradient: pieces of the vocabulary whose G fits 512 MB, of alike width but for the last, which may have a few columns
+// only (pieces that stay in the L2, 64 MB, leave each product too few tiles: 8192 x 64 x 32768 takes 729 us with them, 468 with
+// one piece), and grad_x's sums: parts of one product's k where there are few tiles, the pieces' running sums where there are
+// several.
+struct HeadGradPlan {
+  int64_t piece, ld_g, ld_part;
+  int pieces, split;
+  size_t g_bytes, part_bytes;
+};
+inline HeadGradPlan head_grad_plan(int64_t n, int64_t d, int64_t vocab) {
+  HeadGradPlan p;
+  const int64_t most = std::max<int64_t>(2048, ((int64_t)512 << 20) / (2 * n) / kHeadTile * kHeadTile);
+  p.pieces = (int)((vocab + most - 1) / most);
+  p.piece = ceil_to((vocab + p.pieces - 1) / p.pieces, kHeadTile);
+  p.pieces = (int)((vocab + p.piece - 1) / p.piece);
+  p.ld_g = ceil_to(std::min(p.piece, vocab), 64);
+  const int64_t tiles = ((n + kHeadTile - 1) / kHeadTile) * ((d + kHeadTile - 1) / kHeadTile);
+  const int64_t stages = (std::min(p.piece, vocab) + kHeadStage - 1) / kHeadStage;
+  p.split = (int)std::max<int64_t>(1, std::min<int64_t>({74 / tiles, stages / 4, 16}));
+  p.ld_part = ceil_to(d, 4);
+  p.g_bytes = (size_t)ceil_to(n * p.ld_g * 2, 256);
+  p.part_bytes = p.pieces > 1 || p.split > 1 ? (size_t)p.split * n * p.ld_part * 4 : 0;
+  return p;
+}
+// Parts of k for a piece of `wide` columns: the plan's, but none without a stage, whose tiles would wait for sums that nobody
+// computes.  The first piece has them all; where the last one has fewer, the other parts keep the sums of the pieces before it.
+inline int head_grad_split(const HeadGradPlan& p, int64_t wide) {
+  return (int)std::min<int64_t>(p.split, (wide + kHeadStage - 1) / kHeadStage);
+}
+// The stages s0 .. s1 - 1 of part `at` of `split`.
+PRM_HOST_DEVICE inline void head_part(int stages, int split, int at, int& s0, int& s1) {
+  s0 = (int)((int64_t)stages * at / split);
+  s1 = (int)((int64_t)stages * (at + 1) / split);
 }
 
 // The i-th tile of a pair in a launch of one product (t1 = 0) or two that do not depend on one another; false if it has none
