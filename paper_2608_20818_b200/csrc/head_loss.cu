@@ -43,7 +43,7 @@ constexpr int kFewRows = 64;                     // rows that kFew takes (100 x 
 // The logits' sums are taken out of tensor memory every 1024 k and added in registers: the accumulator cuts off what
 // falls below its last bit at each of its steps (16 k), which over 4096 k puts a logit of the size 1 off by 1e-5.
 constexpr int kChunk = 8;                        // stages
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 // kStats: x (rows) times W (columns).  kFew: the same for few rows, the other way round (the rows are the instruction's N, so
 // that it costs them no more than it has to, and W's bytes have most of shared memory).
@@ -63,8 +63,7 @@ struct HeadArgs {
   // kStats, kGrad
   const int64_t* labels;
   int64_t vocab;
-  float2* part;                    // [2 n_tiles][m] (kFew: [ceil(vocab / 256) 8][n]): largest logit * log2 e, sum of
-                                   // 2^(logit log2 e - that)
+  float2* part;                    // [2 n_tiles][m] (kFew: [ceil(vocab / 256) 8][n]): largest logit, sum of e^(logit - that)
   float* at_label;                 // of each row
   const float* lse;
   const float* grad_loss;
@@ -103,6 +102,13 @@ __device__ __forceinline__ float ex2(float v) {
   return r;
 }
 
+// e^(v - top), of two logits.  The difference comes first: it is exact next to top and gives top itself a share of exactly 1, so
+// that no sum is below 1 and a row that is predicted with certainty has the loss 0.
+__device__ __forceinline__ float2 share2(float2 v, float2 minus_top) {
+  v = mul2(add2(v, minus_top), make_float2(kLog2e, kLog2e));
+  return make_float2(ex2(v.x), ex2(v.y));
+}
+
 // Order of the tiles: bands of `band` m-tiles, in a band n by n, m-tiles fastest; the splits of k one after
 // the other.  Pairs that run at the same time then share the band's rows of P and a few columns' worth of Q.
 __device__ __forceinline__ void tile_origin(const HeadArgs& a, int t, int& split, int& m0, int& n0) {
@@ -137,16 +143,20 @@ __device__ __forceinline__ void stats_tile(const HeadArgs& a, float (&v)[128], i
 #pragma unroll
   for (int j = 4; j < 128; ++j) t[j & 3] = fmaxf(t[j & 3], v[j]);
   const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-  const float top2 = top == -INFINITY ? 0.f : top * kLog2e;         // in base 2
+  const float off = top == -INFINITY ? 0.f : -top;
 #pragma unroll
-  for (int j = 0; j < 128; ++j) s[j & 3] += ex2(fmaf(v[j], kLog2e, -top2));
+  for (int j = 0; j < 128; j += 2) {
+    const float2 e = share2(make_float2(v[j], v[j + 1]), make_float2(off, off));
+    s[j & 3] += e.x;
+    s[(j + 1) & 3] += e.y;
+  }
   if (__any_sync(0xffffffffu, label >= 0)) {
 #pragma unroll
     for (int j = 0; j < 128; ++j)
       if (label == j) a.at_label[row] = v[j];
   }
   if (row < a.m)
-    a.part[(int64_t)column * a.m + row] = make_float2(top == -INFINITY ? top : top2, (s[0] + s[1]) + (s[2] + s[3]));
+    a.part[(int64_t)column * a.m + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
 // kFew: 32 columns (lanes) of 16 rows from n0 on.  They pass through shared memory, so that a lane gets 16 columns of one row.
@@ -163,13 +173,17 @@ __device__ __forceinline__ void few_tile(const HeadArgs& a, const float* v, floa
     top = fmaxf(top, t[j]);
   }
   top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-  const float top2 = top == -INFINITY ? 0.f : top * kLog2e;
+  const float off = top == -INFINITY ? 0.f : -top;
   float s = 0.f;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) s += ex2(fmaf(t[j], kLog2e, -top2));
+  for (int j = 0; j < 16; j += 2) {
+    const float2 e = share2(make_float2(t[j], t[j + 1]), make_float2(off, off));
+    s += e.x;
+    s += e.y;
+  }
   s += __shfl_xor_sync(0xffffffffu, s, 16);
   if (row < a.n && part == 0) {
-    a.part[(int64_t)(m0 / 32) * a.n + row] = make_float2(top == -INFINITY ? top : top2, s);
+    a.part[(int64_t)(m0 / 32) * a.n + row] = make_float2(top, s);
     const int64_t c = a.labels[row] - m0;
     if (c >= 0 && c < 32 && c + m0 < a.vocab) a.at_label[row] = patch[r * 32 + ((int)c ^ r)];
   }
@@ -610,14 +624,14 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
   }
 }
 
-// A row's largest logit (base 2) and sum relative to it.
+// A row's largest logit and sum relative to it.
 struct Softmax {
   float top = -INFINITY, sum = 0.f;
   __device__ __forceinline__ void add(float p_top, float p_sum) {
     const float here = fmaxf(top, p_top);
     // a part of -infinities alone has the sum 0 (NaN with a NaN among them)
-    if (top != here && top != -INFINITY) sum *= exp2f(top - here);
-    sum += p_top == here || p_top == -INFINITY ? p_sum : p_sum * exp2f(p_top - here);
+    if (top != here && top != -INFINITY) sum *= expf(top - here);
+    sum += p_top == here || p_top == -INFINITY ? p_sum : p_sum * expf(p_top - here);
     top = here;
   }
 };
@@ -647,10 +661,11 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float2* part, int 
   if (warp == 0 && lane < each && row < rows) {
 #pragma unroll
     for (int k = 1; k < 8; ++k) m.add(s[k][lane].x, s[k][lane].y);
-    const float l = (m.top + log2f(m.sum)) * kLn2;
+    const float rest = logf(m.sum);        // at least 0
     const int64_t label = labels[row];
-    lse[row] = l;
-    loss[row] = label >= 0 && label < vocab ? l - at_label[row] : 0.f;
+    lse[row] = m.top + rest;
+    // not lse - logit, whose rounding can leave less than 0
+    loss[row] = label >= 0 && label < vocab ? (m.top - at_label[row]) + rest : 0.f;
   }
 }
 

@@ -33,3 +33,31 @@ def test_gradient_whose_last_piece_has_fewer_stages_than_parts(vocab):
     _, _, _, rx, rw, bx, bw = R.head(x, W, labels, gl, part=128)
     close(gx, rx, 1.02 * bx + 1.01 * R.BF16 * rx.abs() + 1e-30, "grad_x")
     close(gw, rw, 1.02 * bw + 1.01 * R.BF16 * rw.abs() + 1e-30, "grad_w")
+
+
+def confident(n, d, vocab, size, seed):
+    """Rows along their labels' columns: their logits are about `size`, the others' some size / sqrt(d)."""
+    W = randn(seed, d, vocab).to(torch.bfloat16)
+    labels = torch.randint(0, vocab, (n,), generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+    return (W.t()[labels].float() * (size / d)).to(torch.bfloat16), W, labels
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("n", [1, 40, 512])
+@pytest.mark.parametrize("d", [64, 1024, 4096])
+@pytest.mark.parametrize("size", [10.0, 20.0, 50.0, 100.0])
+def test_loss_of_confident_rows(n, d, size, transposed):
+    """No loss is below 0, and where nothing but the label counts it is 0: what else there is, less than 2^-25 in all, leaves a
+    sum of 1 as it is."""
+    x, W, labels = confident(n, d, 2000, size, n + d)
+    W = W.t().contiguous().t() if transposed else W
+    loss, lse = B.prm_head_loss(x, W, labels)
+    want, want_lse, off, *_ = R.head(x, W, labels)
+    assert torch.all(loss >= 0)
+    sure = want < 2.0 ** -26
+    assert torch.all(loss[sure] == 0) and (size < 50 or d < 1024 or bool(torch.all(sure)))
+    # the other logits' shares are as far off as two logits and the exponential's rounding; a number is added to the sum 128 times
+    # at most (a thread's 32 and 3, the rows' parts), then the logarithm
+    close(loss, want, torch.expm1(want) * (2 * off + 2.0 ** -20) + 128 * R.F32 * (1 + want), "loss")
+    close(lse, want_lse, off + 2.0 ** -20 + 2 * R.F32 * want_lse.abs(), "lse")
