@@ -41,14 +41,15 @@ constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kEpiWarps *
 constexpr int kMaxStages = 6;
 constexpr int kFewRows = 64;                     // rows that kFew takes (100 x 4096 x 32768: 72 us, the other form 68)
 // The logits' sums are taken out of tensor memory every 1024 k and added in registers: the accumulator cuts off what
-// falls below its last bit at each of its steps (16 k), which over 4096 k puts a logit of the size 1 off by 1e-5.
+// falls below its last bit at each of its steps (16 k), which over 4096 k puts a logit of the size 1 off by 1e-5.  Both directions
+// do so, so that the gradient's logits are those that lse was made of (8192 x 4096 x 65536: 10.5 ms, 10.4 without).
 constexpr int kChunk = 8;                        // stages
 constexpr float kLog2e = 1.4426950408889634f;
 
 // kStats: x (rows) times W (columns).  kFew: the same for few rows, the other way round (the rows are the instruction's N, so
 // that it costs them no more than it has to, and W's bytes have most of shared memory).
 enum Epi { kStats, kFew, kGrad, kStore };
-__host__ __device__ constexpr bool chunked(int epi) { return epi == kStats || epi == kFew; }
+__host__ __device__ constexpr bool chunked(int epi) { return epi != kStore; }
 
 struct HeadArgs {
   int m, n, kblocks;               // of this product: rows, columns, ceil(k / 64)
@@ -235,31 +236,32 @@ __device__ __forceinline__ void copy_live_rows(const HeadArgs& a, int first, int
   }
 }
 
-// 128 columns of the lane's row of G.
-__device__ __forceinline__ void grad_tile(const HeadArgs& a, uint32_t taddr, uint8_t* patch, int m0, int n0, int rows,
+// 128 columns of the lane's row of G, of their logits.
+__device__ __forceinline__ void grad_tile(const HeadArgs& a, const float (&logit)[128], uint8_t* patch, int m0, int n0, int rows,
                                           float unit) {
   const int lane = threadIdx.x & 31, row = m0 + lane;
-  float factor = 0.f, lse2 = 0.f;
+  float factor = 0.f, off = 0.f;
   int label = -1;
   if (row < a.m) {
     const int64_t l = a.labels[row];
     if (l >= 0 && l < a.vocab) {
       factor = __fdiv_rn(a.grad_loss[row], unit);
-      lse2 = a.lse[row] * kLog2e;
+      off = -a.lse[row];
       label = label_column(a, l, n0);
     }
   }
   const bool all = __all_sync(0xffffffffu, factor != 0.f);
   __nv_bfloat16* out = a.g + (int64_t)m0 * a.ld_g + n0;
-#pragma unroll 1
+#pragma unroll
   for (int k = 0; k < 4; ++k) {
     if (n0 + k * 32 >= a.n) break;
-    uint32_t r[32];
-    tmem_ld32(taddr + k * 32, r);
-    tmem_wait_ld();
     float v[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = ex2(fmaf(__uint_as_float(r[j]), kLog2e, -lse2));
+    for (int j = 0; j < 32; j += 2) {
+      const float2 e = share2(make_float2(logit[k * 32 + j], logit[k * 32 + j + 1]), make_float2(off, off));
+      v[j] = e.x;
+      v[j + 1] = e.y;
+    }
     if (__any_sync(0xffffffffu, label >= k * 32 && label < k * 32 + 32)) {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] -= label == k * 32 + j ? 1.f : 0.f;
@@ -553,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         if (lane == 0) arrive_cluster(lead_tempty + 8u * (acc & 1));
         ++acc;
       };
-      if constexpr (EPI == kStats) {
+      if constexpr (EPI == kStats || EPI == kGrad) {
         float v[128];
 #pragma unroll
         for (int j = 0; j < 128; ++j) v[j] = 0.f;
@@ -571,7 +573,11 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
           }
           release();
         }
-        if (ok) stats_tile(a, v, m0 + lane, n0 + half * 128, column);
+        if constexpr (EPI == kStats) {
+          if (ok) stats_tile(a, v, m0 + lane, n0 + half * 128, column);
+        } else {
+          if (ok) grad_tile(a, v, patch, m0, n0 + half * 128, min(32, a.m - m0), unit);
+        }
       } else if constexpr (EPI == kFew) {
         float v[kFewRows / 2];                            // every other 16 of the rows
 #pragma unroll
@@ -603,12 +609,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         const int rows = min(32, a.m - m0);
         const uint32_t taddr = trow + (acc & 1) * kTile + half * 128;
         n0 += half * 128;
-        if constexpr (EPI == kGrad) grad_tile(a, taddr, patch, m0, n0, rows, unit);
-        if constexpr (EPI == kStore) {
-          unit = a.unit ? *a.unit : 1.f;
-          if (a.out_fp32) store_tile<float>(a, taddr, patch, split, m0, n0, rows, unit);
-          else store_tile<__nv_bfloat16>(a, taddr, patch, split, m0, n0, rows, unit);
-        }
+        unit = a.unit ? *a.unit : 1.f;
+        if (a.out_fp32) store_tile<float>(a, taddr, patch, split, m0, n0, rows, unit);
+        else store_tile<__nv_bfloat16>(a, taddr, patch, split, m0, n0, rows, unit);
         release();
       }
     }

@@ -61,3 +61,30 @@ def test_loss_of_confident_rows(n, d, size, transposed):
     # at most (a thread's 32 and 3, the rows' parts), then the logarithm
     close(loss, want, torch.expm1(want) * (2 * off + 2.0 ** -20) + 128 * R.F32 * (1 + want), "loss")
     close(lse, want_lse, off + 2.0 ** -20 + 2 * R.F32 * want_lse.abs(), "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("n,d,size", [(512, 4096, 10.0), (512, 4096, 14.0), (130, 8200, 14.0), (200, 1000, 14.0)])
+def test_gradient_of_confident_rows(n, d, size, transposed):
+    """The gradient's logits are those that lse was made of, so that what is off in them changes 1 - p by its own share only:
+    the label's entry of G has no error of the size of a logit's, however long its sum."""
+    x, W, labels = confident(n, d, 2000, size, d)
+    W = W.t().contiguous().t() if transposed else W
+    _, lse = B.prm_head_loss(x, W, labels)
+    gl = torch.exp(randn(5, n)) / n
+    gx, gw = B.prm_head_loss_backward(gl, x, W, labels, lse)
+    xd, Wd, g1 = x.double(), W.double(), gl.double()[:, None]
+    logits = xd @ Wd
+    p = torch.softmax(logits, 1)
+    rows = torch.arange(n, device="cuda")
+    rest = p.sum(1) - p[rows, labels]                      # 1 - p of the label
+    g = p.clone()
+    g[rows, labels] = -rest
+    off = (d / 16 + 4) * 2.0 ** -23 * (xd.abs() @ Wd.abs()).amax(1, keepdim=True)
+    # an entry's rounding to bf16, the logits', and the exponential's and lse's own roundings, which p carries whole
+    dg = R.BF16 * g.abs() + g.abs() * 2 * off + p * (2.0 ** -21 + 2 * R.F32 * lse.double().abs()[:, None])
+    g, dg = g * g1, dg * g1
+    rx, rw = g @ Wd.t(), xd.t() @ g
+    close(gx, rx, 1.02 * dg @ Wd.t().abs() + 1.01 * R.BF16 * rx.abs() + 1e-30, "grad_x")
+    close(gw, rw, 1.02 * xd.t().abs() @ dg + 1.01 * R.BF16 * rw.abs() + 1e-30, "grad_w")
