@@ -1,0 +1,70 @@
+"""Layer norm and its gradient where rows are constant, far from zero or no numbers, in all layouts, against 64 bits."""
+
+import pytest
+import torch
+
+import train_reference as R
+from paper_2608_20818_b200 import binding as B
+
+# columns, and how the stream lies: aligned, starting anywhere, starting unlike its gradient (single elements), too wide for registers
+LAYOUTS = [(64, "aligned"), (200, "aligned"), (1024, "aligned"), (4096, "aligned"), (8192, "aligned"), (63, "shifted"), (1023, "shifted"),
+           (4099, "shifted"), (1024, "unlike"), (12000, "wide")]
+TYPES = [torch.bfloat16, torch.float32]
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+def close(got, want, room, what):
+    bad = (got.double() - want).abs() - room
+    assert torch.all(bad <= 0), (what, float(bad.max()))
+
+
+def unlike(t, how):
+    """The matrix in rows that start one element off, where that is what is asked for."""
+    if how != "unlike":
+        return t
+    wide = torch.empty(t.shape[0], t.shape[1] + 3, dtype=t.dtype, device=t.device)
+    wide[:, 1:-2] = t
+    return wide[:, 1:-2]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", TYPES)
+@pytest.mark.parametrize("cols,how", LAYOUTS)
+def test_gradient_of_constant_rows(cols, how, io):
+    """xhat is 0: they give the weight nothing, and grad_r is rstd (g - mean g)."""
+    rows, eps = 70, 1e-5
+    h = (301.0 + 7.0 * torch.arange(rows, device="cuda"))[:, None].expand(rows, cols).to(io).contiguous()
+    gy, w = randn(cols, rows, cols).to(io), 1 + 0.2 * randn(1, cols)
+    y, _, mean, rstd = B.prm_layernorm(h, w, None, eps)
+    assert torch.all(y == 0) and torch.equal(mean, h[:, 0].float())
+    gx, _, gw, gb = B.prm_layernorm_backward(unlike(gy, how), h, mean, rstd, w)
+    assert torch.all(gw == 0)
+    g = gy.double() * w.double()
+    want = rstd.double()[:, None] * (g - g.mean(1, keepdim=True))
+    size = rstd.double()[:, None] * (g.abs() + g.abs().mean(1, keepdim=True))
+    # a thread adds 64 numbers in a row at most, then 10 by shuffles; a handful of products
+    close(gx, want, 100 * R.F32 * size + 1.01 * R.store(io) * want.abs(), "grad_x")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", TYPES)
+@pytest.mark.parametrize("cols,how", LAYOUTS)
+def test_gradient_of_rows_far_from_zero(cols, how, io):
+    """Means of 10^4 deviations: what is off in xhat = (h - mean) rstd goes by xhat, not by the mean."""
+    rows = 70
+    h = (100.0 + 100.0 * torch.rand(rows, 1, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)) + 0.01 * randn(3, rows, cols)).to(io)
+    gy, w = randn(cols, rows, cols).to(io), 1 + 0.2 * randn(1, cols)
+    _, _, mean, rstd = B.prm_layernorm(h, w, None, 1e-6)
+    gx, _, gw, gb = B.prm_layernorm_backward(unlike(gy, how), h, mean, rstd, w)
+    r = rstd.double()[:, None]
+    xhat = (h.double() - mean.double()[:, None]) * r
+    g = gy.double() * w.double()
+    want = r * (g - g.mean(1, keepdim=True) - xhat * (g * xhat).mean(1, keepdim=True))
+    size = r * (g.abs() + g.abs().mean(1, keepdim=True) + xhat.abs() * (g * xhat).abs().mean(1, keepdim=True))
+    close(gx, want, 100 * R.F32 * size + 1.01 * R.store(io) * want.abs(), "grad_x")
+    rounds = 100 + rows
+    for got, terms in ((gw, gy.double() * xhat), (gb, gy.double())):
+        close(got, terms.sum(0), rounds * R.F32 * terms.abs().sum(0) + 1.01 * R.F32 * terms.sum(0).abs(), "grad_w, grad_b")
