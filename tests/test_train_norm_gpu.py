@@ -68,3 +68,27 @@ def test_gradient_of_rows_far_from_zero(cols, how, io):
     rounds = 100 + rows
     for got, terms in ((gw, gy.double() * xhat), (gb, gy.double())):
         close(got, terms.sum(0), rounds * R.F32 * terms.abs().sum(0) + 1.01 * R.F32 * terms.sum(0).abs(), "grad_w, grad_b")
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", TYPES)
+@pytest.mark.parametrize("rows,cols,how", [(40, c, h) for c, h in LAYOUTS] + [(9000, 1100, "aligned"), (5001, 2001, "shifted"), (3000, 4096, "aligned")])
+def test_forward_of_rows_far_from_zero(rows, cols, how, io):
+    """y goes by h - mean: the mean that the row was reduced with is off by its own rounding and that of the sums, which the second
+    reduction takes off again.  What is left is the rounding of the sum of h - (first mean), and a few steps of y."""
+    h = (100.0 + 100.0 * torch.rand(rows, 1, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)) + 0.01 * randn(3, rows, cols)).to(io)
+    w, b = 1 + 0.2 * randn(1, cols), randn(4, cols)
+    y, _, mean, rstd = B.prm_layernorm(unlike(h, how), w, b, 1e-6)
+    v = h.double()
+    m = v.mean(1, keepdim=True)
+    rs = 1 / torch.sqrt((v - m).square().mean(1, keepdim=True) + 1e-6)
+    # first mean: 80 sums of which each is off by half a step of the row's mean at most
+    first = 80 * R.F32 * m.abs()
+    off = 100 * R.F32 * ((v - m).abs().mean(1, keepdim=True) + first) + R.F32 * ((v - m).abs() + first)
+    # the variance is sums of squares of h - first, less the square of what is taken off
+    spread = 100 * R.F32 * ((v - m).square().mean(1, keepdim=True) + 2 * first.square()) * rs.square()
+    want = (v - m) * rs * w.double() + b.double()
+    size = ((v - m).abs() + off) * rs * w.double().abs()
+    room = off * rs * w.double().abs() + size * (spread + 8 * R.F32) + 2 * R.F32 * (size + b.double().abs())
+    close(y, want, room + 1.01 * R.store(io) * want.abs(), "y")
+    assert io != torch.float32 or float(room.max()) < 0.05          # the bound says something: y itself is about 1
+    close(rstd, rs[:, 0], (rs * (spread + 4 * R.F32))[:, 0], "rstd")
