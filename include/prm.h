@@ -548,7 +548,7 @@ PRM_API int prm_q8_status(void);
  *   every rows_per_group rows, ld_weight and ld_bias apart (rows_per_group >= rows: one row of each);
  *   add_one: the weight is 1 + what is stored (adaLN).  mean_out and rstd_out, fp32 vectors of rows, are what
  *   the gradient reads.  rows may be 0.  A constant row has y = bias; with eps = 0 it is NaN.  Deviations from
- *   about 1e19 on have infinite squares and rstd 0.
+ *   about 1e19 on have infinite squares and rstd 0.  A NaN leaves its row's mean and rstd NaN, an infinity rstd; such a row's y is NaN.
  * prm_layernorm_backward   with xhat = (h - mean) rstd and g = grad_y weight:
  *     grad_residual = rstd (g - mean(g) - xhat mean(g xhat)) + grad_h   (grad_h, what reaches h from elsewhere, may
  *                     be NULL); without dropout it is the gradient of x too and grad_x is ignored

@@ -34,11 +34,13 @@ namespace {
 // What the row's numbers are: mean and rstd, and what is still to be taken off h - (first mean).
 struct RowStats {
   float mean, rstd, rest;
-  // of the first mean, the sums of h - mean and of its squares
+  // of the first mean, the sums of h - mean and of its squares.  An infinity among the row's elements leaves the mean
+  // infinite and rstd NaN, a NaN both; infinite squares of finite elements leave rstd 0 (rest^2 may be as large).
   __device__ __forceinline__ RowStats(float first, float2 sums, float over, float eps) {
     rest = sums.x * over;
-    mean = first + rest;
-    rstd = rsqrtf(fmaxf(sums.y * over - rest * rest, 0.f) + eps);
+    mean = fabsf(first) < INFINITY ? first + rest : first;
+    const float square = sums.y * over, var = square < INFINITY ? square - rest * rest : square;
+    rstd = rsqrtf((var < 0.f ? 0.f : var) + eps);
   }
 };
 

@@ -92,3 +92,25 @@ def test_forward_of_rows_far_from_zero(rows, cols, how, io):
     close(y, want, room + 1.01 * R.store(io) * want.abs(), "y")
     assert io != torch.float32 or float(room.max()) < 0.05          # the bound says something: y itself is about 1
     close(rstd, rs[:, 0], (rs * (spread + 4 * R.F32))[:, 0], "rstd")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", TYPES)
+@pytest.mark.parametrize("rows,cols,how", [(70, c, h) for c, h in LAYOUTS] + [(9000, 1100, "aligned"), (5001, 2001, "shifted"), (3000, 4096, "aligned")])
+def test_statistics_of_rows_that_are_no_numbers(rows, cols, how, io):
+    """What the formulas give: a NaN leaves mean and rstd NaN, an infinity an infinite mean and rstd NaN; squares beyond fp32 leave
+    rstd 0 and y = bias.  No other row is touched."""
+    h, b = randn(cols, rows, cols).to(io), randn(4, cols)
+    y0, _, mean0, rstd0 = B.prm_layernorm(unlike(h, how), None, b)
+    h[3, cols // 2] = float("nan")
+    h[5, 0] = float("inf")
+    h[rows - 2, cols - 1] = float("-inf")
+    h[9] = torch.where(torch.arange(cols, device="cuda") % 2 == 0, 1e30, -1e30).to(io)
+    h[10] = 1e34
+    y, _, mean, rstd = B.prm_layernorm(unlike(h, how), None, b)
+    odd = [3, 5, rows - 2]
+    assert bool(torch.isnan(mean[3])) and float(mean[5]) == float("inf") and float(mean[rows - 2]) == float("-inf")
+    assert torch.all(torch.isnan(rstd[odd])) and torch.all(torch.isnan(y[odd]))
+    assert float(rstd[9]) == 0 and torch.equal(y[9], b.to(io)) and torch.equal(y[10], b.to(io))
+    rest = [i for i in range(rows) if i not in odd + [9, 10]]
+    assert torch.equal(y[rest], y0[rest]) and torch.equal(mean[rest], mean0[rest]) and torch.equal(rstd[rest], rstd0[rest])
