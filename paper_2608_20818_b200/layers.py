@@ -25,21 +25,65 @@ from .binding import (prm_dropout, prm_head_loss, prm_head_loss_backward, prm_la
 class Draws:
     """Where dropout takes its numbers from: a seed, and a counter on the device.  Every call of a step takes the next
     number; advance() ends the step, after its backward pass (which reads the counter again, and refuses to run if it has been
-    advanced since).  A forward pass that is run again (a checkpointed one) takes new numbers, so it draws other masks: set `calls`
-    back before it."""
+    advanced since).  Ranks that are to draw masks of their own need seeds of their own.
+
+    A part of the forward pass that is run again in the backward pass has to take the numbers that it took at first:
+
+        y = torch.utils.checkpoint.checkpoint(block, x, use_reentrant=False, context_fn=draws.checkpoint)
+
+    Without that a call inside a backward pass is refused: it would draw a mask that the loss has not seen."""
 
     def __init__(self, seed, device="cuda"):
         self.seed = int(seed)
         self.counter = torch.zeros(1, dtype=torch.int64, device=device)
         self.calls = 0
+        self._again = 0
 
     def take(self):
+        if not self._again and torch._C._current_graph_task_id() >= 0:
+            raise RuntimeError("a forward pass that is run again in a backward pass would draw other masks: "
+                               "give the checkpoint use_reentrant=False and context_fn=draws.checkpoint")
         self.calls += 1
         return self.calls - 1
 
     def advance(self):
         self.counter.add_(self.calls)
         self.calls = 0
+
+    def checkpoint(self):
+        """The two contexts of torch.utils.checkpoint's context_fn: the second one's calls take the first one's numbers."""
+        first = _First(self)
+        return first, _Again(first)
+
+
+class _First:
+    def __init__(self, draws):
+        self.draws = draws
+
+    def __enter__(self):
+        self.calls, self.version = self.draws.calls, self.draws.counter._version
+
+    def __exit__(self, *_):
+        return None
+
+
+class _Again:
+    def __init__(self, first):
+        self.first = first
+        self.kept = []
+
+    def __enter__(self):
+        draws = self.first.draws
+        if draws.counter._version != self.first.version:
+            raise RuntimeError("the counter has been advanced since the forward pass that is run again")
+        self.kept.append(draws.calls)
+        draws.calls = self.first.calls
+        draws._again += 1
+
+    def __exit__(self, *_):
+        draws = self.first.draws
+        draws.calls = self.kept.pop()
+        draws._again -= 1
 
 
 def _refuse_second_derivative():
