@@ -95,13 +95,19 @@ def _rows(t, cols):
     return None if t is None else t.reshape(-1, cols)
 
 
+def _result(t, shape):
+    """An operator's rows in the shape of what went in.  Not as a view: autograd forbids writing to a view that a function
+    of its own returns (a caller's relu_, say), and follows what is written to this."""
+    return t.reshape(shape).detach()
+
+
 class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed, offset, counter):
         ctx.save_for_backward(counter)
         ctx.draw = p, seed, offset
         cols = x.shape[-1]
-        return prm_dropout(_rows(x, cols), p, seed, offset, counter, _rows(residual, cols)).reshape(x.shape)
+        return _result(prm_dropout(_rows(x, cols), p, seed, offset, counter, _rows(residual, cols)), x.shape)
 
     @staticmethod
     def backward(ctx, grad):
@@ -125,8 +131,8 @@ class _LayerNorm(torch.autograd.Function):
         ctx.save_for_backward(x2 if h is None else h, mean, rstd, weight, counter)
         ctx.how = add_one, p, seed, offset
         ctx.shape = x.shape
-        y = y.reshape(x.shape)
-        return y if h is None else (y, h.reshape(x.shape))
+        y = _result(y, x.shape)
+        return y if h is None else (y, _result(h, x.shape))
 
     @staticmethod
     def backward(ctx, grad_y, grad_h=None):
