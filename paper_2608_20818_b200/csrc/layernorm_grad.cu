@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(256) layernorm_grad_sum_few_kernel(const Layer
 
 int launch_sum(const LayerNormGradArgs& a, int64_t groups, cudaStream_t stream) {
   if (!a.gw && !a.gb) return PRM_OK;
-  if (a.parts > 16) {
+  if (a.parts > kLinesPerThread) {
     const int chunks = (a.cols + 31) / 32;
     return q8_code(launch_after(layernorm_grad_sum_kernel, (unsigned)(groups * chunks * 2), 1024, 0, stream, 0, a, chunks));
   }
@@ -437,8 +437,7 @@ extern "C" int prm_layernorm_backward(const void* grad_y, int64_t ld_grad_y, con
   }
   rows_per_group = std::min(rows_per_group, rows);
   const int64_t groups = rows / rows_per_group;
-  if (groups * rows_per_group != rows || groups * ((cols + 31) / 32) > 0x3fffffffLL || groups * 1184 > 0x7fffffffLL)
-    return PRM_ERR_SHAPE;
+  if (groups * rows_per_group != rows || !layernorm_grids_ok(rows_per_group, groups, cols)) return PRM_ERR_SHAPE;
   if (!grad_y || !h || !mean || !rstd || !grad_residual || (drop.threshold && !grad_x) || !scratch) return PRM_ERR_ARG;
   if (scratch_bytes < prm_layernorm_scratch_bytes(rows, cols, rows_per_group)) return PRM_ERR_WORKSPACE;
   const uintptr_t stream_bits = (uintptr_t)grad_y | (uintptr_t)h | (uintptr_t)grad_h | (uintptr_t)grad_residual |

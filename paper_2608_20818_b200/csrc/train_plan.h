@@ -37,6 +37,15 @@ inline int64_t layernorm_parts(int64_t rows_per_group, int64_t groups, int64_t c
   return std::min(parts, turns);
 }
 
+// Lines of a group that one thread per column adds; more are added by a block per 32 columns.
+constexpr int kLinesPerThread = 16;
+// Whether the gradient's grids, of its blocks and of those that add their lines, fit a launch: with up to 2^30 - 1 groups, unless
+// rows are very wide as well.
+inline bool layernorm_grids_ok(int64_t rows_per_group, int64_t groups, int64_t cols) {
+  const int64_t parts = layernorm_parts_bound(rows_per_group, groups, cols), width = parts > kLinesPerThread ? 32 : 256;
+  return groups * parts <= 0x7fffffffLL && groups * ((cols + width - 1) / width) * 2 <= 0x7fffffffLL;
+}
+
 constexpr int kHeadTile = 256;                   // edge of the head's tiles
 constexpr int kHeadStage = 128;                  // k that a stage of a tile's main loop holds
 

@@ -114,3 +114,18 @@ def test_statistics_of_rows_that_are_no_numbers(rows, cols, how, io):
     assert float(rstd[9]) == 0 and torch.equal(y[9], b.to(io)) and torch.equal(y[10], b.to(io))
     rest = [i for i in range(rows) if i not in odd + [9, 10]]
     assert torch.equal(y[rest], y0[rest]) and torch.equal(mean[rest], mean0[rest]) and torch.equal(rstd[rest], rstd0[rest])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,per,cols", [(4000000, 1, 8), (4000000, 2, 9), (2000001, 1, 40)])
+def test_gradient_of_millions_of_groups(rows, per, cols):
+    """A weight for each row or two: what the forward pass takes, its gradient takes too."""
+    groups = rows // per
+    h, gy = randn(1, rows, cols), randn(2, rows, cols)
+    w = 1 + 0.2 * randn(3, groups, cols)
+    y, _, mean, rstd = B.prm_layernorm(h, w, w)
+    gx, _, gw, gb = B.prm_layernorm_backward(gy, h, mean, rstd, w)
+    rx, rw, rb, sx, sw, sb = R.norm_backward(gy, h, mean, rstd, w)
+    close(gx, rx, 100 * R.F32 * sx + 1.01 * R.F32 * rx.abs(), "grad_x")
+    close(gw, rw, 100 * R.F32 * sw + 1.01 * R.F32 * rw.abs(), "grad_w")
+    close(gb, rb, 100 * R.F32 * sb + 1.01 * R.F32 * rb.abs(), "grad_b")
