@@ -353,13 +353,6 @@ int launch_sum(const LayerNormGradArgs& a, int64_t groups, cudaStream_t stream) 
   return q8_code(launch_after(layernorm_grad_sum_few_kernel, (unsigned)(groups * chunks * 2), 256, 0, stream, 0, a, chunks));
 }
 
-template <typename IO, bool DROP, bool SHIFT, int NV, int TPR, int BLOCK>
-int launch_layernorm_grad(LayerNormGradArgs a, int64_t groups, cudaStream_t stream) {
-  a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, BLOCK / TPR, 148 * layernorm_grad_blocks<IO>(NV, BLOCK), SHIFT);
-  const int code = q8_code(launch_after(layernorm_grad_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT>, (unsigned)(groups * a.parts),
-                                        BLOCK, 0, stream, 0, a));
-  return code == PRM_OK && a.parts > 1 ? launch_sum(a, groups, stream) : code;
-}
 template <typename IO>
 int launch_layernorm_grad_single(LayerNormGradArgs a, int64_t groups, cudaStream_t stream) {
   a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, 1, 444, false);
@@ -369,6 +362,18 @@ int launch_layernorm_grad_single(LayerNormGradArgs a, int64_t groups, cudaStream
                        : q8_code(launch_after(layernorm_grad_single_kernel<IO, 1024>, (unsigned)(groups * a.parts), 1024, 0,
                                               stream, 0, a));
   return code == PRM_OK ? launch_sum(a, groups, stream) : code;
+}
+template <typename IO, bool DROP, bool SHIFT, int NV, int TPR, int BLOCK>
+int launch_layernorm_grad(LayerNormGradArgs a, int64_t groups, cudaStream_t stream) {
+  const int blocks = 148 * layernorm_grad_blocks<IO>(NV, BLOCK);
+  a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, BLOCK / TPR, blocks, SHIFT);
+  if (SHIFT && a.parts > layernorm_lines(a.rows_per_group, groups, a.cols)) {
+    if (a.ld_h % 8 != 0) return launch_layernorm_grad_single<IO>(a, groups, stream);
+    a.parts = (int)layernorm_parts(a.rows_per_group, groups, a.cols, BLOCK / TPR, blocks, false);       // all rows start alike
+  }
+  const int code = q8_code(launch_after(layernorm_grad_kernel<IO, NV, TPR, BLOCK, DROP, SHIFT>, (unsigned)(groups * a.parts),
+                                        BLOCK, 0, stream, 0, a));
+  return code == PRM_OK && a.parts > 1 ? launch_sum(a, groups, stream) : code;
 }
 
 template <typename IO, bool DROP, bool SHIFT>
@@ -410,7 +415,7 @@ extern "C" size_t prm_layernorm_scratch_bytes(int64_t rows, int64_t cols, int64_
   if (rows < 1 || cols < 1 || rows_per_group < 1) return 0;
   rows_per_group = std::min(rows_per_group, rows);
   const int64_t groups = rows / rows_per_group;
-  return (size_t)(groups * layernorm_parts_bound(rows_per_group, groups, cols)) * 2 * (size_t)cols * 4;
+  return (size_t)(groups * layernorm_lines(rows_per_group, groups, cols)) * 2 * (size_t)cols * 4;
 }
 
 extern "C" int prm_layernorm_backward(const void* grad_y, int64_t ld_grad_y, const void* h, int64_t ld_h, const float* mean,

@@ -37,6 +37,13 @@ inline int64_t layernorm_parts(int64_t rows_per_group, int64_t groups, int64_t c
   return std::min(parts, turns);
 }
 
+// The lines of a group that the scratch holds: with whole octs only what resident blocks leave (1024 groups of 8 rows x 8192: 64
+// MB, with 8 lines 512 MB).  Such rows that all the same start unlike one another, and would need more, go to the kernel of single
+// elements, for which any number will do.
+inline int64_t layernorm_lines(int64_t rows_per_group, int64_t groups, int64_t cols) {
+  if (cols % 8 != 0) return layernorm_parts_bound(rows_per_group, groups, cols);
+  return std::min(rows_per_group, std::max<int64_t>(1, layernorm_parts_most(cols) / groups));
+}
 // Lines of a group that one thread per column adds; more are added by a block per 32 columns.
 constexpr int kLinesPerThread = 16;
 // Whether the gradient's grids, of its blocks and of those that add their lines, fit a launch: with up to 2^30 - 1 groups, unless

@@ -129,3 +129,34 @@ def test_gradient_of_millions_of_groups(rows, per, cols):
     close(gx, rx, 100 * R.F32 * sx + 1.01 * R.F32 * rx.abs(), "grad_x")
     close(gw, rw, 100 * R.F32 * sw + 1.01 * R.F32 * rw.abs(), "grad_w")
     close(gb, rb, 100 * R.F32 * sb + 1.01 * R.F32 * rb.abs(), "grad_b")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", TYPES)
+@pytest.mark.parametrize("groups,per,cols", [(300, 20, 1024), (1024, 8, 512), (200, 9, 200), (149, 33, 2048)])
+@pytest.mark.parametrize("start,ld", [(0, 0), (8, 8), (3, 8), (1, 3)])
+def test_gradient_of_many_groups_in_any_rows(groups, per, cols, start, ld, io):
+    """Whole octs, aligned or not, in rows that start alike (a stride of octs) or do not: no more scratch than there is is written."""
+    rows = groups * per
+
+    def place(t=None):
+        wide = torch.full((rows, cols + ld + 8), float("nan"), dtype=io, device="cuda")[:, :cols + ld]
+        wide = wide.as_strided((rows, cols), (cols + ld, 1), start)
+        return wide if t is None else wide.copy_(t)
+
+    h, gy = place(randn(1, rows, cols)), place(randn(2, rows, cols))
+    w = 1 + 0.2 * randn(3, groups, cols)
+    _, _, mean, rstd = B.prm_layernorm(h, w)
+    gr, gw, gb = place(), torch.empty_like(w), torch.empty_like(w)
+    nbytes = B.lib().prm_layernorm_scratch_bytes(rows, cols, per)
+    scratch = torch.full((nbytes + 4096,), 77, dtype=torch.uint8, device="cuda")
+    code = B.lib().prm_layernorm_backward(gy.data_ptr(), cols + ld, h.data_ptr(), cols + ld, mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
+                                          cols, None, 0, rows, cols, per, int(io == torch.float32), 1, 0, 0.0, 0, 0, None, gr.data_ptr(),
+                                          cols + ld, None, 0, gw.data_ptr(), gb.data_ptr(), scratch.data_ptr(), nbytes,
+                                          torch.cuda.current_stream().cuda_stream)
+    assert code == B.PRM_OK
+    rx, rw, rb, sx, sw, sb = R.norm_backward(gy, h, mean, rstd, w)
+    close(gr, rx, 100 * R.F32 * sx + 1.01 * R.store(io) * rx.abs(), "grad_r")
+    close(gw, rw, (100 + per) * R.F32 * sw + 1.01 * R.F32 * rw.abs(), "grad_w")
+    close(gb, rb, (100 + per) * R.F32 * sb + 1.01 * R.F32 * rb.abs(), "grad_b")
+    assert torch.all(scratch[nbytes:] == 77)

@@ -1,10 +1,15 @@
 """What the gradients of layer norm and the head's loss accept, and the scratch that they ask for, decided before anything touches the
 device."""
 
+import ctypes
+import os
+import subprocess
+
 import pytest
 
 from paper_2608_20818_b200 import binding as B
 
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2608_20818_b200", "csrc")
 P = 1 << 20                     # an address that is never read
 
 
@@ -22,3 +27,44 @@ def layernorm_backward(rows, cols, per, nbytes, **change):
 def test_layernorm_gradient_takes_as_many_groups_as_a_launch_has_blocks(rows, cols, per, code):
     """No scratch is given, so that what is accepted ends there."""
     assert layernorm_backward(rows, cols, per, 0) == code
+
+
+LINES = """
+#include "train_plan.h"
+using namespace prm;
+// Sizes for which a launch would leave more lines than the scratch holds.
+extern "C" long beyond(const long* rows, int n_rows, const long* groups, int n_groups, long most) {
+  long bad = 0;
+  for (long cols = 1; cols <= most; cols += cols < 100 ? 1 : 4)
+    for (int i = 0; i < n_rows; ++i)
+      for (int g = 0; g < n_groups; ++g)
+        for (int turn : {1, 2, 4, 8, 16, 32})
+          for (int blocks : {148, 296, 444, 592, 888, 1184})
+            for (bool shift : {false, true}) {
+              const long lines = layernorm_lines(rows[i], groups[g], cols);
+              const long parts = layernorm_parts(rows[i], groups[g], cols, turn, blocks, shift);
+              // rows that start anywhere and have whole octs: the launch goes by what there is
+              bad += lines < 1 || (parts > lines && !(shift && cols % 8 == 0));
+            }
+  return bad;
+}
+"""
+
+
+def test_layernorm_scratch_holds_what_a_launch_leaves(tmp_path):
+    (tmp_path / "lines.cpp").write_text(LINES)
+    so = str(tmp_path / "lines.so")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-shared", "-fPIC", "-I", CSRC, str(tmp_path / "lines.cpp"), "-o", so], check=True)
+    lib = ctypes.CDLL(so)
+    lib.beyond.restype = ctypes.c_long
+    lib.beyond.argtypes = [ctypes.POINTER(ctypes.c_long), ctypes.c_int, ctypes.POINTER(ctypes.c_long), ctypes.c_int, ctypes.c_long]
+    rows = [1, 2, 3, 7, 8, 9, 31, 100, 148, 1000, 8191, 2 ** 31 - 1]
+    groups = [1, 2, 3, 17, 37, 64, 147, 148, 149, 592, 1184, 1185, 100000]
+    assert lib.beyond((ctypes.c_long * len(rows))(*rows), len(rows), (ctypes.c_long * len(groups))(*groups), len(groups), 20000) == 0
+
+
+@pytest.mark.parametrize("groups,per,cols", [(1024, 8, 8192), (4096, 16, 4096), (64, 256, 2048), (1, 8192, 4096), (300, 200, 64)])
+def test_layernorm_scratch_is_in_proportion(groups, per, cols):
+    """No more than two fp32 lines for each block that a device holds, or for each group."""
+    nbytes = B.lib().prm_layernorm_scratch_bytes(groups * per, cols, per)
+    assert nbytes <= max(groups, 1184) * 2 * cols * 4
