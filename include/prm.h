@@ -569,7 +569,7 @@ PRM_API int prm_q8_status(void);
  *   G is rounded to bf16 (after division by the largest |grad_loss|) for the products, whose sums are fp32.  A row
  *   without a label, or whose grad_loss is 0, has no part in grad_weight and the grad_x 0, whatever it holds.
  *   scratch: device, 256-byte aligned, prm_head_loss_backward_scratch_bytes(n, d, vocab) bytes (G for a piece of the
- *   vocabulary, up to 512 MB, partial sums, the rows of x that have a part), and more for copies as above.  With n = 0 grad_weight is set to zero.
+ *   vocabulary, up to 512 MB, partial sums, the rows of x that have a part), prm_head_loss_copy_bytes(n, d) less without grad_weight, and more for copies as above.  With n = 0 grad_weight is set to zero.
  * prm_q8_status covers the waits inside the head's products too.
  */
 PRM_API int prm_dropout(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int64_t rows,

@@ -952,6 +952,8 @@ def prm_head_loss_backward(grad_loss, x, weight, labels, lse, need_x=True, need_
         gw_ptr = gw.data_ptr()
     L = _lib_handle or lib()
     nbytes = L.prm_head_loss_backward_scratch_bytes(n, d, vocab) + copies
+    if not need_weight:
+        nbytes -= L.prm_head_loss_copy_bytes(n, d)
     scratch = torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=x.device)
     args = (grad_loss.data_ptr(), x.data_ptr(), ld_x, weight.data_ptr(), ld_w, w_t, labels.data_ptr(), lse.data_ptr(), n, d,
             vocab, gx_ptr, d, gw_ptr, d if w_t else vocab, scratch.data_ptr(), nbytes, _raw_stream(index))

@@ -931,7 +931,8 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
   if (code != PRM_OK) return code;
   if (((uintptr_t)grad_loss | (uintptr_t)lse) % 4 != 0 || (uintptr_t)labels % 8 != 0 || ((uintptr_t)scratch & 255) != 0)
     return PRM_ERR_ALIGN;
-  const size_t base = prm_head_loss_backward_scratch_bytes(n, d, vocab);
+  // x is copied for grad_weight only
+  const size_t kept = grad_weight ? copy_bytes(n, d) : 0, base = prm_head_loss_backward_scratch_bytes(n, d, vocab) - copy_bytes(n, d) + kept;
   if (scratch_bytes < base + (operand_aligned(x, ld_x) ? 0 : copy_bytes(n, d)) +
                           (operand_aligned(weight, ld_weight) ? 0 : copy_bytes(w_rows, w_cols)))
     return PRM_ERR_WORKSPACE;
@@ -942,7 +943,7 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
   float* unit = (float*)scratch;
   __nv_bfloat16* g = (__nv_bfloat16*)((char*)scratch + 256);
   float* part = (float*)((char*)g + plan.g_bytes);
-  __nv_bfloat16* clean = (__nv_bfloat16*)((char*)scratch + base - copy_bytes(n, d));
+  __nv_bfloat16* clean = (__nv_bfloat16*)((char*)scratch + base - kept);
   const int64_t ld_clean = ceil_to(d, 8);
   const Operand w = {weight, w_rows, w_cols, ld_weight, !weight_transposed};
   if (code == PRM_OK && n > kUnitRows) code = q8_code(launch_after(head_unit_kernel, 1u, 1024, 0, stream, 0, grad_loss, labels, vocab, (int)n, unit));

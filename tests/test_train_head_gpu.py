@@ -88,3 +88,23 @@ def test_gradient_of_confident_rows(n, d, size, transposed):
     rx, rw = g @ Wd.t(), xd.t() @ g
     close(gx, rx, 1.02 * dg @ Wd.t().abs() + 1.01 * R.BF16 * rx.abs() + 1e-30, "grad_x")
     close(gw, rw, 1.02 * xd.t().abs() @ dg + 1.01 * R.BF16 * rw.abs() + 1e-30, "grad_w")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,d,vocab", [(20, 64, 700), (300, 100, 1003), (2100, 77, 513)])
+def test_gradient_of_x_alone_keeps_to_its_scratch(n, d, vocab):
+    """The least scratch, with what lies behind it untouched; the same bits as with the weight's gradient."""
+    L = B.lib()
+    x, W = randn(1, n, d).to(torch.bfloat16), randn(2, vocab, d).to(torch.bfloat16)
+    labels, gl = torch.arange(n, device="cuda") % vocab, torch.exp(randn(3, n))
+    _, lse = B.prm_head_loss(x, W.t(), labels)
+    want, _ = B.prm_head_loss_backward(gl, x, W.t(), labels, lse)
+    nbytes = L.prm_head_loss_backward_scratch_bytes(n, d, vocab) - L.prm_head_loss_copy_bytes(n, d)
+    if d % 8:
+        nbytes += L.prm_head_loss_copy_bytes(n, d) + L.prm_head_loss_copy_bytes(vocab, d)
+    scratch = torch.full((nbytes + 4096,), 77, dtype=torch.uint8, device="cuda")
+    gx = torch.empty_like(x)
+    code = L.prm_head_loss_backward(gl.data_ptr(), x.data_ptr(), d, W.data_ptr(), d, 1, labels.data_ptr(), lse.data_ptr(), n, d, vocab,
+                                    gx.data_ptr(), d, None, d, scratch.data_ptr(), nbytes, torch.cuda.current_stream().cuda_stream)
+    assert code == B.PRM_OK and torch.equal(gx, want) and torch.all(scratch[nbytes:] == 77)
+    assert torch.equal(B.prm_head_loss_backward(gl, x, W.t(), labels, lse, need_weight=False)[0], want)

@@ -68,3 +68,18 @@ def test_layernorm_scratch_is_in_proportion(groups, per, cols):
     """No more than two fp32 lines for each block that a device holds, or for each group."""
     nbytes = B.lib().prm_layernorm_scratch_bytes(groups * per, cols, per)
     assert nbytes <= max(groups, 1184) * 2 * cols * 4
+
+
+@pytest.mark.parametrize("n,d,vocab", [(4, 64, 128), (1000, 4096, 32768), (300, 100, 700)])
+@pytest.mark.parametrize("ldx", [0, 1])
+def test_head_gradient_without_the_weight_s_needs_no_copy_of_x(n, d, vocab, ldx):
+    """One byte less than what the rest needs is refused; rows off 16 bytes are copied all the same."""
+    L = B.lib()
+    all_of, copy = L.prm_head_loss_backward_scratch_bytes(n, d, vocab), L.prm_head_loss_copy_bytes(n, d)
+    assert 0 < copy < all_of
+    need = all_of - copy + (copy if (d + ldx) % 8 else 0)
+
+    def call(nbytes, gw=None, scratch=P):
+        return L.prm_head_loss_backward(P, P, d + ldx, P, vocab + (-vocab) % 8, 0, P, P, n, d, vocab, P, d, gw, vocab, scratch, nbytes, None)
+
+    assert call(need - 1) == B.PRM_ERR_WORKSPACE and call(need, gw=P) == B.PRM_ERR_WORKSPACE
