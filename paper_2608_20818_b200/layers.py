@@ -92,7 +92,7 @@ def _refuse_second_derivative():
 
 
 def _rows(t, cols):
-    return None if t is None else t.reshape(-1, cols)
+    return None if t is None else t.reshape(t.shape[:-1].numel(), cols)        # cols may be 0
 
 
 def _result(t, shape):

@@ -40,3 +40,17 @@ def test_results_may_be_written_to(f, shape):
     h.add_(1)
     with pytest.raises(RuntimeError, match="inplace"):
         y.sum().backward()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(5, 0), (2, 0, 72), (0,), (0, 72)])
+def test_nothing_is_dropped_out_of_nothing(shape):
+    x = randn(1, *shape).requires_grad_()
+    for residual in (None, x):
+        out = L.dropout(x, 0.5, L.Draws(1), residual=residual)
+        grad, = torch.autograd.grad(out.sum(), [x])
+        assert out.shape == grad.shape == x.shape
+    if shape[-1]:
+        y, h = L.layer_norm(x, torch.ones(shape[-1], device="cuda"), residual=x, p=0.5, draws=L.Draws(1))
+        grad, = torch.autograd.grad((y + h).sum(), [x])
+        assert y.shape == h.shape == grad.shape == x.shape
