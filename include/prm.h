@@ -558,7 +558,7 @@ PRM_API int prm_q8_status(void);
  *   rows must be a multiple of rows_per_group (or at most that: one group).  scratch: device, 16-byte aligned,
  *   prm_layernorm_scratch_bytes(rows, cols, rows_per_group) bytes.  With rows = 0 the sums of one group are set to 0.
  * prm_head_loss   softmax cross entropy of the logits x W (n x d by d x vocab), which are not kept:
- *     lse = log sum_v exp(logit_v),  loss = lse - logit_label, 0 for a row whose label is not in 0..vocab-1
+ *     lse = log sum_v exp(logit_v),  loss = lse - logit_label (never below 0), 0 for a row whose label is not in 0..vocab-1
  *   x and weight bf16; weight_transposed = 0: stored d x vocab, 1: vocab x d (an embedding).  One that is not 16-byte
  *   aligned with a row stride that is a multiple of 8 is copied first.  loss_out, lse_out: fp32 vectors of n.
  *   A row with a logit that is NaN or +infinity gets a NaN (-infinity counts as nothing).  n may be 0; n, d and vocab 2^27 at most.  scratch: device, 16-byte aligned,
@@ -566,10 +566,11 @@ PRM_API int prm_q8_status(void);
  *   prm_head_loss_copy_bytes(rows, columns as stored) more.
  * prm_head_loss_backward   from grad_loss (fp32, n): with G = grad_loss (softmax - [label]), 0 for rows without a label,
  *     grad_x = G W^T (bf16, n x d),  grad_weight = x^T G (bf16, stored like weight); either may be NULL
- *   G is rounded to bf16 (after division by the largest |grad_loss|) for the products, whose sums are fp32.  A row
+ *   G is rounded to bf16 (after division by the largest |grad_loss|) for the products, whose sums are fp32 (of up to
+ *   32768 terms cut off, not rounded, every 16 of them; of more, of parts of 8192).  A row
  *   without a label, or whose grad_loss is 0, has no part in grad_weight and the grad_x 0, whatever it holds.
  *   scratch: device, 256-byte aligned, prm_head_loss_backward_scratch_bytes(n, d, vocab) bytes (G for a piece of the
- *   vocabulary, up to 512 MB, partial sums, the rows of x that have a part), prm_head_loss_copy_bytes(n, d) less without grad_weight, and more for copies as above.  With n = 0 grad_weight is set to zero.
+ *   vocabulary, up to 512 MB or 2048 columns, partial sums, the rows of x that have a part), prm_head_loss_copy_bytes(n, d) less without grad_weight, and more for copies as above.  With n = 0 grad_weight is set to zero.
  * prm_q8_status covers the waits inside the head's products too.
  */
 PRM_API int prm_dropout(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int64_t rows,

@@ -40,16 +40,26 @@ constexpr uint32_t kPatchBytes = 32 * 64;        // a warp's 32 rows of 64 bytes
 constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kPatchBytes;
 constexpr int kMaxStages = 6;
 constexpr int kFewRows = 64;                     // rows that kFew takes (100 x 4096 x 32768: 72 us, the other form 68)
-// The logits' sums are taken out of tensor memory every 1024 k and added in registers: the accumulator cuts off what
-// falls below its last bit at each of its steps (16 k), which over 4096 k puts a logit of the size 1 off by 1e-5.  Both directions
-// do so, so that the gradient's logits are those that lse was made of (8192 x 4096 x 65536: 10.5 ms, 10.4 without).
-constexpr int kChunk = 8;                        // stages
+// Long sums are taken out of tensor memory every so often and added in registers: the accumulator cuts off what falls below its
+// last bit at each of its steps (16 k).  The logits' every 1024 k, in both directions, so that the gradient's are those that
+// lse was made of: over 4096 k a logit of the size 1 would be off by 1e-5 (gradient of 100 x 4096 x 32768: 237 us, 228 without).  Those of the
+// products of G, which are rounded to bf16 in the end, every 8192 k where there are more than 32768 (up to there what is cut
+// off is 2e-4 of a sum of one sign, a twentieth of its rounding; over 2^20 rows grad_W would be 6e-3 short).
+constexpr int kLogitChunk = 8, kStoreChunk = 64; // stages
+constexpr int kStoreLongest = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // kStats: x (rows) times W (columns).  kFew: the same for few rows, the other way round (the rows are the instruction's N, so
 // that it costs them no more than it has to, and W's bytes have most of shared memory).
-enum Epi { kStats, kFew, kGrad, kStore };
-__host__ __device__ constexpr bool chunked(int epi) { return epi != kStore; }
+// kGradLong, kStoreLong: tiles of several chunks (in one kernel with the others their registers cost 8192 x 64 x 32768 551 us
+// instead of 472).
+enum Epi { kStats, kFew, kGrad, kGradLong, kStore, kStoreLong };
+__host__ __device__ constexpr bool is_grad(int epi) { return epi == kGrad || epi == kGradLong; }
+__host__ __device__ constexpr bool is_store(int epi) { return epi == kStore || epi == kStoreLong; }
+// Stages of a chunk: all of a tile's, where it is one.
+__host__ __device__ constexpr int chunk_of(int epi) {
+  return epi == kGrad || epi == kStore ? 1 << 30 : epi == kStoreLong ? kStoreChunk : kLogitChunk;
+}
 
 struct HeadArgs {
   int m, n, kblocks;               // of this product: rows, columns, ceil(k / 64)
@@ -91,7 +101,7 @@ struct HeadLaunch {
 
 template <int EPI>
 __device__ __forceinline__ bool next_tile(const HeadLaunch& l, int pair, int pairs, int i, int& which, int& tile) {
-  if constexpr (EPI == kStore) return pair_tile(l.a[0].tiles, l.a[1].tiles, l.extra, pair, pairs, i, which, tile);
+  if constexpr (is_store(EPI)) return pair_tile(l.a[0].tiles, l.a[1].tiles, l.extra, pair, pairs, i, which, tile);
   which = 0;
   tile = pair + i * pairs;
   return tile < l.a[0].tiles;
@@ -236,8 +246,8 @@ __device__ __forceinline__ void copy_live_rows(const HeadArgs& a, int first, int
   }
 }
 
-// 128 columns of the lane's row of G, of their logits.
-__device__ __forceinline__ void grad_tile(const HeadArgs& a, const float (&logit)[128], uint8_t* patch, int m0, int n0, int rows,
+// 128 columns of the lane's row of G.
+__device__ __forceinline__ void grad_tile(const HeadArgs& a, uint32_t taddr, uint8_t* patch, int m0, int n0, int rows,
                                           float unit) {
   const int lane = threadIdx.x & 31, row = m0 + lane;
   float factor = 0.f, off = 0.f;
@@ -252,13 +262,16 @@ __device__ __forceinline__ void grad_tile(const HeadArgs& a, const float (&logit
   }
   const bool all = __all_sync(0xffffffffu, factor != 0.f);
   __nv_bfloat16* out = a.g + (int64_t)m0 * a.ld_g + n0;
-#pragma unroll
+#pragma unroll 1
   for (int k = 0; k < 4; ++k) {
     if (n0 + k * 32 >= a.n) break;
+    uint32_t r[32];
+    tmem_ld32(taddr + k * 32, r);
+    tmem_wait_ld();
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; j += 2) {
-      const float2 e = share2(make_float2(logit[k * 32 + j], logit[k * 32 + j + 1]), make_float2(off, off));
+      const float2 e = share2(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), make_float2(off, off));
       v[j] = e.x;
       v[j + 1] = e.y;
     }
@@ -367,6 +380,28 @@ __device__ __forceinline__ void store_tile(const HeadArgs& a, uint32_t taddr, ui
   }
 }
 
+// A thread's 128 sums in tensor memory: added to v, and set.
+__device__ __forceinline__ void add_sums(uint32_t taddr, float (&v)[128]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t r[32];
+    tmem_ld32(taddr + k * 32, r);
+    tmem_wait_ld();
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[k * 32 + j] += __uint_as_float(r[j]);
+  }
+}
+__device__ __forceinline__ void put_sums(uint32_t taddr, const float (&v)[128]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t r[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(v[k * 32 + j]);
+    tmem_st32(taddr + k * 32, r);
+  }
+  tmem_wait_st();
+}
+
 // P_MN, Q_MN: as HeadArgs has them (kStore goes by those).
 template <int EPI, bool P_MN, bool Q_MN>
 __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant__ HeadLaunch l) {
@@ -417,10 +452,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
       bool ok = true;
       const uint32_t lead_full = cluster_map(smem_u32(&full[0]), 0);
       for (int i = 0, which, t; ok && next_tile<EPI>(l, pair, pairs, i, which, t); ++i) {
-        const HeadArgs& a = l.a[EPI == kStore ? which : 0];
-        const CUtensorMap* map_p = &l.p[EPI == kStore ? which : 0];
-        const CUtensorMap* map_q = &l.q[EPI == kStore ? which : 0];
-        const bool p_mn = EPI == kStore ? a.p_mn != 0 : P_MN, q_mn = EPI == kStore ? a.q_mn != 0 : Q_MN;
+        const HeadArgs& a = l.a[is_store(EPI) ? which : 0];
+        const CUtensorMap* map_p = &l.p[is_store(EPI) ? which : 0];
+        const CUtensorMap* map_q = &l.q[is_store(EPI) ? which : 0];
+        const bool p_mn = is_store(EPI) ? a.p_mn != 0 : P_MN, q_mn = is_store(EPI) ? a.q_mn != 0 : Q_MN;
         int split, m0, n0, s0, s1;
         tile_origin(a, t, split, m0, n0);
         split_range(a, split, s0, s1);
@@ -470,16 +505,16 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
       bool ok = true;
       const uint32_t smem0 = smem_u32(smem);
       for (int i = 0, which, t; ok && next_tile<EPI>(l, pair, pairs, i, which, t); ++i) {
-        const HeadArgs& a = l.a[EPI == kStore ? which : 0];
-        const bool p_mn = EPI == kStore ? a.p_mn != 0 : P_MN, q_mn = EPI == kStore ? a.q_mn != 0 : Q_MN;
+        const HeadArgs& a = l.a[is_store(EPI) ? which : 0];
+        const bool p_mn = is_store(EPI) ? a.p_mn != 0 : P_MN, q_mn = is_store(EPI) ? a.q_mn != 0 : Q_MN;
         const uint32_t idesc = idesc_bf16(kTile, EPI == kFew ? a.q_tile : kTile, p_mn, q_mn);
         const uint32_t step_p = p_mn ? 128 : 2, step_q = q_mn ? 128 : 2;      // 16 k, in units of 16 bytes
         const int kblocks = a.kblocks;
         int split, m0, n0, s0, s1;
         tile_origin(a, t, split, m0, n0);
         split_range(a, split, s0, s1);
-        for (int c0 = s0; c0 < s1 && ok; c0 += kChunk, ++acc) {
-          const int c1 = chunked(EPI) ? min(c0 + kChunk, s1) : s1;
+        for (int c0 = s0, c1; c0 < s1 && ok; c0 = c1, ++acc) {
+          c1 = c0 + min(chunk_of(EPI), s1 - c0);
           const uint32_t ab = acc & 1;
           if (!mbar_wait(&tempty[ab], ((acc >> 1) & 1) ^ 1, abort_flag, status)) { ok = false; break; }
           tcgen05_after_sync();
@@ -503,10 +538,6 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
             umma_commit_both(smem_u32(&empty[s]));
           }
           if (ok) umma_commit_both(smem_u32(&tfull[ab]));
-          if (!chunked(EPI)) {
-            ++acc;
-            break;
-          }
         }
       }
     }
@@ -516,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
     const uint32_t lead_tempty = cluster_map(smem_u32(&tempty[0]), 0);
     uint8_t* patch = smem + (size_t)stages * stage_bytes + (warp - 2) * kPatchBytes;
     float unit = 1.f;
-    if constexpr (EPI == kGrad) {
+    if constexpr (is_grad(EPI)) {
       const HeadArgs& a = l.a[0];
       if (a.unit) unit = *a.unit;
       if (a.unit_out) {
@@ -537,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
     uint32_t acc = 0;
     bool ok = true;
     for (int i = 0, which, t; ok && next_tile<EPI>(l, pair, pairs, i, which, t); ++i) {
-      const HeadArgs& a = l.a[EPI == kStore ? which : 0];
+      const HeadArgs& a = l.a[is_store(EPI) ? which : 0];
       int split, m0, n0, s0, s1;
       tile_origin(a, t, split, m0, n0);
       const int column = (n0 / kTile) * 2 + half;
@@ -555,13 +586,13 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         if (lane == 0) arrive_cluster(lead_tempty + 8u * (acc & 1));
         ++acc;
       };
-      if constexpr (EPI == kStats || EPI == kGrad) {
+      if constexpr (EPI == kStats) {
         float v[128];
 #pragma unroll
         for (int j = 0; j < 128; ++j) v[j] = 0.f;
         split_range(a, split, s0, s1);
 #pragma unroll 1
-        for (int c = s0; c < s1; c += kChunk) {
+        for (int c = s0; c < s1; c += chunk_of(EPI)) {
           if (!wait()) break;
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
@@ -573,18 +604,14 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
           }
           release();
         }
-        if constexpr (EPI == kStats) {
-          if (ok) stats_tile(a, v, m0 + lane, n0 + half * 128, column);
-        } else {
-          if (ok) grad_tile(a, v, patch, m0, n0 + half * 128, min(32, a.m - m0), unit);
-        }
+        if (ok) stats_tile(a, v, m0 + lane, n0 + half * 128, column);
       } else if constexpr (EPI == kFew) {
         float v[kFewRows / 2];                            // every other 16 of the rows
 #pragma unroll
         for (int j = 0; j < kFewRows / 2; ++j) v[j] = 0.f;
         split_range(a, split, s0, s1);
 #pragma unroll 1
-        for (int c = s0; c < s1; c += kChunk) {
+        for (int c = s0; c < s1; c += chunk_of(EPI)) {
           if (!wait()) break;
 #pragma unroll
           for (int g = 0; g < kFewRows / 32; ++g) {
@@ -605,13 +632,35 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
               few_tile(a, v + g * 16, reinterpret_cast<float*>(patch), m0, n0 + (g * 2 + half) * 16);
         }
       } else {
+        split_range(a, split, s0, s1);
+        const uint32_t at = trow + half * 128;
         if (!wait()) break;
+        if constexpr (EPI == kGradLong || EPI == kStoreLong) {
+          if (s1 - s0 > chunk_of(EPI)) {                  // added in registers, and put where the last chunk's sums were
+            float v[128];
+#pragma unroll
+            for (int j = 0; j < 128; ++j) v[j] = 0.f;
+#pragma unroll 1
+            for (int c = s0;;) {
+              add_sums(at + (acc & 1) * kTile, v);
+              c += chunk_of(EPI);
+              if (c >= s1) break;
+              release();
+              if (!wait()) break;
+            }
+            if (!ok) break;
+            put_sums(at + (acc & 1) * kTile, v);
+          }
+        }
         const int rows = min(32, a.m - m0);
-        const uint32_t taddr = trow + (acc & 1) * kTile + half * 128;
+        const uint32_t taddr = at + (acc & 1) * kTile;
         n0 += half * 128;
-        unit = a.unit ? *a.unit : 1.f;
-        if (a.out_fp32) store_tile<float>(a, taddr, patch, split, m0, n0, rows, unit);
-        else store_tile<__nv_bfloat16>(a, taddr, patch, split, m0, n0, rows, unit);
+        if constexpr (is_grad(EPI)) grad_tile(a, taddr, patch, m0, n0, rows, unit);
+        if constexpr (is_store(EPI)) {
+          unit = a.unit ? *a.unit : 1.f;
+          if (a.out_fp32) store_tile<float>(a, taddr, patch, split, m0, n0, rows, unit);
+          else store_tile<__nv_bfloat16>(a, taddr, patch, split, m0, n0, rows, unit);
+        }
         release();
       }
     }
@@ -796,7 +845,8 @@ int launch_head(const Operand& p, const Operand& q, const HeadArgs& a, int64_t k
   const int code = set_product<EPI>(l, 0, p, q, a, k);
   return code == PRM_OK ? launch_products<EPI, P_MN, Q_MN>(l, stream) : code;
 }
-// How long a tile takes, in stages: its main loop, or its epilogue where that is longer (5 stages).
+// Stages of a tile at most; and how long it takes, in stages: its main loop, or its epilogue where that is longer (5 stages).
+inline int tile_stages(const HeadArgs& a) { return ((a.kblocks + kSub - 1) / kSub + a.split - 1) / a.split; }
 inline int tile_cost(const HeadArgs& a) { return std::max(5, (a.kblocks + kSub - 1) / kSub / std::max(1, a.split)); }
 int launch_few(const Operand& x, const Operand& w, const HeadArgs& a, int64_t d, cudaStream_t stream) {
   return w.mn ? launch_head<kFew, true, false>(w, x, a, d, stream) : launch_head<kFew, false, false>(w, x, a, d, stream);
@@ -968,7 +1018,8 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
     a.clean = grad_weight && v0 == 0 ? clean : nullptr;
     a.ld_clean = ld_clean;
     a.d = (int)d;
-    code = launch_logits<kGrad>({x, n, d, ld_x, false}, w, a, d, stream);
+    const Operand xp = {x, n, d, ld_x, false};
+    code = d <= kLogitChunk * kHeadStage ? launch_logits<kGrad>(xp, w, a, d, stream) : launch_logits<kGradLong>(xp, w, a, d, stream);
     HeadLaunch l = {};                     // the two products that read G: one launch
     int products = 0;
     if (code == PRM_OK && grad_x) {
@@ -1006,7 +1057,9 @@ extern "C" int prm_head_loss_backward(const float* grad_loss, const void* x, int
     }
     if (code == PRM_OK) {
       if (products == 2) l.extra = tile_cost(l.a[0]) / tile_cost(l.a[1]);
-      code = launch_products<kStore, false, false>(l, stream);
+      code = std::max(tile_stages(l.a[0]), products == 2 ? tile_stages(l.a[1]) : 0) > kStoreLongest
+                 ? launch_products<kStoreLong, false, false>(l, stream)
+                 : launch_products<kStore, false, false>(l, stream);
     }
   }
   if (code == PRM_OK && grad_x && parted) {

@@ -108,3 +108,50 @@ def test_gradient_of_x_alone_keeps_to_its_scratch(n, d, vocab):
                                     gx.data_ptr(), d, None, d, scratch.data_ptr(), nbytes, torch.cuda.current_stream().cuda_stream)
     assert code == B.PRM_OK and torch.equal(gx, want) and torch.all(scratch[nbytes:] == 77)
     assert torch.equal(B.prm_head_loss_backward(gl, x, W.t(), labels, lse, need_weight=False)[0], want)
+
+
+def rounded(got, want, longest, chunks, what):
+    """Sums of one sign: in fp32 each is off by what is cut off at each step of 16 of the longest sum that is kept in one place,
+    and by a rounding for each of those sums, relative to itself.  Rounding to bf16 keeps the order of numbers, so that the result
+    lies between the roundings of the ends of that range.  (How results' roundings average says nothing: want lies on
+    a grid like bf16's own here, less n / vocab, so that all of them may go the same way.)"""
+    off = (longest / 16 + 4) * 2.0 ** -23 + (chunks + 4) * R.F32
+    low, high = (want * (1 - off)).to(torch.bfloat16), (want * (1 + off)).to(torch.bfloat16)
+    assert torch.all((got >= low) & (got <= high)), (what, float(((got.double() - want) / want).abs().max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("n", [9000, 1 << 17, 1 << 20])
+def test_weight_s_gradient_of_many_rows(n, transposed):
+    """All logits 0, so that G is 1/256 and 1/256 - 1, exactly: grad_W's sums are over as many terms as there are rows."""
+    d, vocab = 64, 256
+    x = ((1 + 0.1 * randn(1, n, d)) * (1 + torch.arange(d, device="cuda") / d)).to(torch.bfloat16)
+    W = torch.zeros(vocab, d, dtype=torch.bfloat16, device="cuda").t() if transposed else torch.zeros(d, vocab, dtype=torch.bfloat16, device="cuda")
+    labels = torch.randint(0, 4, (n,), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    _, lse = B.prm_head_loss(x, W, labels)
+    _, gw = B.prm_head_loss_backward(torch.ones(n, device="cuda"), x, W, labels, lse, need_x=False)
+    want = x.double().sum(0) / 256
+    longest = n if n <= 32768 else 8192
+    rounded(gw[:, 4:], want[:, None].expand(d, vocab - 4), longest, n // longest, "columns without a label")
+    hot = torch.stack([x[labels == v].double().sum(0) for v in range(4)], 1)
+    close(gw[:, :4], want[:, None] - hot, ((longest / 16 + 4) * 2.0 ** -23 + (n // longest + 4) * R.F32) * (want[:, None] + hot) +
+          1.01 * R.BF16 * (want[:, None] - hot).abs(), "columns with labels")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("n,vocab", [(64, 1 << 15), (64, 1 << 21), (600, 1 << 18)])
+def test_rows_gradient_of_a_long_vocabulary(n, vocab, transposed):
+    """Rows of zeros, so that G is 1 / vocab, exactly, but for the label: its column is 0."""
+    d = 64
+    W = ((1 + 0.1 * randn(1, vocab, d)) * (1 + torch.arange(d, device="cuda") / d)).to(torch.bfloat16)
+    W[:n] = 0
+    want = (W.double().sum(0) / vocab)[None].expand(n, d)
+    W = W.t() if transposed else W.t().contiguous()
+    x = torch.zeros(n, d, dtype=torch.bfloat16, device="cuda")
+    labels = torch.arange(n, device="cuda")
+    _, lse = B.prm_head_loss(x, W, labels)
+    gx, _ = B.prm_head_loss_backward(torch.ones(n, device="cuda"), x, W, labels, lse, need_weight=False)
+    longest = vocab if vocab <= 32768 else 8192
+    rounded(gx, want, longest, vocab // longest, "grad_x")
