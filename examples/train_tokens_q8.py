@@ -13,7 +13,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import torch
 
-from paper_2608_20818_b200.binding import PeriodicRowwiseMuon, prm_adamw_step
+from paper_2608_20818_b200.binding import PRM_OK, PeriodicRowwiseMuon, prm_adamw_step, prm_q8_status
 from paper_2608_20818_b200.layers import Draws, head_loss, layer_norm
 from paper_2608_20818_b200.q8 import Weight8, linear
 
@@ -82,6 +82,8 @@ def train(steps=60, vocab=1000, dim=256, blocks=2, tokens=2048, format="int8", p
         if log and (t % 10 == 0 or t + 1 == steps):
             log(f"step {t:3d}  loss {losses[-1]:.4f}")
     optimizer.close()
+    if prm_q8_status() != PRM_OK:
+        raise RuntimeError("a wait inside a product ran out: the steps since then have wrong gradients")
     return losses
 
 

@@ -13,6 +13,9 @@ No mask and no logits are kept: a mask is drawn again by the backward pass, the 
 captured into a graph, advance() with it; each replay then draws anew.  (As with any function of torch: no eager graph of
 the same leaves may be alive while a backward pass is captured.)  The gradients have no derivatives of their own: a
 backward pass with create_graph=True is refused.
+
+The head's products wait for copies with a limit.  A wait that has run out is not seen by the call: binding.prm_q8_status(), which
+waits for the device, says so; ask it now and then, at the latest before weights are written out.
 """
 
 from __future__ import annotations
@@ -196,7 +199,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, residual=None, p=0.0, draws=
     """Layer norm over the last dimension of h = dropout(x, p) + residual: (y, h).  h is x itself without either.
 
     weight and bias: cols, or groups x cols, a row for each part of the rows of x (..., cols) cut into `groups` equal ones
-    (scale and shift of each sample of a batch); add_one takes 1 + weight."""
+    (scale and shift of each sample of a batch); both in one shape and type, a bias without a weight: cols.  add_one takes 1 + weight."""
     if residual is not None and residual.shape != x.shape:
         raise ValueError("x and residual must have the same shape")
     out = _LayerNorm.apply(x, residual, weight, bias, eps, add_one, p, *_number(p, draws))
