@@ -162,14 +162,14 @@ __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks<IO>(NV, BLOCK)) l
     }
     float total[2] = {sg2.x + sg2.y, sx2.x + sx2.y};
     row_sums<TPR, BLOCK>(total, red[turn][line]);
-    const float2 mg2 = make_float2(-total[0] * over, -total[0] * over), mx2 = make_float2(-total[1] * over, -total[1] * over);
+    const float2 mg2 = make_float2(-total[0] * over, -total[0] * over), mx2 = make_float2(-total[1] * over * rs2.x, -total[1] * over * rs2.x);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = c0 + v * TPR * 8;
       if (c < cols) {
-        float2 g[4], xhat[4], o[4];
+        float2 g[4], h[4], o[4];
         now[v][0].get(g);
-        now[v][1].get(xhat);
+        now[v][1].get(h);
         if (a.gh) {
           now[v][2].get(o);
         } else {
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks<IO>(NV, BLOCK)) l
           for (int e = 0; e < 4; ++e) o[e] = make_float2(0.f, 0.f);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fma2(fma2(mul2(add2(xhat[e], off2), rs2), mx2, fma2(g[e], w[v][e], mg2)), rs2, o[e]);
+        for (int e = 0; e < 4; ++e) o[e] = fma2(fma2(add2(h[e], off2), mx2, fma2(g[e], w[v][e], mg2)), rs2, o[e]);
         IO* gr = reinterpret_cast<IO*>(a.gr) + row * a.ld_gr;
         if constexpr (SHIFT) {
           store_part(gr, c, cols, o);
