@@ -1,7 +1,7 @@
 // out = x dropped out (+ residual); applied to a gradient with the same numbers it is its own gradient.
 //
 // Bound by HBM (2 or 3 elements' bytes each) and by the generator's integer products and exclusive ors, which do not
-// overlap well with one another: 8192 x 8192 in bf16 65 us, with residual 72 us (5.6 TB/s).  A block takes 256 / TPR rows (TPR threads to a row) by 4 TPR
+// overlap well with one another: 8192 x 8192 in bf16 61 us, with residual 67 us (6.0 TB/s); in fp32 89 and 118 us (6.0, 6.8).  A block takes 256 / TPR rows (TPR threads to a row) by 4 TPR
 // octs; a thread's four octs are under way together.
 #include "dropout.cuh"
 
@@ -21,7 +21,7 @@ struct DropoutArgs {
 constexpr int kOcts = 4;                   // per thread
 
 // SHIFT: octs aligned in memory of rows that start anywhere (alike in all matrices); an oct may then need the words of
-// three quads (8192 x 8191: 117 us).
+// three quads (8192 x 8191: 111 us).
 template <typename IO, int TPR, bool SHIFT>
 __global__ void __launch_bounds__(256) dropout_kernel(const DropoutArgs a) {
   grid_wait();

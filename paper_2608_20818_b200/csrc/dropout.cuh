@@ -8,7 +8,7 @@
 // Philox4x32-10 is the generator of Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as
 // 1, 2, 3" (SC 2011): ten rounds of two 32 x 32 -> 64 bit products, whose halves change places, under a key
 // that advances by a constant (the rounds' keys come with the kernel's arguments: computed by every thread they
-// take 8192 x 8192 bf16 elements from 65 to 74 us).  Four elements share one evaluation: 18 to 20 products of four
+// cost 8192 x 8192 bf16 elements 9 us more).  Four elements share one evaluation: 18 to 20 products of four
 // cycles of an SM's quarter and 20 exclusive ors of two, alone 0.66 cycles of an SM, 39 us for 8192 x 8192 elements (memory
 // alone: 41 us); a product as one half from double precision and one from 32-bit integers takes 0.9.
 #pragma once

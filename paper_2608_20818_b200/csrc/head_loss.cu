@@ -18,8 +18,8 @@
 //   warp 1      tcgen05.mma issuer (one lane of the leader); owns its CTA's tensor memory
 //   warps 2..9  epilogue: two warps per lane quadrant, half of the 256 columns each; a thread has a row
 // Two accumulators of 256 columns let the epilogue of a tile run under the next tile's main loop.
-// Measured: 8192 x 4096 x 131072 6.3 ms, 1400 TFLOP/s, its gradient with 65536 columns 10.0 ms, 1325 TFLOP/s (cuBLAS sustains
-// 1374 under the same power cap); 2048 x 1024 x 32768 101 us and 318 us; one token 4096 x 32768 57 us, 4.7 TB/s.
+// Measured, one after another: 8192 x 4096 x 131072 6.4 ms, 1370 TFLOP/s, its gradient with 65536 columns 10.4 ms, 1265 TFLOP/s
+// (cuBLAS sustains 1374 under the same power cap); 2048 x 1024 x 32768 103 us and 319 us; one token 4096 x 32768 52 us, 5.1 TB/s.
 // Every barrier wait is bounded; one that runs out sets the status word, the pair drains and leaves.
 #include "q8_matmul.cuh"
 #include "train_plan.h"
@@ -39,10 +39,10 @@ constexpr uint32_t kStageBytes = 2 * kSub * kBoxBytes;
 constexpr uint32_t kPatchBytes = 32 * 64;        // a warp's 32 rows of 64 bytes on their way out
 constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kPatchBytes;
 constexpr int kMaxStages = 6;
-constexpr int kFewRows = 64;                     // rows that kFew takes (100 x 4096 x 32768: 72 us, the other form 68)
+constexpr int kFewRows = 64;                     // rows that kFew takes (100 x 4096 x 32768: 4 us more than the other form)
 // Long sums are taken out of tensor memory every so often and added in registers: the accumulator cuts off what falls below its
 // last bit at each of its steps (16 k).  The logits' every 1024 k, in both directions, so that the gradient's are those that
-// lse was made of: over 4096 k a logit of the size 1 would be off by 1e-5 (gradient of 100 x 4096 x 32768: 237 us, 228 without).  Those of the
+// lse was made of: over 4096 k a logit of the size 1 would be off by 1e-5 (3 % of the gradient of 100 x 4096 x 32768).  Those of the
 // products of G, which are rounded to bf16 in the end, every 8192 k where there are more than 32768 (up to there what is cut
 // off is 2e-4 of a sum of one sign, a twentieth of its rounding; over 2^20 rows grad_W would be 6e-3 short).
 constexpr int kLogitChunk = 8, kStoreChunk = 64; // stages
@@ -51,8 +51,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // kStats: x (rows) times W (columns).  kFew: the same for few rows, the other way round (the rows are the instruction's N, so
 // that it costs them no more than it has to, and W's bytes have most of shared memory).
-// kGradLong, kStoreLong: tiles of several chunks (in one kernel with the others their registers cost 8192 x 64 x 32768 551 us
-// instead of 472).
+// kGradLong, kStoreLong: tiles of several chunks (in one kernel with the others their registers cost 8192 x 64 x 32768 550 us
+// instead of 470).
 enum Epi { kStats, kFew, kGrad, kGradLong, kStore, kStoreLong };
 __host__ __device__ constexpr bool is_grad(int epi) { return epi == kGrad || epi == kGradLong; }
 __host__ __device__ constexpr bool is_store(int epi) { return epi == kStore || epi == kStoreLong; }

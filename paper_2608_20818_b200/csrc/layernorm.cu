@@ -10,8 +10,8 @@
 // what the first one's rounding has left in it (with a mean of 10^5 deviations, some 10^-2 of one) is taken off
 // again from mean, variance and output.
 //
-// Measured: 8192 x 4096 in bf16 with residual 51 us, 5.2 TB/s (fp32 89 us, 6.0), with dropout 60 us; 16384 x 1024
-// 27 us; 131072 x 128 28 us; one token of 2048 2 us.  (Times here and below are the device's, of calls that follow one another
+// Measured: 8192 x 4096 in bf16 with residual 46 us, 5.8 TB/s (fp32 84 us, 6.4), with dropout 55 us; 16384 x 1024
+// 27 us; 131072 x 128 24 us; 4096 x 16384 110 us, 4.9 TB/s (x 20480, by single elements, 283); one token of 2048 2 us.  (Times here and below are the device's, of calls that follow one another
 // on inputs beyond the L2.)
 #include "layernorm_forward.cuh"
 

@@ -76,8 +76,8 @@ __device__ __forceinline__ RowStats row_stats(float2 (&t)[NV][4], const bool (&i
   return RowStats(sum[0], make_float2(both[0], both[1]), over, eps);
 }
 
-// Blocks per SM of the kernel for many rows: 64 registers per thread, 80 and more for wide rows (8192 x 4096 with dropout: 64.6 us,
-// with 64 registers 69.9; 131072 x 128 without: 30.8 and 28.4).
+// Blocks per SM of the kernel for many rows: 64 registers per thread, 80 and more for wide rows (8192 x 4096 with dropout: 5 us
+// more with 64 registers; 131072 x 128 without: 2 us less).
 constexpr int layernorm_blocks(int tpr, int block) { return tpr >= 256 ? 768 / block : 1024 / block; }
 
 // Few rows: one for each group of TPR threads, BLOCK / TPR rows per block, 8 * NV elements per thread.  SHIFT: octs
@@ -214,9 +214,9 @@ __host__ __device__ inline int staged_words(int cols, bool shift) {
 
 // Many rows: a block's rows are a range, BLOCK / TPR of them at a time, the next rows' loads under way while these are summed.
 // The rows of a group share weight and bias from shared memory, as fp32: fetched by each row for itself they cost as many
-// bytes from L2 as the row, and their conversion (16384 x 2048 with a weight for each of 64 groups, no residual: 31.6
-// us, 4.3 TB/s; a row per block 42).  Asking the L2 for the rows after the next gains nothing here.  ROUND: one group, whose rows go
-// round the blocks, so that rows under way at a time are neighbours (8192 x 4096 with dropout: 60 us, in ranges 64; 8192 x 8192 98, 102).
+// bytes from L2 as the row, and their conversion (16384 x 2048 with a weight for each of 64 groups, no residual: 29
+// us, 4.7 TB/s; a row per block some 10 more).  Asking the L2 for the rows after the next gains nothing here.  ROUND: one group, whose rows go
+// round the blocks, so that rows under way at a time are neighbours (8192 x 4096 with dropout: 55 us, 8192 x 8192 94; in ranges 4 more each).
 template <typename IO, int NV, int TPR, int BLOCK, bool DROP, bool SHIFT, bool ROUND>
 __global__ void __launch_bounds__(BLOCK, layernorm_blocks(TPR, BLOCK)) layernorm_many_kernel(const LayerNormArgs a) {
   constexpr int kLines = BLOCK / TPR;
@@ -459,7 +459,7 @@ int launch_layernorm(LayerNormArgs a, cudaStream_t stream) {
                               dim3((unsigned)((rows + kRows - 1) / kRows), by_group ? (unsigned)(a.rows / rows) : 1u),
                               BLOCK, 0, stream, 0, a));
 }
-// (bf16 only: 32-bit elements leave room for fewer rows under way; 8192 x 4096 with residual 104 us, with a block per row 89.)
+// (bf16 only: 32-bit elements leave room for fewer rows under way; 8192 x 4096 with residual 84 us with a block per row, so 15 more.)
 template <typename IO, bool DROP, bool SHIFT, int NV, int TPR, bool ROUND>
 int launch_layernorm_many_as(const LayerNormArgs& a, cudaStream_t stream) {
   constexpr int BLOCK = TPR < 256 ? 256 : TPR;
@@ -481,7 +481,7 @@ int launch_layernorm_many_as(const LayerNormArgs& a, cudaStream_t stream) {
 }
 template <typename IO, bool DROP, bool SHIFT, int NV, int TPR>
 int launch_layernorm_many(const LayerNormArgs& a, cudaStream_t stream) {
-  // 64 registers per thread leave no room for the step beside the generator (16384 x 2048 with dropout: 78 us instead of 65)
+  // 64 registers per thread leave no room for the step beside the generator (16384 x 2048 with dropout: 60 us, with it 13 more)
   if constexpr (!DROP || TPR >= 256) {
     if (a.rows_per_group >= a.rows) return launch_layernorm_many_as<IO, DROP, SHIFT, NV, TPR, true>(a, stream);
   }
@@ -506,7 +506,7 @@ int run_layernorm(const LayerNormArgs& a, cudaStream_t stream) {
   PRM_TRY(2, 64)
   PRM_TRY(2, 128)
   PRM_TRY(2, 256)
-  // half of the threads idle with the next size (8192 x 4097: 91 us instead of 110)
+  // half of the threads idle with the next size (8192 x 4097: 85 us, with it 19 more)
   if (c <= 8 * 3 * 256) return launch_layernorm<IO, DROP, SHIFT, 3, 256>(a, stream);
   PRM_TRY(2, 512)
 #undef PRM_TRY

@@ -7,9 +7,9 @@
 // Bound by HBM (8 bytes per element of a bf16 stream with grad_h, 10 with dropout).  Blocks walk the rows of
 // one group; a thread keeps the same columns in all its rows, so that its share of grad_w and grad_b stays in
 // registers, and the next row's loads are under way while this one is summed.  With several blocks to a group
-// their lines of sums are added by a second launch, in a fixed order.  Measured: 8192 x 4096 in bf16 with grad_h 54 us, 5.0
-// TB/s (fp32 89 us, 6.0), with dropout 83 us; 16384 x 2048 with a weight for each of 64 groups 54 us; 131072 x 128 32 us;
-// 8192 x 4097 106 us.
+// their lines of sums are added by a second launch, in a fixed order.  Measured: 8192 x 4096 in bf16 with grad_h 51 us, 5.2
+// TB/s (fp32 85 us, 6.3), with dropout 78 us; 16384 x 2048 with a weight for each of 64 groups 50 us; 131072 x 128 29 us;
+// 8192 x 4097 100 us; by single elements 4096 x 12288 364 us.
 #include "layernorm.cuh"
 
 namespace prm {
@@ -37,8 +37,8 @@ __device__ __forceinline__ void store_weight(void* out, int fp32, int64_t at, fl
   else reinterpret_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(v);
 }
 
-// Blocks per SM of the kernel below: 128 registers per thread with two octs or 32-bit elements (16384 x 2048 in fp32: 88 us,
-// with 85 registers 123), else 85.
+// Blocks per SM of the kernel below: 128 registers per thread with two octs or 32-bit elements (16384 x 2048 in fp32: 84 us,
+// with 85 registers 35 more), else 85.
 template <typename IO>
 constexpr int layernorm_grad_blocks(int nv, int block) {
   return (nv == 1 && sizeof(IO) == 2 ? 768 : 512) / block;
@@ -63,8 +63,8 @@ __global__ void __launch_bounds__(BLOCK, layernorm_grad_blocks<IO>(NV, BLOCK)) l
   float2 w[NV][4], gw[NV][4], gb[NV][4];
   Oct<IO> next[NV][3];
   float next_mean = 0.f, next_rstd = 0.f;
-  // Asks the L2 for a row's lines, one lane for 128 bytes.  (8192 x 4096: 54 us with it and the loop unrolled twice, so that no
-  // registers are copied; 62 without.  Rows that start anywhere spill and take 126 us instead of 106.)
+  // Asks the L2 for a row's lines, one lane for 128 bytes.  (8192 x 4096: 8 us less with it and the loop unrolled twice, so
+  // that no registers are copied.  Rows that start anywhere spill and take 20 us more.)
   auto ask = [&](int64_t local) {
     if (local < rows && threadIdx.x % (16 / sizeof(IO)) == 0) {
       const int64_t row = row0 + local;
@@ -380,7 +380,7 @@ template <typename IO, bool DROP, bool SHIFT>
 int run_layernorm_grad(const LayerNormGradArgs& a, int64_t groups, cudaStream_t stream) {
   const int64_t c = (int64_t)a.cols + (SHIFT ? 7 : 0);
   // Two octs per thread halve what a row's reduction costs each; of 32-bit elements they leave the registers, but a block of
-  // 1024 threads has too few for one (4096 x 8192 in fp32: 164 us, so 223).
+  // 1024 threads has too few for one (4096 x 8192 in fp32: 158 us, so 60 more).
   constexpr int NV = sizeof(IO) == 2 ? 2 : 1, T = NV == 2 ? 1 : 2;
   if (c <= 64) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 8, 256>(a, groups, stream);
   if (c <= 128) return launch_layernorm_grad<IO, DROP, SHIFT, 1, 16, 256>(a, groups, stream);

@@ -59,7 +59,7 @@ constexpr int kHeadStage = 128;                  // k that a stage of a tile's m
 inline int64_t ceil_to(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
 
 // The head's gradient: pieces of the vocabulary whose G fits 512 MB, of alike width but for the last, which may have a few columns
-// only (pieces that stay in the L2, 64 MB, leave each product too few tiles: 8192 x 64 x 32768 takes 729 us with them, 468 with
+// only (pieces that stay in the L2, 64 MB, leave each product too few tiles: 8192 x 64 x 32768 takes 729 us with them, 470 with
 // one piece), and grad_x's sums: parts of one product's k where there are few tiles, the pieces' running sums where there are
 // several.
 struct HeadGradPlan {
