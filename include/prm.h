@@ -570,7 +570,8 @@ PRM_API int prm_q8_status(void);
  *   32768 terms cut off, not rounded, every 16 of them; of more, of parts of 8192).  A row
  *   without a label, or whose grad_loss is 0, has no part in grad_weight and the grad_x 0, whatever it holds.
  *   scratch: device, 256-byte aligned, prm_head_loss_backward_scratch_bytes(n, d, vocab) bytes (G for a piece of the
- *   vocabulary, up to 512 MB or 2048 columns, partial sums, the rows of x that have a part), prm_head_loss_copy_bytes(n, d) less without grad_weight, and more for copies as above.  With n = 0 grad_weight is set to zero.
+ *   vocabulary, up to 512 MB or 2048 columns, partial sums, the rows of x that have a part),
+ *   prm_head_loss_copy_bytes(n, d) less without grad_weight, and more for copies as above.  With n = 0 grad_weight is set to zero.
  * prm_q8_status covers the waits inside the head's products too.
  */
 PRM_API int prm_dropout(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int64_t rows,

@@ -774,8 +774,9 @@ def prm_layernorm(x, weight=None, bias=None, eps=1e-6, residual=None, add_one=Fa
     """Layer norm of h = x (dropped out with probability p, see prm_dropout) + residual: (y, h, mean, rstd).
 
     x, residual: rows x cols, bf16 or fp32.  weight, bias: cols, or groups x cols (each row of them for rows /
-    groups neighbouring rows), bf16 or fp32, both in one shape and type, a bias without a weight: cols; add_one takes 1 + weight.  h, in x's type, is what the norm is taken of and
-    what the stream carries on; it is None where it is x itself.  mean and rstd (fp32) go to the gradient."""
+    groups neighbouring rows), bf16 or fp32, both in one shape and type, a bias without a weight: cols; add_one takes 1 + weight.
+    h, in x's type, is what the norm is taken of and what the stream carries on; it is None where it is x itself.  mean and
+    rstd (fp32) go to the gradient."""
     if stream is not None:
         return _on_stream(stream, (x, weight, bias, residual, counter),
                           lambda: prm_layernorm(x, weight, bias, eps, residual, add_one, p, seed, offset, counter))

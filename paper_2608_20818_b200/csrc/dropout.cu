@@ -1,7 +1,8 @@
 // out = x dropped out (+ residual); applied to a gradient with the same numbers it is its own gradient.
 //
 // Bound by HBM (2 or 3 elements' bytes each) and by the generator's integer products and exclusive ors, which do not
-// overlap well with one another: 8192 x 8192 in bf16 61 us, with residual 67 us (6.0 TB/s); in fp32 89 and 118 us (6.0, 6.8).  A block takes 256 / TPR rows (TPR threads to a row) by 4 TPR
+// overlap well with one another: 8192 x 8192 in bf16 61 us, with residual 67 us (6.0 TB/s); in fp32 89 and 118 us (6.0, 6.8).
+// A block takes 256 / TPR rows (TPR threads to a row) by 4 TPR
 // octs; a thread's four octs are under way together.
 #include "dropout.cuh"
 

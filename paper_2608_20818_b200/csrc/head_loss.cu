@@ -42,9 +42,9 @@ constexpr int kMaxStages = 6;
 constexpr int kFewRows = 64;                     // rows that kFew takes (100 x 4096 x 32768: 4 us more than the other form)
 // Long sums are taken out of tensor memory every so often and added in registers: the accumulator cuts off what falls below its
 // last bit at each of its steps (16 k).  The logits' every 1024 k, in both directions, so that the gradient's are those that
-// lse was made of: over 4096 k a logit of the size 1 would be off by 1e-5 (3 % of the gradient of 100 x 4096 x 32768).  Those of the
-// products of G, which are rounded to bf16 in the end, every 8192 k where there are more than 32768 (up to there what is cut
-// off is 2e-4 of a sum of one sign, a twentieth of its rounding; over 2^20 rows grad_W would be 6e-3 short).
+// lse was made of: over 4096 k a logit of the size 1 would be off by 1e-5 (it costs the gradient of 100 x 4096 x 32768 3 %).
+// Those of the products of G, which are rounded to bf16 in the end, every 8192 k where there are more than 32768 (up to there
+// what is cut off is 2e-4 of a sum of one sign, a twentieth of its rounding; over 2^20 rows grad_W would be 6e-3 short).
 constexpr int kLogitChunk = 8, kStoreChunk = 64; // stages
 constexpr int kStoreLongest = 256;
 constexpr float kLog2e = 1.4426950408889634f;
